@@ -1,0 +1,448 @@
+"""The measured cases of the operators that a predictor layer is fine-tuned and served with: attention with capped scores,
+distance bias, document and prefix masks; rotary positions; dropout whose mask is drawn again instead of stored.
+
+Plain forms are elementary torch operations in 32 bits on padded sequences; ``exact`` has the definitions in 64 bits, a
+sequence at a time.  Lengths, documents and prefixes are fixed by the case, contents by the seed."""
+from __future__ import annotations
+
+import functools
+import math
+
+import numpy as np
+import torch
+
+own = False
+DEV = "cuda:0"
+TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+ATTENTION = {"do": "attention", "type": "bf16", "seqs": 1, "shortest": 1, "longest": 512, "queries": 0, "heads": 12, "kv_heads": 12,
+             "size": 64, "causal": False, "prefix": False, "docs": 0, "cap": 0.0, "bias": False, "train": True}
+ROTARY = {"do": "rotary", "type": "bf16", "tokens": 1, "heads": 12, "kv_heads": 12, "size": 64, "rotated": 64, "interleaved": False,
+          "top": 512, "factor": 1.0, "train": True}
+DROPOUT = {"do": "dropout", "type": "bf16", "rows": 1, "cols": 768, "p": 0.1, "bias": True, "residual": True}
+
+
+def listed():
+    return [
+        # a micro-batch's last layer: one row a request over its own tokens, heads as in the six-layer predictor
+        {**ATTENTION, "name": "first_rows_of_8", "seqs": 8, "shortest": 20, "longest": 512, "queries": 1, "train": False},
+        # one new token a request over its cache, shared heads of 128, capped scores; the caches as long as they get
+        {**ATTENTION, "name": "one_token_long_caches", "seqs": 32, "shortest": 500, "longest": 32768, "queries": 1, "heads": 32,
+         "kv_heads": 8, "size": 128, "causal": True, "cap": 50.0, "train": False},
+        # one request alone over one long cache, where only the keys can be shared out
+        {**ATTENTION, "name": "one_token_one_cache", "shortest": 65521, "longest": 65521, "queries": 1, "heads": 16, "kv_heads": 4,
+         "size": 128, "causal": True, "bias": True, "train": False},
+        # fine-tuning the base predictor: a batch of 64 prompts with a distance bias in place of learned positions
+        {**ATTENTION, "name": "train_base_64", "seqs": 64, "shortest": 4, "longest": 512, "bias": True},
+        # the tiny fp32 predictor's batch, the smallest training step
+        {**ATTENTION, "name": "train_fp32_tiny", "type": "fp32", "seqs": 16, "shortest": 8, "longest": 64, "heads": 2, "kv_heads": 2,
+         "docs": 24},
+        # fp32 with heads of a size that is no power of two, capped and biased
+        {**ATTENTION, "name": "train_fp32_heads_of_80", "type": "fp32", "seqs": 8, "shortest": 100, "longest": 1023, "heads": 8,
+         "kv_heads": 4, "size": 80, "causal": True, "cap": 30.0, "bias": True},
+        # long prompts whose head is seen by all of it, shared heads of 128
+        {**ATTENTION, "name": "train_prefix_2048", "seqs": 16, "shortest": 1500, "longest": 2048, "heads": 16, "kv_heads": 4, "size": 128,
+         "causal": True, "prefix": True, "cap": 30.0},
+        # documents packed into two rows of 8192 tokens with padding at the end, the production predictor's heads
+        {**ATTENTION, "name": "train_documents_8192", "seqs": 2, "shortest": 8192, "longest": 8192, "heads": 16, "kv_heads": 16,
+         "docs": 2048, "causal": True},
+        # a step of 64 requests deep in a long context: interleaved, half of each head
+        {**ROTARY, "name": "rotary_64_tokens", "tokens": 64, "heads": 32, "kv_heads": 8, "size": 128, "rotated": 64,
+         "interleaved": True, "top": 131072, "factor": 4.0, "train": False},
+        # queries and keys of a training batch, and their gradients
+        {**ROTARY, "name": "rotary_train_32768", "tokens": 32768, "heads": 16, "kv_heads": 16, "top": 8192},
+        # the rows of a micro-batch, behind the output projection
+        {**DROPOUT, "name": "dropout_tiny_fp32", "type": "fp32", "rows": 577, "cols": 128},
+        # the rows of a training batch of the production predictor
+        {**DROPOUT, "name": "dropout_65536", "rows": 65536, "cols": 1024},
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["train", "train", "train", "token", "token", "rotary", "dropout"])
+    what = rng.choice(["bf16", "bf16", "fp32"])
+    if kind in ("train", "token"):
+        kv = rng.choice([1, 2, 3, 4, 8, 12])
+        size = rng.choice([32, 40, 64, 64, 80, 96, 128])
+        c = {**ATTENTION, "type": what, "kv_heads": kv, "heads": kv * rng.choice([1, 1, 2, 4]), "size": size,
+             "cap": rng.choice([0.0, 0.0, 30.0, 50.0]), "bias": rng.random() < 0.4, "causal": rng.random() < 0.6}
+        if kind == "token":
+            longest = _log(rng, 16, 65521)
+            seqs = max(1, min(_log(rng, 1, 256), 2 ** 29 // (longest * kv * size)))
+            return {**c, "queries": rng.choice([1, 1, 1, 2, 5]), "train": False, "seqs": seqs, "longest": longest,
+                    "shortest": max(5, longest // rng.choice([1, 3, 16]))}
+        longest = min(_log(rng, 16, 8192), math.isqrt(2 ** 28 // c["heads"]))
+        seqs = max(1, min(_log(rng, 1, 64), 2 ** 28 // (longest * longest * c["heads"])))
+        c = {**c, "seqs": seqs, "longest": longest, "shortest": max(2, longest // rng.choice([1, 2, 8])), "prefix": rng.random() < 0.3,
+             "docs": rng.choice([0, 0, max(2, longest // 6)])}
+        return {**c, "causal": c["causal"] or c["prefix"]}
+    if kind == "rotary":
+        size = rng.choice([32, 64, 64, 80, 128])
+        return {**ROTARY, "type": what, "tokens": _log(rng, 1, 16384), "heads": rng.choice([2, 12, 16]), "kv_heads": rng.choice([2, 4, 16]),
+                "size": size, "rotated": rng.choice([size, size, size // 2]), "interleaved": rng.random() < 0.5,
+                "top": _log(rng, 64, 131072), "factor": rng.choice([1.0, 4.0]), "train": rng.random() < 0.6}
+    return {**DROPOUT, "type": what, "rows": _log(rng, 1, 32768), "cols": rng.choice([64, 128, 767, 768, 1000, 1024]),
+            "p": rng.choice([0.0, 0.1, 0.1, 0.5]), "bias": rng.random() < 0.7, "residual": rng.random() < 0.7}
+
+
+# ---- what a case fixes -----------------------------------------------------------------------------------------------------
+@functools.lru_cache(maxsize=64)
+def _shape(items):
+    """Lengths of keys and queries, document of every token (-1: padding), prefixes, the count of visible pairs."""
+    c = dict(items)
+    n, lo, hi = c["seqs"], c["shortest"], c["longest"]
+    klen = [hi if n == 1 else int(round(lo * (hi / lo) ** (((7 * i + 3) % n) / (n - 1)))) if math.gcd(7, n) == 1 else
+            int(round(lo * (hi / lo) ** (i / (n - 1)))) for i in range(n)]
+    qlen = [min(c["queries"], k) if c["queries"] else k for k in klen]
+    prefix = [int(k * ((37 * i + 21) % 60) / 100) for i, k in enumerate(klen)]
+    docs, pairs = [], 0
+    for s, k in enumerate(klen):
+        d = np.zeros(k, np.int64)
+        if c["docs"]:
+            d[:] = -1
+            at, i, end = 0, 0, k - k // 32
+            while at < end:
+                size = max(1, int(c["docs"] * 16 ** (((5 * i + 3 * s) % 8) / 7 - 1)))
+                d[at:min(at + size, end)] = i
+                at, i = at + size, i + 1
+        docs.append(d)
+        a = np.arange(k - qlen[s], k)
+        if not c["docs"]:
+            pairs += int(np.maximum(a + 1, prefix[s] if c["prefix"] else 0).sum()) if c["causal"] else k * len(a)
+            continue
+        for x in range(int(d.max()) + 1):
+            own_ = np.flatnonzero(d == x)
+            first, m, rows = own_[0], own_.size, own_[own_ >= a[0]]
+            ahead = min(max(prefix[s] - first, 0), m) if c["prefix"] else 0
+            pairs += int(np.maximum(rows - first + 1, ahead).sum()) if c["causal"] else m * rows.size
+    return klen, qlen, docs, prefix, pairs
+
+
+def _shape_of(case):
+    return _shape(tuple(sorted((k, v) for k, v in case.items() if k != "name")))
+
+
+def work(case):
+    w = 2 if case["type"] == "bf16" else 4
+    if case["do"] == "attention":
+        klen, qlen, _, _, pairs = _shape_of(case)
+        q, kv = sum(qlen) * case["heads"] * case["size"], sum(klen) * case["kv_heads"] * case["size"]
+        forward, backward = (2 * q + 2 * kv) * w, (4 * q + 4 * kv) * w
+        flops = pairs * case["heads"] * case["size"]
+        return {"bytes": forward + backward if case["train"] else forward, "flops": flops * 14 if case["train"] else flops * 4}
+    if case["do"] == "rotary":
+        n = case["tokens"] * (case["heads"] + case["kv_heads"])
+        passes = 2 if case["train"] else 1
+        return {"bytes": passes * 2 * n * case["size"] * w, "flops": passes * 3 * n * case["rotated"]}
+    n = case["rows"] * case["cols"]
+    return {"bytes": n * w * (4 + case["residual"]), "flops": n * 6}
+
+
+# ---- inputs ----------------------------------------------------------------------------------------------------------------
+def _i32(v):
+    return torch.tensor(np.asarray(v, np.int64), dtype=torch.int32, device=DEV)
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    t = TYPES[case["type"]]
+
+    def normal(*shape, by=1.0):
+        return torch.randn(shape, generator=g, device=DEV, dtype=t) * by
+
+    s = {"case": case}
+    if case["do"] == "attention":
+        klen, qlen, docs, prefix, _ = _shape_of(case)
+        nq, nk, h, hk, d = sum(qlen), sum(klen), case["heads"], case["kv_heads"], case["size"]
+        # capped scores are worth capping: some of them large
+        s.update(q=normal(nq, h, d, by=4.0 if case["cap"] else 1.0), k=normal(nk, hk, d), v=normal(nk, hk, d),
+                 q_offsets=_i32(np.cumsum([0] + qlen)), k_offsets=_i32(np.cumsum([0] + klen)), out=torch.empty(nq, h, d, dtype=t, device=DEV),
+                 lse=torch.empty(h, nq, device=DEV), max_q=max(qlen), max_k=max(klen), klen=klen, qlen=qlen)
+        s["slopes"] = torch.tensor([2.0 ** (-8.0 * (i + 1) / h) for i in range(h)], device=DEV) if case["bias"] else None
+        s["prefix"] = _i32(prefix) if case["prefix"] else None
+        s["k_docs"] = _i32(np.concatenate(docs)) if case["docs"] else None
+        s["q_docs"] = _i32(np.concatenate([x[len(x) - m:] for x, m in zip(docs, qlen)])) if case["docs"] else None
+        if case["train"]:
+            s.update(dout=normal(nq, h, d), **{"d" + n: torch.empty_like(s[n]) for n in "qkv"})
+        if own:
+            from paper_2504_03702_amd import binding as ps
+            s["workspace"] = ps.alloc_workspace(ps.ps_attention_workspace_bytes(
+                len(klen), nq, nk, s["max_q"], s["max_k"], h, hk, d, t, case["train"]), DEV)
+    elif case["do"] == "rotary":
+        n, half = case["tokens"], case["rotated"] // 2
+        for name, heads in (("q", case["heads"]), ("k", case["kv_heads"])):
+            s[name] = normal(n, heads, case["size"])
+            s[name + "_out"] = torch.empty_like(s[name])
+            if case["train"]:
+                s["d" + name] = normal(n, heads, case["size"])
+                s["d" + name + "_out"] = torch.empty_like(s[name])
+        s["positions"] = torch.randint(0, case["top"], (n,), generator=g, device=DEV, dtype=torch.int32)
+        # positions interpolated by `factor`; the magnitude that goes with it
+        s["frequencies"] = torch.tensor([10000.0 ** (-i / half) / case["factor"] for i in range(half)], dtype=torch.float32, device=DEV)
+        s["magnitude"] = 0.1 * math.log(case["factor"]) + 1.0
+    else:
+        n, m = case["rows"], case["cols"]
+        s.update(x=normal(n, m), bias=normal(m) if case["bias"] else None, residual=normal(n, m) if case["residual"] else None,
+                 dout=normal(n, m), out=torch.empty(n, m, dtype=t, device=DEV), dx=torch.empty(n, m, dtype=t, device=DEV),
+                 dbias=torch.empty(m, device=DEV) if case["bias"] else None,
+                 rng=torch.tensor([seed * 0x9E3779B97F4A7C15 % 2 ** 63, seed % 1000], dtype=torch.int64, device=DEV))
+        if own:
+            from paper_2504_03702_amd import binding as ps
+            s["workspace"] = ps.alloc_workspace(ps.ps_dropout_workspace_bytes(n, m), DEV)
+    return s
+
+
+# ---- one pass --------------------------------------------------------------------------------------------------------------
+def run(state):
+    return {"attention": _attention, "rotary": _rotary, "dropout": _dropout}[state["case"]["do"]](state)
+
+
+def _attention(s):
+    c = s["case"]
+    if own:
+        from paper_2504_03702_amd import binding as ps
+        how = dict(softcap=c["cap"], causal=c["causal"], prefix=s["prefix"], slopes=s["slopes"], q_docs=s["q_docs"], k_docs=s["k_docs"])
+        ps.ps_attention_forward(s["q"], s["k"], s["v"], s["q_offsets"], s["k_offsets"], s["max_q"], s["max_k"], s["out"], s["lse"],
+                                s["workspace"], **how)
+        if not c["train"]:
+            return {"out": s["out"], "lse": s["lse"]}
+        ps.ps_attention_backward(s["q"], s["k"], s["v"], s["out"], s["lse"], s["dout"], s["q_offsets"], s["k_offsets"], s["max_q"],
+                                 s["max_k"], s["dq"], s["dk"], s["dv"], s["workspace"], **how)
+        return {n: s[n] for n in ("out", "lse", "dq", "dk", "dv")}
+    n, heads, groups, size = len(s["klen"]), c["heads"], c["heads"] // c["kv_heads"], c["size"]
+    # rows [sequence, place] of the packed tensors, and which of them there are
+    qo, ko = s["q_offsets"].long(), s["k_offsets"].long()
+    at_q, at_k = torch.arange(s["max_q"], device=DEV), torch.arange(s["max_k"], device=DEV)
+    qn, kn = (qo[1:] - qo[:-1])[:, None], (ko[1:] - ko[:-1])[:, None]
+    rows, cols = qo[:-1, None] + torch.minimum(at_q, qn - 1), ko[:-1, None] + torch.minimum(at_k, kn - 1)
+    live = at_q < qn
+    place = (kn - qn + at_q)[:, :, None]                                        # a query's position among the keys
+    seen = live[:, :, None] & (at_k < kn)[:, None, :]
+    if c["causal"]:
+        ahead = at_k > place
+        seen &= ~ahead if s["prefix"] is None else ~ahead | (at_k < s["prefix"].long()[:, None, None])
+    if c["docs"]:
+        dq, dk = s["q_docs"][rows][:, :, None], s["k_docs"][cols][:, None, :]
+        seen &= (dq == dk) & (dq >= 0)
+
+    def padded(x, at):                                                          # [sequence, key head, rows of the group's heads, size]
+        x = x[at.reshape(-1)].float().reshape(n, at.shape[1], c["kv_heads"], -1, size)
+        return x.permute(0, 2, 3, 1, 4).reshape(n, c["kv_heads"], -1, size)
+
+    def scores(x):                                                              # [sequence, head, query, key]
+        return x.reshape(n, heads, s["max_q"], s["max_k"])
+
+    def grouped(x):
+        return x.reshape(n, c["kv_heads"], groups * s["max_q"], s["max_k"])
+
+    def packed(x, at):                                                          # back to [token, head, size]
+        x = x.reshape(n, x.shape[1] * x.shape[2] // at.shape[1], at.shape[1], size)
+        return x.transpose(1, 2)
+
+    scale = 1.0 / math.sqrt(size)
+    q, k, v = padded(s["q"], rows), padded(s["k"], cols), padded(s["v"], cols)
+    z = scores(q @ k.transpose(2, 3)) * scale
+    slope = 1.0
+    if c["cap"]:
+        bent = torch.tanh(z / c["cap"])
+        z, slope = bent * c["cap"], (1 - bent * bent if c["train"] else None)
+        del bent
+    if c["bias"]:
+        z = z - s["slopes"][:, None, None] * (place - at_k).abs()[:, None].float()
+    z = z.masked_fill(~seen[:, None], -math.inf)
+    top = z.amax(-1, keepdim=True)
+    top = torch.where(top == -math.inf, torch.zeros_like(top), top)
+    p = torch.exp(z - top)
+    del z
+    total = p.sum(-1, keepdim=True)
+    p = p / torch.where(total == 0, torch.ones_like(total), total)
+    o = grouped(p) @ v
+    t = s["q"].dtype
+    got = {"out": packed(o, rows)[live].to(t), "lse": (top + total.log())[..., 0].transpose(0, 1)[:, live]}
+    if not c["train"]:
+        return got
+    do = padded(s["dout"], rows)
+    got["dv"] = packed(grouped(p).transpose(2, 3) @ do, cols)[at_k < kn].to(t)
+    d = scores(do @ v.transpose(2, 3)) - (do * o).sum(-1).reshape(n, heads, s["max_q"], 1)
+    d = grouped(p * d * slope * scale)
+    del p
+    got["dq"] = packed(d @ k, rows)[live].to(t)
+    got["dk"] = packed(d.transpose(2, 3) @ q, cols)[at_k < kn].to(t)
+    return got
+
+
+def _turned(x, cos, sin, c):
+    half, x = c["rotated"] // 2, x.float()
+    r = x[..., :c["rotated"]]
+    a, b = (r[..., 0::2], r[..., 1::2]) if c["interleaved"] else (r[..., :half], r[..., half:])
+    a, b = a * cos - b * sin, a * sin + b * cos
+    r = torch.stack((a, b), -1).flatten(-2) if c["interleaved"] else torch.cat((a, b), -1)
+    return torch.cat((r, x[..., c["rotated"]:]), -1)
+
+
+def _rotary(s):
+    c = s["case"]
+    if own:
+        from paper_2504_03702_amd import binding as ps
+        ps.ps_rotary(s["q"], s["positions"], s["frequencies"], s["q_out"], s["k"], s["k_out"], c["interleaved"], s["magnitude"])
+        if not c["train"]:
+            return {"q": s["q_out"], "k": s["k_out"]}
+        ps.ps_rotary(s["dq"], s["positions"], s["frequencies"], s["dq_out"], s["dk"], s["dk_out"], c["interleaved"], s["magnitude"],
+                     inverse=True)
+        return {"q": s["q_out"], "k": s["k_out"], "dq": s["dq_out"], "dk": s["dk_out"]}
+    # position x frequency less whole turns, all in 32 bits: the product's rounding error from halves of 12 bits, the turns in
+    # three pieces whose products with up to 2^15 turns are exact
+    p, f = s["positions"].float()[:, None], s["frequencies"]
+    high = f * 4097.0
+    high = high - (high - f)
+    p_high = (p / 4096.0).floor() * 4096.0
+    angle = p * f
+    error = ((p_high * high - angle) + p_high * (f - high) + (p - p_high) * high) + (p - p_high) * (f - high)
+    turns = (angle / (2 * math.pi)).round()
+    one = 6.28125
+    two = round((2 * math.pi - one) * 2 ** 17) / 2 ** 17
+    angle = ((angle - turns * one) - turns * two) - turns * (2 * math.pi - one - two) + error
+    cos, sin = (angle.cos() * s["magnitude"])[:, None], (angle.sin() * s["magnitude"])[:, None]
+    got = {n: _turned(s[n], cos, sin, c).to(s[n].dtype) for n in ("q", "k")}
+    if c["train"]:
+        got.update({n: _turned(s[n], cos, -sin, c).to(s[n].dtype) for n in ("dq", "dk")})
+    return got
+
+
+def _draws(rng, rows, cols):
+    """[rows, cols] numbers of 16 bits: Philox4x32-10 (Salmon et al. 2011), eight neighbours of a row to a counter."""
+    low = 0xFFFFFFFF
+    row = torch.arange(rows, device=DEV)[:, None]
+    group = torch.arange((cols + 7) // 8, device=DEV)[None]
+    key, key2 = rng[0] & low, (rng[0] >> 32) & low
+    x0, x1 = (group + 0 * row), (row + 0 * group)
+    x2, x3 = (rng[1] & low).expand_as(x0), ((rng[1] >> 32) & low).expand_as(x0)
+    for _ in range(10):
+        a, b = x0 * 0xD2511F53, x2 * 0xCD9E8D57
+        x0, x1, x2, x3 = ((b >> 32) & low) ^ x1 ^ key, b & low, ((a >> 32) & low) ^ x3 ^ key2, a & low
+        key, key2 = (key + 0x9E3779B9) & low, (key2 + 0xBB67AE85) & low
+    words = torch.stack((x0, x1, x2, x3), -1)
+    return torch.stack((words & 0xFFFF, words >> 16), -1).reshape(rows, -1)[:, :cols]
+
+
+def _dropout(s):
+    c = s["case"]
+    if own:
+        from paper_2504_03702_amd import binding as ps
+        ps.ps_dropout_forward(s["x"], s["bias"], s["residual"], s["rng"], c["p"], s["out"])
+        ps.ps_dropout_backward(s["dout"], s["rng"], c["p"], s["dx"], s["dbias"], s["workspace"])
+        return {n: s[n] for n in ("out", "dx", "dbias") if s[n] is not None}
+    out_of = round(c["p"] * 65536)
+    keep = (_draws(s["rng"], c["rows"], c["cols"]) >= out_of).float() * (65536 / (65536 - out_of))
+    y = s["x"].float()
+    if s["bias"] is not None:
+        y = y + s["bias"].float()
+    y = y * keep
+    if s["residual"] is not None:
+        y = y + s["residual"].float()
+    dx = s["dout"].float() * keep
+    got = {"out": y.to(s["x"].dtype), "dx": dx.to(s["x"].dtype)}
+    if s["bias"] is not None:
+        got["dbias"] = dx.sum(0)
+    return got
+
+
+# ---- the definitions in 64 bits --------------------------------------------------------------------------------------------
+def exact(case, seed):
+    global own
+    was, own = own, False
+    s = prepare(case, seed)
+    own = was
+    return {"attention": _exact_attention, "rotary": _exact_rotary, "dropout": _exact_dropout}[case["do"]](case, s)
+
+
+def _exact_attention(c, s):
+    klen, qlen, docs, prefix, _ = _shape_of(c)
+    group, scale = c["heads"] // c["kv_heads"], c["size"] ** -0.5
+    out = torch.zeros(s["q"].shape, dtype=torch.float64, device=DEV)
+    lse = torch.full(s["lse"].shape, -math.inf, dtype=torch.float64, device=DEV)
+    grads = {n: torch.zeros(s[n].shape, dtype=torch.float64, device=DEV) for n in "qkv"} if c["train"] else None
+    q0 = k0 = 0
+    for i, (m, n) in enumerate(zip(qlen, klen)):
+        query, key = torch.arange(n - m, n, device=DEV)[:, None], torch.arange(n, device=DEV)[None]
+        visible = torch.ones(m, n, dtype=torch.bool, device=DEV)
+        if c["causal"]:
+            visible = query >= key
+            if c["prefix"]:
+                visible = visible | (key < prefix[i])
+        if c["docs"]:
+            d = torch.as_tensor(docs[i], device=DEV)
+            visible = visible & (d[n - m:, None] == d[None]) & (d[n - m:, None] >= 0)
+        some = visible.any(1)
+        for h in range(c["heads"]):
+            # Head by head; each product has operands laid out plainly.
+            q, k, v = s["q"][q0:q0 + m, h].double(), s["k"][k0:k0 + n, h // group].double(), s["v"][k0:k0 + n, h // group].double()
+            x = (q @ k.t().contiguous()) * scale
+            y = c["cap"] * (x / c["cap"]).tanh() if c["cap"] else x
+            if c["bias"]:
+                y = y - s["slopes"][h].double() * (query - key).abs()
+            y = torch.where(visible, y, torch.full_like(y, -math.inf))
+            l = torch.logsumexp(y, 1)
+            p = torch.where(some[:, None], (y - torch.where(some, l, torch.zeros_like(l))[:, None]).exp(), torch.zeros_like(y))
+            o = p @ v
+            out[q0:q0 + m, h], lse[h, q0:q0 + m] = o, l
+            if grads is None:
+                continue
+            do = s["dout"][q0:q0 + m, h].double()
+            dp = do @ v.t().contiguous()
+            ds = p * (dp - (p * dp).sum(1, keepdim=True))
+            if c["cap"]:
+                ds = ds / (x / c["cap"]).cosh() ** 2
+            grads["q"][q0:q0 + m, h] = scale * (ds @ k)
+            grads["k"][k0:k0 + n, h // group] += scale * (ds.t().contiguous() @ q)
+            grads["v"][k0:k0 + n, h // group] += p.t().contiguous() @ do
+        q0, k0 = q0 + m, k0 + n
+    got = {"out": out, "lse": lse}
+    if grads is not None:
+        got.update({"d" + n: g for n, g in grads.items()})
+    return got
+
+
+def _exact_rotary(c, s):
+    half = c["rotated"] // 2
+    angle = s["positions"].double()[:, None] * s["frequencies"].double()[None]
+    got = {}
+    for name, sign in (("q", 1.0), ("k", 1.0), ("dq", -1.0), ("dk", -1.0)):
+        if name not in s:
+            continue
+        x = s[name].double()
+        w = torch.polar(torch.full_like(angle, s["magnitude"]), sign * angle)[:, None]
+        first = torch.arange(half, device=DEV) * (2 if c["interleaved"] else 1)
+        second = first + (1 if c["interleaved"] else half)
+        y = torch.complex(x[..., first], x[..., second]) * w
+        x[..., first], x[..., second] = y.real, y.imag
+        got[name] = x
+    return got
+
+
+def _exact_dropout(c, s):
+    u = np.uint64
+    seed, offset = (int(v) for v in s["rng"].tolist())
+    n, m = c["rows"], c["cols"]
+    col, row = np.meshgrid(np.arange((m + 7) // 8, dtype=u), np.arange(n, dtype=u))
+    at = [col, row, np.full_like(col, offset & 0xFFFFFFFF), np.full_like(col, offset >> 32)]
+    for i in range(10):
+        left, right = at[0] * u(0xD2511F53), at[2] * u(0xCD9E8D57)
+        k0, k1 = u((seed + i * 0x9E3779B9) & 0xFFFFFFFF), u(((seed >> 32) + i * 0xBB67AE85) & 0xFFFFFFFF)
+        at = [(right >> u(32)) ^ at[1] ^ k0, right & u(0xFFFFFFFF), (left >> u(32)) ^ at[3] ^ k1, left & u(0xFFFFFFFF)]
+    bits = np.stack(at, -1).astype(np.uint32).view(np.uint16).reshape(n, -1)[:, :m]
+    lost = round(c["p"] * 65536)
+    kept = torch.from_numpy(bits >= lost).to(DEV)
+    by = 65536 / (65536 - lost)
+    inner = s["x"].double() if s["bias"] is None else s["x"].double() + s["bias"].double()[None]
+    y = torch.where(kept, inner * by, torch.zeros_like(inner))
+    dx = torch.where(kept, s["dout"].double() * by, torch.zeros_like(inner))
+    got = {"out": y if s["residual"] is None else y + s["residual"].double(), "dx": dx}
+    if s["bias"] is not None:
+        got["dbias"] = dx.sum(0)
+    return got
