@@ -168,7 +168,7 @@ def prepare(case, seed):
         s["k_docs"] = _i32(np.concatenate(docs)) if case["docs"] else None
         s["q_docs"] = _i32(np.concatenate([x[len(x) - m:] for x, m in zip(docs, qlen)])) if case["docs"] else None
         if case["train"]:
-            s.update(dout=normal(nq, h, d), **{"d" + n: torch.empty_like(s[n]) for n in "qkv"})
+            s.update(dout=normal(nq, h, d), out_rest=torch.empty(nq, h, d, dtype=t, device=DEV) if case["type"] == "bf16" else None, **{"d" + n: torch.empty_like(s[n]) for n in "qkv"})
         if own:
             from paper_2504_03702_amd import binding as ps
             s["workspace"] = ps.alloc_workspace(ps.ps_attention_workspace_bytes(
@@ -206,7 +206,8 @@ def _attention(s):
     c = s["case"]
     if own:
         from paper_2504_03702_amd import binding as ps
-        how = dict(softcap=c["cap"], causal=c["causal"], prefix=s["prefix"], slopes=s["slopes"], q_docs=s["q_docs"], k_docs=s["k_docs"])
+        # a training step in bf16 keeps what the rounding of `out` left, for its backward pass
+        how = dict(out_rest=s.get("out_rest"), softcap=c["cap"], causal=c["causal"], prefix=s["prefix"], slopes=s["slopes"], q_docs=s["q_docs"], k_docs=s["k_docs"])
         ps.ps_attention_forward(s["q"], s["k"], s["v"], s["q_offsets"], s["k_offsets"], s["max_q"], s["max_k"], s["out"], s["lse"],
                                 s["workspace"], **how)
         if not c["train"]:
