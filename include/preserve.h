@@ -273,6 +273,133 @@ int ps_route(const int32_t* prompt_tokens, const int32_t* pred_tokens, int32_t n
 int ps_forecast(const float* weights, int32_t hidden, const float* hist_p, const float* hist_d,
                 int32_t n_services, int32_t k, const float* mu, float* out, void* hip_stream);
 
+/* ---- Operators of a predictor layer that is fine-tuned, or that takes long prompts (Sec. 3.3) -------------------------------
+ * The predictor of ps_predict_load() has learned positions and attention over all of a request's tokens, and is run forwards
+ * only.  The calls below are what a layer needs beyond that: attention with other masks and score functions, with its gradients
+ * and for single tokens over long keys; rotary positions; dropout.  They take caller-owned device tensors, the caller's stream
+ * and workspace, allocate nothing, and can be captured into a HIP graph.  dtype as in ps_model_info: 0 = fp32, 1 = bf16. */
+
+/* Elements from one row (token) to the next, and from one head of a row to the next; the head's own elements are neighbours.
+ * Strides are multiples of 16 bytes, as is the address of element 0; neither may be negative. */
+typedef struct ps_strides { int64_t row, head; } ps_strides;
+
+/* Attention of n_seq sequences packed one after the other.  Row i of sequence s's queries stands at position a = q_start[s] + i of
+ * its keys j = 0 .. k_len - 1, and for head h with its group's key head
+ *     x = scale * (q_i . k_j),  y = softcap * tanh(x / softcap) (x if softcap is 0),  score = y - slopes[h] * |a - j|
+ * over the keys that row i sees:  (not causal, or j <= a, or j < prefix[s])  and  (no documents, or q_docs[i] == k_docs[j] >= 0).
+ * out = sum of softmax(score) v, lse = ln sum exp(score).  A row that sees nothing gets zeros and an lse of -infinity.
+ *   heads       multiple of kv_heads; head h reads key head h / (heads / kv_heads)
+ *   head_dim    a multiple of 8, at most 128
+ *   max_q, max_k  host's bounds on the sequences' rows and keys: a longer sequence is faulty (below)
+ *   scale > 0;  softcap >= 0;  causal 0 or 1
+ *   q .. dv     strides of the tensors a call uses: [n_q][heads] of q, out, dout, dq, [n_k][kv_heads] of k, v, dk, dv */
+typedef struct ps_attention_desc {
+    int32_t dtype, n_seq, heads, kv_heads, head_dim, max_q, max_k, causal;
+    int64_t n_q, n_k;                   /* rows of the query and key tensors (offsets end at or before them) */
+    float scale, softcap;
+    ps_strides q, k, v, out, dout, dq, dk, dv;
+} ps_attention_desc;
+
+/* What the sequences are, on the device.
+ *   q_offsets, k_offsets  [n_seq + 1] int32, non-decreasing: sequence s owns the rows from offsets[s] to offsets[s + 1]
+ *   k_lengths  [n_seq] int32 or NULL: only that many of a sequence's key rows hold keys (a cache with room at its end, whose
+ *              contents are not read)
+ *   q_start    [n_seq] int32 or NULL: position of the first query row; NULL: keys - rows, so that the last row stands at the
+ *              last key (a new token over its cache; itself, in attention of a sequence to itself)
+ *   prefix     [n_seq] int32 or NULL: keys below it are seen by every row, whatever `causal`
+ *   q_docs, k_docs  [n_q], [n_k] int32, both or neither: documents, in any order; a negative one is padding, which sees nothing
+ *              and is not seen
+ *   slopes     [heads] float or NULL */
+typedef struct ps_attention_seqs {
+    const int32_t *q_offsets, *k_offsets, *k_lengths, *q_start, *prefix, *q_docs, *k_docs;
+    const float* slopes;
+} ps_attention_seqs;
+
+/* Bytes of device workspace that ps_attention_forward() (backward = 0), or it and ps_attention_backward() (1) need for calls of
+ * this shape (of `desc`, the strides are not used).  0 on arguments that the calls refuse. */
+size_t ps_attention_workspace_bytes(const ps_attention_desc* desc, int backward);
+
+/* out and lse ([heads][n_q] float; NULL: not wanted) of the rows of all sequences; other rows are left alone.  Statistics and sums are fp32;
+ * bf16 calls round the softmax's weights to bf16 for the product with v.
+ * out_rest: NULL, or in a bf16 call a dense [n_q][heads][head_dim] bf16 tensor for what the rounding of out to bf16 left (NULL in fp32
+ * calls, which leave nothing).  The backward call takes it for dout . out, see there.
+ * A key row's contents matter to nobody if it lies behind its sequence's keys or is padding.  Among the others, rows of v that a
+ * query does not see take part in its sums with weight 0 and have to be finite; masked scores may be anything.
+ * status: a sequence whose offsets or lengths break the rules, or pass n_q, n_k, max_q or max_k, is left out (its rows keep what
+ * they held) and raises PS_ST_BAD_LENGTH with its index.
+ * Errors: PS_EINVAL (null or misaligned pointers, bad sizes, strides or numbers), PS_EWORKSPACE, PS_EUNSUPPORTED (head_dim above 128 or
+ * no multiple of 8; max_q * (heads / kv_heads)^2 of 2^31 or more), PS_EHIP.  n_seq, n_q or n_k of 0 are allowed. */
+int ps_attention_forward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const void* q, const void* k, const void* v,
+                         void* out, float* lse, void* out_rest, void* workspace, size_t workspace_bytes, ps_status* status,
+                         void* hip_stream);
+
+/* Gradients of ps_attention_forward() with respect to q, k and v, given dout, that of `out`, and out, lse and out_rest as the
+ * forward call left them.  With D_i = dout_i . out_i and p_ij the weights:
+ *     dv_j = sum_i p_ij dout_i,  g_ij = p_ij (dout_i . v_j - D_i) (1 - tanh^2(x_ij / softcap)),
+ *     dq_i = scale sum_j g_ij k_j,  dk_j = scale sum_i g_ij q_i,  a key head's over the rows of all its heads.
+ * out_rest may be NULL.  In a bf16 call D_i is then off by what the rounding of out left, which shows where a row's weight lies on few keys:
+ * the terms of its dq cancel to little or, with one key, to zero, and the rounding stays (a tenth of the typical dq there, a thousandth with it).
+ * dq, dk and dv of the rows of all sequences are overwritten (key rows behind k_lengths are left alone).  Slopes have no gradient.
+ * Sums are taken in an order that is fixed by the shapes: the same call gives the same bits.  bf16 calls round p and g to bf16 for the products.
+ * Errors and faulty sequences as above. */
+int ps_attention_backward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const void* q, const void* k, const void* v,
+                          const void* out, const float* lse, const void* out_rest, const void* dout, void* dq, void* dk, void* dv, void* workspace,
+                          size_t workspace_bytes, ps_status* status, void* hip_stream);
+
+/* Rotary positions: of every row t and head, the pairs i < n_pairs of x turn by the angle positions[t] * frequencies[i]
+ *     (a, b) -> magnitude * (a cos - b sin, a sin + b cos)
+ * where pair i is (x[2 i], x[2 i + 1]) if interleaved, else (x[i], x[i + n_pairs]); the head's other elements are copied.
+ * inverse = 1 turns the other way: with the same magnitude, the gradient of x from that of `out`.
+ *   x, out      [n_rows][heads][head_dim]; out may be x (in place, same strides) but may not overlap it otherwise
+ *   x2, out2    NULL, or a second pair of tensors (the keys) with heads2 heads, turned by the same angles
+ *   positions   [n_rows] int32, any value;  frequencies [n_pairs] float, radians a position
+ * The angle is reduced with the product's rounding error taken into account: large positions lose nothing.
+ * Strides: multiples of one element here; rows whose strides and addresses are multiples of 16 bytes are moved faster.
+ * Errors: PS_EINVAL (null pointers, negative sizes or strides, 2 n_pairs > head_dim), PS_EUNSUPPORTED (head_dim above 4096, 2^27
+ * elements or more in a row's heads, n_rows above 2^31 - 1), PS_EHIP. */
+typedef struct ps_rotary_desc {
+    int32_t dtype, head_dim, n_pairs, interleaved, inverse, heads, heads2;
+    float magnitude;
+    int64_t n_rows;
+    ps_strides x, out, x2, out2;
+} ps_rotary_desc;
+int ps_rotary(const ps_rotary_desc* desc, const void* x, void* out, const void* x2, void* out2, const int32_t* positions,
+              const float* frequencies, void* hip_stream);
+
+/* Frequencies of n_pairs pairs for ps_rotary() (host array): base^(-i / n_pairs), changed for contexts longer than the trained one
+ * as `scaling` says:
+ *   PS_ROTARY_PLAIN   not at all
+ *   PS_ROTARY_LINEAR  divided by `factor` (positions interpolated)
+ *   PS_ROTARY_BASE    base * factor^(n_pairs / (n_pairs - 1)): the slowest pair is slowed down by `factor`, the fastest not
+ *   PS_ROTARY_PARTS   pairs that turn less than `slow` times over `trained_len` positions are divided by factor, those that turn
+ *                     more than `fast` times are left alone, those between are mixed linearly in the number of turns
+ * Errors: PS_EINVAL. */
+#define PS_ROTARY_PLAIN  0
+#define PS_ROTARY_LINEAR 1
+#define PS_ROTARY_BASE   2
+#define PS_ROTARY_PARTS  3
+int ps_rotary_frequencies(int32_t n_pairs, double base, int scaling, double factor, int32_t trained_len, double slow, double fast,
+                          float* frequencies /*host*/);
+
+/* Dropout whose mask is drawn where it is needed and never stored, with the bias in front of it and the residual behind it:
+ *     out[r][c] = residual[r][c] + keep(r, c) * (x[r][c] + bias[c]) * 65536 / (65536 - T),   T = rint(65536 p)
+ * keep(r, c) is 1 if u(r, c) >= T, else 0 (the value is then left out, whatever it is), where u are the 16-bit pieces, low halves first, of the four words of
+ * Philox4x32-10 (Salmon et al. 2011) with counter (c / 8, r, rng[1] low, rng[1] high) and key (rng[0] low, rng[0] high); column c takes
+ * piece c % 8.  T = 65536 drops everything.  rng stays on the device, so that a captured graph can move on to other masks.
+ *   x, residual, out  [rows][cols], rows ld elements apart each; bias [cols]; all of `dtype`; bias and residual may be NULL
+ *   out may be x or residual (same ld); the mask does not depend on strides
+ *   rng         [2] int64: seed, and a number that the caller moves on from call to call
+ * Errors: PS_EINVAL (null pointers, negative sizes, ld < cols, p outside [0, 1]), PS_EUNSUPPORTED (rows above 2^31 - 1, cols above 2^20), PS_EHIP. */
+int ps_dropout_forward(const void* x, int64_t ld_x, const void* bias, const void* residual, int64_t ld_residual, const int64_t* rng, float p,
+                       int32_t dtype, int64_t rows, int32_t cols, void* out, int64_t ld_out, void* hip_stream);
+
+/* Its gradients: dx[r][c] = keep(r, c) * dout[r][c] * 65536 / (65536 - T) (dx may be dout), and dbias[c], the sum of its column
+ * before dx is rounded ([cols] float, NULL: not wanted; the order of the sum is fixed by the shape).  The residual's is dout itself.
+ * workspace: ps_dropout_workspace_bytes(rows, cols) bytes, 256-byte aligned; needed for dbias only. */
+size_t ps_dropout_workspace_bytes(int64_t rows, int32_t cols);
+int ps_dropout_backward(const void* dout, int64_t ld_dout, const int64_t* rng, float p, int32_t dtype, int64_t rows, int32_t cols, void* dx,
+                        int64_t ld_dx, float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Kernel-family timing for benchmarks.  While enabled, ps_predict_load() brackets every kernel
  * launch with HIP events on the call's stream (the paper reports only the predictor's end-to-end
  * latency, Sec. 4.5; this splits it by kernel).  ps_profile_read() waits for `hip_stream`, adds

@@ -26,7 +26,9 @@ PS_ST_BAD_TOKEN, PS_ST_BAD_LENGTH, PS_ST_NAN, PS_ST_BAD_RECORD, PS_ST_RANGE = 0x
 EXPORTS = ["ps_model_load", "ps_model_free", "ps_model_get_info", "ps_workspace_bytes", "ps_predict_load",
            "ps_anticipate_workspace_bytes", "ps_anticipate", "ps_anticipate_static", "ps_status_read", "ps_strerror",
            "ps_profile_enable", "ps_profile_read", "ps_profile_clock", "ps_profile_stream_read",
-           "ps_lookahead_workspace_bytes", "ps_lookahead_update", "ps_scaler_scan", "ps_route", "ps_forecast"]
+           "ps_lookahead_workspace_bytes", "ps_lookahead_update", "ps_scaler_scan", "ps_route", "ps_forecast",
+           "ps_attention_workspace_bytes", "ps_attention_forward", "ps_attention_backward", "ps_rotary", "ps_rotary_frequencies",
+           "ps_dropout_workspace_bytes", "ps_dropout_forward", "ps_dropout_backward"]
 PS_FAMILIES = ["embed", "gemm", "attention", "layernorm", "head", "refine"]
 
 
@@ -39,6 +41,25 @@ class PsError(RuntimeError):
 class ps_model_info(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("layers", "hidden", "heads", "ffn", "vocab", "max_pos",
                                               "n_soft", "head_hidden", "dtype", "d_max")]
+
+
+class ps_strides(ctypes.Structure):
+    _fields_ = [("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class ps_attention_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_seq", "heads", "kv_heads", "head_dim", "max_q", "max_k", "causal")] + \
+        [("n_q", ctypes.c_int64), ("n_k", ctypes.c_int64), ("scale", ctypes.c_float), ("softcap", ctypes.c_float)] + \
+        [(n, ps_strides) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+
+
+class ps_attention_seqs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q_offsets", "k_offsets", "k_lengths", "q_start", "prefix", "q_docs", "k_docs", "slopes")]
+
+
+class ps_rotary_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "head_dim", "n_pairs", "interleaved", "inverse", "heads", "heads2")] + \
+        [("magnitude", ctypes.c_float), ("n_rows", ctypes.c_int64)] + [(n, ps_strides) for n in ("x", "out", "x2", "out2")]
 
 
 class ps_status(ctypes.Structure):
@@ -94,12 +115,31 @@ def load_library() -> ctypes.CDLL:
     lib.ps_profile_clock.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_double)]
     lib.ps_profile_stream_read.restype = ctypes.c_int
     lib.ps_profile_stream_read.argtypes = [vp, ctypes.c_int64, vp, vp]
+    desc, seqs = ctypes.POINTER(ps_attention_desc), ctypes.POINTER(ps_attention_seqs)
+    lib.ps_attention_workspace_bytes.restype = sz
+    lib.ps_attention_workspace_bytes.argtypes = [desc, ctypes.c_int]
+    lib.ps_attention_forward.restype = ctypes.c_int
+    lib.ps_attention_forward.argtypes = [desc, seqs, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    lib.ps_attention_backward.restype = ctypes.c_int
+    lib.ps_attention_backward.argtypes = [desc, seqs, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    lib.ps_rotary.restype = ctypes.c_int
+    lib.ps_rotary.argtypes = [ctypes.POINTER(ps_rotary_desc), vp, vp, vp, vp, vp, vp, vp]
+    dbl = ctypes.c_double
+    lib.ps_rotary_frequencies.restype = ctypes.c_int
+    lib.ps_rotary_frequencies.argtypes = [i32, dbl, ctypes.c_int, dbl, i32, dbl, dbl, ctypes.POINTER(ctypes.c_float)]
+    lib.ps_dropout_workspace_bytes.restype = sz
+    lib.ps_dropout_workspace_bytes.argtypes = [i64, i32]
+    lib.ps_dropout_forward.restype = ctypes.c_int
+    lib.ps_dropout_forward.argtypes = [vp, i64, vp, vp, i64, vp, ctypes.c_float, i32, i64, i32, vp, i64, vp]
+    lib.ps_dropout_backward.restype = ctypes.c_int
+    lib.ps_dropout_backward.argtypes = [vp, i64, vp, ctypes.c_float, i32, i64, i32, vp, i64, vp, vp, sz, vp]
     lib.ps_strerror.restype = ctypes.c_char_p
     lib.ps_strerror.argtypes = [ctypes.c_int]
     _native = _extension()
     if _native is not None:
         _native.bind(*[ctypes.cast(getattr(lib, "ps_" + name), vp).value for name in (
-            "predict_load", "anticipate", "anticipate_static", "lookahead_update", "scaler_scan", "route", "forecast")])
+            "predict_load", "anticipate", "anticipate_static", "lookahead_update", "scaler_scan", "route", "forecast",
+            "attention_forward", "attention_backward", "rotary", "dropout_forward", "dropout_backward")])
     _lib = lib
     return lib
 
@@ -353,6 +393,183 @@ def ps_forecast(weights: torch.Tensor, hidden: int, hist_p: torch.Tensor, hist_d
         _ptr(weights, torch.float32, "weights"), hidden, _ptr(hist_p, torch.float32, "hist_p"),
         _ptr(hist_d, torch.float32, "hist_d"), n_services, k, _ptr(mu, torch.float32, "mu"),
         _ptr(out, torch.float32, "out"), _stream()), "ps_forecast")
+
+
+# ---- operators of a layer that is fine-tuned, or takes long prompts -------------------------------------------------------
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _heads_ptr(t: torch.Tensor, shape: Tuple[int, int, int], dtype: torch.dtype, name: str) -> Tuple[int, ps_strides]:
+    """Address and strides of a tensor [rows, heads, head_dim] whose last dimension is dense."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
+        raise TypeError(f"{name}: need a {dtype} tensor on the GPU")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: has shape {tuple(t.shape)}, not {shape}")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}: a head's elements have to be neighbours")
+    # (torch keeps any stride for dimensions of one)
+    return t.data_ptr(), ps_strides(*[t.stride(i) if t.shape[i] > 1 else shape[2] for i in (0, 1)])
+
+
+def _dtype_code(dtype: torch.dtype, where: str) -> int:
+    if dtype not in _DTYPES:
+        raise TypeError(f"{where}: takes float32 and bfloat16, not {dtype}")
+    return _DTYPES[dtype]
+
+
+def _sized_ptr(t: Optional[torch.Tensor], dtype: torch.dtype, n: int, name: str) -> Optional[int]:
+    p = _ptr(t, dtype, name)
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name}: has {t.numel()} elements, not {n}")
+    return p
+
+
+def ps_attention_workspace_bytes(n_seq: int, n_q: int, n_k: int, max_q: int, max_k: int, heads: int, kv_heads: int, head_dim: int,
+                                 dtype: torch.dtype, backward: bool = False) -> int:
+    d = ps_attention_desc(_dtype_code(dtype, "ps_attention_workspace_bytes"), n_seq, heads, kv_heads, head_dim, max_q, max_k, 0, n_q,
+                          n_k, 1.0, 0.0)
+    return int(load_library().ps_attention_workspace_bytes(ctypes.byref(d), int(backward)))
+
+
+def _attention(where, q, k, q_offsets, k_offsets, max_q, max_k, scale, softcap, causal, k_lengths, q_start, prefix, slopes, q_docs,
+               k_docs, tensors):
+    """The call's descriptor, its sequences and the addresses of `tensors` ({name: (tensor, whether it has k's shape)})."""
+    if not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or q.dim() != 3 or k.dim() != 3:
+        raise TypeError(f"{where}: q and k are tensors of rows, heads and elements")
+    n_seq, (n_q, heads, size), (n_k, kv_heads, _) = q_offsets.numel() - 1, q.shape, k.shape
+    if n_seq < 0 or k_offsets.numel() != n_seq + 1 or (q_docs is None) != (k_docs is None):
+        raise ValueError(f"{where}: offsets of n_seq + 1 elements, and documents of both queries and keys or of neither")
+    d = ps_attention_desc(_dtype_code(q.dtype, where), n_seq, heads, kv_heads, size, max_q, max_k, int(causal), n_q, n_k,
+                          size ** -0.5 if scale is None else scale, softcap)
+    at = {}
+    for name, (t, keys) in tensors.items():
+        at[name], strides = _heads_ptr(t, (n_k, kv_heads, size) if keys else (n_q, heads, size), q.dtype, name)
+        setattr(d, name, strides)
+    i32 = torch.int32
+    seqs = ps_attention_seqs(_ptr(q_offsets, i32, "q_offsets"), _ptr(k_offsets, i32, "k_offsets"),
+                             _sized_ptr(k_lengths, i32, n_seq, "k_lengths"), _sized_ptr(q_start, i32, n_seq, "q_start"),
+                             _sized_ptr(prefix, i32, n_seq, "prefix"), _sized_ptr(q_docs, i32, n_q, "q_docs"),
+                             _sized_ptr(k_docs, i32, n_k, "k_docs"), _sized_ptr(slopes, torch.float32, heads, "slopes"))
+    return d, seqs, at, heads * n_q
+
+
+def ps_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_offsets: torch.Tensor,
+                         max_q: int, max_k: int, out: torch.Tensor, lse: Optional[torch.Tensor], workspace: torch.Tensor,
+                         scale: Optional[float] = None, softcap: float = 0.0, causal: bool = False,
+                         k_lengths: Optional[torch.Tensor] = None, q_start: Optional[torch.Tensor] = None,
+                         prefix: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None,
+                         q_docs: Optional[torch.Tensor] = None, k_docs: Optional[torch.Tensor] = None,
+                         status: Optional[torch.Tensor] = None, out_rest: Optional[torch.Tensor] = None) -> None:
+    """q, out [n_q, heads, head_dim]; k, v [n_k, kv_heads, head_dim]; lse [heads, n_q] float32; scale: head_dim ** -0.5 for None;
+    out_rest [n_q, heads, head_dim], in bfloat16 calls whose gradients are wanted, for ps_attention_backward()."""
+    if _made("attention_forward", q, k, v, q_offsets, k_offsets, max_q, max_k, out, lse, workspace, scale, softcap, causal, k_lengths,
+             q_start, prefix, slopes, q_docs, k_docs, status, out_rest):
+        return
+    d, seqs, at, n_lse = _attention("ps_attention_forward", q, k, q_offsets, k_offsets, max_q, max_k, scale, softcap, causal, k_lengths,
+                                    q_start, prefix, slopes, q_docs, k_docs,
+                                    {"q": (q, False), "k": (k, True), "v": (v, True), "out": (out, False)})
+    _check(load_library().ps_attention_forward(
+        ctypes.byref(d), ctypes.byref(seqs), at["q"], at["k"], at["v"], at["out"], _sized_ptr(lse, torch.float32, n_lse, "lse"),
+        _sized_ptr(out_rest, torch.bfloat16, q.numel(), "out_rest"), _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _ptr(status, torch.int64, "status"), _stream()),
+        "ps_attention_forward")
+
+
+def ps_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                          q_offsets: torch.Tensor, k_offsets: torch.Tensor, max_q: int, max_k: int, dq: torch.Tensor, dk: torch.Tensor,
+                          dv: torch.Tensor, workspace: torch.Tensor, scale: Optional[float] = None, softcap: float = 0.0,
+                          causal: bool = False, k_lengths: Optional[torch.Tensor] = None, q_start: Optional[torch.Tensor] = None,
+                          prefix: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None,
+                          q_docs: Optional[torch.Tensor] = None, k_docs: Optional[torch.Tensor] = None,
+                          status: Optional[torch.Tensor] = None, out_rest: Optional[torch.Tensor] = None) -> None:
+    """Arguments as of ps_attention_forward(), which has left `out`, `lse` and `out_rest`; dq like q, dk and dv like k."""
+    if _made("attention_backward", q, k, v, out, lse, dout, q_offsets, k_offsets, max_q, max_k, dq, dk, dv, workspace, scale, softcap,
+             causal, k_lengths, q_start, prefix, slopes, q_docs, k_docs, status, out_rest):
+        return
+    d, seqs, at, n_lse = _attention("ps_attention_backward", q, k, q_offsets, k_offsets, max_q, max_k, scale, softcap, causal, k_lengths,
+                                    q_start, prefix, slopes, q_docs, k_docs,
+                                    {"q": (q, False), "k": (k, True), "v": (v, True), "out": (out, False), "dout": (dout, False),
+                                     "dq": (dq, False), "dk": (dk, True), "dv": (dv, True)})
+    _check(load_library().ps_attention_backward(
+        ctypes.byref(d), ctypes.byref(seqs), at["q"], at["k"], at["v"], at["out"], _sized_ptr(lse, torch.float32, n_lse, "lse"),
+        _sized_ptr(out_rest, torch.bfloat16, q.numel(), "out_rest"), at["dout"], at["dq"], at["dk"], at["dv"], _ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
+        _ptr(status, torch.int64, "status"), _stream()), "ps_attention_backward")
+
+
+PS_ROTARY_PLAIN, PS_ROTARY_LINEAR, PS_ROTARY_BASE, PS_ROTARY_PARTS = 0, 1, 2, 3
+
+
+def ps_rotary_frequencies(n_pairs: int, base: float = 10000.0, scaling: int = PS_ROTARY_PLAIN, factor: float = 1.0,
+                          trained_len: int = 0, slow: float = 1.0, fast: float = 32.0) -> torch.Tensor:
+    """[n_pairs] float32 on the host."""
+    out = torch.empty(max(n_pairs, 0), dtype=torch.float32)
+    _check(load_library().ps_rotary_frequencies(n_pairs, base, scaling, factor, trained_len, slow, fast,
+                                                ctypes.cast(out.data_ptr(), ctypes.POINTER(ctypes.c_float))), "ps_rotary_frequencies")
+    return out
+
+
+def ps_rotary(x: torch.Tensor, positions: torch.Tensor, frequencies: torch.Tensor, out: torch.Tensor, x2: Optional[torch.Tensor] = None,
+              out2: Optional[torch.Tensor] = None, interleaved: bool = False, magnitude: float = 1.0, inverse: bool = False) -> None:
+    """x, out [n_rows, heads, head_dim] and, turned by the same angles, x2, out2 [n_rows, heads2, head_dim]; out may be x."""
+    if _made("rotary", x, positions, frequencies, out, x2, out2, interleaved, magnitude, inverse):
+        return
+    if not isinstance(x, torch.Tensor) or x.dim() != 3 or (x2 is None) != (out2 is None) or (x2 is not None and x2.dim() != 3):
+        raise TypeError("ps_rotary: x and x2 are tensors of rows, heads and elements, each with its out")
+    n, heads, size = x.shape
+    d = ps_rotary_desc(_dtype_code(x.dtype, "ps_rotary"), size, frequencies.numel(), int(interleaved), int(inverse), heads,
+                       0 if x2 is None else x2.shape[1], magnitude, n)
+    at = {}
+    for name, t in (("x", x), ("out", out), ("x2", x2), ("out2", out2)):
+        if t is None:
+            at[name] = None
+            continue
+        at[name], strides = _heads_ptr(t, (n, x2.shape[1] if name.endswith("2") else heads, size), x.dtype, name)
+        setattr(d, name, strides)
+    _check(load_library().ps_rotary(ctypes.byref(d), at["x"], at["out"], at["x2"], at["out2"], _sized_ptr(positions, torch.int32, n, "positions"),
+                                    _ptr(frequencies, torch.float32, "frequencies"), _stream()), "ps_rotary")
+
+
+def _rows_ptr(t: Optional[torch.Tensor], shape: Tuple[int, int], dtype: torch.dtype, name: str) -> Tuple[Optional[int], int]:
+    """Address of a tensor [rows, cols] whose rows are dense, and how far they are apart."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
+        raise TypeError(f"{name}: need a {dtype} tensor on the GPU")
+    if tuple(t.shape) != shape or (shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: need shape {shape} and dense rows")
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def ps_dropout_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load_library().ps_dropout_workspace_bytes(rows, cols))
+
+
+def ps_dropout_forward(x: torch.Tensor, bias: Optional[torch.Tensor], residual: Optional[torch.Tensor], rng: torch.Tensor, p: float,
+                       out: torch.Tensor) -> None:
+    """out = residual + dropout(x + bias) of tensors [rows, cols]; rng: two int64 on the GPU, seed and number of the call."""
+    if _made("dropout_forward", x, bias, residual, rng, p, out):
+        return
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise TypeError("ps_dropout_forward: x is a tensor of rows and columns")
+    shape, code = tuple(x.shape), _dtype_code(x.dtype, "ps_dropout_forward")
+    xp, res, to = (_rows_ptr(t, shape, x.dtype, name) for t, name in ((x, "x"), (residual, "residual"), (out, "out")))
+    if out is None:
+        raise TypeError("out: need a tensor")
+    _check(load_library().ps_dropout_forward(*xp, _sized_ptr(bias, x.dtype, shape[1], "bias"), *res, _sized_ptr(rng, torch.int64, 2, "rng"),
+                                             p, code, *shape, *to, _stream()), "ps_dropout_forward")
+
+
+def ps_dropout_backward(dout: torch.Tensor, rng: torch.Tensor, p: float, dx: torch.Tensor, dbias: Optional[torch.Tensor],
+                        workspace: Optional[torch.Tensor]) -> None:
+    """dx of dropout's x and, unless it is None, dbias ([cols] float32) from dout; rng and p as forwards."""
+    if _made("dropout_backward", dout, rng, p, dx, dbias, workspace):
+        return
+    if not isinstance(dout, torch.Tensor) or dout.dim() != 2 or dx is None:
+        raise TypeError("ps_dropout_backward: dout and dx are tensors of rows and columns")
+    shape, code = tuple(dout.shape), _dtype_code(dout.dtype, "ps_dropout_backward")
+    g, to = (_rows_ptr(t, shape, dout.dtype, name) for t, name in ((dout, "dout"), (dx, "dx")))
+    _check(load_library().ps_dropout_backward(
+        *g, _sized_ptr(rng, torch.int64, 2, "rng"), p, code, *shape, *to, _sized_ptr(dbias, torch.float32, shape[1], "dbias"),
+        _ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(), _stream()), "ps_dropout_backward")
 
 
 def alloc_workspace(nbytes: int, device="cuda") -> torch.Tensor:

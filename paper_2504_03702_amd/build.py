@@ -17,7 +17,8 @@ LIB = os.path.join(HERE, "libpreserve.so")
 MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 SOURCES = ["api.hip", "model_file.cpp", "rowops.hip", "encoder_f32.hip", "encoder_bf16.hip", "gemm_bf16.hip", "skinny_gemm.hip", "small_gemm.hip", "attention_bf16.hip",
-           "anticipate.hip", "lookahead.hip", "scaler.hip", "router.hip", "forecaster.hip", "stream_read.hip"]
+           "anticipate.hip", "lookahead.hip", "scaler.hip", "router.hip", "forecaster.hip", "stream_read.hip",
+           "seq_attention_fwd.hip", "seq_attention_bwd.hip", "rotary.hip", "dropout.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 
@@ -33,7 +34,7 @@ def _hipcc() -> str:
 
 # Per-file additions.  attention: MFMA results go straight to ordinary VGPRs, since the softmax reads
 # every one of them with VALU instructions (the default sends them through the accumulation registers).
-EXTRA_FLAGS = {"attention_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+EXTRA_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("attention_bf16.hip", "seq_attention_fwd.hip", "seq_attention_bwd.hip")}
 
 
 def _compile(src: str) -> str:

@@ -9,6 +9,8 @@
 // says what is wrong.
 #include <Python.h>
 
+#include <cmath>
+
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "preserve.h"
@@ -26,18 +28,25 @@ struct Calls {
     decltype(&ps_scaler_scan) scaler_scan;
     decltype(&ps_route) route;
     decltype(&ps_forecast) forecast;
+    decltype(&ps_attention_forward) attention_forward;
+    decltype(&ps_attention_backward) attention_backward;
+    decltype(&ps_rotary) rotary;
+    decltype(&ps_dropout_forward) dropout_forward;
+    decltype(&ps_dropout_backward) dropout_backward;
 } g_calls;
 
 PyObject* bind(PyObject*, PyObject* const* at, Py_ssize_t n) {
-    void* p[7];
-    if (n != 7) { PyErr_SetString(PyExc_TypeError, "bind: seven addresses"); return nullptr; }
-    for (int i = 0; i < 7; ++i) {
+    constexpr int N = 12;
+    void* p[N];
+    if (n != N) { PyErr_SetString(PyExc_TypeError, "bind: an address for every call"); return nullptr; }
+    for (int i = 0; i < N; ++i) {
         p[i] = PyLong_AsVoidPtr(at[i]);
         if (PyErr_Occurred()) return nullptr;
     }
     g_calls = {(decltype(&ps_predict_load))p[0], (decltype(&ps_anticipate))p[1], (decltype(&ps_anticipate_static))p[2],
                (decltype(&ps_lookahead_update))p[3], (decltype(&ps_scaler_scan))p[4], (decltype(&ps_route))p[5],
-               (decltype(&ps_forecast))p[6]};
+               (decltype(&ps_forecast))p[6], (decltype(&ps_attention_forward))p[7], (decltype(&ps_attention_backward))p[8],
+               (decltype(&ps_rotary))p[9], (decltype(&ps_dropout_forward))p[10], (decltype(&ps_dropout_backward))p[11]};
     Py_RETURN_NONE;
 }
 
@@ -70,6 +79,55 @@ struct Args {
         const long v = PyLong_AsLongAndOverflow(at[i], &overflow);
         if (overflow || v != (int32_t)v) { good = false; return 0; }
         return (int32_t)v;
+    }
+    float f32(int i) {
+        if (!good || !(PyFloat_CheckExact(at[i]) || PyLong_CheckExact(at[i]))) { good = false; return 0.f; }
+        const double v = PyFloat_AsDouble(at[i]);
+        if (PyErr_Occurred()) { PyErr_Clear(); good = false; }
+        return (float)v;
+    }
+    bool truth(int i) {
+        if (at[i] != Py_True && at[i] != Py_False) good = false;
+        return at[i] == Py_True;
+    }
+    // A tensor [rows][heads][size] with dense heads; its shape goes to `shape`, or has to be that if its size is known.
+    void* heads(int i, at::ScalarType* type, int64_t (&shape)[3], ps_strides& s) {
+        PyObject* o = at[i];
+        if (!good || !THPVariable_CheckExact(o)) { good = false; return nullptr; }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.defined() || !t.is_cuda() || t.dim() != 3) { good = false; return nullptr; }
+        if (shape[2] < 0) {
+            *type = t.scalar_type();
+            if (*type != at::kFloat && *type != at::kBFloat16) good = false;
+            for (int d = 0; d < 3; ++d)
+                if (shape[d] < 0) shape[d] = t.size(d);
+        }
+        if (t.scalar_type() != *type || t.size(0) != shape[0] || t.size(1) != shape[1] || t.size(2) != shape[2] ||
+            (shape[2] > 1 && t.stride(2) != 1)) { good = false; return nullptr; }
+        s.row = shape[0] > 1 ? t.stride(0) : shape[2];       // (torch keeps any stride for dimensions of one)
+        s.head = shape[1] > 1 ? t.stride(1) : shape[2];
+        return t.data_ptr();
+    }
+    // A tensor [rows][cols] with dense rows, the same way; *ld: how far they are apart.
+    void* rows(int i, at::ScalarType* type, int64_t (&shape)[2], int64_t* ld, bool optional = false) {
+        PyObject* o = at[i];
+        *ld = 0;
+        if (o == Py_None && optional) return nullptr;
+        if (!good || !THPVariable_CheckExact(o)) { good = false; return nullptr; }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.defined() || !t.is_cuda() || t.dim() != 2) { good = false; return nullptr; }
+        if (shape[0] < 0) {
+            *type = t.scalar_type();
+            if (*type != at::kFloat && *type != at::kBFloat16) good = false;
+            shape[0] = t.size(0);
+            shape[1] = t.size(1);
+        }
+        if (t.scalar_type() != *type || t.size(0) != shape[0] || t.size(1) != shape[1] || (shape[1] > 1 && t.stride(1) != 1)) {
+            good = false;
+            return nullptr;
+        }
+        *ld = shape[0] > 1 ? t.stride(0) : shape[1];
+        return t.data_ptr();
     }
     // a count of elements that the call takes as an int32
     int32_t count32(int64_t n) {
@@ -250,9 +308,161 @@ PyObject* forecast(PyObject*, PyObject* const* at, Py_ssize_t n) {
     });
 }
 
+// What the two attention calls share: at[i] and on are scale .. status.
+struct Attention {
+    ps_attention_desc d = {};
+    ps_attention_seqs s = {};
+    at::ScalarType type = at::kFloat;
+    int64_t q_shape[3] = {-1, -1, -1}, k_shape[3] = {-1, -1, -1};
+    void* workspace = nullptr;
+    int64_t ws = 0;
+    ps_status* status = nullptr;
+
+    void* queries(Args& a, int i, ps_strides ps_attention_desc::*s) { return a.heads(i, &type, q_shape, d.*s); }
+    void* keys(Args& a, int i, ps_strides ps_attention_desc::*s) {
+        if (k_shape[2] >= 0) return a.heads(i, &type, k_shape, d.*s);
+        at::ScalarType own;
+        void* p = a.heads(i, &own, k_shape, d.*s);
+        if (own != type || k_shape[2] != q_shape[2]) a.good = false;
+        return p;
+    }
+    void others(Args& a, int offsets, int max, int workspace_at, int i) {
+        int64_t n = 0;
+        s.q_offsets = a.tensor<int32_t>(offsets, kI32, &n);
+        s.k_offsets = a.sized<int32_t>(offsets + 1, kI32, n);
+        d.n_seq = a.count32(n - 1);
+        d.max_q = a.i32(max);
+        d.max_k = a.i32(max + 1);
+        workspace = a.tensor<void>(workspace_at, kU8, &ws);
+        if (!a.good) return;
+        d.dtype = type == at::kBFloat16;
+        d.heads = a.count32(q_shape[1]);
+        d.kv_heads = a.count32(k_shape[1]);
+        d.head_dim = a.count32(q_shape[2]);
+        d.n_q = q_shape[0];
+        d.n_k = k_shape[0];
+        d.scale = a.at[i] == Py_None ? (float)std::pow((double)d.head_dim, -0.5) : a.f32(i);
+        d.softcap = a.f32(i + 1);
+        d.causal = a.truth(i + 2);
+        s.k_lengths = a.sized<int32_t>(i + 3, kI32, d.n_seq, true);
+        s.q_start = a.sized<int32_t>(i + 4, kI32, d.n_seq, true);
+        s.prefix = a.sized<int32_t>(i + 5, kI32, d.n_seq, true);
+        s.slopes = a.sized<float>(i + 6, kF32, d.heads, true);
+        s.q_docs = a.sized<int32_t>(i + 7, kI32, d.n_q, true);
+        s.k_docs = a.sized<int32_t>(i + 8, kI32, d.n_k, true);
+        status = a.tensor<ps_status>(i + 9, kI64, nullptr, true);
+        if (!s.q_docs != !s.k_docs) a.good = false;
+    }
+    // (fp32 calls have none)
+    void* rest(Args& a, int i) { return a.sized<void>(i, at::kBFloat16, q_shape[0] * q_shape[1] * q_shape[2], true); }
+};
+
+PyObject* attention_forward(PyObject*, PyObject* const* at, Py_ssize_t n) {
+    return make_call(at, n, 21, [](Args& a) {
+        using D = ps_attention_desc;
+        Attention t;
+        const void* q = t.queries(a, 0, &D::q);
+        const void *k = t.keys(a, 1, &D::k), *v = t.keys(a, 2, &D::v);
+        void* out = t.queries(a, 7, &D::out);
+        float* lse = a.sized<float>(8, kF32, t.q_shape[0] * t.q_shape[1], true);
+        t.others(a, 3, 5, 9, 10);
+        void* rest = t.rest(a, 20);
+        return [=](void* s) {
+            return g_calls.attention_forward(&t.d, &t.s, q, k, v, out, lse, rest, t.workspace, (size_t)t.ws, t.status, s);
+        };
+    });
+}
+
+PyObject* attention_backward(PyObject*, PyObject* const* at, Py_ssize_t n) {
+    return make_call(at, n, 25, [](Args& a) {
+        using D = ps_attention_desc;
+        Attention t;
+        const void* q = t.queries(a, 0, &D::q);
+        const void *k = t.keys(a, 1, &D::k), *v = t.keys(a, 2, &D::v), *out = t.queries(a, 3, &D::out);
+        const float* lse = a.sized<float>(4, kF32, t.q_shape[0] * t.q_shape[1]);
+        const void* dout = t.queries(a, 5, &D::dout);
+        void *dq = t.queries(a, 10, &D::dq), *dk = t.keys(a, 11, &D::dk), *dv = t.keys(a, 12, &D::dv);
+        t.others(a, 6, 8, 13, 14);
+        const void* rest = t.rest(a, 24);
+        return [=](void* s) {
+            return g_calls.attention_backward(&t.d, &t.s, q, k, v, out, lse, rest, dout, dq, dk, dv, t.workspace, (size_t)t.ws, t.status,
+                                              s);
+        };
+    });
+}
+
+PyObject* rotary(PyObject*, PyObject* const* at, Py_ssize_t n) {
+    return make_call(at, n, 9, [](Args& a) {
+        ps_rotary_desc d = {};
+        at::ScalarType type = at::kFloat;
+        int64_t shape[3] = {-1, -1, -1}, pairs = 0;
+        const void* x = a.heads(0, &type, shape, d.x);
+        const int32_t* positions = a.sized<int32_t>(1, kI32, shape[0]);
+        const float* frequencies = a.tensor<float>(2, kF32, &pairs);
+        void* out = a.heads(3, &type, shape, d.out);
+        const void* x2 = nullptr;
+        void* out2 = nullptr;
+        if (a.at[4] != Py_None || a.at[5] != Py_None) {
+            at::ScalarType own;
+            int64_t shape2[3] = {shape[0], -1, -1};
+            x2 = a.heads(4, &own, shape2, d.x2);
+            if (a.good && (own != type || shape2[2] != shape[2])) a.good = false;
+            out2 = a.heads(5, &type, shape2, d.out2);
+            d.heads2 = a.count32(shape2[1]);
+        }
+        d.dtype = type == at::kBFloat16;
+        d.head_dim = a.count32(shape[2]);
+        d.n_pairs = a.count32(pairs);
+        d.heads = a.count32(shape[1]);
+        d.n_rows = shape[0];
+        d.interleaved = a.truth(6);
+        d.magnitude = a.f32(7);
+        d.inverse = a.truth(8);
+        return [=](void* s) { return g_calls.rotary(&d, x, out, x2, out2, positions, frequencies, s); };
+    });
+}
+
+PyObject* dropout_forward(PyObject*, PyObject* const* at, Py_ssize_t n) {
+    return make_call(at, n, 6, [](Args& a) {
+        at::ScalarType type = at::kFloat;
+        int64_t shape[2] = {-1, -1}, ld_x, ld_residual, ld_out;
+        const void* x = a.rows(0, &type, shape, &ld_x);
+        const void* bias = a.sized<void>(1, type, shape[1], true);
+        const void* residual = a.rows(2, &type, shape, &ld_residual, true);
+        const int64_t* rng = a.sized<int64_t>(3, kI64, 2);
+        const float p = a.f32(4);
+        void* out = a.rows(5, &type, shape, &ld_out);
+        const int32_t dtype = type == at::kBFloat16, cols = a.count32(shape[1]);
+        const int64_t rows = shape[0];
+        return [=](void* s) {
+            return g_calls.dropout_forward(x, ld_x, bias, residual, ld_residual, rng, p, dtype, rows, cols, out, ld_out, s);
+        };
+    });
+}
+
+PyObject* dropout_backward(PyObject*, PyObject* const* at, Py_ssize_t n) {
+    return make_call(at, n, 6, [](Args& a) {
+        at::ScalarType type = at::kFloat;
+        int64_t shape[2] = {-1, -1}, ld_dout, ld_dx, ws = 0;
+        const void* dout = a.rows(0, &type, shape, &ld_dout);
+        const int64_t* rng = a.sized<int64_t>(1, kI64, 2);
+        const float p = a.f32(2);
+        void* dx = a.rows(3, &type, shape, &ld_dx);
+        float* dbias = a.sized<float>(4, kF32, shape[1], true);
+        void* workspace = a.tensor<void>(5, kU8, &ws, true);
+        const int32_t dtype = type == at::kBFloat16, cols = a.count32(shape[1]);
+        const int64_t rows = shape[0];
+        return [=](void* s) {
+            return g_calls.dropout_backward(dout, ld_dout, rng, p, dtype, rows, cols, dx, ld_dx, dbias, workspace, (size_t)(ws < 0 ? 0 : ws), s);
+        };
+    });
+}
+
 #define PS_METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PS_METHOD(bind), PS_METHOD(predict_load), PS_METHOD(anticipate), PS_METHOD(anticipate_static), PS_METHOD(lookahead_update),
-                         PS_METHOD(scaler_scan), PS_METHOD(route), PS_METHOD(forecast), {nullptr, nullptr, 0, nullptr}};
+                         PS_METHOD(scaler_scan), PS_METHOD(route), PS_METHOD(forecast),
+                         PS_METHOD(attention_forward), PS_METHOD(attention_backward), PS_METHOD(rotary), PS_METHOD(dropout_forward),
+                         PS_METHOD(dropout_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,173 @@
+// Rotary positions.  A call reads and writes its tensors once and computes next to nothing, so memory bounds it: a workgroup takes a
+// few rows, puts the cosines and sines of their pairs into LDS once, and streams all heads past them.
+#include <math.h>
+
+#include "device_util.h"
+#include "internal.h"
+
+typedef __bf16 bf16;
+
+namespace {
+
+struct RotaryArgs {
+    const void* x[2];
+    void* out[2];
+    ps_strides xs[2], os[2];
+    const int32_t* positions;
+    const float* frequencies;
+    int64_t n_rows;
+    int32_t heads, heads2, head_dim, n_pairs, interleaved, rows, heads_each;   // rows, heads of a workgroup
+    float magnitude, sign;
+    int32_t in_place[2];
+};
+
+constexpr int TABLE = 2048;            // pairs of a workgroup's rows, at most
+
+// VEC elements at a time (16 bytes), or one.
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
+    __shared__ float2 table[TABLE];
+    constexpr int VEC = WIDE ? 16 / (int)sizeof(T) : 1;
+    const int64_t row0 = (int64_t)blockIdx.x * a.rows;
+    const int rows = (int)min((int64_t)a.rows, a.n_rows - row0), n = a.n_pairs;
+    for (int i = threadIdx.x; i < rows * n; i += 256) {
+        // whole turns go in 64 bits: a position of 31 bits times a frequency of 24 leaves the fraction all a float can hold
+        double turns = (double)a.positions[row0 + i / n] * (double)a.frequencies[i % n] * 0.15915494309189533577;
+        turns -= rint(turns);
+        float s, c;
+        sincospif(2.f * (float)turns, &s, &c);
+        table[i] = make_float2(c * a.magnitude, s * a.magnitude * a.sign);
+    }
+    __syncthreads();
+    const int head0 = blockIdx.y * a.heads_each, heads = min(a.heads_each, a.heads + a.heads2 - head0);
+    // units of a head: its turning pairs (VEC of them in halves, VEC / 2 or one interleaved), then what is copied, VEC a unit
+    const int turning = a.interleaved ? (WIDE ? 2 * n / VEC : n) : n / VEC, units = turning + (a.head_dim - 2 * n) / VEC;
+    for (int i = threadIdx.x; i < rows * heads * units; i += 256) {
+        const int unit = i % units, h = head0 + i / units % heads, r = i / units / heads, second = h >= a.heads;
+        const int64_t row = row0 + r;
+        const int hh = second ? h - a.heads : h;
+        const T* x = (const T*)a.x[second] + row * a.xs[second].row + hh * a.xs[second].head;
+        T* out = (T*)a.out[second] + row * a.os[second].row + hh * a.os[second].head;
+        const float2* cs = table + r * n;
+        struct alignas(WIDE ? 16 : sizeof(T)) Piece { T v[VEC]; };
+        if (unit >= turning) {
+            if (!a.in_place[second]) {
+                const int e = 2 * n + (unit - turning) * VEC;
+                *(Piece*)(out + e) = *(const Piece*)(x + e);
+            }
+        } else if (!a.interleaved) {
+            const int e = unit * VEC;
+            Piece p = *(const Piece*)(x + e), q = *(const Piece*)(x + n + e);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float u = (float)p.v[j], v = (float)q.v[j];
+                const float2 w = cs[e + j];
+                p.v[j] = (T)(u * w.x - v * w.y);
+                q.v[j] = (T)(u * w.y + v * w.x);
+            }
+            *(Piece*)(out + e) = p;
+            *(Piece*)(out + n + e) = q;
+        } else if constexpr (WIDE) {
+            const int e = unit * VEC;
+            Piece p = *(const Piece*)(x + e);
+#pragma unroll
+            for (int j = 0; j < VEC; j += 2) {
+                const float u = (float)p.v[j], v = (float)p.v[j + 1];
+                const float2 w = cs[(e + j) / 2];
+                p.v[j] = (T)(u * w.x - v * w.y);
+                p.v[j + 1] = (T)(u * w.y + v * w.x);
+            }
+            *(Piece*)(out + e) = p;
+        } else {
+            const float u = (float)x[2 * unit], v = (float)x[2 * unit + 1];
+            const float2 w = cs[unit];
+            out[2 * unit] = (T)(u * w.x - v * w.y);
+            out[2 * unit + 1] = (T)(u * w.y + v * w.x);
+        }
+    }
+}
+
+bool strides_ok(const ps_strides& s, bool written, int heads, int head_dim, int64_t rows) {
+    if (s.row < 0 || s.head < 0) return false;
+    return !written || ((heads <= 1 || s.head >= head_dim) && (rows <= 1 || s.row >= head_dim));
+}
+
+template <typename T>
+void launch(const RotaryArgs& a, bool wide, dim3 grid, hipStream_t st) {
+    if (wide)
+        hipLaunchKernelGGL((rotary_kernel<T, true>), grid, dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((rotary_kernel<T, false>), grid, dim3(256), 0, st, a);
+}
+
+}  // namespace
+
+extern "C" int ps_rotary(const ps_rotary_desc* d, const void* x, void* out, const void* x2, void* out2, const int32_t* positions,
+                         const float* frequencies, void* hip_stream) {
+    if (!d || (d->dtype != 0 && d->dtype != 1) || d->head_dim < 1 || d->n_pairs < 0 || (int64_t)2 * d->n_pairs > d->head_dim ||
+        d->heads < 1 || d->heads2 < 0 || d->n_rows < 0 || (d->interleaved & ~1) || (d->inverse & ~1) || !x2 != !out2 || (d->heads2 > 0) != (x2 != nullptr))
+        return PS_EINVAL;
+    // (a workgroup counts the elements of its rows, 8 at most, in 32 bits)
+    if (d->head_dim > 4096 || ((int64_t)d->heads + d->heads2) * d->head_dim > 1 << 27 || d->n_rows > INT32_MAX) return PS_EUNSUPPORTED;
+    if (!strides_ok(d->x, false, d->heads, d->head_dim, d->n_rows) || !strides_ok(d->out, true, d->heads, d->head_dim, d->n_rows) ||
+        (x2 && (!strides_ok(d->x2, false, d->heads2, d->head_dim, d->n_rows) || !strides_ok(d->out2, true, d->heads2, d->head_dim, d->n_rows))))
+        return PS_EINVAL;
+    if (d->n_rows == 0) return PS_OK;
+    if (!x || !out || (d->n_pairs > 0 && (!positions || !frequencies))) return PS_EINVAL;
+    const size_t es = d->dtype == 1 ? 2 : 4;
+    if (((uintptr_t)x | (uintptr_t)out | (uintptr_t)x2 | (uintptr_t)out2) % es != 0) return PS_EINVAL;
+    RotaryArgs a = {{x, x2}, {out, out2}, {d->x, d->x2}, {d->out, d->out2}, positions, frequencies, d->n_rows, d->heads, d->heads2,
+                    d->head_dim, d->n_pairs, d->interleaved, 1, 1, d->magnitude, d->inverse ? -1.f : 1.f, {x == out, x2 == out2}};
+    if ((x == out && (d->x.row != d->out.row || d->x.head != d->out.head)) || (x2 && x2 == out2 && (d->x2.row != d->out2.row || d->x2.head != d->out2.head)))
+        return PS_EINVAL;
+    // 16 bytes at a time where every address and the pieces of a head allow it
+    const int vec = (int)(16 / es);
+    uintptr_t bits = (uintptr_t)x | (uintptr_t)out | (uintptr_t)x2 | (uintptr_t)out2;
+    int64_t steps = d->x.row | d->x.head | d->out.row | d->out.head;
+    if (x2) steps |= d->x2.row | d->x2.head | d->out2.row | d->out2.head;
+    const bool wide = bits % 16 == 0 && steps % vec == 0 && d->head_dim % vec == 0 && (d->interleaved ? 2 * d->n_pairs : d->n_pairs) % vec == 0;
+    // Rows of a workgroup: a pair a thread for the table; heads are shared out where rows alone do not fill the chip.
+    const int all = d->heads + d->heads2;
+    const int64_t most = d->n_pairs > 0 ? (d->n_pairs >= 256 ? 1 : 256 / d->n_pairs) : 8;
+    a.rows = (int32_t)(most < 8 ? most : 8);
+    while (a.rows > 1 && (d->n_rows + a.rows - 1) / a.rows < 1024) a.rows /= 2;
+    const int64_t blocks = (d->n_rows + a.rows - 1) / a.rows;
+    const int shares = (int)(blocks >= 512 ? 1 : 512 / blocks < all ? 512 / blocks : all);
+    a.heads_each = (all + shares - 1) / shares;
+    (void)hipGetLastError();
+    const int64_t per = 1 << 22;       // (a grid holds fewer than 2^32 threads)
+    for (int64_t b0 = 0; b0 < blocks; b0 += per) {
+        RotaryArgs b = a;
+        const int64_t first = b0 * a.rows;
+        for (int i = 0; i < 2; ++i) {
+            if (!b.x[i]) continue;
+            b.x[i] = (const char*)a.x[i] + (size_t)first * a.xs[i].row * es;
+            b.out[i] = (char*)a.out[i] + (size_t)first * a.os[i].row * es;
+        }
+        if (positions) b.positions = positions + first;
+        b.n_rows = d->n_rows - first;
+        const dim3 grid((unsigned)(blocks - b0 < per ? blocks - b0 : per), (unsigned)((all + a.heads_each - 1) / a.heads_each));
+        d->dtype == 1 ? launch<bf16>(b, wide, grid, (hipStream_t)hip_stream) : launch<float>(b, wide, grid, (hipStream_t)hip_stream);
+    }
+    return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
+}
+
+extern "C" int ps_rotary_frequencies(int32_t n, double base, int scaling, double factor, int32_t trained_len, double slow, double fast,
+                                     float* f) {
+    if (n < 1 || !f || !(base > 0) || isinf(base) || scaling < PS_ROTARY_PLAIN || scaling > PS_ROTARY_PARTS) return PS_EINVAL;
+    if (scaling != PS_ROTARY_PLAIN && (!(factor > 0) || isinf(factor))) return PS_EINVAL;
+    if (scaling == PS_ROTARY_BASE && n < 2) return PS_EINVAL;
+    if (scaling == PS_ROTARY_PARTS && (trained_len < 1 || !(slow >= 0) || !(fast > slow))) return PS_EINVAL;
+    if (scaling == PS_ROTARY_BASE) base *= pow(factor, (double)n / (n - 1));
+    for (int32_t i = 0; i < n; ++i) {
+        double w = pow(base, -(double)i / n);
+        if (scaling == PS_ROTARY_LINEAR) w /= factor;
+        if (scaling == PS_ROTARY_PARTS) {
+            const double turns = trained_len * w * 0.15915494309189533577;
+            const double kept = turns <= slow ? 0.0 : turns >= fast ? 1.0 : (turns - slow) / (fast - slow);
+            w = w / factor * (1.0 - kept) + w * kept;
+        }
+        f[i] = (float)w;
+    }
+    return PS_OK;
+}

@@ -1,0 +1,286 @@
+// What the kernels of ps_attention_forward() and ps_attention_backward() share: arguments, sequences, tiles in LDS and their
+// products on the matrix cores, which tiles a block of rows sees, scores.
+//
+// The rows of a key head's queries are those of all its heads, r = G i + g for row i and head g of the G: keys and values are
+// read once for all of them, and their gradients add the heads up without a word of traffic.  "Fixed" rows belong to lanes: a
+// wavefront owns 32, a lane one of them (and the other half of the wavefront the same 32), in registers.  "Passing" rows come
+// by in tiles through LDS.  A product of a tile with the fixed rows (v_mfma_f32_32x32x16_bf16, v_mfma_f32_32x32x2_f32; A = the
+// tile, B = the fixed rows) leaves a lane with the scores of its own row: accumulator element e of half-wavefront h is passing
+// row 8 (e / 4) + 4 h + e % 4 of 32.  Row maxima and sums are then a lane's own, and the weights are the B operand of the second
+// product (A = the tile's transpose) as they stand: the order of the contracted rows is free, so it is the accumulator's.
+#pragma once
+
+#include "device_util.h"
+#include "internal.h"
+
+namespace seqatt {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int FIXED = 128;             // fixed rows of a workgroup, 32 a wavefront
+constexpr int DOC_BLOCK = 64;          // tokens to a summary of their documents
+
+struct Args {
+    const void *q, *k, *v, *out, *dout;
+    void *out_w, *dq, *dk, *dv;
+    void* rest_w;                      // bf16 calls: what rounding left of out, dense, or null
+    const void* rest;
+    float* lse_w;
+    const float* lse;
+    const int32_t *q_offsets, *k_offsets, *k_lengths, *q_start, *prefix, *q_docs, *k_docs;
+    const float* slopes;
+    int2 *q_blocks, *k_blocks;         // smallest and largest document of every DOC_BLOCK tokens
+    float2* stats;                     // [heads][n_q]: lse in powers of two (+infinity for rows that see nothing), dout . out
+    float* part_o;                     // [parts][n_q * heads][head_dim], unnormalised
+    float2* part_ml;                   // [parts][n_q * heads]: reference exponent, sum
+    ps_status* status;
+    ps_strides qs, ks, vs, os, gs, dqs, dks, dvs;
+    int64_t n_q, n_k;
+    int32_t n_seq, seq0, heads, kv_heads, head_dim, group, max_q, max_k, causal;
+    int32_t row_blocks;                // blocks of FIXED rows that the grid has for every sequence
+    int32_t parts, part_tiles;         // shares of a row block's key tiles
+    uint32_t by_group;                 // 2^32 / group + 1 (group > 1)
+    float scale, cap;
+};
+
+struct Seq {
+    int q0, qn, k0, kn, start, prefix;
+};
+
+// Sequence s, checked against the tensors and the host's bounds; false if it is faulty.
+__device__ __forceinline__ bool sequence(const Args& a, int s, Seq& r) {
+    r.q0 = a.q_offsets[s];
+    r.k0 = a.k_offsets[s];
+    const int q1 = a.q_offsets[s + 1], k1 = a.k_offsets[s + 1];
+    const int len = a.k_lengths ? a.k_lengths[s] : k1 - r.k0;
+    // (ends before starts: a negative offset, or one that falls, fails one of these)
+    if (r.q0 < 0 || q1 < r.q0 || q1 > a.n_q || r.k0 < 0 || k1 < r.k0 || k1 > a.n_k) return false;
+    if (len < 0 || len > k1 - r.k0 || len > a.max_k || q1 - r.q0 > a.max_q) return false;
+    r.qn = q1 - r.q0;
+    r.kn = len;
+    r.start = a.q_start ? a.q_start[s] : r.kn - r.qn;
+    r.prefix = a.prefix ? a.prefix[s] : 0;
+    return true;
+}
+
+__device__ __forceinline__ unsigned over_group(const Args& a, unsigned r) { return a.group == 1 ? r : __umulhi(r, a.by_group); }
+
+// Where sequence summaries of documents start: sequences never share one.
+__device__ __forceinline__ int64_t doc_block0(int first_token, int s) { return first_token / DOC_BLOCK + s; }
+
+// ---- tiles in LDS: rows of DP elements (head_dim and zeros), 16-byte chunks swizzled so that 16 rows' equal chunks, and the
+// transposing reads, fall into different banks -------------------------------------------------------------------------------
+template <typename T, int DP>
+struct Tile {
+    static constexpr int EB = sizeof(T), ROWB = DP * EB, ROWS = EB == 2 ? 64 : 32, BLOCKS = ROWS / 32, BYTES = ROWS * ROWB;
+    static constexpr int CPR = ROWB / 16, PER_THREAD = BYTES / 16 / 256, EPC = 16 / EB, NF = ROWB / 32, NA = DP / 32;
+    static __device__ __forceinline__ int swz(int r) {
+        if (EB == 4) return ((r >> 2) & 1) << 3 | (r & 3) << 1 | ((r >> 3) & 1);
+        if (DP == 64) return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) | ((r >> 3) & 1) << 1;
+        return (r & 3) << 2 | ((r >> 2) & 3);
+    }
+    static __device__ __forceinline__ int at(int r, int chunk) { return r * ROWB + ((chunk ^ swz(r)) << 4); }
+};
+
+// A lane's fixed row: chunks 2 i + half.
+template <typename T, int DP>
+struct Fixed {
+    uint4 c[Tile<T, DP>::NF];
+    __device__ __forceinline__ void load(const T* row, bool valid, int head_dim, int half) {
+#pragma unroll
+        for (int i = 0; i < Tile<T, DP>::NF; ++i) {
+            const int e = (2 * i + half) * Tile<T, DP>::EPC;
+            c[i] = valid && e < head_dim ? *(const uint4*)(row + e) : make_uint4(0, 0, 0, 0);
+        }
+    }
+};
+
+// Lane-constant parts of the LDS addresses.
+template <typename T, int DP>
+struct Lanes {
+    int row, turned;
+    __device__ __forceinline__ Lanes(int lane) {
+        using L = Tile<T, DP>;
+        const int half = lane >> 5, r = lane & 31;
+        row = L::at(r, half);
+        if (L::EB == 2) {
+            const int li = lane & 15, g = (lane >> 4) & 1, rl = 4 * half + (li >> 2);
+            turned = L::at(rl, 2 * g + ((li & 3) >> 1)) + (li & 1) * 8;
+        } else {
+            turned = L::at(4 * half, r >> 2) + (r & 3) * 4;
+        }
+    }
+};
+
+#define SEQATT_LDS __attribute__((address_space(3)))
+
+__device__ __forceinline__ bf16x8 as_bf16x8(uint4 u) { return __builtin_bit_cast(bf16x8, u); }
+
+// 32 passing rows (block b of the tile) times the fixed rows.
+template <typename T, int DP>
+__device__ __forceinline__ f32x16 dot(const unsigned char* tile, int b, const Fixed<T, DP>& f, const Lanes<T, DP>& l) {
+    using L = Tile<T, DP>;
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < L::NF; ++i) {
+        const uint4 a = *(const uint4*)(tile + b * 32 * L::ROWB + (l.row ^ (i << 5)));
+        if constexpr (L::EB == 2) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(f.c[i]), s, 0, 0, 0);
+        } else {
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(f.c[i].x), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(f.c[i].y), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(f.c[i].z), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(f.c[i].w), s, 0, 0, 0);
+        }
+    }
+    return s;
+}
+
+// What the rounding of w to bf16 leaves.  In tiles that a mask cuts rows see few keys, so weights are large and g has few terms:
+// the rounding of g, which averages out over many, is made up for there by a second product (a diagonal tile in 32 of 2048 keys).
+__device__ __forceinline__ void keep_rest(float (&w)[16]) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) w[e] -= (float)(__bf16)w[e];
+}
+
+// acc[feature][fixed row] += sum over the block's 32 passing rows of tile[row][feature] w[row].
+template <typename T, int DP>
+__device__ __forceinline__ void weigh(const unsigned char* tile, int b, const float (&w)[16], f32x16 (&acc)[Tile<T, DP>::NA],
+                                      const Lanes<T, DP>& l) {
+    using L = Tile<T, DP>;
+    const unsigned char* base = tile + b * 32 * L::ROWB;
+    if constexpr (L::EB == 2) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            uint4 p;
+            p.x = cvt_pk_bf16(w[8 * j], w[8 * j + 1]);
+            p.y = cvt_pk_bf16(w[8 * j + 2], w[8 * j + 3]);
+            p.z = cvt_pk_bf16(w[8 * j + 4], w[8 * j + 5]);
+            p.w = cvt_pk_bf16(w[8 * j + 6], w[8 * j + 7]);
+#pragma unroll
+            for (int i = 0; i < L::NA; ++i) {
+                union { s16x4 h[2]; bf16x8 v; } a;
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    a.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (SEQATT_LDS s16x4*)(base + (16 * j + 8 * x) * L::ROWB + (l.turned ^ (i << 6) ^ (x << 5))));
+                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, as_bf16x8(p), acc[i], 0, 0, 0);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+#pragma unroll
+            for (int i = 0; i < L::NA; ++i) {
+                const int swz = (e & 3) << 1 | ((e >> 2) & 1);
+                const float v = *(const float*)(base + (8 * (e >> 2) + (e & 3)) * L::ROWB + (l.turned ^ (swz << 4) ^ (i << 7)));
+                acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w[e], acc[i], 0, 0, 0);
+            }
+    }
+}
+
+// A tile on its way from memory: a thread's chunks of two tensors.  Rows that `valid` leaves out become zeros.
+template <typename T, int DP>
+struct Coming {
+    uint4 c[Tile<T, DP>::PER_THREAD];
+    // row(i): address of passing row i's element 0, null for one that is to be zeros
+    template <typename Row>
+    __device__ __forceinline__ void load(int head_dim, Row row) {
+        using L = Tile<T, DP>;
+#pragma unroll
+        for (int j = 0; j < L::PER_THREAD; ++j) {
+            const int id = j * 256 + (int)threadIdx.x, e = id % L::CPR * L::EPC;
+            const T* p = row(id / L::CPR);
+            c[j] = p && e < head_dim ? *(const uint4*)(p + e) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void store(unsigned char* tile) const {
+        using L = Tile<T, DP>;
+#pragma unroll
+        for (int j = 0; j < L::PER_THREAD; ++j) {
+            const int id = j * 256 + (int)threadIdx.x;
+            *(uint4*)(tile + L::at(id / L::CPR, id % L::CPR)) = c[j];
+        }
+    }
+};
+
+// ---- which tiles are seen: 64 of them at a time, a lane each, as two masks ----------------------------------------------------
+struct Walk {
+    int group = -1;
+    uint64_t seen = 0, whole = 0;
+    // The first tile from t on that is seen, `end` if none is.  classify(tile, whole): whether tile is seen, and by all.
+    template <typename Classify>
+    __device__ __forceinline__ int next(int t, int end, Classify classify) {
+        while (t < end) {
+            if ((t >> 6) != group) {
+                group = t >> 6;
+                const int mine = group * 64 + (int)(threadIdx.x & 63);
+                bool all = false;
+                const bool some = mine < end && classify(mine, all);
+                seen = __ballot(some);
+                whole = __ballot(some && all);
+            }
+            const uint64_t m = seen >> (t & 63);
+            if (m) return t + __builtin_ctzll(m);
+            t = (group + 1) << 6;
+        }
+        return end;
+    }
+    __device__ __forceinline__ bool is_whole(int t) const { return whole >> (t & 63) & 1; }
+};
+
+// ---- scores ------------------------------------------------------------------------------------------------------------------
+// tanh for the cap.  bf16 calls: the exponential's 1 - 2 / (1 + e^2u), whose absolute error of 1e-7 is that of a score near the cap;
+// fp32 calls take the library's, good to the last places everywhere.
+template <typename T>
+__device__ __forceinline__ float bend(float u) {
+    if constexpr (sizeof(T) == 4) return tanhf(u);
+    return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * (2.f * LOG2E)));
+}
+
+// Row of accumulator element e.
+__device__ __forceinline__ constexpr int row_of(int e) { return 8 * (e >> 2) + (e & 3); }   // + 4 half
+
+// A lane's accumulators [feature][its row] times `by` to memory, 4 features at a time.
+template <typename T, int DP>
+__device__ __forceinline__ void put_row(T* row, const f32x16 (&acc)[DP / 32], float by, int head_dim, int half) {
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int f = 32 * i + 8 * g + 4 * half;
+            if (f >= head_dim) continue;
+            if constexpr (sizeof(T) == 2)
+                *(uint2*)(row + f) = make_uint2(cvt_pk_bf16(acc[i][4 * g] * by, acc[i][4 * g + 1] * by),
+                                                cvt_pk_bf16(acc[i][4 * g + 2] * by, acc[i][4 * g + 3] * by));
+            else
+                *(float4*)(row + f) = make_float4(acc[i][4 * g] * by, acc[i][4 * g + 1] * by, acc[i][4 * g + 2] * by, acc[i][4 * g + 3] * by);
+        }
+}
+
+// The same for what rounding to bf16 left of them.
+template <int DP>
+__device__ __forceinline__ void put_rest(__bf16* row, const f32x16 (&acc)[DP / 32], float by, int head_dim, int half) {
+    f32x16 left[DP / 32];
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) left[i][e] = acc[i][e] * by - (float)(__bf16)(acc[i][e] * by);
+    put_row<__bf16, DP>(row, left, 1.f, head_dim, half);
+}
+
+// Checked arguments as the kernels take them, and the plan of a call; PS_OK or an error.
+struct Plan {
+    Args a;
+    size_t bytes;                      // of workspace
+};
+int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, void* workspace, Plan& p);
+int check_strides(const ps_attention_desc* d, const ps_strides& s, const void* base, bool written, int64_t heads);
+void summarise_documents(const Args& a, hipStream_t st);
+
+}  // namespace seqatt

@@ -1,0 +1,402 @@
+// Attention with capped scores, distance bias, document and prefix masks: the host's side of both directions, and forwards.
+#include <math.h>
+#include <string.h>
+
+#include "seq_attention.h"
+
+using namespace seqatt;
+typedef __bf16 bf16;
+
+namespace {
+
+constexpr float SLACK = 8.f;           // powers of two that a score may exceed the exponent's reference by
+
+// A workgroup: FIXED rows of a key head's queries, against a share of the key tiles that any of them sees (one pass, running
+// maximum and sum).
+template <typename T, int DP, bool PARTS>
+__global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
+    using L = Tile<T, DP>;
+    __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][keys, values]
+    __shared__ __align__(16) int s_doc[2][L::ROWS];
+
+    unsigned id = blockIdx.x;
+    const int hk = id % a.kv_heads;
+    id /= a.kv_heads;
+    const int part = PARTS ? id % a.parts : 0;
+    if (PARTS) id /= a.parts;
+    const int rb = a.row_blocks - 1 - (int)(id % a.row_blocks);           // (causal: the rows with the most keys first)
+    const int s = a.seq0 + (int)(id / a.row_blocks);
+    Seq q;
+    if (!sequence(a, s, q)) {
+        if (threadIdx.x == 0 && hk == 0 && rb == 0 && part == 0) report_fault(a.status, PS_ST_BAD_LENGTH, s);
+        return;
+    }
+    const int rows = q.qn * a.group, r0 = rb * FIXED;
+    if (r0 >= rows) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int tiles = (q.kn + L::ROWS - 1) / L::ROWS;
+    const int t0 = PARTS ? part * a.part_tiles : 0, t1 = PARTS ? min(tiles, t0 + a.part_tiles) : tiles;
+    if (PARTS && t0 > 0 && t0 >= tiles) return;                           // (part 0 writes, keys or not)
+
+    // this lane's row
+    const int r = r0 + 32 * wave + col, wr0 = r0 + 32 * wave;
+    const bool live = r < rows;
+    const int qi = (int)over_group(a, min(r, rows - 1)), head = hk * a.group + min(r, rows - 1) - qi * a.group;
+    const int64_t token = q.q0 + qi;
+    const int place = q.start + qi;
+    const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.f;
+    const int doc = a.q_docs && live ? max(a.q_docs[token], -1) : -1;
+    Fixed<T, DP> qf;
+    qf.load((const T*)a.q + token * a.qs.row + head * a.qs.head, live, a.head_dim, half);
+    const Lanes<T, DP> lanes(lane);
+
+    // what the workgroup's and the wavefront's rows see
+    const int last = min(r0 + FIXED, rows) - 1;
+    const int far = q.start + (int)over_group(a, last);                   // largest place
+    const int wfar = q.start + (int)over_group(a, min(wr0 + 31, rows - 1)), wnear = q.start + (int)over_group(a, min(wr0, rows - 1));
+    int dmin = 0, dmax = 0;                                               // documents of the workgroup's rows
+    if (a.q_docs) {
+        const int x = a.q_docs[q.q0 + (int)over_group(a, min(r0 + lane, last))], y = a.q_docs[q.q0 + (int)over_group(a, min(r0 + 64 + lane, last))];
+        dmin = min(x, y);
+        dmax = max(x, y);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            dmin = min(dmin, __shfl_xor(dmin, o, 64));
+            dmax = max(dmax, __shfl_xor(dmax, o, 64));
+        }
+    }
+    const int64_t kblock0 = doc_block0(q.k0, s);
+    auto classify = [&](int t, bool& all) {
+        const int k0 = t * L::ROWS;
+        bool some = true;
+        all = k0 + L::ROWS <= q.kn;
+        if (a.causal) {
+            some = k0 <= far || k0 < q.prefix;
+            all = all && (k0 + L::ROWS - 1 <= wnear || k0 + L::ROWS <= q.prefix);
+        }
+        if (a.k_docs && some) {
+            const int2 m = a.k_blocks[kblock0 + k0 / DOC_BLOCK];
+            some = dmax >= 0 && m.y >= max(dmin, 0) && m.x <= dmax;
+            all = all && m.x == m.y && dmin == dmax && m.x == dmin;
+        }
+        return some;
+    };
+
+    const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
+    const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
+    Coming<T, DP> ck, cv;
+    int cdoc = 0;
+    auto request = [&](int t) {
+        const int k0 = t * L::ROWS;
+        auto there = [&](int i) { return k0 + i < q.kn && (!a.k_docs || a.k_docs[q.k0 + k0 + i] >= 0); };
+        ck.load(a.head_dim, [&](int i) { return there(i) ? kbase + (int64_t)(k0 + i) * a.ks.row : nullptr; });
+        cv.load(a.head_dim, [&](int i) { return there(i) ? vbase + (int64_t)(k0 + i) * a.vs.row : nullptr; });
+        if (a.k_docs && threadIdx.x < L::ROWS)
+            cdoc = k0 + (int)threadIdx.x < q.kn ? a.k_docs[q.k0 + k0 + threadIdx.x] : -2;
+    };
+    auto arrive = [&](int buf) {
+        ck.store(smem[buf][0]);
+        cv.store(smem[buf][1]);
+        if (a.k_docs && threadIdx.x < L::ROWS) s_doc[buf][threadIdx.x] = cdoc < 0 ? -2 : cdoc;
+    };
+
+    f32x16 o[L::NA];
+#pragma unroll
+    for (int i = 0; i < L::NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    float m = -INFINITY, l = 0.f;      // the exponent's reference, in powers of two; this lane's share of the sum
+    const float c1 = a.scale * LOG2E, inner = a.cap > 0.f ? a.scale / a.cap : 0.f, outer = a.cap * LOG2E;
+
+    Walk walk;
+    int t = walk.next(t0, t1, classify), buf = 0;
+    if (t < t1) {
+        request(t);
+        arrive(0);
+        __syncthreads();
+    }
+    while (t < t1) {
+        const bool whole = walk.is_whole(t);
+        const int now = t, k0 = now * L::ROWS;
+        t = walk.next(t + 1, t1, classify);
+        if (t < t1) request(t);
+        // (a wavefront whose rows all stand before the tile has nothing in it)
+        if (wr0 < rows && !(a.causal && k0 > wfar && k0 >= q.prefix)) {
+            f32x16 sc[L::BLOCKS];
+#pragma unroll
+            for (int b = 0; b < L::BLOCKS; ++b) sc[b] = dot<T, DP>(smem[buf][0], b, qf, lanes);
+            float c = c1;
+            if (a.cap > 0.f) {
+#pragma unroll
+                for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sc[b][e] = bend<T>(sc[b][e] * inner) * outer;
+                c = 1.f;
+            }
+            if (a.slopes) {
+                const int from = place - k0 - 4 * half;
+#pragma unroll
+                for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        sc[b][e] = fmaf(-slope, fabsf((float)(from - 32 * b - row_of(e))), sc[b][e] * c);
+                c = 1.f;
+            }
+            if (!whole) {
+#pragma unroll
+                for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int i = 32 * b + row_of(e) + 4 * half, key = k0 + i;
+                        bool seen = key < q.kn && (!a.causal || key <= place || key < q.prefix);
+                        if (a.k_docs) seen = seen && s_doc[buf][i] == doc;
+                        if (!seen) sc[b][e] = -INFINITY;
+                    }
+            }
+            float mx = sc[0][0];
+#pragma unroll
+            for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[b][e]);
+            const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            mx = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1])) * c;
+            // the reference follows the maximum lazily: it moves when a tile exceeds it by more than SLACK, so weights reach
+            // 2^SLACK and the accumulators are rescaled a few times a row instead of at nearly every tile
+            if (__any(mx > m + SLACK)) {
+                const float next = mx > m + SLACK ? mx : m;
+                const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
+                m = next;
+#pragma unroll
+                for (int i = 0; i < L::NA; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
+                l *= alpha;
+            }
+            const float ref = m == -INFINITY ? 0.f : m;                   // (a row that has seen nothing yet)
+#pragma unroll
+            for (int b = 0; b < L::BLOCKS; ++b) {
+                float w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    w[e] = __builtin_amdgcn_exp2f(fmaf(sc[b][e], c, -ref));
+                    l += w[e];
+                }
+                weigh<T, DP>(smem[buf][1], b, w, o, lanes);
+            }
+        }
+        if (t < t1) arrive(buf ^ 1);
+        __syncthreads();
+        buf ^= 1;
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (!live) return;
+    if (PARTS) {
+        const int64_t row = ((int64_t)part * a.n_q + token) * a.heads + head;
+        put_row<float, DP>(a.part_o + row * a.head_dim, o, 1.f, a.head_dim, half);
+        if (half == 0) a.part_ml[row] = make_float2(m, l);
+        return;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    put_row<T, DP>((T*)a.out_w + token * a.os.row + head * a.os.head, o, inv, a.head_dim, half);
+    if (a.rest_w) put_rest<DP>((bf16*)a.rest_w + (token * a.heads + head) * a.head_dim, o, inv, a.head_dim, half);
+    if (a.lse_w && half == 0) a.lse_w[(int64_t)head * a.n_q + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+}
+
+// The parts of a row put together: a wavefront a row, lane f has elements f and f + 64.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(Args a) {
+    // rows of sequence s: (token, head) neighbours
+    const int s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 63;
+    Seq q;
+    if (!sequence(a, s, q)) return;
+    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (i >= (int64_t)q.qn * a.heads) return;
+    const int64_t row = (int64_t)q.q0 * a.heads + i, token = row / a.heads;
+    const int head = (int)(row - token * a.heads);
+    constexpr int TR = sizeof(T) == 2 ? 64 : 32;
+    const int tiles = (q.kn + TR - 1) / TR, parts = max(1, min(a.parts, (tiles + a.part_tiles - 1) / a.part_tiles));
+    const int64_t step = a.n_q * a.heads;
+    float m = -INFINITY;
+    for (int p = lane; p < parts; p += 64) m = fmaxf(m, a.part_ml[p * step + row].x);
+    m = wave_max(m);
+    float l = 0.f, x = 0.f, y = 0.f;
+    for (int p = 0; p < parts; ++p) {
+        const float2 ml = a.part_ml[p * step + row];
+        const float by = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+        const float* o = a.part_o + (p * step + row) * a.head_dim;
+        l = fmaf(ml.y, by, l);
+        if (lane < a.head_dim) x = fmaf(o[lane], by, x);
+        if (lane + 64 < a.head_dim) y = fmaf(o[lane + 64], by, y);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* out = (T*)a.out_w + token * a.os.row + head * a.os.head;
+    bf16* rest = (bf16*)a.rest_w + row * a.head_dim;
+    if (lane < a.head_dim) {
+        out[lane] = (T)(x * inv);
+        if (a.rest_w) rest[lane] = (bf16)(x * inv - (float)(T)(x * inv));
+    }
+    if (lane + 64 < a.head_dim) {
+        out[lane + 64] = (T)(y * inv);
+        if (a.rest_w) rest[lane + 64] = (bf16)(y * inv - (float)(T)(y * inv));
+    }
+    if (a.lse_w && lane == 0) a.lse_w[(int64_t)head * a.n_q + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+}
+
+// Smallest and largest document of every DOC_BLOCK tokens, a wavefront each; padding counts as -1.
+__global__ __launch_bounds__(256) void documents_kernel(Args a, int queries) {
+    const int s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 63, b = blockIdx.x * 4 + (threadIdx.x >> 6);
+    Seq q;
+    if (!sequence(a, s, q)) return;
+    const int n = queries ? q.qn : q.kn, first = queries ? q.q0 : q.k0;
+    if (b * DOC_BLOCK >= n) return;
+    const int32_t* docs = queries ? a.q_docs : a.k_docs;
+    int lo = max(docs[first + min(b * DOC_BLOCK + lane, n - 1)], -1), hi = lo;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        lo = min(lo, __shfl_xor(lo, o, 64));
+        hi = max(hi, __shfl_xor(hi, o, 64));
+    }
+    if (lane == 0) (queries ? a.q_blocks : a.k_blocks)[doc_block0(first, s) + b] = make_int2(lo, hi);
+}
+
+template <typename T, int DP>
+void launch_attend(const Args& a, hipStream_t st) {
+    const int64_t per_seq = (int64_t)a.kv_heads * a.row_blocks * a.parts;
+    Args b = a;
+    for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
+        const int64_t most = max((int64_t)1, (int64_t)(1 << 22) / per_seq);       // (a grid holds fewer than 2^32 threads)
+        n = (int32_t)min((int64_t)(a.n_seq - s0), most);
+        b.seq0 = s0;
+        const dim3 grid((unsigned)(per_seq * n));
+        if (a.parts > 1)
+            hipLaunchKernelGGL((attend_kernel<T, DP, true>), grid, dim3(256), 0, st, b);
+        else
+            hipLaunchKernelGGL((attend_kernel<T, DP, false>), grid, dim3(256), 0, st, b);
+    }
+    if (a.parts == 1) return;
+    for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
+        n = min(a.n_seq - s0, 32768);
+        b.seq0 = s0;
+        const dim3 grid((unsigned)(((int64_t)a.max_q * a.heads + 3) / 4), (unsigned)n);
+        hipLaunchKernelGGL(join_kernel<T>, grid, dim3(256), 0, st, b);
+    }
+}
+
+// `align`: what a row's address has to be a multiple of, in elements.
+bool good_strides(const ps_attention_desc* d, const ps_strides& s) {
+    const int64_t align = d->dtype == 1 ? 8 : 4;
+    return s.row >= 0 && s.head >= 0 && s.row % align == 0 && s.head % align == 0;
+}
+
+}  // namespace
+
+namespace seqatt {
+
+// A tensor that a call reads or writes.  Heads or rows of a written one may not fall on one another.
+int check_strides(const ps_attention_desc* d, const ps_strides& s, const void* base, bool written, int64_t heads) {
+    if (!base || ((uintptr_t)base & 15) != 0 || !good_strides(d, s)) return PS_EINVAL;
+    if (written && ((heads > 1 && s.head < d->head_dim) || s.row < d->head_dim)) return PS_EINVAL;
+    return PS_OK;
+}
+
+int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, void* workspace, Plan& p) {
+    if (!d || d->n_seq < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 || d->head_dim < 1 || d->max_q < 0 ||
+        d->max_k < 0 || d->n_q < 0 || d->n_k < 0 || d->n_q > INT32_MAX || d->n_k > INT32_MAX || (d->dtype != 0 && d->dtype != 1) ||
+        (d->causal != 0 && d->causal != 1))
+        return PS_EINVAL;
+    if (!(d->scale > 0.f) || !(d->softcap >= 0.f) || isinf(d->scale) || isinf(d->softcap)) return PS_EINVAL;
+    if (d->head_dim > 128 || d->head_dim % 8 != 0) return PS_EUNSUPPORTED;
+    const int64_t group = d->heads / d->kv_heads;
+    if (group > 32768 || (int64_t)d->max_q * group >= ((int64_t)1 << 31) / group) return PS_EUNSUPPORTED;
+    if (d->heads > 65536) return PS_EUNSUPPORTED;
+    Args& a = p.a;
+    memset(&a, 0, sizeof(a));
+    if (s) {
+        if (!s->q_offsets || !s->k_offsets || !s->q_docs != !s->k_docs) return PS_EINVAL;
+        a.q_offsets = s->q_offsets; a.k_offsets = s->k_offsets; a.k_lengths = s->k_lengths; a.q_start = s->q_start;
+        a.prefix = s->prefix; a.q_docs = s->q_docs; a.k_docs = s->k_docs; a.slopes = s->slopes;
+    }
+    a.qs = d->q; a.ks = d->k; a.vs = d->v; a.os = d->out; a.gs = d->dout; a.dqs = d->dq; a.dks = d->dk; a.dvs = d->dv;
+    a.n_q = d->n_q; a.n_k = d->n_k; a.n_seq = d->n_seq; a.heads = d->heads; a.kv_heads = d->kv_heads; a.head_dim = d->head_dim;
+    a.group = (int32_t)group; a.max_q = d->max_q; a.max_k = d->max_k; a.causal = d->causal;
+    a.scale = d->scale; a.cap = d->softcap;
+    a.by_group = group > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)group + 1) : 0;
+    a.row_blocks = (int32_t)(((int64_t)d->max_q * group + FIXED - 1) / FIXED);
+    // Row blocks that do not fill the chip: their keys are shared out, 256 keys or more to a part, two workgroups a unit.
+    const int tile = d->dtype == 1 ? 64 : 32, tiles = (d->max_k + tile - 1) / tile;
+    const int64_t blocks = max((int64_t)1, (int64_t)a.n_seq * a.kv_heads * a.row_blocks);
+    const int64_t parts = min((int64_t)512 / blocks, (int64_t)tiles / (256 / tile));
+    a.part_tiles = tiles;
+    a.parts = 1;
+    if (parts > 1) {
+        a.part_tiles = (int32_t)((tiles + parts - 1) / parts);
+        a.parts = (tiles + a.part_tiles - 1) / a.part_tiles;
+    }
+    size_t off = 0;
+    uint8_t* base = (uint8_t*)workspace;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = align_up(off + bytes, 256);
+        return (void*)(base + at);
+    };
+    a.q_blocks = (int2*)take(sizeof(int2) * (size_t)(d->n_q / DOC_BLOCK + d->n_seq + 1));
+    a.k_blocks = (int2*)take(sizeof(int2) * (size_t)(d->n_k / DOC_BLOCK + d->n_seq + 1));
+    const size_t rows = (size_t)d->n_q * d->heads, shared = off;
+    if (a.parts > 1) {
+        a.part_o = (float*)take(sizeof(float) * rows * d->head_dim * a.parts);
+        a.part_ml = (float2*)take(sizeof(float2) * rows * a.parts);
+    }
+    p.bytes = off;
+    if (backward) {
+        off = shared;
+        a.stats = (float2*)take(sizeof(float2) * rows);
+        p.bytes = off > p.bytes ? off : p.bytes;
+    }
+    return PS_OK;
+}
+
+void summarise_documents(const Args& a, hipStream_t st) {
+    if (!a.q_docs) return;
+    Args b = a;
+    for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
+        n = min(a.n_seq - s0, 32768);
+        b.seq0 = s0;
+        for (int queries = 0; queries < 2; ++queries) {
+            const int blocks = ((queries ? a.max_q : a.max_k) + DOC_BLOCK - 1) / DOC_BLOCK;
+            if (blocks > 0)
+                hipLaunchKernelGGL(documents_kernel, dim3((unsigned)((blocks + 3) / 4), (unsigned)n), dim3(256), 0, st, b, queries);
+        }
+    }
+}
+
+}  // namespace seqatt
+
+extern "C" size_t ps_attention_workspace_bytes(const ps_attention_desc* desc, int backward) {
+    Plan p;
+    return plan(desc, nullptr, backward != 0, nullptr, p) == PS_OK ? p.bytes : 0;
+}
+
+extern "C" int ps_attention_forward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const void* q, const void* k,
+                                    const void* v, void* out, float* lse, void* out_rest, void* workspace, size_t workspace_bytes,
+                                    ps_status* status, void* hip_stream) {
+    Plan p;
+    if (!seqs) return PS_EINVAL;
+    const int code = plan(desc, seqs, false, workspace, p);
+    if (code != PS_OK) return code;
+    if (p.a.n_seq == 0 || p.a.n_q == 0 || p.a.max_q == 0) return PS_OK;
+    if (check_strides(desc, desc->q, q, false, desc->heads) || check_strides(desc, desc->out, out, true, desc->heads)) return PS_EINVAL;
+    if (p.a.n_k > 0 && (check_strides(desc, desc->k, k, false, desc->kv_heads) || check_strides(desc, desc->v, v, false, desc->kv_heads)))
+        return PS_EINVAL;
+    if (((uintptr_t)out_rest & 15) != 0 || (out_rest && desc->dtype != 1) || (uintptr_t)lse % 4 != 0) return PS_EINVAL;
+    if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < p.bytes) return PS_EWORKSPACE;
+    Args& a = p.a;
+    a.q = q; a.k = k; a.v = v; a.out_w = out; a.lse_w = lse; a.rest_w = out_rest; a.status = status;
+    hipStream_t st = (hipStream_t)hip_stream;
+    (void)hipGetLastError();
+    summarise_documents(a, st);
+    if (desc->dtype == 1)
+        desc->head_dim <= 64 ? launch_attend<bf16, 64>(a, st) : launch_attend<bf16, 128>(a, st);
+    else
+        desc->head_dim <= 64 ? launch_attend<float, 64>(a, st) : launch_attend<float, 128>(a, st);
+    return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
+}
