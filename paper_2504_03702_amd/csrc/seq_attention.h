@@ -33,15 +33,17 @@ struct Args {
     const int32_t *q_offsets, *k_offsets, *k_lengths, *q_start, *prefix, *q_docs, *k_docs;
     const float* slopes;
     int2 *q_blocks, *k_blocks;         // smallest and largest document of every DOC_BLOCK tokens
-    float2* stats;                     // [heads][n_q]: lse in powers of two (+infinity for rows that see nothing), dout . out
-    float* part_o;                     // [parts][n_q * heads][head_dim], unnormalised
+    float *row_lse, *row_delta;        // [heads][n_q]: lse in powers of two (+infinity for rows that see nothing); dout . out
+    float* part_o;                     // [parts][n_q * heads][head_dim]: unnormalised out, or dq
     float2* part_ml;                   // [parts][n_q * heads]: reference exponent, sum
+    float *part_dk, *part_dv;          // [key_parts][n_k * kv_heads][head_dim]
     ps_status* status;
     ps_strides qs, ks, vs, os, gs, dqs, dks, dvs;
     int64_t n_q, n_k;
     int32_t n_seq, seq0, heads, kv_heads, head_dim, group, max_q, max_k, causal;
     int32_t row_blocks;                // blocks of FIXED rows that the grid has for every sequence
-    int32_t parts, part_tiles;         // shares of a row block's key tiles
+    int32_t parts, part_tiles;         // shares of a row block's key tiles, and tiles of a share
+    int32_t key_parts, key_part_tiles; // shares of a key block's row tiles
     uint32_t by_group;                 // 2^32 / group + 1 (group > 1)
     float scale, cap;
 };
@@ -89,6 +91,17 @@ struct Tile {
 template <typename T, int DP>
 struct Fixed {
     uint4 c[Tile<T, DP>::NF];
+    // This half-wavefront's share of the product with another row that is laid out the same.
+    __device__ __forceinline__ float share(const Fixed& o) const {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < Tile<T, DP>::NF; ++i) {
+            const T *x = (const T*)&c[i], *y = (const T*)&o.c[i];
+#pragma unroll
+            for (int j = 0; j < Tile<T, DP>::EPC; ++j) sum = fmaf((float)x[j], (float)y[j], sum);
+        }
+        return sum;
+    }
     __device__ __forceinline__ void load(const T* row, bool valid, int head_dim, int half) {
 #pragma unroll
         for (int i = 0; i < Tile<T, DP>::NF; ++i) {
@@ -184,46 +197,46 @@ __device__ __forceinline__ void weigh(const unsigned char* tile, int b, const fl
     }
 }
 
-// A tile on its way from memory: a thread's chunks of two tensors.  Rows that `valid` leaves out become zeros.
-template <typename T, int DP>
-struct Coming {
-    uint4 c[Tile<T, DP>::PER_THREAD];
-    // row(i): address of passing row i's element 0, null for one that is to be zeros
-    template <typename Row>
-    __device__ __forceinline__ void load(int head_dim, Row row) {
-        using L = Tile<T, DP>;
-#pragma unroll
-        for (int j = 0; j < L::PER_THREAD; ++j) {
-            const int id = j * 256 + (int)threadIdx.x, e = id % L::CPR * L::EPC;
-            const T* p = row(id / L::CPR);
-            c[j] = p && e < head_dim ? *(const uint4*)(p + e) : make_uint4(0, 0, 0, 0);
-        }
-    }
-    __device__ __forceinline__ void store(unsigned char* tile) const {
-        using L = Tile<T, DP>;
-#pragma unroll
-        for (int j = 0; j < L::PER_THREAD; ++j) {
-            const int id = j * 256 + (int)threadIdx.x;
-            *(uint4*)(tile + L::at(id / L::CPR, id % L::CPR)) = c[j];
-        }
-    }
-};
+static __device__ const uint4 zeros = {0, 0, 0, 0};
 
-// ---- which tiles are seen: 64 of them at a time, a lane each, as two masks ----------------------------------------------------
+// Sends for a tile: 16 bytes a lane go from memory into LDS without a register (a lane picks the chunk whose swizzled place it
+// fills).  row(i): address of passing row i's element 0; null for a row of zeros.  Landed after vm_wait() and a barrier.
+template <typename T, int DP, typename Row>
+__device__ __forceinline__ void send_tile(unsigned char* tile, int head_dim, Row row) {
+    using L = Tile<T, DP>;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < L::PER_THREAD; ++j) {
+        const int place = (j * 4 + wave) * 64 + lane, r = place / L::CPR, e = ((place % L::CPR) ^ L::swz(r)) * L::EPC;
+        const T* p = row(r);
+        const void* from = p && (head_dim == DP || e < head_dim) ? (const void*)(p + e) : (const void*)&zeros;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                         (SEQATT_LDS void*)(tile + (j * 4 + wave) * 1024), 16, 0, 0);
+    }
+}
+// The same for a word a lane of this wavefront.
+__device__ __forceinline__ void send_words(void* to, const void* from) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)to, 4, 0, 0);
+}
+__device__ __forceinline__ void vm_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// ---- which tiles are seen: 64 of them at a time, a lane each, as masks ----------------------------------------------------
 struct Walk {
     int group = -1;
-    uint64_t seen = 0, whole = 0;
-    // The first tile from t on that is seen, `end` if none is.  classify(tile, whole): whether tile is seen, and by all.
+    uint64_t seen = 0, whole = 0, padded = 0;
+    // The first tile from t on that is seen, `end` if none is.  classify(tile, whole, padded): whether tile is seen; whether by all; whether
+    // some of it is padding.
     template <typename Classify>
     __device__ __forceinline__ int next(int t, int end, Classify classify) {
         while (t < end) {
             if ((t >> 6) != group) {
                 group = t >> 6;
                 const int mine = group * 64 + (int)(threadIdx.x & 63);
-                bool all = false;
-                const bool some = mine < end && classify(mine, all);
+                bool all = false, pad = false;
+                const bool some = mine < end && classify(mine, all, pad);
                 seen = __ballot(some);
                 whole = __ballot(some && all);
+                padded = __ballot(some && pad);
             }
             const uint64_t m = seen >> (t & 63);
             if (m) return t + __builtin_ctzll(m);
@@ -232,6 +245,7 @@ struct Walk {
         return end;
     }
     __device__ __forceinline__ bool is_whole(int t) const { return whole >> (t & 63) & 1; }
+    __device__ __forceinline__ bool is_padded(int t) const { return padded >> (t & 63) & 1; }
 };
 
 // ---- scores ------------------------------------------------------------------------------------------------------------------

@@ -1,7 +1,7 @@
-// Gradients of the attention of seq_attention_fwd.hip, in three launches: what a row brings along (its lse and dout . out), the
-// gradients of keys and values (keys fixed, queries passing), that of the queries (queries fixed, keys passing).  Scores are computed
-// again in both of the latter; every gradient is then a sum in one wavefront's registers, in an order that the shapes fix, and
-// nothing is added up in memory.
+// Gradients of the attention of seq_attention_fwd.hip, in two launches: that of the queries (queries fixed, keys passing), which also
+// leaves each row's dout . out, and those of keys and values (keys fixed, queries passing).  Scores are computed again in both;
+// every gradient is then a sum in one wavefront's registers, in an order that the shapes fix.  Where blocks do not fill the chip
+// their passing tiles are shared out, and a launch more adds up the shares, one after the other.
 #include "seq_attention.h"
 
 using namespace seqatt;
@@ -9,61 +9,43 @@ typedef __bf16 bf16;
 
 namespace {
 
-// stats[head][token]: 16 lanes a row, 8 elements a lane.
-template <typename T>
-__global__ __launch_bounds__(256) void stats_kernel(Args a) {
-    const int e = (threadIdx.x & 15) * 8;
-    for (int64_t first = (int64_t)blockIdx.x * 16; first < a.n_q * a.heads; first += (int64_t)gridDim.x * 16) {
-        const int64_t row = first + (threadIdx.x >> 4);
-        const bool live = row < a.n_q * a.heads;
-        const int64_t token = live ? row / a.heads : 0;
-        const int head = live ? (int)(row - token * a.heads) : 0;
-        float sum = 0.f;
-        if (live && e < a.head_dim) {
-            const T *o = (const T*)a.out + token * a.os.row + head * a.os.head + e, *g = (const T*)a.dout + token * a.gs.row + head * a.gs.head + e;
-            T x[8], y[8];
+// The weights p and the gradients d of x = scale q . k of one block, from the products s = q . k and g = dout . v.  row(e): what
+// element e's query brings along, distance(e): how far it stands from the key, seen(e): whether it sees it.  Everything that is
+// the same for all elements is asked outside their loops, so that these are straight lines.
+template <typename T, typename Row, typename Distance, typename Seen>
+__device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, float (&p)[16], float (&d)[16], bool whole, Row row,
+                                          Distance distance, Seen seen) {
+    const float c1 = a.scale * LOG2E;
+    if (a.cap > 0.f) {
+        const float inner = a.scale / a.cap, outer = a.cap * LOG2E;
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(x) / 16; ++i) {
-                ((uint4*)x)[i] = ((const uint4*)o)[i];
-                ((uint4*)y)[i] = ((const uint4*)g)[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf((float)x[i], (float)y[i], sum);
-            if (sizeof(T) == 2 && a.rest) {
-                *(uint4*)x = *(const uint4*)((const bf16*)a.rest + row * a.head_dim + e);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum = fmaf((float)x[i], (float)y[i], sum);
-            }
+        for (int e = 0; e < 16; ++e) {
+            const float u = bend<T>(s[e] * inner);
+            p[e] = u * outer;
+            d[e] = fmaf(-u, u, 1.f);
         }
+    } else {
 #pragma unroll
-        for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        if (live && e == 0) {
-            const float lse = a.lse[(int64_t)head * a.n_q + token];
-            a.stats[(int64_t)head * a.n_q + token] = make_float2(lse == -INFINITY ? INFINITY : lse * LOG2E, sum);
-        }
+        for (int e = 0; e < 16; ++e) p[e] = s[e] * c1;
     }
-}
-
-// The weights and the gradients of x = scale q . k of one block, from the products s = q . k and g = dout . v.
-// row(e, lse, delta, slope_times_distance, seen): what element e's query and key are to one another.
-template <typename T, typename Row>
-__device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, float (&p)[16], float (&d)[16], Row row) {
-    const float c1 = a.scale * LOG2E, inner = a.cap > 0.f ? a.scale / a.cap : 0.f, outer = a.cap * LOG2E;
+    if (a.slopes) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[e] -= distance(e);
+    }
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-        float lse, delta, off;
-        const bool seen = row(e, lse, delta, off);
-        float y, slope = 1.f;
-        if (a.cap > 0.f) {
-            const float u = bend<T>(s[e] * inner);
-            slope = fmaf(-u, u, 1.f);
-            y = fmaf(u, outer, -(lse + off));
-        } else {
-            y = fmaf(s[e], c1, -(lse + off));
+        const float2 r = row(e);
+        p[e] = __builtin_amdgcn_exp2f(p[e] - r.x);
+        const float w = p[e] * (g[e] - r.y);
+        d[e] = a.cap > 0.f ? d[e] * w : w;
+    }
+    if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const bool is = seen(e);
+            p[e] = is ? p[e] : 0.f;
+            d[e] = is ? d[e] : 0.f;
         }
-        const float w = __builtin_amdgcn_exp2f(y);
-        p[e] = seen ? w : 0.f;
-        d[e] = seen ? w * (g[e] - delta) * slope : 0.f;
     }
 }
 
@@ -79,6 +61,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void key_gradients_kernel(Ar
     unsigned id = blockIdx.x;
     const int hk = id % a.kv_heads;
     id /= a.kv_heads;
+    const int part = id % a.key_parts;
+    id /= a.key_parts;
     const int kb = (int)(id % key_blocks), s = a.seq0 + (int)(id / key_blocks);   // (causal: the keys that most rows see first)
     Seq q;
     if (!sequence(a, s, q)) return;                                       // (reported by the queries' launch)
@@ -86,13 +70,15 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void key_gradients_kernel(Ar
     if (k0 >= q.kn) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
     const int rows = q.qn * a.group, tiles = (rows + L::ROWS - 1) / L::ROWS;
+    const int t0 = part * a.key_part_tiles, t1 = min(tiles, t0 + a.key_part_tiles);
+    if (t0 > 0 && t0 >= tiles) return;                                    // (part 0 writes, rows or not)
 
     // this lane's key
     const int wk0 = k0 + 32 * wave, key = wk0 + col;
     const bool live = key < q.kn;
     const int64_t token = q.k0 + min(key, q.kn - 1);
-    const int doc = a.k_docs ? (live && a.k_docs[token] >= 0 ? a.k_docs[token] : -2) : 0;
-    const bool there = live && (!a.k_docs || doc >= 0);
+    const int doc = a.k_docs ? a.k_docs[token] : 0;
+    const bool there = live && doc >= 0;
     Fixed<T, DP> kf, vf;
     kf.load((const T*)a.k + token * a.ks.row + hk * a.ks.head, there, a.head_dim, half);
     vf.load((const T*)a.v + token * a.vs.row + hk * a.vs.head, there, a.head_dim, half);
@@ -111,7 +97,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void key_gradients_kernel(Ar
         }
     }
     const int64_t qblock0 = doc_block0(q.q0, s);
-    auto classify = [&](int t, bool& all) {
+    auto classify = [&](int t, bool& all, bool& pad) {
         const int first = (int)over_group(a, t * L::ROWS), end = (int)over_group(a, min(t * L::ROWS + L::ROWS, rows) - 1);
         bool some = true;
         all = true;
@@ -124,55 +110,43 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void key_gradients_kernel(Ar
             const int lo = min(m.x, n.x), hi = max(m.y, n.y);
             some = dmax >= 0 && hi >= max(dmin, 0) && lo <= dmax;
             all = all && lo == hi && dmin == dmax && lo == dmin;
+            pad = lo < 0;
         }
         return some;
     };
 
-    Coming<T, DP> cq, cg;
-    float2 cstats = make_float2(INFINITY, 0.f);
-    float cslope = 0.f;
-    int cplace = 0, cdoc = -1;
-    auto request = [&](int t) {
+    auto request = [&](int t, bool padded, int buf) {
         const int r0 = t * L::ROWS;
-        // (a row's token and head; padding and rows past the end are zeros)
+        // a row's token and head; padding and rows past the end are zeros that see nothing
         auto find = [&](int i, int64_t& tok, int& head) {
             const int r = r0 + i;
             if (r >= rows) return false;
             const int qi = (int)over_group(a, r);
             head = hk * a.group + r - qi * a.group;
             tok = q.q0 + qi;
-            return !a.q_docs || a.q_docs[tok] >= 0;
+            return !padded || a.q_docs[tok] >= 0;
         };
-        cq.load(a.head_dim, [&](int i) {
-            int64_t tok;
-            int head;
-            return find(i, tok, head) ? (const T*)a.q + tok * a.qs.row + head * a.qs.head : nullptr;
-        });
-        cg.load(a.head_dim, [&](int i) {
-            int64_t tok;
-            int head;
-            return find(i, tok, head) ? (const T*)a.dout + tok * a.gs.row + head * a.gs.head : nullptr;
-        });
         if (threadIdx.x < L::ROWS) {
             int64_t tok;
             int head;
             const bool is = find(threadIdx.x, tok, head);
-            cstats = is ? a.stats[head * a.n_q + tok] : make_float2(INFINITY, 0.f);
-            cslope = is && a.slopes ? a.slopes[head] * LOG2E : 0.f;
-            cplace = is ? q.start + (int)(tok - q.q0) : 0;
-            cdoc = a.q_docs ? (is ? a.q_docs[tok] : -1) : 0;
+            const int64_t at = head * a.n_q + tok;
+            s_lse[buf][threadIdx.x] = is ? a.row_lse[at] : INFINITY;
+            s_delta[buf][threadIdx.x] = is ? a.row_delta[at] : 0.f;
+            s_place[buf][threadIdx.x] = is ? q.start + (int)(tok - q.q0) : 0;
+            if (a.slopes) s_slope[buf][threadIdx.x] = is ? a.slopes[head] * LOG2E : 0.f;
+            if (a.q_docs) s_doc[buf][threadIdx.x] = is ? a.q_docs[tok] : -1;
         }
-    };
-    auto arrive = [&](int buf) {
-        cq.store(smem[buf][0]);
-        cg.store(smem[buf][1]);
-        if (threadIdx.x < L::ROWS) {
-            s_lse[buf][threadIdx.x] = cstats.x;
-            s_delta[buf][threadIdx.x] = cstats.y;
-            s_slope[buf][threadIdx.x] = cslope;
-            s_place[buf][threadIdx.x] = cplace;
-            s_doc[buf][threadIdx.x] = cdoc;
-        }
+        send_tile<T, DP>(smem[buf][0], a.head_dim, [&](int i) {
+            int64_t tok;
+            int head;
+            return find(i, tok, head) ? (const T*)a.q + tok * a.qs.row + head * a.qs.head : nullptr;
+        });
+        send_tile<T, DP>(smem[buf][1], a.head_dim, [&](int i) {
+            int64_t tok;
+            int head;
+            return find(i, tok, head) ? (const T*)a.dout + tok * a.gs.row + head * a.gs.head : nullptr;
+        });
     };
 
     f32x16 dk[L::NA], dv[L::NA];
@@ -182,32 +156,35 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void key_gradients_kernel(Ar
         for (int e = 0; e < 16; ++e) dk[i][e] = dv[i][e] = 0.f;
 
     Walk walk;
-    int t = walk.next(0, tiles, classify), buf = 0;
-    if (t < tiles) {
-        request(t);
-        arrive(0);
-        __syncthreads();
-    }
-    while (t < tiles) {
+    int t = walk.next(t0, t1, classify), buf = 0;
+    if (t < t1) request(t, walk.is_padded(t), 0);
+    while (t < t1) {
         const bool whole = walk.is_whole(t);
         const int far = q.start + (int)over_group(a, min(t * L::ROWS + L::ROWS, rows) - 1);
-        t = walk.next(t + 1, tiles, classify);
-        if (t < tiles) request(t);
+        t = walk.next(t + 1, t1, classify);
+        vm_wait();
+        __syncthreads();                                                  // the tile has landed, the one before it is no longer read
+        if (t < t1) request(t, walk.is_padded(t), buf ^ 1);
         if (wk0 < q.kn && !(a.causal && wk0 > far && wk0 >= q.prefix)) {
-#pragma unroll
-            for (int b = 0; b < L::BLOCKS; ++b) {
+#pragma unroll 1
+            for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
                 const f32x16 sc = dot<T, DP>(smem[buf][0], b, kf, lanes), g = dot<T, DP>(smem[buf][1], b, vf, lanes);
                 float p[16], d[16];
-                gradients<T>(a, sc, g, p, d, [&](int e, float& lse, float& delta, float& off) {
-                    const int i = 32 * b + row_of(e) + 4 * half;
-                    lse = s_lse[buf][i];
-                    delta = s_delta[buf][i];
-                    off = a.slopes ? s_slope[buf][i] * fabsf((float)(s_place[buf][i] - key)) : 0.f;
-                    if (whole) return true;
-                    bool seen = !a.causal || key <= s_place[buf][i] || key < q.prefix;
-                    if (a.q_docs) seen = seen && s_doc[buf][i] == doc;
-                    return seen;
-                });
+                float4 lse[4], delta[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    lse[j] = *(const float4*)&s_lse[buf][32 * b + 8 * j + 4 * half];
+                    delta[j] = *(const float4*)&s_delta[buf][32 * b + 8 * j + 4 * half];
+                }
+                auto at = [&](int e) { return 32 * b + row_of(e) + 4 * half; };
+                gradients<T>(a, sc, g, p, d, whole,
+                             [&](int e) { return make_float2((&lse[e >> 2].x)[e & 3], (&delta[e >> 2].x)[e & 3]); },
+                             [&](int e) { return s_slope[buf][at(e)] * fabsf((float)(s_place[buf][at(e)] - key)); },
+                             [&](int e) {
+                                 bool is = !a.causal || key <= s_place[buf][at(e)] || key < q.prefix;
+                                 if (a.q_docs) is = is && s_doc[buf][at(e)] == doc && there;
+                                 return is;
+                             });
                 weigh<T, DP>(smem[buf][1], b, p, dv, lanes);
                 weigh<T, DP>(smem[buf][0], b, d, dk, lanes);
                 if (sizeof(T) == 2 && !whole) {
@@ -216,11 +193,15 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void key_gradients_kernel(Ar
                 }
             }
         }
-        if (t < tiles) arrive(buf ^ 1);
-        __syncthreads();
         buf ^= 1;
     }
     if (!live) return;
+    if (a.key_parts > 1) {
+        const int64_t row = ((int64_t)part * a.n_k + token) * a.kv_heads + hk;
+        put_row<float, DP>(a.part_dk + row * a.head_dim, dk, 1.f, a.head_dim, half);
+        put_row<float, DP>(a.part_dv + row * a.head_dim, dv, 1.f, a.head_dim, half);
+        return;
+    }
     put_row<T, DP>((T*)a.dk + token * a.dks.row + hk * a.dks.head, dk, a.scale, a.head_dim, half);
     put_row<T, DP>((T*)a.dv + token * a.dvs.row + hk * a.dvs.head, dv, 1.f, a.head_dim, half);
 }
@@ -230,21 +211,25 @@ template <typename T, int DP>
 __global__ __launch_bounds__(256, 2) void query_gradients_kernel(Args a) {
     using L = Tile<T, DP>;
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][keys, values]
-    __shared__ __align__(16) int s_doc[2][L::ROWS];
+    __shared__ __align__(16) int s_doc[2][64];
 
     unsigned id = blockIdx.x;
     const int hk = id % a.kv_heads;
     id /= a.kv_heads;
+    const int part = id % a.parts;
+    id /= a.parts;
     const int rb = a.row_blocks - 1 - (int)(id % a.row_blocks), s = a.seq0 + (int)(id / a.row_blocks);
     Seq q;
     if (!sequence(a, s, q)) {
-        if (threadIdx.x == 0 && hk == 0 && rb == 0) report_fault(a.status, PS_ST_BAD_LENGTH, s);
+        if (threadIdx.x == 0 && hk == 0 && rb == 0 && part == 0) report_fault(a.status, PS_ST_BAD_LENGTH, s);
         return;
     }
     const int rows = q.qn * a.group, r0 = rb * FIXED;
     if (r0 >= rows) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
     const int tiles = (q.kn + L::ROWS - 1) / L::ROWS;
+    const int t0 = part * a.part_tiles, t1 = min(tiles, t0 + a.part_tiles);
+    if (t0 > 0 && t0 >= tiles) return;                                    // (part 0 writes, keys or not)
 
     const int wr0 = r0 + 32 * wave, r = min(wr0 + col, rows - 1);
     const bool live = wr0 + col < rows;
@@ -252,13 +237,30 @@ __global__ __launch_bounds__(256, 2) void query_gradients_kernel(Args a) {
     const int64_t token = q.q0 + qi;
     const int place = q.start + qi;
     const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.f;
-    const int doc = a.q_docs && live ? max(a.q_docs[token], -1) : -1;
-    const bool there = live && (!a.q_docs || doc >= 0);
+    const int doc = a.q_docs ? a.q_docs[token] : 0;
+    const bool there = live && doc >= 0;
     Fixed<T, DP> qf, gf;
     qf.load((const T*)a.q + token * a.qs.row + head * a.qs.head, there, a.head_dim, half);
     gf.load((const T*)a.dout + token * a.gs.row + head * a.gs.head, there, a.head_dim, half);
-    const float2 st = there ? a.stats[(int64_t)head * a.n_q + token] : make_float2(INFINITY, 0.f);
     const Lanes<T, DP> lanes(lane);
+    // what the row brings along, for this launch and the keys'
+    float2 st;
+    {
+        Fixed<T, DP> of;
+        of.load((const T*)a.out + token * a.os.row + head * a.os.head, there, a.head_dim, half);
+        float delta = gf.share(of);
+        if (sizeof(T) == 2 && a.rest) {
+            of.load((const T*)a.rest + (token * a.heads + head) * a.head_dim, there, a.head_dim, half);
+            delta += gf.share(of);
+        }
+        const int64_t at = (int64_t)head * a.n_q + token;
+        const float lse = there ? a.lse[at] : -INFINITY;
+        st = make_float2(lse == -INFINITY ? INFINITY : lse * LOG2E, delta + __shfl_xor(delta, 32, 64));
+        if (live && half == 0 && part == 0) {
+            a.row_lse[at] = st.x;
+            a.row_delta[at] = st.y;
+        }
+    }
 
     const int last = min(r0 + FIXED, rows) - 1;
     const int far = q.start + (int)over_group(a, last);
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(256, 2) void query_gradients_kernel(Args a) {
         }
     }
     const int64_t kblock0 = doc_block0(q.k0, s);
-    auto classify = [&](int t, bool& all) {
+    auto classify = [&](int t, bool& all, bool& pad) {
         const int k0 = t * L::ROWS;
         bool some = true;
         all = k0 + L::ROWS <= q.kn;
@@ -287,26 +289,24 @@ __global__ __launch_bounds__(256, 2) void query_gradients_kernel(Args a) {
             const int2 m = a.k_blocks[kblock0 + k0 / DOC_BLOCK];
             some = dmax >= 0 && m.y >= max(dmin, 0) && m.x <= dmax;
             all = all && m.x == m.y && dmin == dmax && m.x == dmin;
+            pad = m.x < 0;
         }
         return some;
     };
 
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
-    Coming<T, DP> ck, cv;
-    int cdoc = 0;
-    auto request = [&](int t) {
+    auto request = [&](int t, bool padded, int buf) {
         const int k0 = t * L::ROWS;
-        auto is = [&](int i) { return k0 + i < q.kn && (!a.k_docs || a.k_docs[q.k0 + k0 + i] >= 0); };
-        ck.load(a.head_dim, [&](int i) { return is(i) ? kbase + (int64_t)(k0 + i) * a.ks.row : nullptr; });
-        cv.load(a.head_dim, [&](int i) { return is(i) ? vbase + (int64_t)(k0 + i) * a.vs.row : nullptr; });
-        if (a.k_docs && threadIdx.x < L::ROWS)
-            cdoc = k0 + (int)threadIdx.x < q.kn ? a.k_docs[q.k0 + k0 + threadIdx.x] : -2;
-    };
-    auto arrive = [&](int buf) {
-        ck.store(smem[buf][0]);
-        cv.store(smem[buf][1]);
-        if (a.k_docs && threadIdx.x < L::ROWS) s_doc[buf][threadIdx.x] = cdoc < 0 ? -2 : cdoc;
+        auto is = [&](int i) { return k0 + i < q.kn && (!padded || a.k_docs[q.k0 + k0 + i] >= 0); };
+        if (k0 + L::ROWS <= q.kn && !padded) {
+            send_tile<T, DP>(smem[buf][0], a.head_dim, [&](int i) { return kbase + (int64_t)k0 * a.ks.row + i * a.ks.row; });
+            send_tile<T, DP>(smem[buf][1], a.head_dim, [&](int i) { return vbase + (int64_t)k0 * a.vs.row + i * a.vs.row; });
+        } else {
+            send_tile<T, DP>(smem[buf][0], a.head_dim, [&](int i) { return is(i) ? kbase + (int64_t)(k0 + i) * a.ks.row : nullptr; });
+            send_tile<T, DP>(smem[buf][1], a.head_dim, [&](int i) { return is(i) ? vbase + (int64_t)(k0 + i) * a.vs.row : nullptr; });
+        }
+        if (a.k_docs && wave == 0) send_words(s_doc[buf], a.k_docs + q.k0 + min(k0 + lane, q.kn - 1));
     };
 
     f32x16 dq[L::NA];
@@ -316,32 +316,29 @@ __global__ __launch_bounds__(256, 2) void query_gradients_kernel(Args a) {
         for (int e = 0; e < 16; ++e) dq[i][e] = 0.f;
 
     Walk walk;
-    int t = walk.next(0, tiles, classify), buf = 0;
-    if (t < tiles) {
-        request(t);
-        arrive(0);
-        __syncthreads();
-    }
-    while (t < tiles) {
+    int t = walk.next(t0, t1, classify), buf = 0;
+    if (t < t1) request(t, walk.is_padded(t), 0);
+    while (t < t1) {
         const bool whole = walk.is_whole(t);
         const int k0 = t * L::ROWS;
-        t = walk.next(t + 1, tiles, classify);
-        if (t < tiles) request(t);
+        t = walk.next(t + 1, t1, classify);
+        vm_wait();
+        __syncthreads();                                                  // the tile has landed, the one before it is no longer read
+        if (t < t1) request(t, walk.is_padded(t), buf ^ 1);
         if (wr0 < rows && !(a.causal && k0 > wfar && k0 >= q.prefix)) {
-#pragma unroll
-            for (int b = 0; b < L::BLOCKS; ++b) {
+#pragma unroll 1
+            for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
                 const f32x16 sc = dot<T, DP>(smem[buf][0], b, qf, lanes), g = dot<T, DP>(smem[buf][1], b, gf, lanes);
                 float p[16], d[16];
-                gradients<T>(a, sc, g, p, d, [&](int e, float& lse, float& delta, float& off) {
-                    const int i = 32 * b + row_of(e) + 4 * half, key = k0 + i;
-                    lse = st.x;
-                    delta = st.y;
-                    off = a.slopes ? slope * fabsf((float)(place - key)) : 0.f;
-                    if (whole) return true;
-                    bool seen = key < q.kn && (!a.causal || key <= place || key < q.prefix);
-                    if (a.k_docs) seen = seen && s_doc[buf][i] == doc;
-                    return seen;
-                });
+                auto at = [&](int e) { return 32 * b + row_of(e) + 4 * half; };
+                gradients<T>(a, sc, g, p, d, whole, [&](int) { return st; },
+                             [&](int e) { return slope * fabsf((float)(place - k0 - at(e))); },
+                             [&](int e) {
+                                 const int key = k0 + at(e);
+                                 bool is = key < q.kn && (!a.causal || key <= place || key < q.prefix);
+                                 if (a.k_docs) is = is && s_doc[buf][at(e)] == doc && there;
+                                 return is;
+                             });
                 weigh<T, DP>(smem[buf][0], b, d, dq, lanes);
                 if (sizeof(T) == 2 && !whole) {
                     keep_rest(d);
@@ -349,33 +346,66 @@ __global__ __launch_bounds__(256, 2) void query_gradients_kernel(Args a) {
                 }
             }
         }
-        if (t < tiles) arrive(buf ^ 1);
-        __syncthreads();
         buf ^= 1;
     }
-    if (live) put_row<T, DP>((T*)a.dq + token * a.dqs.row + head * a.dqs.head, dq, a.scale, a.head_dim, half);
+    if (!live) return;
+    if (a.parts > 1)
+        put_row<float, DP>(a.part_o + (((int64_t)part * a.n_q + token) * a.heads + head) * a.head_dim, dq, 1.f, a.head_dim, half);
+    else
+        put_row<T, DP>((T*)a.dq + token * a.dqs.row + head * a.dqs.head, dq, a.scale, a.head_dim, half);
+}
+
+// A gradient's shares added up, a thread an element: those of queries (z = 0), keys (1) and values (2).
+template <typename T>
+__global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
+    const int z = z0 + (int)blockIdx.z, s = a.seq0 + (int)blockIdx.y;
+    Seq q;
+    if (!sequence(a, s, q)) return;
+    const int heads = z == 0 ? a.heads : a.kv_heads, of = z == 0 ? a.parts : a.key_parts, each = z == 0 ? a.part_tiles : a.key_part_tiles;
+    const int64_t all = z == 0 ? a.n_q : a.n_k;
+    const ps_strides to = z == 0 ? a.dqs : z == 1 ? a.dks : a.dvs;
+    const float* part = z == 0 ? a.part_o : z == 1 ? a.part_dk : a.part_dv;
+    T* out = (T*)(z == 0 ? a.dq : z == 1 ? a.dk : a.dv);
+    const float by = z == 2 ? 1.f : a.scale;
+    constexpr int TR = sizeof(T) == 2 ? 64 : 32;
+    const int passing = z == 0 ? q.kn : q.qn * a.group, parts = max(1, min(of, ((passing + TR - 1) / TR + each - 1) / each));
+    const int64_t n = (int64_t)(z == 0 ? q.qn : q.kn) * heads * a.head_dim, first = (int64_t)(z == 0 ? q.q0 : q.k0) * heads * a.head_dim;
+    const int64_t step = all * heads * a.head_dim;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        float sum = 0.f;
+#pragma unroll 8
+        for (int p = 0; p < parts; ++p) sum += part[p * step + first + i];
+        const int64_t row = (first + i) / a.head_dim, token = row / heads;
+        out[token * to.row + (row - token * heads) * to.head + (first + i - row * a.head_dim)] = (T)(sum * by);
+    }
 }
 
 template <typename T, int DP>
 void launch(const Args& a, hipStream_t st) {
-    const int64_t rows = a.n_q * a.heads;
-    // (a grid holds fewer than 2^32 threads: rows are taken in turn by what workgroups there are)
-    if (rows > 0) hipLaunchKernelGGL(stats_kernel<T>, dim3((unsigned)min((rows + 15) / 16, (int64_t)1 << 22)), dim3(256), 0, st, a);
     Args b = a;
-    auto in_parts = [&](int64_t per_seq, auto launch_one) {
+    auto in_turn = [&](int64_t per_seq, int64_t most_seqs, auto launch_one) {
         if (per_seq == 0) return;
-        const int64_t most = max((int64_t)1, (int64_t)(1 << 22) / per_seq);
+        const int64_t most = min(most_seqs, max((int64_t)1, (int64_t)(1 << 22) / per_seq));   // (a grid holds fewer than 2^32 threads)
         for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
             n = (int32_t)min((int64_t)(a.n_seq - s0), most);
             b.seq0 = s0;
-            launch_one(dim3((unsigned)(per_seq * n)));
+            launch_one((unsigned)n);
         }
     };
-    in_parts((int64_t)a.kv_heads * ((a.max_k + FIXED - 1) / FIXED), [&](dim3 grid) {
-        hipLaunchKernelGGL((key_gradients_kernel<T, DP>), grid, dim3(256), 0, st, b);
+    const int64_t row_jobs = (int64_t)a.kv_heads * a.row_blocks * a.parts;
+    const int64_t key_jobs = (int64_t)a.kv_heads * ((a.max_k + FIXED - 1) / FIXED) * a.key_parts;
+    in_turn(row_jobs, a.n_seq, [&](unsigned n) {
+        hipLaunchKernelGGL((query_gradients_kernel<T, DP>), dim3((unsigned)row_jobs * n), dim3(256), 0, st, b);
     });
-    in_parts((int64_t)a.kv_heads * a.row_blocks, [&](dim3 grid) {
-        hipLaunchKernelGGL((query_gradients_kernel<T, DP>), grid, dim3(256), 0, st, b);
+    in_turn(key_jobs, a.n_seq, [&](unsigned n) {
+        hipLaunchKernelGGL((key_gradients_kernel<T, DP>), dim3((unsigned)key_jobs * n), dim3(256), 0, st, b);
+    });
+    const int z0 = a.parts > 1 ? 0 : 1, z1 = a.key_parts > 1 ? 3 : 1;
+    if (z0 == z1) return;
+    const int64_t most = max(z0 == 0 ? (int64_t)a.max_q * a.heads : 0, z1 == 3 ? (int64_t)a.max_k * a.kv_heads : 0) * a.head_dim;
+    const unsigned blocks = (unsigned)min((most + 255) / 256, (int64_t)4096);
+    in_turn(blocks, 32768, [&](unsigned n) {
+        hipLaunchKernelGGL(add_kernel<T>, dim3(blocks, n, (unsigned)(z1 - z0)), dim3(256), 0, st, b, z0);
     });
 }
 

@@ -17,7 +17,7 @@ template <typename T, int DP, bool PARTS>
 __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     using L = Tile<T, DP>;
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][keys, values]
-    __shared__ __align__(16) int s_doc[2][L::ROWS];
+    __shared__ __align__(16) int s_doc[2][64];
 
     unsigned id = blockIdx.x;
     const int hk = id % a.kv_heads;
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     const int64_t token = q.q0 + qi;
     const int place = q.start + qi;
     const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.f;
-    const int doc = a.q_docs && live ? max(a.q_docs[token], -1) : -1;
+    const int doc = a.q_docs ? a.q_docs[token] : 0;
     Fixed<T, DP> qf;
     qf.load((const T*)a.q + token * a.qs.row + head * a.qs.head, live, a.head_dim, half);
     const Lanes<T, DP> lanes(lane);
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
         }
     }
     const int64_t kblock0 = doc_block0(q.k0, s);
-    auto classify = [&](int t, bool& all) {
+    auto classify = [&](int t, bool& all, bool& pad) {
         const int k0 = t * L::ROWS;
         bool some = true;
         all = k0 + L::ROWS <= q.kn;
@@ -78,26 +78,25 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
             const int2 m = a.k_blocks[kblock0 + k0 / DOC_BLOCK];
             some = dmax >= 0 && m.y >= max(dmin, 0) && m.x <= dmax;
             all = all && m.x == m.y && dmin == dmax && m.x == dmin;
+            pad = m.x < 0;
         }
         return some;
     };
 
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
-    Coming<T, DP> ck, cv;
-    int cdoc = 0;
-    auto request = [&](int t) {
+    auto request = [&](int t, bool padded, int buf) {
         const int k0 = t * L::ROWS;
-        auto there = [&](int i) { return k0 + i < q.kn && (!a.k_docs || a.k_docs[q.k0 + k0 + i] >= 0); };
-        ck.load(a.head_dim, [&](int i) { return there(i) ? kbase + (int64_t)(k0 + i) * a.ks.row : nullptr; });
-        cv.load(a.head_dim, [&](int i) { return there(i) ? vbase + (int64_t)(k0 + i) * a.vs.row : nullptr; });
-        if (a.k_docs && threadIdx.x < L::ROWS)
-            cdoc = k0 + (int)threadIdx.x < q.kn ? a.k_docs[q.k0 + k0 + threadIdx.x] : -2;
-    };
-    auto arrive = [&](int buf) {
-        ck.store(smem[buf][0]);
-        cv.store(smem[buf][1]);
-        if (a.k_docs && threadIdx.x < L::ROWS) s_doc[buf][threadIdx.x] = cdoc < 0 ? -2 : cdoc;
+        // (rows past the keys, and padding, are zeros: their weights are, and nothing is to come of them)
+        auto is = [&](int i) { return k0 + i < q.kn && (!padded || a.k_docs[q.k0 + k0 + i] >= 0); };
+        if (k0 + L::ROWS <= q.kn && !padded) {
+            send_tile<T, DP>(smem[buf][0], a.head_dim, [&](int i) { return kbase + (int64_t)k0 * a.ks.row + i * a.ks.row; });
+            send_tile<T, DP>(smem[buf][1], a.head_dim, [&](int i) { return vbase + (int64_t)k0 * a.vs.row + i * a.vs.row; });
+        } else {
+            send_tile<T, DP>(smem[buf][0], a.head_dim, [&](int i) { return is(i) ? kbase + (int64_t)(k0 + i) * a.ks.row : nullptr; });
+            send_tile<T, DP>(smem[buf][1], a.head_dim, [&](int i) { return is(i) ? vbase + (int64_t)(k0 + i) * a.vs.row : nullptr; });
+        }
+        if (a.k_docs && wave == 0) send_words(s_doc[buf], a.k_docs + q.k0 + min(k0 + lane, q.kn - 1));
     };
 
     f32x16 o[L::NA];
@@ -110,16 +109,14 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
 
     Walk walk;
     int t = walk.next(t0, t1, classify), buf = 0;
-    if (t < t1) {
-        request(t);
-        arrive(0);
-        __syncthreads();
-    }
+    if (t < t1) request(t, walk.is_padded(t), 0);
     while (t < t1) {
         const bool whole = walk.is_whole(t);
-        const int now = t, k0 = now * L::ROWS;
+        const int k0 = t * L::ROWS;
         t = walk.next(t + 1, t1, classify);
-        if (t < t1) request(t);
+        vm_wait();
+        __syncthreads();                                                  // the tile has landed, the one before it is no longer read
+        if (t < t1) request(t, walk.is_padded(t), buf ^ 1);
         // (a wavefront whose rows all stand before the tile has nothing in it)
         if (wr0 < rows && !(a.causal && k0 > wfar && k0 >= q.prefix)) {
             f32x16 sc[L::BLOCKS];
@@ -149,7 +146,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
                     for (int e = 0; e < 16; ++e) {
                         const int i = 32 * b + row_of(e) + 4 * half, key = k0 + i;
                         bool seen = key < q.kn && (!a.causal || key <= place || key < q.prefix);
-                        if (a.k_docs) seen = seen && s_doc[buf][i] == doc;
+                        if (a.k_docs) seen = seen && s_doc[buf][i] == doc && doc >= 0;
                         if (!seen) sc[b][e] = -INFINITY;
                     }
             }
@@ -184,8 +181,6 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
                 weigh<T, DP>(smem[buf][1], b, w, o, lanes);
             }
         }
-        if (t < t1) arrive(buf ^ 1);
-        __syncthreads();
         buf ^= 1;
     }
     l += __shfl_xor(l, 32, 64);
@@ -202,16 +197,14 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     if (a.lse_w && half == 0) a.lse_w[(int64_t)head * a.n_q + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
 }
 
-// The parts of a row put together: a wavefront a row, lane f has elements f and f + 64.
+// The parts of a row put together: a workgroup a row, a wavefront a quarter of its parts, lane f elements f and f + 64.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(Args a) {
-    // rows of sequence s: (token, head) neighbours
-    const int s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 63;
+    __shared__ float s_l[4], s_o[4][128];
+    const int s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Seq q;
-    if (!sequence(a, s, q)) return;
-    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (i >= (int64_t)q.qn * a.heads) return;
-    const int64_t row = (int64_t)q.q0 * a.heads + i, token = row / a.heads;
+    if (!sequence(a, s, q) || (int64_t)blockIdx.x >= (int64_t)q.qn * a.heads) return;
+    const int64_t row = (int64_t)q.q0 * a.heads + blockIdx.x, token = row / a.heads;
     const int head = (int)(row - token * a.heads);
     constexpr int TR = sizeof(T) == 2 ? 64 : 32;
     const int tiles = (q.kn + TR - 1) / TR, parts = max(1, min(a.parts, (tiles + a.part_tiles - 1) / a.part_tiles));
@@ -220,31 +213,35 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
     for (int p = lane; p < parts; p += 64) m = fmaxf(m, a.part_ml[p * step + row].x);
     m = wave_max(m);
     float l = 0.f, x = 0.f, y = 0.f;
-    for (int p = 0; p < parts; ++p) {
+    const bool first = lane < a.head_dim, second = lane + 64 < a.head_dim;
+#pragma unroll 4
+    for (int p = wave; p < parts; p += 4) {
         const float2 ml = a.part_ml[p * step + row];
+        const float* o = a.part_o + (p * step + row) * a.head_dim + lane;
+        const float u = first ? o[0] : 0.f, v = second ? o[64] : 0.f;
         const float by = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-        const float* o = a.part_o + (p * step + row) * a.head_dim;
         l = fmaf(ml.y, by, l);
-        if (lane < a.head_dim) x = fmaf(o[lane], by, x);
-        if (lane + 64 < a.head_dim) y = fmaf(o[lane + 64], by, y);
+        x = fmaf(u, by, x);
+        y = fmaf(v, by, y);
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* out = (T*)a.out_w + token * a.os.row + head * a.os.head;
-    bf16* rest = (bf16*)a.rest_w + row * a.head_dim;
-    if (lane < a.head_dim) {
-        out[lane] = (T)(x * inv);
-        if (a.rest_w) rest[lane] = (bf16)(x * inv - (float)(T)(x * inv));
+    s_o[wave][lane] = x;
+    s_o[wave][lane + 64] = y;
+    if (lane == 0) s_l[wave] = l;
+    __syncthreads();
+    const int f = threadIdx.x;
+    l = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
+    if (f < a.head_dim) {
+        const float o = ((s_o[0][f] + s_o[1][f]) + (s_o[2][f] + s_o[3][f])) * (l == 0.f ? 0.f : 1.f / l);
+        const T t = (T)o;
+        ((T*)a.out_w)[token * a.os.row + head * a.os.head + f] = t;
+        if (a.rest_w) ((bf16*)a.rest_w)[row * a.head_dim + f] = (bf16)(o - (float)t);
     }
-    if (lane + 64 < a.head_dim) {
-        out[lane + 64] = (T)(y * inv);
-        if (a.rest_w) rest[lane + 64] = (bf16)(y * inv - (float)(T)(y * inv));
-    }
-    if (a.lse_w && lane == 0) a.lse_w[(int64_t)head * a.n_q + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    if (a.lse_w && f == 0) a.lse_w[(int64_t)head * a.n_q + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
 }
 
 // Smallest and largest document of every DOC_BLOCK tokens, a wavefront each; padding counts as -1.
-__global__ __launch_bounds__(256) void documents_kernel(Args a, int queries) {
-    const int s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 63, b = blockIdx.x * 4 + (threadIdx.x >> 6);
+__global__ __launch_bounds__(256) void documents_kernel(Args a) {
+    const int queries = blockIdx.z, s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 63, b = blockIdx.x * 4 + (threadIdx.x >> 6);
     Seq q;
     if (!sequence(a, s, q)) return;
     const int n = queries ? q.qn : q.kn, first = queries ? q.q0 : q.k0;
@@ -277,7 +274,7 @@ void launch_attend(const Args& a, hipStream_t st) {
     for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
         n = min(a.n_seq - s0, 32768);
         b.seq0 = s0;
-        const dim3 grid((unsigned)(((int64_t)a.max_q * a.heads + 3) / 4), (unsigned)n);
+        const dim3 grid((unsigned)((int64_t)a.max_q * a.heads), (unsigned)n);
         hipLaunchKernelGGL(join_kernel<T>, grid, dim3(256), 0, st, b);
     }
 }
@@ -318,20 +315,30 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
     }
     a.qs = d->q; a.ks = d->k; a.vs = d->v; a.os = d->out; a.gs = d->dout; a.dqs = d->dq; a.dks = d->dk; a.dvs = d->dv;
     a.n_q = d->n_q; a.n_k = d->n_k; a.n_seq = d->n_seq; a.heads = d->heads; a.kv_heads = d->kv_heads; a.head_dim = d->head_dim;
-    a.group = (int32_t)group; a.max_q = d->max_q; a.max_k = d->max_k; a.causal = d->causal;
+    a.group = (int32_t)group; a.max_q = (int32_t)min((int64_t)d->max_q, d->n_q); a.max_k = (int32_t)min((int64_t)d->max_k, d->n_k); a.causal = d->causal;
     a.scale = d->scale; a.cap = d->softcap;
     a.by_group = group > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)group + 1) : 0;
-    a.row_blocks = (int32_t)(((int64_t)d->max_q * group + FIXED - 1) / FIXED);
-    // Row blocks that do not fill the chip: their keys are shared out, 256 keys or more to a part, two workgroups a unit.
-    const int tile = d->dtype == 1 ? 64 : 32, tiles = (d->max_k + tile - 1) / tile;
-    const int64_t blocks = max((int64_t)1, (int64_t)a.n_seq * a.kv_heads * a.row_blocks);
-    const int64_t parts = min((int64_t)512 / blocks, (int64_t)tiles / (256 / tile));
-    a.part_tiles = tiles;
-    a.parts = 1;
-    if (parts > 1) {
-        a.part_tiles = (int32_t)((tiles + parts - 1) / parts);
-        a.parts = (tiles + a.part_tiles - 1) / a.part_tiles;
-    }
+    a.row_blocks = (int32_t)(((int64_t)a.max_q * group + FIXED - 1) / FIXED);
+    // Blocks that do not fill the chip, or of which the longest would be waited for: their tiles are shared out, so that there are
+    // some 2048 shares of a length, of 256 keys (rows) or more each.  What blocks and tiles there are is estimated from the tensors'
+    // rows: lengths stand on the device.
+    const int tile = d->dtype == 1 ? 64 : 32;
+    auto share = [&](int64_t blocks_a_seq, int64_t tokens, int64_t tokens_a_block, int tiles, int64_t all_tiles, int32_t& parts, int32_t& part_tiles) {
+        const int64_t blocks = a.kv_heads * min((int64_t)a.n_seq * blocks_a_seq, tokens / tokens_a_block + a.n_seq);
+        parts = 1;
+        part_tiles = tiles;
+        if (blocks >= 512 || tiles < 2 * 256 / tile) return;
+        const int64_t jobs = a.kv_heads * all_tiles * max((int64_t)1, blocks / max(1, a.n_seq * a.kv_heads));
+        part_tiles = (int32_t)min((int64_t)tiles, max((int64_t)256 / tile, jobs / 2048));
+        // (what the shares leave to be added up stays within 256 MB)
+        const int64_t most = max((int64_t)1, ((int64_t)64 << 20) / max((int64_t)1, tokens * a.kv_heads * a.head_dim));
+        part_tiles = (int32_t)max((int64_t)part_tiles, (tiles + most - 1) / most);
+        parts = (tiles + part_tiles - 1) / part_tiles;
+    };
+    const int64_t rows_a_seq = (int64_t)a.max_q * group;
+    share(a.row_blocks, d->n_q * group, FIXED, (a.max_k + tile - 1) / tile, d->n_k / tile + d->n_seq, a.parts, a.part_tiles);
+    share((a.max_k + FIXED - 1) / FIXED, d->n_k, FIXED, (int)((rows_a_seq + tile - 1) / tile), d->n_q * group / tile + d->n_seq,
+          a.key_parts, a.key_part_tiles);
     size_t off = 0;
     uint8_t* base = (uint8_t*)workspace;
     auto take = [&](size_t bytes) {
@@ -349,7 +356,14 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
     p.bytes = off;
     if (backward) {
         off = shared;
-        a.stats = (float2*)take(sizeof(float2) * rows);
+        a.row_lse = (float*)take(sizeof(float) * rows);
+        a.row_delta = (float*)take(sizeof(float) * rows);
+        if (a.parts > 1) a.part_o = (float*)take(sizeof(float) * rows * d->head_dim * a.parts);
+        if (a.key_parts > 1) {
+            const size_t part = sizeof(float) * (size_t)d->n_k * d->kv_heads * d->head_dim * a.key_parts;
+            a.part_dk = (float*)take(part);
+            a.part_dv = (float*)take(part);
+        }
         p.bytes = off > p.bytes ? off : p.bytes;
     }
     return PS_OK;
@@ -361,11 +375,9 @@ void summarise_documents(const Args& a, hipStream_t st) {
     for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
         n = min(a.n_seq - s0, 32768);
         b.seq0 = s0;
-        for (int queries = 0; queries < 2; ++queries) {
-            const int blocks = ((queries ? a.max_q : a.max_k) + DOC_BLOCK - 1) / DOC_BLOCK;
-            if (blocks > 0)
-                hipLaunchKernelGGL(documents_kernel, dim3((unsigned)((blocks + 3) / 4), (unsigned)n), dim3(256), 0, st, b, queries);
-        }
+        const int blocks = (max(a.max_q, a.max_k) + DOC_BLOCK - 1) / DOC_BLOCK;
+        if (blocks > 0)
+            hipLaunchKernelGGL(documents_kernel, dim3((unsigned)((blocks + 3) / 4), (unsigned)n, 2), dim3(256), 0, st, b);
     }
 }
 
