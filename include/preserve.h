@@ -304,7 +304,7 @@ typedef struct ps_attention_desc {
  *   q_offsets, k_offsets  [n_seq + 1] int32, non-decreasing: sequence s owns the rows from offsets[s] to offsets[s + 1]
  *   k_lengths  [n_seq] int32 or NULL: only that many of a sequence's key rows hold keys (a cache with room at its end, whose
  *              contents are not read)
- *   q_start    [n_seq] int32 or NULL: position of the first query row; NULL: keys - rows, so that the last row stands at the
+ *   q_start    [n_seq] int32 or NULL: position of the first query row, within 2^30 of 0; NULL: keys - rows, so that the last row stands at the
  *              last key (a new token over its cache; itself, in attention of a sequence to itself)
  *   prefix     [n_seq] int32 or NULL: keys below it are seen by every row, whatever `causal`
  *   q_docs, k_docs  [n_q], [n_k] int32, both or neither: documents, in any order; a negative one is padding, which sees nothing

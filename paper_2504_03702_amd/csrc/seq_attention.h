@@ -44,6 +44,7 @@ struct Args {
     int32_t row_blocks;                // blocks of FIXED rows that the grid has for every sequence
     int32_t parts, part_tiles;         // shares of a row block's key tiles, and tiles of a share
     int32_t key_parts, key_part_tiles; // shares of a key block's row tiles
+    int32_t tile, key_tile;            // rows of a tile that passes by fixed queries, by fixed keys
     uint32_t by_group;                 // 2^32 / group + 1 (group > 1)
     float scale, cap;
 };
@@ -65,7 +66,7 @@ __device__ __forceinline__ bool sequence(const Args& a, int s, Seq& r) {
     r.kn = len;
     r.start = a.q_start ? a.q_start[s] : r.kn - r.qn;
     r.prefix = a.prefix ? a.prefix[s] : 0;
-    return true;
+    return r.start >= -(1 << 30) && r.start <= 1 << 30;                   // (places and distances are 32 bits)
 }
 
 __device__ __forceinline__ unsigned over_group(const Args& a, unsigned r) { return a.group == 1 ? r : __umulhi(r, a.by_group); }
@@ -75,9 +76,13 @@ __device__ __forceinline__ int64_t doc_block0(int first_token, int s) { return f
 
 // ---- tiles in LDS: rows of DP elements (head_dim and zeros), 16-byte chunks swizzled so that 16 rows' equal chunks, and the
 // transposing reads, fall into different banks -------------------------------------------------------------------------------
-template <typename T, int DP>
+constexpr int tile_rows(int eb) { return eb == 2 ? 64 : 32; }
+// Rows of a tile that passes by fixed keys: for heads of 128 half as many, which leaves room for a workgroup's values (below).
+constexpr int key_tile_rows(int eb, int dp) { return eb == 2 && dp == 64 ? 64 : 32; }
+
+template <typename T, int DP, int R = tile_rows(sizeof(T))>
 struct Tile {
-    static constexpr int EB = sizeof(T), ROWB = DP * EB, ROWS = EB == 2 ? 64 : 32, BLOCKS = ROWS / 32, BYTES = ROWS * ROWB;
+    static constexpr int EB = sizeof(T), ROWB = DP * EB, ROWS = R, BLOCKS = ROWS / 32, BYTES = ROWS * ROWB;
     static constexpr int CPR = ROWB / 16, PER_THREAD = BYTES / 16 / 256, EPC = 16 / EB, NF = ROWB / 32, NA = DP / 32;
     static __device__ __forceinline__ int swz(int r) {
         if (EB == 4) return ((r >> 2) & 1) << 3 | (r & 3) << 1 | ((r >> 3) & 1);
@@ -91,6 +96,7 @@ struct Tile {
 template <typename T, int DP>
 struct Fixed {
     uint4 c[Tile<T, DP>::NF];
+    __device__ __forceinline__ const uint4& operator[](int i) const { return c[i]; }
     // This half-wavefront's share of the product with another row that is laid out the same.
     __device__ __forceinline__ float share(const Fixed& o) const {
         float sum = 0.f;
@@ -132,23 +138,35 @@ struct Lanes {
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 u) { return __builtin_bit_cast(bf16x8, u); }
 
-// 32 passing rows (block b of the tile) times the fixed rows.
+// Fixed rows in LDS instead, the wavefront's own 32 of them: where registers are short.
 template <typename T, int DP>
-__device__ __forceinline__ f32x16 dot(const unsigned char* tile, int b, const Fixed<T, DP>& f, const Lanes<T, DP>& l) {
+struct FixedInLds {
+    const unsigned char* rows;
+    int at;
+    __device__ __forceinline__ FixedInLds(unsigned char* to, const Fixed<T, DP>& f, const Lanes<T, DP>& l) : rows(to), at(l.row) {
+#pragma unroll
+        for (int i = 0; i < Tile<T, DP>::NF; ++i) *(uint4*)(to + (at ^ (i << 5))) = f.c[i];
+    }
+    __device__ __forceinline__ uint4 operator[](int i) const { return *(const uint4*)(rows + (at ^ (i << 5))); }
+};
+
+// 32 passing rows (block b of the tile) times the fixed rows.
+template <typename T, int DP, typename F>
+__device__ __forceinline__ f32x16 dot(const unsigned char* tile, int b, const F& f, const Lanes<T, DP>& l) {
     using L = Tile<T, DP>;
     f32x16 s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
     for (int i = 0; i < L::NF; ++i) {
-        const uint4 a = *(const uint4*)(tile + b * 32 * L::ROWB + (l.row ^ (i << 5)));
+        const uint4 a = *(const uint4*)(tile + b * 32 * L::ROWB + (l.row ^ (i << 5))), c = f[i];
         if constexpr (L::EB == 2) {
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(f.c[i]), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(c), s, 0, 0, 0);
         } else {
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(f.c[i].x), s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(f.c[i].y), s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(f.c[i].z), s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(f.c[i].w), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(c.x), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(c.y), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(c.z), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(c.w), s, 0, 0, 0);
         }
     }
     return s;
@@ -201,9 +219,9 @@ static __device__ const uint4 zeros = {0, 0, 0, 0};
 
 // Sends for a tile: 16 bytes a lane go from memory into LDS without a register (a lane picks the chunk whose swizzled place it
 // fills).  row(i): address of passing row i's element 0; null for a row of zeros.  Landed after vm_wait() and a barrier.
-template <typename T, int DP, typename Row>
+template <typename T, int DP, int R = tile_rows(sizeof(T)), typename Row>
 __device__ __forceinline__ void send_tile(unsigned char* tile, int head_dim, Row row) {
-    using L = Tile<T, DP>;
+    using L = Tile<T, DP, R>;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
 #pragma unroll
     for (int j = 0; j < L::PER_THREAD; ++j) {

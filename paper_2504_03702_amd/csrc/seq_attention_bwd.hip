@@ -9,12 +9,13 @@ typedef __bf16 bf16;
 
 namespace {
 
-// The weights p and the gradients d of x = scale q . k of one block, from the products s = q . k and g = dout . v.  row(e): what
-// element e's query brings along, distance(e): how far it stands from the key, seen(e): whether it sees it.  Everything that is
-// the same for all elements is asked outside their loops, so that these are straight lines.
-template <typename T, typename Row, typename Distance, typename Seen>
-__device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, float (&p)[16], float (&d)[16], bool whole, Row row,
-                                          Distance distance, Seen seen) {
+// The weights p and the gradients d of x = scale q . k of one block, from the products s = q . k and g = dout . v, for the four
+// neighbours of every j: lse(j) and delta(j), what their queries bring along; distance(j), how far they stand from their keys, times the
+// slope; seen(j, is), which see them.  Everything that is the same for all elements is asked outside their loops, so that these are
+// straight lines.
+template <typename T, typename Lse, typename Delta, typename Distance, typename Seen>
+__device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, float (&p)[16], float (&d)[16], bool whole, Lse lse,
+                                          Delta delta, Distance distance, Seen seen) {
     const float c1 = a.scale * LOG2E;
     if (a.cap > 0.f) {
         const float inner = a.scale / a.cap, outer = a.cap * LOG2E;
@@ -30,29 +31,55 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
     }
     if (a.slopes) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) p[e] -= distance(e);
+        for (int j = 0; j < 4; ++j) {
+            const float4 off = distance(j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[4 * j + i] -= (&off.x)[i];
+        }
     }
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const float2 r = row(e);
-        p[e] = __builtin_amdgcn_exp2f(p[e] - r.x);
-        const float w = p[e] * (g[e] - r.y);
-        d[e] = a.cap > 0.f ? d[e] * w : w;
+    for (int j = 0; j < 4; ++j) {
+        const float4 l = lse(j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_amdgcn_exp2f(p[4 * j + i] - (&l.x)[i]);
+    }
+    if (a.cap > 0.f) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float4 t = delta(j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[4 * j + i] *= p[4 * j + i] * (g[4 * j + i] - (&t.x)[i]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float4 t = delta(j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[4 * j + i] = p[4 * j + i] * (g[4 * j + i] - (&t.x)[i]);
+        }
     }
     if (!whole) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const bool is = seen(e);
-            p[e] = is ? p[e] : 0.f;
-            d[e] = is ? d[e] : 0.f;
+        for (int j = 0; j < 4; ++j) {
+            bool is[4];
+            seen(j, is);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[4 * j + i] = is[i] ? p[4 * j + i] : 0.f;
+                d[4 * j + i] = is[i] ? d[4 * j + i] : 0.f;
+            }
         }
     }
 }
 
 // Keys fixed: dk and dv of FIXED keys of a key head, from the rows of all its heads.
 template <typename T, int DP>
-__global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void key_gradients_kernel(Args a) {
-    using L = Tile<T, DP>;
+__global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_gradients_kernel(Args a) {
+    using L = Tile<T, DP, key_tile_rows(sizeof(T), DP)>;
+    // Two workgroups a unit need 256 registers a lane.  In bf16 the gradients of 32 keys by 128 features take half of them, so the values
+    // wait in LDS (a quarter more reads there).
+    constexpr bool IN_LDS = sizeof(T) == 2 && DP == 128;
+    __shared__ __align__(1024) unsigned char s_values[IN_LDS ? 4 : 1][IN_LDS ? 32 * L::ROWB : 16];
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][queries, dout]
     __shared__ __align__(16) float s_lse[2][L::ROWS], s_delta[2][L::ROWS], s_slope[2][L::ROWS];
     __shared__ __align__(16) int s_place[2][L::ROWS], s_doc[2][L::ROWS];
@@ -79,11 +106,19 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void key_gradients_kernel(Ar
     const int64_t token = q.k0 + min(key, q.kn - 1);
     const int doc = a.k_docs ? a.k_docs[token] : 0;
     const bool there = live && doc >= 0;
-    Fixed<T, DP> kf, vf;
-    kf.load((const T*)a.k + token * a.ks.row + hk * a.ks.head, there, a.head_dim, half);
-    vf.load((const T*)a.v + token * a.vs.row + hk * a.vs.head, there, a.head_dim, half);
     const Lanes<T, DP> lanes(lane);
+    Fixed<T, DP> kf, v;
+    kf.load((const T*)a.k + token * a.ks.row + hk * a.ks.head, there, a.head_dim, half);
+    v.load((const T*)a.v + token * a.vs.row + hk * a.vs.head, there, a.head_dim, half);
+    auto keep = [&] {
+        if constexpr (IN_LDS)
+            return FixedInLds<T, DP>(s_values[wave], v, lanes);
+        else
+            return v;
+    };
+    const auto vf = keep();
 
+    const bool always = !a.causal || key < q.prefix;                      // (seen from every place)
     const int last = min(k0 + FIXED, q.kn) - 1, wlast = min(wk0 + 31, q.kn - 1);
     int dmin = 0, dmax = 0;
     if (a.k_docs) {
@@ -137,12 +172,12 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void key_gradients_kernel(Ar
             if (a.slopes) s_slope[buf][threadIdx.x] = is ? a.slopes[head] * LOG2E : 0.f;
             if (a.q_docs) s_doc[buf][threadIdx.x] = is ? a.q_docs[tok] : -1;
         }
-        send_tile<T, DP>(smem[buf][0], a.head_dim, [&](int i) {
+        send_tile<T, DP, L::ROWS>(smem[buf][0], a.head_dim, [&](int i) {
             int64_t tok;
             int head;
             return find(i, tok, head) ? (const T*)a.q + tok * a.qs.row + head * a.qs.head : nullptr;
         });
-        send_tile<T, DP>(smem[buf][1], a.head_dim, [&](int i) {
+        send_tile<T, DP, L::ROWS>(smem[buf][1], a.head_dim, [&](int i) {
             int64_t tok;
             int head;
             return find(i, tok, head) ? (const T*)a.dout + tok * a.gs.row + head * a.gs.head : nullptr;
@@ -170,20 +205,20 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void key_gradients_kernel(Ar
             for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
                 const f32x16 sc = dot<T, DP>(smem[buf][0], b, kf, lanes), g = dot<T, DP>(smem[buf][1], b, vf, lanes);
                 float p[16], d[16];
-                float4 lse[4], delta[4];
+                auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
+                gradients<T>(a, sc, g, p, d, whole, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
+                             [&](int j) { return *(const float4*)&s_delta[buf][at(j)]; },
+                             [&](int j) {
+                                 const float4 by = *(const float4*)&s_slope[buf][at(j)];
+                                 const int4 place = *(const int4*)&s_place[buf][at(j)];
+                                 return make_float4(by.x * fabsf((float)(place.x - key)), by.y * fabsf((float)(place.y - key)),
+                                                    by.z * fabsf((float)(place.z - key)), by.w * fabsf((float)(place.w - key)));
+                             },
+                             [&](int j, bool(&is)[4]) {
+                                 const int4 place = *(const int4*)&s_place[buf][at(j)];
+                                 const int4 of = a.q_docs ? *(const int4*)&s_doc[buf][at(j)] : make_int4(0, 0, 0, 0);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    lse[j] = *(const float4*)&s_lse[buf][32 * b + 8 * j + 4 * half];
-                    delta[j] = *(const float4*)&s_delta[buf][32 * b + 8 * j + 4 * half];
-                }
-                auto at = [&](int e) { return 32 * b + row_of(e) + 4 * half; };
-                gradients<T>(a, sc, g, p, d, whole,
-                             [&](int e) { return make_float2((&lse[e >> 2].x)[e & 3], (&delta[e >> 2].x)[e & 3]); },
-                             [&](int e) { return s_slope[buf][at(e)] * fabsf((float)(s_place[buf][at(e)] - key)); },
-                             [&](int e) {
-                                 bool is = !a.causal || key <= s_place[buf][at(e)] || key < q.prefix;
-                                 if (a.q_docs) is = is && s_doc[buf][at(e)] == doc && there;
-                                 return is;
+                                 for (int i = 0; i < 4; ++i) is[i] = ((key <= (&place.x)[i]) | always) & ((&of.x)[i] == doc) & there;
                              });
                 weigh<T, DP>(smem[buf][1], b, p, dv, lanes);
                 weigh<T, DP>(smem[buf][0], b, d, dk, lanes);
@@ -208,7 +243,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void key_gradients_kernel(Ar
 
 // Queries fixed: dq of FIXED rows of a key head's queries.
 template <typename T, int DP>
-__global__ __launch_bounds__(256, 2) void query_gradients_kernel(Args a) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void query_gradients_kernel(Args a) {
     using L = Tile<T, DP>;
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][keys, values]
     __shared__ __align__(16) int s_doc[2][64];
@@ -244,24 +279,27 @@ __global__ __launch_bounds__(256, 2) void query_gradients_kernel(Args a) {
     gf.load((const T*)a.dout + token * a.gs.row + head * a.gs.head, there, a.head_dim, half);
     const Lanes<T, DP> lanes(lane);
     // what the row brings along, for this launch and the keys'
-    float2 st;
+    float lse, delta;
     {
         Fixed<T, DP> of;
         of.load((const T*)a.out + token * a.os.row + head * a.os.head, there, a.head_dim, half);
-        float delta = gf.share(of);
+        delta = gf.share(of);
         if (sizeof(T) == 2 && a.rest) {
             of.load((const T*)a.rest + (token * a.heads + head) * a.head_dim, there, a.head_dim, half);
             delta += gf.share(of);
         }
         const int64_t at = (int64_t)head * a.n_q + token;
-        const float lse = there ? a.lse[at] : -INFINITY;
-        st = make_float2(lse == -INFINITY ? INFINITY : lse * LOG2E, delta + __shfl_xor(delta, 32, 64));
+        const float mine = there ? a.lse[at] : -INFINITY;
+        lse = mine == -INFINITY ? INFINITY : mine * LOG2E;
+        delta += __shfl_xor(delta, 32, 64);
         if (live && half == 0 && part == 0) {
-            a.row_lse[at] = st.x;
-            a.row_delta[at] = st.y;
+            a.row_lse[at] = lse;
+            a.row_delta[at] = delta;
         }
     }
 
+    // keys in front of `end` are seen, if their documents are
+    const int end = a.causal ? min(q.kn, max(place + 1, q.prefix)) : q.kn;
     const int last = min(r0 + FIXED, rows) - 1;
     const int far = q.start + (int)over_group(a, last);
     const int wfar = q.start + (int)over_group(a, min(wr0 + 31, rows - 1)), wnear = q.start + (int)over_group(a, min(wr0, rows - 1));
@@ -330,14 +368,18 @@ __global__ __launch_bounds__(256, 2) void query_gradients_kernel(Args a) {
             for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
                 const f32x16 sc = dot<T, DP>(smem[buf][0], b, qf, lanes), g = dot<T, DP>(smem[buf][1], b, gf, lanes);
                 float p[16], d[16];
-                auto at = [&](int e) { return 32 * b + row_of(e) + 4 * half; };
-                gradients<T>(a, sc, g, p, d, whole, [&](int) { return st; },
-                             [&](int e) { return slope * fabsf((float)(place - k0 - at(e))); },
-                             [&](int e) {
-                                 const int key = k0 + at(e);
-                                 bool is = key < q.kn && (!a.causal || key <= place || key < q.prefix);
-                                 if (a.k_docs) is = is && s_doc[buf][at(e)] == doc && there;
-                                 return is;
+                auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
+                gradients<T>(a, sc, g, p, d, whole, [&](int) { return make_float4(lse, lse, lse, lse); },
+                             [&](int) { return make_float4(delta, delta, delta, delta); },
+                             [&](int j) {
+                                 const int from = place - k0 - at(j);
+                                 return make_float4(slope * fabsf((float)from), slope * fabsf((float)(from - 1)),
+                                                    slope * fabsf((float)(from - 2)), slope * fabsf((float)(from - 3)));
+                             },
+                             [&](int j, bool(&is)[4]) {
+                                 const int4 of = a.k_docs ? *(const int4*)&s_doc[buf][at(j)] : make_int4(0, 0, 0, 0);
+#pragma unroll
+                                 for (int i = 0; i < 4; ++i) is[i] = (k0 + at(j) + i < end) & ((&of.x)[i] == doc) & there;
                              });
                 weigh<T, DP>(smem[buf][0], b, d, dq, lanes);
                 if (sizeof(T) == 2 && !whole) {
@@ -367,8 +409,8 @@ __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
     const float* part = z == 0 ? a.part_o : z == 1 ? a.part_dk : a.part_dv;
     T* out = (T*)(z == 0 ? a.dq : z == 1 ? a.dk : a.dv);
     const float by = z == 2 ? 1.f : a.scale;
-    constexpr int TR = sizeof(T) == 2 ? 64 : 32;
-    const int passing = z == 0 ? q.kn : q.qn * a.group, parts = max(1, min(of, ((passing + TR - 1) / TR + each - 1) / each));
+    const int tile = z == 0 ? a.tile : a.key_tile, tiles = ((z == 0 ? q.kn : q.qn * a.group) + tile - 1) / tile;
+    const int parts = max(1, min(of, (tiles + each - 1) / each));
     const int64_t n = (int64_t)(z == 0 ? q.qn : q.kn) * heads * a.head_dim, first = (int64_t)(z == 0 ? q.q0 : q.k0) * heads * a.head_dim;
     const int64_t step = all * heads * a.head_dim;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {

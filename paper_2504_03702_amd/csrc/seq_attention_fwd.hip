@@ -50,7 +50,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     qf.load((const T*)a.q + token * a.qs.row + head * a.qs.head, live, a.head_dim, half);
     const Lanes<T, DP> lanes(lane);
 
-    // what the workgroup's and the wavefront's rows see
+    // what the workgroup's and the wavefront's rows see; keys in front of `end` this one, if their documents are
+    const int end = doc < 0 ? 0 : a.causal ? min(q.kn, max(place + 1, q.prefix)) : q.kn;
     const int last = min(r0 + FIXED, rows) - 1;
     const int far = q.start + (int)over_group(a, last);                   // largest place
     const int wfar = q.start + (int)over_group(a, min(wr0 + 31, rows - 1)), wnear = q.start + (int)over_group(a, min(wr0, rows - 1));
@@ -144,10 +145,18 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
                 for (int b = 0; b < L::BLOCKS; ++b)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const int i = 32 * b + row_of(e) + 4 * half, key = k0 + i;
-                        bool seen = key < q.kn && (!a.causal || key <= place || key < q.prefix);
-                        if (a.k_docs) seen = seen && s_doc[buf][i] == doc && doc >= 0;
-                        if (!seen) sc[b][e] = -INFINITY;
+                        if (k0 + 32 * b + row_of(e) + 4 * half >= end) sc[b][e] = -INFINITY;
+                    }
+            }
+            if (!whole && a.k_docs) {
+#pragma unroll
+                for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int4 of = *(const int4*)&s_doc[buf][32 * b + 8 * j + 4 * half];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if ((&of.x)[i] != doc) sc[b][4 * j + i] = -INFINITY;
                     }
             }
             float mx = sc[0][0];
@@ -206,8 +215,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
     if (!sequence(a, s, q) || (int64_t)blockIdx.x >= (int64_t)q.qn * a.heads) return;
     const int64_t row = (int64_t)q.q0 * a.heads + blockIdx.x, token = row / a.heads;
     const int head = (int)(row - token * a.heads);
-    constexpr int TR = sizeof(T) == 2 ? 64 : 32;
-    const int tiles = (q.kn + TR - 1) / TR, parts = max(1, min(a.parts, (tiles + a.part_tiles - 1) / a.part_tiles));
+    const int tiles = (q.kn + a.tile - 1) / a.tile, parts = max(1, min(a.parts, (tiles + a.part_tiles - 1) / a.part_tiles));
     const int64_t step = a.n_q * a.heads;
     float m = -INFINITY;
     for (int p = lane; p < parts; p += 64) m = fmaxf(m, a.part_ml[p * step + row].x);
@@ -322,8 +330,12 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
     // Blocks that do not fill the chip, or of which the longest would be waited for: their tiles are shared out, so that there are
     // some 2048 shares of a length, of 256 keys (rows) or more each.  What blocks and tiles there are is estimated from the tensors'
     // rows: lengths stand on the device.
-    const int tile = d->dtype == 1 ? 64 : 32;
-    auto share = [&](int64_t blocks_a_seq, int64_t tokens, int64_t tokens_a_block, int tiles, int64_t all_tiles, int32_t& parts, int32_t& part_tiles) {
+    a.tile = tile_rows(d->dtype == 1 ? 2 : 4);
+    a.key_tile = key_tile_rows(d->dtype == 1 ? 2 : 4, d->head_dim <= 64 ? 64 : 128);
+    auto share = [&](int64_t blocks_a_seq, int64_t tokens, int64_t tokens_a_block, int64_t passing, int64_t all_passing, int tile, int32_t& parts,
+                     int32_t& part_tiles) {
+        const int tiles = (int)((passing + tile - 1) / tile);
+        const int64_t all_tiles = all_passing / tile + a.n_seq;
         const int64_t blocks = a.kv_heads * min((int64_t)a.n_seq * blocks_a_seq, tokens / tokens_a_block + a.n_seq);
         parts = 1;
         part_tiles = tiles;
@@ -336,9 +348,8 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
         parts = (tiles + part_tiles - 1) / part_tiles;
     };
     const int64_t rows_a_seq = (int64_t)a.max_q * group;
-    share(a.row_blocks, d->n_q * group, FIXED, (a.max_k + tile - 1) / tile, d->n_k / tile + d->n_seq, a.parts, a.part_tiles);
-    share((a.max_k + FIXED - 1) / FIXED, d->n_k, FIXED, (int)((rows_a_seq + tile - 1) / tile), d->n_q * group / tile + d->n_seq,
-          a.key_parts, a.key_part_tiles);
+    share(a.row_blocks, d->n_q * group, FIXED, a.max_k, d->n_k, a.tile, a.parts, a.part_tiles);
+    share((a.max_k + FIXED - 1) / FIXED, d->n_k, FIXED, rows_a_seq, d->n_q * group, a.key_tile, a.key_parts, a.key_part_tiles);
     size_t off = 0;
     uint8_t* base = (uint8_t*)workspace;
     auto take = [&](size_t bytes) {
