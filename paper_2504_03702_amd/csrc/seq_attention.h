@@ -216,22 +216,49 @@ __device__ __forceinline__ void weigh(const unsigned char* tile, int b, const fl
 }
 
 static __device__ const uint4 zeros = {0, 0, 0, 0};
+static __device__ const uint32_t infinity_word = 0x7f800000u, minus_one = 0xffffffffu;
 
-// Sends for a tile: 16 bytes a lane go from memory into LDS without a register (a lane picks the chunk whose swizzled place it
-// fills).  row(i): address of passing row i's element 0; null for a row of zeros.  Landed after vm_wait() and a barrier.
-template <typename T, int DP, int R = tile_rows(sizeof(T)), typename Row>
-__device__ __forceinline__ void send_tile(unsigned char* tile, int head_dim, Row row) {
+// Sends for tiles: 16 bytes a lane go from memory into LDS without a register (a lane picks the chunk whose swizzled place it
+// fills).  Landed after vm_wait() and a barrier.  Chunks behind a head's elements repeat its last one: they meet zeros in the fixed
+// rows, or make features that nobody stores.
+template <typename T, int DP, int R = tile_rows(sizeof(T))>
+struct Sender {
     using L = Tile<T, DP, R>;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-#pragma unroll
-    for (int j = 0; j < L::PER_THREAD; ++j) {
-        const int place = (j * 4 + wave) * 64 + lane, r = place / L::CPR, e = ((place % L::CPR) ^ L::swz(r)) * L::EPC;
-        const T* p = row(r);
-        const void* from = p && (head_dim == DP || e < head_dim) ? (const void*)(p + e) : (const void*)&zeros;
+    unsigned off[L::PER_THREAD];       // where a lane's chunks lie from the tile's first element on, in bytes
+    bool regular;                      // the same in every tile
+    static __device__ __forceinline__ int row_of(int j) { return ((j * 4 + (int)(threadIdx.x >> 6)) * 64 + (int)(threadIdx.x & 63)) / L::CPR; }
+    static __device__ __forceinline__ int element(int j, int head_dim) {
+        const int r = row_of(j);
+        return min((((int)threadIdx.x % L::CPR) ^ L::swz(r)) * L::EPC, head_dim - L::EPC);
+    }
+    static __device__ __forceinline__ void send(unsigned char* tile, int j, const void* from) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                          (SEQATT_LDS void*)(tile + (j * 4 + wave) * 1024), 16, 0, 0);
     }
-}
+    // rows of `group` heads to a token
+    __device__ __forceinline__ Sender(const ps_strides& s, int group, int head_dim) {
+        regular = R % group == 0 && s.row < 1 << 20 && s.head < 1 << 20;
+#pragma unroll
+        for (int j = 0; j < L::PER_THREAD; ++j) {
+            const int r = row_of(j), token = r / group;
+            off[j] = regular ? (unsigned)(token * (int)s.row + (r - token * group) * (int)s.head + element(j, head_dim)) * L::EB : 0u;
+        }
+    }
+    __device__ __forceinline__ void whole(unsigned char* tile, const T* first) const {
+#pragma unroll
+        for (int j = 0; j < L::PER_THREAD; ++j) send(tile, j, (const char*)first + off[j]);
+    }
+    // row(i): address of passing row i's element 0; null for a row of zeros.
+    template <typename Row>
+    __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, Row row) const {
+#pragma unroll
+        for (int j = 0; j < L::PER_THREAD; ++j) {
+            const T* p = row(row_of(j));
+            send(tile, j, p ? (const void*)(p + element(j, head_dim)) : (const void*)&zeros);
+        }
+    }
+};
 // The same for a word a lane of this wavefront.
 __device__ __forceinline__ void send_words(void* to, const void* from) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)to, 4, 0, 0);
@@ -267,13 +294,28 @@ struct Walk {
 };
 
 // ---- scores ------------------------------------------------------------------------------------------------------------------
-// tanh for the cap.  bf16 calls: the exponential's 1 - 2 / (1 + e^2u), whose absolute error of 1e-7 is that of a score near the cap;
-// fp32 calls take the library's, good to the last places everywhere.
-template <typename T>
-__device__ __forceinline__ float bend(float u) {
-    if constexpr (sizeof(T) == 4) return tanhf(u);
-    return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * (2.f * LOG2E)));
-}
+// The cap.  bf16 calls take tanh u = 1 - 2 r, r = 1 / (1 + e^2u), whose absolute error of 1e-7 is that of a score near the cap; r is
+// what they go on with.  fp32 calls take the library's, good to the last places everywhere.
+struct Cap {
+    float inner, outer;                // what the product is multiplied by on the way in, and tanh on the way out (powers of two)
+    template <typename T>
+    static __device__ __forceinline__ Cap of(const Args& a) {
+        return {a.cap > 0.f ? a.scale / a.cap * (sizeof(T) == 4 ? 1.f : 2.f * LOG2E) : 0.f, a.cap * LOG2E};
+    }
+    template <typename T>
+    __device__ __forceinline__ float bent(float s) const {                // r, or tanh
+        if constexpr (sizeof(T) == 4) return tanhf(s * inner);
+        return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * inner));
+    }
+    template <typename T>
+    __device__ __forceinline__ float score(float b, float less) const {   // in powers of two, less something
+        return sizeof(T) == 4 ? fmaf(b, outer, -less) : fmaf(b, -2.f * outer, outer - less);
+    }
+    template <typename T>
+    static __device__ __forceinline__ float slope(float b) {              // 1 - tanh^2, in bf16 a quarter of it
+        return sizeof(T) == 4 ? fmaf(-b, b, 1.f) : fmaf(-b, b, b);
+    }
+};
 
 // Row of accumulator element e.
 __device__ __forceinline__ constexpr int row_of(int e) { return 8 * (e >> 2) + (e & 3); }   // + 4 half

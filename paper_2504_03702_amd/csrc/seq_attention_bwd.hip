@@ -9,48 +9,58 @@ typedef __bf16 bf16;
 
 namespace {
 
-// The weights p and the gradients d of x = scale q . k of one block, from the products s = q . k and g = dout . v, for the four
+// The weights p and the gradients d of x = scale q . k (by_x() times d) of one block, from the products s = q . k and g = dout . v, for the four
 // neighbours of every j: lse(j) and delta(j), what their queries bring along; distance(j), how far they stand from their keys, times the
 // slope; seen(j, is), which see them.  Everything that is the same for all elements is asked outside their loops, so that these are
 // straight lines.
 template <typename T, typename Lse, typename Delta, typename Distance, typename Seen>
 __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, float (&p)[16], float (&d)[16], bool whole, Lse lse,
                                           Delta delta, Distance distance, Seen seen) {
-    const float c1 = a.scale * LOG2E;
     if (a.cap > 0.f) {
-        const float inner = a.scale / a.cap, outer = a.cap * LOG2E;
+        const Cap cap = Cap::of<T>(a);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float u = bend<T>(s[e] * inner);
-            p[e] = u * outer;
-            d[e] = fmaf(-u, u, 1.f);
+        for (int e = 0; e < 16; ++e) d[e] = cap.bent<T>(s[e]);
+        if (a.slopes) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 l = lse(j), off = distance(j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_amdgcn_exp2f(cap.score<T>(d[4 * j + i], (&l.x)[i] + (&off.x)[i]));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 l = lse(j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_amdgcn_exp2f(cap.score<T>(d[4 * j + i], (&l.x)[i]));
+            }
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) p[e] = s[e] * c1;
-    }
-    if (a.slopes) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float4 off = distance(j);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[4 * j + i] -= (&off.x)[i];
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float4 l = lse(j);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_amdgcn_exp2f(p[4 * j + i] - (&l.x)[i]);
-    }
-    if (a.cap > 0.f) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float4 t = delta(j);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) d[4 * j + i] *= p[4 * j + i] * (g[4 * j + i] - (&t.x)[i]);
+            for (int i = 0; i < 4; ++i) {
+                const int e = 4 * j + i;
+                d[e] = Cap::slope<T>(d[e]) * (p[e] * (g[e] - (&t.x)[i]));
+            }
         }
     } else {
+        const float c1 = a.scale * LOG2E;
+        if (a.slopes) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 l = lse(j), off = distance(j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * j + i], c1, -((&l.x)[i] + (&off.x)[i])));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 l = lse(j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * j + i], c1, -(&l.x)[i]));
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float4 t = delta(j);
@@ -72,6 +82,9 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
     }
 }
 
+template <typename T>
+__device__ __forceinline__ float by_x(const Args& a) { return a.cap > 0.f && sizeof(T) == 2 ? 4.f * a.scale : a.scale; }
+
 // Keys fixed: dk and dv of FIXED keys of a key head, from the rows of all its heads.
 template <typename T, int DP>
 __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_gradients_kernel(Args a) {
@@ -81,8 +94,8 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     constexpr bool IN_LDS = sizeof(T) == 2 && DP == 128;
     __shared__ __align__(1024) unsigned char s_values[IN_LDS ? 4 : 1][IN_LDS ? 32 * L::ROWB : 16];
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][queries, dout]
-    __shared__ __align__(16) float s_lse[2][L::ROWS], s_delta[2][L::ROWS], s_slope[2][L::ROWS];
-    __shared__ __align__(16) int s_place[2][L::ROWS], s_doc[2][L::ROWS];
+    __shared__ __align__(16) float s_lse[2][64], s_delta[2][64], s_slope[2][64];
+    __shared__ __align__(16) int s_place[2][64], s_doc[2][64];
 
     const int key_blocks = (a.max_k + FIXED - 1) / FIXED;
     unsigned id = blockIdx.x;
@@ -150,38 +163,33 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         return some;
     };
 
+    const Sender<T, DP, L::ROWS> queries(a.qs, a.group, a.head_dim), gradients_out(a.gs, a.group, a.head_dim);
+    const bool regular = queries.regular && gradients_out.regular;
+    const T *qbase = (const T*)a.q + q.q0 * a.qs.row + (int64_t)hk * a.group * a.qs.head, *gbase = (const T*)a.dout + q.q0 * a.gs.row + (int64_t)hk * a.group * a.gs.head;
     auto request = [&](int t, bool padded, int buf) {
         const int r0 = t * L::ROWS;
-        // a row's token and head; padding and rows past the end are zeros that see nothing
-        auto find = [&](int i, int64_t& tok, int& head) {
-            const int r = r0 + i;
-            if (r >= rows) return false;
-            const int qi = (int)over_group(a, r);
-            head = hk * a.group + r - qi * a.group;
-            tok = q.q0 + qi;
-            return !padded || a.q_docs[tok] >= 0;
-        };
-        if (threadIdx.x < L::ROWS) {
-            int64_t tok;
-            int head;
-            const bool is = find(threadIdx.x, tok, head);
-            const int64_t at = head * a.n_q + tok;
-            s_lse[buf][threadIdx.x] = is ? a.row_lse[at] : INFINITY;
-            s_delta[buf][threadIdx.x] = is ? a.row_delta[at] : 0.f;
-            s_place[buf][threadIdx.x] = is ? q.start + (int)(tok - q.q0) : 0;
-            if (a.slopes) s_slope[buf][threadIdx.x] = is ? a.slopes[head] * LOG2E : 0.f;
-            if (a.q_docs) s_doc[buf][threadIdx.x] = is ? a.q_docs[tok] : -1;
+        if (r0 + L::ROWS <= rows && !padded && regular) {
+            const int first = (int)over_group(a, r0);
+            queries.whole(smem[buf][0], qbase + first * a.qs.row);
+            gradients_out.whole(smem[buf][1], gbase + first * a.gs.row);
+        } else {
+            // (padding and rows past the end are zeros)
+            auto row = [&](const T* base, const ps_strides& st, int i) -> const T* {
+                const int qi = (int)over_group(a, min(r0 + i, rows - 1)), head = r0 + i - qi * a.group;
+                return r0 + i < rows && (!padded || a.q_docs[q.q0 + qi] >= 0) ? base + qi * st.row + head * st.head : nullptr;
+            };
+            queries.rows(smem[buf][0], a.head_dim, [&](int i) { return row(qbase, a.qs, i); });
+            gradients_out.rows(smem[buf][1], a.head_dim, [&](int i) { return row(gbase, a.gs, i); });
         }
-        send_tile<T, DP, L::ROWS>(smem[buf][0], a.head_dim, [&](int i) {
-            int64_t tok;
-            int head;
-            return find(i, tok, head) ? (const T*)a.q + tok * a.qs.row + head * a.qs.head : nullptr;
-        });
-        send_tile<T, DP, L::ROWS>(smem[buf][1], a.head_dim, [&](int i) {
-            int64_t tok;
-            int head;
-            return find(i, tok, head) ? (const T*)a.dout + tok * a.gs.row + head * a.gs.head : nullptr;
-        });
+        // what the rows bring along, a wavefront for each of its words (rows past the end see nothing)
+        const int r = r0 + lane, qi = (int)over_group(a, min(r, rows - 1)), head = hk * a.group + min(r, rows - 1) - qi * a.group;
+        const int64_t at = head * a.n_q + q.q0 + qi;
+        const bool is = r < rows;
+        if (wave == 0) send_words(s_lse[buf], is ? (const void*)(a.row_lse + at) : (const void*)&infinity_word);
+        if (wave == 1) send_words(s_delta[buf], is ? (const void*)(a.row_delta + at) : (const void*)&zeros);
+        if (wave == 2 && a.slopes) send_words(s_slope[buf], a.slopes + head);
+        if (wave == 3 && a.q_docs) send_words(s_doc[buf], is ? (const void*)(a.q_docs + q.q0 + qi) : (const void*)&minus_one);
+        if (wave == 0 && lane < L::ROWS) s_place[buf][lane] = q.start + qi;
     };
 
     f32x16 dk[L::NA], dv[L::NA];
@@ -211,8 +219,8 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
                              [&](int j) {
                                  const float4 by = *(const float4*)&s_slope[buf][at(j)];
                                  const int4 place = *(const int4*)&s_place[buf][at(j)];
-                                 return make_float4(by.x * fabsf((float)(place.x - key)), by.y * fabsf((float)(place.y - key)),
-                                                    by.z * fabsf((float)(place.z - key)), by.w * fabsf((float)(place.w - key)));
+                                 return make_float4(by.x * LOG2E * fabsf((float)(place.x - key)), by.y * LOG2E * fabsf((float)(place.y - key)),
+                                                    by.z * LOG2E * fabsf((float)(place.z - key)), by.w * LOG2E * fabsf((float)(place.w - key)));
                              },
                              [&](int j, bool(&is)[4]) {
                                  const int4 place = *(const int4*)&s_place[buf][at(j)];
@@ -237,7 +245,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         put_row<float, DP>(a.part_dv + row * a.head_dim, dv, 1.f, a.head_dim, half);
         return;
     }
-    put_row<T, DP>((T*)a.dk + token * a.dks.row + hk * a.dks.head, dk, a.scale, a.head_dim, half);
+    put_row<T, DP>((T*)a.dk + token * a.dks.row + hk * a.dks.head, dk, by_x<T>(a), a.head_dim, half);
     put_row<T, DP>((T*)a.dv + token * a.dvs.row + hk * a.dvs.head, dv, 1.f, a.head_dim, half);
 }
 
@@ -334,15 +342,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void quer
 
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
+    const Sender<T, DP> keys(a.ks, 1, a.head_dim), values(a.vs, 1, a.head_dim);
+    const bool regular = keys.regular && values.regular;
     auto request = [&](int t, bool padded, int buf) {
         const int k0 = t * L::ROWS;
         auto is = [&](int i) { return k0 + i < q.kn && (!padded || a.k_docs[q.k0 + k0 + i] >= 0); };
-        if (k0 + L::ROWS <= q.kn && !padded) {
-            send_tile<T, DP>(smem[buf][0], a.head_dim, [&](int i) { return kbase + (int64_t)k0 * a.ks.row + i * a.ks.row; });
-            send_tile<T, DP>(smem[buf][1], a.head_dim, [&](int i) { return vbase + (int64_t)k0 * a.vs.row + i * a.vs.row; });
+        if (k0 + L::ROWS <= q.kn && !padded && regular) {
+            keys.whole(smem[buf][0], kbase + k0 * a.ks.row);
+            values.whole(smem[buf][1], vbase + k0 * a.vs.row);
         } else {
-            send_tile<T, DP>(smem[buf][0], a.head_dim, [&](int i) { return is(i) ? kbase + (int64_t)(k0 + i) * a.ks.row : nullptr; });
-            send_tile<T, DP>(smem[buf][1], a.head_dim, [&](int i) { return is(i) ? vbase + (int64_t)(k0 + i) * a.vs.row : nullptr; });
+            keys.rows(smem[buf][0], a.head_dim, [&](int i) { return is(i) ? kbase + (k0 + i) * a.ks.row : nullptr; });
+            values.rows(smem[buf][1], a.head_dim, [&](int i) { return is(i) ? vbase + (k0 + i) * a.vs.row : nullptr; });
         }
         if (a.k_docs && wave == 0) send_words(s_doc[buf], a.k_docs + q.k0 + min(k0 + lane, q.kn - 1));
     };
@@ -394,7 +404,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void quer
     if (a.parts > 1)
         put_row<float, DP>(a.part_o + (((int64_t)part * a.n_q + token) * a.heads + head) * a.head_dim, dq, 1.f, a.head_dim, half);
     else
-        put_row<T, DP>((T*)a.dq + token * a.dqs.row + head * a.dqs.head, dq, a.scale, a.head_dim, half);
+        put_row<T, DP>((T*)a.dq + token * a.dqs.row + head * a.dqs.head, dq, by_x<T>(a), a.head_dim, half);
 }
 
 // A gradient's shares added up, a thread an element: those of queries (z = 0), keys (1) and values (2).
@@ -408,7 +418,7 @@ __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
     const ps_strides to = z == 0 ? a.dqs : z == 1 ? a.dks : a.dvs;
     const float* part = z == 0 ? a.part_o : z == 1 ? a.part_dk : a.part_dv;
     T* out = (T*)(z == 0 ? a.dq : z == 1 ? a.dk : a.dv);
-    const float by = z == 2 ? 1.f : a.scale;
+    const float by = z == 2 ? 1.f : by_x<T>(a);
     const int tile = z == 0 ? a.tile : a.key_tile, tiles = ((z == 0 ? q.kn : q.qn * a.group) + tile - 1) / tile;
     const int parts = max(1, min(of, (tiles + each - 1) / each));
     const int64_t n = (int64_t)(z == 0 ? q.qn : q.kn) * heads * a.head_dim, first = (int64_t)(z == 0 ? q.q0 : q.k0) * heads * a.head_dim;

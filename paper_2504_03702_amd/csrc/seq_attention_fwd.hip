@@ -86,16 +86,18 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
 
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
+    const Sender<T, DP> keys(a.ks, 1, a.head_dim), values(a.vs, 1, a.head_dim);
+    const bool regular = keys.regular && values.regular;
     auto request = [&](int t, bool padded, int buf) {
         const int k0 = t * L::ROWS;
         // (rows past the keys, and padding, are zeros: their weights are, and nothing is to come of them)
         auto is = [&](int i) { return k0 + i < q.kn && (!padded || a.k_docs[q.k0 + k0 + i] >= 0); };
-        if (k0 + L::ROWS <= q.kn && !padded) {
-            send_tile<T, DP>(smem[buf][0], a.head_dim, [&](int i) { return kbase + (int64_t)k0 * a.ks.row + i * a.ks.row; });
-            send_tile<T, DP>(smem[buf][1], a.head_dim, [&](int i) { return vbase + (int64_t)k0 * a.vs.row + i * a.vs.row; });
+        if (k0 + L::ROWS <= q.kn && !padded && regular) {
+            keys.whole(smem[buf][0], kbase + k0 * a.ks.row);
+            values.whole(smem[buf][1], vbase + k0 * a.vs.row);
         } else {
-            send_tile<T, DP>(smem[buf][0], a.head_dim, [&](int i) { return is(i) ? kbase + (int64_t)(k0 + i) * a.ks.row : nullptr; });
-            send_tile<T, DP>(smem[buf][1], a.head_dim, [&](int i) { return is(i) ? vbase + (int64_t)(k0 + i) * a.vs.row : nullptr; });
+            keys.rows(smem[buf][0], a.head_dim, [&](int i) { return is(i) ? kbase + (k0 + i) * a.ks.row : nullptr; });
+            values.rows(smem[buf][1], a.head_dim, [&](int i) { return is(i) ? vbase + (k0 + i) * a.vs.row : nullptr; });
         }
         if (a.k_docs && wave == 0) send_words(s_doc[buf], a.k_docs + q.k0 + min(k0 + lane, q.kn - 1));
     };
@@ -106,7 +108,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
     float m = -INFINITY, l = 0.f;      // the exponent's reference, in powers of two; this lane's share of the sum
-    const float c1 = a.scale * LOG2E, inner = a.cap > 0.f ? a.scale / a.cap : 0.f, outer = a.cap * LOG2E;
+    const float c1 = a.scale * LOG2E;
+    const Cap cap = Cap::of<T>(a);
 
     Walk walk;
     int t = walk.next(t0, t1, classify), buf = 0;
@@ -128,7 +131,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
 #pragma unroll
                 for (int b = 0; b < L::BLOCKS; ++b)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) sc[b][e] = bend<T>(sc[b][e] * inner) * outer;
+                    for (int e = 0; e < 16; ++e) sc[b][e] = cap.score<T>(cap.bent<T>(sc[b][e]), 0.f);
                 c = 1.f;
             }
             if (a.slopes) {
