@@ -95,8 +95,9 @@ struct Tile {
 // A lane's fixed row: chunks 2 i + half.
 template <typename T, int DP>
 struct Fixed {
+    static constexpr bool READS = false;
     uint4 c[Tile<T, DP>::NF];
-    __device__ __forceinline__ const uint4& operator[](int i) const { return c[i]; }
+    __device__ __forceinline__ const uint4& chunk(int i, int) const { return c[i]; }
     // This half-wavefront's share of the product with another row that is laid out the same.
     __device__ __forceinline__ float share(const Fixed& o) const {
         float sum = 0.f;
@@ -136,82 +137,126 @@ struct Lanes {
 
 #define SEQATT_LDS __attribute__((address_space(3)))
 
+// An address that the compiler takes for a new one: what is made of it by a few XORs is then made again where it is used, instead of
+// in registers throughout the loop (16 of them for heads of 128, which the accumulators need).
+template <int ROWB>
+__device__ __forceinline__ int anew(int at) {
+    if (ROWB > 128) asm volatile("" : "+v"(at));
+    return at;
+}
+
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 u) { return __builtin_bit_cast(bf16x8, u); }
 
 // Fixed rows in LDS instead, the wavefront's own 32 of them: where registers are short.
 template <typename T, int DP>
 struct FixedInLds {
+    static constexpr bool READS = true;
     const unsigned char* rows;
-    int at;
-    __device__ __forceinline__ FixedInLds(unsigned char* to, const Fixed<T, DP>& f, const Lanes<T, DP>& l) : rows(to), at(l.row) {
+    __device__ __forceinline__ FixedInLds(unsigned char* to, const Fixed<T, DP>& f, const Lanes<T, DP>& l) : rows(to) {
 #pragma unroll
-        for (int i = 0; i < Tile<T, DP>::NF; ++i) *(uint4*)(to + (at ^ (i << 5))) = f.c[i];
+        for (int i = 0; i < Tile<T, DP>::NF; ++i) *(uint4*)(to + (l.row ^ (i << 5))) = f.c[i];
     }
-    __device__ __forceinline__ uint4 operator[](int i) const { return *(const uint4*)(rows + (at ^ (i << 5))); }
+    __device__ __forceinline__ uint4 chunk(int i, int row) const { return *(const uint4*)(rows + (row ^ (i << 5))); }   // row: Lanes'
 };
+
+// What a step reads from LDS is read in one go before its products: left alone the compiler, short of registers, reads for each
+// product when its turn comes and waits for LDS every time (heads of 128, gradients of keys: 60 % of a wavefront's time).
+__device__ __forceinline__ void reads_first() { __builtin_amdgcn_sched_barrier(0); }
 
 // 32 passing rows (block b of the tile) times the fixed rows.
 template <typename T, int DP, typename F>
 __device__ __forceinline__ f32x16 dot(const unsigned char* tile, int b, const F& f, const Lanes<T, DP>& l) {
     using L = Tile<T, DP>;
+    constexpr int N = F::READS ? 2 : L::NF < 8 ? L::NF : 8;
+    const int at = anew<L::ROWB>(l.row);
     f32x16 s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < L::NF; ++i) {
-        const uint4 a = *(const uint4*)(tile + b * 32 * L::ROWB + (l.row ^ (i << 5))), c = f[i];
-        if constexpr (L::EB == 2) {
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(c), s, 0, 0, 0);
-        } else {
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(c.x), s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(c.y), s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(c.z), s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(c.w), s, 0, 0, 0);
+    for (int n = 0; n < L::NF; n += N) {
+        uint4 as[N], cs[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            as[i] = *(const uint4*)(tile + b * 32 * L::ROWB + (at ^ ((n + i) << 5)));
+            cs[i] = f.chunk(n + i, at);
+        }
+        reads_first();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint4 a = as[i], c = cs[i];
+            if constexpr (L::EB == 2) {
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(c), s, 0, 0, 0);
+            } else {
+                s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(c.x), s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(c.y), s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(c.z), s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(c.w), s, 0, 0, 0);
+            }
         }
     }
     return s;
 }
 
-// What the rounding of w to bf16 leaves.  In tiles that a mask cuts rows see few keys, so weights are large and g has few terms:
-// the rounding of g, which averages out over many, is made up for there by a second product (a diagonal tile in 32 of 2048 keys).
-__device__ __forceinline__ void keep_rest(float (&w)[16]) {
+// The weights of a block's 32 passing rows for a lane's fixed row, as the second product takes them: floats, or bf16 in the order of
+// the accumulator's elements.
+template <typename T>
+struct Weights {
+    float w[16];
+    __device__ __forceinline__ void set(int j, float4 v) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) w[e] -= (float)(__bf16)w[e];
-}
+        for (int i = 0; i < 4; ++i) w[4 * j + i] = (&v.x)[i];
+    }
+};
+template <>
+struct Weights<__bf16> {
+    uint32_t w[8];
+    __device__ __forceinline__ void set(int j, float4 v) {
+        w[2 * j] = cvt_pk_bf16(v.x, v.y);
+        w[2 * j + 1] = cvt_pk_bf16(v.z, v.w);
+    }
+    __device__ __forceinline__ float4 get(int j) const {
+        return make_float4(__uint_as_float(w[2 * j] << 16), __uint_as_float(w[2 * j] & 0xffff0000u), __uint_as_float(w[2 * j + 1] << 16),
+                           __uint_as_float(w[2 * j + 1] & 0xffff0000u));
+    }
+};
 
 // acc[feature][fixed row] += sum over the block's 32 passing rows of tile[row][feature] w[row].
 template <typename T, int DP>
-__device__ __forceinline__ void weigh(const unsigned char* tile, int b, const float (&w)[16], f32x16 (&acc)[Tile<T, DP>::NA],
+__device__ __forceinline__ void weigh(const unsigned char* tile, int b, const Weights<T>& w, f32x16 (&acc)[Tile<T, DP>::NA],
                                       const Lanes<T, DP>& l) {
     using L = Tile<T, DP>;
     const unsigned char* base = tile + b * 32 * L::ROWB;
+    const int at = anew<L::ROWB>(l.turned);
     if constexpr (L::EB == 2) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            uint4 p;
-            p.x = cvt_pk_bf16(w[8 * j], w[8 * j + 1]);
-            p.y = cvt_pk_bf16(w[8 * j + 2], w[8 * j + 3]);
-            p.z = cvt_pk_bf16(w[8 * j + 4], w[8 * j + 5]);
-            p.w = cvt_pk_bf16(w[8 * j + 6], w[8 * j + 7]);
+            union { s16x4 h[2]; bf16x8 v; } a[L::NA];
 #pragma unroll
-            for (int i = 0; i < L::NA; ++i) {
-                union { s16x4 h[2]; bf16x8 v; } a;
+            for (int i = 0; i < L::NA; ++i)
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
-                    a.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (SEQATT_LDS s16x4*)(base + (16 * j + 8 * x) * L::ROWB + (l.turned ^ (i << 6) ^ (x << 5))));
-                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, as_bf16x8(p), acc[i], 0, 0, 0);
-            }
+                    a[i].h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (SEQATT_LDS s16x4*)(base + (16 * j + 8 * x) * L::ROWB + (at ^ (i << 6) ^ (x << 5))));
+            reads_first();
+            const bf16x8 p = as_bf16x8(make_uint4(w.w[4 * j], w.w[4 * j + 1], w.w[4 * j + 2], w.w[4 * j + 3]));
+#pragma unroll
+            for (int i = 0; i < L::NA; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i].v, p, acc[i], 0, 0, 0);
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
+        for (int g = 0; g < 4; ++g) {
+            float v[4][L::NA];
 #pragma unroll
-            for (int i = 0; i < L::NA; ++i) {
-                const int swz = (e & 3) << 1 | ((e >> 2) & 1);
-                const float v = *(const float*)(base + (8 * (e >> 2) + (e & 3)) * L::ROWB + (l.turned ^ (swz << 4) ^ (i << 7)));
-                acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w[e], acc[i], 0, 0, 0);
-            }
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < L::NA; ++i)
+                    v[e][i] = *(const float*)(base + (8 * g + e) * L::ROWB + (at ^ ((e << 1 | (g & 1)) << 4) ^ (i << 7)));
+            reads_first();
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < L::NA; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e][i], w.w[4 * g + e], acc[i], 0, 0, 0);
+        }
     }
 }
 
@@ -245,13 +290,14 @@ struct Sender {
             off[j] = regular ? (unsigned)(token * (int)s.row + (r - token * group) * (int)s.head + element(j, head_dim)) * L::EB : 0u;
         }
     }
-    __device__ __forceinline__ void whole(unsigned char* tile, const T* first) const {
+    static __device__ __forceinline__ void whole(unsigned char* tile, const T* first, const unsigned (&off)[L::PER_THREAD]) {
 #pragma unroll
         for (int j = 0; j < L::PER_THREAD; ++j) send(tile, j, (const char*)first + off[j]);
     }
+    __device__ __forceinline__ void whole(unsigned char* tile, const T* first) const { whole(tile, first, off); }
     // row(i): address of passing row i's element 0; null for a row of zeros.
     template <typename Row>
-    __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, Row row) const {
+    static __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, Row row) {
 #pragma unroll
         for (int j = 0; j < L::PER_THREAD; ++j) {
             const T* p = row(row_of(j));

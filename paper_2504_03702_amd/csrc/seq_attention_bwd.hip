@@ -9,76 +9,53 @@ typedef __bf16 bf16;
 
 namespace {
 
-// The weights p and the gradients d of x = scale q . k (by_x() times d) of one block, from the products s = q . k and g = dout . v, for the four
-// neighbours of every j: lse(j) and delta(j), what their queries bring along; distance(j), how far they stand from their keys, times the
-// slope; seen(j, is), which see them.  Everything that is the same for all elements is asked outside their loops, so that these are
-// straight lines.
+// The weights p and the gradients d of x = scale q . k (by_x() times d) of one block, from the products s = q . k and g = dout . v, four
+// neighbours j at a time so that few registers wait: lse(j) and delta(j), what their queries bring along; distance(j), how far they
+// stand from their keys, times the slope; seen(j, is), which see them.
+// rest: what the rounding of d to bf16 leaves, of blocks that a mask cuts: rows see few keys there, so weights are large and a gradient
+// has few terms; a second product makes up for the rounding, which averages out over many.
 template <typename T, typename Lse, typename Delta, typename Distance, typename Seen>
-__device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, float (&p)[16], float (&d)[16], bool whole, Lse lse,
-                                          Delta delta, Distance distance, Seen seen) {
-    if (a.cap > 0.f) {
-        const Cap cap = Cap::of<T>(a);
+__device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, Weights<T>& p, Weights<T>& d, Weights<T>& rest,
+                                          bool whole, Lse lse, Delta delta, Distance distance, Seen seen) {
+    const Cap cap = Cap::of<T>(a);
+    const float c1 = a.scale * LOG2E;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) d[e] = cap.bent<T>(s[e]);
+    for (int j = 0; j < 4; ++j) {
+        float4 l = lse(j), t = delta(j), u, v;
         if (a.slopes) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 l = lse(j), off = distance(j);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_amdgcn_exp2f(cap.score<T>(d[4 * j + i], (&l.x)[i] + (&off.x)[i]));
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 l = lse(j);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_amdgcn_exp2f(cap.score<T>(d[4 * j + i], (&l.x)[i]));
-            }
+            const float4 off = distance(j);
+            l = make_float4(l.x + off.x, l.y + off.y, l.z + off.z, l.w + off.w);
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float4 t = delta(j);
+        if (a.cap > 0.f) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int e = 4 * j + i;
-                d[e] = Cap::slope<T>(d[e]) * (p[e] * (g[e] - (&t.x)[i]));
-            }
-        }
-    } else {
-        const float c1 = a.scale * LOG2E;
-        if (a.slopes) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 l = lse(j), off = distance(j);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * j + i], c1, -((&l.x)[i] + (&off.x)[i])));
+                const float b = cap.bent<T>(s[4 * j + i]);
+                (&u.x)[i] = __builtin_amdgcn_exp2f(cap.score<T>(b, (&l.x)[i]));
+                (&v.x)[i] = Cap::slope<T>(b) * ((&u.x)[i] * (g[4 * j + i] - (&t.x)[i]));
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 l = lse(j);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * j + i], c1, -(&l.x)[i]));
+            for (int i = 0; i < 4; ++i) {
+                (&u.x)[i] = __builtin_amdgcn_exp2f(fmaf(s[4 * j + i], c1, -(&l.x)[i]));
+                (&v.x)[i] = (&u.x)[i] * (g[4 * j + i] - (&t.x)[i]);
             }
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float4 t = delta(j);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) d[4 * j + i] = p[4 * j + i] * (g[4 * j + i] - (&t.x)[i]);
-        }
-    }
-    if (!whole) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        if (!whole) {
             bool is[4];
             seen(j, is);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                p[4 * j + i] = is[i] ? p[4 * j + i] : 0.f;
-                d[4 * j + i] = is[i] ? d[4 * j + i] : 0.f;
+                (&u.x)[i] = is[i] ? (&u.x)[i] : 0.f;
+                (&v.x)[i] = is[i] ? (&v.x)[i] : 0.f;
             }
         }
+        p.set(j, u);
+        d.set(j, v);
+        if constexpr (sizeof(T) == 2)
+            if (!whole) {
+                const float4 r = d.get(j);
+                rest.set(j, make_float4(v.x - r.x, v.y - r.y, v.z - r.z, v.w - r.w));
+            }
     }
 }
 
@@ -108,7 +85,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     if (!sequence(a, s, q)) return;                                       // (reported by the queries' launch)
     const int k0 = kb * FIXED;
     if (k0 >= q.kn) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int rows = q.qn * a.group, tiles = (rows + L::ROWS - 1) / L::ROWS;
     const int t0 = part * a.key_part_tiles, t1 = min(tiles, t0 + a.key_part_tiles);
     if (t0 > 0 && t0 >= tiles) return;                                    // (part 0 writes, rows or not)
@@ -166,30 +143,53 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     const Sender<T, DP, L::ROWS> queries(a.qs, a.group, a.head_dim), gradients_out(a.gs, a.group, a.head_dim);
     const bool regular = queries.regular && gradients_out.regular;
     const T *qbase = (const T*)a.q + q.q0 * a.qs.row + (int64_t)hk * a.group * a.qs.head, *gbase = (const T*)a.dout + q.q0 * a.gs.row + (int64_t)hk * a.group * a.gs.head;
+    // What a tile's rows bring along, words that each of the wavefronts has one of: lse, dout . out, slope, document.
+    const int steps = L::ROWS / a.group;                                  // tokens from tile to tile, if regular
+    const int lane_token = (int)over_group(a, lane % L::ROWS), lane_head = hk * a.group + lane % L::ROWS - lane_token * a.group;
+    float* const words = wave == 0 ? s_lse[0] : wave == 1 ? s_delta[0] : wave == 2 ? s_slope[0] : (float*)s_doc[0];
+    const bool has_words = wave < 2 || (wave == 2 ? a.slopes != nullptr : a.q_docs != nullptr);
+    const int word_step = wave == 2 ? 0 : steps;
+    auto word = [&](int64_t token, int head) -> const void* {
+        return wave < 2 ? (wave == 0 ? a.row_lse : a.row_delta) + head * a.n_q + token : wave == 2 ? (const void*)(a.slopes + head) : (const void*)(a.q_docs + token);
+    };
+    // What a lane needs for that only once a tile, the offsets of its chunks and its first word's address, waits in LDS where registers
+    // are short: spilled to memory it would be read behind the tile just sent for, and waited for with it.
+    constexpr int PER = L::PER_THREAD;
+    struct Needs {
+        unsigned q[PER], g[PER];
+        const int32_t* word;
+    } needs;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        needs.q[j] = queries.off[j];
+        needs.g[j] = gradients_out.off[j];
+    }
+    needs.word = (const int32_t*)word(q.q0 + lane_token, lane_head);
+    __shared__ Needs s_needs[IN_LDS ? 256 : 1];
+    if (IN_LDS) s_needs[threadIdx.x] = needs;
+    auto fetch = [&]() -> Needs { return IN_LDS ? s_needs[threadIdx.x] : needs; };
     auto request = [&](int t, bool padded, int buf) {
         const int r0 = t * L::ROWS;
-        if (r0 + L::ROWS <= rows && !padded && regular) {
-            const int first = (int)over_group(a, r0);
-            queries.whole(smem[buf][0], qbase + first * a.qs.row);
-            gradients_out.whole(smem[buf][1], gbase + first * a.gs.row);
-        } else {
-            // (padding and rows past the end are zeros)
-            auto row = [&](const T* base, const ps_strides& st, int i) -> const T* {
-                const int qi = (int)over_group(a, min(r0 + i, rows - 1)), head = r0 + i - qi * a.group;
-                return r0 + i < rows && (!padded || a.q_docs[q.q0 + qi] >= 0) ? base + qi * st.row + head * st.head : nullptr;
-            };
-            queries.rows(smem[buf][0], a.head_dim, [&](int i) { return row(qbase, a.qs, i); });
-            gradients_out.rows(smem[buf][1], a.head_dim, [&](int i) { return row(gbase, a.gs, i); });
+        if (regular && r0 + L::ROWS <= rows && !padded) {
+            const int64_t token = t * steps;
+            const Needs mine = fetch();
+            Sender<T, DP, L::ROWS>::whole(smem[buf][0], qbase + token * a.qs.row, mine.q);
+            Sender<T, DP, L::ROWS>::whole(smem[buf][1], gbase + token * a.gs.row, mine.g);
+            if (has_words) send_words(words + 64 * buf, mine.word + (int64_t)t * word_step);
+            if (wave == 0) s_place[buf][lane] = q.start + (int)token + (int)over_group(a, lane % L::ROWS);
+            return;
         }
-        // what the rows bring along, a wavefront for each of its words (rows past the end see nothing)
-        const int r = r0 + lane, qi = (int)over_group(a, min(r, rows - 1)), head = hk * a.group + min(r, rows - 1) - qi * a.group;
-        const int64_t at = head * a.n_q + q.q0 + qi;
-        const bool is = r < rows;
-        if (wave == 0) send_words(s_lse[buf], is ? (const void*)(a.row_lse + at) : (const void*)&infinity_word);
-        if (wave == 1) send_words(s_delta[buf], is ? (const void*)(a.row_delta + at) : (const void*)&zeros);
-        if (wave == 2 && a.slopes) send_words(s_slope[buf], a.slopes + head);
-        if (wave == 3 && a.q_docs) send_words(s_doc[buf], is ? (const void*)(a.q_docs + q.q0 + qi) : (const void*)&minus_one);
-        if (wave == 0 && lane < L::ROWS) s_place[buf][lane] = q.start + qi;
+        // (padding and rows past the end are zeros that see nothing)
+        auto row = [&](const T* base, const ps_strides& st, int i) -> const T* {
+            const int qi = (int)over_group(a, min(r0 + i, rows - 1)), head = r0 + i - qi * a.group;
+            return r0 + i < rows && (!padded || a.q_docs[q.q0 + qi] >= 0) ? base + qi * st.row + head * st.head : nullptr;
+        };
+        Sender<T, DP, L::ROWS>::rows(smem[buf][0], a.head_dim, [&](int i) { return row(qbase, a.qs, i); });
+        Sender<T, DP, L::ROWS>::rows(smem[buf][1], a.head_dim, [&](int i) { return row(gbase, a.gs, i); });
+        const int r = min(r0 + lane, rows - 1), qi = (int)over_group(a, r);
+        const void* none = wave == 0 ? (const void*)&infinity_word : wave == 3 ? (const void*)&minus_one : (const void*)&zeros;
+        if (has_words) send_words(words + 64 * buf, r0 + lane < rows ? word(q.q0 + qi, hk * a.group + r - qi * a.group) : none);
+        if (wave == 0) s_place[buf][lane] = q.start + qi;
     };
 
     f32x16 dk[L::NA], dv[L::NA];
@@ -211,10 +211,11 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         if (wk0 < q.kn && !(a.causal && wk0 > far && wk0 >= q.prefix)) {
 #pragma unroll 1
             for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
-                const f32x16 sc = dot<T, DP>(smem[buf][0], b, kf, lanes), g = dot<T, DP>(smem[buf][1], b, vf, lanes);
-                float p[16], d[16];
+                const f32x16 sc = dot<T, DP>(smem[buf][0], b, kf, lanes);
+                const f32x16 g = dot<T, DP>(smem[buf][1], b, vf, lanes);
+                Weights<T> p, d, rest;
                 auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
-                gradients<T>(a, sc, g, p, d, whole, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
+                gradients<T>(a, sc, g, p, d, rest, whole, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
                              [&](int j) { return *(const float4*)&s_delta[buf][at(j)]; },
                              [&](int j) {
                                  const float4 by = *(const float4*)&s_slope[buf][at(j)];
@@ -230,23 +231,22 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
                              });
                 weigh<T, DP>(smem[buf][1], b, p, dv, lanes);
                 weigh<T, DP>(smem[buf][0], b, d, dk, lanes);
-                if (sizeof(T) == 2 && !whole) {
-                    keep_rest(d);
-                    weigh<T, DP>(smem[buf][0], b, d, dk, lanes);
-                }
+                if (sizeof(T) == 2 && !whole) weigh<T, DP>(smem[buf][0], b, rest, dk, lanes);
             }
         }
         buf ^= 1;
     }
-    if (!live) return;
+    const int mine = wk0 + (anew<256>((int)threadIdx.x) & 31);             // (the key, worked out again)
+    if (mine >= q.kn) return;
+    const int64_t to = q.k0 + mine;
     if (a.key_parts > 1) {
-        const int64_t row = ((int64_t)part * a.n_k + token) * a.kv_heads + hk;
+        const int64_t row = ((int64_t)part * a.n_k + to) * a.kv_heads + hk;
         put_row<float, DP>(a.part_dk + row * a.head_dim, dk, 1.f, a.head_dim, half);
         put_row<float, DP>(a.part_dv + row * a.head_dim, dv, 1.f, a.head_dim, half);
         return;
     }
-    put_row<T, DP>((T*)a.dk + token * a.dks.row + hk * a.dks.head, dk, by_x<T>(a), a.head_dim, half);
-    put_row<T, DP>((T*)a.dv + token * a.dvs.row + hk * a.dvs.head, dv, 1.f, a.head_dim, half);
+    put_row<T, DP>((T*)a.dk + to * a.dks.row + hk * a.dks.head, dk, by_x<T>(a), a.head_dim, half);
+    put_row<T, DP>((T*)a.dv + to * a.dvs.row + hk * a.dvs.head, dv, 1.f, a.head_dim, half);
 }
 
 // Queries fixed: dq of FIXED rows of a key head's queries.
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void quer
     }
     const int rows = q.qn * a.group, r0 = rb * FIXED;
     if (r0 >= rows) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int tiles = (q.kn + L::ROWS - 1) / L::ROWS;
     const int t0 = part * a.part_tiles, t1 = min(tiles, t0 + a.part_tiles);
     if (t0 > 0 && t0 >= tiles) return;                                    // (part 0 writes, keys or not)
@@ -377,9 +377,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void quer
 #pragma unroll 1
             for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
                 const f32x16 sc = dot<T, DP>(smem[buf][0], b, qf, lanes), g = dot<T, DP>(smem[buf][1], b, gf, lanes);
-                float p[16], d[16];
+                Weights<T> p, d, rest;
                 auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
-                gradients<T>(a, sc, g, p, d, whole, [&](int) { return make_float4(lse, lse, lse, lse); },
+                gradients<T>(a, sc, g, p, d, rest, whole, [&](int) { return make_float4(lse, lse, lse, lse); },
                              [&](int) { return make_float4(delta, delta, delta, delta); },
                              [&](int j) {
                                  const int from = place - k0 - at(j);
@@ -392,10 +392,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void quer
                                  for (int i = 0; i < 4; ++i) is[i] = (k0 + at(j) + i < end) & ((&of.x)[i] == doc) & there;
                              });
                 weigh<T, DP>(smem[buf][0], b, d, dq, lanes);
-                if (sizeof(T) == 2 && !whole) {
-                    keep_rest(d);
-                    weigh<T, DP>(smem[buf][0], b, d, dq, lanes);
-                }
+                if (sizeof(T) == 2 && !whole) weigh<T, DP>(smem[buf][0], b, rest, dq, lanes);
             }
         }
         buf ^= 1;

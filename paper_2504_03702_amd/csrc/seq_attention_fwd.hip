@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     }
     const int rows = q.qn * a.group, r0 = rb * FIXED;
     if (r0 >= rows) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int tiles = (q.kn + L::ROWS - 1) / L::ROWS;
     const int t0 = PARTS ? part * a.part_tiles : 0, t1 = PARTS ? min(tiles, t0 + a.part_tiles) : tiles;
     if (PARTS && t0 > 0 && t0 >= tiles) return;                           // (part 0 writes, keys or not)
@@ -184,11 +184,16 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
             const float ref = m == -INFINITY ? 0.f : m;                   // (a row that has seen nothing yet)
 #pragma unroll
             for (int b = 0; b < L::BLOCKS; ++b) {
-                float w[16];
+                Weights<T> w;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    w[e] = __builtin_amdgcn_exp2f(fmaf(sc[b][e], c, -ref));
-                    l += w[e];
+                for (int j = 0; j < 4; ++j) {
+                    float4 x;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        (&x.x)[i] = __builtin_amdgcn_exp2f(fmaf(sc[b][4 * j + i], c, -ref));
+                        l += (&x.x)[i];
+                    }
+                    w.set(j, x);
                 }
                 weigh<T, DP>(smem[buf][1], b, w, o, lanes);
             }
