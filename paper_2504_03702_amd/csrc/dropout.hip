@@ -124,20 +124,25 @@ __global__ __launch_bounds__(256) void dropout_sums_kernel(DropoutArgs a, int lo
         for (int j = 0; j < 8; ++j) a.sums[((int64_t)blockIdx.y * a.groups + g) * 8 + j] = part[threadIdx.x][j];
 }
 
-// 32 columns a workgroup, 8 shares of the row blocks.
+// 8 columns a workgroup, 32 shares of the 256 row blocks at most: eight loads of a thread, at once (32 columns and 8 shares 11.2 us of
+// 1024 columns).
 __global__ __launch_bounds__(256) void bias_kernel(const float* sums, int blocks, int stride, int cols, float* dbias) {
-    __shared__ float part[8][32];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), share = threadIdx.x >> 5;
+    __shared__ float part[32][8];
+    const int c = blockIdx.x * 8 + (threadIdx.x & 7), share = threadIdx.x >> 3;
     float s = 0.f;
-    if (c < cols)
-        for (int b = share; b < blocks; b += 8) s += sums[(int64_t)b * stride + c];
-    part[share][threadIdx.x & 31] = s;
-    __syncthreads();
-    if (share == 0 && c < cols) {
+    if (c < cols) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) s += part[i][threadIdx.x];
-        dbias[c] = s;
+        for (int i = 0; i < 8; ++i) {
+            const int b = share + 32 * i;
+            if (b < blocks) s += sums[(int64_t)b * stride + c];
+        }
     }
+    part[share][threadIdx.x & 7] = s;
+    for (int half = 16; half > 0; half /= 2) {
+        __syncthreads();
+        if (share < half) part[share][threadIdx.x & 7] += part[share + half][threadIdx.x & 7];
+    }
+    if (share == 0 && c < cols) dbias[c] = part[0][threadIdx.x];
 }
 
 // Rows of a row block: 256 blocks at most, so that the second sum is short, of 32 rows at least.
@@ -182,7 +187,7 @@ void launch_sums(const DropoutArgs& a, bool wide, float* dbias, hipStream_t st) 
         hipLaunchKernelGGL((dropout_sums_kernel<T, true>), grid, dim3(256), 0, st, a, log);
     else
         hipLaunchKernelGGL((dropout_sums_kernel<T, false>), grid, dim3(256), 0, st, a, log);
-    hipLaunchKernelGGL(bias_kernel, dim3((unsigned)((a.cols + 31) / 32)), dim3(256), 0, st, a.sums, blocks, a.groups * 8, a.cols, dbias);
+    hipLaunchKernelGGL(bias_kernel, dim3((unsigned)((a.cols + 7) / 8)), dim3(256), 0, st, a.sums, blocks, a.groups * 8, a.cols, dbias);
 }
 
 }  // namespace
@@ -231,7 +236,7 @@ extern "C" int ps_dropout_backward(const void* dout, int64_t ld_dout, const int6
     if (!dbias)
         dtype == 1 ? launch<bf16>(a, wide, st) : launch<float>(a, wide, st);
     else if (rows == 0)
-        hipLaunchKernelGGL(bias_kernel, dim3((unsigned)((cols + 31) / 32)), dim3(256), 0, st, a.sums, 0, 0, cols, dbias);
+        hipLaunchKernelGGL(bias_kernel, dim3((unsigned)((cols + 7) / 8)), dim3(256), 0, st, a.sums, 0, 0, cols, dbias);
     else
         dtype == 1 ? launch_sums<bf16>(a, wide, dbias, st) : launch_sums<float>(a, wide, dbias, st);
     return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;

@@ -9,52 +9,75 @@ typedef __bf16 bf16;
 
 namespace {
 
-// The weights p and the gradients d of x = scale q . k (by_x() times d) of one block, from the products s = q . k and g = dout . v, four
-// neighbours j at a time so that few registers wait: lse(j) and delta(j), what their queries bring along; distance(j), how far they
-// stand from their keys, times the slope; seen(j, is), which see them.
+// The weights p and the gradients d of x = scale q . k (by_x() times d) of one block, from the products s = q . k and g = dout . v, with
+// four neighbours to every j: lse(j) and delta(j), what their queries bring along; distance(j), how far they stand from their keys, times
+// the slope; seen(j, is), which see them.  STEP fours at a time: what is the same for all of them is asked once a step, so four at a time
+// make straight lines (two rows of 8192 tokens, queries' / keys' gradients 184 / 243 -> 169 / 236 us), and one keeps few registers waiting.
 // rest: what the rounding of d to bf16 leaves, of blocks that a mask cuts: rows see few keys there, so weights are large and a gradient
 // has few terms; a second product makes up for the rounding, which averages out over many.
-template <typename T, typename Lse, typename Delta, typename Distance, typename Seen>
+template <typename T, int STEP, typename Lse, typename Delta, typename Distance, typename Seen>
 __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, Weights<T>& p, Weights<T>& d, Weights<T>& rest,
                                           bool whole, Lse lse, Delta delta, Distance distance, Seen seen) {
     const Cap cap = Cap::of<T>(a);
     const float c1 = a.scale * LOG2E;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        float4 l = lse(j), t = delta(j), u, v;
+    for (int j0 = 0; j0 < 4; j0 += STEP) {
+        float4 u[STEP], v[STEP];
+#pragma unroll
+        for (int k = 0; k < STEP; ++k) u[k] = lse(j0 + k);
         if (a.slopes) {
-            const float4 off = distance(j);
-            l = make_float4(l.x + off.x, l.y + off.y, l.z + off.z, l.w + off.w);
+#pragma unroll
+            for (int k = 0; k < STEP; ++k) {
+                const float4 off = distance(j0 + k);
+                u[k] = make_float4(u[k].x + off.x, u[k].y + off.y, u[k].z + off.z, u[k].w + off.w);
+            }
         }
         if (a.cap > 0.f) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float b = cap.bent<T>(s[4 * j + i]);
-                (&u.x)[i] = __builtin_amdgcn_exp2f(cap.score<T>(b, (&l.x)[i]));
-                (&v.x)[i] = Cap::slope<T>(b) * ((&u.x)[i] * (g[4 * j + i] - (&t.x)[i]));
+            for (int e = 0; e < 4 * STEP; ++e) {
+                const float b = cap.bent<T>(s[4 * j0 + e]);
+                float& w = (&u[e >> 2].x)[e & 3];
+                w = __builtin_amdgcn_exp2f(cap.score<T>(b, w));
+                (&v[e >> 2].x)[e & 3] = Cap::slope<T>(b) * w;
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                (&u.x)[i] = __builtin_amdgcn_exp2f(fmaf(s[4 * j + i], c1, -(&l.x)[i]));
-                (&v.x)[i] = (&u.x)[i] * (g[4 * j + i] - (&t.x)[i]);
+            for (int e = 0; e < 4 * STEP; ++e) {
+                float& w = (&u[e >> 2].x)[e & 3];
+                w = __builtin_amdgcn_exp2f(fmaf(s[4 * j0 + e], c1, -w));
+                (&v[e >> 2].x)[e & 3] = w;
             }
+        }
+#pragma unroll
+        for (int k = 0; k < STEP; ++k) {
+            const float4 t = delta(j0 + k);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) (&v[k].x)[i] *= g[4 * (j0 + k) + i] - (&t.x)[i];
         }
         if (!whole) {
-            bool is[4];
-            seen(j, is);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                (&u.x)[i] = is[i] ? (&u.x)[i] : 0.f;
-                (&v.x)[i] = is[i] ? (&v.x)[i] : 0.f;
+            for (int k = 0; k < STEP; ++k) {
+                bool is[4];
+                seen(j0 + k, is);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    (&u[k].x)[i] = is[i] ? (&u[k].x)[i] : 0.f;
+                    (&v[k].x)[i] = is[i] ? (&v[k].x)[i] : 0.f;
+                }
             }
         }
-        p.set(j, u);
-        d.set(j, v);
+#pragma unroll
+        for (int k = 0; k < STEP; ++k) {
+            p.set(j0 + k, u[k]);
+            d.set(j0 + k, v[k]);
+        }
         if constexpr (sizeof(T) == 2)
             if (!whole) {
-                const float4 r = d.get(j);
-                rest.set(j, make_float4(v.x - r.x, v.y - r.y, v.z - r.z, v.w - r.w));
+#pragma unroll
+                for (int k = 0; k < STEP; ++k) {
+                    const float4 r = d.get(j0 + k);
+                    rest.set(j0 + k, make_float4(v[k].x - r.x, v[k].y - r.y, v[k].z - r.z, v[k].w - r.w));
+                }
             }
     }
 }
@@ -74,13 +97,13 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     __shared__ __align__(16) float s_lse[2][64], s_delta[2][64], s_slope[2][64];
     __shared__ __align__(16) int s_place[2][64], s_doc[2][64];
 
-    const int key_blocks = (a.max_k + FIXED - 1) / FIXED;
     unsigned id = blockIdx.x;
     const int hk = id % a.kv_heads;
     id /= a.kv_heads;
     const int part = id % a.key_parts;
     id /= a.key_parts;
-    const int kb = (int)(id % key_blocks), s = a.seq0 + (int)(id / key_blocks);   // (causal: the keys that most rows see first)
+    int s, kb;
+    block_of(a, id, (a.max_k + FIXED - 1) / FIXED, s, kb);                // (causal: the keys that most rows see first)
     Seq q;
     if (!sequence(a, s, q)) return;                                       // (reported by the queries' launch)
     const int k0 = kb * FIXED;
@@ -215,7 +238,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
                 const f32x16 g = dot<T, DP>(smem[buf][1], b, vf, lanes);
                 Weights<T> p, d, rest;
                 auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
-                gradients<T>(a, sc, g, p, d, rest, whole, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
+                gradients<T, DP == 128 ? 1 : 4>(a, sc, g, p, d, rest, whole, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
                              [&](int j) { return *(const float4*)&s_delta[buf][at(j)]; },
                              [&](int j) {
                                  const float4 by = *(const float4*)&s_slope[buf][at(j)];
@@ -261,7 +284,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void quer
     id /= a.kv_heads;
     const int part = id % a.parts;
     id /= a.parts;
-    const int rb = a.row_blocks - 1 - (int)(id % a.row_blocks), s = a.seq0 + (int)(id / a.row_blocks);
+    int s, rb;
+    block_of(a, id, a.row_blocks, s, rb);
+    rb = a.row_blocks - 1 - rb;
     Seq q;
     if (!sequence(a, s, q)) {
         if (threadIdx.x == 0 && hk == 0 && rb == 0 && part == 0) report_fault(a.status, PS_ST_BAD_LENGTH, s);
@@ -379,7 +404,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void quer
                 const f32x16 sc = dot<T, DP>(smem[buf][0], b, qf, lanes), g = dot<T, DP>(smem[buf][1], b, gf, lanes);
                 Weights<T> p, d, rest;
                 auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
-                gradients<T>(a, sc, g, p, d, rest, whole, [&](int) { return make_float4(lse, lse, lse, lse); },
+                gradients<T, 4>(a, sc, g, p, d, rest, whole, [&](int) { return make_float4(lse, lse, lse, lse); },
                              [&](int) { return make_float4(delta, delta, delta, delta); },
                              [&](int j) {
                                  const int from = place - k0 - at(j);
@@ -404,28 +429,35 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void quer
         put_row<T, DP>((T*)a.dq + token * a.dqs.row + head * a.dqs.head, dq, by_x<T>(a), a.head_dim, half);
 }
 
-// A gradient's shares added up, a thread an element: those of queries (z = 0), keys (1) and values (2).
+// A gradient's shares added up, a thread four neighbours: those of queries (z = 0), keys (1) and values (2).
 template <typename T>
 __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
     const int z = z0 + (int)blockIdx.z, s = a.seq0 + (int)blockIdx.y;
     Seq q;
     if (!sequence(a, s, q)) return;
     const int heads = z == 0 ? a.heads : a.kv_heads, of = z == 0 ? a.parts : a.key_parts, each = z == 0 ? a.part_tiles : a.key_part_tiles;
-    const int64_t all = z == 0 ? a.n_q : a.n_k;
     const ps_strides to = z == 0 ? a.dqs : z == 1 ? a.dks : a.dvs;
-    const float* part = z == 0 ? a.part_o : z == 1 ? a.part_dk : a.part_dv;
-    T* out = (T*)(z == 0 ? a.dq : z == 1 ? a.dk : a.dv);
-    const float by = z == 2 ? 1.f : by_x<T>(a);
     const int tile = z == 0 ? a.tile : a.key_tile, tiles = ((z == 0 ? q.kn : q.qn * a.group) + tile - 1) / tile;
     const int parts = max(1, min(of, (tiles + each - 1) / each));
-    const int64_t n = (int64_t)(z == 0 ? q.qn : q.kn) * heads * a.head_dim, first = (int64_t)(z == 0 ? q.q0 : q.k0) * heads * a.head_dim;
-    const int64_t step = all * heads * a.head_dim;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        float sum = 0.f;
-#pragma unroll 8
-        for (int p = 0; p < parts; ++p) sum += part[p * step + first + i];
-        const int64_t row = (first + i) / a.head_dim, token = row / heads;
-        out[token * to.row + (row - token * heads) * to.head + (first + i - row * a.head_dim)] = (T)(sum * by);
+    // (calls of few blocks: all of a tensor's rows are counted in 32 bits)
+    const int fours = a.head_dim / 4, n = (z == 0 ? q.qn : q.kn) * heads * fours, token0 = z == 0 ? q.q0 : q.k0;
+    const int64_t step = (z == 0 ? a.n_q : a.n_k) * heads * fours;
+    const float4* part = (const float4*)(z == 0 ? a.part_o : z == 1 ? a.part_dk : a.part_dv) + (int64_t)token0 * heads * fours;
+    T* out = (T*)(z == 0 ? a.dq : z == 1 ? a.dk : a.dv);
+    const float by = z == 2 ? 1.f : by_x<T>(a);
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+        float4 sum = part[i];
+#pragma unroll 4
+        for (int p = 1; p < parts; ++p) {
+            const float4 v = part[p * step + i];
+            sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+        }
+        const int row = i / fours, token = token0 + row / heads;
+        T* at = out + token * to.row + row % heads * to.head + i % fours * 4;
+        if constexpr (sizeof(T) == 2)
+            *(uint2*)at = make_uint2(cvt_pk_bf16(sum.x * by, sum.y * by), cvt_pk_bf16(sum.z * by, sum.w * by));
+        else
+            *(float4*)at = make_float4(sum.x * by, sum.y * by, sum.z * by, sum.w * by);
     }
 }
 
@@ -438,6 +470,8 @@ void launch(const Args& a, hipStream_t st) {
         for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
             n = (int32_t)min((int64_t)(a.n_seq - s0), most);
             b.seq0 = s0;
+            b.seqs = n;
+            b.together = turns(per_seq, n);
             launch_one((unsigned)n);
         }
     };
@@ -451,7 +485,7 @@ void launch(const Args& a, hipStream_t st) {
     });
     const int z0 = a.parts > 1 ? 0 : 1, z1 = a.key_parts > 1 ? 3 : 1;
     if (z0 == z1) return;
-    const int64_t most = max(z0 == 0 ? (int64_t)a.max_q * a.heads : 0, z1 == 3 ? (int64_t)a.max_k * a.kv_heads : 0) * a.head_dim;
+    const int64_t most = max(z0 == 0 ? (int64_t)a.max_q * a.heads : 0, z1 == 3 ? (int64_t)a.max_k * a.kv_heads : 0) * a.head_dim / 4;
     const unsigned blocks = (unsigned)min((most + 255) / 256, (int64_t)4096);
     in_turn(blocks, 32768, [&](unsigned n) {
         hipLaunchKernelGGL(add_kernel<T>, dim3(blocks, n, (unsigned)(z1 - z0)), dim3(256), 0, st, b, z0);

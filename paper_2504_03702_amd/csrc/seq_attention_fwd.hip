@@ -24,8 +24,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     id /= a.kv_heads;
     const int part = PARTS ? id % a.parts : 0;
     if (PARTS) id /= a.parts;
-    const int rb = a.row_blocks - 1 - (int)(id % a.row_blocks);           // (causal: the rows with the most keys first)
-    const int s = a.seq0 + (int)(id / a.row_blocks);
+    int s, rb;
+    block_of(a, id, a.row_blocks, s, rb);
+    rb = a.row_blocks - 1 - rb;                                           // (causal: the rows with the most keys first)
     Seq q;
     if (!sequence(a, s, q)) {
         if (threadIdx.x == 0 && hk == 0 && rb == 0 && part == 0) report_fault(a.status, PS_ST_BAD_LENGTH, s);
@@ -214,15 +215,16 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     if (a.lse_w && half == 0) a.lse_w[(int64_t)head * a.n_q + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
 }
 
-// The parts of a row put together: a workgroup a row, a wavefront a quarter of its parts, lane f elements f and f + 64.
-template <typename T>
+// The parts of a row put together by W of a workgroup's four wavefronts, each the W-th part of them; lane f has elements f and f + 64.
+template <typename T, int W>
 __global__ __launch_bounds__(256) void join_kernel(Args a) {
     __shared__ float s_l[4], s_o[4][128];
-    const int s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Seq q;
-    if (!sequence(a, s, q) || (int64_t)blockIdx.x >= (int64_t)q.qn * a.heads) return;
-    const int64_t row = (int64_t)q.q0 * a.heads + blockIdx.x, token = row / a.heads;
-    const int head = (int)(row - token * a.heads);
+    if (!sequence(a, s, q) || (int64_t)blockIdx.x * (4 / W) >= (int64_t)q.qn * a.heads) return;
+    const int i = min((int)blockIdx.x * (4 / W) + wave / W, q.qn * a.heads - 1);
+    const int64_t row = (int64_t)q.q0 * a.heads + i, token = q.q0 + i / a.heads;
+    const int head = i % a.heads;
     const int tiles = (q.kn + a.tile - 1) / a.tile, parts = max(1, min(a.parts, (tiles + a.part_tiles - 1) / a.part_tiles));
     const int64_t step = a.n_q * a.heads;
     float m = -INFINITY;
@@ -231,7 +233,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
     float l = 0.f, x = 0.f, y = 0.f;
     const bool first = lane < a.head_dim, second = lane + 64 < a.head_dim;
 #pragma unroll 4
-    for (int p = wave; p < parts; p += 4) {
+    for (int p = wave % W; p < parts; p += W) {
         const float2 ml = a.part_ml[p * step + row];
         const float* o = a.part_o + (p * step + row) * a.head_dim + lane;
         const float u = first ? o[0] : 0.f, v = second ? o[64] : 0.f;
@@ -240,19 +242,27 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
         x = fmaf(u, by, x);
         y = fmaf(v, by, y);
     }
-    s_o[wave][lane] = x;
-    s_o[wave][lane + 64] = y;
-    if (lane == 0) s_l[wave] = l;
-    __syncthreads();
-    const int f = threadIdx.x;
-    l = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
-    if (f < a.head_dim) {
-        const float o = ((s_o[0][f] + s_o[1][f]) + (s_o[2][f] + s_o[3][f])) * (l == 0.f ? 0.f : 1.f / l);
-        const T t = (T)o;
-        ((T*)a.out_w)[token * a.os.row + head * a.os.head + f] = t;
-        if (a.rest_w) ((bf16*)a.rest_w)[row * a.head_dim + f] = (bf16)(o - (float)t);
+    if constexpr (W == 4) {
+        s_o[wave][lane] = x;
+        s_o[wave][lane + 64] = y;
+        if (lane == 0) s_l[wave] = l;
+        __syncthreads();
+        if (wave != 0) return;
+        l = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
+        x = (s_o[0][lane] + s_o[1][lane]) + (s_o[2][lane] + s_o[3][lane]);
+        y = (s_o[0][lane + 64] + s_o[1][lane + 64]) + (s_o[2][lane + 64] + s_o[3][lane + 64]);
     }
-    if (a.lse_w && f == 0) a.lse_w[(int64_t)head * a.n_q + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* out = (T*)a.out_w + token * a.os.row + head * a.os.head;
+    bf16* rest = (bf16*)a.rest_w + row * a.head_dim;
+    auto put = [&](int e, float o) {
+        const T t = (T)o;
+        out[e] = t;
+        if (a.rest_w) rest[e] = (bf16)(o - (float)t);
+    };
+    if (first) put(lane, x * inv);
+    if (second) put(lane + 64, y * inv);
+    if (a.lse_w && lane == 0) a.lse_w[(int64_t)head * a.n_q + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
 }
 
 // Smallest and largest document of every DOC_BLOCK tokens, a wavefront each; padding counts as -1.
@@ -280,6 +290,8 @@ void launch_attend(const Args& a, hipStream_t st) {
         const int64_t most = max((int64_t)1, (int64_t)(1 << 22) / per_seq);       // (a grid holds fewer than 2^32 threads)
         n = (int32_t)min((int64_t)(a.n_seq - s0), most);
         b.seq0 = s0;
+        b.seqs = n;
+        b.together = turns(per_seq, n);
         const dim3 grid((unsigned)(per_seq * n));
         if (a.parts > 1)
             hipLaunchKernelGGL((attend_kernel<T, DP, true>), grid, dim3(256), 0, st, b);
@@ -290,8 +302,12 @@ void launch_attend(const Args& a, hipStream_t st) {
     for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
         n = min(a.n_seq - s0, 32768);
         b.seq0 = s0;
-        const dim3 grid((unsigned)((int64_t)a.max_q * a.heads), (unsigned)n);
-        hipLaunchKernelGGL(join_kernel<T>, grid, dim3(256), 0, st, b);
+        // few rows have many parts and the chip to themselves; many rows a wavefront each (25600 rows of 4 parts 53 us by four)
+        const int64_t rows = (int64_t)a.max_q * a.heads;
+        if (a.n_q * a.heads <= 4096)
+            hipLaunchKernelGGL((join_kernel<T, 4>), dim3((unsigned)rows, (unsigned)n), dim3(256), 0, st, b);
+        else
+            hipLaunchKernelGGL((join_kernel<T, 1>), dim3((unsigned)((rows + 3) / 4), (unsigned)n), dim3(256), 0, st, b);
     }
 }
 
