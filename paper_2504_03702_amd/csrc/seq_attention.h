@@ -45,6 +45,7 @@ struct Args {
     int32_t row_blocks;                // blocks of FIXED rows that the grid has for every sequence
     int32_t parts, part_tiles;         // shares of a row block's key tiles, and tiles of a share
     int32_t key_parts, key_part_tiles; // shares of a key block's row tiles
+    int32_t few;                       // at most 32 rows to a key head
     int32_t tile, key_tile;            // rows of a tile that passes by fixed queries, by fixed keys
     uint32_t by_group;                 // 2^32 / group + 1 (group > 1)
     float scale, cap;
@@ -76,15 +77,15 @@ __device__ __forceinline__ unsigned over_group(const Args& a, unsigned r) { retu
 // their work, most first.  In a launch of few blocks all sequences take turns, so that the last to start are short (two rows of 8192
 // tokens, forwards / keys' gradients: 119 / 243 us one after the other, 108 / 226 in turns; 16 x 2048, keys' 1213, 993); in one of many
 // only as many as fill the chip, so that blocks that run at a time read the same keys from the caches (16 x 2048, forwards / queries':
-// 460 / 609 us two at a time, 540 / 727 eight).
+// 460 / 609 us two at a time, 540 / 727 eight).  Blocks that are shared out are alike (fp32 heads of 80, keys' 233 us, 284 in turns).
 __device__ __forceinline__ void block_of(const Args& a, unsigned id, int blocks, int& s, int& block) {
     const unsigned turn = id / (unsigned)(blocks * a.together), first = turn * a.together, rest = id - first * blocks;
     const unsigned here = min((unsigned)a.together, a.seqs - first);
     block = rest / here;
     s = a.seq0 + first + rest % here;
 }
-inline int32_t turns(int64_t blocks_a_seq, int32_t seqs) {
-    if (blocks_a_seq * seqs <= 2048) return seqs;
+inline int32_t turns(int64_t blocks_a_seq, int32_t parts, int32_t seqs) {
+    if (parts == 1 && blocks_a_seq * seqs <= 2048) return seqs;
     return (int32_t)(blocks_a_seq >= 512 ? 1 : 512 / blocks_a_seq);
 }
 

@@ -464,30 +464,30 @@ __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
 template <typename T, int DP>
 void launch(const Args& a, hipStream_t st) {
     Args b = a;
-    auto in_turn = [&](int64_t per_seq, int64_t most_seqs, auto launch_one) {
+    auto in_turn = [&](int64_t per_seq, int32_t parts, int64_t most_seqs, auto launch_one) {
         if (per_seq == 0) return;
         const int64_t most = min(most_seqs, max((int64_t)1, (int64_t)(1 << 22) / per_seq));   // (a grid holds fewer than 2^32 threads)
         for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
             n = (int32_t)min((int64_t)(a.n_seq - s0), most);
             b.seq0 = s0;
             b.seqs = n;
-            b.together = turns(per_seq, n);
+            b.together = turns(per_seq, parts, n);
             launch_one((unsigned)n);
         }
     };
     const int64_t row_jobs = (int64_t)a.kv_heads * a.row_blocks * a.parts;
     const int64_t key_jobs = (int64_t)a.kv_heads * ((a.max_k + FIXED - 1) / FIXED) * a.key_parts;
-    in_turn(row_jobs, a.n_seq, [&](unsigned n) {
+    in_turn(row_jobs, a.parts, a.n_seq, [&](unsigned n) {
         hipLaunchKernelGGL((query_gradients_kernel<T, DP>), dim3((unsigned)row_jobs * n), dim3(256), 0, st, b);
     });
-    in_turn(key_jobs, a.n_seq, [&](unsigned n) {
+    in_turn(key_jobs, a.key_parts, a.n_seq, [&](unsigned n) {
         hipLaunchKernelGGL((key_gradients_kernel<T, DP>), dim3((unsigned)key_jobs * n), dim3(256), 0, st, b);
     });
     const int z0 = a.parts > 1 ? 0 : 1, z1 = a.key_parts > 1 ? 3 : 1;
     if (z0 == z1) return;
     const int64_t most = max(z0 == 0 ? (int64_t)a.max_q * a.heads : 0, z1 == 3 ? (int64_t)a.max_k * a.kv_heads : 0) * a.head_dim / 4;
     const unsigned blocks = (unsigned)min((most + 255) / 256, (int64_t)4096);
-    in_turn(blocks, 32768, [&](unsigned n) {
+    in_turn(blocks, 1, 32768, [&](unsigned n) {
         hipLaunchKernelGGL(add_kernel<T>, dim3(blocks, n, (unsigned)(z1 - z0)), dim3(256), 0, st, b, z0);
     });
 }

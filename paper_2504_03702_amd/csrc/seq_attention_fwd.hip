@@ -11,6 +11,125 @@ namespace {
 
 constexpr float SLACK = 8.f;           // powers of two that a score may exceed the exponent's reference by
 
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * LN2; }
+
+// A lane's row: what it sees, and its running maximum, sum and weighted values.
+template <typename T, int DP, int R>
+struct Row {
+    using L = Tile<T, DP, R>;
+    int head, place, doc, end;         // keys in front of `end` are seen, if their documents are
+    int64_t token;
+    float slope, m = -INFINITY, l = 0.f;   // the exponent's reference, in powers of two; this lane's share of the sum
+    Fixed<T, DP> qf;
+    f32x16 o[L::NA];
+    const Lanes<T, DP> lanes;
+    const int half;
+
+    // row r of key head hk's queries; live: whether there is one
+    __device__ __forceinline__ Row(const Args& a, const Seq& q, int hk, int r, bool live) : lanes(threadIdx.x & 63), half((threadIdx.x & 63) >> 5) {
+        const int qi = (int)over_group(a, r);
+        head = hk * a.group + r - qi * a.group;
+        token = q.q0 + qi;
+        place = q.start + qi;
+        slope = a.slopes ? a.slopes[head] * LOG2E : 0.f;
+        doc = a.q_docs ? a.q_docs[token] : 0;
+        end = doc < 0 ? 0 : a.causal ? min(q.kn, max(place + 1, q.prefix)) : q.kn;
+        qf.load((const T*)a.q + token * a.qs.row + head * a.qs.head, live, a.head_dim, half);
+#pragma unroll
+        for (int i = 0; i < L::NA; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    }
+
+    // A tile of keys from k0 on and its values; whole: every key in it is seen by all rows of the wavefront.
+    __device__ __forceinline__ void step(const Args& a, const unsigned char* keys, const unsigned char* values, const int* docs, int k0, bool whole) {
+        f32x16 sc[L::BLOCKS];
+#pragma unroll
+        for (int b = 0; b < L::BLOCKS; ++b) sc[b] = dot<T, DP>(keys, b, qf, lanes);
+        const Cap cap = Cap::of<T>(a);
+        float c = a.scale * LOG2E;
+        if (a.cap > 0.f) {
+#pragma unroll
+            for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc[b][e] = cap.score<T>(cap.bent<T>(sc[b][e]), 0.f);
+            c = 1.f;
+        }
+        if (a.slopes) {
+            const int from = place - k0 - 4 * half;
+#pragma unroll
+            for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    sc[b][e] = fmaf(-slope, fabsf((float)(from - 32 * b - row_of(e))), sc[b][e] * c);
+            c = 1.f;
+        }
+        if (!whole) {
+#pragma unroll
+            for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    if (k0 + 32 * b + row_of(e) + 4 * half >= end) sc[b][e] = -INFINITY;
+                }
+        }
+        if (!whole && a.k_docs) {
+#pragma unroll
+            for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int4 of = *(const int4*)&docs[32 * b + 8 * j + 4 * half];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if ((&of.x)[i] != doc) sc[b][4 * j + i] = -INFINITY;
+                }
+        }
+        float mx = sc[0][0];
+#pragma unroll
+        for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[b][e]);
+        const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1])) * c;
+        // the reference follows the maximum lazily: it moves when a tile exceeds it by more than SLACK, so weights reach
+        // 2^SLACK and the accumulators are rescaled a few times a row instead of at nearly every tile
+        if (__any(mx > m + SLACK)) {
+            const float next = mx > m + SLACK ? mx : m;
+            const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
+            m = next;
+#pragma unroll
+            for (int i = 0; i < L::NA; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
+            l *= alpha;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;                   // (a row that has seen nothing yet)
+#pragma unroll
+        for (int b = 0; b < L::BLOCKS; ++b) {
+            Weights<T> w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float4 x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    (&x.x)[i] = __builtin_amdgcn_exp2f(fmaf(sc[b][4 * j + i], c, -ref));
+                    l += (&x.x)[i];
+                }
+                w.set(j, x);
+            }
+            weigh<T, DP>(values, b, w, o, lanes);
+        }
+    }
+
+    // What is left to do once the halves of the wavefront have put their sums together.
+    __device__ __forceinline__ void add_halves() { l += __shfl_xor(l, 32, 64); }
+    __device__ __forceinline__ void put(const Args& a) const {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        put_row<T, DP>((T*)a.out_w + token * a.os.row + head * a.os.head, o, inv, a.head_dim, half);
+        if (a.rest_w) put_rest<DP>((bf16*)a.rest_w + (token * a.heads + head) * a.head_dim, o, inv, a.head_dim, half);
+        if (a.lse_w && half == 0) a.lse_w[(int64_t)head * a.n_q + token] = lse_of(m, l);
+    }
+};
+
 // A workgroup: FIXED rows of a key head's queries, against a share of the key tiles that any of them sees (one pass, running
 // maximum and sum).
 template <typename T, int DP, bool PARTS>
@@ -39,20 +158,11 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     const int t0 = PARTS ? part * a.part_tiles : 0, t1 = PARTS ? min(tiles, t0 + a.part_tiles) : tiles;
     if (PARTS && t0 > 0 && t0 >= tiles) return;                           // (part 0 writes, keys or not)
 
-    // this lane's row
-    const int r = r0 + 32 * wave + col, wr0 = r0 + 32 * wave;
-    const bool live = r < rows;
-    const int qi = (int)over_group(a, min(r, rows - 1)), head = hk * a.group + min(r, rows - 1) - qi * a.group;
-    const int64_t token = q.q0 + qi;
-    const int place = q.start + qi;
-    const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.f;
-    const int doc = a.q_docs ? a.q_docs[token] : 0;
-    Fixed<T, DP> qf;
-    qf.load((const T*)a.q + token * a.qs.row + head * a.qs.head, live, a.head_dim, half);
-    const Lanes<T, DP> lanes(lane);
+    const int wr0 = r0 + 32 * wave;
+    const bool live = wr0 + col < rows;
+    Row<T, DP, L::ROWS> row(a, q, hk, min(wr0 + col, rows - 1), live);
 
-    // what the workgroup's and the wavefront's rows see; keys in front of `end` this one, if their documents are
-    const int end = doc < 0 ? 0 : a.causal ? min(q.kn, max(place + 1, q.prefix)) : q.kn;
+    // what the workgroup's and the wavefront's rows see
     const int last = min(r0 + FIXED, rows) - 1;
     const int far = q.start + (int)over_group(a, last);                   // largest place
     const int wfar = q.start + (int)over_group(a, min(wr0 + 31, rows - 1)), wnear = q.start + (int)over_group(a, min(wr0, rows - 1));
@@ -103,15 +213,6 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
         if (a.k_docs && wave == 0) send_words(s_doc[buf], a.k_docs + q.k0 + min(k0 + lane, q.kn - 1));
     };
 
-    f32x16 o[L::NA];
-#pragma unroll
-    for (int i = 0; i < L::NA; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-    float m = -INFINITY, l = 0.f;      // the exponent's reference, in powers of two; this lane's share of the sum
-    const float c1 = a.scale * LOG2E;
-    const Cap cap = Cap::of<T>(a);
-
     Walk walk;
     int t = walk.next(t0, t1, classify), buf = 0;
     if (t < t1) request(t, walk.is_padded(t), 0);
@@ -124,95 +225,177 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
         if (t < t1) request(t, walk.is_padded(t), buf ^ 1);
         // (a wavefront whose rows all stand before the tile has nothing in it)
         if (wr0 < rows && !(a.causal && k0 > wfar && k0 >= q.prefix)) {
-            f32x16 sc[L::BLOCKS];
-#pragma unroll
-            for (int b = 0; b < L::BLOCKS; ++b) sc[b] = dot<T, DP>(smem[buf][0], b, qf, lanes);
-            float c = c1;
-            if (a.cap > 0.f) {
-#pragma unroll
-                for (int b = 0; b < L::BLOCKS; ++b)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) sc[b][e] = cap.score<T>(cap.bent<T>(sc[b][e]), 0.f);
-                c = 1.f;
-            }
-            if (a.slopes) {
-                const int from = place - k0 - 4 * half;
-#pragma unroll
-                for (int b = 0; b < L::BLOCKS; ++b)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        sc[b][e] = fmaf(-slope, fabsf((float)(from - 32 * b - row_of(e))), sc[b][e] * c);
-                c = 1.f;
-            }
-            if (!whole) {
-#pragma unroll
-                for (int b = 0; b < L::BLOCKS; ++b)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        if (k0 + 32 * b + row_of(e) + 4 * half >= end) sc[b][e] = -INFINITY;
-                    }
-            }
-            if (!whole && a.k_docs) {
-#pragma unroll
-                for (int b = 0; b < L::BLOCKS; ++b)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int4 of = *(const int4*)&s_doc[buf][32 * b + 8 * j + 4 * half];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if ((&of.x)[i] != doc) sc[b][4 * j + i] = -INFINITY;
-                    }
-            }
-            float mx = sc[0][0];
-#pragma unroll
-            for (int b = 0; b < L::BLOCKS; ++b)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[b][e]);
-            const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-            mx = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1])) * c;
-            // the reference follows the maximum lazily: it moves when a tile exceeds it by more than SLACK, so weights reach
-            // 2^SLACK and the accumulators are rescaled a few times a row instead of at nearly every tile
-            if (__any(mx > m + SLACK)) {
-                const float next = mx > m + SLACK ? mx : m;
-                const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
-                m = next;
-#pragma unroll
-                for (int i = 0; i < L::NA; ++i)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
-                l *= alpha;
-            }
-            const float ref = m == -INFINITY ? 0.f : m;                   // (a row that has seen nothing yet)
-#pragma unroll
-            for (int b = 0; b < L::BLOCKS; ++b) {
-                Weights<T> w;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float4 x;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        (&x.x)[i] = __builtin_amdgcn_exp2f(fmaf(sc[b][4 * j + i], c, -ref));
-                        l += (&x.x)[i];
-                    }
-                    w.set(j, x);
-                }
-                weigh<T, DP>(smem[buf][1], b, w, o, lanes);
-            }
+            row.step(a, smem[buf][0], smem[buf][1], s_doc[buf], k0, whole);
         }
         buf ^= 1;
     }
-    l += __shfl_xor(l, 32, 64);
+    row.add_halves();
     if (!live) return;
     if (PARTS) {
-        const int64_t row = ((int64_t)part * a.n_q + token) * a.heads + head;
-        put_row<float, DP>(a.part_o + row * a.head_dim, o, 1.f, a.head_dim, half);
-        if (half == 0) a.part_ml[row] = make_float2(m, l);
+        const int64_t at = ((int64_t)part * a.n_q + row.token) * a.heads + row.head;
+        put_row<float, DP>(a.part_o + at * a.head_dim, row.o, 1.f, a.head_dim, half);
+        if (half == 0) a.part_ml[at] = make_float2(row.m, row.l);
         return;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    put_row<T, DP>((T*)a.out_w + token * a.os.row + head * a.os.head, o, inv, a.head_dim, half);
-    if (a.rest_w) put_rest<DP>((bf16*)a.rest_w + (token * a.heads + head) * a.head_dim, o, inv, a.head_dim, half);
-    if (a.lse_w && half == 0) a.lse_w[(int64_t)head * a.n_q + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    row.put(a);
+}
+
+// Few rows, at most 32 of a key head's queries: single tokens over their keys, where the time goes into reading keys and values.  The
+// workgroup's wavefronts have the same rows and take tiles of 32 keys in turn, each with tiles of its own on their way through LDS, so
+// none waits for another until their rows are put together at the end.
+template <typename T, int DP>
+struct Few {
+    using L = Tile<T, DP, 32>;
+    static constexpr int SENDS = L::BYTES / 1024;                         // of 64 lanes, for a tile
+    // Tiles of a wavefront in LDS: two, or one of the largest; 128 KB of a unit's 160 either way, in bf16 with heads of 64 by two workgroups.
+    static constexpr int STAGES = L::BYTES >= 16384 ? 1 : 2, WORKGROUPS = L::BYTES >= 8192 ? 1 : 2;
+    static constexpr int PERIOD = L::CPR / 4, ROWS_A_SEND = 64 / L::CPR;  // sends whose lanes' chunks differ; the others repeat them
+    static constexpr int WAIT = (STAGES - 1) * (2 * SENDS + 1);           // sends behind the oldest tile's, and a word for documents
+    unsigned off[2][PERIOD];
+    int64_t step[2];                                                      // bytes from row to row
+    __device__ __forceinline__ Few(const Args& a) : step{a.ks.row * L::EB, a.vs.row * L::EB} {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < PERIOD; ++j) {
+            const int r = j * ROWS_A_SEND + lane / L::CPR;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) off[x][j] = (unsigned)(lane / L::CPR) * (unsigned)step[x] + element(r, a.head_dim) * L::EB;
+        }
+    }
+    static __device__ __forceinline__ int element(int r, int head_dim) {
+        return min((((int)(threadIdx.x & 63) % L::CPR) ^ L::swz(r)) * L::EPC, head_dim - L::EPC);
+    }
+    static __device__ __forceinline__ void send(unsigned char* tile, int j, const void* from) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)(tile + j * 1024), 16, 0, 0);
+    }
+    __device__ __forceinline__ void whole(unsigned char* tile, int x, const void* first) const {
+#pragma unroll
+        for (int j = 0; j < SENDS; ++j) send(tile, j, (const char*)first + j * ROWS_A_SEND * step[x] + off[x][j % PERIOD]);
+    }
+    // row(i): address of row i, null for zeros
+    template <typename Address>
+    static __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, Address row) {
+#pragma unroll
+        for (int j = 0; j < SENDS; ++j) {
+            const int r = j * ROWS_A_SEND + (int)(threadIdx.x & 63) / L::CPR;
+            const T* p = row(r);
+            send(tile, j, p ? (const void*)(p + element(r, head_dim)) : (const void*)&zeros);
+        }
+    }
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kernel(Args a) {
+    using F = Few<T, DP>;
+    using L = typename F::L;
+    constexpr int STAGES = F::STAGES;
+    __shared__ __align__(1024) unsigned char smem[4][STAGES][2][L::BYTES];   // [wavefront][stage][keys, values]; at the end the rows' sums
+    __shared__ __align__(16) int s_doc[4][STAGES][64];
+    __shared__ float2 s_ml[4][32];
+    static_assert(sizeof(smem) >= 4 * 32 * DP * sizeof(float), "the wavefronts' sums");
+
+    unsigned id = blockIdx.x;
+    const int hk = id % a.kv_heads;
+    id /= a.kv_heads;
+    const int part = id % a.parts, s = a.seq0 + (int)(id / a.parts);
+    Seq q;
+    if (!sequence(a, s, q)) {
+        if (threadIdx.x == 0 && hk == 0 && part == 0) report_fault(a.status, PS_ST_BAD_LENGTH, s);
+        return;
+    }
+    const int rows = q.qn * a.group;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+    const int tiles = (q.kn + 31) / 32, t0 = part * a.part_tiles, t1 = min(tiles, t0 + a.part_tiles);
+    if (rows == 0 || (t0 > 0 && t0 >= tiles)) return;                     // (part 0 writes, keys or not)
+
+    const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
+    const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
+    const F few(a);
+    const bool regular = a.ks.row < 1 << 20 && a.vs.row < 1 << 20;
+    auto request = [&](int t, int stage) {
+        const int k0 = t * 32;
+        unsigned char *keys = smem[wave][stage][0], *values = smem[wave][stage][1];
+        if (regular && k0 + 32 <= q.kn && !a.k_docs) {
+            few.whole(keys, 0, kbase + k0 * a.ks.row);
+            few.whole(values, 1, vbase + k0 * a.vs.row);
+        } else {
+            auto is = [&](int i) { return k0 + i < q.kn && (!a.k_docs || a.k_docs[q.k0 + k0 + i] >= 0); };
+            F::rows(keys, a.head_dim, [&](int i) { return is(i) ? kbase + (k0 + i) * a.ks.row : nullptr; });
+            F::rows(values, a.head_dim, [&](int i) { return is(i) ? vbase + (k0 + i) * a.vs.row : nullptr; });
+        }
+        send_words(s_doc[wave][stage], a.k_docs ? (const void*)(a.k_docs + q.k0 + min(k0 + lane, q.kn - 1)) : (const void*)&zeros);
+    };
+    const int near = q.start, far = q.start + q.qn - 1;                   // places of the rows
+    auto classify = [&](int t, bool& all, bool& pad) {
+        const int k0 = t * 32;
+        pad = false;
+        all = k0 + 32 <= q.kn && !a.k_docs && (!a.causal || k0 + 31 <= near || k0 + 32 <= q.prefix);
+        return (t & 3) == wave && (!a.causal || k0 <= far || k0 < q.prefix);
+    };
+
+    Walk walk, ahead;                                                     // the tile to work on, the last one sent for
+    int t = walk.next(t0, t1, classify), sent = ahead.next(t0, t1, classify), stage = 0, next_stage = 0;
+    auto send_next = [&] {
+        request(sent, next_stage);
+        next_stage = next_stage + 1 < STAGES ? next_stage + 1 : 0;
+        sent = ahead.next(sent + 1, t1, classify);
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i)
+        if (sent < t1) send_next();
+    Row<T, DP, 32> row(a, q, hk, min(col, rows - 1), col < rows);
+    while (t < t1) {
+        // (with a tile behind it every send of this one is WAIT sends old; the last ones wait for all)
+        if (STAGES > 1 && sent < t1)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(F::WAIT) : "memory");
+        else
+            vm_wait();
+        row.step(a, smem[wave][stage][0], smem[wave][stage][1], s_doc[wave][stage], t * 32, walk.is_whole(t));
+        asm volatile("" ::: "memory");                                    // (its reads are over: their products are on their way)
+        stage = stage + 1 < STAGES ? stage + 1 : 0;
+        t = walk.next(t + 1, t1, classify);
+        if (sent < t1) send_next();
+    }
+    row.add_halves();
+
+    // the wavefronts' rows put together
+    __syncthreads();
+    float* sums = (float*)smem;                                           // [wavefront][row][DP]
+    put_row<float, DP>(sums + (wave * 32 + col) * DP, row.o, 1.f, DP, half);
+    if (half == 0) s_ml[wave][col] = make_float2(row.m, row.l);
+    __syncthreads();
+    const int fours = a.head_dim / 4;
+    for (int i = threadIdx.x; i < rows * fours; i += 256) {
+        const int r = i / fours, f = i % fours * 4;
+        float m = s_ml[0][r].x, l = 0.f, by[4];
+        for (int w = 1; w < 4; ++w) m = fmaxf(m, s_ml[w][r].x);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            by[w] = s_ml[w][r].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_ml[w][r].x - m);
+            l = fmaf(s_ml[w][r].y, by[w], l);
+            const float4 x = *(const float4*)(sums + (w * 32 + r) * DP + f);
+            o = make_float4(fmaf(x.x, by[w], o.x), fmaf(x.y, by[w], o.y), fmaf(x.z, by[w], o.z), fmaf(x.w, by[w], o.w));
+        }
+        const int qi = (int)over_group(a, r), head = hk * a.group + r - qi * a.group;
+        const int64_t token = q.q0 + qi, at = token * a.heads + head;
+        if (a.parts > 1) {
+            const int64_t mine = part * a.n_q * a.heads + at;
+            *(float4*)(a.part_o + mine * a.head_dim + f) = o;
+            if (f == 0) a.part_ml[mine] = make_float2(m, l);
+            continue;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float v[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+        T* out = (T*)a.out_w + token * a.os.row + head * a.os.head + f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const T x = (T)v[j];
+            out[j] = x;
+            if (a.rest_w) ((bf16*)a.rest_w)[at * a.head_dim + f + j] = (bf16)(v[j] - (float)x);
+        }
+        if (f == 0 && a.lse_w) a.lse_w[(int64_t)head * a.n_q + token] = lse_of(m, l);
+    }
 }
 
 // The parts of a row put together by W of a workgroup's four wavefronts, each the W-th part of them; lane f has elements f and f + 64.
@@ -262,7 +445,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
     };
     if (first) put(lane, x * inv);
     if (second) put(lane + 64, y * inv);
-    if (a.lse_w && lane == 0) a.lse_w[(int64_t)head * a.n_q + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    if (a.lse_w && lane == 0) a.lse_w[(int64_t)head * a.n_q + token] = lse_of(m, l);
 }
 
 // Smallest and largest document of every DOC_BLOCK tokens, a wavefront each; padding counts as -1.
@@ -291,9 +474,11 @@ void launch_attend(const Args& a, hipStream_t st) {
         n = (int32_t)min((int64_t)(a.n_seq - s0), most);
         b.seq0 = s0;
         b.seqs = n;
-        b.together = turns(per_seq, n);
+        b.together = turns(per_seq, a.parts, n);
         const dim3 grid((unsigned)(per_seq * n));
-        if (a.parts > 1)
+        if (a.few)
+            hipLaunchKernelGGL((attend_few_kernel<T, DP>), grid, dim3(256), 0, st, b);
+        else if (a.parts > 1)
             hipLaunchKernelGGL((attend_kernel<T, DP, true>), grid, dim3(256), 0, st, b);
         else
             hipLaunchKernelGGL((attend_kernel<T, DP, false>), grid, dim3(256), 0, st, b);
@@ -372,8 +557,21 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
         parts = (tiles + part_tiles - 1) / part_tiles;
     };
     const int64_t rows_a_seq = (int64_t)a.max_q * group;
-    share(a.row_blocks, d->n_q * group, FIXED, a.max_k, d->n_k, a.tile, a.parts, a.part_tiles);
+    // Few rows: shares of 16 tiles or more (four a wavefront), so many that there are some 1024, long sequences' and short ones'.
+    a.few = !backward && (int64_t)a.max_q * group <= 32;
+    if (a.few) {
+        a.tile = 32;
+        const int64_t tiles = ((int64_t)a.max_k + 31) / 32, jobs = a.kv_heads * (d->n_k / 32 + d->n_seq);
+        const int64_t most = max((int64_t)1, ((int64_t)64 << 20) / max((int64_t)1, d->n_q * d->heads * d->head_dim));
+        a.part_tiles = (int32_t)max(max((int64_t)16, jobs / 1024), (tiles + most - 1) / most);
+        a.parts = (int32_t)max((int64_t)1, (tiles + a.part_tiles - 1) / a.part_tiles);
+    } else {
+        share(a.row_blocks, d->n_q * group, FIXED, a.max_k, d->n_k, a.tile, a.parts, a.part_tiles);
+    }
     share((a.max_k + FIXED - 1) / FIXED, d->n_k, FIXED, rows_a_seq, d->n_q * group, a.key_tile, a.key_parts, a.key_part_tiles);
+    // (a grid holds fewer than 2^32 threads)
+    if ((int64_t)a.kv_heads * a.row_blocks * a.parts >= 1 << 24 || (int64_t)a.kv_heads * ((a.max_k + FIXED - 1) / FIXED) * a.key_parts >= 1 << 24)
+        return PS_EUNSUPPORTED;
     size_t off = 0;
     uint8_t* base = (uint8_t*)workspace;
     auto take = [&](size_t bytes) {
@@ -383,24 +581,21 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
     };
     a.q_blocks = (int2*)take(sizeof(int2) * (size_t)(d->n_q / DOC_BLOCK + d->n_seq + 1));
     a.k_blocks = (int2*)take(sizeof(int2) * (size_t)(d->n_k / DOC_BLOCK + d->n_seq + 1));
-    const size_t rows = (size_t)d->n_q * d->heads, shared = off;
+    const size_t rows = (size_t)d->n_q * d->heads;
     if (a.parts > 1) {
         a.part_o = (float*)take(sizeof(float) * rows * d->head_dim * a.parts);
-        a.part_ml = (float2*)take(sizeof(float2) * rows * a.parts);
+        if (!backward) a.part_ml = (float2*)take(sizeof(float2) * rows * a.parts);
     }
-    p.bytes = off;
     if (backward) {
-        off = shared;
         a.row_lse = (float*)take(sizeof(float) * rows);
         a.row_delta = (float*)take(sizeof(float) * rows);
-        if (a.parts > 1) a.part_o = (float*)take(sizeof(float) * rows * d->head_dim * a.parts);
         if (a.key_parts > 1) {
             const size_t part = sizeof(float) * (size_t)d->n_k * d->kv_heads * d->head_dim * a.key_parts;
             a.part_dk = (float*)take(part);
             a.part_dv = (float*)take(part);
         }
-        p.bytes = off > p.bytes ? off : p.bytes;
     }
+    p.bytes = off;
     return PS_OK;
 }
 
@@ -419,8 +614,9 @@ void summarise_documents(const Args& a, hipStream_t st) {
 }  // namespace seqatt
 
 extern "C" size_t ps_attention_workspace_bytes(const ps_attention_desc* desc, int backward) {
-    Plan p;
-    return plan(desc, nullptr, backward != 0, nullptr, p) == PS_OK ? p.bytes : 0;
+    Plan p, b;
+    if (plan(desc, nullptr, false, nullptr, p) != PS_OK || plan(desc, nullptr, true, nullptr, b) != PS_OK) return 0;
+    return backward && b.bytes > p.bytes ? b.bytes : p.bytes;
 }
 
 extern "C" int ps_attention_forward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const void* q, const void* k,
@@ -440,7 +636,7 @@ extern "C" int ps_attention_forward(const ps_attention_desc* desc, const ps_atte
     a.q = q; a.k = k; a.v = v; a.out_w = out; a.lse_w = lse; a.rest_w = out_rest; a.status = status;
     hipStream_t st = (hipStream_t)hip_stream;
     (void)hipGetLastError();
-    summarise_documents(a, st);
+    if (!a.few) summarise_documents(a, st);
     if (desc->dtype == 1)
         desc->head_dim <= 64 ? launch_attend<bf16, 64>(a, st) : launch_attend<bf16, 128>(a, st);
     else
