@@ -96,18 +96,25 @@ __device__ __forceinline__ int64_t doc_block0(int first_token, int s) { return f
 // transposing reads, fall into different banks -------------------------------------------------------------------------------
 constexpr int tile_rows(int eb) { return eb == 2 ? 64 : 32; }
 // Rows of a tile that passes by fixed keys: for heads of 128 half as many, which leaves room for a workgroup's values (below).
-constexpr int key_tile_rows(int eb, int dp) { return eb == 2 && dp == 64 ? 64 : 32; }
+constexpr int key_tile_rows(int eb, int dp) { return eb == 2 && dp < 128 ? 64 : 32; }
+constexpr int padded(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : 128; }   // features of a tile
 
 template <typename T, int DP, int R = tile_rows(sizeof(T))>
 struct Tile {
     static constexpr int EB = sizeof(T), ROWB = DP * EB, ROWS = R, BLOCKS = ROWS / 32, BYTES = ROWS * ROWB;
     static constexpr int CPR = ROWB / 16, PER_THREAD = BYTES / 16 / 256, EPC = 16 / EB, NF = ROWB / 32, NA = DP / 32;
-    static __device__ __forceinline__ int swz(int r) {
-        if (EB == 4) return ((r >> 2) & 1) << 3 | (r & 3) << 1 | ((r >> 3) & 1);
-        if (DP == 64) return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) | ((r >> 3) & 1) << 1;
+    // The swizzle turns as many low bits of a chunk's number as rows of this length leave free (rows are multiples of 2^BITS chunks).
+    static constexpr int BITS = ROWB % 256 == 0 ? 4 : ROWB % 128 == 0 ? 3 : 2, LOW = (1 << BITS) - 1;
+    static __device__ __forceinline__ constexpr int swz(int r) {
+        if (EB == 4 && BITS == 4) return ((r >> 2) & 1) << 3 | (r & 3) << 1 | ((r >> 3) & 1);
+        if (EB == 4) return (r >> 1) & 7;
+        if (BITS == 3) return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) | ((r >> 3) & 1) << 1;
+        if (BITS == 2) return (r >> 2) & 3;
         return (r & 3) << 2 | ((r >> 2) & 3);
     }
     static __device__ __forceinline__ int at(int r, int chunk) { return r * ROWB + ((chunk ^ swz(r)) << 4); }
+    // at(r, chunk + more) from at(r, chunk), for chunk < the power of two that `more` is a multiple of.
+    static __device__ __forceinline__ int further(int at, int more) { return (at ^ ((more & LOW) << 4)) + ((more & ~LOW) << 4); }
 };
 
 // A lane's fixed row: chunks 2 i + half.
@@ -172,9 +179,9 @@ struct FixedInLds {
     const unsigned char* rows;
     __device__ __forceinline__ FixedInLds(unsigned char* to, const Fixed<T, DP>& f, const Lanes<T, DP>& l) : rows(to) {
 #pragma unroll
-        for (int i = 0; i < Tile<T, DP>::NF; ++i) *(uint4*)(to + (l.row ^ (i << 5))) = f.c[i];
+        for (int i = 0; i < Tile<T, DP>::NF; ++i) *(uint4*)(to + Tile<T, DP>::further(l.row, 2 * i)) = f.c[i];
     }
-    __device__ __forceinline__ uint4 chunk(int i, int row) const { return *(const uint4*)(rows + (row ^ (i << 5))); }   // row: Lanes'
+    __device__ __forceinline__ uint4 chunk(int i, int row) const { return *(const uint4*)(rows + Tile<T, DP>::further(row, 2 * i)); }   // row: Lanes'
 };
 
 // What a step reads from LDS is read in one go before its products: left alone the compiler, short of registers, reads for each
@@ -185,7 +192,7 @@ __device__ __forceinline__ void reads_first() { __builtin_amdgcn_sched_barrier(0
 template <typename T, int DP, typename F>
 __device__ __forceinline__ f32x16 dot(const unsigned char* tile, int b, const F& f, const Lanes<T, DP>& l) {
     using L = Tile<T, DP>;
-    constexpr int N = F::READS ? 2 : L::NF < 8 ? L::NF : 8;
+    constexpr int N = F::READS ? 2 : L::NF <= 8 ? L::NF : L::NF / 2;
     const int at = anew<L::ROWB>(l.row);
     f32x16 s;
 #pragma unroll
@@ -195,7 +202,7 @@ __device__ __forceinline__ f32x16 dot(const unsigned char* tile, int b, const F&
         uint4 as[N], cs[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            as[i] = *(const uint4*)(tile + b * 32 * L::ROWB + (at ^ ((n + i) << 5)));
+            as[i] = *(const uint4*)(tile + b * 32 * L::ROWB + L::further(at, 2 * (n + i)));
             cs[i] = f.chunk(n + i, at);
         }
         reads_first();
@@ -254,7 +261,7 @@ __device__ __forceinline__ void weigh(const unsigned char* tile, int b, const We
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
                     a[i].h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (SEQATT_LDS s16x4*)(base + (16 * j + 8 * x) * L::ROWB + (at ^ (i << 6) ^ (x << 5))));
+                        (SEQATT_LDS s16x4*)(base + (16 * j + 8 * x) * L::ROWB + (L::further(at, 4 * i) ^ (L::swz(8 * x) << 4))));
             reads_first();
             const bf16x8 p = as_bf16x8(make_uint4(w.w[4 * j], w.w[4 * j + 1], w.w[4 * j + 2], w.w[4 * j + 3]));
 #pragma unroll
@@ -268,7 +275,7 @@ __device__ __forceinline__ void weigh(const unsigned char* tile, int b, const We
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int i = 0; i < L::NA; ++i)
-                    v[e][i] = *(const float*)(base + (8 * g + e) * L::ROWB + (at ^ ((e << 1 | (g & 1)) << 4) ^ (i << 7)));
+                    v[e][i] = *(const float*)(base + (8 * g + e) * L::ROWB + L::further(at ^ (L::swz(8 * g + e) << 4), 8 * i));
             reads_first();
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -289,10 +296,9 @@ struct Sender {
     using L = Tile<T, DP, R>;
     unsigned off[L::PER_THREAD];       // where a lane's chunks lie from the tile's first element on, in bytes
     bool regular;                      // the same in every tile
-    static __device__ __forceinline__ int row_of(int j) { return ((j * 4 + (int)(threadIdx.x >> 6)) * 64 + (int)(threadIdx.x & 63)) / L::CPR; }
+    static __device__ __forceinline__ int row_of(int j) { return (j * 256 + (int)threadIdx.x) / L::CPR; }
     static __device__ __forceinline__ int element(int j, int head_dim) {
-        const int r = row_of(j);
-        return min((((int)threadIdx.x % L::CPR) ^ L::swz(r)) * L::EPC, head_dim - L::EPC);
+        return min((((j * 256 + (int)threadIdx.x) % L::CPR) ^ L::swz(row_of(j))) * L::EPC, head_dim - L::EPC);
     }
     static __device__ __forceinline__ void send(unsigned char* tile, int j, const void* from) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

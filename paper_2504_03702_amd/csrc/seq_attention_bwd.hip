@@ -153,7 +153,10 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
             some = k0 <= q.start + end || k0 < q.prefix;
             all = wlast <= q.start + first || wlast < q.prefix;
         }
-        if (a.q_docs && some) {
+        if (a.q_docs && !a.q_blocks) {
+            all = false;
+            pad = true;
+        } else if (a.q_docs && some) {
             const int2 m = a.q_blocks[qblock0 + first / DOC_BLOCK], n = a.q_blocks[qblock0 + end / DOC_BLOCK];
             const int lo = min(m.x, n.x), hi = max(m.y, n.y);
             some = dmax >= 0 && hi >= max(dmin, 0) && lo <= dmax;
@@ -238,7 +241,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
                 const f32x16 g = dot<T, DP>(smem[buf][1], b, vf, lanes);
                 Weights<T> p, d, rest;
                 auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
-                gradients<T, DP == 128 ? 1 : 4>(a, sc, g, p, d, rest, whole, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
+                gradients<T, (DP > 64 ? 1 : 4)>(a, sc, g, p, d, rest, whole, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
                              [&](int j) { return *(const float4*)&s_delta[buf][at(j)]; },
                              [&](int j) {
                                  const float4 by = *(const float4*)&s_slope[buf][at(j)];
@@ -274,7 +277,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
 
 // Queries fixed: dq of FIXED rows of a key head's queries.
 template <typename T, int DP>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void query_gradients_kernel(Args a) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_gradients_kernel(Args a) {
     using L = Tile<T, DP>;
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][keys, values]
     __shared__ __align__(16) int s_doc[2][64];
@@ -356,7 +359,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void quer
             some = k0 <= far || k0 < q.prefix;
             all = all && (k0 + L::ROWS - 1 <= wnear || k0 + L::ROWS <= q.prefix);
         }
-        if (a.k_docs && some) {
+        if (a.k_docs && !a.k_blocks) {
+            all = false;
+            pad = true;
+        } else if (a.k_docs && some) {
             const int2 m = a.k_blocks[kblock0 + k0 / DOC_BLOCK];
             some = dmax >= 0 && m.y >= max(dmin, 0) && m.x <= dmax;
             all = all && m.x == m.y && dmin == dmax && m.x == dmin;
@@ -516,9 +522,10 @@ extern "C" int ps_attention_backward(const ps_attention_desc* desc, const ps_att
     hipStream_t st = (hipStream_t)hip_stream;
     (void)hipGetLastError();
     summarise_documents(a, st);
-    if (desc->dtype == 1)
-        desc->head_dim <= 64 ? launch<bf16, 64>(a, st) : launch<bf16, 128>(a, st);
-    else
-        desc->head_dim <= 64 ? launch<float, 64>(a, st) : launch<float, 128>(a, st);
+    switch (padded(desc->head_dim)) {
+        case 64: desc->dtype == 1 ? launch<bf16, 64>(a, st) : launch<float, 64>(a, st); break;
+        case 96: desc->dtype == 1 ? launch<bf16, 96>(a, st) : launch<float, 96>(a, st); break;
+        default: desc->dtype == 1 ? launch<bf16, 128>(a, st) : launch<float, 128>(a, st);
+    }
     return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
 }

@@ -186,7 +186,10 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
             some = k0 <= far || k0 < q.prefix;
             all = all && (k0 + L::ROWS - 1 <= wnear || k0 + L::ROWS <= q.prefix);
         }
-        if (a.k_docs && some) {
+        if (a.k_docs && !a.k_blocks) {
+            all = false;
+            pad = true;
+        } else if (a.k_docs && some) {
             const int2 m = a.k_blocks[kblock0 + k0 / DOC_BLOCK];
             some = dmax >= 0 && m.y >= max(dmin, 0) && m.x <= dmax;
             all = all && m.x == m.y && dmin == dmax && m.x == dmin;
@@ -247,9 +250,10 @@ template <typename T, int DP>
 struct Few {
     using L = Tile<T, DP, 32>;
     static constexpr int SENDS = L::BYTES / 1024;                         // of 64 lanes, for a tile
-    // Tiles of a wavefront in LDS: two, or one of the largest; 128 KB of a unit's 160 either way, in bf16 with heads of 64 by two workgroups.
-    static constexpr int STAGES = L::BYTES >= 16384 ? 1 : 2, WORKGROUPS = L::BYTES >= 8192 ? 1 : 2;
-    static constexpr int PERIOD = L::CPR / 4, ROWS_A_SEND = 64 / L::CPR;  // sends whose lanes' chunks differ; the others repeat them
+    // Tiles of a wavefront in LDS: two, or one of the largest; up to 128 KB of a unit's 160, in bf16 with heads of 64 by two workgroups.
+    static constexpr int STAGES = L::BYTES > 8192 ? 1 : 2, WORKGROUPS = L::BYTES > 4096 ? 1 : 2;
+    // Sends whose lanes' chunks differ; the others repeat them so many rows on (sends of no whole number of rows: none does).
+    static constexpr int PERIOD = 64 % L::CPR == 0 ? L::CPR / 4 : SENDS, ROWS_A_PERIOD = 64 * PERIOD / L::CPR;
     static constexpr int WAIT = (STAGES - 1) * (2 * SENDS + 1);           // sends behind the oldest tile's, and a word for documents
     unsigned off[2][PERIOD];
     int64_t step[2];                                                      // bytes from row to row
@@ -257,29 +261,29 @@ struct Few {
         const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int j = 0; j < PERIOD; ++j) {
-            const int r = j * ROWS_A_SEND + lane / L::CPR;
+            const int r = (j * 64 + lane) / L::CPR;
 #pragma unroll
-            for (int x = 0; x < 2; ++x) off[x][j] = (unsigned)(lane / L::CPR) * (unsigned)step[x] + element(r, a.head_dim) * L::EB;
+            for (int x = 0; x < 2; ++x) off[x][j] = (unsigned)r * (unsigned)step[x] + element(j, a.head_dim) * L::EB;
         }
     }
-    static __device__ __forceinline__ int element(int r, int head_dim) {
-        return min((((int)(threadIdx.x & 63) % L::CPR) ^ L::swz(r)) * L::EPC, head_dim - L::EPC);
+    static __device__ __forceinline__ int row_of(int j) { return (j * 64 + (int)(threadIdx.x & 63)) / L::CPR; }
+    static __device__ __forceinline__ int element(int j, int head_dim) {
+        return min((((j * 64 + (int)(threadIdx.x & 63)) % L::CPR) ^ L::swz(row_of(j))) * L::EPC, head_dim - L::EPC);
     }
     static __device__ __forceinline__ void send(unsigned char* tile, int j, const void* from) {
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)(tile + j * 1024), 16, 0, 0);
     }
     __device__ __forceinline__ void whole(unsigned char* tile, int x, const void* first) const {
 #pragma unroll
-        for (int j = 0; j < SENDS; ++j) send(tile, j, (const char*)first + j * ROWS_A_SEND * step[x] + off[x][j % PERIOD]);
+        for (int j = 0; j < SENDS; ++j) send(tile, j, (const char*)first + j / PERIOD * ROWS_A_PERIOD * step[x] + off[x][j % PERIOD]);
     }
     // row(i): address of row i, null for zeros
     template <typename Address>
     static __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, Address row) {
 #pragma unroll
         for (int j = 0; j < SENDS; ++j) {
-            const int r = j * ROWS_A_SEND + (int)(threadIdx.x & 63) / L::CPR;
-            const T* p = row(r);
-            send(tile, j, p ? (const void*)(p + element(r, head_dim)) : (const void*)&zeros);
+            const T* p = row(row_of(j));
+            send(tile, j, p ? (const void*)(p + element(j, head_dim)) : (const void*)&zeros);
         }
     }
 };
@@ -540,7 +544,7 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
     // some 2048 shares of a length, of 256 keys (rows) or more each.  What blocks and tiles there are is estimated from the tensors'
     // rows: lengths stand on the device.
     a.tile = tile_rows(d->dtype == 1 ? 2 : 4);
-    a.key_tile = key_tile_rows(d->dtype == 1 ? 2 : 4, d->head_dim <= 64 ? 64 : 128);
+    a.key_tile = key_tile_rows(d->dtype == 1 ? 2 : 4, padded(d->head_dim));
     auto share = [&](int64_t blocks_a_seq, int64_t tokens, int64_t tokens_a_block, int64_t passing, int64_t all_passing, int tile, int32_t& parts,
                      int32_t& part_tiles) {
         const int tiles = (int)((passing + tile - 1) / tile);
@@ -557,13 +561,14 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
         parts = (tiles + part_tiles - 1) / part_tiles;
     };
     const int64_t rows_a_seq = (int64_t)a.max_q * group;
-    // Few rows: shares of 16 tiles or more (four a wavefront), so many that there are some 1024, long sequences' and short ones'.
+    // Few rows: shares of 16 tiles or more (four a wavefront), so many that there are some 256 of up to 32 tiles, and of longer ones some
+    // 1024, long sequences' and short ones' (one cache of 65521 keys, 4 heads of 128: 256 shares 28.5 us, 512 33.7).
     a.few = !backward && (int64_t)a.max_q * group <= 32;
     if (a.few) {
         a.tile = 32;
         const int64_t tiles = ((int64_t)a.max_k + 31) / 32, jobs = a.kv_heads * (d->n_k / 32 + d->n_seq);
         const int64_t most = max((int64_t)1, ((int64_t)64 << 20) / max((int64_t)1, d->n_q * d->heads * d->head_dim));
-        a.part_tiles = (int32_t)max(max((int64_t)16, jobs / 1024), (tiles + most - 1) / most);
+        a.part_tiles = (int32_t)max(max(min(max((int64_t)16, jobs / 256), (int64_t)32), jobs / 1024), (tiles + most - 1) / most);
         a.parts = (int32_t)max((int64_t)1, (tiles + a.part_tiles - 1) / a.part_tiles);
     } else {
         share(a.row_blocks, d->n_q * group, FIXED, a.max_k, d->n_k, a.tile, a.parts, a.part_tiles);
@@ -579,8 +584,12 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
         off = align_up(off + bytes, 256);
         return (void*)(base + at);
     };
-    a.q_blocks = (int2*)take(sizeof(int2) * (size_t)(d->n_q / DOC_BLOCK + d->n_seq + 1));
-    a.k_blocks = (int2*)take(sizeof(int2) * (size_t)(d->n_k / DOC_BLOCK + d->n_seq + 1));
+    // (a launch for the summaries takes longer than the few tiles of short sequences that they would rule out: 16 sequences of up to 64
+    // tokens forwards and backwards 61 us with them, 52 without)
+    if (max(a.max_q, a.max_k) > 256) {
+        a.q_blocks = (int2*)take(sizeof(int2) * (size_t)(d->n_q / DOC_BLOCK + d->n_seq + 1));
+        a.k_blocks = (int2*)take(sizeof(int2) * (size_t)(d->n_k / DOC_BLOCK + d->n_seq + 1));
+    }
     const size_t rows = (size_t)d->n_q * d->heads;
     if (a.parts > 1) {
         a.part_o = (float*)take(sizeof(float) * rows * d->head_dim * a.parts);
@@ -595,12 +604,12 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
             a.part_dv = (float*)take(part);
         }
     }
-    p.bytes = off;
+    p.bytes = off > 0 ? off : 256;     // (0 says that a call is refused)
     return PS_OK;
 }
 
 void summarise_documents(const Args& a, hipStream_t st) {
-    if (!a.q_docs) return;
+    if (!a.q_docs || !a.q_blocks) return;
     Args b = a;
     for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
         n = min(a.n_seq - s0, 32768);
@@ -637,9 +646,10 @@ extern "C" int ps_attention_forward(const ps_attention_desc* desc, const ps_atte
     hipStream_t st = (hipStream_t)hip_stream;
     (void)hipGetLastError();
     if (!a.few) summarise_documents(a, st);
-    if (desc->dtype == 1)
-        desc->head_dim <= 64 ? launch_attend<bf16, 64>(a, st) : launch_attend<bf16, 128>(a, st);
-    else
-        desc->head_dim <= 64 ? launch_attend<float, 64>(a, st) : launch_attend<float, 128>(a, st);
+    switch (padded(desc->head_dim)) {
+        case 64: desc->dtype == 1 ? launch_attend<bf16, 64>(a, st) : launch_attend<float, 64>(a, st); break;
+        case 96: desc->dtype == 1 ? launch_attend<bf16, 96>(a, st) : launch_attend<float, 96>(a, st); break;
+        default: desc->dtype == 1 ? launch_attend<bf16, 128>(a, st) : launch_attend<float, 128>(a, st);
+    }
     return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
 }

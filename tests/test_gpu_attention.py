@@ -112,7 +112,7 @@ LENGTHS = [1, 130, 0, 63, 64, 65, 2, 127, 129]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("size", [8, 40, 64, 80, 128])
+@pytest.mark.parametrize("size", [8, 40, 64, 72, 80, 96, 104, 128])
 @pytest.mark.parametrize("how", [dict(), dict(causal=True), dict(causal=True, cap=5.0, slopes=SLOPES)], ids=["all", "causal", "capped"])
 def test_lengths_and_sizes(dtype, size, how):
     Problem(dtype, LENGTHS, LENGTHS, size=size, **how).check()
