@@ -45,6 +45,7 @@ struct Args {
     int32_t row_blocks;                // blocks of FIXED rows that the grid has for every sequence
     int32_t parts, part_tiles;         // shares of a row block's key tiles, and tiles of a share
     int32_t key_parts, key_part_tiles; // shares of a key block's row tiles
+    int32_t listed;                    // workgroups find their work by adding up what there is
     int32_t few;                       // at most 32 rows to a key head
     int32_t tile, key_tile;            // rows of a tile that passes by fixed queries, by fixed keys
     uint32_t by_group;                 // 2^32 / group + 1 (group > 1)
@@ -73,20 +74,104 @@ __device__ __forceinline__ bool sequence(const Args& a, int s, Seq& r) {
 
 __device__ __forceinline__ unsigned over_group(const Args& a, unsigned r) { return a.group == 1 ? r : __umulhi(r, a.by_group); }
 
-// Sequence and block of a workgroup: `together` sequences take turns, block by block, then the next so many.  Blocks come in order of
-// their work, most first.  In a launch of few blocks all sequences take turns, so that the last to start are short (two rows of 8192
+// Tiles of keys, from the first on, that some of the FIXED rows from r0 on may see; tiles of rows, from `first` on, that may see some of
+// the FIXED keys from k0 on.  Shares are of these.
+__device__ __forceinline__ int key_tiles(const Args& a, const Seq& q, int r0) {
+    const int far = q.start + (int)over_group(a, min(r0 + FIXED, q.qn * a.group) - 1);
+    return (max(0, a.causal ? min(q.kn, max(far + 1, q.prefix)) : q.kn) + a.tile - 1) / a.tile;
+}
+__device__ __forceinline__ int row_tiles(const Args& a, const Seq& q, int k0, int& first) {
+    const int rows = q.qn * a.group, n = (rows + a.key_tile - 1) / a.key_tile;
+    first = a.causal && k0 >= q.prefix ? (int)min((int64_t)n, max((int64_t)0, (int64_t)(k0 - q.start) * a.group / a.key_tile)) : 0;
+    return n;
+}
+__device__ __forceinline__ int shares(int tiles, int parts, int part_tiles) { return max(1, min(parts, (tiles + part_tiles - 1) / part_tiles)); }
+
+// A workgroup's part of a launch over blocks of rows (of keys, with KEYS) and shares of their tiles.
+// Sequence and block as the grid counts them: `together` sequences take turns, block by block, then the next so many.  Blocks come in order
+// of their work, most first.  In a launch of few blocks all sequences take turns, so that the last to start are short (two rows of 8192
 // tokens, forwards / keys' gradients: 119 / 243 us one after the other, 108 / 226 in turns; 16 x 2048, keys' 1213, 993); in one of many
 // only as many as fill the chip, so that blocks that run at a time read the same keys from the caches (16 x 2048, forwards / queries':
-// 460 / 609 us two at a time, 540 / 727 eight).  Blocks that are shared out are alike (fp32 heads of 80, keys' 233 us, 284 in turns).
-__device__ __forceinline__ void block_of(const Args& a, unsigned id, int blocks, int& s, int& block) {
-    const unsigned turn = id / (unsigned)(blocks * a.together), first = turn * a.together, rest = id - first * blocks;
-    const unsigned here = min((unsigned)a.together, a.seqs - first);
-    block = rest / here;
-    s = a.seq0 + first + rest % here;
-}
-inline int32_t turns(int64_t blocks_a_seq, int32_t parts, int32_t seqs) {
-    if (parts == 1 && blocks_a_seq * seqs <= 2048) return seqs;
+// 460 / 609 us two at a time, 540 / 727 eight).
+inline int32_t turns(int64_t blocks_a_seq, int32_t seqs) {
+    if (blocks_a_seq * seqs <= 2048) return seqs;
     return (int32_t)(blocks_a_seq >= 512 ? 1 : 512 / blocks_a_seq);
+}
+struct Work {
+    int s, hk, block, part;
+};
+template <bool KEYS>
+__device__ __forceinline__ int shares_of(const Args& a, const Seq& q, int block) {
+    const int n = KEYS ? q.kn : q.qn * a.group;
+    if (block * FIXED >= n) return 0;
+    if ((KEYS ? a.key_parts : a.parts) == 1) return 1;
+    int first = 0;
+    const int tiles = KEYS ? row_tiles(a, q, block * FIXED, first) : key_tiles(a, q, block * FIXED);
+    return shares(tiles - first, KEYS ? a.key_parts : a.parts, KEYS ? a.key_part_tiles : a.part_tiles);
+}
+// a.listed (at most 64 sequences of at most 64 blocks): the grid has a workgroup for what there could be, and the first so many take
+// what there is, found by adding it up a sequence to a lane.  Counted as the grid counts, what there is lay anywhere among it, and
+// three or more long workgroups on one unit beside empty ones (8 sequences of 100 to 1023 tokens, 408 workgroups of 2048 with work to do: 26 to
+// 40 tiles on the fullest units, 10 on average).
+template <bool KEYS>
+__device__ __forceinline__ bool look_for_work(const Args& a, Seq& q, Work& w) {
+    const int blocks = KEYS ? (a.max_k + FIXED - 1) / FIXED : a.row_blocks, parts = KEYS ? a.key_parts : a.parts, lane = threadIdx.x & 63;
+    unsigned id = blockIdx.x;
+    w.hk = id % a.kv_heads;
+    id /= a.kv_heads;
+    if (!a.listed) {
+        w.part = id % parts;
+        id /= parts;
+        const unsigned turn = id / (unsigned)(blocks * a.together), first = turn * a.together, rest = id - first * blocks;
+        const unsigned here = min((unsigned)a.together, a.seqs - first);
+        w.block = rest / here;
+        if (!KEYS) w.block = blocks - 1 - w.block;
+        w.s = a.seq0 + first + rest % here;
+        if (!sequence(a, w.s, q)) {
+            if (!KEYS && threadIdx.x == 0 && w.hk == 0 && w.block == 0 && w.part == 0) report_fault(a.status, PS_ST_BAD_LENGTH, w.s);
+            return false;
+        }
+        return w.block * FIXED < (KEYS ? q.kn : q.qn * a.group);
+    }
+    auto sum_in_front = [&](int v, int& upto) {                            // over the lanes
+        upto = v;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int u = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += u;
+        }
+        return upto - v;
+    };
+    Seq mine = {};
+    const bool there = lane < a.seqs, good = there && sequence(a, a.seq0 + lane, mine);
+    if (there && !good && !KEYS && blockIdx.x == 0 && threadIdx.x < 64) report_fault(a.status, PS_ST_BAD_LENGTH, a.seq0 + lane);
+    int n = 0, upto;
+    if (good)
+        for (int b = 0; b < blocks; ++b) {
+            const int c = shares_of<KEYS>(a, mine, b);
+            if (c == 0) break;
+            n += c;
+        }
+    const int front = sum_in_front(n, upto), s = __popcll(__ballot(upto <= (int)id));
+    if (s >= a.seqs) return false;
+    id -= __builtin_amdgcn_readlane(front, s);
+    w.s = a.seq0 + s;
+    sequence(a, w.s, q);
+    const int own = ((KEYS ? q.kn : q.qn * a.group) + FIXED - 1) / FIXED, b = KEYS ? lane : own - 1 - lane;   // (most work first)
+    const int in_front = sum_in_front(b >= 0 ? shares_of<KEYS>(a, q, b) : 0, upto), at = __popcll(__ballot(upto <= (int)id));
+    w.block = KEYS ? at : own - 1 - at;
+    w.part = (int)id - __builtin_amdgcn_readlane(in_front, at);
+    return true;
+}
+
+// The same, as scalars: the compiler does not see that all lanes have found the same.
+template <bool KEYS>
+__device__ __forceinline__ bool find_work(const Args& a, Seq& q, Work& w) {
+    if (!look_for_work<KEYS>(a, q, w)) return false;
+    int* const x[] = {&q.q0, &q.qn, &q.k0, &q.kn, &q.start, &q.prefix, &w.s, &w.hk, &w.block, &w.part};
+#pragma unroll
+    for (int i = 0; i < 10; ++i) *x[i] = __builtin_amdgcn_readfirstlane(*x[i]);
+    return true;
 }
 
 // Where sequence summaries of documents start: sequences never share one.
@@ -291,14 +376,18 @@ static __device__ const uint32_t infinity_word = 0x7f800000u, minus_one = 0xffff
 // Sends for tiles: 16 bytes a lane go from memory into LDS without a register (a lane picks the chunk whose swizzled place it
 // fills).  Landed after vm_wait() and a barrier.  Chunks behind a head's elements repeat its last one: they meet zeros in the fixed
 // rows, or make features that nobody stores.
-template <typename T, int DP, int R = tile_rows(sizeof(T))>
+// ROWS_ARE_TOKENS: group is 1.  A thread's chunks are then, for most lengths of a row, the same one so many rows apart.
+template <typename T, int DP, int R = tile_rows(sizeof(T)), bool ROWS_ARE_TOKENS = false>
 struct Sender {
     using L = Tile<T, DP, R>;
-    unsigned off[L::PER_THREAD];       // where a lane's chunks lie from the tile's first element on, in bytes
+    static constexpr bool SAME = ROWS_ARE_TOKENS && 256 % L::CPR == 0 && 256 / L::CPR % 16 == 0;
+    static constexpr int N = SAME ? 1 : L::PER_THREAD, ROWS_APART = 256 / L::CPR;
+    unsigned off[N];                   // where a lane's chunks lie from the tile's first element on, in bytes
+    int64_t apart;
     bool regular;                      // the same in every tile
-    static __device__ __forceinline__ int row_of(int j) { return (j * 256 + (int)threadIdx.x) / L::CPR; }
-    static __device__ __forceinline__ int element(int j, int head_dim) {
-        return min((((j * 256 + (int)threadIdx.x) % L::CPR) ^ L::swz(row_of(j))) * L::EPC, head_dim - L::EPC);
+    static __device__ __forceinline__ int row_of(int j, int thread) { return (j * 256 + thread) / L::CPR; }
+    static __device__ __forceinline__ int element(int j, int thread, int head_dim) {
+        return min((((j * 256 + thread) % L::CPR) ^ L::swz(row_of(j, thread))) * L::EPC, head_dim - L::EPC);
     }
     static __device__ __forceinline__ void send(unsigned char* tile, int j, const void* from) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -308,24 +397,26 @@ struct Sender {
     // rows of `group` heads to a token
     __device__ __forceinline__ Sender(const ps_strides& s, int group, int head_dim) {
         regular = R % group == 0 && s.row < 1 << 20 && s.head < 1 << 20;
+        apart = SAME ? ROWS_APART * s.row * L::EB : 0;
 #pragma unroll
-        for (int j = 0; j < L::PER_THREAD; ++j) {
-            const int r = row_of(j), token = r / group;
-            off[j] = regular ? (unsigned)(token * (int)s.row + (r - token * group) * (int)s.head + element(j, head_dim)) * L::EB : 0u;
+        for (int j = 0; j < N; ++j) {
+            const int r = row_of(j, threadIdx.x), token = r / group;
+            off[j] = regular ? (unsigned)(token * (int)s.row + (r - token * group) * (int)s.head + element(j, threadIdx.x, head_dim)) * L::EB : 0u;
         }
     }
-    static __device__ __forceinline__ void whole(unsigned char* tile, const T* first, const unsigned (&off)[L::PER_THREAD]) {
+    static __device__ __forceinline__ void whole(unsigned char* tile, const T* first, const unsigned (&off)[N], int64_t apart = 0) {
 #pragma unroll
-        for (int j = 0; j < L::PER_THREAD; ++j) send(tile, j, (const char*)first + off[j]);
+        for (int j = 0; j < L::PER_THREAD; ++j) send(tile, j, (const char*)first + (SAME ? j * apart : 0) + off[SAME ? 0 : j]);
     }
-    __device__ __forceinline__ void whole(unsigned char* tile, const T* first) const { whole(tile, first, off); }
-    // row(i): address of passing row i's element 0; null for a row of zeros.
+    __device__ __forceinline__ void whole(unsigned char* tile, const T* first) const { whole(tile, first, off, apart); }
+    // row(i): address of passing row i's element 0; null for a row of zeros.  (Worked out anew for the few tiles that need it.)
     template <typename Row>
     static __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, Row row) {
+        const int thread = anew<256>((int)threadIdx.x);
 #pragma unroll
         for (int j = 0; j < L::PER_THREAD; ++j) {
-            const T* p = row(row_of(j));
-            send(tile, j, p ? (const void*)(p + element(j, head_dim)) : (const void*)&zeros);
+            const T* p = row(row_of(j, thread));
+            send(tile, j, p ? (const void*)(p + element(j, thread, head_dim)) : (const void*)&zeros);
         }
     }
 };
@@ -426,5 +517,6 @@ struct Plan {
 int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, void* workspace, Plan& p);
 int check_strides(const ps_attention_desc* d, const ps_strides& s, const void* base, bool written, int64_t heads);
 void summarise_documents(const Args& a, hipStream_t st);
+bool add_up(int32_t seqs, int64_t blocks, int32_t parts);
 
 }  // namespace seqatt

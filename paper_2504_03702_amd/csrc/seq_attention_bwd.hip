@@ -97,21 +97,16 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     __shared__ __align__(16) float s_lse[2][64], s_delta[2][64], s_slope[2][64];
     __shared__ __align__(16) int s_place[2][64], s_doc[2][64];
 
-    unsigned id = blockIdx.x;
-    const int hk = id % a.kv_heads;
-    id /= a.kv_heads;
-    const int part = id % a.key_parts;
-    id /= a.key_parts;
-    int s, kb;
-    block_of(a, id, (a.max_k + FIXED - 1) / FIXED, s, kb);                // (causal: the keys that most rows see first)
     Seq q;
-    if (!sequence(a, s, q)) return;                                       // (reported by the queries' launch)
-    const int k0 = kb * FIXED;
-    if (k0 >= q.kn) return;
+    Work w;
+    if (!find_work<true>(a, q, w)) return;                                // (faulty sequences: reported by the queries' launch)
+    const int hk = w.hk, s = w.s, part = w.part, k0 = w.block * FIXED;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-    const int rows = q.qn * a.group, tiles = (rows + L::ROWS - 1) / L::ROWS;
-    const int t0 = part * a.key_part_tiles, t1 = min(tiles, t0 + a.key_part_tiles);
-    if (t0 > 0 && t0 >= tiles) return;                                    // (part 0 writes, rows or not)
+    const int rows = q.qn * a.group;
+    int first_tile;
+    const int tiles = row_tiles(a, q, k0, first_tile);
+    const int t0 = first_tile + part * a.key_part_tiles, t1 = min(tiles, t0 + a.key_part_tiles);
+    if (part > 0 && t0 >= tiles) return;                                  // (part 0 writes, rows or not)
 
     // this lane's key
     const int wk0 = k0 + 32 * wave, key = wk0 + col;
@@ -282,23 +277,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][keys, values]
     __shared__ __align__(16) int s_doc[2][64];
 
-    unsigned id = blockIdx.x;
-    const int hk = id % a.kv_heads;
-    id /= a.kv_heads;
-    const int part = id % a.parts;
-    id /= a.parts;
-    int s, rb;
-    block_of(a, id, a.row_blocks, s, rb);
-    rb = a.row_blocks - 1 - rb;
     Seq q;
-    if (!sequence(a, s, q)) {
-        if (threadIdx.x == 0 && hk == 0 && rb == 0 && part == 0) report_fault(a.status, PS_ST_BAD_LENGTH, s);
-        return;
-    }
-    const int rows = q.qn * a.group, r0 = rb * FIXED;
-    if (r0 >= rows) return;
+    Work w;
+    if (!find_work<false>(a, q, w)) return;
+    const int hk = w.hk, s = w.s, part = w.part, rows = q.qn * a.group, r0 = w.block * FIXED;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-    const int tiles = (q.kn + L::ROWS - 1) / L::ROWS;
+    const int tiles = key_tiles(a, q, r0);
     const int t0 = part * a.part_tiles, t1 = min(tiles, t0 + a.part_tiles);
     if (t0 > 0 && t0 >= tiles) return;                                    // (part 0 writes, keys or not)
 
@@ -373,7 +357,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
 
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
-    const Sender<T, DP> keys(a.ks, 1, a.head_dim), values(a.vs, 1, a.head_dim);
+    const Sender<T, DP, L::ROWS, true> keys(a.ks, 1, a.head_dim), values(a.vs, 1, a.head_dim);
     const bool regular = keys.regular && values.regular;
     auto request = [&](int t, bool padded, int buf) {
         const int k0 = t * L::ROWS;
@@ -443,8 +427,6 @@ __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
     if (!sequence(a, s, q)) return;
     const int heads = z == 0 ? a.heads : a.kv_heads, of = z == 0 ? a.parts : a.key_parts, each = z == 0 ? a.part_tiles : a.key_part_tiles;
     const ps_strides to = z == 0 ? a.dqs : z == 1 ? a.dks : a.dvs;
-    const int tile = z == 0 ? a.tile : a.key_tile, tiles = ((z == 0 ? q.kn : q.qn * a.group) + tile - 1) / tile;
-    const int parts = max(1, min(of, (tiles + each - 1) / each));
     // (calls of few blocks: all of a tensor's rows are counted in 32 bits)
     const int fours = a.head_dim / 4, n = (z == 0 ? q.qn : q.kn) * heads * fours, token0 = z == 0 ? q.q0 : q.k0;
     const int64_t step = (z == 0 ? a.n_q : a.n_k) * heads * fours;
@@ -452,14 +434,17 @@ __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
     T* out = (T*)(z == 0 ? a.dq : z == 1 ? a.dk : a.dv);
     const float by = z == 2 ? 1.f : by_x<T>(a);
     for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+        const int row = i / fours, mine = row / heads, head = row % heads;
+        int first = 0;
+        const int tiles = z == 0 ? key_tiles(a, q, (mine * a.group + head % a.group) / FIXED * FIXED) : row_tiles(a, q, mine / FIXED * FIXED, first);
+        const int parts = shares(tiles - first, of, each);
         float4 sum = part[i];
 #pragma unroll 4
         for (int p = 1; p < parts; ++p) {
             const float4 v = part[p * step + i];
             sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
         }
-        const int row = i / fours, token = token0 + row / heads;
-        T* at = out + token * to.row + row % heads * to.head + i % fours * 4;
+        T* at = out + (token0 + mine) * to.row + head * to.head + i % fours * 4;
         if constexpr (sizeof(T) == 2)
             *(uint2*)at = make_uint2(cvt_pk_bf16(sum.x * by, sum.y * by), cvt_pk_bf16(sum.z * by, sum.w * by));
         else
@@ -470,30 +455,32 @@ __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
 template <typename T, int DP>
 void launch(const Args& a, hipStream_t st) {
     Args b = a;
-    auto in_turn = [&](int64_t per_seq, int32_t parts, int64_t most_seqs, auto launch_one) {
+    auto in_turn = [&](int64_t per_seq, int64_t most_seqs, auto launch_one) {
         if (per_seq == 0) return;
         const int64_t most = min(most_seqs, max((int64_t)1, (int64_t)(1 << 22) / per_seq));   // (a grid holds fewer than 2^32 threads)
         for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
             n = (int32_t)min((int64_t)(a.n_seq - s0), most);
             b.seq0 = s0;
             b.seqs = n;
-            b.together = turns(per_seq, parts, n);
+            b.together = turns(per_seq, n);
             launch_one((unsigned)n);
         }
     };
     const int64_t row_jobs = (int64_t)a.kv_heads * a.row_blocks * a.parts;
-    const int64_t key_jobs = (int64_t)a.kv_heads * ((a.max_k + FIXED - 1) / FIXED) * a.key_parts;
-    in_turn(row_jobs, a.parts, a.n_seq, [&](unsigned n) {
+    const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED, key_jobs = a.kv_heads * key_blocks * a.key_parts;
+    in_turn(row_jobs, a.n_seq, [&](unsigned n) {
+        b.listed = add_up(n, a.row_blocks, a.parts);
         hipLaunchKernelGGL((query_gradients_kernel<T, DP>), dim3((unsigned)row_jobs * n), dim3(256), 0, st, b);
     });
-    in_turn(key_jobs, a.key_parts, a.n_seq, [&](unsigned n) {
+    in_turn(key_jobs, a.n_seq, [&](unsigned n) {
+        b.listed = add_up(n, key_blocks, a.key_parts);
         hipLaunchKernelGGL((key_gradients_kernel<T, DP>), dim3((unsigned)key_jobs * n), dim3(256), 0, st, b);
     });
     const int z0 = a.parts > 1 ? 0 : 1, z1 = a.key_parts > 1 ? 3 : 1;
     if (z0 == z1) return;
     const int64_t most = max(z0 == 0 ? (int64_t)a.max_q * a.heads : 0, z1 == 3 ? (int64_t)a.max_k * a.kv_heads : 0) * a.head_dim / 4;
     const unsigned blocks = (unsigned)min((most + 255) / 256, (int64_t)4096);
-    in_turn(blocks, 1, 32768, [&](unsigned n) {
+    in_turn(blocks, 32768, [&](unsigned n) {
         hipLaunchKernelGGL(add_kernel<T>, dim3(blocks, n, (unsigned)(z1 - z0)), dim3(256), 0, st, b, z0);
     });
 }

@@ -138,23 +138,12 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][keys, values]
     __shared__ __align__(16) int s_doc[2][64];
 
-    unsigned id = blockIdx.x;
-    const int hk = id % a.kv_heads;
-    id /= a.kv_heads;
-    const int part = PARTS ? id % a.parts : 0;
-    if (PARTS) id /= a.parts;
-    int s, rb;
-    block_of(a, id, a.row_blocks, s, rb);
-    rb = a.row_blocks - 1 - rb;                                           // (causal: the rows with the most keys first)
     Seq q;
-    if (!sequence(a, s, q)) {
-        if (threadIdx.x == 0 && hk == 0 && rb == 0 && part == 0) report_fault(a.status, PS_ST_BAD_LENGTH, s);
-        return;
-    }
-    const int rows = q.qn * a.group, r0 = rb * FIXED;
-    if (r0 >= rows) return;
+    Work w;
+    if (!find_work<false>(a, q, w)) return;
+    const int hk = w.hk, s = w.s, part = PARTS ? w.part : 0, rows = q.qn * a.group, r0 = w.block * FIXED;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-    const int tiles = (q.kn + L::ROWS - 1) / L::ROWS;
+    const int tiles = key_tiles(a, q, r0);
     const int t0 = PARTS ? part * a.part_tiles : 0, t1 = PARTS ? min(tiles, t0 + a.part_tiles) : tiles;
     if (PARTS && t0 > 0 && t0 >= tiles) return;                           // (part 0 writes, keys or not)
 
@@ -200,7 +189,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
 
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
-    const Sender<T, DP> keys(a.ks, 1, a.head_dim), values(a.vs, 1, a.head_dim);
+    const Sender<T, DP, L::ROWS, true> keys(a.ks, 1, a.head_dim), values(a.vs, 1, a.head_dim);
     const bool regular = keys.regular && values.regular;
     auto request = [&](int t, bool padded, int buf) {
         const int k0 = t * L::ROWS;
@@ -261,14 +250,13 @@ struct Few {
         const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int j = 0; j < PERIOD; ++j) {
-            const int r = (j * 64 + lane) / L::CPR;
 #pragma unroll
-            for (int x = 0; x < 2; ++x) off[x][j] = (unsigned)r * (unsigned)step[x] + element(j, a.head_dim) * L::EB;
+            for (int x = 0; x < 2; ++x) off[x][j] = (unsigned)row_of(j, lane) * (unsigned)step[x] + element(j, lane, a.head_dim) * L::EB;
         }
     }
-    static __device__ __forceinline__ int row_of(int j) { return (j * 64 + (int)(threadIdx.x & 63)) / L::CPR; }
-    static __device__ __forceinline__ int element(int j, int head_dim) {
-        return min((((j * 64 + (int)(threadIdx.x & 63)) % L::CPR) ^ L::swz(row_of(j))) * L::EPC, head_dim - L::EPC);
+    static __device__ __forceinline__ int row_of(int j, int lane) { return (j * 64 + lane) / L::CPR; }
+    static __device__ __forceinline__ int element(int j, int lane, int head_dim) {
+        return min((((j * 64 + lane) % L::CPR) ^ L::swz(row_of(j, lane))) * L::EPC, head_dim - L::EPC);
     }
     static __device__ __forceinline__ void send(unsigned char* tile, int j, const void* from) {
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)(tile + j * 1024), 16, 0, 0);
@@ -280,10 +268,11 @@ struct Few {
     // row(i): address of row i, null for zeros
     template <typename Address>
     static __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, Address row) {
+        const int lane = anew<256>((int)(threadIdx.x & 63));
 #pragma unroll
         for (int j = 0; j < SENDS; ++j) {
-            const T* p = row(row_of(j));
-            send(tile, j, p ? (const void*)(p + element(j, head_dim)) : (const void*)&zeros);
+            const T* p = row(row_of(j, lane));
+            send(tile, j, p ? (const void*)(p + element(j, lane, head_dim)) : (const void*)&zeros);
         }
     }
 };
@@ -309,8 +298,9 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
     }
     const int rows = q.qn * a.group;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-    const int tiles = (q.kn + 31) / 32, t0 = part * a.part_tiles, t1 = min(tiles, t0 + a.part_tiles);
-    if (rows == 0 || (t0 > 0 && t0 >= tiles)) return;                     // (part 0 writes, keys or not)
+    if (rows == 0) return;
+    const int tiles = key_tiles(a, q, 0), t0 = part * a.part_tiles, t1 = min(tiles, t0 + a.part_tiles);
+    if (t0 > 0 && t0 >= tiles) return;                                    // (part 0 writes, keys or not)
 
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
@@ -412,7 +402,8 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
     const int i = min((int)blockIdx.x * (4 / W) + wave / W, q.qn * a.heads - 1);
     const int64_t row = (int64_t)q.q0 * a.heads + i, token = q.q0 + i / a.heads;
     const int head = i % a.heads;
-    const int tiles = (q.kn + a.tile - 1) / a.tile, parts = max(1, min(a.parts, (tiles + a.part_tiles - 1) / a.part_tiles));
+    const int block = (i / a.heads * a.group + head % a.group) / FIXED;
+    const int parts = shares(key_tiles(a, q, block * FIXED), a.parts, a.part_tiles);
     const int64_t step = a.n_q * a.heads;
     float m = -INFINITY;
     for (int p = lane; p < parts; p += 64) m = fmaxf(m, a.part_ml[p * step + row].x);
@@ -478,7 +469,8 @@ void launch_attend(const Args& a, hipStream_t st) {
         n = (int32_t)min((int64_t)(a.n_seq - s0), most);
         b.seq0 = s0;
         b.seqs = n;
-        b.together = turns(per_seq, a.parts, n);
+        b.together = turns(per_seq, n);
+        b.listed = add_up(n, a.row_blocks, a.parts);
         const dim3 grid((unsigned)(per_seq * n));
         if (a.few)
             hipLaunchKernelGGL((attend_few_kernel<T, DP>), grid, dim3(256), 0, st, b);
@@ -509,6 +501,10 @@ bool good_strides(const ps_attention_desc* d, const ps_strides& s) {
 }  // namespace
 
 namespace seqatt {
+
+// Whether workgroups add up what work there is: where blocks are shared out, which leaves much of the grid without any.  Of whole blocks
+// the empty ones do not matter (64 sequences of 4 to 512 tokens, forwards / keys' gradients 37 / 53 us, 41 / 54 added up).
+bool add_up(int32_t seqs, int64_t blocks, int32_t parts) { return seqs <= 64 && blocks <= 64 && parts > 1; }
 
 // A tensor that a call reads or writes.  Heads or rows of a written one may not fall on one another.
 int check_strides(const ps_attention_desc* d, const ps_strides& s, const void* base, bool written, int64_t heads) {
