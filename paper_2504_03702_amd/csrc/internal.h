@@ -261,3 +261,9 @@ struct ProfScope {
 };
 
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+// Whether no two elements of a tensor [rows][heads][size] that a call writes are the same: heads lie within rows, or rows within heads.
+static inline bool strides_apart(const ps_strides& s, int64_t rows, int64_t heads, int64_t size) {
+    if (rows <= 1 || heads <= 1) return (rows <= 1 || s.row >= size) && (heads <= 1 || s.head >= size);
+    return (s.head >= size && s.row >= (heads - 1) * s.head + size) || (s.row >= size && s.head >= (rows - 1) * s.row + size);
+}

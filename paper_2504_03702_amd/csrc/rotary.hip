@@ -88,8 +88,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
 }
 
 bool strides_ok(const ps_strides& s, bool written, int heads, int head_dim, int64_t rows) {
-    if (s.row < 0 || s.head < 0) return false;
-    return !written || ((heads <= 1 || s.head >= head_dim) && (rows <= 1 || s.row >= head_dim));
+    return s.row >= 0 && s.head >= 0 && (!written || strides_apart(s, rows, heads, head_dim));
 }
 
 template <typename T>

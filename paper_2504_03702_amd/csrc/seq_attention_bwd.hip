@@ -499,11 +499,11 @@ extern "C" int ps_attention_backward(const ps_attention_desc* desc, const ps_att
     if (code != PS_OK) return code;
     if (p.a.n_seq == 0 || (p.a.n_q == 0 && p.a.n_k == 0)) return PS_OK;
     const ps_attention_desc* d = desc;
-    if (p.a.n_q > 0 && (check_strides(d, d->q, q, false, d->heads) || check_strides(d, d->out, out, false, d->heads) || !lse ||
-                        check_strides(d, d->dout, dout, false, d->heads) || check_strides(d, d->dq, dq, true, d->heads)))
+    if (p.a.n_q > 0 && (check_strides(d, d->q, q, d->n_q, d->heads, false) || check_strides(d, d->out, out, d->n_q, d->heads, false) || !lse ||
+                        check_strides(d, d->dout, dout, d->n_q, d->heads, false) || check_strides(d, d->dq, dq, d->n_q, d->heads, true)))
         return PS_EINVAL;
-    if (p.a.n_k > 0 && (check_strides(d, d->k, k, false, d->kv_heads) || check_strides(d, d->v, v, false, d->kv_heads) ||
-                        check_strides(d, d->dk, dk, true, d->kv_heads) || check_strides(d, d->dv, dv, true, d->kv_heads)))
+    if (p.a.n_k > 0 && (check_strides(d, d->k, k, d->n_k, d->kv_heads, false) || check_strides(d, d->v, v, d->n_k, d->kv_heads, false) ||
+                        check_strides(d, d->dk, dk, d->n_k, d->kv_heads, true) || check_strides(d, d->dv, dv, d->n_k, d->kv_heads, true)))
         return PS_EINVAL;
     if (((uintptr_t)out_rest & 15) != 0 || (out_rest && d->dtype != 1) || (uintptr_t)lse % 4 != 0) return PS_EINVAL;
     if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < p.bytes) return PS_EWORKSPACE;

@@ -507,10 +507,9 @@ namespace seqatt {
 bool add_up(int32_t seqs, int64_t blocks, int32_t parts) { return seqs <= 64 && blocks <= 64 && parts > 1; }
 
 // A tensor that a call reads or writes.  Heads or rows of a written one may not fall on one another.
-int check_strides(const ps_attention_desc* d, const ps_strides& s, const void* base, bool written, int64_t heads) {
+int check_strides(const ps_attention_desc* d, const ps_strides& s, const void* base, int64_t rows, int64_t heads, bool written) {
     if (!base || ((uintptr_t)base & 15) != 0 || !good_strides(d, s)) return PS_EINVAL;
-    if (written && ((heads > 1 && s.head < d->head_dim) || s.row < d->head_dim)) return PS_EINVAL;
-    return PS_OK;
+    return written && !strides_apart(s, rows, heads, d->head_dim) ? PS_EINVAL : PS_OK;
 }
 
 int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, void* workspace, Plan& p) {
@@ -632,8 +631,10 @@ extern "C" int ps_attention_forward(const ps_attention_desc* desc, const ps_atte
     const int code = plan(desc, seqs, false, workspace, p);
     if (code != PS_OK) return code;
     if (p.a.n_seq == 0 || p.a.n_q == 0 || p.a.max_q == 0) return PS_OK;
-    if (check_strides(desc, desc->q, q, false, desc->heads) || check_strides(desc, desc->out, out, true, desc->heads)) return PS_EINVAL;
-    if (p.a.n_k > 0 && (check_strides(desc, desc->k, k, false, desc->kv_heads) || check_strides(desc, desc->v, v, false, desc->kv_heads)))
+    if (check_strides(desc, desc->q, q, desc->n_q, desc->heads, false) ||
+        check_strides(desc, desc->out, out, desc->n_q, desc->heads, true)) return PS_EINVAL;
+    if (p.a.n_k > 0 && (check_strides(desc, desc->k, k, desc->n_k, desc->kv_heads, false) ||
+                         check_strides(desc, desc->v, v, desc->n_k, desc->kv_heads, false)))
         return PS_EINVAL;
     if (((uintptr_t)out_rest & 15) != 0 || (out_rest && desc->dtype != 1) || (uintptr_t)lse % 4 != 0) return PS_EINVAL;
     if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < p.bytes) return PS_EWORKSPACE;
