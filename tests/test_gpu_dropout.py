@@ -62,6 +62,12 @@ def test_long_columns(dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(767, 20), (768, 8), (769, 100), (800, 1030)])
+def test_one_row_block_and_more(dtype, rows, cols):
+    test_both_directions(dtype, rows, cols, 0.25, True, True)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_strides_and_places(dtype):
     """Rows apart, at any element, in place over x or the residual: the mask goes by row and column alone."""
     x, r, b = torch.randn(50, 96, device=DEV).to(dtype), torch.randn(50, 96, device=DEV).to(dtype), torch.randn(96, device=DEV).to(dtype)
