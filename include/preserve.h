@@ -324,11 +324,12 @@ size_t ps_attention_workspace_bytes(const ps_attention_desc* desc, int backward)
  * out_rest: NULL, or in a bf16 call a dense [n_q][heads][head_dim] bf16 tensor for what the rounding of out to bf16 left (NULL in fp32
  * calls, which leave nothing).  The backward call takes it for dout . out, see there.
  * A key row's contents matter to nobody if it lies behind its sequence's keys or is padding.  Among the others, rows of v that a
- * query does not see take part in its sums with weight 0 and have to be finite; masked scores may be anything.
+ * query does not see take part in its sums with weight 0 and have to be finite (in the backward call, those of q, k and dout too); masked
+ * scores may be anything.
  * status: a sequence whose offsets or lengths break the rules, or pass n_q, n_k, max_q or max_k, is left out (its rows keep what
  * they held) and raises PS_ST_BAD_LENGTH with its index.
  * Errors: PS_EINVAL (null or misaligned pointers, bad sizes, strides or numbers), PS_EWORKSPACE, PS_EUNSUPPORTED (head_dim above 128 or
- * no multiple of 8; max_q * (heads / kv_heads)^2 of 2^31 or more), PS_EHIP.  n_seq, n_q or n_k of 0 are allowed. */
+ * no multiple of 8; sequences of more than 2^30 rows or keys; max_q * (heads / kv_heads)^2 of 2^31 or more), PS_EHIP.  n_seq, n_q or n_k of 0 are allowed. */
 int ps_attention_forward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const void* q, const void* k, const void* v,
                          void* out, float* lse, void* out_rest, void* workspace, size_t workspace_bytes, ps_status* status,
                          void* hip_stream);

@@ -219,11 +219,14 @@ struct Fixed {
         }
         return sum;
     }
+    // `row` has to be readable whether `valid` or not
     __device__ __forceinline__ void load(const T* row, bool valid, int head_dim, int half) {
 #pragma unroll
         for (int i = 0; i < Tile<T, DP>::NF; ++i) {
             const int e = (2 * i + half) * Tile<T, DP>::EPC;
-            c[i] = valid && e < head_dim ? *(const uint4*)(row + e) : make_uint4(0, 0, 0, 0);
+            const uint4 x = *(const uint4*)(row + min(e, head_dim - Tile<T, DP>::EPC));
+            const bool is = valid && e < head_dim;
+            c[i] = make_uint4(is ? x.x : 0, is ? x.y : 0, is ? x.z : 0, is ? x.w : 0);
         }
     }
 };
@@ -305,6 +308,38 @@ __device__ __forceinline__ f32x16 dot(const unsigned char* tile, int b, const F&
         }
     }
     return s;
+}
+
+// Two such products, taken in turns: neither waits for its own last step, or for LDS more than once (documents in two rows of 8192, forwards
+// 108 -> 100 us).
+template <typename T, int DP, typename F, typename G>
+__device__ __forceinline__ void dots(const unsigned char* tile, int b, const F& f, f32x16& s, const unsigned char* tile2, int b2, const G& g, f32x16& s2,
+                                     const Lanes<T, DP>& l) {
+    using L = Tile<T, DP>;
+    if constexpr (L::EB == 4 || F::READS || G::READS) {
+        s = dot<T, DP>(tile, b, f, l);
+        s2 = dot<T, DP>(tile2, b2, g, l);
+    } else {
+        constexpr int N = L::NF <= 4 ? L::NF : L::NF / 2;
+        const int at = anew<L::ROWB>(l.row);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = s2[e] = 0.f;
+#pragma unroll
+        for (int n = 0; n < L::NF; n += N) {
+            uint4 x[N], y[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                x[i] = *(const uint4*)(tile + b * 32 * L::ROWB + L::further(at, 2 * (n + i)));
+                y[i] = *(const uint4*)(tile2 + b2 * 32 * L::ROWB + L::further(at, 2 * (n + i)));
+            }
+            reads_first();
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x[i]), as_bf16x8(f.chunk(n + i, at)), s, 0, 0, 0);
+                s2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(y[i]), as_bf16x8(g.chunk(n + i, at)), s2, 0, 0, 0);
+            }
+        }
+    }
 }
 
 // The weights of a block's 32 passing rows for a lane's fixed row, as the second product takes them: floats, or bf16 in the order of
@@ -427,30 +462,34 @@ __device__ __forceinline__ void send_words(void* to, const void* from) {
 __device__ __forceinline__ void vm_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // ---- which tiles are seen: 64 of them at a time, a lane each, as masks ----------------------------------------------------
+// (scalars: the compiler does not see that all lanes have the same, and would count and address tiles in vector registers)
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t scalars(uint64_t x) { return (uint64_t)(uint32_t)scalar((int)(x >> 32)) << 32 | (uint32_t)scalar((int)x); }
 struct Walk {
     int group = -1;
-    uint64_t seen = 0, whole = 0, padded = 0;
-    // The first tile from t on that is seen, `end` if none is.  classify(tile, whole, padded): whether tile is seen; whether by all; whether
-    // some of it is padding.
+    uint64_t seen = 0, one = 0, padded = 0;
+    // The first tile from t on that is seen, `end` if none is.  classify(tile, one, padded): whether some of the tile is seen; whether its
+    // and the fixed rows are all of one document; whether some of it is padding.
     template <typename Classify>
-    __device__ __forceinline__ int next(int t, int end, Classify classify) {
-        while (t < end) {
+    __device__ __forceinline__ int next(int from, int end, Classify classify) {
+        int t = scalar(from);
+        while (t < scalar(end)) {
             if ((t >> 6) != group) {
                 group = t >> 6;
                 const int mine = group * 64 + (int)(threadIdx.x & 63);
                 bool all = false, pad = false;
                 const bool some = mine < end && classify(mine, all, pad);
-                seen = __ballot(some);
-                whole = __ballot(some && all);
-                padded = __ballot(some && pad);
+                seen = scalars(__ballot(some));
+                one = scalars(__ballot(some && all));
+                padded = scalars(__ballot(some && pad));
             }
             const uint64_t m = seen >> (t & 63);
-            if (m) return t + __builtin_ctzll(m);
+            if (m) return scalar(t + __builtin_ctzll(m));
             t = (group + 1) << 6;
         }
-        return end;
+        return scalar(end);
     }
-    __device__ __forceinline__ bool is_whole(int t) const { return whole >> (t & 63) & 1; }
+    __device__ __forceinline__ bool is_one(int t) const { return one >> (t & 63) & 1; }
     __device__ __forceinline__ bool is_padded(int t) const { return padded >> (t & 63) & 1; }
 };
 
@@ -498,15 +537,48 @@ __device__ __forceinline__ void put_row(T* row, const f32x16 (&acc)[DP / 32], fl
         }
 }
 
-// The same for what rounding to bf16 left of them.
-template <int DP>
-__device__ __forceinline__ void put_rest(__bf16* row, const f32x16 (&acc)[DP / 32], float by, int head_dim, int half) {
-    f32x16 left[DP / 32];
+// The accumulators of a wavefront, [feature][a lane's row] times the lane's `by`, to its 32 rows in memory: by way of LDS, 64 features at a
+// time, so that 8 or 16 lanes write a row's lines whole (64 sequences of 512 tokens, 12 heads of 64, forwards 125 -> 107 us: from the registers
+// a store has 32 pieces of 16 bytes, of 32 lines, and there are 16 of them).  row(r): address of row r's element 0, null if there is none.  mine: PUT_BYTES that no
+// other wavefront uses.  LEFT: not the values, but what their rounding to bf16 leaves.
+constexpr int PUT_BYTES = 32 * 64 * 4;
+template <typename T, int DP, bool LEFT = false, typename Row>
+__device__ __forceinline__ void put_rows(unsigned char* mine, const f32x16 (&acc)[DP / 32], float by, int head_dim, Row row) {
+    using P = Tile<T, 64, 32>;
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
+    for (int p = 0; p < DP / 32; p += 2) {
+        const int here = DP / 32 - p < 2 ? 1 : 2, chunks = here * 32 / P::EPC;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) left[i][e] = acc[i][e] * by - (float)(__bf16)(acc[i][e] * by);
-    put_row<__bf16, DP>(row, left, 1.f, head_dim, half);
+        for (int i = 0; i < here; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[p + i][4 * g + e] * by;
+                if constexpr (P::EB == 2) {
+                    uint2 x;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        uint32_t pair = cvt_pk_bf16(v[2 * e], v[2 * e + 1]);
+                        if (LEFT) pair = cvt_pk_bf16(v[2 * e] - __uint_as_float(pair << 16), v[2 * e + 1] - __uint_as_float(pair & 0xffff0000u));
+                        (&x.x)[e] = pair;
+                    }
+                    *(uint2*)(mine + P::at(col, 4 * i + g) + 8 * half) = x;
+                } else {
+                    *(float4*)(mine + P::at(col, 8 * i + 2 * g + half)) = make_float4(v[0], v[1], v[2], v[3]);
+                }
+            }
+        __builtin_amdgcn_wave_barrier();                                  // (a wavefront's accesses to LDS keep their order)
+#pragma unroll
+        for (int j = 0; j < chunks / 2; ++j) {
+            const int r = (j * 64 + lane) / chunks, chunk = (j * 64 + lane) % chunks, e = 32 * p + chunk * P::EPC;
+            const uint4 x = *(const uint4*)(mine + P::at(r, chunk));
+            T* const to = row(r);
+            if (to && e < head_dim) *(uint4*)(to + e) = x;
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 // Checked arguments as the kernels take them, and the plan of a call; PS_OK or an error.

@@ -11,16 +11,17 @@ namespace {
 
 // The weights p and the gradients d of x = scale q . k (by_x() times d) of one block, from the products s = q . k and g = dout . v, with
 // four neighbours to every j: lse(j) and delta(j), what their queries bring along; distance(j), how far they stand from their keys, times
-// the slope; seen(j, is), which see them.  STEP fours at a time: what is the same for all of them is asked once a step, so four at a time
+// the slope; in_front(j, is) if the block is cut, which of the keys stand in front of their query's end; same(j, is) if it is of several
+// documents, which are of their query's.  STEP fours at a time: what is the same for all of them is asked once a step, so four at a time
 // make straight lines (two rows of 8192 tokens, queries' / keys' gradients 184 / 243 -> 169 / 236 us), and one keeps few registers waiting.
 // rest: what the rounding of d to bf16 leaves.  Where a row's weight lies on few keys it does not average out, and what those keys have in
 // common is multiplied by the sum of the roundings instead of the sum of d, which is zero.  So where weights are like that, in blocks that
 // a mask cuts (rows see few keys) and under a cap (scores are large), a second product makes up for it: 16 x 2048 with prefix and cap,
 // queries' / keys' gradients 596 / 1044 -> 695 / 1103 us, error against 64 bits 2.7e-3 -> 1.8e-3 of the norm (1.7e-3 is that of dq's and dk's
 // own rounding; 2.4e-3 without cap, where a product more would cost 5 to 10 %).
-template <typename T, int STEP, typename Lse, typename Delta, typename Distance, typename Seen>
+template <typename T, int STEP, typename Lse, typename Delta, typename Distance, typename Front, typename Same>
 __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, Weights<T>& p, Weights<T>& d, Weights<T>& rest,
-                                          bool whole, Lse lse, Delta delta, Distance distance, Seen seen) {
+                                          bool cut, bool docs, Lse lse, Delta delta, Distance distance, Front in_front, Same same) {
     const Cap cap = Cap::of<T>(a);
     const float c1 = a.scale * LOG2E;
 #pragma unroll
@@ -57,7 +58,7 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
 #pragma unroll
             for (int i = 0; i < 4; ++i) (&v[k].x)[i] *= g[4 * (j0 + k) + i] - (&t.x)[i];
         }
-        if (!whole) {
+        auto only = [&](auto seen) {
 #pragma unroll
             for (int k = 0; k < STEP; ++k) {
                 bool is[4];
@@ -68,14 +69,16 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
                     (&v[k].x)[i] = is[i] ? (&v[k].x)[i] : 0.f;
                 }
             }
-        }
+        };
+        if (cut) only(in_front);
+        if (docs) only(same);
 #pragma unroll
         for (int k = 0; k < STEP; ++k) {
             p.set(j0 + k, u[k]);
             d.set(j0 + k, v[k]);
         }
         if constexpr (sizeof(T) == 2)
-            if (!whole || a.cap > 0.f) {
+            if (cut || docs || a.cap > 0.f) {
 #pragma unroll
                 for (int k = 0; k < STEP; ++k) {
                     const float4 r = d.get(j0 + k);
@@ -97,8 +100,8 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     constexpr bool IN_LDS = sizeof(T) == 2 && DP == 128;
     __shared__ __align__(1024) unsigned char s_values[IN_LDS ? 4 : 1][IN_LDS ? 32 * L::ROWB : 16];
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][queries, dout]
-    __shared__ __align__(16) float s_lse[2][64], s_delta[2][64], s_slope[2][64];
-    __shared__ __align__(16) int s_place[2][64], s_doc[2][64];
+    __shared__ __align__(16) float s_lse[2][64], s_delta[2][64], s_slope[2][64], s_place[2][64];   // (places from k0 on)
+    __shared__ __align__(16) int s_doc[2][64];
 
     Seq q;
     Work w;
@@ -129,7 +132,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     };
     const auto vf = keep();
 
-    const bool always = !a.causal || key < q.prefix;                      // (seen from every place)
+    const float keyf = (float)(32 * wave + col), seen_from = !a.causal || key < q.prefix ? -INFINITY : keyf;   // places from k0 on
     const int last = min(k0 + FIXED, q.kn) - 1, wlast = min(wk0 + 31, q.kn - 1);
     int dmin = 0, dmax = 0;
     if (a.k_docs) {
@@ -143,22 +146,17 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         }
     }
     const int64_t qblock0 = doc_block0(q.q0, s);
-    auto classify = [&](int t, bool& all, bool& pad) {
+    auto classify = [&](int t, bool& one, bool& pad) {
         const int first = (int)over_group(a, t * L::ROWS), end = (int)over_group(a, min(t * L::ROWS + L::ROWS, rows) - 1);
-        bool some = true;
-        all = true;
-        if (a.causal) {
-            some = k0 <= q.start + end || k0 < q.prefix;
-            all = wlast <= q.start + first || wlast < q.prefix;
-        }
+        bool some = !a.causal || k0 <= q.start + end || k0 < q.prefix;
+        one = !a.q_docs;
         if (a.q_docs && !a.q_blocks) {
-            all = false;
             pad = true;
         } else if (a.q_docs && some) {
             const int2 m = a.q_blocks[qblock0 + first / DOC_BLOCK], n = a.q_blocks[qblock0 + end / DOC_BLOCK];
             const int lo = min(m.x, n.x), hi = max(m.y, n.y);
             some = dmax >= 0 && hi >= max(dmin, 0) && lo <= dmax;
-            all = all && lo == hi && dmin == dmax && lo == dmin;
+            one = lo == hi && dmin == dmax && lo == dmin;
             pad = lo < 0;
         }
         return some;
@@ -200,7 +198,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
             Sender<T, DP, L::ROWS>::whole(smem[buf][0], qbase + token * a.qs.row, mine.q);
             Sender<T, DP, L::ROWS>::whole(smem[buf][1], gbase + token * a.gs.row, mine.g);
             if (has_words) send_words(words + 64 * buf, mine.word + (int64_t)t * word_step);
-            if (wave == 0) s_place[buf][lane] = q.start + (int)token + (int)over_group(a, lane % L::ROWS);
+            if (wave == 0) s_place[buf][lane] = (float)(q.start - k0 + (int)token + (int)over_group(a, lane % L::ROWS));
             return;
         }
         // (padding and rows past the end are zeros that see nothing)
@@ -213,7 +211,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         const int r = min(r0 + lane, rows - 1), qi = (int)over_group(a, r);
         const void* none = wave == 0 ? (const void*)&infinity_word : wave == 3 ? (const void*)&minus_one : (const void*)&zeros;
         if (has_words) send_words(words + 64 * buf, r0 + lane < rows ? word(q.q0 + qi, hk * a.group + r - qi * a.group) : none);
-        if (wave == 0) s_place[buf][lane] = q.start + qi;
+        if (wave == 0) s_place[buf][lane] = (float)(q.start - k0 + qi);
     };
 
     f32x16 dk[L::NA], dv[L::NA];
@@ -226,7 +224,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     int t = walk.next(t0, t1, classify), buf = 0;
     if (t < t1) request(t, walk.is_padded(t), 0);
     while (t < t1) {
-        const bool whole = walk.is_whole(t);
+        const bool docs = !walk.is_one(t), cut = a.causal && wlast > q.start + (int)over_group(a, t * L::ROWS) && wlast >= q.prefix;
         const int far = q.start + (int)over_group(a, min(t * L::ROWS + L::ROWS, rows) - 1);
         t = walk.next(t + 1, t1, classify);
         vm_wait();
@@ -235,42 +233,50 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         if (wk0 < q.kn && !(a.causal && wk0 > far && wk0 >= q.prefix)) {
 #pragma unroll 1
             for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
-                const f32x16 sc = dot<T, DP>(smem[buf][0], b, kf, lanes);
-                const f32x16 g = dot<T, DP>(smem[buf][1], b, vf, lanes);
+                f32x16 sc, g;
+                dots<T, DP>(smem[buf][0], b, kf, sc, smem[buf][1], b, vf, g, lanes);
                 Weights<T> p, d, rest;
                 auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
-                gradients<T, (DP > 64 ? 1 : 4)>(a, sc, g, p, d, rest, whole, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
+                gradients<T, (DP > 64 ? 1 : 4)>(a, sc, g, p, d, rest, cut, docs, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
                              [&](int j) { return *(const float4*)&s_delta[buf][at(j)]; },
                              [&](int j) {
-                                 const float4 by = *(const float4*)&s_slope[buf][at(j)];
-                                 const int4 place = *(const int4*)&s_place[buf][at(j)];
-                                 return make_float4(by.x * LOG2E * fabsf((float)(place.x - key)), by.y * LOG2E * fabsf((float)(place.y - key)),
-                                                    by.z * LOG2E * fabsf((float)(place.z - key)), by.w * LOG2E * fabsf((float)(place.w - key)));
+                                 const float4 by = *(const float4*)&s_slope[buf][at(j)], place = *(const float4*)&s_place[buf][at(j)];
+                                 return make_float4(by.x * LOG2E * fabsf(place.x - keyf), by.y * LOG2E * fabsf(place.y - keyf),
+                                                    by.z * LOG2E * fabsf(place.z - keyf), by.w * LOG2E * fabsf(place.w - keyf));
                              },
                              [&](int j, bool(&is)[4]) {
-                                 const int4 place = *(const int4*)&s_place[buf][at(j)];
-                                 const int4 of = a.q_docs ? *(const int4*)&s_doc[buf][at(j)] : make_int4(0, 0, 0, 0);
+                                 const float4 place = *(const float4*)&s_place[buf][at(j)];
 #pragma unroll
-                                 for (int i = 0; i < 4; ++i) is[i] = ((key <= (&place.x)[i]) | always) & ((&of.x)[i] == doc) & there;
+                                 for (int i = 0; i < 4; ++i) is[i] = seen_from <= (&place.x)[i];
+                             },
+                             // (padding: rows' weights are 0 by their lse, keys' because no row is of their documents)
+                             [&](int j, bool(&is)[4]) {
+                                 const int4 of = *(const int4*)&s_doc[buf][at(j)];
+#pragma unroll
+                                 for (int i = 0; i < 4; ++i) is[i] = (&of.x)[i] == doc;
                              });
                 weigh<T, DP>(smem[buf][1], b, p, dv, lanes);
                 weigh<T, DP>(smem[buf][0], b, d, dk, lanes);
-                if (sizeof(T) == 2 && (!whole || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dk, lanes);
+                if (sizeof(T) == 2 && (cut || docs || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dk, lanes);
             }
         }
         buf ^= 1;
     }
-    const int mine = wk0 + (anew<256>((int)threadIdx.x) & 31);             // (the key, worked out again)
-    if (mine >= q.kn) return;
-    const int64_t to = q.k0 + mine;
+    __syncthreads();                                                      // (tiles are no longer read)
+    if (wk0 >= q.kn) return;
+    unsigned char* const mine = smem[0][0] + wave * PUT_BYTES;
+    static_assert(sizeof(smem) >= 4 * PUT_BYTES, "rows on their way out");
+    auto each = [&](auto* first, int64_t step) {                          // the wavefront's keys, from the tensor's first one of this head on
+        return [&, first, step](int r) { return wk0 + r < q.kn ? first + (q.k0 + wk0 + r) * step : nullptr; };
+    };
     if (a.key_parts > 1) {
-        const int64_t row = ((int64_t)part * a.n_k + to) * a.kv_heads + hk;
-        put_row<float, DP>(a.part_dk + row * a.head_dim, dk, 1.f, a.head_dim, half);
-        put_row<float, DP>(a.part_dv + row * a.head_dim, dv, 1.f, a.head_dim, half);
+        const int64_t first = ((int64_t)part * a.n_k * a.kv_heads + hk) * a.head_dim, step = (int64_t)a.kv_heads * a.head_dim;
+        put_rows<float, DP>(mine, dk, 1.f, a.head_dim, each(a.part_dk + first, step));
+        put_rows<float, DP>(mine, dv, 1.f, a.head_dim, each(a.part_dv + first, step));
         return;
     }
-    put_row<T, DP>((T*)a.dk + to * a.dks.row + hk * a.dks.head, dk, by_x<T>(a), a.head_dim, half);
-    put_row<T, DP>((T*)a.dv + to * a.dvs.row + hk * a.dvs.head, dv, 1.f, a.head_dim, half);
+    put_rows<T, DP>(mine, dk, by_x<T>(a), a.head_dim, each((T*)a.dk + hk * a.dks.head, a.dks.row));
+    put_rows<T, DP>(mine, dv, 1.f, a.head_dim, each((T*)a.dv + hk * a.dvs.head, a.dvs.row));
 }
 
 // Queries fixed: dq of FIXED rows of a key head's queries.
@@ -338,21 +344,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
         }
     }
     const int64_t kblock0 = doc_block0(q.k0, s);
-    auto classify = [&](int t, bool& all, bool& pad) {
+    auto classify = [&](int t, bool& one, bool& pad) {
         const int k0 = t * L::ROWS;
-        bool some = true;
-        all = k0 + L::ROWS <= q.kn;
-        if (a.causal) {
-            some = k0 <= far || k0 < q.prefix;
-            all = all && (k0 + L::ROWS - 1 <= wnear || k0 + L::ROWS <= q.prefix);
-        }
+        bool some = !a.causal || k0 <= far || k0 < q.prefix;
+        one = !a.k_docs;
         if (a.k_docs && !a.k_blocks) {
-            all = false;
             pad = true;
         } else if (a.k_docs && some) {
             const int2 m = a.k_blocks[kblock0 + k0 / DOC_BLOCK];
             some = dmax >= 0 && m.y >= max(dmin, 0) && m.x <= dmax;
-            all = all && m.x == m.y && dmin == dmax && m.x == dmin;
+            one = m.x == m.y && dmin == dmax && m.x == dmin;
             pad = m.x < 0;
         }
         return some;
@@ -385,8 +386,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     int t = walk.next(t0, t1, classify), buf = 0;
     if (t < t1) request(t, walk.is_padded(t), 0);
     while (t < t1) {
-        const bool whole = walk.is_whole(t);
+        const bool docs = !walk.is_one(t);
         const int k0 = t * L::ROWS;
+        const bool cut = k0 + L::ROWS > q.kn || (a.causal && k0 + L::ROWS - 1 > wnear && k0 + L::ROWS > q.prefix);
+        const float from = (float)(place - k0 - 4 * half);
         t = walk.next(t + 1, t1, classify);
         vm_wait();
         __syncthreads();                                                  // the tile has landed, the one before it is no longer read
@@ -394,32 +397,49 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
         if (wr0 < rows && !(a.causal && k0 > wfar && k0 >= q.prefix)) {
 #pragma unroll 1
             for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
-                const f32x16 sc = dot<T, DP>(smem[buf][0], b, qf, lanes), g = dot<T, DP>(smem[buf][1], b, gf, lanes);
+                f32x16 sc, g;
+                dots<T, DP>(smem[buf][0], b, qf, sc, smem[buf][1], b, gf, g, lanes);
                 Weights<T> p, d, rest;
                 auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
-                gradients<T, 4>(a, sc, g, p, d, rest, whole, [&](int) { return make_float4(lse, lse, lse, lse); },
+                const int left = end - k0 - 32 * b - 4 * half;
+                const float off = from - (float)(32 * b);
+                gradients<T, 4>(a, sc, g, p, d, rest, cut, docs, [&](int) { return make_float4(lse, lse, lse, lse); },
                              [&](int) { return make_float4(delta, delta, delta, delta); },
                              [&](int j) {
-                                 const int from = place - k0 - at(j);
-                                 return make_float4(slope * fabsf((float)from), slope * fabsf((float)(from - 1)),
-                                                    slope * fabsf((float)(from - 2)), slope * fabsf((float)(from - 3)));
+                                 return make_float4(slope * fabsf(off - (float)(8 * j)), slope * fabsf(off - (float)(8 * j + 1)),
+                                                    slope * fabsf(off - (float)(8 * j + 2)), slope * fabsf(off - (float)(8 * j + 3)));
                              },
                              [&](int j, bool(&is)[4]) {
-                                 const int4 of = a.k_docs ? *(const int4*)&s_doc[buf][at(j)] : make_int4(0, 0, 0, 0);
 #pragma unroll
-                                 for (int i = 0; i < 4; ++i) is[i] = (k0 + at(j) + i < end) & ((&of.x)[i] == doc) & there;
+                                 for (int i = 0; i < 4; ++i) is[i] = left > 8 * j + i;
+                             },
+                             // (padding is zeros on both sides, and its weights are 0 by its lse)
+                             [&](int j, bool(&is)[4]) {
+                                 const int4 of = *(const int4*)&s_doc[buf][at(j)];
+#pragma unroll
+                                 for (int i = 0; i < 4; ++i) is[i] = (&of.x)[i] == doc;
                              });
                 weigh<T, DP>(smem[buf][0], b, d, dq, lanes);
-                if (sizeof(T) == 2 && (!whole || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dq, lanes);
+                if (sizeof(T) == 2 && (cut || docs || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dq, lanes);
             }
         }
         buf ^= 1;
     }
-    if (!live) return;
+    __syncthreads();                                                      // (tiles are no longer read)
+    if (wr0 >= rows) return;
+    unsigned char* const mine = smem[0][0] + wave * PUT_BYTES;
+    static_assert(sizeof(smem) >= 4 * PUT_BYTES, "rows on their way out");
+    auto each = [&](auto put) {                                           // row r of the wavefront, as token and head
+        return [&, put](int r) {
+            const int at = wr0 + r, qi = (int)over_group(a, min(at, rows - 1)), head = hk * a.group + min(at, rows - 1) - qi * a.group;
+            return at < rows ? put((int64_t)q.q0 + qi, head) : nullptr;
+        };
+    };
     if (a.parts > 1)
-        put_row<float, DP>(a.part_o + (((int64_t)part * a.n_q + token) * a.heads + head) * a.head_dim, dq, 1.f, a.head_dim, half);
+        put_rows<float, DP>(mine, dq, 1.f, a.head_dim,
+                            each([&](int64_t token, int head) { return a.part_o + (((int64_t)part * a.n_q + token) * a.heads + head) * a.head_dim; }));
     else
-        put_row<T, DP>((T*)a.dq + token * a.dqs.row + head * a.dqs.head, dq, by_x<T>(a), a.head_dim, half);
+        put_rows<T, DP>(mine, dq, by_x<T>(a), a.head_dim, each([&](int64_t token, int head) { return (T*)a.dq + token * a.dqs.row + head * a.dqs.head; }));
 }
 
 // A gradient's shares added up, a thread four neighbours: those of queries (z = 0), keys (1) and values (2).

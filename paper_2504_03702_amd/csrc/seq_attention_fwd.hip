@@ -19,7 +19,7 @@ struct Row {
     using L = Tile<T, DP, R>;
     int head, place, doc, end;         // keys in front of `end` are seen, if their documents are
     int64_t token;
-    float slope, m = -INFINITY, l = 0.f;   // the exponent's reference, in powers of two; this lane's share of the sum
+    float slope, m = -INFINITY, l = 0.f;   // what goes with step()'s scores; the exponent's reference, in powers of two; this lane's share of the sum
     Fixed<T, DP> qf;
     f32x16 o[L::NA];
     const Lanes<T, DP> lanes;
@@ -31,21 +31,27 @@ struct Row {
         head = hk * a.group + r - qi * a.group;
         token = q.q0 + qi;
         place = q.start + qi;
-        slope = a.slopes ? a.slopes[head] * LOG2E : 0.f;
+        slope = a.slopes ? a.slopes[head] * (a.cap > 0.f ? LOG2E : 1.f / a.scale) : 0.f;
         doc = a.q_docs ? a.q_docs[token] : 0;
-        end = doc < 0 ? 0 : a.causal ? min(q.kn, max(place + 1, q.prefix)) : q.kn;
-        qf.load((const T*)a.q + token * a.qs.row + head * a.qs.head, live, a.head_dim, half);
+        end = a.causal ? min(q.kn, max(place + 1, q.prefix)) : q.kn;
+        qf.load((const T*)a.q + token * a.qs.row + head * a.qs.head, live && doc >= 0, a.head_dim, half);
 #pragma unroll
         for (int i = 0; i < L::NA; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
     }
 
-    // A tile of keys from k0 on and its values; whole: every key in it is seen by all rows of the wavefront.
-    __device__ __forceinline__ void step(const Args& a, const unsigned char* keys, const unsigned char* values, const int* docs, int k0, bool whole) {
+    // A tile of keys from k0 on and its values.  cut: some of the wavefront's rows see only the keys in front of their `end`; docs: documents
+    // of its keys, null if the tile's and all rows' are one.
+    __device__ __forceinline__ void step(const Args& a, const unsigned char* keys, const unsigned char* values, const int* docs, int k0, bool cut) {
         f32x16 sc[L::BLOCKS];
 #pragma unroll
-        for (int b = 0; b < L::BLOCKS; ++b) sc[b] = dot<T, DP>(keys, b, qf, lanes);
+        for (int b = 0; b < L::BLOCKS; b += 2) {
+            if constexpr (L::BLOCKS % 2 == 0)
+                dots<T, DP>(keys, b, qf, sc[b], keys, b + 1, qf, sc[b + 1], lanes);
+            else
+                sc[b] = dot<T, DP>(keys, b, qf, lanes);
+        }
         const Cap cap = Cap::of<T>(a);
         float c = a.scale * LOG2E;
         if (a.cap > 0.f) {
@@ -56,31 +62,27 @@ struct Row {
             c = 1.f;
         }
         if (a.slopes) {
-            const int from = place - k0 - 4 * half;
+            const float from = (float)(place - k0 - 4 * half);
 #pragma unroll
             for (int b = 0; b < L::BLOCKS; ++b)
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    sc[b][e] = fmaf(-slope, fabsf((float)(from - 32 * b - row_of(e))), sc[b][e] * c);
-            c = 1.f;
+                for (int e = 0; e < 16; ++e) sc[b][e] = fmaf(-slope, fabsf(from - (float)(32 * b + row_of(e))), sc[b][e]);
         }
-        if (!whole) {
+        if (cut) {
+            const int left = end - k0 - 4 * half;
 #pragma unroll
             for (int b = 0; b < L::BLOCKS; ++b)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    if (k0 + 32 * b + row_of(e) + 4 * half >= end) sc[b][e] = -INFINITY;
-                }
+                for (int e = 0; e < 16; ++e) sc[b][e] = left > 32 * b + row_of(e) ? sc[b][e] : -INFINITY;
         }
-        if (!whole && a.k_docs) {
+        if (docs) {
 #pragma unroll
             for (int b = 0; b < L::BLOCKS; ++b)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int4 of = *(const int4*)&docs[32 * b + 8 * j + 4 * half];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if ((&of.x)[i] != doc) sc[b][4 * j + i] = -INFINITY;
+                    for (int i = 0; i < 4; ++i) sc[b][4 * j + i] = (&of.x)[i] == doc ? sc[b][4 * j + i] : -INFINITY;
                 }
         }
         float mx = sc[0][0];
@@ -120,13 +122,13 @@ struct Row {
         }
     }
 
-    // What is left to do once the halves of the wavefront have put their sums together.
-    __device__ __forceinline__ void add_halves() { l += __shfl_xor(l, 32, 64); }
-    __device__ __forceinline__ void put(const Args& a) const {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        put_row<T, DP>((T*)a.out_w + token * a.os.row + head * a.os.head, o, inv, a.head_dim, half);
-        if (a.rest_w) put_rest<DP>((bf16*)a.rest_w + (token * a.heads + head) * a.head_dim, o, inv, a.head_dim, half);
-        if (a.lse_w && half == 0) a.lse_w[(int64_t)head * a.n_q + token] = lse_of(m, l);
+    // The halves of the wavefront put their sums together.  (Padding has seen the padding of cut tiles, zeros like itself: it sees nothing.)
+    __device__ __forceinline__ void add_halves() {
+        l += __shfl_xor(l, 32, 64);
+        if (doc < 0) {
+            l = 0.f;
+            m = -INFINITY;
+        }
     }
 };
 
@@ -167,25 +169,21 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
         }
     }
     const int64_t kblock0 = doc_block0(q.k0, s);
-    auto classify = [&](int t, bool& all, bool& pad) {
+    auto classify = [&](int t, bool& one, bool& pad) {
         const int k0 = t * L::ROWS;
-        bool some = true;
-        all = k0 + L::ROWS <= q.kn;
-        if (a.causal) {
-            some = k0 <= far || k0 < q.prefix;
-            all = all && (k0 + L::ROWS - 1 <= wnear || k0 + L::ROWS <= q.prefix);
-        }
+        bool some = !a.causal || k0 <= far || k0 < q.prefix;
+        one = !a.k_docs;
         if (a.k_docs && !a.k_blocks) {
-            all = false;
             pad = true;
         } else if (a.k_docs && some) {
             const int2 m = a.k_blocks[kblock0 + k0 / DOC_BLOCK];
             some = dmax >= 0 && m.y >= max(dmin, 0) && m.x <= dmax;
-            all = all && m.x == m.y && dmin == dmax && m.x == dmin;
+            one = m.x == m.y && dmin == dmax && m.x == dmin;
             pad = m.x < 0;
         }
         return some;
     };
+    auto is_cut = [&](int k0) { return k0 + L::ROWS > q.kn || (a.causal && k0 + L::ROWS - 1 > wnear && k0 + L::ROWS > q.prefix); };
 
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
@@ -209,7 +207,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     int t = walk.next(t0, t1, classify), buf = 0;
     if (t < t1) request(t, walk.is_padded(t), 0);
     while (t < t1) {
-        const bool whole = walk.is_whole(t);
+        const bool one = walk.is_one(t);
         const int k0 = t * L::ROWS;
         t = walk.next(t + 1, t1, classify);
         vm_wait();
@@ -217,19 +215,32 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
         if (t < t1) request(t, walk.is_padded(t), buf ^ 1);
         // (a wavefront whose rows all stand before the tile has nothing in it)
         if (wr0 < rows && !(a.causal && k0 > wfar && k0 >= q.prefix)) {
-            row.step(a, smem[buf][0], smem[buf][1], s_doc[buf], k0, whole);
+            row.step(a, smem[buf][0], smem[buf][1], one ? nullptr : s_doc[buf], k0, is_cut(k0));
         }
         buf ^= 1;
     }
     row.add_halves();
-    if (!live) return;
+    __syncthreads();                                                      // (tiles are no longer read)
+    if (wr0 >= rows) return;
+    unsigned char* const mine = smem[0][0] + wave * PUT_BYTES;
+    static_assert(sizeof(smem) >= 4 * PUT_BYTES, "rows on their way out");
+    auto each = [&](auto put) {                                           // row r of the wavefront, as token and head
+        return [&, put](int r) {
+            const int at = wr0 + r, qi = (int)over_group(a, min(at, rows - 1)), head = hk * a.group + min(at, rows - 1) - qi * a.group;
+            return at < rows ? put((int64_t)q.q0 + qi, head) : nullptr;
+        };
+    };
     if (PARTS) {
-        const int64_t at = ((int64_t)part * a.n_q + row.token) * a.heads + row.head;
-        put_row<float, DP>(a.part_o + at * a.head_dim, row.o, 1.f, a.head_dim, half);
-        if (half == 0) a.part_ml[at] = make_float2(row.m, row.l);
+        const int64_t first = (int64_t)part * a.n_q;
+        put_rows<float, DP>(mine, row.o, 1.f, a.head_dim, each([&](int64_t token, int head) { return a.part_o + ((first + token) * a.heads + head) * a.head_dim; }));
+        if (live && half == 0) a.part_ml[(first + row.token) * a.heads + row.head] = make_float2(row.m, row.l);
         return;
     }
-    row.put(a);
+    const float inv = row.l == 0.f ? 0.f : 1.f / row.l;
+    put_rows<T, DP>(mine, row.o, inv, a.head_dim, each([&](int64_t token, int head) { return (T*)a.out_w + token * a.os.row + head * a.os.head; }));
+    if (sizeof(T) == 2 && a.rest_w)
+        put_rows<T, DP, true>(mine, row.o, inv, a.head_dim, each([&](int64_t token, int head) { return (T*)a.rest_w + (token * a.heads + head) * a.head_dim; }));
+    if (a.lse_w && live && half == 0) a.lse_w[(int64_t)row.head * a.n_q + row.token] = lse_of(row.m, row.l);
 }
 
 // Few rows, at most 32 of a key head's queries: single tokens over their keys, where the time goes into reading keys and values.  The
@@ -320,10 +331,8 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
         send_words(s_doc[wave][stage], a.k_docs ? (const void*)(a.k_docs + q.k0 + min(k0 + lane, q.kn - 1)) : (const void*)&zeros);
     };
     const int near = q.start, far = q.start + q.qn - 1;                   // places of the rows
-    auto classify = [&](int t, bool& all, bool& pad) {
+    auto classify = [&](int t, bool&, bool&) {
         const int k0 = t * 32;
-        pad = false;
-        all = k0 + 32 <= q.kn && !a.k_docs && (!a.causal || k0 + 31 <= near || k0 + 32 <= q.prefix);
         return (t & 3) == wave && (!a.causal || k0 <= far || k0 < q.prefix);
     };
 
@@ -344,7 +353,8 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(F::WAIT) : "memory");
         else
             vm_wait();
-        row.step(a, smem[wave][stage][0], smem[wave][stage][1], s_doc[wave][stage], t * 32, walk.is_whole(t));
+        row.step(a, smem[wave][stage][0], smem[wave][stage][1], a.k_docs ? s_doc[wave][stage] : nullptr, t * 32,
+                 t * 32 + 32 > q.kn || (a.causal && t * 32 + 31 > near && t * 32 + 32 > q.prefix));
         asm volatile("" ::: "memory");                                    // (its reads are over: their products are on their way)
         stage = stage + 1 < STAGES ? stage + 1 : 0;
         t = walk.next(t + 1, t1, classify);
@@ -520,6 +530,7 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
     if (!(d->scale > 0.f) || !(d->softcap >= 0.f) || isinf(d->scale) || isinf(d->softcap)) return PS_EINVAL;
     if (d->head_dim > 128 || d->head_dim % 8 != 0) return PS_EUNSUPPORTED;
     const int64_t group = d->heads / d->kv_heads;
+    if (max(min((int64_t)d->max_q, d->n_q), min((int64_t)d->max_k, d->n_k)) > 1 << 30) return PS_EUNSUPPORTED;   // (places stay in 32 bits)
     if (group > 32768 || (int64_t)d->max_q * group >= ((int64_t)1 << 31) / group) return PS_EUNSUPPORTED;
     if (d->heads > 65536) return PS_EUNSUPPORTED;
     Args& a = p.a;

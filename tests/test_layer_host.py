@@ -68,6 +68,13 @@ def test_a_rest_is_for_bf16(lib):
     assert forward(lib, desc(dtype=0), seqs(), rest=256) == EINVAL
 
 
+@pytest.mark.parametrize("n", [(1 << 30) + 1, (1 << 31) - 1])
+def test_sequences_whose_places_would_not_fit_are_refused(lib, n):
+    assert forward(lib, desc(max_k=n, n_k=n), seqs()) == EUNSUPPORTED
+    assert forward(lib, desc(heads=2, max_q=n, n_q=n), seqs()) == EUNSUPPORTED
+    assert lib.ps_attention_workspace_bytes(ctypes.byref(desc(max_k=n, n_k=n)), 1) == 0
+
+
 def test_backward_refuses(lib):
     def call(d, **change):
         a = dict(q=256, k=256, v=256, out=256, lse=256, rest=None, dout=256, dq=256, dk=256, dv=256, ws=256, n=1 << 20)
