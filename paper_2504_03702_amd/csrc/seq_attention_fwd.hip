@@ -402,17 +402,15 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
     }
 }
 
-// The parts of a row put together by W of a workgroup's four wavefronts, each the W-th part of them; lane f has elements f and f + 64.
-template <typename T, int W>
-__global__ __launch_bounds__(256) void join_kernel(Args a) {
+// The parts of a row put together by a workgroup's four wavefronts, each a fourth of them; lane f has elements f and f + 64.
+template <typename T>
+__global__ __launch_bounds__(256) void join_few_kernel(Args a) {
     __shared__ float s_l[4], s_o[4][128];
-    const int s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = blockIdx.x;
     Seq q;
-    if (!sequence(a, s, q) || (int64_t)blockIdx.x * (4 / W) >= (int64_t)q.qn * a.heads) return;
-    const int i = min((int)blockIdx.x * (4 / W) + wave / W, q.qn * a.heads - 1);
+    if (!sequence(a, s, q) || (int64_t)i >= (int64_t)q.qn * a.heads) return;
     const int64_t row = (int64_t)q.q0 * a.heads + i, token = q.q0 + i / a.heads;
-    const int head = i % a.heads;
-    const int block = (i / a.heads * a.group + head % a.group) / FIXED;
+    const int head = i % a.heads, block = (i / a.heads * a.group + head % a.group) / FIXED;
     const int parts = shares(key_tiles(a, q, block * FIXED), a.parts, a.part_tiles);
     const int64_t step = a.n_q * a.heads;
     float m = -INFINITY;
@@ -421,7 +419,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
     float l = 0.f, x = 0.f, y = 0.f;
     const bool first = lane < a.head_dim, second = lane + 64 < a.head_dim;
 #pragma unroll 4
-    for (int p = wave % W; p < parts; p += W) {
+    for (int p = wave; p < parts; p += 4) {
         const float2 ml = a.part_ml[p * step + row];
         const float* o = a.part_o + (p * step + row) * a.head_dim + lane;
         const float u = first ? o[0] : 0.f, v = second ? o[64] : 0.f;
@@ -430,16 +428,14 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
         x = fmaf(u, by, x);
         y = fmaf(v, by, y);
     }
-    if constexpr (W == 4) {
-        s_o[wave][lane] = x;
-        s_o[wave][lane + 64] = y;
-        if (lane == 0) s_l[wave] = l;
-        __syncthreads();
-        if (wave != 0) return;
-        l = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
-        x = (s_o[0][lane] + s_o[1][lane]) + (s_o[2][lane] + s_o[3][lane]);
-        y = (s_o[0][lane + 64] + s_o[1][lane + 64]) + (s_o[2][lane + 64] + s_o[3][lane + 64]);
-    }
+    s_o[wave][lane] = x;
+    s_o[wave][lane + 64] = y;
+    if (lane == 0) s_l[wave] = l;
+    __syncthreads();
+    if (wave != 0) return;
+    l = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
+    x = (s_o[0][lane] + s_o[1][lane]) + (s_o[2][lane] + s_o[3][lane]);
+    y = (s_o[0][lane + 64] + s_o[1][lane + 64]) + (s_o[2][lane + 64] + s_o[3][lane + 64]);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T* out = (T*)a.out_w + token * a.os.row + head * a.os.head;
     bf16* rest = (bf16*)a.rest_w + row * a.head_dim;
@@ -451,6 +447,46 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
     if (first) put(lane, x * inv);
     if (second) put(lane + 64, y * inv);
     if (a.lse_w && lane == 0) a.lse_w[(int64_t)head * a.n_q + token] = lse_of(m, l);
+}
+
+// The same where rows are many and parts few, a thread four neighbours of a row.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(Args a) {
+    const int s = a.seq0 + (int)blockIdx.y;
+    Seq q;
+    if (!sequence(a, s, q)) return;
+    const int fours = a.head_dim / 4;
+    const int64_t n = (int64_t)q.qn * a.heads * fours, step = a.n_q * a.heads;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int mine = (int)(i / fours), f = (int)(i - (int64_t)mine * fours) * 4, qi = mine / a.heads, head = mine - qi * a.heads;
+        const int64_t token = q.q0 + qi, row = token * a.heads + head;
+        const int parts = shares(key_tiles(a, q, (qi * a.group + head % a.group) / FIXED * FIXED), a.parts, a.part_tiles);
+        float m = -INFINITY, l = 0.f;
+        for (int p = 0; p < parts; ++p) m = fmaxf(m, a.part_ml[p * step + row].x);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int p = 0; p < parts; ++p) {
+            const float2 ml = a.part_ml[p * step + row];
+            const float4 x = *(const float4*)(a.part_o + (p * step + row) * a.head_dim + f);
+            const float by = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+            l = fmaf(ml.y, by, l);
+            o = make_float4(fmaf(x.x, by, o.x), fmaf(x.y, by, o.y), fmaf(x.z, by, o.z), fmaf(x.w, by, o.w));
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        T* const out = (T*)a.out_w + token * a.os.row + head * a.os.head + f;
+        if constexpr (sizeof(T) == 2) {
+            const uint2 x = make_uint2(cvt_pk_bf16(o.x, o.y), cvt_pk_bf16(o.z, o.w));
+            *(uint2*)out = x;
+            if (a.rest_w)
+                *(uint2*)((bf16*)a.rest_w + row * a.head_dim + f) =
+                    make_uint2(cvt_pk_bf16(o.x - __uint_as_float(x.x << 16), o.y - __uint_as_float(x.x & 0xffff0000u)),
+                               cvt_pk_bf16(o.z - __uint_as_float(x.y << 16), o.w - __uint_as_float(x.y & 0xffff0000u)));
+        } else {
+            *(float4*)out = o;
+        }
+        if (a.lse_w && f == 0) a.lse_w[(int64_t)head * a.n_q + token] = lse_of(m, l);
+    }
 }
 
 // Smallest and largest document of every DOC_BLOCK tokens, a wavefront each; padding counts as -1.
@@ -493,12 +529,13 @@ void launch_attend(const Args& a, hipStream_t st) {
     for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
         n = min(a.n_seq - s0, 32768);
         b.seq0 = s0;
-        // few rows have many parts and the chip to themselves; many rows a wavefront each (25600 rows of 4 parts 53 us by four)
+        // few rows have many parts and the chip to themselves; of many, threads have four elements each (25600 rows of 4 parts 9 us, a wavefront
+        // a row 22, four wavefronts 53)
         const int64_t rows = (int64_t)a.max_q * a.heads;
         if (a.n_q * a.heads <= 4096)
-            hipLaunchKernelGGL((join_kernel<T, 4>), dim3((unsigned)rows, (unsigned)n), dim3(256), 0, st, b);
+            hipLaunchKernelGGL(join_few_kernel<T>, dim3((unsigned)rows, (unsigned)n), dim3(256), 0, st, b);
         else
-            hipLaunchKernelGGL((join_kernel<T, 1>), dim3((unsigned)((rows + 3) / 4), (unsigned)n), dim3(256), 0, st, b);
+            hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)min((rows * (a.head_dim / 4) + 255) / 256, (int64_t)4096), (unsigned)n), dim3(256), 0, st, b);
     }
 }
 
