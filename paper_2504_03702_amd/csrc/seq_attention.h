@@ -90,9 +90,9 @@ __device__ __forceinline__ int shares(int tiles, int parts, int part_tiles) { re
 // A workgroup's part of a launch over blocks of rows (of keys, with KEYS) and shares of their tiles.
 // Sequence and block as the grid counts them: `together` sequences take turns, block by block, then the next so many.  Blocks come in order
 // of their work, most first.  In a launch of few blocks all sequences take turns, so that the last to start are short (two rows of 8192
-// tokens, forwards / keys' gradients: 119 / 243 us one after the other, 108 / 226 in turns; 16 x 2048, keys' 1213, 993); in one of many
-// only as many as fill the chip, so that blocks that run at a time read the same keys from the caches (16 x 2048, forwards / queries':
-// 460 / 609 us two at a time, 540 / 727 eight).
+// tokens, forwards / queries' / keys' gradients: 110 / 177 / 191 us one after the other, 100 / 161 / 182 in turns; 16 x 2048, keys'
+// 1430, 1120); in one of many only as many as fill the chip, so that blocks that run at a time read the same keys from the caches
+// (16 x 2048, forwards / queries': 450 / 680 us two at a time, 520 / 800 eight).
 inline int32_t turns(int64_t blocks_a_seq, int32_t seqs) {
     if (blocks_a_seq * seqs <= 2048) return seqs;
     return (int32_t)(blocks_a_seq >= 512 ? 1 : 512 / blocks_a_seq);
@@ -112,7 +112,8 @@ __device__ __forceinline__ int shares_of(const Args& a, const Seq& q, int block)
 // a.listed (at most 64 sequences of at most 64 blocks): the grid has a workgroup for what there could be, and the first so many take
 // what there is, found by adding it up a sequence to a lane.  Counted as the grid counts, what there is lay anywhere among it, and
 // three or more long workgroups on one unit beside empty ones (8 sequences of 100 to 1023 tokens, 408 workgroups of 2048 with work to do: 26 to
-// 40 tiles on the fullest units, 10 on average).
+// 40 tiles on the fullest units, 10 on average; forwards / queries' / keys' gradients in fp32 with heads of 80 128 / 173 / 293 us, 77 / 104 / 157
+// added up).
 template <bool KEYS>
 __device__ __forceinline__ bool look_for_work(const Args& a, Seq& q, Work& w) {
     const int blocks = KEYS ? (a.max_k + FIXED - 1) / FIXED : a.row_blocks, parts = KEYS ? a.key_parts : a.parts, lane = threadIdx.x & 63;

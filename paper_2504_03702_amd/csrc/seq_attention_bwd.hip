@@ -13,12 +13,12 @@ namespace {
 // four neighbours to every j: lse(j) and delta(j), what their queries bring along; distance(j), how far they stand from their keys, times
 // the slope; in_front(j, is) if the block is cut, which of the keys stand in front of their query's end; same(j, is) if it is of several
 // documents, which are of their query's.  STEP fours at a time: what is the same for all of them is asked once a step, so four at a time
-// make straight lines (two rows of 8192 tokens, queries' / keys' gradients 184 / 243 -> 169 / 236 us), and one keeps few registers waiting.
+// make straight lines (two rows of 8192 tokens, queries' / keys' gradients 191 / 210 -> 160 / 181 us), and one keeps few registers waiting.
 // rest: what the rounding of d to bf16 leaves.  Where a row's weight lies on few keys it does not average out, and what those keys have in
 // common is multiplied by the sum of the roundings instead of the sum of d, which is zero.  So where weights are like that, in blocks that
 // a mask cuts (rows see few keys) and under a cap (scores are large), a second product makes up for it: 16 x 2048 with prefix and cap,
-// queries' / keys' gradients 596 / 1044 -> 695 / 1103 us, error against 64 bits 2.7e-3 -> 1.8e-3 of the norm (1.7e-3 is that of dq's and dk's
-// own rounding; 2.4e-3 without cap, where a product more would cost 5 to 10 %).
+// queries' / keys' gradients 590 / 1044 -> 680 / 1120 us, error against 64 bits 2.7e-3 -> 2.1e-3 of the norm (1.7e-3 is that of dq's and dk's
+// own rounding; 2.3e-3 without cap, where a product more would cost 5 to 10 %).
 template <typename T, int STEP, typename Lse, typename Delta, typename Distance, typename Front, typename Same>
 __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, Weights<T>& p, Weights<T>& d, Weights<T>& rest,
                                           bool cut, bool docs, Lse lse, Delta delta, Distance distance, Front in_front, Same same) {
@@ -91,7 +91,10 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
 template <typename T>
 __device__ __forceinline__ float by_x(const Args& a) { return a.cap > 0.f && sizeof(T) == 2 ? 4.f * a.scale : a.scale; }
 
-// Keys fixed: dk and dv of FIXED keys of a key head, from the rows of all its heads.
+// Keys fixed: dk and dv of FIXED keys of a key head, from the rows of all its heads.  Four products a tile (a fifth for the rest), and twice the
+// accumulators of the queries' launch, which leaves two workgroups a unit (one in fp32 above 64 features): 16 x 2048 with prefix and cap, heads
+// of 128, 1.08 to 1.12 ms, 0.42 PFLOP/s, vector units issuing 32 % and matrix units busy 25 % of the time, 36 % of a wavefront's time at
+// barriers and waits; documents in two rows of 8192, heads of 64: 181 us, 0.40 PFLOP/s.
 template <typename T, int DP>
 __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_gradients_kernel(Args a) {
     using L = Tile<T, DP, key_tile_rows(sizeof(T), DP)>;
@@ -279,7 +282,9 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     put_rows<T, DP>(mine, dv, 1.f, a.head_dim, each((T*)a.dv + hk * a.dvs.head, a.dvs.row));
 }
 
-// Queries fixed: dq of FIXED rows of a key head's queries.
+// Queries fixed: dq of FIXED rows of a key head's queries.  Three products a tile (a fourth for the rest): 16 x 2048 with prefix and cap, heads of
+// 128, 680 us, 0.51 PFLOP/s, vector units issuing 47 % and matrix units busy 33 % of the time; documents in two rows of 8192, heads of 64: 160 us,
+// 0.34 PFLOP/s.
 template <typename T, int DP>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_gradients_kernel(Args a) {
     using L = Tile<T, DP>;
@@ -442,7 +447,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
         put_rows<T, DP>(mine, dq, by_x<T>(a), a.head_dim, each([&](int64_t token, int head) { return (T*)a.dq + token * a.dqs.row + head * a.dqs.head; }));
 }
 
-// A gradient's shares added up, a thread four neighbours: those of queries (z = 0), keys (1) and values (2).
+// A gradient's shares added up, a thread four neighbours: those of queries (z = 0), keys (1) and values (2).  3365 tokens, 8 heads of 80 on 4,
+// up to 4 shares: 61 MB in 18 us.
 template <typename T>
 __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
     const int z = z0 + (int)blockIdx.z, s = a.seq0 + (int)blockIdx.y;

@@ -133,7 +133,13 @@ struct Row {
 };
 
 // A workgroup: FIXED rows of a key head's queries, against a share of the key tiles that any of them sees (one pass, running
-// maximum and sum).
+// maximum and sum).  32 rows a wavefront, because a lane then has its row's maximum and sum to itself and its weights where the second product
+// takes them; tiles of 64 keys (32 in fp32), two of them in LDS, for two or three workgroups a unit.  Bound by the issue of vector
+// instructions beside the matrix ones: with heads of 128 under a cap (16 prompts of 1500 to 2048 tokens with prefix, 16 heads on 4) 450 us,
+// 0.52 PFLOP/s, vector units issuing 47 % and matrix units busy 26 % of the time with 1.7 wavefronts a SIMD; documents in two rows of 8192, 16
+// heads of 64: 100 us, 0.36 PFLOP/s.  A call of short prompts (64 of 4 to 512 tokens, 12 heads of 64: 36 us) waits for its first tiles 45 % of a
+// wavefront's time.  Three tiles in LDS, priorities around the matrix instructions and the sum of a row's weights by dot products made
+// no difference (100 +- 2 us).
 template <typename T, int DP, bool PARTS>
 __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     using L = Tile<T, DP>;
@@ -245,7 +251,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
 
 // Few rows, at most 32 of a key head's queries: single tokens over their keys, where the time goes into reading keys and values.  The
 // workgroup's wavefronts have the same rows and take tiles of 32 keys in turn, each with tiles of its own on their way through LDS, so
-// none waits for another until their rows are put together at the end.
+// none waits for another until their rows are put together at the end.  Bound by memory: 32 caches of 500 to 32768 keys, 8 heads of 128, 1.05 GB
+// in 203 us, 5.2 TB/s (a copy reaches 5.1); one cache of 65521 keys, 4 heads, 134 MB in 28 us, 4.8 TB/s; 8 first rows over up to 512 keys
+// 8.7 us, most of it the way to the first tile and out.
 template <typename T, int DP>
 struct Few {
     using L = Tile<T, DP, 32>;
@@ -550,7 +558,7 @@ bool good_strides(const ps_attention_desc* d, const ps_strides& s) {
 namespace seqatt {
 
 // Whether workgroups add up what work there is: where blocks are shared out, which leaves much of the grid without any.  Of whole blocks
-// the empty ones do not matter (64 sequences of 4 to 512 tokens, forwards / keys' gradients 37 / 53 us, 41 / 54 added up).
+// the empty ones do not matter (64 sequences of 4 to 512 tokens, forwards / keys' gradients 37 / 53 us either way).
 bool add_up(int32_t seqs, int64_t blocks, int32_t parts) { return seqs <= 64 && blocks <= 64 && parts > 1; }
 
 // A tensor that a call reads or writes.  Heads or rows of a written one may not fall on one another.
@@ -627,8 +635,8 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
         off = align_up(off + bytes, 256);
         return (void*)(base + at);
     };
-    // (a launch for the summaries takes longer than the few tiles of short sequences that they would rule out: 16 sequences of up to 64
-    // tokens forwards and backwards 61 us with them, 52 without)
+    // (a launch for the summaries, 4.7 us in each direction, takes longer than the few tiles of short sequences that they would rule out: 16
+    // sequences of up to 64 tokens, the other three launches 53 us with them, 50 without)
     if (max(a.max_q, a.max_k) > 256) {
         a.q_blocks = (int2*)take(sizeof(int2) * (size_t)(d->n_q / DOC_BLOCK + d->n_seq + 1));
         a.k_blocks = (int2*)take(sizeof(int2) * (size_t)(d->n_k / DOC_BLOCK + d->n_seq + 1));
