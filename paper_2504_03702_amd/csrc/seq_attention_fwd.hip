@@ -592,7 +592,8 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
     a.by_group = group > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)group + 1) : 0;
     a.row_blocks = (int32_t)(((int64_t)a.max_q * group + FIXED - 1) / FIXED);
     // Blocks that do not fill the chip, or of which the longest would be waited for: their tiles are shared out, so that there are
-    // some 2048 shares of a length, of 256 keys (rows) or more each.  What blocks and tiles there are is estimated from the tensors'
+    // some 2048 shares of a length, of 256 keys (rows) or more each (fp32, one sequence of 3571, 12 heads of 80: 1024, 2048, 4096 shares 1766, 1602,
+    // 1684 us a pass; bf16, 8192 tokens of 4 heads of 64: 430, 432, 620).  What blocks and tiles there are is estimated from the tensors'
     // rows: lengths stand on the device.
     a.tile = tile_rows(d->dtype == 1 ? 2 : 4);
     a.key_tile = key_tile_rows(d->dtype == 1 ? 2 : 4, padded(d->head_dim));
