@@ -50,26 +50,30 @@ struct Args {
     int32_t tile, key_tile;            // rows of a tile that passes by fixed queries, by fixed keys
     uint32_t by_group;                 // 2^32 / group + 1 (group > 1)
     float scale, cap;
+    float slope_by, cap_in;            // see Row and Cap
 };
 
 struct Seq {
     int q0, qn, k0, kn, start, prefix;
 };
 
-// Sequence s, checked against the tensors and the host's bounds; false if it is faulty.
+// Sequence s, checked against the tensors and the host's bounds; false if it is faulty.  All its words are asked for at once, without a
+// branch: a workgroup of a short sequence waits for them a tenth of its time.
 __device__ __forceinline__ bool sequence(const Args& a, int s, Seq& r) {
-    r.q0 = a.q_offsets[s];
-    r.k0 = a.k_offsets[s];
-    const int q1 = a.q_offsets[s + 1], k1 = a.k_offsets[s + 1];
-    const int len = a.k_lengths ? a.k_lengths[s] : k1 - r.k0;
-    // (ends before starts: a negative offset, or one that falls, fails one of these)
-    if (r.q0 < 0 || q1 < r.q0 || q1 > a.n_q || r.k0 < 0 || k1 < r.k0 || k1 > a.n_k) return false;
-    if (len < 0 || len > k1 - r.k0 || len > a.max_k || q1 - r.q0 > a.max_q) return false;
-    r.qn = q1 - r.q0;
-    r.kn = len;
-    r.start = a.q_start ? a.q_start[s] : r.kn - r.qn;
-    r.prefix = a.prefix ? a.prefix[s] : 0;
-    return r.start >= -(1 << 30) && r.start <= 1 << 30;                   // (places and distances are 32 bits)
+    typedef const __attribute__((address_space(4))) int32_t* Words;       // (written by no kernel that reads them: scalar loads)
+    const int32_t *lengths = a.k_lengths ? a.k_lengths : a.k_offsets, *starts = a.q_start ? a.q_start : a.q_offsets, *prefixes = a.prefix ? a.prefix : a.q_offsets;
+    const Words qo = (Words)(a.q_offsets + s), ko = (Words)(a.k_offsets + s);
+    const int q0 = qo[0], q1 = qo[1], k0 = ko[0], k1 = ko[1], length = *(Words)(lengths + s), start = *(Words)(starts + s), prefix = *(Words)(prefixes + s);
+    r.q0 = q0;
+    r.k0 = k0;
+    r.qn = (int)((unsigned)q1 - (unsigned)q0);
+    const int room = (int)((unsigned)k1 - (unsigned)k0);
+    r.kn = a.k_lengths ? length : room;
+    r.start = a.q_start ? start : (int)((unsigned)r.kn - (unsigned)r.qn);
+    r.prefix = a.prefix ? prefix : 0;
+    // (ends before starts: a negative offset, or one that falls, fails one of these; places and distances are 32 bits)
+    const bool offsets = (q0 >= 0) & (q1 >= q0) & (q1 <= a.n_q) & (k0 >= 0) & (k1 >= k0) & (k1 <= a.n_k);
+    return offsets & (r.kn >= 0) & (r.kn <= room) & (r.kn <= a.max_k) & (r.qn <= a.max_q) & (r.start >= -(1 << 30)) & (r.start <= 1 << 30);
 }
 
 __device__ __forceinline__ unsigned over_group(const Args& a, unsigned r) { return a.group == 1 ? r : __umulhi(r, a.by_group); }
@@ -445,18 +449,24 @@ struct Sender {
         for (int j = 0; j < L::PER_THREAD; ++j) send(tile, j, (const char*)first + (SAME ? j * apart : 0) + off[SAME ? 0 : j]);
     }
     __device__ __forceinline__ void whole(unsigned char* tile, const T* first) const { whole(tile, first, off, apart); }
-    // row(i): address of passing row i's element 0; null for a row of zeros.  (Worked out anew for the few tiles that need it.)
+    // row(i): address of passing row i's element 0; there: bit i tells whether it is one, and not a row of zeros.  (Worked out anew for the few
+    // tiles that need it.)
     template <typename Row>
-    static __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, Row row) {
+    static __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, uint64_t there, Row row) {
         const int thread = anew<256>((int)threadIdx.x);
 #pragma unroll
         for (int j = 0; j < L::PER_THREAD; ++j) {
-            const T* p = row(row_of(j, thread));
-            send(tile, j, p ? (const void*)(p + element(j, thread, head_dim)) : (const void*)&zeros);
+            const int i = row_of(j, thread);
+            send(tile, j, there >> i & 1 ? (const void*)(row(i) + element(j, thread, head_dim)) : (const void*)&zeros);
         }
     }
 };
-// The same for a word a lane of this wavefront.
+// Which rows of a tile from k0 on are keys and no padding (asked only of tiles that have some), a bit each.
+__device__ __forceinline__ uint64_t keys_there(const Args& a, const Seq& q, int k0, bool padded) {
+    const int k = k0 + (int)(threadIdx.x & 63), doc = padded ? a.k_docs[q.k0 + min(k, q.kn - 1)] : 0;
+    return __ballot(k < q.kn && doc >= 0);
+}
+// A word a lane of this wavefront, sent like a tile.
 __device__ __forceinline__ void send_words(void* to, const void* from) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)to, 4, 0, 0);
 }
@@ -501,7 +511,7 @@ struct Cap {
     float inner, outer;                // what the product is multiplied by on the way in, and tanh on the way out (powers of two)
     template <typename T>
     static __device__ __forceinline__ Cap of(const Args& a) {
-        return {a.cap > 0.f ? a.scale / a.cap * (sizeof(T) == 4 ? 1.f : 2.f * LOG2E) : 0.f, a.cap * LOG2E};
+        return {a.cap_in * (sizeof(T) == 4 ? 1.f : 2.f * LOG2E), a.cap * LOG2E};
     }
     template <typename T>
     __device__ __forceinline__ float bent(float s) const {                // r, or tanh
@@ -540,11 +550,11 @@ __device__ __forceinline__ void put_row(T* row, const f32x16 (&acc)[DP / 32], fl
 
 // The accumulators of a wavefront, [feature][a lane's row] times the lane's `by`, to its 32 rows in memory: by way of LDS, 64 features at a
 // time, so that 8 or 16 lanes write a row's lines whole (64 sequences of 512 tokens, 12 heads of 64, forwards 125 -> 107 us: from the registers
-// a store has 32 pieces of 16 bytes, of 32 lines, and there are 16 of them).  row(r): address of row r's element 0, null if there is none.  mine: PUT_BYTES that no
-// other wavefront uses.  LEFT: not the values, but what their rounding to bf16 leaves.
+// a store has 32 pieces of 16 bytes, of 32 lines, and there are 16 of them).  own: the lane's row in memory, null if there is none.  mine: PUT_BYTES
+// of LDS that no other wavefront uses.  LEFT: not the values, but what their rounding to bf16 leaves.
 constexpr int PUT_BYTES = 32 * 64 * 4;
-template <typename T, int DP, bool LEFT = false, typename Row>
-__device__ __forceinline__ void put_rows(unsigned char* mine, const f32x16 (&acc)[DP / 32], float by, int head_dim, Row row) {
+template <typename T, int DP, bool LEFT = false>
+__device__ __forceinline__ void put_rows(unsigned char* mine, const f32x16 (&acc)[DP / 32], float by, int head_dim, T* own) {
     using P = Tile<T, 64, 32>;
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
 #pragma unroll
@@ -575,7 +585,7 @@ __device__ __forceinline__ void put_rows(unsigned char* mine, const f32x16 (&acc
         for (int j = 0; j < chunks / 2; ++j) {
             const int r = (j * 64 + lane) / chunks, chunk = (j * 64 + lane) % chunks, e = 32 * p + chunk * P::EPC;
             const uint4 x = *(const uint4*)(mine + P::at(r, chunk));
-            T* const to = row(r);
+            T* const to = (T*)((uint64_t)(uint32_t)__shfl((int)((uint64_t)own >> 32), r, 64) << 32 | (uint32_t)__shfl((int)(uint64_t)own, r, 64));
             if (to && e < head_dim) *(uint4*)(to + e) = x;
         }
         __builtin_amdgcn_wave_barrier();

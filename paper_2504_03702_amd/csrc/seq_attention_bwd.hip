@@ -207,11 +207,12 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         // (padding and rows past the end are zeros that see nothing)
         auto row = [&](const T* base, const ps_strides& st, int i) -> const T* {
             const int qi = (int)over_group(a, min(r0 + i, rows - 1)), head = r0 + i - qi * a.group;
-            return r0 + i < rows && (!padded || a.q_docs[q.q0 + qi] >= 0) ? base + qi * st.row + head * st.head : nullptr;
+            return base + qi * st.row + head * st.head;
         };
-        Sender<T, DP, L::ROWS>::rows(smem[buf][0], a.head_dim, [&](int i) { return row(qbase, a.qs, i); });
-        Sender<T, DP, L::ROWS>::rows(smem[buf][1], a.head_dim, [&](int i) { return row(gbase, a.gs, i); });
-        const int r = min(r0 + lane, rows - 1), qi = (int)over_group(a, r);
+        const int r = min(r0 + lane, rows - 1), qi = (int)over_group(a, r), of = padded ? a.q_docs[q.q0 + qi] : 0;
+        const uint64_t there = __ballot(r0 + lane < rows && of >= 0);
+        Sender<T, DP, L::ROWS>::rows(smem[buf][0], a.head_dim, there, [&](int i) { return row(qbase, a.qs, i); });
+        Sender<T, DP, L::ROWS>::rows(smem[buf][1], a.head_dim, there, [&](int i) { return row(gbase, a.gs, i); });
         const void* none = wave == 0 ? (const void*)&infinity_word : wave == 3 ? (const void*)&minus_one : (const void*)&zeros;
         if (has_words) send_words(words + 64 * buf, r0 + lane < rows ? word(q.q0 + qi, hk * a.group + r - qi * a.group) : none);
         if (wave == 0) s_place[buf][lane] = (float)(q.start - k0 + qi);
@@ -269,17 +270,17 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     if (wk0 >= q.kn) return;
     unsigned char* const mine = smem[0][0] + wave * PUT_BYTES;
     static_assert(sizeof(smem) >= 4 * PUT_BYTES, "rows on their way out");
-    auto each = [&](auto* first, int64_t step) {                          // the wavefront's keys, from the tensor's first one of this head on
-        return [&, first, step](int r) { return wk0 + r < q.kn ? first + (q.k0 + wk0 + r) * step : nullptr; };
-    };
+    const int own = wk0 + (anew<256>((int)threadIdx.x) & 31);              // (the key, worked out again)
+    const bool is = own < q.kn;
+    const int64_t to = q.k0 + own;
     if (a.key_parts > 1) {
-        const int64_t first = ((int64_t)part * a.n_k * a.kv_heads + hk) * a.head_dim, step = (int64_t)a.kv_heads * a.head_dim;
-        put_rows<float, DP>(mine, dk, 1.f, a.head_dim, each(a.part_dk + first, step));
-        put_rows<float, DP>(mine, dv, 1.f, a.head_dim, each(a.part_dv + first, step));
+        const int64_t at = (((int64_t)part * a.n_k + to) * a.kv_heads + hk) * a.head_dim;
+        put_rows<float, DP>(mine, dk, 1.f, a.head_dim, is ? a.part_dk + at : nullptr);
+        put_rows<float, DP>(mine, dv, 1.f, a.head_dim, is ? a.part_dv + at : nullptr);
         return;
     }
-    put_rows<T, DP>(mine, dk, by_x<T>(a), a.head_dim, each((T*)a.dk + hk * a.dks.head, a.dks.row));
-    put_rows<T, DP>(mine, dv, 1.f, a.head_dim, each((T*)a.dv + hk * a.dvs.head, a.dvs.row));
+    put_rows<T, DP>(mine, dk, by_x<T>(a), a.head_dim, is ? (T*)a.dk + to * a.dks.row + hk * a.dks.head : nullptr);
+    put_rows<T, DP>(mine, dv, 1.f, a.head_dim, is ? (T*)a.dv + to * a.dvs.row + hk * a.dvs.head : nullptr);
 }
 
 // Queries fixed: dq of FIXED rows of a key head's queries.  Three products a tile (a fourth for the rest): 16 x 2048 with prefix and cap, heads of
@@ -370,13 +371,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     const bool regular = keys.regular && values.regular;
     auto request = [&](int t, bool padded, int buf) {
         const int k0 = t * L::ROWS;
-        auto is = [&](int i) { return k0 + i < q.kn && (!padded || a.k_docs[q.k0 + k0 + i] >= 0); };
         if (k0 + L::ROWS <= q.kn && !padded && regular) {
             keys.whole(smem[buf][0], kbase + k0 * a.ks.row);
             values.whole(smem[buf][1], vbase + k0 * a.vs.row);
         } else {
-            keys.rows(smem[buf][0], a.head_dim, [&](int i) { return is(i) ? kbase + (k0 + i) * a.ks.row : nullptr; });
-            values.rows(smem[buf][1], a.head_dim, [&](int i) { return is(i) ? vbase + (k0 + i) * a.vs.row : nullptr; });
+            const uint64_t there = keys_there(a, q, k0, padded);
+            keys.rows(smem[buf][0], a.head_dim, there, [&](int i) { return kbase + (k0 + i) * a.ks.row; });
+            values.rows(smem[buf][1], a.head_dim, there, [&](int i) { return vbase + (k0 + i) * a.vs.row; });
         }
         if (a.k_docs && wave == 0) send_words(s_doc[buf], a.k_docs + q.k0 + min(k0 + lane, q.kn - 1));
     };
@@ -434,17 +435,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     if (wr0 >= rows) return;
     unsigned char* const mine = smem[0][0] + wave * PUT_BYTES;
     static_assert(sizeof(smem) >= 4 * PUT_BYTES, "rows on their way out");
-    auto each = [&](auto put) {                                           // row r of the wavefront, as token and head
-        return [&, put](int r) {
-            const int at = wr0 + r, qi = (int)over_group(a, min(at, rows - 1)), head = hk * a.group + min(at, rows - 1) - qi * a.group;
-            return at < rows ? put((int64_t)q.q0 + qi, head) : nullptr;
-        };
-    };
     if (a.parts > 1)
         put_rows<float, DP>(mine, dq, 1.f, a.head_dim,
-                            each([&](int64_t token, int head) { return a.part_o + (((int64_t)part * a.n_q + token) * a.heads + head) * a.head_dim; }));
+                            live ? a.part_o + (((int64_t)part * a.n_q + token) * a.heads + head) * a.head_dim : nullptr);
     else
-        put_rows<T, DP>(mine, dq, by_x<T>(a), a.head_dim, each([&](int64_t token, int head) { return (T*)a.dq + token * a.dqs.row + head * a.dqs.head; }));
+        put_rows<T, DP>(mine, dq, by_x<T>(a), a.head_dim, live ? (T*)a.dq + token * a.dqs.row + head * a.dqs.head : nullptr);
 }
 
 // A gradient's shares added up, a thread four neighbours: those of queries (z = 0), keys (1) and values (2).  3365 tokens, 8 heads of 80 on 4,

@@ -31,7 +31,7 @@ struct Row {
         head = hk * a.group + r - qi * a.group;
         token = q.q0 + qi;
         place = q.start + qi;
-        slope = a.slopes ? a.slopes[head] * (a.cap > 0.f ? LOG2E : 1.f / a.scale) : 0.f;
+        slope = a.slopes ? a.slopes[head] * a.slope_by : 0.f;
         doc = a.q_docs ? a.q_docs[token] : 0;
         end = a.causal ? min(q.kn, max(place + 1, q.prefix)) : q.kn;
         qf.load((const T*)a.q + token * a.qs.row + head * a.qs.head, live && doc >= 0, a.head_dim, half);
@@ -198,13 +198,13 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     auto request = [&](int t, bool padded, int buf) {
         const int k0 = t * L::ROWS;
         // (rows past the keys, and padding, are zeros: their weights are, and nothing is to come of them)
-        auto is = [&](int i) { return k0 + i < q.kn && (!padded || a.k_docs[q.k0 + k0 + i] >= 0); };
         if (k0 + L::ROWS <= q.kn && !padded && regular) {
             keys.whole(smem[buf][0], kbase + k0 * a.ks.row);
             values.whole(smem[buf][1], vbase + k0 * a.vs.row);
         } else {
-            keys.rows(smem[buf][0], a.head_dim, [&](int i) { return is(i) ? kbase + (k0 + i) * a.ks.row : nullptr; });
-            values.rows(smem[buf][1], a.head_dim, [&](int i) { return is(i) ? vbase + (k0 + i) * a.vs.row : nullptr; });
+            const uint64_t there = keys_there(a, q, k0, padded);
+            keys.rows(smem[buf][0], a.head_dim, there, [&](int i) { return kbase + (k0 + i) * a.ks.row; });
+            values.rows(smem[buf][1], a.head_dim, there, [&](int i) { return vbase + (k0 + i) * a.vs.row; });
         }
         if (a.k_docs && wave == 0) send_words(s_doc[buf], a.k_docs + q.k0 + min(k0 + lane, q.kn - 1));
     };
@@ -230,22 +230,16 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     if (wr0 >= rows) return;
     unsigned char* const mine = smem[0][0] + wave * PUT_BYTES;
     static_assert(sizeof(smem) >= 4 * PUT_BYTES, "rows on their way out");
-    auto each = [&](auto put) {                                           // row r of the wavefront, as token and head
-        return [&, put](int r) {
-            const int at = wr0 + r, qi = (int)over_group(a, min(at, rows - 1)), head = hk * a.group + min(at, rows - 1) - qi * a.group;
-            return at < rows ? put((int64_t)q.q0 + qi, head) : nullptr;
-        };
-    };
     if (PARTS) {
-        const int64_t first = (int64_t)part * a.n_q;
-        put_rows<float, DP>(mine, row.o, 1.f, a.head_dim, each([&](int64_t token, int head) { return a.part_o + ((first + token) * a.heads + head) * a.head_dim; }));
-        if (live && half == 0) a.part_ml[(first + row.token) * a.heads + row.head] = make_float2(row.m, row.l);
+        const int64_t at = ((int64_t)part * a.n_q + row.token) * a.heads + row.head;
+        put_rows<float, DP>(mine, row.o, 1.f, a.head_dim, live ? a.part_o + at * a.head_dim : nullptr);
+        if (live && half == 0) a.part_ml[at] = make_float2(row.m, row.l);
         return;
     }
     const float inv = row.l == 0.f ? 0.f : 1.f / row.l;
-    put_rows<T, DP>(mine, row.o, inv, a.head_dim, each([&](int64_t token, int head) { return (T*)a.out_w + token * a.os.row + head * a.os.head; }));
+    put_rows<T, DP>(mine, row.o, inv, a.head_dim, live ? (T*)a.out_w + row.token * a.os.row + row.head * a.os.head : nullptr);
     if (sizeof(T) == 2 && a.rest_w)
-        put_rows<T, DP, true>(mine, row.o, inv, a.head_dim, each([&](int64_t token, int head) { return (T*)a.rest_w + (token * a.heads + head) * a.head_dim; }));
+        put_rows<T, DP, true>(mine, row.o, inv, a.head_dim, live ? (T*)a.rest_w + (row.token * a.heads + row.head) * a.head_dim : nullptr);
     if (a.lse_w && live && half == 0) a.lse_w[(int64_t)row.head * a.n_q + row.token] = lse_of(row.m, row.l);
 }
 
@@ -284,14 +278,14 @@ struct Few {
 #pragma unroll
         for (int j = 0; j < SENDS; ++j) send(tile, j, (const char*)first + j / PERIOD * ROWS_A_PERIOD * step[x] + off[x][j % PERIOD]);
     }
-    // row(i): address of row i, null for zeros
+    // row(i): address of row i; there: bit i tells whether it is one, and not zeros
     template <typename Address>
-    static __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, Address row) {
+    static __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, uint64_t there, Address row) {
         const int lane = anew<256>((int)(threadIdx.x & 63));
 #pragma unroll
         for (int j = 0; j < SENDS; ++j) {
-            const T* p = row(row_of(j, lane));
-            send(tile, j, p ? (const void*)(p + element(j, lane, head_dim)) : (const void*)&zeros);
+            const int i = row_of(j, lane);
+            send(tile, j, there >> i & 1 ? (const void*)(row(i) + element(j, lane, head_dim)) : (const void*)&zeros);
         }
     }
 };
@@ -332,9 +326,9 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
             few.whole(keys, 0, kbase + k0 * a.ks.row);
             few.whole(values, 1, vbase + k0 * a.vs.row);
         } else {
-            auto is = [&](int i) { return k0 + i < q.kn && (!a.k_docs || a.k_docs[q.k0 + k0 + i] >= 0); };
-            F::rows(keys, a.head_dim, [&](int i) { return is(i) ? kbase + (k0 + i) * a.ks.row : nullptr; });
-            F::rows(values, a.head_dim, [&](int i) { return is(i) ? vbase + (k0 + i) * a.vs.row : nullptr; });
+            const uint64_t there = keys_there(a, q, k0, a.k_docs != nullptr);
+            F::rows(keys, a.head_dim, there, [&](int i) { return kbase + (k0 + i) * a.ks.row; });
+            F::rows(values, a.head_dim, there, [&](int i) { return vbase + (k0 + i) * a.vs.row; });
         }
         send_words(s_doc[wave][stage], a.k_docs ? (const void*)(a.k_docs + q.k0 + min(k0 + lane, q.kn - 1)) : (const void*)&zeros);
     };
@@ -589,6 +583,8 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
     a.n_q = d->n_q; a.n_k = d->n_k; a.n_seq = d->n_seq; a.heads = d->heads; a.kv_heads = d->kv_heads; a.head_dim = d->head_dim;
     a.group = (int32_t)group; a.max_q = (int32_t)min((int64_t)d->max_q, d->n_q); a.max_k = (int32_t)min((int64_t)d->max_k, d->n_k); a.causal = d->causal;
     a.scale = d->scale; a.cap = d->softcap;
+    a.slope_by = d->softcap > 0.f ? LOG2E : 1.f / d->scale;
+    a.cap_in = d->softcap > 0.f ? d->scale / d->softcap : 0.f;
     a.by_group = group > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)group + 1) : 0;
     a.row_blocks = (int32_t)(((int64_t)a.max_q * group + FIXED - 1) / FIXED);
     // Blocks that do not fill the chip, or of which the longest would be waited for: their tiles are shared out, so that there are
