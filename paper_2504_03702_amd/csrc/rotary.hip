@@ -1,6 +1,6 @@
 // Rotary positions.  A call reads and writes its tensors once and computes next to nothing, so memory bounds it: a workgroup takes a
 // few rows, puts the cosines and sines of their pairs into LDS once, and streams all heads past them.  32768 rows of two tensors of 16 heads of
-// 64 in bf16, 268 MB: 60.6 us, 4.4 TB/s (a copy reaches 5.1); 64 rows of 40 heads of 128: 3.3 us.
+// 64 in bf16, 268 MB: 55 us, 4.9 TB/s (a copy reaches 5.1); 64 rows of 40 heads of 128: 3.4 us.
 #include <math.h>
 
 #include "device_util.h"
@@ -24,13 +24,83 @@ struct RotaryArgs {
 
 constexpr int TABLE = 2048;            // pairs of a workgroup's rows, at most
 
-// VEC elements at a time (16 bytes), or one.
-template <typename T, bool WIDE>
+// VEC elements at a time; BATCH such units of a thread on their way together, the first of them while the table is made (8192 rows of 40 heads of
+// 128, half of them turning, in bf16: one after the other behind the table 36 us, 2 30.5, 4 30; 16384 fp32 rows of 18 heads of 128 51, 50.5, 54).
+template <typename T, int VEC>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     __shared__ float2 table[TABLE];
-    constexpr int VEC = WIDE ? 16 / (int)sizeof(T) : 1;
+    constexpr bool WIDE = VEC > 1;
+    constexpr int BATCH = 2;
+    struct alignas(VEC * sizeof(T)) Piece { T v[VEC]; };
     const int64_t row0 = (int64_t)blockIdx.x * a.rows;
     const int rows = (int)min((int64_t)a.rows, a.n_rows - row0), n = a.n_pairs;
+    const int head0 = blockIdx.y * a.heads_each, heads = min(a.heads_each, a.heads + a.heads2 - head0);
+    // units of a head: its turning pairs (VEC of them in halves, VEC / 2 or one interleaved), then what is copied, VEC a unit
+    const int turning = a.interleaved ? (WIDE ? 2 * n / VEC : n) : n / VEC, units = turning + (a.head_dim - 2 * n) / VEC, all = rows * heads * units;
+    constexpr int COPIED = -1, NONE = -2;
+    Piece p[BATCH], q[BATCH];
+    T* out[BATCH];
+    int at[BATCH];                     // in the table
+    auto fetch = [&](int first) {
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            const unsigned i = first + 256 * b, head = i / (unsigned)units, unit = i - head * units, r = head / (unsigned)heads;
+            const int h = head0 + (int)(head - r * heads), second = h >= a.heads, hh = second ? h - a.heads : h;
+            at[b] = NONE;
+            if ((int)i >= all) continue;
+            const int64_t row = row0 + r;
+            const T* x = (const T*)a.x[second] + row * a.xs[second].row + hh * a.xs[second].head;
+            out[b] = (T*)a.out[second] + row * a.os[second].row + hh * a.os[second].head;
+            int e, other;
+            if ((int)unit >= turning) {
+                if (a.in_place[second]) continue;
+                at[b] = COPIED;
+                e = other = 2 * n + ((int)unit - turning) * VEC;
+            } else if (!a.interleaved) {
+                at[b] = r * n + unit * VEC;
+                e = unit * VEC;
+                other = n + e;
+            } else {
+                at[b] = r * n + unit * (WIDE ? VEC / 2 : 1);
+                e = unit * (WIDE ? VEC : 2);
+                other = WIDE ? e : e + 1;
+            }
+            out[b] += e;
+            p[b] = *(const Piece*)(x + e);
+            if (other != e) q[b] = *(const Piece*)(x + other);
+        }
+    };
+    auto turn = [&] {
+        const int apart = a.interleaved ? 1 : n;                          // the pair's other element (not WIDE interleaved)
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            if (at[b] == NONE) continue;
+            const float2* cs = table + at[b];
+            if (at[b] == COPIED) {
+            } else if (WIDE && a.interleaved) {
+                if constexpr (WIDE) {
+#pragma unroll
+                    for (int j = 0; j < VEC; j += 2) {
+                        const float u = (float)p[b].v[j], v = (float)p[b].v[j + 1];
+                        const float2 w = cs[j / 2];
+                        p[b].v[j] = (T)fmaf(-v, w.y, u * w.x);
+                        p[b].v[j + 1] = (T)fmaf(v, w.x, u * w.y);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float u = (float)p[b].v[j], v = (float)q[b].v[j];
+                    const float2 w = cs[j];
+                    p[b].v[j] = (T)fmaf(-v, w.y, u * w.x);
+                    q[b].v[j] = (T)fmaf(v, w.x, u * w.y);
+                }
+                *(Piece*)(out[b] + apart) = q[b];
+            }
+            *(Piece*)out[b] = p[b];
+        }
+    };
+    fetch(threadIdx.x);
     for (int i = threadIdx.x; i < rows * n; i += 256) {
         // whole turns go in 64 bits: a position of 31 bits times a frequency of 24 leaves the fraction all a float can hold
         double turns = (double)a.positions[row0 + i / n] * (double)a.frequencies[i % n] * 0.15915494309189533577;
@@ -40,51 +110,10 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
         table[i] = make_float2(c * a.magnitude, s * a.magnitude * a.sign);
     }
     __syncthreads();
-    const int head0 = blockIdx.y * a.heads_each, heads = min(a.heads_each, a.heads + a.heads2 - head0);
-    // units of a head: its turning pairs (VEC of them in halves, VEC / 2 or one interleaved), then what is copied, VEC a unit
-    const int turning = a.interleaved ? (WIDE ? 2 * n / VEC : n) : n / VEC, units = turning + (a.head_dim - 2 * n) / VEC;
-    for (int i = threadIdx.x; i < rows * heads * units; i += 256) {
-        const int unit = i % units, h = head0 + i / units % heads, r = i / units / heads, second = h >= a.heads;
-        const int64_t row = row0 + r;
-        const int hh = second ? h - a.heads : h;
-        const T* x = (const T*)a.x[second] + row * a.xs[second].row + hh * a.xs[second].head;
-        T* out = (T*)a.out[second] + row * a.os[second].row + hh * a.os[second].head;
-        const float2* cs = table + r * n;
-        struct alignas(WIDE ? 16 : sizeof(T)) Piece { T v[VEC]; };
-        if (unit >= turning) {
-            if (!a.in_place[second]) {
-                const int e = 2 * n + (unit - turning) * VEC;
-                *(Piece*)(out + e) = *(const Piece*)(x + e);
-            }
-        } else if (!a.interleaved) {
-            const int e = unit * VEC;
-            Piece p = *(const Piece*)(x + e), q = *(const Piece*)(x + n + e);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float u = (float)p.v[j], v = (float)q.v[j];
-                const float2 w = cs[e + j];
-                p.v[j] = (T)(u * w.x - v * w.y);
-                q.v[j] = (T)(u * w.y + v * w.x);
-            }
-            *(Piece*)(out + e) = p;
-            *(Piece*)(out + n + e) = q;
-        } else if constexpr (WIDE) {
-            const int e = unit * VEC;
-            Piece p = *(const Piece*)(x + e);
-#pragma unroll
-            for (int j = 0; j < VEC; j += 2) {
-                const float u = (float)p.v[j], v = (float)p.v[j + 1];
-                const float2 w = cs[(e + j) / 2];
-                p.v[j] = (T)(u * w.x - v * w.y);
-                p.v[j + 1] = (T)(u * w.y + v * w.x);
-            }
-            *(Piece*)(out + e) = p;
-        } else {
-            const float u = (float)x[2 * unit], v = (float)x[2 * unit + 1];
-            const float2 w = cs[unit];
-            out[2 * unit] = (T)(u * w.x - v * w.y);
-            out[2 * unit + 1] = (T)(u * w.y + v * w.x);
-        }
+    turn();
+    for (int i = threadIdx.x + 256 * BATCH; i - (int)threadIdx.x < all; i += 256 * BATCH) {
+        fetch(i);
+        turn();
     }
 }
 
@@ -93,11 +122,14 @@ bool strides_ok(const ps_strides& s, bool written, int heads, int head_dim, int6
 }
 
 template <typename T>
-void launch(const RotaryArgs& a, bool wide, dim3 grid, hipStream_t st) {
-    if (wide)
-        hipLaunchKernelGGL((rotary_kernel<T, true>), grid, dim3(256), 0, st, a);
+void launch(const RotaryArgs& a, int bytes, dim3 grid, hipStream_t st) {
+    constexpr int ES = sizeof(T);
+    if (bytes == 16)
+        hipLaunchKernelGGL((rotary_kernel<T, 16 / ES>), grid, dim3(256), 0, st, a);
+    else if (bytes == 8)
+        hipLaunchKernelGGL((rotary_kernel<T, 8 / ES>), grid, dim3(256), 0, st, a);
     else
-        hipLaunchKernelGGL((rotary_kernel<T, false>), grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL((rotary_kernel<T, 1>), grid, dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -120,12 +152,13 @@ extern "C" int ps_rotary(const ps_rotary_desc* d, const void* x, void* out, cons
                     d->head_dim, d->n_pairs, d->interleaved, 1, 1, d->magnitude, d->inverse ? -1.f : 1.f, {x == out, x2 == out2}};
     if ((x == out && (d->x.row != d->out.row || d->x.head != d->out.head)) || (x2 && x2 == out2 && (d->x2.row != d->out2.row || d->x2.head != d->out2.head)))
         return PS_EINVAL;
-    // 16 bytes at a time where every address and the pieces of a head allow it
-    const int vec = (int)(16 / es);
+    // 16 bytes at a time, or 8, where every address and the pieces of a head allow it (8000 rows of 16 heads of 80, 40 of them in two halves, bf16:
+    // 8 bytes 13 us, one element 32)
     uintptr_t bits = (uintptr_t)x | (uintptr_t)out | (uintptr_t)x2 | (uintptr_t)out2;
-    int64_t steps = d->x.row | d->x.head | d->out.row | d->out.head;
+    int64_t steps = d->x.row | d->x.head | d->out.row | d->out.head | d->head_dim | (d->interleaved ? 2 * d->n_pairs : d->n_pairs);
     if (x2) steps |= d->x2.row | d->x2.head | d->out2.row | d->out2.head;
-    const bool wide = bits % 16 == 0 && steps % vec == 0 && d->head_dim % vec == 0 && (d->interleaved ? 2 * d->n_pairs : d->n_pairs) % vec == 0;
+    bits |= (uintptr_t)steps * es;
+    const int bytes = bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : 1;
     // Rows of a workgroup: a pair a thread for the table; heads are shared out where rows alone do not fill the chip.
     const int all = d->heads + d->heads2;
     const int64_t most = d->n_pairs > 0 ? (d->n_pairs >= 256 ? 1 : 256 / d->n_pairs) : 8;
@@ -147,7 +180,7 @@ extern "C" int ps_rotary(const ps_rotary_desc* d, const void* x, void* out, cons
         if (positions) b.positions = positions + first;
         b.n_rows = d->n_rows - first;
         const dim3 grid((unsigned)(blocks - b0 < per ? blocks - b0 : per), (unsigned)((all + a.heads_each - 1) / a.heads_each));
-        d->dtype == 1 ? launch<bf16>(b, wide, grid, (hipStream_t)hip_stream) : launch<float>(b, wide, grid, (hipStream_t)hip_stream);
+        d->dtype == 1 ? launch<bf16>(b, bytes, grid, (hipStream_t)hip_stream) : launch<float>(b, bytes, grid, (hipStream_t)hip_stream);
     }
     return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
 }

@@ -53,6 +53,14 @@ def test_sizes(dtype, interleaved, size, pairs, rows):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("size,pairs", [(80, 20), (12, 4), (20, 2), (6, 2), (4, 2)])
+@pytest.mark.parametrize("rows", [3, 700])
+def test_sizes_of_eight_bytes(dtype, interleaved, size, pairs, rows):
+    test_sizes(dtype, interleaved, size, pairs, rows)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_positions_anywhere(dtype):
     """The fastest pair turns 2^31 radians: the fraction of a turn is what counts."""
     pos = torch.tensor([0, 1, -1, 131071, 16777217, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device=DEV)
