@@ -355,7 +355,7 @@ int ps_attention_backward(const ps_attention_desc* desc, const ps_attention_seqs
  *   x2, out2    NULL, or a second pair of tensors (the keys) with heads2 heads, turned by the same angles
  *   positions   [n_rows] int32, any value;  frequencies [n_pairs] float, radians a position
  * The angle is reduced with the product's rounding error taken into account: large positions lose nothing.
- * Strides: multiples of one element here; rows whose strides, addresses and halves are multiples of 16 bytes, or 8, are moved faster.
+ * Strides: multiples of one element here; heads whose size and turning pieces are multiples of 16 bytes, or 8, are moved faster.
  * Errors: PS_EINVAL (null pointers, negative sizes or strides, 2 n_pairs > head_dim), PS_EUNSUPPORTED (head_dim above 4096, 2^27
  * elements or more in a row's heads, n_rows above 2^31 - 1), PS_EHIP. */
 typedef struct ps_rotary_desc {

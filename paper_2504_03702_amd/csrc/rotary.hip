@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     __shared__ float2 table[TABLE];
     constexpr bool WIDE = VEC > 1;
     constexpr int BATCH = 2;
-    struct alignas(VEC * sizeof(T)) Piece { T v[VEC]; };
+    struct Piece { T v[VEC]; };          // (moved whole at any address)
     const int64_t row0 = (int64_t)blockIdx.x * a.rows;
     const int rows = (int)min((int64_t)a.rows, a.n_rows - row0), n = a.n_pairs;
     const int head0 = blockIdx.y * a.heads_each, heads = min(a.heads_each, a.heads + a.heads2 - head0);
@@ -152,13 +152,10 @@ extern "C" int ps_rotary(const ps_rotary_desc* d, const void* x, void* out, cons
                     d->head_dim, d->n_pairs, d->interleaved, 1, 1, d->magnitude, d->inverse ? -1.f : 1.f, {x == out, x2 == out2}};
     if ((x == out && (d->x.row != d->out.row || d->x.head != d->out.head)) || (x2 && x2 == out2 && (d->x2.row != d->out2.row || d->x2.head != d->out2.head)))
         return PS_EINVAL;
-    // 16 bytes at a time, or 8, where every address and the pieces of a head allow it (8000 rows of 16 heads of 80, 40 of them in two halves, bf16:
-    // 8 bytes 13 us, one element 32)
-    uintptr_t bits = (uintptr_t)x | (uintptr_t)out | (uintptr_t)x2 | (uintptr_t)out2;
-    int64_t steps = d->x.row | d->x.head | d->out.row | d->out.head | d->head_dim | (d->interleaved ? 2 * d->n_pairs : d->n_pairs);
-    if (x2) steps |= d->x2.row | d->x2.head | d->out2.row | d->out2.head;
-    bits |= (uintptr_t)steps * es;
-    const int bytes = bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : 1;
+    // 16 bytes at a time, or 8, where the pieces of a head allow it, at whatever addresses (8000 rows of 16 heads of 80, 40 of them in two halves,
+    // bf16: 8 bytes 13 us, one element 32; 16384 rows of 16 heads of 64 that start an odd element apart 14, one element 35)
+    const uintptr_t pieces = (uintptr_t)(d->head_dim | (d->interleaved ? 2 * d->n_pairs : d->n_pairs)) * es;
+    const int bytes = pieces % 16 == 0 ? 16 : pieces % 8 == 0 ? 8 : 1;
     // Rows of a workgroup: a pair a thread for the table; heads are shared out where rows alone do not fill the chip.
     const int all = d->heads + d->heads2;
     const int64_t most = d->n_pairs > 0 ? (d->n_pairs >= 256 ? 1 : 256 / d->n_pairs) : 8;
