@@ -594,15 +594,16 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
     a.tile = tile_rows(d->dtype == 1 ? 2 : 4);
     a.key_tile = key_tile_rows(d->dtype == 1 ? 2 : 4, padded(d->head_dim));
     auto share = [&](int64_t blocks_a_seq, int64_t tokens, int64_t tokens_a_block, int64_t passing, int64_t all_passing, int tile, int32_t& parts,
-                     int32_t& part_tiles) {
+                     int32_t& part_tiles, int64_t chain) {
         const int tiles = (int)((passing + tile - 1) / tile);
         const int64_t all_tiles = all_passing / tile + a.n_seq;
         const int64_t blocks = a.kv_heads * min((int64_t)a.n_seq * blocks_a_seq, tokens / tokens_a_block + a.n_seq);
         parts = 1;
         part_tiles = tiles;
-        if (blocks >= 512 || tiles < 2 * 256 / tile) return;
+        const int least = blocks < 128 && passing > chain ? 64 : 256;
+        if (blocks >= 512 || tiles < 2 * least / tile) return;
         const int64_t jobs = a.kv_heads * all_tiles * max((int64_t)1, blocks / max(1, a.n_seq * a.kv_heads));
-        part_tiles = (int32_t)min((int64_t)tiles, max((int64_t)256 / tile, jobs / 2048));
+        part_tiles = (int32_t)min((int64_t)tiles, max((int64_t)least / tile, jobs / 2048));
         // (what the shares leave to be added up stays within 256 MB)
         const int64_t most = max((int64_t)1, ((int64_t)64 << 20) / max((int64_t)1, tokens * a.kv_heads * a.head_dim));
         part_tiles = (int32_t)max((int64_t)part_tiles, (tiles + most - 1) / most);
@@ -619,9 +620,12 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
         a.part_tiles = (int32_t)max(max(min(max((int64_t)16, jobs / 256), (int64_t)32), jobs / 1024), (tiles + most - 1) / most);
         a.parts = (int32_t)max((int64_t)1, (tiles + a.part_tiles - 1) / a.part_tiles);
     } else {
-        share(a.row_blocks, d->n_q * group, FIXED, a.max_k, d->n_k, a.tile, a.parts, a.part_tiles);
+        share(a.row_blocks, d->n_q * group, FIXED, a.max_k, d->n_k, a.tile, a.parts, a.part_tiles, INT32_MAX);
     }
-    share((a.max_k + FIXED - 1) / FIXED, d->n_k, FIXED, rows_a_seq, d->n_q * group, a.key_tile, a.key_parts, a.key_part_tiles);
+    // Of few blocks of keys, shares of 64 rows: a block's chain of tiles, the rows of all its head's heads, is all that takes time.  The sum's launch
+    // is worth it above 256 rows, 128 in fp32 (passes of 1 sequence of 191 tokens, 48 heads on 12, 61 -> 52 us; 14 of up to 70, 16 heads of 128 on
+    // 4, 49 -> 43; fp32, 4 of 56, 4 heads on 1, 82 -> 56; 4 of 128 rows, 12 heads, would take 34 for 28).
+    share((a.max_k + FIXED - 1) / FIXED, d->n_k, FIXED, rows_a_seq, d->n_q * group, a.key_tile, a.key_parts, a.key_part_tiles, d->dtype == 1 ? 256 : 128);
     // (a grid holds fewer than 2^32 threads)
     if ((int64_t)a.kv_heads * a.row_blocks * a.parts >= 1 << 24 || (int64_t)a.kv_heads * ((a.max_k + FIXED - 1) / FIXED) * a.key_parts >= 1 << 24)
         return PS_EUNSUPPORTED;
