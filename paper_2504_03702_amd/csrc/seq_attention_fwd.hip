@@ -137,7 +137,7 @@ struct Row {
 // takes them; tiles of 64 keys (32 in fp32), two of them in LDS, for two or three workgroups a unit.  Bound by the issue of vector
 // instructions beside the matrix ones: with heads of 128 under a cap (16 prompts of 1500 to 2048 tokens with prefix, 16 heads on 4) 450 us,
 // 0.52 PFLOP/s, vector units issuing 47 % and matrix units busy 26 % of the time with 1.7 wavefronts a SIMD; documents in two rows of 8192, 16
-// heads of 64: 100 us, 0.36 PFLOP/s.  A call of short prompts (64 of 4 to 512 tokens, 12 heads of 64: 36 us) waits for its first tiles 45 % of a
+// heads of 64: 95 us, 0.38 PFLOP/s.  A call of short prompts (64 of 4 to 512 tokens, 12 heads of 64: 34 us) waits for its first tiles 43 % of a
 // wavefront's time.  Three tiles in LDS, priorities around the matrix instructions and the sum of a row's weights by dot products made
 // no difference (100 +- 2 us).
 template <typename T, int DP, bool PARTS>
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
 // workgroup's wavefronts have the same rows and take tiles of 32 keys in turn, each with tiles of its own on their way through LDS, so
 // none waits for another until their rows are put together at the end.  Bound by memory: 32 caches of 500 to 32768 keys, 8 heads of 128, 1.05 GB
 // in 203 us, 5.2 TB/s (a copy reaches 5.1); one cache of 65521 keys, 4 heads, 134 MB in 28 us, 4.8 TB/s; 8 first rows over up to 512 keys
-// 8.7 us, most of it the way to the first tile and out.
+// 8.5 us, most of it the way to the first tile and out.
 template <typename T, int DP>
 struct Few {
     using L = Tile<T, DP, 32>;
