@@ -32,7 +32,7 @@ class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, seqs, scale, softcap, causal, slopes):
         train = any(ctx.needs_input_grad[:3])
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)             # (the kernels leave rows that no sequence has alone)
         lse = torch.empty(q.shape[1], q.shape[0], device=q.device)
         rest = torch.empty_like(out) if train and q.dtype == torch.bfloat16 else None
         shape = (seqs.q_offsets.numel() - 1, q.shape[0], k.shape[0], seqs.max_q, seqs.max_k, q.shape[1], k.shape[1], q.shape[2], q.dtype)
@@ -56,7 +56,8 @@ class _Attention(torch.autograd.Function):
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: Sequences, scale: Optional[float] = None, softcap: float = 0.0,
               causal: bool = False, slopes: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Attention of packed q [n_q, heads, size] to k, v [n_k, kv_heads, size]; slopes are constants."""
+    """Attention of packed q [n_q, heads, size] to k, v [n_k, kv_heads, size]; slopes are constants.  Rows that no sequence has, or a
+    faulty one, are zeros, as is their gradient."""
     return _Attention.apply(q, k, v, seqs, scale, softcap, causal, slopes)
 
 

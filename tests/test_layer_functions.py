@@ -1,0 +1,112 @@
+"""The layer functions around the kernels: what they hand over, keep for the gradients and refuse.  The 64-bit definitions stand in
+for the kernels, on the CPU, and write what those write: rows of sequences that keep the rules, no others."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer as ol
+from paper_2504_03702_amd import binding as ps
+from paper_2504_03702_amd import layers
+
+
+def of(t):
+    return None if t is None else t.detach().double().numpy()
+
+
+def put(to, rows):
+    """Rows that the definition has (the others are NaN there) into a call's tensor."""
+    rows = torch.from_numpy(rows)
+    there = ~rows.isnan()
+    to[there] = rows[there].to(to.dtype)
+
+
+def attention(q, k, v, q_offsets, k_offsets, max_q, max_k, softcap, causal, slopes, status, **how):
+    """A call's sequences that keep the rules: (out, lse) or the gradients too."""
+    dout = how.pop("dout", None)
+    n = q_offsets.diff().tolist()
+    good = [i for i in range(len(n)) if n[i] <= max_q and k_offsets.diff()[i] <= max_k]
+    if len(good) < len(n) and status is not None:
+        status[0] = ps.PS_ST_BAD_LENGTH
+    q_docs, k_docs = how.pop("q_docs"), how.pop("k_docs")
+    got = None
+    for i in good:
+        rows, keys = slice(*q_offsets[i:i + 2].tolist()), slice(*k_offsets[i:i + 2].tolist())
+        one = {m: None if t is None else t[i:i + 1].numpy() for m, t in how.items()}
+        offsets = ([0, rows.stop - rows.start], [0, keys.stop - keys.start])
+        parts = ol.attention(of(q)[rows], of(k)[keys], of(v)[keys], *offsets, causal=causal, cap=softcap, slopes=of(slopes),
+                             q_docs=None if q_docs is None else q_docs[rows].numpy(), k_docs=None if k_docs is None else k_docs[keys].numpy(),
+                             dout=None if dout is None else of(dout)[rows], **one)
+        if got is None:
+            got = [np.full(s, np.nan) for s in (q.shape, (q.shape[1], q.shape[0]), q.shape, k.shape, k.shape)][:len(parts)]
+        for to, part, at in zip(got, parts, (rows, (slice(None), rows), rows, keys, keys)):
+            to[at] = part
+    return got
+
+
+@pytest.fixture
+def stand_ins(monkeypatch):
+    """The calls made, by name; tensors that are not filled on purpose hold NaN."""
+    calls = []
+
+    def forward(q, k, v, q_offsets, k_offsets, max_q, max_k, out, lse, workspace, scale=None, softcap=0.0, causal=False, slopes=None,
+                status=None, out_rest=None, **how):
+        calls.append(("forward", status))
+        for to, rows in zip((out, lse), attention(q, k, v, q_offsets, k_offsets, max_q, max_k, softcap, causal, slopes, status, **how) or ()):
+            put(to, rows)
+        if out_rest is not None:
+            out_rest.zero_()
+
+    def backward(q, k, v, out, lse, dout, q_offsets, k_offsets, max_q, max_k, dq, dk, dv, workspace, scale=None, softcap=0.0, causal=False,
+                 slopes=None, status=None, out_rest=None, **how):
+        calls.append(("backward", status))
+        if dout.data_ptr() % 16:
+            raise ps.PsError(-1, "dout")
+        got = attention(q, k, v, q_offsets, k_offsets, max_q, max_k, softcap, causal, slopes, status, dout=dout, **how)
+        for to, rows in zip((dq, dk, dv), got[2:] if got else ()):
+            put(to, rows)
+
+    def rotary(x, positions, frequencies, out, x2=None, out2=None, interleaved=False, magnitude=1.0, inverse=False):
+        for t, to in ((x, out), (x2, out2)):
+            put(to, ol.rotate(of(t), positions.numpy(), of(frequencies), interleaved, magnitude, inverse))
+
+    def dropout(x, bias, residual, rng, p, out):
+        calls.append(("dropout", tuple(rng.tolist())))
+        put(out, ol.dropout(of(x), of(bias), of(residual), *rng.tolist(), p))
+
+    def dropout_gradients(dout, rng, p, dx, dbias, workspace):
+        calls.append(("dropout gradients", tuple(rng.tolist())))
+        for to, rows in zip((dx, dbias), ol.dropout_gradients(of(dout), *rng.tolist(), p)):
+            if to is not None:
+                put(to, rows)
+
+    for name, f in (("attention_forward", forward), ("attention_backward", backward), ("rotary", rotary), ("dropout_forward", dropout),
+                    ("dropout_backward", dropout_gradients)):
+        monkeypatch.setattr(ps, "ps_" + name, f)
+    real = torch.empty
+
+    def empty(*a, **k):
+        t = real(*a, **k)
+        return t.fill_(float("nan")) if t.is_floating_point() else t
+
+    monkeypatch.setattr(torch, "empty", empty)
+    return calls
+
+
+def drawn(*shapes, dtype=torch.float32, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.randn(s, generator=g).to(dtype).requires_grad_() for s in shapes]
+
+
+def offsets(*at):
+    return torch.tensor(at, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_of_no_sequence_are_zeros(stand_ins, dtype):
+    """And what follows on them stays finite: their gradient is zero, but zero times NaN is not."""
+    q, k, v = drawn((10, 2, 16), (10, 2, 16), (10, 2, 16), dtype=dtype)
+    (w,) = drawn((32, 8), dtype=dtype, seed=1)
+    out = layers.attention(q, k, v, layers.Sequences(offsets(2, 6), offsets(0, 4), 4, 4))
+    assert torch.all(out[:2] == 0) and torch.all(out[6:] == 0) and torch.all(out[2:6] != 0)
+    (out.reshape(10, 32) @ w)[2:6].sum().backward()
+    assert all(torch.isfinite(t.grad).all() for t in (q, k, v, w))
