@@ -23,9 +23,10 @@ class Sequences:
     prefix: Optional[torch.Tensor] = None
     q_docs: Optional[torch.Tensor] = None
     k_docs: Optional[torch.Tensor] = None
+    status: Optional[torch.Tensor] = None      # raised by faulty sequences, in both directions (``binding.new_status``, ``ps_status_read``)
 
     def arguments(self) -> dict:
-        return {n: getattr(self, n) for n in ("k_lengths", "q_start", "prefix", "q_docs", "k_docs")}
+        return {n: getattr(self, n) for n in ("k_lengths", "q_start", "prefix", "q_docs", "k_docs", "status")}
 
 
 class _Attention(torch.autograd.Function):
@@ -57,7 +58,7 @@ class _Attention(torch.autograd.Function):
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: Sequences, scale: Optional[float] = None, softcap: float = 0.0,
               causal: bool = False, slopes: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of packed q [n_q, heads, size] to k, v [n_k, kv_heads, size]; slopes are constants.  Rows that no sequence has, or a
-    faulty one, are zeros, as is their gradient."""
+    faulty one, are zeros, as is their gradient; faulty sequences are told in ``seqs.status``."""
     return _Attention.apply(q, k, v, seqs, scale, softcap, causal, slopes)
 
 

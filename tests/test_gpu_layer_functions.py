@@ -37,3 +37,15 @@ def test_rows_of_no_sequence_are_zeros(dtype):
     assert torch.all(out[:2] == 0) and torch.all(out[6:] == 0) and torch.all(out[2:6] != 0)
     (out.reshape(10, 32) @ w)[2:6].sum().backward()
     assert all(torch.isfinite(t.grad).all() for t in (q, k, v, w))
+
+
+def test_faulty_sequences_are_told():
+    q, k, v = drawn((10, 2, 16), (10, 2, 16), (10, 2, 16))
+    status = ps.new_status(DEV)
+    leave_nan(q.shape, dtype=torch.float32)
+    out = layers.attention(q, k, v, layers.Sequences(offsets(0, 4, 10), offsets(0, 4, 10), 5, 5, status=status))
+    assert ps.ps_status_read(status) == (ps.PS_ST_BAD_LENGTH, 1) and torch.all(out[4:] == 0) and torch.all(out[:4] != 0)
+    status.zero_()
+    out.sum().backward()
+    assert ps.ps_status_read(status)[0] == ps.PS_ST_BAD_LENGTH
+    assert all(torch.all(t.grad[4:] == 0) for t in (q, k, v))

@@ -110,3 +110,13 @@ def test_rows_of_no_sequence_are_zeros(stand_ins, dtype):
     assert torch.all(out[:2] == 0) and torch.all(out[6:] == 0) and torch.all(out[2:6] != 0)
     (out.reshape(10, 32) @ w)[2:6].sum().backward()
     assert all(torch.isfinite(t.grad).all() for t in (q, k, v, w))
+
+
+def test_faulty_sequences_are_told(stand_ins):
+    q, k, v = drawn((10, 2, 16), (10, 2, 16), (10, 2, 16))
+    status = torch.zeros(2, dtype=torch.int64)
+    out = layers.attention(q, k, v, layers.Sequences(offsets(0, 4, 10), offsets(0, 4, 10), 5, 5, status=status))
+    assert status[0] == ps.PS_ST_BAD_LENGTH and torch.all(out[4:] == 0) and torch.all(out[:4] != 0)
+    out.sum().backward()
+    assert [s is status for _, s in stand_ins] == [True, True]
+    assert all(torch.all(t.grad[4:] == 0) for t in (q, k, v))
