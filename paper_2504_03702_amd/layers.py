@@ -90,26 +90,35 @@ class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, bias, residual, rng, p):
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        drawn = rng.clone()                                     # what this call draws from: `rng` moves on
-        rng[1:].add_(1)
-        ps.ps_dropout_forward(x, bias, residual, drawn, p, out)
-        ctx.save_for_backward(drawn)
+        ps.ps_dropout_forward(x, bias, residual, rng, p, out)
+        ctx.save_for_backward(rng)
         ctx.p, ctx.bias = p, None if bias is None else bias.dtype
         return out
 
     @staticmethod
     def backward(ctx, dout):
-        (drawn,) = ctx.saved_tensors
+        (rng,) = ctx.saved_tensors
         dout = dout.contiguous()
         dx = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
         dbias = ws = None
         if ctx.bias is not None and ctx.needs_input_grad[1]:
             dbias = torch.empty(dout.shape[1], device=dout.device)
             ws = ps.alloc_workspace(ps.ps_dropout_workspace_bytes(*dout.shape), dout.device)
-        ps.ps_dropout_backward(dout, drawn, ctx.p, dx, dbias, ws)
+        ps.ps_dropout_backward(dout, rng, ctx.p, dx, dbias, ws)
         return dx, None if dbias is None else dbias.to(ctx.bias), dout if ctx.needs_input_grad[2] else None, None, None
 
 
-def dropout_add(x: torch.Tensor, bias: Optional[torch.Tensor], residual: Optional[torch.Tensor], rng: torch.Tensor, p: float) -> torch.Tensor:
-    """residual + dropout(x + bias) of [rows, cols]; rng: two int64 on the GPU, seed and number of the call, which moves on by one."""
-    return _Dropout.apply(x, bias, residual, rng, p)
+def dropout_add(x: torch.Tensor, bias: Optional[torch.Tensor], residual: Optional[torch.Tensor], rng: torch.Tensor, p: float,
+                move_on: bool = True) -> torch.Tensor:
+    """residual + dropout(x + bias) of [rows, cols]; rng: two int64 on the GPU, seed and number of the call, which moves on by one.
+
+    With ``move_on=False`` rng stays as it is, and has to until the gradients are taken.  A pass that is made again for its gradients
+    (activation checkpointing) needs that, since it has to draw what it drew the first time: calls in it get tensors of their own
+    (``rng + rng.new_tensor([0, n])``), and the caller goes on to others.  A call that would move on in such a pass is refused."""
+    if not move_on:
+        return _Dropout.apply(x, bias, residual, rng, p)
+    if torch._C._current_graph_task_id() != -1:                 # (gradients are being taken)
+        raise RuntimeError("dropout_add: a pass that is made again for its gradients would draw another mask; call it with move_on=False")
+    drawn = rng.clone()                                         # what this call draws from
+    rng[1:].add_(1)
+    return _Dropout.apply(x, bias, residual, drawn, p)

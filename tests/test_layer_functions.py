@@ -3,6 +3,7 @@ for the kernels, on the CPU, and write what those write: rows of sequences that 
 import numpy as np
 import pytest
 import torch
+from torch.utils.checkpoint import checkpoint
 
 from oracle import layer as ol
 from paper_2504_03702_amd import binding as ps
@@ -86,7 +87,7 @@ def stand_ins(monkeypatch):
 
     def empty(*a, **k):
         t = real(*a, **k)
-        return t.fill_(float("nan")) if t.is_floating_point() else t
+        return t.fill_(float("nan")) if t.is_floating_point() and not t.requires_grad else t
 
     monkeypatch.setattr(torch, "empty", empty)
     return calls
@@ -95,6 +96,14 @@ def stand_ins(monkeypatch):
 def drawn(*shapes, dtype=torch.float32, seed=0):
     g = torch.Generator().manual_seed(seed)
     return [torch.randn(s, generator=g).to(dtype).requires_grad_() for s in shapes]
+
+
+def gradients_of(out, inputs, g):
+    """By backward(): a region that is made again the older way takes no other."""
+    for t in inputs:
+        t.grad = None
+    out.backward(g)
+    return [t.grad for t in inputs]
 
 
 def offsets(*at):
@@ -120,3 +129,43 @@ def test_faulty_sequences_are_told(stand_ins):
     out.sum().backward()
     assert [s is status for _, s in stand_ins] == [True, True]
     assert all(torch.all(t.grad[4:] == 0) for t in (q, k, v))
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_recomputed_passes_draw_the_same_masks(stand_ins, reentrant):
+    """Two masks in a region whose activations are made again: the gradients are those of the pass that was kept, bit for bit."""
+    (x, b), g = drawn((40, 24), (24,)), torch.randn(40, 24)
+
+    def region(x, b, rng):
+        y = layers.dropout_add(x, b, x, rng, 0.5, move_on=False)
+        return layers.dropout_add(y * y, None, y, rng + rng.new_tensor([0, 1]), 0.5, move_on=False)
+
+    grads = []
+    for again in (False, True):
+        rng = torch.tensor([3, 7])
+        out = checkpoint(region, x, b, rng, use_reentrant=reentrant) if again else region(x, b, rng)
+        grads.append((out, *gradients_of(out, (x, b), g)))
+        assert rng.tolist() == [3, 7]
+    assert all(torch.equal(a, c) for a, c in zip(*grads))
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_recomputed_passes_do_not_move_on(stand_ins, reentrant):
+    (x,), rng = drawn((40, 24)), torch.tensor([3, 7])
+    out = checkpoint(lambda x: layers.dropout_add(x, None, None, rng, 0.5), x, use_reentrant=reentrant)
+    assert rng.tolist() == [3, 8]
+    with pytest.raises(RuntimeError, match="move_on=False"):
+        out.sum().backward()
+    assert rng.tolist() == [3, 8]
+
+
+def test_masks_stay_until_the_gradients_are_taken(stand_ins):
+    (x,), rng = drawn((40, 24)), torch.tensor([3, 7])
+    kept = layers.dropout_add(x, None, None, rng, 0.5)
+    rng[1:].add_(1)
+    kept.sum().backward()                                      # (of a number of its own)
+    assert torch.equal(x.grad, torch.tensor(ol.dropout_gradients(np.ones((40, 24)), 3, 7, 0.5)[0]).to(x.grad))
+    kept = layers.dropout_add(x, None, None, rng, 0.5, move_on=False)
+    rng[1:].add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        kept.sum().backward()
