@@ -4,6 +4,7 @@ library's kernels; there is no fallback.  A program that owns its buffers calls 
 from __future__ import annotations
 
 import dataclasses
+import functools
 from typing import Optional, Tuple
 
 import torch
@@ -29,6 +30,29 @@ class Sequences:
         return {n: getattr(self, n) for n in ("k_lengths", "q_start", "prefix", "q_docs", "k_docs", "status")}
 
 
+class _NoSecond(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, grad):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("the layer functions have no second derivatives")
+
+
+def _first_only(backward):
+    """A backward pass whose gradients, where a graph of them is asked for (``create_graph=True``), raise an error when differentiated.
+    (torch's ``once_differentiable`` does so only if the incoming gradient has a graph of its own, and a sum's has none.)"""
+    @functools.wraps(backward)
+    def run(ctx, *grads):
+        with torch.no_grad():
+            got = backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return got
+        return tuple(None if g is None else _NoSecond.apply(g.detach().requires_grad_()) for g in got)
+    return run
+
+
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, seqs, scale, softcap, causal, slopes):
@@ -45,6 +69,7 @@ class _Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @_first_only
     def backward(ctx, dout):
         q, k, v, out, lse, rest = ctx.saved_tensors
         # (rows that no sequence has get no gradient)
@@ -72,6 +97,7 @@ class _Rotary(torch.autograd.Function):
         return tuple(out)
 
     @staticmethod
+    @_first_only
     def backward(ctx, dq, dk):
         positions, frequencies = ctx.saved_tensors
         dq, dk = (t if t.stride(-1) == 1 else t.contiguous() for t in (dq, dk))
@@ -96,6 +122,7 @@ class _Dropout(torch.autograd.Function):
         return out
 
     @staticmethod
+    @_first_only
     def backward(ctx, dout):
         (rng,) = ctx.saved_tensors
         dout = dout.contiguous()

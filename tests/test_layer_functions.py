@@ -169,3 +169,23 @@ def test_masks_stay_until_the_gradients_are_taken(stand_ins):
     rng[1:].add_(1)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         kept.sum().backward()
+
+
+@pytest.mark.parametrize("what", ["attention", "rotary", "dropout"])
+@pytest.mark.parametrize("weight", [False, True])
+def test_second_derivatives_are_refused(stand_ins, what, weight):
+    """Gradients with a graph can be had, and are right; to differentiate them is an error, not nothing."""
+    q, k, v = drawn((4, 2, 16), (4, 2, 16), (4, 2, 16))
+    (w,) = drawn((4, 2, 16), seed=1)
+    if what == "attention":
+        out = layers.attention(q, k, v, layers.Sequences(offsets(0, 4), offsets(0, 4), 4, 4))
+    elif what == "rotary":
+        out = sum(layers.rotary(q, k, offsets(0, 1, 2, 3), torch.ones(8)))
+    else:
+        out = layers.dropout_add(q.view(8, 16), None, None, torch.tensor([1, 1]), 0.1).view(4, 2, 16)
+    loss = (out * w).sum() if weight else out.sum()
+    (plain,) = torch.autograd.grad(loss, q, retain_graph=True)
+    (again,) = torch.autograd.grad(loss, q, create_graph=True)
+    assert torch.equal(plain, again)
+    with pytest.raises(RuntimeError, match="no second derivatives"):
+        (loss + again.square().sum()).backward()
