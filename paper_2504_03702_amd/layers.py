@@ -62,21 +62,23 @@ class _Attention(torch.autograd.Function):
         rest = torch.empty_like(out) if train and q.dtype == torch.bfloat16 else None
         shape = (seqs.q_offsets.numel() - 1, q.shape[0], k.shape[0], seqs.max_q, seqs.max_k, q.shape[1], k.shape[1], q.shape[2], q.dtype)
         ws = ps.alloc_workspace(ps.ps_attention_workspace_bytes(*shape), q.device)
-        ctx.how = dict(scale=scale, softcap=softcap, causal=causal, slopes=slopes, **seqs.arguments())
-        ps.ps_attention_forward(q, k, v, seqs.q_offsets, seqs.k_offsets, seqs.max_q, seqs.max_k, out, lse, ws, out_rest=rest, **ctx.how)
-        ctx.save_for_backward(q, k, v, out, lse, rest)
-        ctx.seqs, ctx.shape = seqs, shape
+        masks = dict(seqs.arguments(), slopes=slopes)
+        ctx.how = dict(scale=scale, softcap=softcap, causal=causal, status=masks.pop("status"))
+        ctx.bounds, ctx.shape, ctx.masks = (seqs.max_q, seqs.max_k), shape, tuple(masks)
+        ps.ps_attention_forward(q, k, v, seqs.q_offsets, seqs.k_offsets, *ctx.bounds, out, lse, ws, out_rest=rest, **masks, **ctx.how)
+        # (all that the gradients depend on, so that what is written again in between does not go unnoticed)
+        ctx.save_for_backward(q, k, v, out, lse, rest, seqs.q_offsets, seqs.k_offsets, *masks.values())
         return out
 
     @staticmethod
     @_first_only
     def backward(ctx, dout):
-        q, k, v, out, lse, rest = ctx.saved_tensors
+        q, k, v, out, lse, rest, q_offsets, k_offsets, *masks = ctx.saved_tensors
         # (rows that no sequence has get no gradient)
         grads = [torch.zeros(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v)]
         ws = ps.alloc_workspace(ps.ps_attention_workspace_bytes(*ctx.shape, backward=True), q.device)
-        ps.ps_attention_backward(q, k, v, out, lse, dout.contiguous(), ctx.seqs.q_offsets, ctx.seqs.k_offsets, ctx.seqs.max_q, ctx.seqs.max_k,
-                                 *grads, ws, out_rest=rest, **ctx.how)
+        ps.ps_attention_backward(q, k, v, out, lse, dout.contiguous(), q_offsets, k_offsets, *ctx.bounds, *grads, ws, out_rest=rest,
+                                 **dict(zip(ctx.masks, masks)), **ctx.how)
         return (*grads, None, None, None, None, None)
 
 

@@ -189,3 +189,18 @@ def test_second_derivatives_are_refused(stand_ins, what, weight):
     assert torch.equal(plain, again)
     with pytest.raises(RuntimeError, match="no second derivatives"):
         (loss + again.square().sum()).backward()
+
+
+@pytest.mark.parametrize("name", ["q_offsets", "k_offsets", "k_lengths", "q_start", "prefix", "q_docs", "k_docs", "slopes"])
+def test_what_gradients_depend_on_may_not_be_written_again(stand_ins, name):
+    q, k, v = drawn((4, 2, 16), (4, 2, 16), (4, 2, 16))
+    more = dict(k_lengths=offsets(3), q_start=offsets(0), prefix=offsets(1), q_docs=offsets(0, 0, 1, 1), k_docs=offsets(0, 0, 1, 1))
+    seqs, slopes = layers.Sequences(offsets(0, 4), offsets(0, 4), 4, 4, **more), torch.ones(2)
+    for change in (False, True):
+        out = layers.attention(q, k, v, seqs, causal=True, slopes=slopes)
+        if not change:
+            out.sum().backward()
+            continue
+        (slopes if name == "slopes" else getattr(seqs, name)).add_(1)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            out.sum().backward()
