@@ -30,6 +30,11 @@ class Sequences:
         return {n: getattr(self, n) for n in ("k_lengths", "q_start", "prefix", "q_docs", "k_docs", "status")}
 
 
+def _constant(t: Optional[torch.Tensor], where: str, name: str) -> None:
+    if t is not None and t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{where}: {name} have no gradient; detach them")
+
+
 class _NoSecond(torch.autograd.Function):
     @staticmethod
     def forward(ctx, grad):
@@ -86,6 +91,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: Sequences
               causal: bool = False, slopes: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of packed q [n_q, heads, size] to k, v [n_k, kv_heads, size]; slopes are constants.  Rows that no sequence has, or a
     faulty one, are zeros, as is their gradient; faulty sequences are told in ``seqs.status``."""
+    _constant(slopes, "attention", "slopes")
     return _Attention.apply(q, k, v, seqs, scale, softcap, causal, slopes)
 
 
@@ -110,7 +116,8 @@ class _Rotary(torch.autograd.Function):
 
 def rotary(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, frequencies: torch.Tensor, interleaved: bool = False,
            magnitude: float = 1.0) -> Tuple[torch.Tensor, torch.Tensor]:
-    """Queries and keys turned to their positions."""
+    """Queries and keys turned to their positions; frequencies are constants."""
+    _constant(frequencies, "rotary", "frequencies")
     return _Rotary.apply(q, k, positions, frequencies, interleaved, magnitude)
 
 

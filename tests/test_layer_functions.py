@@ -204,3 +204,16 @@ def test_what_gradients_depend_on_may_not_be_written_again(stand_ins, name):
         (slopes if name == "slopes" else getattr(seqs, name)).add_(1)
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             out.sum().backward()
+
+
+def test_constants_that_want_a_gradient_are_refused(stand_ins):
+    q, k, v, slopes, f = drawn((4, 2, 16), (4, 2, 16), (4, 2, 16), (2,), (8,))
+    seqs = layers.Sequences(offsets(0, 4), offsets(0, 4), 4, 4)
+    with pytest.raises(ValueError, match="slopes"):
+        layers.attention(q, k, v, seqs, slopes=slopes)
+    with pytest.raises(ValueError, match="frequencies"):
+        layers.rotary(q, k, offsets(0, 1, 2, 3), f)
+    layers.attention(q, k, v, seqs, slopes=slopes.detach())
+    with torch.no_grad():
+        layers.attention(q, k, v, seqs, slopes=slopes)
+        layers.rotary(q, k, offsets(0, 1, 2, 3), f)
