@@ -79,10 +79,13 @@ class _Attention(torch.autograd.Function):
     @_first_only
     def backward(ctx, dout):
         q, k, v, out, lse, rest, q_offsets, k_offsets, *masks = ctx.saved_tensors
+        dout = dout.contiguous()
+        if dout.data_ptr() % 16:                                # (part of a larger gradient, as torch.cat hands them back)
+            dout = dout.clone()
         # (rows that no sequence has get no gradient)
         grads = [torch.zeros(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v)]
         ws = ps.alloc_workspace(ps.ps_attention_workspace_bytes(*ctx.shape, backward=True), q.device)
-        ps.ps_attention_backward(q, k, v, out, lse, dout.contiguous(), q_offsets, k_offsets, *ctx.bounds, *grads, ws, out_rest=rest,
+        ps.ps_attention_backward(q, k, v, out, lse, dout, q_offsets, k_offsets, *ctx.bounds, *grads, ws, out_rest=rest,
                                  **dict(zip(ctx.masks, masks)), **ctx.how)
         return (*grads, None, None, None, None, None)
 

@@ -217,3 +217,12 @@ def test_constants_that_want_a_gradient_are_refused(stand_ins):
     with torch.no_grad():
         layers.attention(q, k, v, seqs, slopes=slopes)
         layers.rotary(q, k, offsets(0, 1, 2, 3), f)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_incoming_gradients_lie_at_any_address(stand_ins, dtype):
+    (q, k, v, first), seqs = drawn((4, 2, 16), (4, 2, 16), (4, 2, 16), (1,), dtype=dtype), layers.Sequences(offsets(0, 4), offsets(0, 4), 4, 4)
+    (w,) = drawn((129,), dtype=dtype, seed=1)
+    want = torch.autograd.grad((layers.attention(q, k, v, seqs).reshape(-1) * w[1:]).sum(), (q, k, v))
+    got = torch.autograd.grad((torch.cat((first, layers.attention(q, k, v, seqs).reshape(-1))) * w).sum(), (q, k, v))
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
