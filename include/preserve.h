@@ -291,7 +291,8 @@ typedef struct ps_strides { int64_t row, head; } ps_strides;
  *   heads       multiple of kv_heads; head h reads key head h / (heads / kv_heads)
  *   head_dim    a multiple of 8, at most 128
  *   max_q, max_k  host's bounds on the sequences' rows and keys: a longer sequence is faulty (below)
- *   scale > 0;  softcap >= 0;  causal 0 or 1
+ *   scale > 0;  softcap >= 0, of any size (2^100 and more: no cap; above 256 bf16 calls take longer, for a tanh that keeps its places);
+ *   causal 0 or 1
  *   q .. dv     strides of the tensors a call uses: [n_q][heads] of q, out, dout, dq, [n_k][kv_heads] of k, v, dk, dv */
 typedef struct ps_attention_desc {
     int32_t dtype, n_seq, heads, kv_heads, head_dim, max_q, max_k, causal;

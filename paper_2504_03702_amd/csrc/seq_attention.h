@@ -10,6 +10,8 @@
 // product (A = the tile's transpose) as they stand: the order of the contracted rows is free, so it is the accumulator's.
 #pragma once
 
+#include <type_traits>
+
 #include "device_util.h"
 #include "internal.h"
 
@@ -505,26 +507,36 @@ struct Walk {
 };
 
 // ---- scores ------------------------------------------------------------------------------------------------------------------
-// The cap.  bf16 calls take tanh u = 1 - 2 r, r = 1 / (1 + e^2u), whose absolute error of 1e-7 is that of a score near the cap; r is
-// what they go on with.  fp32 calls take the library's, good to the last places everywhere.
+// The cap.  bf16 calls take tanh u = 1 - 2 r, r = 1 / (1 + e^2u), whose absolute error of 1.4e-7 is that of a score near the cap; r is
+// what they go on with.  Times a cap of up to NEAR that is 4e-5 of a score and less, a fiftieth of the rounding of its weight; above (FAR) it would
+// be more, and 0.14 at 1e6.  There it is tanh itself, with its error relative: the series in front of a quarter, up to u^9 (1e-8 there), 1 - 2 r
+// behind (6e-7).  (16 x 2048 with prefix, forwards / gradients 431 / 2000 us with 1 - 2 r, 546 / 2262 with the series; 8 x 2048 with heads of 64
+// 128 / 459, 191 / 569.)  fp32 calls take the library's, good to the last places everywhere.
 struct Cap {
+    static constexpr float NEAR = 256.f;
     float inner, outer;                // what the product is multiplied by on the way in, and tanh on the way out (powers of two)
     template <typename T>
     static __device__ __forceinline__ Cap of(const Args& a) {
         return {a.cap_in * (sizeof(T) == 4 ? 1.f : 2.f * LOG2E), a.cap * LOG2E};
     }
     template <typename T>
+    static __device__ __forceinline__ bool far(const Args& a) { return sizeof(T) == 2 && a.cap > NEAR; }
+    template <typename T, bool FAR>
     __device__ __forceinline__ float bent(float s) const {                // r, or tanh
         if constexpr (sizeof(T) == 4) return tanhf(s * inner);
-        return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * inner));
+        const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * inner));
+        if (!FAR) return r;
+        const float u = s * inner * (0.5f * LN2), x = u * u;
+        const float series = fmaf(u * x, fmaf(x, fmaf(x, fmaf(x, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), u);
+        return fabsf(u) < 0.25f ? series : fmaf(-2.f, r, 1.f);
     }
-    template <typename T>
+    template <typename T, bool FAR>
     __device__ __forceinline__ float score(float b, float less) const {   // in powers of two, less something
-        return sizeof(T) == 4 ? fmaf(b, outer, -less) : fmaf(b, -2.f * outer, outer - less);
+        return sizeof(T) == 4 || FAR ? fmaf(b, outer, -less) : fmaf(b, -2.f * outer, outer - less);
     }
-    template <typename T>
+    template <typename T, bool FAR>
     static __device__ __forceinline__ float slope(float b) {              // 1 - tanh^2, in bf16 a quarter of it
-        return sizeof(T) == 4 ? fmaf(-b, b, 1.f) : fmaf(-b, b, b);
+        return sizeof(T) == 4 ? fmaf(-b, b, 1.f) : FAR ? fmaf(-0.25f * b, b, 0.25f) : fmaf(-b, b, b);
     }
 };
 

@@ -37,13 +37,19 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
             }
         }
         if (a.cap > 0.f) {
+            auto bend = [&](auto far) {
 #pragma unroll
-            for (int e = 0; e < 4 * STEP; ++e) {
-                const float b = cap.bent<T>(s[4 * j0 + e]);
-                float& w = (&u[e >> 2].x)[e & 3];
-                w = __builtin_amdgcn_exp2f(cap.score<T>(b, w));
-                (&v[e >> 2].x)[e & 3] = Cap::slope<T>(b) * w;
-            }
+                for (int e = 0; e < 4 * STEP; ++e) {
+                    const float b = cap.bent<T, far>(s[4 * j0 + e]);
+                    float& w = (&u[e >> 2].x)[e & 3];
+                    w = __builtin_amdgcn_exp2f(cap.score<T, far>(b, w));
+                    (&v[e >> 2].x)[e & 3] = Cap::slope<T, far>(b) * w;
+                }
+            };
+            if (Cap::far<T>(a))
+                bend(std::true_type());
+            else
+                bend(std::false_type());
         } else {
 #pragma unroll
             for (int e = 0; e < 4 * STEP; ++e) {

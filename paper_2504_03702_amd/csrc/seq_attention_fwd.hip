@@ -52,13 +52,19 @@ struct Row {
             else
                 sc[b] = dot<T, DP>(keys, b, qf, lanes);
         }
-        const Cap cap = Cap::of<T>(a);
         float c = a.scale * LOG2E;
         if (a.cap > 0.f) {
+            const Cap cap = Cap::of<T>(a);
+            auto bend = [&](auto far) {
 #pragma unroll
-            for (int b = 0; b < L::BLOCKS; ++b)
+                for (int b = 0; b < L::BLOCKS; ++b)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sc[b][e] = cap.score<T>(cap.bent<T>(sc[b][e]), 0.f);
+                    for (int e = 0; e < 16; ++e) sc[b][e] = cap.score<T, far>(cap.bent<T, far>(sc[b][e]), 0.f);
+            };
+            if (Cap::far<T>(a))
+                bend(std::true_type());
+            else
+                bend(std::false_type());
             c = 1.f;
         }
         if (a.slopes) {
@@ -582,9 +588,10 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
     a.qs = d->q; a.ks = d->k; a.vs = d->v; a.os = d->out; a.gs = d->dout; a.dqs = d->dq; a.dks = d->dk; a.dvs = d->dv;
     a.n_q = d->n_q; a.n_k = d->n_k; a.n_seq = d->n_seq; a.heads = d->heads; a.kv_heads = d->kv_heads; a.head_dim = d->head_dim;
     a.group = (int32_t)group; a.max_q = (int32_t)min((int64_t)d->max_q, d->n_q); a.max_k = (int32_t)min((int64_t)d->max_k, d->n_k); a.causal = d->causal;
-    a.scale = d->scale; a.cap = d->softcap;
-    a.slope_by = d->softcap > 0.f ? LOG2E : 1.f / d->scale;
-    a.cap_in = d->softcap > 0.f ? d->scale / d->softcap : 0.f;
+    a.scale = d->scale;
+    a.cap = d->softcap < 0x1p100f ? d->softcap : 0.f;                     // (above, it bends no score by a place, and cap log2(e) is no float)
+    a.slope_by = a.cap > 0.f ? LOG2E : 1.f / d->scale;
+    a.cap_in = a.cap > 0.f ? d->scale / a.cap : 0.f;
     a.by_group = group > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint64_t)group + 1) : 0;
     a.row_blocks = (int32_t)(((int64_t)a.max_q * group + FIXED - 1) / FIXED);
     // Blocks that do not fill the chip, or of which the longest would be waited for: their tiles are shared out, so that there are
