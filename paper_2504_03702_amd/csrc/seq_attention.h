@@ -611,6 +611,7 @@ struct Plan {
 };
 int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, void* workspace, Plan& p);
 int check_strides(const ps_attention_desc* d, const ps_strides& s, const void* base, int64_t rows, int64_t heads, bool written);
+int check_sequences(const Args& a, hipStream_t st);
 void summarise_documents(const Args& a, hipStream_t st);
 bool add_up(int32_t seqs, int64_t blocks, int32_t parts);
 

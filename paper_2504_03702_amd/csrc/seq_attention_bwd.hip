@@ -524,7 +524,8 @@ extern "C" int ps_attention_backward(const ps_attention_desc* desc, const ps_att
     if (!seqs) return PS_EINVAL;
     const int code = plan(desc, seqs, true, workspace, p);
     if (code != PS_OK) return code;
-    if (p.a.n_seq == 0 || (p.a.n_q == 0 && p.a.n_k == 0)) return PS_OK;
+    p.a.status = status;
+    if (p.a.n_seq == 0 || (p.a.n_q == 0 && p.a.n_k == 0)) return check_sequences(p.a, (hipStream_t)hip_stream);
     const ps_attention_desc* d = desc;
     if (p.a.n_q > 0 && (check_strides(d, d->q, q, d->n_q, d->heads, false) || check_strides(d, d->out, out, d->n_q, d->heads, false) || !lse ||
                         check_strides(d, d->dout, dout, d->n_q, d->heads, false) || check_strides(d, d->dq, dq, d->n_q, d->heads, true)))
@@ -535,8 +536,9 @@ extern "C" int ps_attention_backward(const ps_attention_desc* desc, const ps_att
     if (((uintptr_t)out_rest & 15) != 0 || (out_rest && d->dtype != 1) || (uintptr_t)lse % 4 != 0) return PS_EINVAL;
     if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < p.bytes) return PS_EWORKSPACE;
     Args& a = p.a;
-    a.q = q; a.k = k; a.v = v; a.out = out; a.lse = lse; a.rest = out_rest; a.dout = dout; a.dq = dq; a.dk = dk; a.dv = dv; a.status = status;
+    a.q = q; a.k = k; a.v = v; a.out = out; a.lse = lse; a.rest = out_rest; a.dout = dout; a.dq = dq; a.dk = dk; a.dv = dv;
     hipStream_t st = (hipStream_t)hip_stream;
+    if (a.max_q == 0 && check_sequences(a, st) != PS_OK) return PS_EHIP;   // (else the queries' launch finds them)
     (void)hipGetLastError();
     summarise_documents(a, st);
     switch (padded(desc->head_dim)) {

@@ -514,6 +514,13 @@ __global__ __launch_bounds__(256) void documents_kernel(Args a) {
     if (lane == 0) (queries ? a.q_blocks : a.k_blocks)[doc_block0(first, s) + b] = make_int2(lo, hi);
 }
 
+// Where no sequence may have rows, and no launch over rows finds the faulty ones.
+__global__ __launch_bounds__(256) void check_kernel(Args a) {
+    const int s = (int)(blockIdx.x * 256 + threadIdx.x);
+    Seq q;
+    if (s < a.n_seq && !sequence(a, s, q)) report_fault(a.status, PS_ST_BAD_LENGTH, s);
+}
+
 template <typename T, int DP>
 void launch_attend(const Args& a, hipStream_t st) {
     const int64_t per_seq = (int64_t)a.kv_heads * a.row_blocks * a.parts;
@@ -679,6 +686,13 @@ void summarise_documents(const Args& a, hipStream_t st) {
     }
 }
 
+int check_sequences(const Args& a, hipStream_t st) {
+    if (!a.status || a.n_seq == 0) return PS_OK;
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(check_kernel, dim3(((unsigned)a.n_seq + 255) / 256), dim3(256), 0, st, a);
+    return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
+}
+
 }  // namespace seqatt
 
 extern "C" size_t ps_attention_workspace_bytes(const ps_attention_desc* desc, int backward) {
@@ -694,7 +708,8 @@ extern "C" int ps_attention_forward(const ps_attention_desc* desc, const ps_atte
     if (!seqs) return PS_EINVAL;
     const int code = plan(desc, seqs, false, workspace, p);
     if (code != PS_OK) return code;
-    if (p.a.n_seq == 0 || p.a.n_q == 0 || p.a.max_q == 0) return PS_OK;
+    p.a.status = status;
+    if (p.a.n_seq == 0 || p.a.max_q == 0) return check_sequences(p.a, (hipStream_t)hip_stream);
     if (check_strides(desc, desc->q, q, desc->n_q, desc->heads, false) ||
         check_strides(desc, desc->out, out, desc->n_q, desc->heads, true)) return PS_EINVAL;
     if (p.a.n_k > 0 && (check_strides(desc, desc->k, k, desc->n_k, desc->kv_heads, false) ||
@@ -703,7 +718,7 @@ extern "C" int ps_attention_forward(const ps_attention_desc* desc, const ps_atte
     if (((uintptr_t)out_rest & 15) != 0 || (out_rest && desc->dtype != 1) || (uintptr_t)lse % 4 != 0) return PS_EINVAL;
     if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < p.bytes) return PS_EWORKSPACE;
     Args& a = p.a;
-    a.q = q; a.k = k; a.v = v; a.out_w = out; a.lse_w = lse; a.rest_w = out_rest; a.status = status;
+    a.q = q; a.k = k; a.v = v; a.out_w = out; a.lse_w = lse; a.rest_w = out_rest;
     hipStream_t st = (hipStream_t)hip_stream;
     (void)hipGetLastError();
     if (!a.few) summarise_documents(a, st);

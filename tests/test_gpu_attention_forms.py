@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2504_03702_amd import binding as ps
 from tests.test_gpu_attention import Problem, SLOPES
 
 pytestmark = pytest.mark.gpu
@@ -17,3 +18,20 @@ def test_caps_of_any_size(dtype, cap):
     for size in (64, 96, 128):
         Problem(dtype, [100, 1, 70], [100, 1, 70], size=size, causal=True, cap=cap, big=3.0).check()
     Problem(dtype, [1, 2], [900, 40], size=64, causal=True, cap=cap, slopes=SLOPES, big=3.0).check(backward=False)
+
+
+@pytest.mark.parametrize("q_lens,k_lens,rows", [([3, 0, 2], [4, 1, 4], 5), ([0, 1], [2, 0], 0)])
+def test_calls_without_rows_tell_faulty_sequences(q_lens, k_lens, rows):
+    """A bound, or a tensor, of no rows: sequences that have some are faulty, and the others get their gradients."""
+    p = Problem(torch.float32, q_lens, k_lens)
+    p.max_q = 0
+    p.q, p.dout = p.q[:rows], p.dout[:rows]
+    bad = q_lens.index(max(q_lens))
+    out, lse = p.forward()
+    assert torch.all(out == 7.0) and ps.ps_status_read(p.status) == (ps.PS_ST_BAD_LENGTH, bad)
+    p.status.zero_()
+    dq, dk, dv = p.backward(out, lse)
+    assert ps.ps_status_read(p.status) == (ps.PS_ST_BAD_LENGTH, bad) and torch.all(dq == 7.0)
+    left = torch.tensor(np.repeat(np.array(q_lens) > 0, k_lens))
+    for t in (dk, dv):
+        assert torch.all(t[left] == 7.0) and torch.all(t[~left] == 0)
