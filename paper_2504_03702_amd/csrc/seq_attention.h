@@ -80,11 +80,16 @@ __device__ __forceinline__ bool sequence(const Args& a, int s, Seq& r) {
 
 __device__ __forceinline__ unsigned over_group(const Args& a, unsigned r) { return a.group == 1 ? r : __umulhi(r, a.by_group); }
 
+// Keys in front of this one are seen from a place, if their documents are.  (The largest place, 2^30 rows from 2^30 on, has none behind it.)
+__device__ __forceinline__ int seen_end(const Args& a, const Seq& q, int place) {
+    return a.causal ? min(q.kn, max(min(place, q.kn) + 1, q.prefix)) : q.kn;
+}
+
 // Tiles of keys, from the first on, that some of the FIXED rows from r0 on may see; tiles of rows, from `first` on, that may see some of
 // the FIXED keys from k0 on.  Shares are of these.
 __device__ __forceinline__ int key_tiles(const Args& a, const Seq& q, int r0) {
     const int far = q.start + (int)over_group(a, min(r0 + FIXED, q.qn * a.group) - 1);
-    return (max(0, a.causal ? min(q.kn, max(far + 1, q.prefix)) : q.kn) + a.tile - 1) / a.tile;
+    return (max(0, seen_end(a, q, far)) + a.tile - 1) / a.tile;
 }
 __device__ __forceinline__ int row_tiles(const Args& a, const Seq& q, int k0, int& first) {
     const int rows = q.qn * a.group, n = (rows + a.key_tile - 1) / a.key_tile;

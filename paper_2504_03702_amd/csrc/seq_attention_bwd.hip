@@ -340,7 +340,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     }
 
     // keys in front of `end` are seen, if their documents are
-    const int end = a.causal ? min(q.kn, max(place + 1, q.prefix)) : q.kn;
+    const int end = seen_end(a, q, place);
     const int last = min(r0 + FIXED, rows) - 1;
     const int far = q.start + (int)over_group(a, last);
     const int wfar = q.start + (int)over_group(a, min(wr0 + 31, rows - 1)), wnear = q.start + (int)over_group(a, min(wr0, rows - 1));

@@ -33,7 +33,7 @@ struct Row {
         place = q.start + qi;
         slope = a.slopes ? a.slopes[head] * a.slope_by : 0.f;
         doc = a.q_docs ? a.q_docs[token] : 0;
-        end = a.causal ? min(q.kn, max(place + 1, q.prefix)) : q.kn;
+        end = seen_end(a, q, place);
         qf.load((const T*)a.q + token * a.qs.row + head * a.qs.head, live && doc >= 0, a.head_dim, half);
 #pragma unroll
         for (int i = 0; i < L::NA; ++i)

@@ -35,3 +35,17 @@ def test_calls_without_rows_tell_faulty_sequences(q_lens, k_lens, rows):
     left = torch.tensor(np.repeat(np.array(q_lens) > 0, k_lens))
     for t in (dk, dv):
         assert torch.all(t[left] == 7.0) and torch.all(t[~left] == 0)
+
+
+def test_the_largest_place():
+    """2^30 rows from place 2^30 on: the last one stands at 2^31 - 1, and sees the keys like the others."""
+    n = 1 << 30
+    q, out = torch.zeros(n, 1, 8, dtype=torch.bfloat16, device=DEV), torch.zeros(n, 1, 8, dtype=torch.bfloat16, device=DEV)
+    k = torch.ones(3, 1, 8, dtype=torch.bfloat16, device=DEV)
+    nb = ps.ps_attention_workspace_bytes(1, n, 3, n, 3, 1, 1, 8, torch.bfloat16)
+    rows, keys, start = (torch.tensor(v, dtype=torch.int32, device=DEV) for v in ([0, n], [0, 3], [n]))
+    status = ps.new_status(DEV)
+    ps.ps_attention_forward(q, k, k, rows, keys, n, 3, out, None, ps.alloc_workspace(nb, DEV), causal=True, q_start=start, status=status)
+    assert ps.ps_status_read(status) == (0, -1)
+    for some in (out[:1000], out[n // 2:n // 2 + 1000], out[-1000:]):
+        assert torch.all(some == 1.0)
