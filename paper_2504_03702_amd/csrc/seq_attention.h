@@ -548,23 +548,6 @@ struct Cap {
 // Row of accumulator element e.
 __device__ __forceinline__ constexpr int row_of(int e) { return 8 * (e >> 2) + (e & 3); }   // + 4 half
 
-// A lane's accumulators [feature][its row] times `by` to memory, 4 features at a time.
-template <typename T, int DP>
-__device__ __forceinline__ void put_row(T* row, const f32x16 (&acc)[DP / 32], float by, int head_dim, int half) {
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int f = 32 * i + 8 * g + 4 * half;
-            if (f >= head_dim) continue;
-            if constexpr (sizeof(T) == 2)
-                *(uint2*)(row + f) = make_uint2(cvt_pk_bf16(acc[i][4 * g] * by, acc[i][4 * g + 1] * by),
-                                                cvt_pk_bf16(acc[i][4 * g + 2] * by, acc[i][4 * g + 3] * by));
-            else
-                *(float4*)(row + f) = make_float4(acc[i][4 * g] * by, acc[i][4 * g + 1] * by, acc[i][4 * g + 2] * by, acc[i][4 * g + 3] * by);
-        }
-}
-
 // The accumulators of a wavefront, [feature][a lane's row] times the lane's `by`, to its 32 rows in memory: by way of LDS, 64 features at a
 // time, so that 8 or 16 lanes write a row's lines whole (64 sequences of 512 tokens, 12 heads of 64, forwards 125 -> 107 us: from the registers
 // a store has 32 pieces of 16 bytes, of 32 lines, and there are 16 of them).  own: the lane's row in memory, null if there is none.  mine: PUT_BYTES

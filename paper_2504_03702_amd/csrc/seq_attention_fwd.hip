@@ -373,7 +373,12 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
     // the wavefronts' rows put together
     __syncthreads();
     float* sums = (float*)smem;                                           // [wavefront][row][DP]
-    put_row<float, DP>(sums + (wave * 32 + col) * DP, row.o, 1.f, DP, half);
+#pragma unroll
+    for (int i = 0; i < L::NA; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *(float4*)(sums + (wave * 32 + col) * DP + 32 * i + 8 * g + 4 * half) =
+                make_float4(row.o[i][4 * g], row.o[i][4 * g + 1], row.o[i][4 * g + 2], row.o[i][4 * g + 3]);
     if (half == 0) s_ml[wave][col] = make_float2(row.m, row.l);
     __syncthreads();
     const int fours = a.head_dim / 4;
@@ -554,7 +559,7 @@ void launch_attend(const Args& a, hipStream_t st) {
     }
 }
 
-// `align`: what a row's address has to be a multiple of, in elements.
+// Rows and heads at multiples of 16 bytes.
 bool good_strides(const ps_attention_desc* d, const ps_strides& s) {
     const int64_t align = d->dtype == 1 ? 8 : 4;
     return s.row >= 0 && s.head >= 0 && s.row % align == 0 && s.head % align == 0;
