@@ -47,9 +47,9 @@ class Layer(torch.nn.Module):
         return (y if first_rows is not None else y[firsts]).float() @ self.head
 
 
-def draw(rows, generator):
+def draw(rows, generator, status=None):
     """Documents packed into rows of ROW tokens: a log-length is one of four, said by the second token.  Returns what Layer takes, and
-    the log-lengths."""
+    the log-lengths; status: told of faulty sequences."""
     tokens, docs, positions, firsts, lengths, targets = [], [], [], [], [], []
     for r in range(rows):
         at, doc = 0, 0
@@ -73,12 +73,12 @@ def draw(rows, generator):
     i32 = lambda v: (torch.cat(v) if isinstance(v, list) else v).to(DEV, torch.int32)
     offsets = i32(torch.arange(rows + 1) * ROW)
     docs, firsts, lengths = i32(docs), torch.tensor(firsts), torch.tensor(lengths)
-    packed = layers.Sequences(offsets, offsets, ROW, ROW, q_docs=docs, k_docs=docs)
+    packed = layers.Sequences(offsets, offsets, ROW, ROW, q_docs=docs, k_docs=docs, status=status)
     # for scoring: a sequence a document, its one query in front of its keys; documents lie one after the other, padding behind the last of
     # a row, so that a document's keys are a span with room at its end
     n = len(firsts)
     single = layers.Sequences(i32(torch.arange(n + 1)), i32(torch.cat((firsts, torch.tensor([rows * ROW])))), 1, int(lengths.max()),
-                              k_lengths=i32(lengths), q_start=i32(torch.zeros(n)))
+                              k_lengths=i32(lengths), q_start=i32(torch.zeros(n)), status=status)
     return torch.cat(tokens).to(DEV), i32(positions), firsts.to(DEV), packed, single, torch.tensor(targets, device=DEV)
 
 
@@ -88,9 +88,9 @@ def main(steps=60, dtype=torch.bfloat16, rows=8, seed=0):
     layer = Layer(dtype, generator)
     rng = torch.tensor([seed, 0], dtype=torch.int64, device=DEV)
     optimizer = torch.optim.Adam(layer.parameters(), lr=3e-3)
-    losses = []
+    losses, status = [], ps.new_status(DEV)
     for step in range(steps):
-        tokens, positions, firsts, packed, _, targets = draw(rows, generator)
+        tokens, positions, firsts, packed, _, targets = draw(rows, generator, status)
         loss = torch.nn.functional.mse_loss(layer(tokens, positions, firsts, packed, rng, 0.1), targets)
         optimizer.zero_grad()
         loss.backward()
@@ -99,11 +99,13 @@ def main(steps=60, dtype=torch.bfloat16, rows=8, seed=0):
         if step % 10 == 0 or step == steps - 1:
             print(f"step {step}: loss {float(losses[-1]):.4f}", flush=True)
     with torch.no_grad():
-        tokens, positions, firsts, packed, single, targets = draw(rows, generator)
+        tokens, positions, firsts, packed, single, targets = draw(rows, generator, status)
         by_rows = layer(tokens, positions, firsts, packed, rng, 0.0)
         by_firsts = layer(tokens, positions, firsts, packed, rng, 0.0, first_rows=single)
         off = float((by_rows - by_firsts).abs().max())
         print(f"new prompts: loss {float(torch.nn.functional.mse_loss(by_firsts, targets)):.4f}, scored by their first rows alone to {off:.2g}")
+    if ps.ps_status_read(status)[0]:
+        raise RuntimeError(f"faulty sequences: {ps.ps_status_read(status)}")
     return float(losses[0]), float(losses[-1]), off
 
 
