@@ -101,9 +101,9 @@ __device__ __forceinline__ int shares(int tiles, int parts, int part_tiles) { re
 // A workgroup's part of a launch over blocks of rows (of keys, with KEYS) and shares of their tiles.
 // Sequence and block as the grid counts them: `together` sequences take turns, block by block, then the next so many.  Blocks come in order
 // of their work, most first.  In a launch of few blocks all sequences take turns, so that the last to start are short (two rows of 8192
-// tokens, forwards / queries' / keys' gradients: 110 / 177 / 191 us one after the other, 100 / 161 / 182 in turns; 16 x 2048, keys'
-// 1430, 1120); in one of many only as many as fill the chip, so that blocks that run at a time read the same keys from the caches
-// (16 x 2048, forwards / queries': 450 / 680 us two at a time, 520 / 800 eight).
+// tokens, forwards / queries' / keys' gradients: 99 / 159 / 171 us one after the other, 85 / 144 / 160 in turns; 16 x 2048, keys' eight at a
+// time 1035, 977); in one of many only as many as fill the chip, so that blocks that run at a time read the same keys from the caches
+// (16 x 2048, forwards / queries': 390 / 589 us two at a time, 438 / 665 sixteen).
 inline int32_t turns(int64_t blocks_a_seq, int32_t seqs) {
     if (blocks_a_seq * seqs <= 2048) return seqs;
     return (int32_t)(blocks_a_seq >= 512 ? 1 : 512 / blocks_a_seq);

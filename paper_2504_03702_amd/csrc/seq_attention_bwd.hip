@@ -17,8 +17,9 @@ namespace {
 // rest: what the rounding of d to bf16 leaves.  Where a row's weight lies on few keys it does not average out, and what those keys have in
 // common is multiplied by the sum of the roundings instead of the sum of d, which is zero.  So where weights are like that, in blocks that
 // a mask cuts (rows see few keys) and under a cap (scores are large), a second product makes up for it: 16 x 2048 with prefix and cap,
-// queries' / keys' gradients 590 / 1044 -> 680 / 1120 us, error against 64 bits 2.7e-3 -> 2.1e-3 of the norm (1.7e-3 is that of dq's and dk's
-// own rounding; 2.3e-3 without cap, where a product more would cost 5 to 10 %).
+// queries' / keys' gradients 499 / 860 -> 589 / 977 us, error against 64 bits 2.7e-3 -> 2.1e-3 of the norm (1.7e-3 is that of dq's and dk's
+// own rounding; 2.3e-3 without cap, where a product more would cost 5 to 10 %).  (Documents in two rows of 8192, where blocks are cut: 130 / 146
+// -> 144 / 160.)
 template <typename T, int STEP, typename Lse, typename Delta, typename Distance, typename Front, typename Same>
 __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, Weights<T>& p, Weights<T>& d, Weights<T>& rest,
                                           bool cut, bool docs, Lse lse, Delta delta, Distance distance, Front in_front, Same same) {
@@ -98,9 +99,11 @@ template <typename T>
 __device__ __forceinline__ float by_x(const Args& a) { return a.cap > 0.f && sizeof(T) == 2 ? 4.f * a.scale : a.scale; }
 
 // Keys fixed: dk and dv of FIXED keys of a key head, from the rows of all its heads.  Four products a tile (a fifth for the rest), and twice the
-// accumulators of the queries' launch, which leaves two workgroups a unit (one in fp32 above 64 features): 16 x 2048 with prefix and cap, heads
-// of 128, 1.08 to 1.12 ms, 0.42 PFLOP/s, vector units issuing 32 % and matrix units busy 25 % of the time, 36 % of a wavefront's time at
-// barriers and waits; documents in two rows of 8192, heads of 64: 181 us, 0.40 PFLOP/s.
+// accumulators of the queries' launch, which leaves two workgroups a unit (one in fp32 above 64 features).  Bound by waits, as forwards: 16 x 2048
+// with prefix and cap, heads of 128, 978 us, 0.48 PFLOP/s, vector units issuing 31 % and matrix units busy 24 % of the time, 1.3 wavefronts a
+// SIMD at barriers and waits 36 % of theirs; documents in two rows of 8192, heads of 64: 166 us, 0.44 PFLOP/s, 33 %, 22 %, 1.6 wavefronts, 40 %.
+// Where the heads of a key head are no divisor of a tile's rows, addresses are worked out a row at a time, which costs some 15 % (8 causal sequences
+// of 1500 to 2048, 4 key heads of 64, this launch with 2, 3, 4, 5 heads to each: 119, 182, 198, 282 us).
 template <typename T, int DP>
 __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_gradients_kernel(Args a) {
     using L = Tile<T, DP, key_tile_rows(sizeof(T), DP)>;
@@ -289,9 +292,9 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     put_rows<T, DP>(mine, dv, 1.f, a.head_dim, is ? (T*)a.dv + to * a.dvs.row + hk * a.dvs.head : nullptr);
 }
 
-// Queries fixed: dq of FIXED rows of a key head's queries.  Three products a tile (a fourth for the rest): 16 x 2048 with prefix and cap, heads of
-// 128, 680 us, 0.51 PFLOP/s, vector units issuing 47 % and matrix units busy 33 % of the time; documents in two rows of 8192, heads of 64: 160 us,
-// 0.34 PFLOP/s.
+// Queries fixed: dq of FIXED rows of a key head's queries.  Three products a tile (a fourth for the rest).  Bound by waits too: 16 x 2048 with
+// prefix and cap, heads of 128, 586 us, 0.59 PFLOP/s, vector units issuing 48 % and matrix units busy 34 % of the time, 1.7 wavefronts a SIMD
+// waiting 22 % of theirs; documents in two rows of 8192, heads of 64: 147 us, 0.37 PFLOP/s, 33 %, 19 %, 1.5 wavefronts, 40 %.
 template <typename T, int DP>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_gradients_kernel(Args a) {
     using L = Tile<T, DP>;

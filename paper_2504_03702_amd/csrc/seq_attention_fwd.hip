@@ -140,12 +140,13 @@ struct Row {
 
 // A workgroup: FIXED rows of a key head's queries, against a share of the key tiles that any of them sees (one pass, running
 // maximum and sum).  32 rows a wavefront, because a lane then has its row's maximum and sum to itself and its weights where the second product
-// takes them; tiles of 64 keys (32 in fp32), two of them in LDS, for two or three workgroups a unit.  Bound by the issue of vector
-// instructions beside the matrix ones: with heads of 128 under a cap (16 prompts of 1500 to 2048 tokens with prefix, 16 heads on 4) 450 us,
-// 0.52 PFLOP/s, vector units issuing 47 % and matrix units busy 26 % of the time with 1.7 wavefronts a SIMD; documents in two rows of 8192, 16
-// heads of 64: 95 us, 0.38 PFLOP/s.  A call of short prompts (64 of 4 to 512 tokens, 12 heads of 64: 34 us) waits for its first tiles 43 % of a
-// wavefront's time.  Three tiles in LDS, priorities around the matrix instructions and the sum of a row's weights by dot products made
-// no difference (100 +- 2 us).
+// takes them; tiles of 64 keys (32 in fp32), two of them in LDS, for two or three workgroups a unit.  Bound by waits with few wavefronts
+// there: no unit is full, and each wavefront waits for its own products, reads of LDS and barriers while one or two others have the SIMD.  With
+// heads of 128 under a cap (16 prompts of 1500 to 2048 tokens with prefix, 16 heads on 4) 389 us, 0.60 PFLOP/s: vector units issue 46 %
+// and matrix units are busy 26 % of the time, 1.7 wavefronts a SIMD wait 25 % of theirs; documents in two rows of 8192, 16 heads of 64: 87 us,
+// 0.42 PFLOP/s, 40 %, 19 %, 2.1 wavefronts, 36 %.  A call of short prompts (64 of 4 to 512 tokens, 12 heads of 64: 33 us) waits 42 % of a
+// wavefront's time, for its first tiles.  Three tiles in LDS, priorities around the matrix instructions and the sum of a row's weights by dot
+// products made no difference (2 %).
 template <typename T, int DP, bool PARTS>
 __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     using L = Tile<T, DP>;
@@ -252,8 +253,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
 // Few rows, at most 32 of a key head's queries: single tokens over their keys, where the time goes into reading keys and values.  The
 // workgroup's wavefronts have the same rows and take tiles of 32 keys in turn, each with tiles of its own on their way through LDS, so
 // none waits for another until their rows are put together at the end.  Bound by memory: 32 caches of 500 to 32768 keys, 8 heads of 128, 1.05 GB
-// in 203 us, 5.2 TB/s (a copy reaches 5.1); one cache of 65521 keys, 4 heads, 134 MB in 28 us, 4.8 TB/s; 8 first rows over up to 512 keys
-// 8.5 us, most of it the way to the first tile and out.
+// in 203 us, 5.2 TB/s (a copy reaches 5.1); one cache of 65521 keys, 4 heads, 134 MB in 27 us, 4.9 TB/s; 8 first rows over up to 512 keys
+// 8.5 us, most of it the way to the first tile and out.  In fp32 a tile of 128 features leaves room for one a wavefront: the caches, 2.1 GB,
+// 525 us, 4.0 TB/s; with heads of 64, two tiles a wavefront in one workgroup a unit, 1.05 GB at 4.1; 8 first rows 16 us.
 template <typename T, int DP>
 struct Few {
     using L = Tile<T, DP, 32>;
