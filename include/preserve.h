@@ -383,6 +383,36 @@ int ps_rotary(const ps_rotary_desc* desc, const void* x, void* out, const void* 
 int ps_rotary_frequencies(int32_t n_pairs, double base, int scaling, double factor, int32_t trained_len, double slow, double fast,
                           float* frequencies /*host*/);
 
+/* Norms of queries and keys, a head of a row at a time, with the rotary positions in the same pass: of every row t and head
+ *     u = x / sqrt(mean of x^2 over the head + eps),  out = u * weight, its pairs turned as ps_rotary() turns them
+ * in fp32, rounded once at the end.
+ *   x, out      [n_rows][heads][head_dim]; out may be x (in place, same strides) but may not overlap it otherwise
+ *   weight      [head_dim] of `dtype`, the same for all heads, or NULL: ones
+ *   x2, weight2, out2  NULL, or a second pair of tensors (the keys) with heads2 heads and a weight of their own (or NULL), turned by the same angles
+ *   positions   [n_rows] int32, any value;  frequencies [n_pairs] float (ps_rotary_frequencies()); n_pairs 0: no rotation, both may be NULL
+ *   eps > 0;  strides: multiples of one element; heads whose size and turning pieces are multiples of 16 bytes, or 8, are moved faster
+ * Errors: PS_EINVAL (null pointers, negative sizes or strides, 2 n_pairs > head_dim, eps), PS_EUNSUPPORTED (head_dim above 512, 2^27
+ * elements or more in a row's heads, n_rows above 2^31 - 1), PS_EHIP. */
+typedef struct ps_norm_rotary_desc {
+    int32_t dtype, head_dim, n_pairs, interleaved, heads, heads2;
+    float magnitude, eps;
+    int64_t n_rows;
+    ps_strides x, out, x2, out2;        /* out, out2: forwards */
+    ps_strides dout, dx, dout2, dx2;    /* backwards */
+} ps_norm_rotary_desc;
+int ps_norm_rotary_forward(const ps_norm_rotary_desc* desc, const void* x, const void* weight, void* out, const void* x2, const void* weight2,
+                           void* out2, const int32_t* positions, const float* frequencies, void* hip_stream);
+
+/* Its gradients from that of `out`: with g = dout turned back, dweight[e] = sum of g u over all rows and heads ([head_dim] float, NULL: not
+ * wanted; the order of the sum is fixed by the shape), dx = (g weight - u * mean of (g weight u)) / sqrt(mean x^2 + eps).
+ *   dx          may be dout or x (in place, same strides) but may not overlap them otherwise
+ *   workspace   ps_norm_rotary_workspace_bytes() bytes, 256-byte aligned (0 on arguments that the calls refuse)
+ * Errors: as above, PS_EWORKSPACE. */
+size_t ps_norm_rotary_workspace_bytes(int64_t n_rows, int32_t heads, int32_t heads2, int32_t head_dim);
+int ps_norm_rotary_backward(const ps_norm_rotary_desc* desc, const void* x, const void* weight, const void* dout, void* dx, float* dweight,
+                            const void* x2, const void* weight2, const void* dout2, void* dx2, float* dweight2, const int32_t* positions,
+                            const float* frequencies, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Dropout whose mask is drawn where it is needed and never stored, with the bias in front of it and the residual behind it:
  *     out[r][c] = residual[r][c] + keep(r, c) * (x[r][c] + bias[c]) * 65536 / (65536 - T),   T = rint(65536 p)
  * keep(r, c) is 1 if u(r, c) >= T, else 0 (the value is then left out, whatever it is), where u are the 16-bit pieces, low halves first, of the four words of

@@ -1,5 +1,5 @@
 """64-bit definitions of the operators of a layer that is fine-tuned or takes long prompts: attention with capped scores, distance
-bias, document and prefix masks, and its gradients; rotary positions; dropout from a counter-based generator.  Plain numpy, a
+bias, document and prefix masks, and its gradients; rotary positions, alone and behind norms of heads; dropout from a counter-based generator.  Plain numpy, a
 sequence and a head at a time."""
 from __future__ import annotations
 
@@ -121,3 +121,14 @@ def dropout_gradients(dout, seed, offset, p):
     keep, by = kept(*dout.shape, seed, offset, p)
     dx = np.where(keep, dout * by, 0.0)
     return dx, dx.sum(0)
+
+
+def norm_rotate(x, weight, positions, frequencies, eps=1e-6, interleaved=False, magnitude=1.0, dout=None):
+    """x [rows, heads, size], each head's norm taken, weighed (weight [size] or None) and turned: out or, with dout, (dx, dweight)."""
+    x = np.asarray(x, np.float64)
+    w = np.ones(x.shape[2]) if weight is None else np.asarray(weight, np.float64)
+    by = 1.0 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    if dout is None:
+        return rotate(x * by * w, positions, frequencies, interleaved, magnitude)
+    g = rotate(dout, positions, frequencies, interleaved, magnitude, inverse=True)
+    return by * (g * w - x * by * (g * w * x * by).mean(-1, keepdims=True)), (g * x * by).sum((0, 1))

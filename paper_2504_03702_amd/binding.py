@@ -28,7 +28,8 @@ EXPORTS = ["ps_model_load", "ps_model_free", "ps_model_get_info", "ps_workspace_
            "ps_profile_enable", "ps_profile_read", "ps_profile_clock", "ps_profile_stream_read",
            "ps_lookahead_workspace_bytes", "ps_lookahead_update", "ps_scaler_scan", "ps_route", "ps_forecast",
            "ps_attention_workspace_bytes", "ps_attention_forward", "ps_attention_backward", "ps_rotary", "ps_rotary_frequencies",
-           "ps_dropout_workspace_bytes", "ps_dropout_forward", "ps_dropout_backward"]
+           "ps_dropout_workspace_bytes", "ps_dropout_forward", "ps_dropout_backward",
+           "ps_norm_rotary_workspace_bytes", "ps_norm_rotary_forward", "ps_norm_rotary_backward"]
 PS_FAMILIES = ["embed", "gemm", "attention", "layernorm", "head", "refine"]
 
 
@@ -60,6 +61,12 @@ class ps_attention_seqs(ctypes.Structure):
 class ps_rotary_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "head_dim", "n_pairs", "interleaved", "inverse", "heads", "heads2")] + \
         [("magnitude", ctypes.c_float), ("n_rows", ctypes.c_int64)] + [(n, ps_strides) for n in ("x", "out", "x2", "out2")]
+
+
+class ps_norm_rotary_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "head_dim", "n_pairs", "interleaved", "heads", "heads2")] + \
+        [("magnitude", ctypes.c_float), ("eps", ctypes.c_float), ("n_rows", ctypes.c_int64)] + \
+        [(n, ps_strides) for n in ("x", "out", "x2", "out2", "dout", "dx", "dout2", "dx2")]
 
 
 class ps_status(ctypes.Structure):
@@ -133,13 +140,21 @@ def load_library() -> ctypes.CDLL:
     lib.ps_dropout_forward.argtypes = [vp, i64, vp, vp, i64, vp, ctypes.c_float, i32, i64, i32, vp, i64, vp]
     lib.ps_dropout_backward.restype = ctypes.c_int
     lib.ps_dropout_backward.argtypes = [vp, i64, vp, ctypes.c_float, i32, i64, i32, vp, i64, vp, vp, sz, vp]
+    norm = ctypes.POINTER(ps_norm_rotary_desc)
+    lib.ps_norm_rotary_workspace_bytes.restype = sz
+    lib.ps_norm_rotary_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    lib.ps_norm_rotary_forward.restype = ctypes.c_int
+    lib.ps_norm_rotary_forward.argtypes = [norm, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.ps_norm_rotary_backward.restype = ctypes.c_int
+    lib.ps_norm_rotary_backward.argtypes = [norm, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.ps_strerror.restype = ctypes.c_char_p
     lib.ps_strerror.argtypes = [ctypes.c_int]
     _native = _extension()
     if _native is not None:
         _native.bind(*[ctypes.cast(getattr(lib, "ps_" + name), vp).value for name in (
             "predict_load", "anticipate", "anticipate_static", "lookahead_update", "scaler_scan", "route", "forecast",
-            "attention_forward", "attention_backward", "rotary", "dropout_forward", "dropout_backward")])
+            "attention_forward", "attention_backward", "rotary", "dropout_forward", "dropout_backward", "norm_rotary_forward",
+            "norm_rotary_backward")])
     _lib = lib
     return lib
 
@@ -570,6 +585,72 @@ def ps_dropout_backward(dout: torch.Tensor, rng: torch.Tensor, p: float, dx: tor
     _check(load_library().ps_dropout_backward(
         *g, _sized_ptr(rng, torch.int64, 2, "rng"), p, code, *shape, *to, _sized_ptr(dbias, torch.float32, shape[1], "dbias"),
         _ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(), _stream()), "ps_dropout_backward")
+
+
+def _on_current_device(where: str, *tensors) -> None:
+    """The stream is the current device's: tensors of another would be read by a kernel of the wrong one."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != here:
+            raise ValueError(f"{where}: a tensor is on cuda:{t.device.index}, the current device is cuda:{here}")
+
+
+def ps_norm_rotary_workspace_bytes(n_rows: int, heads: int, heads2: int, head_dim: int) -> int:
+    return int(load_library().ps_norm_rotary_workspace_bytes(n_rows, heads, heads2, head_dim))
+
+
+def _norm_rotary(where, x, x2, positions, frequencies, eps, interleaved, magnitude, tensors):
+    """The call's descriptor and the addresses of `tensors` ({name: tensor}; names that end in 2 have x2's shape)."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 3 or (x2 is not None and (not isinstance(x2, torch.Tensor) or x2.dim() != 3)):
+        raise TypeError(f"{where}: x and x2 are tensors of rows, heads and elements")
+    (n, heads, size), heads2 = x.shape, 0 if x2 is None else x2.shape[1]
+    if frequencies is not None and positions is None:
+        raise TypeError(f"{where}: frequencies go with positions")
+    d = ps_norm_rotary_desc(_dtype_code(x.dtype, where), size, 0 if frequencies is None else frequencies.numel(), int(interleaved), heads, heads2,
+                            magnitude, eps, n)
+    at = {}
+    for name, t in tensors.items():
+        second = name.endswith("2")
+        if t is None and second and x2 is None:
+            at[name] = None
+            continue
+        at[name], strides = _heads_ptr(t, (n, heads2 if second else heads, size), x.dtype, name)
+        setattr(d, name, strides)
+    return d, at, _sized_ptr(positions, torch.int32, n, "positions"), _ptr(frequencies, torch.float32, "frequencies"), size
+
+
+def ps_norm_rotary_forward(x: torch.Tensor, weight: Optional[torch.Tensor], positions: Optional[torch.Tensor], frequencies: Optional[torch.Tensor],
+                           out: torch.Tensor, x2: Optional[torch.Tensor] = None, weight2: Optional[torch.Tensor] = None,
+                           out2: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False, magnitude: float = 1.0) -> None:
+    """x, out [n_rows, heads, head_dim]; weight [head_dim] of the same type, None: ones; x2, weight2, out2: a second tensor's, turned by the same
+    angles.  out may be x.  frequencies None: no rotation."""
+    if _made("norm_rotary_forward", x, weight, positions, frequencies, out, x2, weight2, out2, eps, interleaved, magnitude):
+        return
+    d, at, pos, freq, size = _norm_rotary("ps_norm_rotary_forward", x, x2, positions, frequencies, eps, interleaved, magnitude,
+                                          {"x": x, "out": out, "x2": x2, "out2": out2})
+    _on_current_device("ps_norm_rotary_forward", x, weight, positions, frequencies, out, x2, weight2, out2)
+    _check(load_library().ps_norm_rotary_forward(
+        ctypes.byref(d), at["x"], _sized_ptr(weight, x.dtype, size, "weight"), at["out"], at["x2"], _sized_ptr(weight2, x.dtype, size, "weight2"),
+        at["out2"], pos, freq, _stream()), "ps_norm_rotary_forward")
+
+
+def ps_norm_rotary_backward(x: torch.Tensor, weight: Optional[torch.Tensor], positions: Optional[torch.Tensor], frequencies: Optional[torch.Tensor],
+                            dout: torch.Tensor, dx: torch.Tensor, dweight: Optional[torch.Tensor], workspace: torch.Tensor,
+                            x2: Optional[torch.Tensor] = None, weight2: Optional[torch.Tensor] = None, dout2: Optional[torch.Tensor] = None,
+                            dx2: Optional[torch.Tensor] = None, dweight2: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                            interleaved: bool = False, magnitude: float = 1.0) -> None:
+    """dx like x and, unless they are None, dweight and dweight2 ([head_dim] float32), from dout; the rest as forwards.  dx may be dout or x."""
+    if _made("norm_rotary_backward", x, weight, positions, frequencies, dout, dx, dweight, workspace, x2, weight2, dout2, dx2, dweight2, eps,
+             interleaved, magnitude):
+        return
+    d, at, pos, freq, size = _norm_rotary("ps_norm_rotary_backward", x, x2, positions, frequencies, eps, interleaved, magnitude,
+                                          {"x": x, "dout": dout, "dx": dx, "x2": x2, "dout2": dout2, "dx2": dx2})
+    _on_current_device("ps_norm_rotary_backward", x, weight, positions, frequencies, dout, dx, dweight, workspace, x2, weight2, dout2, dx2, dweight2)
+    f32 = torch.float32
+    _check(load_library().ps_norm_rotary_backward(
+        ctypes.byref(d), at["x"], _sized_ptr(weight, x.dtype, size, "weight"), at["dout"], at["dx"], _sized_ptr(dweight, f32, size, "dweight"),
+        at["x2"], _sized_ptr(weight2, x.dtype, size, "weight2"), at["dout2"], at["dx2"], _sized_ptr(dweight2, f32, size, "dweight2"), pos, freq,
+        _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()), "ps_norm_rotary_backward")
 
 
 def alloc_workspace(nbytes: int, device="cuda") -> torch.Tensor:

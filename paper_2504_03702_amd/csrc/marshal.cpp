@@ -33,10 +33,12 @@ struct Calls {
     decltype(&ps_rotary) rotary;
     decltype(&ps_dropout_forward) dropout_forward;
     decltype(&ps_dropout_backward) dropout_backward;
+    decltype(&ps_norm_rotary_forward) norm_rotary_forward;
+    decltype(&ps_norm_rotary_backward) norm_rotary_backward;
 } g_calls;
 
 PyObject* bind(PyObject*, PyObject* const* at, Py_ssize_t n) {
-    constexpr int N = 12;
+    constexpr int N = 14;
     void* p[N];
     if (n != N) { PyErr_SetString(PyExc_TypeError, "bind: an address for every call"); return nullptr; }
     for (int i = 0; i < N; ++i) {
@@ -46,13 +48,22 @@ PyObject* bind(PyObject*, PyObject* const* at, Py_ssize_t n) {
     g_calls = {(decltype(&ps_predict_load))p[0], (decltype(&ps_anticipate))p[1], (decltype(&ps_anticipate_static))p[2],
                (decltype(&ps_lookahead_update))p[3], (decltype(&ps_scaler_scan))p[4], (decltype(&ps_route))p[5],
                (decltype(&ps_forecast))p[6], (decltype(&ps_attention_forward))p[7], (decltype(&ps_attention_backward))p[8],
-               (decltype(&ps_rotary))p[9], (decltype(&ps_dropout_forward))p[10], (decltype(&ps_dropout_backward))p[11]};
+               (decltype(&ps_rotary))p[9], (decltype(&ps_dropout_forward))p[10], (decltype(&ps_dropout_backward))p[11],
+               (decltype(&ps_norm_rotary_forward))p[12], (decltype(&ps_norm_rotary_backward))p[13]};
     Py_RETURN_NONE;
 }
 
 struct Args {
     PyObject* const* at;
     bool good = true;
+    int device = -1;                     // of the first tensor
+    bool one_device = true;
+
+    void seen(const at::Tensor& t) {
+        const int d = t.get_device();
+        if (device < 0) device = d;
+        if (d != device) one_device = false;
+    }
 
     // A tensor's device pointer (null for None); n: its elements, if not null.
     template <typename T>
@@ -63,6 +74,7 @@ struct Args {
         if (!good || !THPVariable_CheckExact(o)) { good = false; return nullptr; }
         const at::Tensor& t = THPVariable_Unpack(o);
         if (!t.defined() || !t.is_cuda() || t.scalar_type() != type || !t.is_contiguous()) { good = false; return nullptr; }
+        seen(t);
         if (n) *n = t.numel();
         return (T*)t.data_ptr();
     }
@@ -96,6 +108,7 @@ struct Args {
         if (!good || !THPVariable_CheckExact(o)) { good = false; return nullptr; }
         const at::Tensor& t = THPVariable_Unpack(o);
         if (!t.defined() || !t.is_cuda() || t.dim() != 3) { good = false; return nullptr; }
+        seen(t);
         if (shape[2] < 0) {
             *type = t.scalar_type();
             if (*type != at::kFloat && *type != at::kBFloat16) good = false;
@@ -145,9 +158,10 @@ struct Args {
 constexpr at::ScalarType kI32 = at::kInt, kI64 = at::kLong, kF32 = at::kFloat, kF64 = at::kDouble, kU8 = at::kByte;
 
 // The current stream of the current device; false with an exception set if torch cannot say.
-bool current_stream(void** s) {
+bool current_stream(void** s, long* device) {
     PyObject* dev = PyObject_CallNoArgs(g_device);
     if (!dev) return false;
+    *device = PyLong_AsLong(dev);
     PyObject* raw = PyObject_CallOneArg(g_raw_stream, dev);
     Py_DECREF(dev);
     if (!raw) return false;
@@ -157,15 +171,18 @@ bool current_stream(void** s) {
 }
 
 // parse: fills in the arguments and returns the call (given the stream), which is made without the interpreter's lock.
+// here: the tensors have to be on the current device.
 template <typename Parse>
-PyObject* make_call(PyObject* const* at, Py_ssize_t n, Py_ssize_t want, Parse parse) {
+PyObject* make_call(PyObject* const* at, Py_ssize_t n, Py_ssize_t want, Parse parse, bool here = false) {
     if (n != want) Py_RETURN_NOTIMPLEMENTED;
     try {
         Args a{at};
         auto call = parse(a);
         if (!a.good) Py_RETURN_NOTIMPLEMENTED;
         void* stream;
-        if (!current_stream(&stream)) return nullptr;
+        long device = -1;
+        if (!current_stream(&stream, &device)) return nullptr;
+        if (here && (!a.one_device || a.device != device)) Py_RETURN_NOTIMPLEMENTED;
         int code = PS_OK;
         bool thrown = false;
         Py_BEGIN_ALLOW_THREADS
@@ -458,11 +475,86 @@ PyObject* dropout_backward(PyObject*, PyObject* const* at, Py_ssize_t n) {
     });
 }
 
+// What the two calls of a normed and turned tensor, and of a second one, share.
+struct NormRotary {
+    ps_norm_rotary_desc d = {};
+    at::ScalarType type = at::kFloat, type2 = at::kFloat;
+    int64_t shape[3] = {-1, -1, -1}, shape2[3] = {-1, -1, -1}, pairs = 0;
+    bool two = false;
+    const int32_t* positions = nullptr;
+    const float* frequencies = nullptr;
+
+    void* first(Args& a, int i, ps_strides ps_norm_rotary_desc::*s) { return a.heads(i, &type, shape, d.*s); }
+    // (the second tensors are there or not together)
+    void* second(Args& a, int i, ps_strides ps_norm_rotary_desc::*s) {
+        if (!two) {
+            if (a.at[i] != Py_None) a.good = false;
+            return nullptr;
+        }
+        return a.heads(i, &type2, shape2, d.*s);
+    }
+    void open(Args& a, int x2) {
+        two = a.at[x2] != Py_None;
+        shape2[0] = shape[0];
+    }
+    // at[i] and on are positions and frequencies, at[j] and on eps, interleaved and magnitude
+    void others(Args& a, int i, int j) {
+        if (two && a.good && (type2 != type || shape2[2] != shape[2])) a.good = false;
+        frequencies = a.tensor<float>(i + 1, kF32, &pairs, true);
+        positions = a.sized<int32_t>(i, kI32, shape[0], true);
+        if (pairs >= 0 && !positions) a.good = false;
+        d.dtype = type == at::kBFloat16;
+        d.head_dim = a.count32(shape[2]);
+        d.n_pairs = a.count32(pairs < 0 ? 0 : pairs);
+        d.heads = a.count32(shape[1]);
+        d.heads2 = two ? a.count32(shape2[1]) : 0;
+        d.n_rows = shape[0];
+        d.eps = a.f32(j);
+        d.interleaved = a.truth(j + 1);
+        d.magnitude = a.f32(j + 2);
+    }
+};
+
+PyObject* norm_rotary_forward(PyObject*, PyObject* const* at, Py_ssize_t n) {
+    return make_call(at, n, 11, [](Args& a) {
+        using D = ps_norm_rotary_desc;
+        NormRotary t;
+        const void* x = t.first(a, 0, &D::x);
+        void* out = t.first(a, 4, &D::out);
+        t.open(a, 5);
+        const void* x2 = t.second(a, 5, &D::x2);
+        void* out2 = t.second(a, 7, &D::out2);
+        t.others(a, 2, 8);
+        const void *w = a.sized<void>(1, t.type, t.shape[2], true), *w2 = a.sized<void>(6, t.type, t.shape[2], true);
+        return [=](void* s) { return g_calls.norm_rotary_forward(&t.d, x, w, out, x2, w2, out2, t.positions, t.frequencies, s); };
+    }, true);
+}
+
+PyObject* norm_rotary_backward(PyObject*, PyObject* const* at, Py_ssize_t n) {
+    return make_call(at, n, 16, [](Args& a) {
+        using D = ps_norm_rotary_desc;
+        NormRotary t;
+        const void *x = t.first(a, 0, &D::x), *dout = t.first(a, 4, &D::dout);
+        void* dx = t.first(a, 5, &D::dx);
+        t.open(a, 8);
+        const void *x2 = t.second(a, 8, &D::x2), *dout2 = t.second(a, 10, &D::dout2);
+        void* dx2 = t.second(a, 11, &D::dx2);
+        t.others(a, 2, 13);
+        const void *w = a.sized<void>(1, t.type, t.shape[2], true), *w2 = a.sized<void>(9, t.type, t.shape[2], true);
+        float *dw = a.sized<float>(6, kF32, t.shape[2], true), *dw2 = a.sized<float>(12, kF32, t.shape[2], true);
+        int64_t ws = 0;
+        void* workspace = a.tensor<void>(7, kU8, &ws);
+        return [=](void* s) {
+            return g_calls.norm_rotary_backward(&t.d, x, w, dout, dx, dw, x2, w2, dout2, dx2, dw2, t.positions, t.frequencies, workspace, (size_t)ws, s);
+        };
+    }, true);
+}
+
 #define PS_METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PS_METHOD(bind), PS_METHOD(predict_load), PS_METHOD(anticipate), PS_METHOD(anticipate_static), PS_METHOD(lookahead_update),
                          PS_METHOD(scaler_scan), PS_METHOD(route), PS_METHOD(forecast),
                          PS_METHOD(attention_forward), PS_METHOD(attention_backward), PS_METHOD(rotary), PS_METHOD(dropout_forward),
-                         PS_METHOD(dropout_backward), {nullptr, nullptr, 0, nullptr}};
+                         PS_METHOD(dropout_backward), PS_METHOD(norm_rotary_forward), PS_METHOD(norm_rotary_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

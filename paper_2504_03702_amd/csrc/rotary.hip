@@ -3,8 +3,8 @@
 // 64 in bf16, 268 MB: 55 us, 4.9 TB/s (a copy reaches 5.1); 64 rows of 40 heads of 128: 3.4 us.
 #include <math.h>
 
-#include "device_util.h"
 #include "internal.h"
+#include "rotary.h"
 
 typedef __bf16 bf16;
 
@@ -102,12 +102,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     };
     fetch(threadIdx.x);
     for (int i = threadIdx.x; i < rows * n; i += 256) {
-        // whole turns go in 64 bits: a position of 31 bits times a frequency of 24 leaves the fraction all a float can hold
-        double turns = (double)a.positions[row0 + i / n] * (double)a.frequencies[i % n] * 0.15915494309189533577;
-        turns -= rint(turns);
-        float s, c;
-        sincospif(2.f * (float)turns, &s, &c);
-        table[i] = make_float2(c * a.magnitude, s * a.magnitude * a.sign);
+        const float2 w = turn_of(a.positions[row0 + i / n], a.frequencies[i % n]);
+        table[i] = make_float2(w.x * a.magnitude, w.y * a.magnitude * a.sign);
     }
     __syncthreads();
     turn();

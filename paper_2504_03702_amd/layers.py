@@ -124,6 +124,36 @@ def rotary(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, frequencie
     return _Rotary.apply(q, k, positions, frequencies, interleaved, magnitude)
 
 
+class _NormRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, frequencies, eps, interleaved, magnitude):
+        out = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k)]
+        ps.ps_norm_rotary_forward(q, q_weight, positions, frequencies, out[0], k, k_weight, out[1], eps, interleaved, magnitude)
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions, frequencies)
+        ctx.how = eps, interleaved, magnitude
+        return tuple(out)
+
+    @staticmethod
+    @_first_only
+    def backward(ctx, dq_out, dk_out):
+        q, k, q_weight, k_weight, positions, frequencies = ctx.saved_tensors
+        dq_out, dk_out = (t if t.stride(-1) == 1 else t.contiguous() for t in (dq_out, dk_out))
+        dq, dk = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        dweights = [torch.empty(q.shape[2], device=q.device) if ctx.needs_input_grad[i] else None for i in (2, 3)]
+        ws = ps.alloc_workspace(ps.ps_norm_rotary_workspace_bytes(q.shape[0], q.shape[1], k.shape[1], q.shape[2]), q.device)
+        ps.ps_norm_rotary_backward(q, q_weight, positions, frequencies, dq_out, dq, dweights[0], ws, k, k_weight, dk_out, dk, dweights[1], *ctx.how)
+        return (dq, dk, *[None if d is None else d.to(w.dtype) for d, w in zip(dweights, (q_weight, k_weight))], None, None, None, None, None)
+
+
+def norm_rotary(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
+                positions: Optional[torch.Tensor], frequencies: Optional[torch.Tensor], eps: float = 1e-6, interleaved: bool = False,
+                magnitude: float = 1.0) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Queries and keys, each head's norm taken and weighed ([head_dim] of their type, None: ones), turned to their positions (frequencies None:
+    not turned); frequencies are constants."""
+    _constant(frequencies, "norm_rotary", "frequencies")
+    return _NormRotary.apply(q, k, q_weight, k_weight, positions, frequencies, eps, interleaved, magnitude)
+
+
 class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, bias, residual, rng, p):
