@@ -348,6 +348,42 @@ int ps_attention_backward(const ps_attention_desc* desc, const ps_attention_seqs
                           const void* out, const float* lse, const void* out_rest, const void* dout, void* dq, void* dk, void* dv, void* workspace,
                           size_t workspace_bytes, ps_status* status, void* hip_stream);
 
+/* The same attention of rows that see a window of places and the first few keys, and with a learned bias by buckets of distances:
+ *     score = y - slopes[h] * |a - j| + bias[buckets[reach + clamp(j - a, -reach, reach)]][h]
+ * over the keys of ps_attention_forward() that are, besides, among the first ones or in the window:  j < sinks  or  a - left <= j <= a + right.
+ *   left, right  >= 0, or negative: without end (causal calls see nothing behind a row, whatever `right`, but a prefix that is in the window)
+ *   sinks        >= 0
+ *   n_buckets    0: no bias (buckets and bias are not read); at most 64
+ *   reach        >= 0, at most 65536: larger distances have the bucket of that one
+ *   buckets      [2 reach + 1] int32 on the device, as ps_bias_buckets() makes them or any others; a bucket that there is not (-1): no bias
+ *   bias         [n_buckets][heads] float on the device
+ * A key head's rows have at most 32 heads where there is a bias.  The time goes by the keys that are seen; tiles outside of all windows of a block of
+ * rows are not read. */
+typedef struct ps_attention_local {
+    int32_t left, right, sinks, n_buckets, reach;
+    const int32_t* buckets;
+    const float* bias;
+} ps_attention_local;
+
+/* Arguments, results and errors as of ps_attention_workspace_bytes(), ps_attention_forward() and ps_attention_backward(); PS_EINVAL for a null `local`
+ * and its bad numbers and pointers, PS_EUNSUPPORTED for n_buckets, reach and heads above those.  Of `local`, the workspace goes by the numbers alone, and
+ * not by `causal` of `desc`.
+ * dbias: [n_buckets][heads] float, NULL: not wanted; overwritten with the gradient of the bias, of pair ij and its distance's bucket p_ij (dout_i . v_j - D_i),
+ * over all rows of all sequences that are not faulty.  Its sums are fp32 too, in an order that is fixed by the shapes. */
+size_t ps_local_attention_workspace_bytes(const ps_attention_desc* desc, const ps_attention_local* local, int backward);
+int ps_local_attention_forward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const ps_attention_local* local, const void* q, const void* k,
+                               const void* v, void* out, float* lse, void* out_rest, void* workspace, size_t workspace_bytes, ps_status* status,
+                               void* hip_stream);
+int ps_local_attention_backward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const ps_attention_local* local, const void* q, const void* k,
+                                const void* v, const void* out, const float* lse, const void* out_rest, const void* dout, void* dq, void* dk, void* dv,
+                                float* dbias, void* workspace, size_t workspace_bytes, ps_status* status, void* hip_stream);
+
+/* Buckets of the distances -reach .. reach (host array of 2 reach + 1), n of them: those of a side's first half are single distances from 0 on, the others
+ * ever wider, their borders equally far apart as logarithms, up to `reach` (a side's last one holds all that is further).  both_sides: keys behind
+ * a row have the second half of the buckets (n even, distance 0 on the first side), else they share that of distance 0 (causal calls).
+ * Errors: PS_EINVAL (n above 64, a side of fewer than two, reach below a side's single distances or above 65536). */
+int ps_bias_buckets(int32_t n_buckets, int32_t reach, int both_sides, int32_t* buckets /*host*/);
+
 /* Rotary positions: of every row t and head, the pairs i < n_pairs of x turn by the angle positions[t] * frequencies[i]
  *     (a, b) -> magnitude * (a cos - b sin, a sin + b cos)
  * where pair i is (x[2 i], x[2 i + 1]) if interleaved, else (x[i], x[i + n_pairs]); the head's other elements are copied.

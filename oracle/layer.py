@@ -6,19 +6,25 @@ from __future__ import annotations
 import numpy as np
 
 
-def visible(nq, nk, start, causal=False, prefix=0, q_docs=None, k_docs=None):
+def visible(nq, nk, start, causal=False, prefix=0, q_docs=None, k_docs=None, left=-1, right=-1, sinks=0):
     """[nq, nk] truth: which keys row i, at position start + i, sees."""
     place, key = start + np.arange(nq)[:, None], np.arange(nk)[None]
     seen = np.ones((nq, nk), bool)
     if causal:
         seen = (key <= place) | (key < prefix)
+    if left >= 0:
+        seen &= (key >= place - left) | (key < sinks)
+    if right >= 0:
+        seen &= (key <= place + right) | (key < sinks)
     if q_docs is not None:
         seen &= (q_docs[:, None] == k_docs[None]) & (q_docs[:, None] >= 0)
     return seen
 
 
-def attend(q, k, v, seen, start, scale, cap=0.0, slope=0.0, dout=None):
-    """One head of one sequence: (out, lse) and, with dout, (dq, dk, dv).  Only what is seen is ever touched."""
+def attend(q, k, v, seen, start, scale, cap=0.0, slope=0.0, dout=None, buckets=None, bias=None):
+    """One head of one sequence: (out, lse) and, with dout, (dq, dk, dv) and, with a bias ([buckets], and buckets of the distances
+    -reach .. reach), dbias.  Only what is seen is ever touched."""
+    dbias = None if bias is None else np.zeros(len(bias))
     nq, nk = seen.shape
     out, lse = np.zeros((nq, v.shape[1])), np.full(nq, -np.inf)
     dq, dk, dv = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)
@@ -29,6 +35,11 @@ def attend(q, k, v, seen, start, scale, cap=0.0, slope=0.0, dout=None):
         x = scale * (k[j] @ q[i])
         bent = np.tanh(x / cap) if cap > 0 else None
         y = (cap * bent if cap > 0 else x) - slope * np.abs(start + i - j)
+        if bias is not None:
+            reach = len(buckets) // 2
+            of = np.asarray(buckets)[np.clip(j - (start + i), -reach, reach) + reach]
+            has = (of >= 0) & (of < len(bias))
+            y = y + np.where(has, np.asarray(bias, np.float64)[np.where(has, of, 0)], 0.0)
         top = y.max()
         e = np.exp(y - top)
         p = e / e.sum()
@@ -37,20 +48,24 @@ def attend(q, k, v, seen, start, scale, cap=0.0, slope=0.0, dout=None):
         if dout is not None:
             dv[j] += p[:, None] * dout[i]
             g = p * (v[j] @ dout[i] - dout[i] @ out[i])
+            if bias is not None:
+                np.add.at(dbias, of[has], g[has])
             if cap > 0:
                 g = g * (1 - bent * bent)
             dq[i] = scale * (g @ k[j])
             dk[j] += scale * g[:, None] * q[i]
-    return (out, lse) if dout is None else (out, lse, dq, dk, dv)
+    return (out, lse) if dout is None else (out, lse, dq, dk, dv) if bias is None else (out, lse, dq, dk, dv, dbias)
 
 
 def attention(q, k, v, q_offsets, k_offsets, k_lengths=None, q_start=None, prefix=None, q_docs=None, k_docs=None, slopes=None,
-              causal=False, scale=None, cap=0.0, dout=None):
-    """Packed tensors [rows, heads, size]: (out, lse [heads, rows]) and, with dout, (dq, dk, dv).  Rows outside the sequences: NaN."""
+              causal=False, scale=None, cap=0.0, dout=None, left=-1, right=-1, sinks=0, buckets=None, bias=None):
+    """Packed tensors [rows, heads, size]: (out, lse [heads, rows]) and, with dout, (dq, dk, dv) and, with bias [buckets, heads], dbias.  Rows
+    outside the sequences: NaN."""
     q, k, v = (np.asarray(t, np.float64) for t in (q, k, v))
     heads, kv_heads, scale = q.shape[1], k.shape[1], q.shape[2] ** -0.5 if scale is None else scale
     out, lse = np.full(q.shape, np.nan), np.full((heads, q.shape[0]), np.nan)
     dq, dk, dv = np.full(q.shape, np.nan), np.full(k.shape, np.nan), np.full(v.shape, np.nan)
+    dbias = None if bias is None else np.zeros(np.shape(bias))
     for s in range(len(q_offsets) - 1):
         rows = slice(q_offsets[s], q_offsets[s + 1])
         n = k_offsets[s + 1] - k_offsets[s] if k_lengths is None else k_lengths[s]
@@ -58,18 +73,33 @@ def attention(q, k, v, q_offsets, k_offsets, k_lengths=None, q_start=None, prefi
         nq = rows.stop - rows.start
         start = n - nq if q_start is None else q_start[s]
         seen = visible(nq, n, start, causal, 0 if prefix is None else prefix[s], None if q_docs is None else q_docs[rows],
-                       None if k_docs is None else k_docs[keys])
+                       None if k_docs is None else k_docs[keys], left, right, sinks)
         dk[keys], dv[keys] = 0.0, 0.0
         for h in range(heads):
             c = h * kv_heads // heads
             got = attend(q[rows, h], k[keys, c], v[keys, c], seen, start, scale, cap, 0.0 if slopes is None else float(slopes[h]),
-                         None if dout is None else np.asarray(dout, np.float64)[rows, h])
+                         None if dout is None else np.asarray(dout, np.float64)[rows, h], buckets, None if bias is None else np.asarray(bias)[:, h])
             out[rows, h], lse[h, rows] = got[:2]
             if dout is not None:
                 dq[rows, h] = got[2]
                 dk[keys, c] += got[3]
                 dv[keys, c] += got[4]
-    return (out, lse) if dout is None else (out, lse, dq, dk, dv)
+                if bias is not None:
+                    dbias[:, h] += got[5]
+    return (out, lse) if dout is None else (out, lse, dq, dk, dv) if bias is None else (out, lse, dq, dk, dv, dbias)
+
+
+def buckets(n, reach, both_sides=True):
+    """Buckets of the distances -reach .. reach, their borders found in whole numbers: a side's bucket single + b starts at the first
+    distance m with m^(side - single) >= single^(side - single - b) reach^b."""
+    side = n // 2 if both_sides else n
+    single, found = side // 2, []
+    wide = side - single
+    for d in range(-reach, reach + 1):
+        m = -d if d < 0 else d if both_sides else 0
+        b = m if m < single else single + sum(m ** wide >= single ** (wide - i) * reach ** i for i in range(1, wide))
+        found.append(b + (side if both_sides and d > 0 else 0))
+    return np.array(found)
 
 
 def rotate(x, positions, frequencies, interleaved=False, magnitude=1.0, inverse=False):

@@ -29,7 +29,8 @@ EXPORTS = ["ps_model_load", "ps_model_free", "ps_model_get_info", "ps_workspace_
            "ps_lookahead_workspace_bytes", "ps_lookahead_update", "ps_scaler_scan", "ps_route", "ps_forecast",
            "ps_attention_workspace_bytes", "ps_attention_forward", "ps_attention_backward", "ps_rotary", "ps_rotary_frequencies",
            "ps_dropout_workspace_bytes", "ps_dropout_forward", "ps_dropout_backward",
-           "ps_norm_rotary_workspace_bytes", "ps_norm_rotary_forward", "ps_norm_rotary_backward"]
+           "ps_norm_rotary_workspace_bytes", "ps_norm_rotary_forward", "ps_norm_rotary_backward",
+           "ps_local_attention_workspace_bytes", "ps_local_attention_forward", "ps_local_attention_backward", "ps_bias_buckets"]
 PS_FAMILIES = ["embed", "gemm", "attention", "layernorm", "head", "refine"]
 
 
@@ -56,6 +57,11 @@ class ps_attention_desc(ctypes.Structure):
 
 class ps_attention_seqs(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("q_offsets", "k_offsets", "k_lengths", "q_start", "prefix", "q_docs", "k_docs", "slopes")]
+
+
+class ps_attention_local(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("left", "right", "sinks", "n_buckets", "reach")] + \
+        [("buckets", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
 
 
 class ps_rotary_desc(ctypes.Structure):
@@ -147,6 +153,15 @@ def load_library() -> ctypes.CDLL:
     lib.ps_norm_rotary_forward.argtypes = [norm, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.ps_norm_rotary_backward.restype = ctypes.c_int
     lib.ps_norm_rotary_backward.argtypes = [norm, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    local = ctypes.POINTER(ps_attention_local)
+    lib.ps_local_attention_workspace_bytes.restype = sz
+    lib.ps_local_attention_workspace_bytes.argtypes = [desc, local, ctypes.c_int]
+    lib.ps_local_attention_forward.restype = ctypes.c_int
+    lib.ps_local_attention_forward.argtypes = [desc, seqs, local, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    lib.ps_local_attention_backward.restype = ctypes.c_int
+    lib.ps_local_attention_backward.argtypes = [desc, seqs, local, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    lib.ps_bias_buckets.restype = ctypes.c_int
+    lib.ps_bias_buckets.argtypes = [i32, i32, ctypes.c_int, ctypes.POINTER(i32)]
     lib.ps_strerror.restype = ctypes.c_char_p
     lib.ps_strerror.argtypes = [ctypes.c_int]
     _native = _extension()
@@ -154,7 +169,7 @@ def load_library() -> ctypes.CDLL:
         _native.bind(*[ctypes.cast(getattr(lib, "ps_" + name), vp).value for name in (
             "predict_load", "anticipate", "anticipate_static", "lookahead_update", "scaler_scan", "route", "forecast",
             "attention_forward", "attention_backward", "rotary", "dropout_forward", "dropout_backward", "norm_rotary_forward",
-            "norm_rotary_backward")])
+            "norm_rotary_backward", "local_attention_forward", "local_attention_backward")])
     _lib = lib
     return lib
 
@@ -651,6 +666,88 @@ def ps_norm_rotary_backward(x: torch.Tensor, weight: Optional[torch.Tensor], pos
         ctypes.byref(d), at["x"], _sized_ptr(weight, x.dtype, size, "weight"), at["dout"], at["dx"], _sized_ptr(dweight, f32, size, "dweight"),
         at["x2"], _sized_ptr(weight2, x.dtype, size, "weight2"), at["dout2"], at["dx2"], _sized_ptr(dweight2, f32, size, "dweight2"), pos, freq,
         _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()), "ps_norm_rotary_backward")
+
+
+def ps_bias_buckets(n_buckets: int, reach: int, both_sides: bool = True) -> torch.Tensor:
+    """[2 reach + 1] int32 on the host: the bucket of a key `reach` in front of its row, ..., `reach` behind it."""
+    out = torch.empty(max(2 * reach + 1, 1), dtype=torch.int32)
+    _check(load_library().ps_bias_buckets(n_buckets, reach, int(both_sides), ctypes.cast(out.data_ptr(), ctypes.POINTER(ctypes.c_int32))),
+           "ps_bias_buckets")
+    return out
+
+
+def ps_local_attention_workspace_bytes(n_seq: int, n_q: int, n_k: int, max_q: int, max_k: int, heads: int, kv_heads: int, head_dim: int,
+                                       dtype: torch.dtype, backward: bool = False, left: int = -1, right: int = -1, sinks: int = 0,
+                                       n_buckets: int = 0, reach: int = 0) -> int:
+    """n_buckets, reach: of the learned bias, 0 without one."""
+    d = ps_attention_desc(_dtype_code(dtype, "ps_local_attention_workspace_bytes"), n_seq, heads, kv_heads, head_dim, max_q, max_k, 0, n_q,
+                          n_k, 1.0, 0.0)
+    return int(load_library().ps_local_attention_workspace_bytes(ctypes.byref(d), ctypes.byref(ps_attention_local(left, right, sinks, n_buckets, reach)),
+                                                                 int(backward)))
+
+
+def _local(where, heads, left, right, sinks, buckets, bias, dbias=None):
+    if (buckets is None) != (bias is None) or (dbias is not None and bias is None):
+        raise ValueError(f"{where}: a bias goes with its buckets")
+    if bias is None:
+        return ps_attention_local(left, right, sinks)
+    if bias.dim() != 2 or bias.shape[1] != heads or buckets.dim() != 1 or buckets.numel() % 2 == 0:
+        raise ValueError(f"{where}: need a bias of buckets and {heads} heads, and a bucket for each of 2 reach + 1 distances")
+    return ps_attention_local(left, right, sinks, bias.shape[0], buckets.numel() // 2, _ptr(buckets, torch.int32, "buckets"),
+                              _ptr(bias, torch.float32, "bias"))
+
+
+def ps_local_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_offsets: torch.Tensor,
+                               max_q: int, max_k: int, out: torch.Tensor, lse: Optional[torch.Tensor], workspace: torch.Tensor,
+                               left: int = -1, right: int = -1, sinks: int = 0, buckets: Optional[torch.Tensor] = None,
+                               bias: Optional[torch.Tensor] = None, scale: Optional[float] = None, softcap: float = 0.0, causal: bool = False,
+                               k_lengths: Optional[torch.Tensor] = None, q_start: Optional[torch.Tensor] = None,
+                               prefix: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None,
+                               q_docs: Optional[torch.Tensor] = None, k_docs: Optional[torch.Tensor] = None,
+                               status: Optional[torch.Tensor] = None, out_rest: Optional[torch.Tensor] = None) -> None:
+    """ps_attention_forward() of rows that see the keys from `left` in front of them to `right` behind (-1: without end) and the first
+    `sinks`, with bias [n_buckets, heads] (float32) by the distance's bucket, buckets [2 reach + 1] (int32)."""
+    if _made("local_attention_forward", q, k, v, q_offsets, k_offsets, max_q, max_k, out, lse, workspace, left, right, sinks, buckets, bias,
+             scale, softcap, causal, k_lengths, q_start, prefix, slopes, q_docs, k_docs, status, out_rest):
+        return
+    where = "ps_local_attention_forward"
+    d, seqs, at, n_lse = _attention(where, q, k, q_offsets, k_offsets, max_q, max_k, scale, softcap, causal, k_lengths, q_start, prefix, slopes,
+                                    q_docs, k_docs, {"q": (q, False), "k": (k, True), "v": (v, True), "out": (out, False)})
+    local = _local(where, q.shape[1], left, right, sinks, buckets, bias)
+    _on_current_device(where, q, k, v, q_offsets, k_offsets, out, lse, workspace, buckets, bias, k_lengths, q_start, prefix, slopes, q_docs, k_docs,
+                       status, out_rest)
+    _check(load_library().ps_local_attention_forward(
+        ctypes.byref(d), ctypes.byref(seqs), ctypes.byref(local), at["q"], at["k"], at["v"], at["out"], _sized_ptr(lse, torch.float32, n_lse, "lse"),
+        _sized_ptr(out_rest, torch.bfloat16, q.numel(), "out_rest"), _ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
+        _ptr(status, torch.int64, "status"), _stream()), where)
+
+
+def ps_local_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                                q_offsets: torch.Tensor, k_offsets: torch.Tensor, max_q: int, max_k: int, dq: torch.Tensor, dk: torch.Tensor,
+                                dv: torch.Tensor, workspace: torch.Tensor, left: int = -1, right: int = -1, sinks: int = 0,
+                                buckets: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                                dbias: Optional[torch.Tensor] = None, scale: Optional[float] = None, softcap: float = 0.0,
+                                causal: bool = False, k_lengths: Optional[torch.Tensor] = None, q_start: Optional[torch.Tensor] = None,
+                                prefix: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None,
+                                q_docs: Optional[torch.Tensor] = None, k_docs: Optional[torch.Tensor] = None,
+                                status: Optional[torch.Tensor] = None, out_rest: Optional[torch.Tensor] = None) -> None:
+    """Arguments as of ps_local_attention_forward(), which has left `out`, `lse` and `out_rest`; dq like q, dk and dv like k, dbias like bias or
+    None."""
+    if _made("local_attention_backward", q, k, v, out, lse, dout, q_offsets, k_offsets, max_q, max_k, dq, dk, dv, workspace, left, right, sinks,
+             buckets, bias, dbias, scale, softcap, causal, k_lengths, q_start, prefix, slopes, q_docs, k_docs, status, out_rest):
+        return
+    where = "ps_local_attention_backward"
+    d, seqs, at, n_lse = _attention(where, q, k, q_offsets, k_offsets, max_q, max_k, scale, softcap, causal, k_lengths, q_start, prefix, slopes,
+                                    q_docs, k_docs, {"q": (q, False), "k": (k, True), "v": (v, True), "out": (out, False), "dout": (dout, False),
+                                                     "dq": (dq, False), "dk": (dk, True), "dv": (dv, True)})
+    local = _local(where, q.shape[1], left, right, sinks, buckets, bias, dbias)
+    _on_current_device(where, q, k, v, out, lse, dout, q_offsets, k_offsets, dq, dk, dv, workspace, buckets, bias, dbias, k_lengths, q_start, prefix,
+                       slopes, q_docs, k_docs, status, out_rest)
+    _check(load_library().ps_local_attention_backward(
+        ctypes.byref(d), ctypes.byref(seqs), ctypes.byref(local), at["q"], at["k"], at["v"], at["out"], _sized_ptr(lse, torch.float32, n_lse, "lse"),
+        _sized_ptr(out_rest, torch.bfloat16, q.numel(), "out_rest"), at["dout"], at["dq"], at["dk"], at["dv"],
+        None if dbias is None else _sized_ptr(dbias, torch.float32, bias.numel(), "dbias"), _ptr(workspace, torch.uint8, "workspace"),
+        workspace.numel(), _ptr(status, torch.int64, "status"), _stream()), where)
 
 
 def alloc_workspace(nbytes: int, device="cuda") -> torch.Tensor:

@@ -35,10 +35,12 @@ struct Calls {
     decltype(&ps_dropout_backward) dropout_backward;
     decltype(&ps_norm_rotary_forward) norm_rotary_forward;
     decltype(&ps_norm_rotary_backward) norm_rotary_backward;
+    decltype(&ps_local_attention_forward) local_attention_forward;
+    decltype(&ps_local_attention_backward) local_attention_backward;
 } g_calls;
 
 PyObject* bind(PyObject*, PyObject* const* at, Py_ssize_t n) {
-    constexpr int N = 14;
+    constexpr int N = 16;
     void* p[N];
     if (n != N) { PyErr_SetString(PyExc_TypeError, "bind: an address for every call"); return nullptr; }
     for (int i = 0; i < N; ++i) {
@@ -49,7 +51,8 @@ PyObject* bind(PyObject*, PyObject* const* at, Py_ssize_t n) {
                (decltype(&ps_lookahead_update))p[3], (decltype(&ps_scaler_scan))p[4], (decltype(&ps_route))p[5],
                (decltype(&ps_forecast))p[6], (decltype(&ps_attention_forward))p[7], (decltype(&ps_attention_backward))p[8],
                (decltype(&ps_rotary))p[9], (decltype(&ps_dropout_forward))p[10], (decltype(&ps_dropout_backward))p[11],
-               (decltype(&ps_norm_rotary_forward))p[12], (decltype(&ps_norm_rotary_backward))p[13]};
+               (decltype(&ps_norm_rotary_forward))p[12], (decltype(&ps_norm_rotary_backward))p[13],
+               (decltype(&ps_local_attention_forward))p[14], (decltype(&ps_local_attention_backward))p[15]};
     Py_RETURN_NONE;
 }
 
@@ -550,11 +553,67 @@ PyObject* norm_rotary_backward(PyObject*, PyObject* const* at, Py_ssize_t n) {
     }, true);
 }
 
+// at[i] and on: left, right, sinks, buckets, bias
+ps_attention_local local_of(Args& a, int i, int64_t heads) {
+    ps_attention_local l = {};
+    l.left = a.i32(i);
+    l.right = a.i32(i + 1);
+    l.sinks = a.i32(i + 2);
+    int64_t distances = 0, values = 0;
+    l.buckets = a.tensor<int32_t>(i + 3, kI32, &distances, true);
+    l.bias = a.tensor<float>(i + 4, kF32, &values, true);
+    if (!a.good) return l;
+    if ((distances < 0) != (values < 0)) a.good = false;
+    if (distances < 0 || !a.good) return l;
+    const at::Tensor &b = THPVariable_Unpack(a.at[i + 4]), &d = THPVariable_Unpack(a.at[i + 3]);
+    if (b.dim() != 2 || b.size(1) != heads || d.dim() != 1 || distances % 2 == 0) { a.good = false; return l; }
+    l.n_buckets = a.count32(b.size(0));
+    l.reach = a.count32(distances / 2);
+    return l;
+}
+
+PyObject* local_attention_forward(PyObject*, PyObject* const* at, Py_ssize_t n) {
+    return make_call(at, n, 26, [](Args& a) {
+        using D = ps_attention_desc;
+        Attention t;
+        const void* q = t.queries(a, 0, &D::q);
+        const void *k = t.keys(a, 1, &D::k), *v = t.keys(a, 2, &D::v);
+        void* out = t.queries(a, 7, &D::out);
+        float* lse = a.sized<float>(8, kF32, t.q_shape[0] * t.q_shape[1], true);
+        t.others(a, 3, 5, 9, 15);
+        void* rest = t.rest(a, 25);
+        const ps_attention_local l = local_of(a, 10, t.q_shape[1]);
+        return [=](void* s) {
+            return g_calls.local_attention_forward(&t.d, &t.s, &l, q, k, v, out, lse, rest, t.workspace, (size_t)t.ws, t.status, s);
+        };
+    }, true);
+}
+
+PyObject* local_attention_backward(PyObject*, PyObject* const* at, Py_ssize_t n) {
+    return make_call(at, n, 31, [](Args& a) {
+        using D = ps_attention_desc;
+        Attention t;
+        const void* q = t.queries(a, 0, &D::q);
+        const void *k = t.keys(a, 1, &D::k), *v = t.keys(a, 2, &D::v), *out = t.queries(a, 3, &D::out);
+        const float* lse = a.sized<float>(4, kF32, t.q_shape[0] * t.q_shape[1]);
+        const void* dout = t.queries(a, 5, &D::dout);
+        void *dq = t.queries(a, 10, &D::dq), *dk = t.keys(a, 11, &D::dk), *dv = t.keys(a, 12, &D::dv);
+        t.others(a, 6, 8, 13, 20);
+        const void* rest = t.rest(a, 30);
+        const ps_attention_local l = local_of(a, 14, t.q_shape[1]);
+        float* dbias = a.sized<float>(19, kF32, l.bias ? (int64_t)l.n_buckets * t.q_shape[1] : -1, true);
+        return [=](void* s) {
+            return g_calls.local_attention_backward(&t.d, &t.s, &l, q, k, v, out, lse, rest, dout, dq, dk, dv, dbias, t.workspace, (size_t)t.ws, t.status, s);
+        };
+    }, true);
+}
+
 #define PS_METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PS_METHOD(bind), PS_METHOD(predict_load), PS_METHOD(anticipate), PS_METHOD(anticipate_static), PS_METHOD(lookahead_update),
                          PS_METHOD(scaler_scan), PS_METHOD(route), PS_METHOD(forecast),
                          PS_METHOD(attention_forward), PS_METHOD(attention_backward), PS_METHOD(rotary), PS_METHOD(dropout_forward),
-                         PS_METHOD(dropout_backward), PS_METHOD(norm_rotary_forward), PS_METHOD(norm_rotary_backward), {nullptr, nullptr, 0, nullptr}};
+                         PS_METHOD(dropout_backward), PS_METHOD(norm_rotary_forward), PS_METHOD(norm_rotary_backward),
+                         PS_METHOD(local_attention_forward), PS_METHOD(local_attention_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

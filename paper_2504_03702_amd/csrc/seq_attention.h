@@ -53,7 +53,27 @@ struct Args {
     uint32_t by_group;                 // 2^32 / group + 1 (group > 1)
     float scale, cap;
     float slope_by, cap_in;            // see Row and Cap
+    // ps_local_attention_*() alone, whose kernels are the same with LOCAL:
+    int32_t left, right, sinks;        // a row's window, and the first keys that it sees all the same
+    int32_t sink_blocks, sink_parts, sink_part_tiles;   // blocks of keys that have some of those, if they are shared out apart
+    float *sink_dk, *sink_dv;          // [sink_parts][n_seq][sink_blocks * FIXED][kv_heads][head_dim]
+    const float* table;                // [heads][2 reach + 1]: the learned bias of a distance, null without one (see Bias)
+    const int32_t* bucket_words;       // [2 reach + 1]: where in a lane's sums the distance's bucket is
+    float* bias_parts;                 // [parts][blocks of rows][buckets][heads]: sums of a bucket's gradients, null if not wanted
+    int64_t bias_blocks;
+    int32_t reach, n_buckets;
+    int32_t bias_width, bias_words;    // distances that a head has in a tile; words of all heads of a tile, in whole wavefronts
+    uint32_t by_width;                 // 2^32 / bias_width + 1
 };
+
+// The arguments read again where they are used, by what the compiler takes for another address each time: what is wanted once a tile and no more does not wait
+// in scalar registers, of which the gradients' kernels have too few.  (All kernels have them as their first argument.)
+typedef const __attribute__((address_space(4))) Args* ArgsAgain;
+__device__ __forceinline__ ArgsAgain again() {
+    ArgsAgain a = (ArgsAgain)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(a));
+    return a;
+}
 
 struct Seq {
     int q0, qn, k0, kn, start, prefix;
@@ -85,17 +105,52 @@ __device__ __forceinline__ int seen_end(const Args& a, const Seq& q, int place) 
     return a.causal ? min(q.kn, max(min(place, q.kn) + 1, q.prefix)) : q.kn;
 }
 
-// Tiles of keys, from the first on, that some of the FIXED rows from r0 on may see; tiles of rows, from `first` on, that may see some of
-// the FIXED keys from k0 on.  Shares are of these.
-__device__ __forceinline__ int key_tiles(const Args& a, const Seq& q, int r0) {
-    const int far = q.start + (int)over_group(a, min(r0 + FIXED, q.qn * a.group) - 1);
-    return (max(0, seen_end(a, q, far)) + a.tile - 1) / a.tile;
+// With a window, keys from `window_begin` on and in front of `seen_to`, and those in front of a.sinks that are in front of seen_to too.  Both never
+// fall from place to place.  (A window without an end has 2^31 - 1 places.)
+__device__ __forceinline__ int window_begin(const Args& a, int place) { return (int)max((int64_t)0, (int64_t)place - a.left); }
+template <bool LOCAL>
+__device__ __forceinline__ int seen_to(const Args& a, const Seq& q, int place) {
+    const int end = seen_end(a, q, place);
+    return LOCAL ? min(end, max((int)min((int64_t)q.kn, (int64_t)place + a.right + 1), a.sinks)) : end;
 }
+
+// Tiles of keys that some of the FIXED rows from r0 on may see: `tiles` of them, `front` from the first on and the others `skip` further on (without
+// a window there is nothing between).
+struct Span {
+    int tiles, front, skip;
+    template <bool LOCAL>
+    __device__ __forceinline__ int at(int t) const { return LOCAL && t >= front ? t + skip : t; }
+};
+template <bool LOCAL>
+__device__ __forceinline__ Span key_tiles(const Args& a, const Seq& q, int r0) {
+    const int far = q.start + (int)over_group(a, min(r0 + FIXED, q.qn * a.group) - 1);
+    const int end = max(0, seen_to<LOCAL>(a, q, far));
+    Span s = {(end + a.tile - 1) / a.tile, 0, 0};
+    if (LOCAL) {
+        s.front = (min(a.sinks, end) + a.tile - 1) / a.tile;
+        s.skip = max(0, min(window_begin(a, q.start + (int)over_group(a, r0)) / a.tile, s.tiles) - s.front);
+        s.tiles -= s.skip;
+    }
+    return s;
+}
+// Tiles of rows, from `first` on and in front of the returned one, that may see some of the FIXED keys from k0 on.  Shares are of these.
+template <bool LOCAL>
 __device__ __forceinline__ int row_tiles(const Args& a, const Seq& q, int k0, int& first) {
     const int rows = q.qn * a.group, n = (rows + a.key_tile - 1) / a.key_tile;
     first = a.causal && k0 >= q.prefix ? (int)min((int64_t)n, max((int64_t)0, (int64_t)(k0 - q.start) * a.group / a.key_tile)) : 0;
-    return n;
+    if (!LOCAL || k0 < a.sinks) return n;
+    auto tile_of = [&](int64_t place) { return (int)min((int64_t)n, max((int64_t)0, (place - q.start) * a.group / a.key_tile)); };
+    first = max(first, tile_of((int64_t)k0 - a.right));
+    const int64_t behind = (int64_t)min(k0 + FIXED, q.kn) + a.left - q.start;   // the first token that none of them is seen by
+    return max(first, behind >= q.qn ? n : behind <= 0 ? 0 : (int)((behind * a.group + a.key_tile - 1) / a.key_tile));
 }
+// The shares that a block of keys' row tiles may have, and a share's tiles.
+template <bool LOCAL>
+__device__ __forceinline__ bool shared_apart(const Args& a, int block) { return LOCAL && block < a.sink_blocks; }
+template <bool LOCAL>
+__device__ __forceinline__ int key_parts_of(const Args& a, int block) { return shared_apart<LOCAL>(a, block) ? a.sink_parts : a.key_parts; }
+template <bool LOCAL>
+__device__ __forceinline__ int key_part_tiles_of(const Args& a, int block) { return shared_apart<LOCAL>(a, block) ? a.sink_part_tiles : a.key_part_tiles; }
 __device__ __forceinline__ int shares(int tiles, int parts, int part_tiles) { return max(1, min(parts, (tiles + part_tiles - 1) / part_tiles)); }
 
 // A workgroup's part of a launch over blocks of rows (of keys, with KEYS) and shares of their tiles.
@@ -111,26 +166,36 @@ inline int32_t turns(int64_t blocks_a_seq, int32_t seqs) {
 struct Work {
     int s, hk, block, part;
 };
-template <bool KEYS>
+template <bool KEYS, bool LOCAL>
 __device__ __forceinline__ int shares_of(const Args& a, const Seq& q, int block) {
     const int n = KEYS ? q.kn : q.qn * a.group;
     if (block * FIXED >= n) return 0;
-    if ((KEYS ? a.key_parts : a.parts) == 1) return 1;
+    if ((KEYS ? key_parts_of<LOCAL>(a, block) : a.parts) == 1) return 1;
     int first = 0;
-    const int tiles = KEYS ? row_tiles(a, q, block * FIXED, first) : key_tiles(a, q, block * FIXED);
-    return shares(tiles - first, KEYS ? a.key_parts : a.parts, KEYS ? a.key_part_tiles : a.part_tiles);
+    const int tiles = KEYS ? row_tiles<LOCAL>(a, q, block * FIXED, first) : key_tiles<LOCAL>(a, q, block * FIXED).tiles;
+    return shares(tiles - first, KEYS ? key_parts_of<LOCAL>(a, block) : a.parts, KEYS ? key_part_tiles_of<LOCAL>(a, block) : a.part_tiles);
 }
 // a.listed (at most 64 sequences of at most 64 blocks): the grid has a workgroup for what there could be, and the first so many take
 // what there is, found by adding it up a sequence to a lane.  Counted as the grid counts, what there is lay anywhere among it, and
 // three or more long workgroups on one unit beside empty ones (8 sequences of 100 to 1023 tokens, 408 workgroups of 2048 with work to do: 26 to
 // 40 tiles on the fullest units, 10 on average; forwards / queries' / keys' gradients in fp32 with heads of 80 128 / 173 / 293 us, 77 / 104 / 157
 // added up).
-template <bool KEYS>
+template <bool KEYS, bool LOCAL>
 __device__ __forceinline__ bool look_for_work(const Args& a, Seq& q, Work& w) {
     const int blocks = KEYS ? (a.max_k + FIXED - 1) / FIXED : a.row_blocks, parts = KEYS ? a.key_parts : a.parts, lane = threadIdx.x & 63;
     unsigned id = blockIdx.x;
     w.hk = id % a.kv_heads;
     id /= a.kv_heads;
+    if (LOCAL && KEYS && !a.listed && a.sink_blocks > 0) {                // (the longest first: blocks whose rows are shared out apart)
+        const int apart = min(a.sink_blocks, blocks) * a.sink_parts;
+        const unsigned jobs = apart + max(0, blocks - a.sink_blocks) * parts;
+        const unsigned first = id / (jobs * a.together) * a.together, rest = id - first * jobs, here = min((unsigned)a.together, a.seqs - first);
+        const int job = rest / here;
+        w.s = a.seq0 + first + rest % here;
+        w.block = job < apart ? job / a.sink_parts : a.sink_blocks + (job - apart) / parts;
+        w.part = job < apart ? job % a.sink_parts : (job - apart) % parts;
+        return sequence(a, w.s, q) && w.block * FIXED < q.kn;
+    }
     if (!a.listed) {
         w.part = id % parts;
         id /= parts;
@@ -160,7 +225,7 @@ __device__ __forceinline__ bool look_for_work(const Args& a, Seq& q, Work& w) {
     int n = 0, upto;
     if (good)
         for (int b = 0; b < blocks; ++b) {
-            const int c = shares_of<KEYS>(a, mine, b);
+            const int c = shares_of<KEYS, LOCAL>(a, mine, b);
             if (c == 0) break;
             n += c;
         }
@@ -170,16 +235,16 @@ __device__ __forceinline__ bool look_for_work(const Args& a, Seq& q, Work& w) {
     w.s = a.seq0 + s;
     sequence(a, w.s, q);
     const int own = ((KEYS ? q.kn : q.qn * a.group) + FIXED - 1) / FIXED, b = KEYS ? lane : own - 1 - lane;   // (most work first)
-    const int in_front = sum_in_front(b >= 0 ? shares_of<KEYS>(a, q, b) : 0, upto), at = __popcll(__ballot(upto <= (int)id));
+    const int in_front = sum_in_front(b >= 0 ? shares_of<KEYS, LOCAL>(a, q, b) : 0, upto), at = __popcll(__ballot(upto <= (int)id));
     w.block = KEYS ? at : own - 1 - at;
     w.part = (int)id - __builtin_amdgcn_readlane(in_front, at);
     return true;
 }
 
 // The same, as scalars: the compiler does not see that all lanes have found the same.
-template <bool KEYS>
+template <bool KEYS, bool LOCAL>
 __device__ __forceinline__ bool find_work(const Args& a, Seq& q, Work& w) {
-    if (!look_for_work<KEYS>(a, q, w)) return false;
+    if (!look_for_work<KEYS, LOCAL>(a, q, w)) return false;
     int* const x[] = {&q.q0, &q.qn, &q.k0, &q.kn, &q.start, &q.prefix, &w.s, &w.hk, &w.block, &w.part};
 #pragma unroll
     for (int i = 0; i < 10; ++i) *x[i] = __builtin_amdgcn_readfirstlane(*x[i]);
@@ -545,6 +610,34 @@ struct Cap {
     }
 };
 
+// ---- a learned bias -----------------------------------------------------------------------------------------------------------
+// The bias of a distance d = key - place, clamped to -reach .. reach, is table[head][reach + d], made from buckets and values by a launch in
+// front.  A tile meets few of them, and as they are the same along its diagonals a stretch of bias_width for each head will do: it comes by DMA with the tile,
+// head g's words at g bias_width, of distances from `lowest` on.
+struct Bias {
+    static __device__ __forceinline__ void send(int hk, int lowest, float* to) {
+        const ArgsAgain a = again();
+        const int lane = anew<256>((int)threadIdx.x) & 63, words = a->bias_words, width = a->bias_width, group = a->group, reach = a->reach;
+        for (int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64; w < words; w += 256) {
+            const int g = min((int)__umulhi((unsigned)(w + lane), a->by_width), group - 1), d = lowest + min(w + lane - g * width, width - 1);
+            const float* from = a->table + (int64_t)(hk * group + g) * (2 * reach + 1) + reach + max(-reach, min(d, reach));
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)(to + w), 4, 0, 0);
+        }
+    }
+    // the same distances' places in a lane's sums of buckets
+    static __device__ __forceinline__ void send_buckets(int lowest, int* to) {
+        const ArgsAgain a = again();
+        const int lane = anew<256>((int)threadIdx.x) & 63, width = a->bias_width, reach = a->reach;
+        for (int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64; w < width; w += 256) {
+            const int d = lowest + min(w + lane, width - 1);
+            const int32_t* from = a->bucket_words + reach + max(-reach, min(d, reach));
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)(to + w), 4, 0, 0);
+        }
+    }
+    // (places as far from all keys as any: distances stay in 32 bits)
+    static __device__ __forceinline__ int place(int place) { return max(place, -(1 << 29)); }
+};
+
 // Row of accumulator element e.
 __device__ __forceinline__ constexpr int row_of(int e) { return 8 * (e >> 2) + (e & 3); }   // + 4 half
 
@@ -592,12 +685,15 @@ __device__ __forceinline__ void put_rows(unsigned char* mine, const f32x16 (&acc
     }
 }
 
-// Checked arguments as the kernels take them, and the plan of a call; PS_OK or an error.
+// Checked arguments as the kernels take them, and the plan of a call; PS_OK or an error.  ahead: rows may see keys behind their place.
 struct Plan {
     Args a;
     size_t bytes;                      // of workspace
 };
-int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, void* workspace, Plan& p);
+int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attention_local* local, bool backward, void* workspace, Plan& p, bool ahead);
+inline bool sees_ahead(const ps_attention_desc* d, const ps_attention_seqs* s) { return d && (!d->causal || s->prefix); }
+void set_width(Args& a, int width);
+void make_table(const Args& a, const ps_attention_local* local, float by, hipStream_t st);
 int check_strides(const ps_attention_desc* d, const ps_strides& s, const void* base, int64_t rows, int64_t heads, bool written);
 int check_sequences(const Args& a, hipStream_t st);
 void summarise_documents(const Args& a, hipStream_t st);

@@ -20,9 +20,17 @@ namespace {
 // queries' / keys' gradients 499 / 860 -> 589 / 977 us, error against 64 bits 2.7e-3 -> 2.1e-3 of the norm (1.7e-3 is that of dq's and dk's
 // own rounding; 2.3e-3 without cap, where a product more would cost 5 to 10 %).  (Documents in two rows of 8192, where blocks are cut: 130 / 146
 // -> 144 / 160.)
-template <typename T, int STEP, typename Lse, typename Delta, typename Distance, typename Front, typename Same>
+// LOCAL: bias(j), the learned bias, in powers of two, if there is one; late and windowed(j, is), which keys are in the window, as with `cut`; sums(j, e)
+// takes the gradients of the scores themselves, if they are wanted (that of x has the cap's slope too).
+struct Nothing {
+    __device__ __forceinline__ float4 operator()(int) const { return make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void operator()(int, bool (&)[4]) const {}
+    __device__ __forceinline__ void operator()(int, const float (&)[4]) const {}
+};
+template <typename T, int STEP, bool LOCAL, bool BIASED, typename Lse, typename Delta, typename Distance, typename Front, typename Same, typename Learned, typename Windowed, typename Sums>
 __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, Weights<T>& p, Weights<T>& d, Weights<T>& rest,
-                                          bool cut, bool docs, Lse lse, Delta delta, Distance distance, Front in_front, Same same) {
+                                          bool cut, bool docs, bool late, bool summed, Lse lse, Delta delta, Distance distance, Front in_front, Same same,
+                                          Learned bias, Windowed windowed, Sums sums) {
     const Cap cap = Cap::of<T>(a);
     const float c1 = a.scale * LOG2E;
 #pragma unroll
@@ -35,6 +43,13 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
             for (int k = 0; k < STEP; ++k) {
                 const float4 off = distance(j0 + k);
                 u[k] = make_float4(u[k].x + off.x, u[k].y + off.y, u[k].z + off.z, u[k].w + off.w);
+            }
+        }
+        if (BIASED) {
+#pragma unroll
+            for (int k = 0; k < STEP; ++k) {
+                const float4 off = bias(j0 + k);
+                u[k] = make_float4(u[k].x - off.x, u[k].y - off.y, u[k].z - off.z, u[k].w - off.w);
             }
         }
         if (a.cap > 0.f) {
@@ -79,13 +94,24 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
         };
         if (cut) only(in_front);
         if (docs) only(same);
+        if (LOCAL && late) only(windowed);
+        if (BIASED && summed) {
+#pragma unroll
+            for (int k = 0; k < STEP; ++k) {
+                const float4 t = delta(j0 + k);
+                float e[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = (&u[k].x)[i] * (g[4 * (j0 + k) + i] - (&t.x)[i]);
+                sums(j0 + k, e);
+            }
+        }
 #pragma unroll
         for (int k = 0; k < STEP; ++k) {
             p.set(j0 + k, u[k]);
             d.set(j0 + k, v[k]);
         }
         if constexpr (sizeof(T) == 2)
-            if (cut || docs || a.cap > 0.f) {
+            if (cut || docs || (LOCAL && late) || a.cap > 0.f) {
 #pragma unroll
                 for (int k = 0; k < STEP; ++k) {
                     const float4 r = d.get(j0 + k);
@@ -104,26 +130,29 @@ __device__ __forceinline__ float by_x(const Args& a) { return a.cap > 0.f && siz
 // SIMD at barriers and waits 36 % of theirs; documents in two rows of 8192, heads of 64: 166 us, 0.44 PFLOP/s, 33 %, 22 %, 1.6 wavefronts, 40 %.
 // Where the heads of a key head are no divisor of a tile's rows, addresses are worked out a row at a time, which costs some 15 % (8 causal sequences
 // of 1500 to 2048, 4 key heads of 64, this launch with 2, 3, 4, 5 heads to each: 119, 182, 198, 282 us).
-template <typename T, int DP>
+template <typename T, int DP, bool LOCAL, bool BIASED>
 __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_gradients_kernel(Args a) {
     using L = Tile<T, DP, key_tile_rows(sizeof(T), DP)>;
     // Two workgroups a unit need 256 registers a lane.  In bf16 the gradients of 32 keys by 128 features take half of them, so the values
     // wait in LDS (a quarter more reads there).
-    constexpr bool IN_LDS = sizeof(T) == 2 && DP == 128;
+    // (LOCAL: above 64 features, there is more to keep)
+    constexpr bool IN_LDS = sizeof(T) == 2 && DP > (LOCAL ? 64 : 96), NEEDS_IN_LDS = sizeof(T) == 2 && DP == 128;
     __shared__ __align__(1024) unsigned char s_values[IN_LDS ? 4 : 1][IN_LDS ? 32 * L::ROWB : 16];
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][queries, dout]
     __shared__ __align__(16) float s_lse[2][64], s_delta[2][64], s_slope[2][64], s_place[2][64];   // (places from k0 on)
     __shared__ __align__(16) int s_doc[2][64];
+    __shared__ __align__(16) int s_at[LOCAL ? 2 : 1][LOCAL ? 64 : 4], s_bias_at[BIASED ? 2 : 1][BIASED ? 64 : 4];   // rows' places from k0 on; their words of the bias
+    extern __shared__ __align__(16) float s_bias[];                       // [buffer][a.bias_words]
 
     Seq q;
     Work w;
-    if (!find_work<true>(a, q, w)) return;                                // (faulty sequences: reported by the queries' launch)
+    if (!find_work<true, LOCAL>(a, q, w)) return;                                // (faulty sequences: reported by the queries' launch)
     const int hk = w.hk, s = w.s, part = w.part, k0 = w.block * FIXED;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int rows = q.qn * a.group;
     int first_tile;
-    const int tiles = row_tiles(a, q, k0, first_tile);
-    const int t0 = first_tile + part * a.key_part_tiles, t1 = min(tiles, t0 + a.key_part_tiles);
+    const int tiles = row_tiles<LOCAL>(a, q, k0, first_tile), each = key_part_tiles_of<LOCAL>(a, w.block);
+    const int t0 = first_tile + part * each, t1 = min(tiles, t0 + each);
     if (part > 0 && t0 >= tiles) return;                                  // (part 0 writes, rows or not)
 
     // this lane's key
@@ -144,7 +173,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     };
     const auto vf = keep();
 
-    const float keyf = (float)(32 * wave + col), seen_from = !a.causal || key < q.prefix ? -INFINITY : keyf;   // places from k0 on
+    const float own_keyf = (float)(32 * wave + col), own_seen_from = !a.causal || key < q.prefix ? -INFINITY : own_keyf;   // places from k0 on
     const int last = min(k0 + FIXED, q.kn) - 1, wlast = min(wk0 + 31, q.kn - 1);
     int dmin = 0, dmax = 0;
     if (a.k_docs) {
@@ -160,7 +189,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     const int64_t qblock0 = doc_block0(q.q0, s);
     auto classify = [&](int t, bool& one, bool& pad) {
         const int first = (int)over_group(a, t * L::ROWS), end = (int)over_group(a, min(t * L::ROWS + L::ROWS, rows) - 1);
-        bool some = !a.causal || k0 <= q.start + end || k0 < q.prefix;
+        bool some = LOCAL || !a.causal || k0 <= q.start + end || k0 < q.prefix;
         one = !a.q_docs;
         if (a.q_docs && !a.q_blocks) {
             pad = true;
@@ -199,9 +228,19 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         needs.g[j] = gradients_out.off[j];
     }
     needs.word = (const int32_t*)word(q.q0 + lane_token, lane_head);
-    __shared__ Needs s_needs[IN_LDS ? 256 : 1];
-    if (IN_LDS) s_needs[threadIdx.x] = needs;
-    auto fetch = [&]() -> Needs { return IN_LDS ? s_needs[threadIdx.x] : needs; };
+    __shared__ Needs s_needs[NEEDS_IN_LDS ? 256 : 1];
+    if (NEEDS_IN_LDS) s_needs[threadIdx.x] = needs;
+    auto fetch = [&]() -> Needs { return NEEDS_IN_LDS ? s_needs[threadIdx.x] : needs; };
+    // A learned bias: a lane's row's words for the keys from k0 on, if its token is the qi-th and the tile's last row's the last-th.
+    auto places = [&](int buf, int qi, int head, int last) {
+        if (!LOCAL) return;
+        if (wave == 0) s_at[buf][lane] = q.start - k0 + qi;
+        if (BIASED) {
+            const int place = Bias::place(q.start + qi), far = Bias::place(q.start + last);
+            if (wave == 0) s_bias_at[buf][lane] = (head - hk * a.group) * a.bias_width + far - place;
+            Bias::send(hk, k0 - far, s_bias + buf * a.bias_words);
+        }
+    };
     auto request = [&](int t, bool padded, int buf) {
         const int r0 = t * L::ROWS;
         if (regular && r0 + L::ROWS <= rows && !padded) {
@@ -211,6 +250,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
             Sender<T, DP, L::ROWS>::whole(smem[buf][1], gbase + token * a.gs.row, mine.g);
             if (has_words) send_words(words + 64 * buf, mine.word + (int64_t)t * word_step);
             if (wave == 0) s_place[buf][lane] = (float)(q.start - k0 + (int)token + (int)over_group(a, lane % L::ROWS));
+            places(buf, (int)token + lane_token, lane_head, (int)token + (L::ROWS - 1) / a.group);
             return;
         }
         // (padding and rows past the end are zeros that see nothing)
@@ -225,6 +265,9 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         const void* none = wave == 0 ? (const void*)&infinity_word : wave == 3 ? (const void*)&minus_one : (const void*)&zeros;
         if (has_words) send_words(words + 64 * buf, r0 + lane < rows ? word(q.q0 + qi, hk * a.group + r - qi * a.group) : none);
         if (wave == 0) s_place[buf][lane] = (float)(q.start - k0 + qi);
+        // (of 64 lanes only those of the tile's rows have words in it)
+        const int of_tile = min(r0 + lane % L::ROWS, rows - 1), token = (int)over_group(a, of_tile);
+        places(buf, token, hk * a.group + of_tile - token * a.group, (int)over_group(a, min(r0 + L::ROWS, rows) - 1));
     };
 
     f32x16 dk[L::NA], dv[L::NA];
@@ -239,26 +282,41 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     while (t < t1) {
         const bool docs = !walk.is_one(t), cut = a.causal && wlast > q.start + (int)over_group(a, t * L::ROWS) && wlast >= q.prefix;
         const int far = q.start + (int)over_group(a, min(t * L::ROWS + L::ROWS, rows) - 1);
+        // whether some of the wavefront's keys are not in some rows' windows, and none in any's (64 bits: a window may end beyond 32)
+        bool late = false, none = false;
+        if (LOCAL) {
+            const ArgsAgain w = again();
+            const int64_t left = w->left, right = w->right;
+            const int near = q.start + (int)over_group(a, t * L::ROWS), sinks = w->sinks;
+            late = wlast >= sinks && (near + right < wlast || far - left > max(wk0, sinks));
+            none = wk0 >= sinks && (far + right < wk0 || near - left > wlast);
+        }
         t = walk.next(t + 1, t1, classify);
         vm_wait();
         __syncthreads();                                                  // the tile has landed, the one before it is no longer read
         if (t < t1) request(t, walk.is_padded(t), buf ^ 1);
-        if (wk0 < q.kn && !(a.causal && wk0 > far && wk0 >= q.prefix)) {
+        if (wk0 < q.kn && !(a.causal && wk0 > far && wk0 >= q.prefix) && !none) {
 #pragma unroll 1
             for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
                 f32x16 sc, g;
                 dots<T, DP>(smem[buf][0], b, kf, sc, smem[buf][1], b, vf, g, lanes);
                 Weights<T> p, d, rest;
                 auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
-                gradients<T, (DP > 64 ? 1 : 4)>(a, sc, g, p, d, rest, cut, docs, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
+                gradients<T, (DP > 64 ? 1 : 4), LOCAL, BIASED>(a, sc, g, p, d, rest, cut, docs, late, false, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
                              [&](int j) { return *(const float4*)&s_delta[buf][at(j)]; },
                              [&](int j) {
                                  const float4 by = *(const float4*)&s_slope[buf][at(j)], place = *(const float4*)&s_place[buf][at(j)];
+                                 const float keyf = LOCAL ? (float)(32 * wave + (anew<256>((int)threadIdx.x) & 31)) : own_keyf;
                                  return make_float4(by.x * LOG2E * fabsf(place.x - keyf), by.y * LOG2E * fabsf(place.y - keyf),
                                                     by.z * LOG2E * fabsf(place.z - keyf), by.w * LOG2E * fabsf(place.w - keyf));
                              },
                              [&](int j, bool(&is)[4]) {
                                  const float4 place = *(const float4*)&s_place[buf][at(j)];
+                                 float seen_from = own_seen_from;
+                                 if (LOCAL) {                             // (worked out again: registers)
+                                     const int own = 32 * wave + (anew<256>((int)threadIdx.x) & 31);
+                                     seen_from = k0 + own < q.prefix ? -INFINITY : (float)own;
+                                 }
 #pragma unroll
                                  for (int i = 0; i < 4; ++i) is[i] = seen_from <= (&place.x)[i];
                              },
@@ -267,10 +325,26 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
                                  const int4 of = *(const int4*)&s_doc[buf][at(j)];
 #pragma unroll
                                  for (int i = 0; i < 4; ++i) is[i] = (&of.x)[i] == doc;
-                             });
+                             },
+                             [&](int j) {
+                                 const int4 of = *(const int4*)&s_bias_at[buf][at(j)];
+                                 const float* own = s_bias + buf * a.bias_words + 32 * wave + (anew<256>((int)threadIdx.x) & 31);
+                                 return make_float4(own[of.x], own[of.y], own[of.z], own[of.w]);
+                             },
+                             [&](int j, bool(&is)[4]) {
+                                 // (worked out again: few tiles are cut by a window.  Distances are 33 bits at most, a window without end 31)
+                                 const int own = 32 * wave + (anew<256>((int)threadIdx.x) & 31);
+                                 const int4 place = *(const int4*)&s_at[buf][at(j)];
+#pragma unroll
+                                 for (int i = 0; i < 4; ++i) {
+                                     const int off = (&place.x)[i] - own;   // (a row's place less the key's)
+                                     is[i] = (off <= a.left && off >= -a.right) || k0 + own < a.sinks;
+                                 }
+                             },
+                             Nothing());
                 weigh<T, DP>(smem[buf][1], b, p, dv, lanes);
                 weigh<T, DP>(smem[buf][0], b, d, dk, lanes);
-                if (sizeof(T) == 2 && (cut || docs || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dk, lanes);
+                if (sizeof(T) == 2 && (cut || docs || late || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dk, lanes);
             }
         }
         buf ^= 1;
@@ -282,7 +356,14 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     const int own = wk0 + (anew<256>((int)threadIdx.x) & 31);              // (the key, worked out again)
     const bool is = own < q.kn;
     const int64_t to = q.k0 + own;
-    if (a.key_parts > 1) {
+    if (shared_apart<LOCAL>(a, w.block)) {
+        if (a.sink_parts > 1) {
+            const int64_t at = ((((int64_t)part * a.n_seq + s) * a.sink_blocks * FIXED + own) * a.kv_heads + hk) * a.head_dim;
+            put_rows<float, DP>(mine, dk, 1.f, a.head_dim, is ? a.sink_dk + at : nullptr);
+            put_rows<float, DP>(mine, dv, 1.f, a.head_dim, is ? a.sink_dv + at : nullptr);
+            return;
+        }
+    } else if (a.key_parts > 1) {
         const int64_t at = (((int64_t)part * a.n_k + to) * a.kv_heads + hk) * a.head_dim;
         put_rows<float, DP>(mine, dk, 1.f, a.head_dim, is ? a.part_dk + at : nullptr);
         put_rows<float, DP>(mine, dv, 1.f, a.head_dim, is ? a.part_dv + at : nullptr);
@@ -295,18 +376,22 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
 // Queries fixed: dq of FIXED rows of a key head's queries.  Three products a tile (a fourth for the rest).  Bound by waits too: 16 x 2048 with
 // prefix and cap, heads of 128, 586 us, 0.59 PFLOP/s, vector units issuing 48 % and matrix units busy 34 % of the time, 1.7 wavefronts a SIMD
 // waiting 22 % of theirs; documents in two rows of 8192, heads of 64: 147 us, 0.37 PFLOP/s, 33 %, 19 %, 1.5 wavefronts, 40 %.
-template <typename T, int DP>
+template <typename T, int DP, bool LOCAL, bool BIASED>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_gradients_kernel(Args a) {
     using L = Tile<T, DP>;
+    // LOCAL with a bias: [buffer][a.bias_words], then, if its gradient is wanted, [buffer][bias_width, in whole wavefronts] places in a lane's sums, and
+    // [wavefront][buckets, and one for distances without][lane] sums
+    extern __shared__ __align__(16) float s_bias[];
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][keys, values]
     __shared__ __align__(16) int s_doc[2][64];
 
     Seq q;
     Work w;
-    if (!find_work<false>(a, q, w)) return;
+    if (!find_work<false, LOCAL>(a, q, w)) return;
     const int hk = w.hk, s = w.s, part = w.part, rows = q.qn * a.group, r0 = w.block * FIXED;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-    const int tiles = key_tiles(a, q, r0);
+    const Span span = key_tiles<LOCAL>(a, q, r0);
+    const int tiles = span.tiles;
     const int t0 = part * a.part_tiles, t1 = min(tiles, t0 + a.part_tiles);
     if (t0 > 0 && t0 >= tiles) return;                                    // (part 0 writes, keys or not)
 
@@ -343,7 +428,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     }
 
     // keys in front of `end` are seen, if their documents are
-    const int end = seen_end(a, q, place);
+    const int end = seen_to<LOCAL>(a, q, place);
     const int last = min(r0 + FIXED, rows) - 1;
     const int far = q.start + (int)over_group(a, last);
     const int wfar = q.start + (int)over_group(a, min(wr0 + 31, rows - 1)), wnear = q.start + (int)over_group(a, min(wr0, rows - 1));
@@ -360,8 +445,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     }
     const int64_t kblock0 = doc_block0(q.k0, s);
     auto classify = [&](int t, bool& one, bool& pad) {
-        const int k0 = t * L::ROWS;
-        bool some = !a.causal || k0 <= far || k0 < q.prefix;
+        const int k0 = span.at<LOCAL>(t) * L::ROWS;
+        bool some = LOCAL || !a.causal || k0 <= far || k0 < q.prefix;
         one = !a.k_docs;
         if (a.k_docs && !a.k_blocks) {
             pad = true;
@@ -378,8 +463,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
     const Sender<T, DP, L::ROWS, true> keys(a.ks, 1, a.head_dim), values(a.vs, 1, a.head_dim);
     const bool regular = keys.regular && values.regular;
+    const int wend = LOCAL ? seen_to<LOCAL>(a, q, wnear) : 0, wbegin = LOCAL ? window_begin(a, wfar) : 0;   // the first to end, the last to begin
+    const int wend_far = LOCAL ? seen_to<LOCAL>(a, q, wfar) : 0, wbegin_near = LOCAL ? window_begin(a, wnear) : 0;
+    const int bias_place = Bias::place(far), bias_from = BIASED ? (head - hk * a.group) * a.bias_width + bias_place - Bias::place(place) : 0;
+    const int widths = (a.bias_width + 63) & ~63, sums_a_wave = (a.n_buckets + 1) * 64;
+    int* const s_bucket = (int*)(s_bias + 2 * a.bias_words);
+    float* const s_sums = (float*)(s_bucket + 2 * widths);
+    const bool summed = BIASED && a.bias_parts != nullptr;
+    if (summed)
+        for (int i = threadIdx.x; i < 4 * sums_a_wave; i += 256) s_sums[i] = 0.f;   // (the first tile's barrier is behind this)
     auto request = [&](int t, bool padded, int buf) {
-        const int k0 = t * L::ROWS;
+        const int k0 = span.at<LOCAL>(t) * L::ROWS;
         if (k0 + L::ROWS <= q.kn && !padded && regular) {
             keys.whole(smem[buf][0], kbase + k0 * a.ks.row);
             values.whole(smem[buf][1], vbase + k0 * a.vs.row);
@@ -389,6 +483,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
             values.rows(smem[buf][1], a.head_dim, there, [&](int i) { return vbase + (k0 + i) * a.vs.row; });
         }
         if (a.k_docs && wave == 0) send_words(s_doc[buf], a.k_docs + q.k0 + min(k0 + lane, q.kn - 1));
+        if (BIASED) {
+            Bias::send(hk, k0 - bias_place, s_bias + buf * a.bias_words);
+            if (summed) Bias::send_buckets(k0 - bias_place, s_bucket + buf * widths);
+        }
     };
 
     f32x16 dq[L::NA];
@@ -402,14 +500,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     if (t < t1) request(t, walk.is_padded(t), 0);
     while (t < t1) {
         const bool docs = !walk.is_one(t);
-        const int k0 = t * L::ROWS;
-        const bool cut = k0 + L::ROWS > q.kn || (a.causal && k0 + L::ROWS - 1 > wnear && k0 + L::ROWS > q.prefix);
+        const int k0 = span.at<LOCAL>(t) * L::ROWS;
+        const bool cut = LOCAL ? k0 + L::ROWS > wend : k0 + L::ROWS > q.kn || (a.causal && k0 + L::ROWS - 1 > wnear && k0 + L::ROWS > q.prefix);
+        const bool late = LOCAL && k0 < wbegin && k0 + L::ROWS > a.sinks;
+        const bool none = LOCAL ? k0 >= wend_far || (k0 + L::ROWS <= wbegin_near && k0 >= a.sinks) : a.causal && k0 > wfar && k0 >= q.prefix;
         const float from = (float)(place - k0 - 4 * half);
         t = walk.next(t + 1, t1, classify);
         vm_wait();
         __syncthreads();                                                  // the tile has landed, the one before it is no longer read
         if (t < t1) request(t, walk.is_padded(t), buf ^ 1);
-        if (wr0 < rows && !(a.causal && k0 > wfar && k0 >= q.prefix)) {
+        if (wr0 < rows && !none) {
 #pragma unroll 1
             for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
                 f32x16 sc, g;
@@ -418,7 +518,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
                 auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
                 const int left = end - k0 - 32 * b - 4 * half;
                 const float off = from - (float)(32 * b);
-                gradients<T, 4>(a, sc, g, p, d, rest, cut, docs, [&](int) { return make_float4(lse, lse, lse, lse); },
+                // keys behind the first ones that are in front of the window (late tiles alone: the places are near enough to the window's length)
+                const unsigned hidden = LOCAL ? max(place - a.left - a.sinks, 0) : 0;
+                gradients<T, (BIASED && DP > 96 ? 1 : 4), LOCAL, BIASED>(a, sc, g, p, d, rest, cut, docs, late, summed, [&](int) { return make_float4(lse, lse, lse, lse); },
                              [&](int) { return make_float4(delta, delta, delta, delta); },
                              [&](int j) {
                                  return make_float4(slope * fabsf(off - (float)(8 * j)), slope * fabsf(off - (float)(8 * j + 1)),
@@ -433,14 +535,42 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
                                  const int4 of = *(const int4*)&s_doc[buf][at(j)];
 #pragma unroll
                                  for (int i = 0; i < 4; ++i) is[i] = (&of.x)[i] == doc;
+                             },
+                             [&](int j) {
+                                 const float* own = s_bias + buf * a.bias_words + bias_from + at(j);
+                                 return make_float4(own[0], own[1], own[2], own[3]);
+                             },
+                             [&](int j, bool(&is)[4]) {
+#pragma unroll
+                                 for (int i = 0; i < 4; ++i) is[i] = (unsigned)(k0 + at(j) + i - a.sinks) >= hidden;
+                             },
+                             [&](int j, const float(&e)[4]) {
+                                 const int* of = s_bucket + buf * widths + bias_place - Bias::place(place) + at(j);
+                                 float* mine = s_sums + wave * sums_a_wave + (anew<256>((int)threadIdx.x) & 63);
+#pragma unroll
+                                 for (int i = 0; i < 4; ++i) __hip_atomic_fetch_add(mine + of[i], e[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                              });
                 weigh<T, DP>(smem[buf][0], b, d, dq, lanes);
-                if (sizeof(T) == 2 && (cut || docs || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dq, lanes);
+                if (sizeof(T) == 2 && (cut || docs || late || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dq, lanes);
             }
         }
         buf ^= 1;
     }
     __syncthreads();                                                      // (tiles are no longer read)
+    if (summed) {
+        // a bucket's sums of a head's lanes added up, a thread each, the four wavefronts' rows one after the other
+        float* const to = a.bias_parts + ((int64_t)part * a.bias_blocks + (int64_t)q.q0 * a.group / FIXED + s + w.block) * a.n_buckets * a.heads;
+        for (int i = threadIdx.x; i < a.n_buckets * a.group; i += 256) {
+            const int b = i / a.group, h = i - b * a.group;
+            float sum = 0.f;
+            // (row r0 + x has head (r0 + x) % group; both halves of a wavefront have its rows)
+            for (int x = (h + a.group - r0 % a.group) % a.group; x < FIXED; x += a.group) {
+                const float* of = s_sums + (x >> 5) * sums_a_wave + b * 64 + (x & 31);
+                sum += of[0] + of[32];
+            }
+            to[b * a.heads + hk * a.group + h] = sum;
+        }
+    }
     if (wr0 >= rows) return;
     unsigned char* const mine = smem[0][0] + wave * PUT_BYTES;
     static_assert(sizeof(smem) >= 4 * PUT_BYTES, "rows on their way out");
@@ -453,7 +583,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
 
 // A gradient's shares added up, a thread four neighbours: those of queries (z = 0), keys (1) and values (2).  3365 tokens, 8 heads of 80 on 4,
 // up to 4 shares: 61 MB in 18 us.
-template <typename T>
+template <typename T, bool LOCAL>
 __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
     const int z = z0 + (int)blockIdx.z, s = a.seq0 + (int)blockIdx.y;
     Seq q;
@@ -468,8 +598,9 @@ __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
     const float by = z == 2 ? 1.f : by_x<T>(a);
     for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
         const int row = i / fours, mine = row / heads, head = row % heads;
+        if (LOCAL && z > 0 && mine < a.sink_blocks * FIXED) continue;     // (shared out apart, added up apart)
         int first = 0;
-        const int tiles = z == 0 ? key_tiles(a, q, (mine * a.group + head % a.group) / FIXED * FIXED) : row_tiles(a, q, mine / FIXED * FIXED, first);
+        const int tiles = z == 0 ? key_tiles<LOCAL>(a, q, (mine * a.group + head % a.group) / FIXED * FIXED).tiles : row_tiles<LOCAL>(a, q, mine / FIXED * FIXED, first);
         const int parts = shares(tiles - first, of, each);
         float4 sum = part[i];
 #pragma unroll 4
@@ -485,7 +616,59 @@ __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
     }
 }
 
-template <typename T, int DP>
+// The same of the first keys' gradients, dk (z = 0) and dv (1).
+template <typename T>
+__global__ __launch_bounds__(256) void add_sinks_kernel(Args a) {
+    const int z = blockIdx.z, s = a.seq0 + (int)blockIdx.y;
+    Seq q;
+    if (!sequence(a, s, q)) return;
+    const int fours = a.head_dim / 4, a_key = a.kv_heads * fours, keys = a.sink_blocks * FIXED;
+    const int64_t n = (int64_t)min(q.kn, keys) * a_key, step = (int64_t)a.n_seq * keys * a_key;
+    const float4* part = (const float4*)(z == 0 ? a.sink_dk : a.sink_dv) + (int64_t)s * keys * a_key;
+    const ps_strides to = z == 0 ? a.dks : a.dvs;
+    T* out = (T*)(z == 0 ? a.dk : a.dv);
+    const float by = z == 1 ? 1.f : by_x<T>(a);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int key = (int)(i / a_key), in_key = (int)(i - (int64_t)key * a_key), head = in_key / fours;
+        int first = 0;
+        const int tiles = row_tiles<true>(a, q, key / FIXED * FIXED, first), parts = shares(tiles - first, a.sink_parts, a.sink_part_tiles);
+        float4 sum = part[i];
+#pragma unroll 4
+        for (int p = 1; p < parts; ++p) {
+            const float4 v = part[p * step + i];
+            sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+        }
+        T* at = out + (int64_t)(q.k0 + key) * to.row + head * to.head + (in_key - head * fours) * 4;
+        if constexpr (sizeof(T) == 2)
+            *(uint2*)at = make_uint2(cvt_pk_bf16(sum.x * by, sum.y * by), cvt_pk_bf16(sum.z * by, sum.w * by));
+        else
+            *(float4*)at = make_float4(sum.x * by, sum.y * by, sum.z * by, sum.w * by);
+    }
+}
+
+// A learned bias's gradient from the sums of blocks of rows: 64 values a workgroup, four threads to each, a fourth of the blocks each.  Blocks are counted
+// over all of the tensor's rows, so that some belong to no sequence: those are left out.
+__global__ __launch_bounds__(256) void add_bias_kernel(Args a, float* dbias) {
+    __shared__ float s_sum[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n_buckets * a.heads, i = blockIdx.x * 64 + lane;
+    float sum = 0.f;
+    for (int s = 0; s < a.n_seq; ++s) {
+        Seq q;
+        if (!sequence(a, s, q)) continue;
+        const int blocks = (q.qn * a.group + FIXED - 1) / FIXED;
+        const float* from = a.bias_parts + ((int64_t)q.q0 * a.group / FIXED + s) * n + i;
+        for (int b = wave; b < blocks; b += 4) {
+            const int parts = shares_of<false, true>(a, q, b);
+            for (int p = 0; p < parts; ++p)
+                if (i < n) sum += from[((int64_t)p * a.bias_blocks + b) * n];
+        }
+    }
+    s_sum[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && i < n) dbias[i] = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
+}
+
+template <typename T, int DP, bool LOCAL, bool BIASED>
 void launch(const Args& a, hipStream_t st) {
     Args b = a;
     auto in_turn = [&](int64_t per_seq, int64_t most_seqs, auto launch_one) {
@@ -500,35 +683,65 @@ void launch(const Args& a, hipStream_t st) {
         }
     };
     const int64_t row_jobs = (int64_t)a.kv_heads * a.row_blocks * a.parts;
-    const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED, key_jobs = a.kv_heads * key_blocks * a.key_parts;
+    const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED, apart = min(key_blocks, (int64_t)a.sink_blocks);
+    const int64_t key_jobs = a.kv_heads * (apart * a.sink_parts + (key_blocks - apart) * a.key_parts);
+    const unsigned tile_lds = BIASED ? 2 * a.bias_words * sizeof(float) : 0;
+    const unsigned sums_lds = a.bias_parts ? (2 * ((a.bias_width + 63) & ~63) + 4 * (a.n_buckets + 1) * 64) * sizeof(float) : 0;
+    if (BIASED && tile_lds + sums_lds > 32 << 10) {
+        static bool lds_attr_set = false;     // raising the limit twice is harmless, so no lock
+        if (!lds_attr_set && hipFuncSetAttribute((const void*)query_gradients_kernel<T, DP, LOCAL, BIASED>, hipFuncAttributeMaxDynamicSharedMemorySize, 92 << 10) != hipSuccess) return;
+        lds_attr_set = true;
+    }
     in_turn(row_jobs, a.n_seq, [&](unsigned n) {
         b.listed = add_up(n, a.row_blocks, a.parts);
-        hipLaunchKernelGGL((query_gradients_kernel<T, DP>), dim3((unsigned)row_jobs * n), dim3(256), 0, st, b);
+        hipLaunchKernelGGL((query_gradients_kernel<T, DP, LOCAL, BIASED>), dim3((unsigned)row_jobs * n), dim3(256), tile_lds + sums_lds, st, b);
     });
     in_turn(key_jobs, a.n_seq, [&](unsigned n) {
-        b.listed = add_up(n, key_blocks, a.key_parts);
-        hipLaunchKernelGGL((key_gradients_kernel<T, DP>), dim3((unsigned)key_jobs * n), dim3(256), 0, st, b);
+        b.listed = add_up(n, key_blocks, max(a.key_parts, a.sink_parts));
+        if (BIASED) set_width(b, FIXED + (a.key_tile - 1) / a.group + 2);
+        hipLaunchKernelGGL((key_gradients_kernel<T, DP, LOCAL, BIASED>), dim3((unsigned)key_jobs * n), dim3(256), BIASED ? 2 * b.bias_words * sizeof(float) : 0, st, b);
     });
+    if (LOCAL && a.sink_parts > 1) {
+        const unsigned blocks = (unsigned)min((apart * FIXED * a.kv_heads * a.head_dim / 4 + 255) / 256, (int64_t)4096);
+        in_turn(blocks, 32768, [&](unsigned n) { hipLaunchKernelGGL(add_sinks_kernel<T>, dim3(blocks, n, 2), dim3(256), 0, st, b); });
+    }
     const int z0 = a.parts > 1 ? 0 : 1, z1 = a.key_parts > 1 ? 3 : 1;
     if (z0 == z1) return;
     const int64_t most = max(z0 == 0 ? (int64_t)a.max_q * a.heads : 0, z1 == 3 ? (int64_t)a.max_k * a.kv_heads : 0) * a.head_dim / 4;
     const unsigned blocks = (unsigned)min((most + 255) / 256, (int64_t)4096);
     in_turn(blocks, 32768, [&](unsigned n) {
-        hipLaunchKernelGGL(add_kernel<T>, dim3(blocks, n, (unsigned)(z1 - z0)), dim3(256), 0, st, b, z0);
+        hipLaunchKernelGGL((add_kernel<T, LOCAL>), dim3(blocks, n, (unsigned)(z1 - z0)), dim3(256), 0, st, b, z0);
     });
 }
 
 }  // namespace
 
-extern "C" int ps_attention_backward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const void* q, const void* k,
-                                     const void* v, const void* out, const float* lse, const void* out_rest, const void* dout, void* dq,
-                                     void* dk, void* dv, void* workspace, size_t workspace_bytes, ps_status* status, void* hip_stream) {
+namespace {
+
+template <bool LOCAL>
+int backward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const ps_attention_local* local, const void* q, const void* k, const void* v,
+             const void* out, const float* lse, const void* out_rest, const void* dout, void* dq, void* dk, void* dv, float* dbias, void* workspace,
+             size_t workspace_bytes, ps_status* status, void* hip_stream) {
     Plan p;
-    if (!seqs) return PS_EINVAL;
-    const int code = plan(desc, seqs, true, workspace, p);
+    if (!seqs || (LOCAL && !local)) return PS_EINVAL;
+    const int code = plan(desc, seqs, local, true, workspace, p, sees_ahead(desc, seqs));
     if (code != PS_OK) return code;
     p.a.status = status;
-    if (p.a.n_seq == 0 || (p.a.n_q == 0 && p.a.n_k == 0)) return check_sequences(p.a, (hipStream_t)hip_stream);
+    if (dbias && (p.a.n_buckets == 0 || (uintptr_t)dbias % 4 != 0)) return PS_EINVAL;
+    if (!dbias) p.a.bias_parts = nullptr;
+    auto add_bias = [&](int32_t n_seq) {
+        Args b = p.a;
+        b.n_seq = n_seq;
+        if (dbias) hipLaunchKernelGGL(add_bias_kernel, dim3((unsigned)((b.n_buckets * b.heads + 63) / 64)), dim3(256), 0, (hipStream_t)hip_stream, b, dbias);
+    };
+    if (p.a.n_seq == 0 || (p.a.n_q == 0 && p.a.n_k == 0)) {
+        if (dbias) {
+            (void)hipGetLastError();
+            add_bias(0);
+            if (hipGetLastError() != hipSuccess) return PS_EHIP;
+        }
+        return check_sequences(p.a, (hipStream_t)hip_stream);
+    }
     const ps_attention_desc* d = desc;
     if (p.a.n_q > 0 && (check_strides(d, d->q, q, d->n_q, d->heads, false) || check_strides(d, d->out, out, d->n_q, d->heads, false) || !lse ||
                         check_strides(d, d->dout, dout, d->n_q, d->heads, false) || check_strides(d, d->dq, dq, d->n_q, d->heads, true)))
@@ -544,10 +757,37 @@ extern "C" int ps_attention_backward(const ps_attention_desc* desc, const ps_att
     if (a.max_q == 0 && check_sequences(a, st) != PS_OK) return PS_EHIP;   // (else the queries' launch finds them)
     (void)hipGetLastError();
     summarise_documents(a, st);
-    switch (padded(desc->head_dim)) {
-        case 64: desc->dtype == 1 ? launch<bf16, 64>(a, st) : launch<float, 64>(a, st); break;
-        case 96: desc->dtype == 1 ? launch<bf16, 96>(a, st) : launch<float, 96>(a, st); break;
-        default: desc->dtype == 1 ? launch<bf16, 128>(a, st) : launch<float, 128>(a, st);
+    if (LOCAL) make_table(a, local, LOG2E, st);
+    auto of_type = [&](auto biased) {
+        constexpr bool B = decltype(biased)::value;
+        switch (padded(desc->head_dim)) {
+            case 64: desc->dtype == 1 ? launch<bf16, 64, LOCAL, B>(a, st) : launch<float, 64, LOCAL, B>(a, st); break;
+            case 96: desc->dtype == 1 ? launch<bf16, 96, LOCAL, B>(a, st) : launch<float, 96, LOCAL, B>(a, st); break;
+            default: desc->dtype == 1 ? launch<bf16, 128, LOCAL, B>(a, st) : launch<float, 128, LOCAL, B>(a, st);
+        }
+    };
+    if constexpr (LOCAL) {
+        if (a.table) {
+            of_type(std::true_type());
+            add_bias(a.n_seq);
+            return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
+        }
     }
+    of_type(std::false_type());
     return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
+}
+
+}  // namespace
+
+extern "C" int ps_attention_backward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const void* q, const void* k,
+                                     const void* v, const void* out, const float* lse, const void* out_rest, const void* dout, void* dq,
+                                     void* dk, void* dv, void* workspace, size_t workspace_bytes, ps_status* status, void* hip_stream) {
+    return backward<false>(desc, seqs, nullptr, q, k, v, out, lse, out_rest, dout, dq, dk, dv, nullptr, workspace, workspace_bytes, status, hip_stream);
+}
+
+extern "C" int ps_local_attention_backward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const ps_attention_local* local, const void* q,
+                                           const void* k, const void* v, const void* out, const float* lse, const void* out_rest, const void* dout,
+                                           void* dq, void* dk, void* dv, float* dbias, void* workspace, size_t workspace_bytes, ps_status* status,
+                                           void* hip_stream) {
+    return backward<true>(desc, seqs, local, q, k, v, out, lse, out_rest, dout, dq, dk, dv, dbias, workspace, workspace_bytes, status, hip_stream);
 }

@@ -14,10 +14,10 @@ constexpr float SLACK = 8.f;           // powers of two that a score may exceed 
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * LN2; }
 
 // A lane's row: what it sees, and its running maximum, sum and weighted values.
-template <typename T, int DP, int R>
+template <typename T, int DP, int R, bool LOCAL, bool BIASED>
 struct Row {
     using L = Tile<T, DP, R>;
-    int head, place, doc, end;         // keys in front of `end` are seen, if their documents are
+    int head, place, doc, end;         // keys in front of `end` are seen, if their documents are, and with a window a.left in front of `place` or of a.sinks
     int64_t token;
     float slope, m = -INFINITY, l = 0.f;   // what goes with step()'s scores; the exponent's reference, in powers of two; this lane's share of the sum
     Fixed<T, DP> qf;
@@ -33,7 +33,7 @@ struct Row {
         place = q.start + qi;
         slope = a.slopes ? a.slopes[head] * a.slope_by : 0.f;
         doc = a.q_docs ? a.q_docs[token] : 0;
-        end = seen_end(a, q, place);
+        end = seen_to<LOCAL>(a, q, place);
         qf.load((const T*)a.q + token * a.qs.row + head * a.qs.head, live && doc >= 0, a.head_dim, half);
 #pragma unroll
         for (int i = 0; i < L::NA; ++i)
@@ -42,8 +42,10 @@ struct Row {
     }
 
     // A tile of keys from k0 on and its values.  cut: some of the wavefront's rows see only the keys in front of their `end`; docs: documents
-    // of its keys, null if the tile's and all rows' are one.
-    __device__ __forceinline__ void step(const Args& a, const unsigned char* keys, const unsigned char* values, const int* docs, int k0, bool cut) {
+    // of its keys, null if the tile's and all rows' are one; late: some of the rows' windows begin behind keys that are not in front of a.sinks;
+    // bias(i): the learned bias of key k0 + i, null if there is none.
+    template <typename Bias>
+    __device__ __forceinline__ void step(const Args& a, const unsigned char* keys, const unsigned char* values, const int* docs, int k0, bool cut, bool late, Bias bias) {
         f32x16 sc[L::BLOCKS];
 #pragma unroll
         for (int b = 0; b < L::BLOCKS; b += 2) {
@@ -73,6 +75,23 @@ struct Row {
             for (int b = 0; b < L::BLOCKS; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sc[b][e] = fmaf(-slope, fabsf(from - (float)(32 * b + row_of(e))), sc[b][e]);
+        }
+        if constexpr (LOCAL) {
+            if (BIASED) {
+#pragma unroll
+                for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sc[b][e] += bias(32 * b + row_of(e) + 4 * half);
+            }
+            if (late) {
+                const int from = k0 + 4 * half - a.sinks;
+                // keys behind the first ones that are in front of the window (late tiles alone: places are near enough to the window's length)
+                const unsigned hidden = max(place - a.left - a.sinks, 0);
+#pragma unroll
+                for (int b = 0; b < L::BLOCKS; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sc[b][e] = (unsigned)(from + 32 * b + row_of(e)) < hidden ? -INFINITY : sc[b][e];
+            }
         }
         if (cut) {
             const int left = end - k0 - 4 * half;
@@ -113,7 +132,7 @@ struct Row {
         const float ref = m == -INFINITY ? 0.f : m;                   // (a row that has seen nothing yet)
 #pragma unroll
         for (int b = 0; b < L::BLOCKS; ++b) {
-            Weights<T> w;
+            Weights<T> w, rest;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float4 x;
@@ -123,8 +142,16 @@ struct Row {
                     l += (&x.x)[i];
                 }
                 w.set(j, x);
+                if constexpr (BIASED && sizeof(T) == 2) {
+                    const float4 r = w.get(j);
+                    rest.set(j, make_float4(x.x - r.x, x.y - r.y, x.z - r.z, x.w - r.w));
+                }
             }
             weigh<T, DP>(values, b, w, o, lanes);
+            // what the rounding of the weights left, where gradients are to come: the bias's is made of fp32 sums, and dout . out, which every pair's
+            // gradient is less, would be off by as much as weights of 8 bits make it (1e-3 of the norm of dbias; 3e-6 with it)
+            if constexpr (BIASED && sizeof(T) == 2)
+                if (a.rest_w) weigh<T, DP>(values, b, rest, o, lanes);
         }
     }
 
@@ -147,24 +174,26 @@ struct Row {
 // 0.42 PFLOP/s, 40 %, 19 %, 2.1 wavefronts, 36 %.  A call of short prompts (64 of 4 to 512 tokens, 12 heads of 64: 33 us) waits 42 % of a
 // wavefront's time, for its first tiles.  Three tiles in LDS, priorities around the matrix instructions and the sum of a row's weights by dot
 // products made no difference (2 %).
-template <typename T, int DP, bool PARTS>
-__global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
+template <typename T, int DP, bool PARTS, bool LOCAL, bool BIASED>
+__global__ __launch_bounds__(256, DP == 64 && !BIASED ? 3 : 2) void attend_kernel(Args a) {
     using L = Tile<T, DP>;
+    extern __shared__ __align__(16) float s_bias[];                       // [buffer][a.bias_words]
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][keys, values]
     __shared__ __align__(16) int s_doc[2][64];
 
     Seq q;
     Work w;
-    if (!find_work<false>(a, q, w)) return;
+    if (!find_work<false, LOCAL>(a, q, w)) return;
     const int hk = w.hk, s = w.s, part = PARTS ? w.part : 0, rows = q.qn * a.group, r0 = w.block * FIXED;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-    const int tiles = key_tiles(a, q, r0);
+    const Span span = key_tiles<LOCAL>(a, q, r0);
+    const int tiles = span.tiles;
     const int t0 = PARTS ? part * a.part_tiles : 0, t1 = PARTS ? min(tiles, t0 + a.part_tiles) : tiles;
     if (PARTS && t0 > 0 && t0 >= tiles) return;                           // (part 0 writes, keys or not)
 
     const int wr0 = r0 + 32 * wave;
     const bool live = wr0 + col < rows;
-    Row<T, DP, L::ROWS> row(a, q, hk, min(wr0 + col, rows - 1), live);
+    Row<T, DP, L::ROWS, LOCAL, BIASED> row(a, q, hk, min(wr0 + col, rows - 1), live);
 
     // what the workgroup's and the wavefront's rows see
     const int last = min(r0 + FIXED, rows) - 1;
@@ -183,8 +212,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     }
     const int64_t kblock0 = doc_block0(q.k0, s);
     auto classify = [&](int t, bool& one, bool& pad) {
-        const int k0 = t * L::ROWS;
-        bool some = !a.causal || k0 <= far || k0 < q.prefix;
+        const int k0 = span.at<LOCAL>(t) * L::ROWS;
+        bool some = LOCAL || !a.causal || k0 <= far || k0 < q.prefix;     // (a window's tiles are those that it has some of)
         one = !a.k_docs;
         if (a.k_docs && !a.k_blocks) {
             pad = true;
@@ -196,14 +225,20 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
         }
         return some;
     };
-    auto is_cut = [&](int k0) { return k0 + L::ROWS > q.kn || (a.causal && k0 + L::ROWS - 1 > wnear && k0 + L::ROWS > q.prefix); };
+    const int wend = LOCAL ? seen_to<LOCAL>(a, q, wnear) : 0, wbegin = LOCAL ? window_begin(a, wfar) : 0;   // the first to end, the last to begin
+    const int wend_far = LOCAL ? seen_to<LOCAL>(a, q, wfar) : 0, wbegin_near = LOCAL ? window_begin(a, wnear) : 0;
+    auto is_cut = [&](int k0) {
+        if (LOCAL) return k0 + L::ROWS > wend;
+        return k0 + L::ROWS > q.kn || (a.causal && k0 + L::ROWS - 1 > wnear && k0 + L::ROWS > q.prefix);
+    };
+    const int place = Bias::place(far);
 
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
     const Sender<T, DP, L::ROWS, true> keys(a.ks, 1, a.head_dim), values(a.vs, 1, a.head_dim);
     const bool regular = keys.regular && values.regular;
     auto request = [&](int t, bool padded, int buf) {
-        const int k0 = t * L::ROWS;
+        const int k0 = span.at<LOCAL>(t) * L::ROWS;
         // (rows past the keys, and padding, are zeros: their weights are, and nothing is to come of them)
         if (k0 + L::ROWS <= q.kn && !padded && regular) {
             keys.whole(smem[buf][0], kbase + k0 * a.ks.row);
@@ -214,6 +249,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
             values.rows(smem[buf][1], a.head_dim, there, [&](int i) { return vbase + (k0 + i) * a.vs.row; });
         }
         if (a.k_docs && wave == 0) send_words(s_doc[buf], a.k_docs + q.k0 + min(k0 + lane, q.kn - 1));
+        if (BIASED) Bias::send(hk, k0 - place, s_bias + buf * a.bias_words);
     };
 
     Walk walk;
@@ -221,14 +257,17 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attend_kernel(Args a) {
     if (t < t1) request(t, walk.is_padded(t), 0);
     while (t < t1) {
         const bool one = walk.is_one(t);
-        const int k0 = t * L::ROWS;
+        const int k0 = span.at<LOCAL>(t) * L::ROWS;
         t = walk.next(t + 1, t1, classify);
         vm_wait();
         __syncthreads();                                                  // the tile has landed, the one before it is no longer read
         if (t < t1) request(t, walk.is_padded(t), buf ^ 1);
-        // (a wavefront whose rows all stand before the tile has nothing in it)
-        if (wr0 < rows && !(a.causal && k0 > wfar && k0 >= q.prefix)) {
-            row.step(a, smem[buf][0], smem[buf][1], one ? nullptr : s_doc[buf], k0, is_cut(k0));
+        // (a wavefront whose rows all stand before the tile, or whose windows do, has nothing in it)
+        const bool none = LOCAL ? k0 >= wend_far || (k0 + L::ROWS <= wbegin_near && k0 >= a.sinks) : a.causal && k0 > wfar && k0 >= q.prefix;
+        if (wr0 < rows && !none) {
+            const float* bias = BIASED ? s_bias + buf * a.bias_words + (row.head - hk * a.group) * a.bias_width + place - Bias::place(row.place) : nullptr;
+            row.step(a, smem[buf][0], smem[buf][1], one ? nullptr : s_doc[buf], k0, is_cut(k0), LOCAL && k0 < wbegin && k0 + L::ROWS > a.sinks,
+                     [&](int i) { return bias[i]; });
         }
         buf ^= 1;
     }
@@ -298,7 +337,7 @@ struct Few {
     }
 };
 
-template <typename T, int DP>
+template <typename T, int DP, bool LOCAL, bool BIASED>
 __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kernel(Args a) {
     using F = Few<T, DP>;
     using L = typename F::L;
@@ -320,7 +359,8 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
     const int rows = q.qn * a.group;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     if (rows == 0) return;
-    const int tiles = key_tiles(a, q, 0), t0 = part * a.part_tiles, t1 = min(tiles, t0 + a.part_tiles);
+    const Span span = key_tiles<LOCAL>(a, q, 0);
+    const int tiles = span.tiles, t0 = part * a.part_tiles, t1 = min(tiles, t0 + a.part_tiles);
     if (t0 > 0 && t0 >= tiles) return;                                    // (part 0 writes, keys or not)
 
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
@@ -328,7 +368,7 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
     const F few(a);
     const bool regular = a.ks.row < 1 << 20 && a.vs.row < 1 << 20;
     auto request = [&](int t, int stage) {
-        const int k0 = t * 32;
+        const int k0 = span.at<LOCAL>(t) * 32;
         unsigned char *keys = smem[wave][stage][0], *values = smem[wave][stage][1];
         if (regular && k0 + 32 <= q.kn && !a.k_docs) {
             few.whole(keys, 0, kbase + k0 * a.ks.row);
@@ -343,8 +383,9 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
     const int near = q.start, far = q.start + q.qn - 1;                   // places of the rows
     auto classify = [&](int t, bool&, bool&) {
         const int k0 = t * 32;
-        return (t & 3) == wave && (!a.causal || k0 <= far || k0 < q.prefix);
+        return (t & 3) == wave && (LOCAL || !a.causal || k0 <= far || k0 < q.prefix);
     };
+    const int end = LOCAL ? seen_to<LOCAL>(a, q, near) : 0, begin = LOCAL ? window_begin(a, far) : 0;   // the first to end, the last to begin
 
     Walk walk, ahead;                                                     // the tile to work on, the last one sent for
     int t = walk.next(t0, t1, classify), sent = ahead.next(t0, t1, classify), stage = 0, next_stage = 0;
@@ -356,15 +397,19 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
 #pragma unroll
     for (int i = 0; i < STAGES; ++i)
         if (sent < t1) send_next();
-    Row<T, DP, 32> row(a, q, hk, min(col, rows - 1), col < rows);
+    Row<T, DP, 32, LOCAL, BIASED> row(a, q, hk, min(col, rows - 1), col < rows);
+    const float* table = BIASED ? a.table + (int64_t)row.head * (2 * a.reach + 1) + a.reach : nullptr;
+    const int place = Bias::place(row.place);
     while (t < t1) {
         // (with a tile behind it every send of this one is WAIT sends old; the last ones wait for all)
         if (STAGES > 1 && sent < t1)
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(F::WAIT) : "memory");
         else
             vm_wait();
-        row.step(a, smem[wave][stage][0], smem[wave][stage][1], a.k_docs ? s_doc[wave][stage] : nullptr, t * 32,
-                 t * 32 + 32 > q.kn || (a.causal && t * 32 + 31 > near && t * 32 + 32 > q.prefix));
+        const int k0 = span.at<LOCAL>(t) * 32;
+        const bool cut = LOCAL ? k0 + 32 > end : k0 + 32 > q.kn || (a.causal && k0 + 31 > near && k0 + 32 > q.prefix);
+        row.step(a, smem[wave][stage][0], smem[wave][stage][1], a.k_docs ? s_doc[wave][stage] : nullptr, k0, cut,
+                 LOCAL && k0 < begin && k0 + 32 > a.sinks, [&](int i) { return table[max(-a.reach, min(k0 + i - place, a.reach))]; });
         asm volatile("" ::: "memory");                                    // (its reads are over: their products are on their way)
         stage = stage + 1 < STAGES ? stage + 1 : 0;
         t = walk.next(t + 1, t1, classify);
@@ -418,7 +463,7 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
 }
 
 // The parts of a row put together by a workgroup's four wavefronts, each a fourth of them; lane f has elements f and f + 64.
-template <typename T>
+template <typename T, bool LOCAL>
 __global__ __launch_bounds__(256) void join_few_kernel(Args a) {
     __shared__ float s_l[4], s_o[4][128];
     const int s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = blockIdx.x;
@@ -426,7 +471,7 @@ __global__ __launch_bounds__(256) void join_few_kernel(Args a) {
     if (!sequence(a, s, q) || (int64_t)i >= (int64_t)q.qn * a.heads) return;
     const int64_t row = (int64_t)q.q0 * a.heads + i, token = q.q0 + i / a.heads;
     const int head = i % a.heads, block = (i / a.heads * a.group + head % a.group) / FIXED;
-    const int parts = shares(key_tiles(a, q, block * FIXED), a.parts, a.part_tiles);
+    const int parts = shares(key_tiles<LOCAL>(a, q, block * FIXED).tiles, a.parts, a.part_tiles);
     const int64_t step = a.n_q * a.heads;
     float m = -INFINITY;
     for (int p = lane; p < parts; p += 64) m = fmaxf(m, a.part_ml[p * step + row].x);
@@ -465,7 +510,7 @@ __global__ __launch_bounds__(256) void join_few_kernel(Args a) {
 }
 
 // The same where rows are many and parts few, a thread four neighbours of a row.
-template <typename T>
+template <typename T, bool LOCAL>
 __global__ __launch_bounds__(256) void join_kernel(Args a) {
     const int s = a.seq0 + (int)blockIdx.y;
     Seq q;
@@ -475,7 +520,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int mine = (int)(i / fours), f = (int)(i - (int64_t)mine * fours) * 4, qi = mine / a.heads, head = mine - qi * a.heads;
         const int64_t token = q.q0 + qi, row = token * a.heads + head;
-        const int parts = shares(key_tiles(a, q, (qi * a.group + head % a.group) / FIXED * FIXED), a.parts, a.part_tiles);
+        const int parts = shares(key_tiles<LOCAL>(a, q, (qi * a.group + head % a.group) / FIXED * FIXED).tiles, a.parts, a.part_tiles);
         float m = -INFINITY, l = 0.f;
         for (int p = 0; p < parts; ++p) m = fmaxf(m, a.part_ml[p * step + row].x);
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -528,7 +573,19 @@ __global__ __launch_bounds__(256) void check_kernel(Args a) {
     if (s < a.n_seq && !sequence(a, s, q)) report_fault(a.status, PS_ST_BAD_LENGTH, s);
 }
 
-template <typename T, int DP>
+// The learned bias of every distance, a thread each of a head's, `by` times what the caller has (none for a bucket that there is not), and
+// where its bucket is in a lane's sums.
+__global__ __launch_bounds__(256) void table_kernel(const int32_t* buckets, const float* bias, float* table, int32_t* words, int reach, int n_buckets, int heads,
+                                                    float by) {
+    const int d = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y;
+    if (d > 2 * reach) return;
+    const int b = buckets[d];
+    const bool is = b >= 0 && b < n_buckets;
+    table[(int64_t)h * (2 * reach + 1) + d] = is ? bias[(int64_t)b * heads + h] * by : 0.f;
+    if (words && h == 0) words[d] = (is ? b : n_buckets) * 64;
+}
+
+template <typename T, int DP, bool LOCAL, bool BIASED>
 void launch_attend(const Args& a, hipStream_t st) {
     const int64_t per_seq = (int64_t)a.kv_heads * a.row_blocks * a.parts;
     Args b = a;
@@ -540,12 +597,13 @@ void launch_attend(const Args& a, hipStream_t st) {
         b.together = turns(per_seq, n);
         b.listed = add_up(n, a.row_blocks, a.parts);
         const dim3 grid((unsigned)(per_seq * n));
+        const unsigned lds = BIASED ? 2 * a.bias_words * sizeof(float) : 0;
         if (a.few)
-            hipLaunchKernelGGL((attend_few_kernel<T, DP>), grid, dim3(256), 0, st, b);
+            hipLaunchKernelGGL((attend_few_kernel<T, DP, LOCAL, BIASED>), grid, dim3(256), 0, st, b);
         else if (a.parts > 1)
-            hipLaunchKernelGGL((attend_kernel<T, DP, true>), grid, dim3(256), 0, st, b);
+            hipLaunchKernelGGL((attend_kernel<T, DP, true, LOCAL, BIASED>), grid, dim3(256), lds, st, b);
         else
-            hipLaunchKernelGGL((attend_kernel<T, DP, false>), grid, dim3(256), 0, st, b);
+            hipLaunchKernelGGL((attend_kernel<T, DP, false, LOCAL, BIASED>), grid, dim3(256), lds, st, b);
     }
     if (a.parts == 1) return;
     for (int32_t s0 = 0, n; s0 < a.n_seq; s0 += n) {
@@ -555,9 +613,9 @@ void launch_attend(const Args& a, hipStream_t st) {
         // a row 22, four wavefronts 53)
         const int64_t rows = (int64_t)a.max_q * a.heads;
         if (a.n_q * a.heads <= 4096)
-            hipLaunchKernelGGL(join_few_kernel<T>, dim3((unsigned)rows, (unsigned)n), dim3(256), 0, st, b);
+            hipLaunchKernelGGL((join_few_kernel<T, LOCAL>), dim3((unsigned)rows, (unsigned)n), dim3(256), 0, st, b);
         else
-            hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)min((rows * (a.head_dim / 4) + 255) / 256, (int64_t)4096), (unsigned)n), dim3(256), 0, st, b);
+            hipLaunchKernelGGL((join_kernel<T, LOCAL>), dim3((unsigned)min((rows * (a.head_dim / 4) + 255) / 256, (int64_t)4096), (unsigned)n), dim3(256), 0, st, b);
     }
 }
 
@@ -575,13 +633,20 @@ namespace seqatt {
 // the empty ones do not matter (64 sequences of 4 to 512 tokens, forwards / keys' gradients 37 / 53 us either way).
 bool add_up(int32_t seqs, int64_t blocks, int32_t parts) { return seqs <= 64 && blocks <= 64 && parts > 1; }
 
+// Distances that a head has in a tile, and the words of all heads.
+void set_width(Args& a, int width) {
+    a.bias_width = width;
+    a.bias_words = (width * a.group + 63) / 64 * 64;
+    a.by_width = (uint32_t)(((uint64_t)1 << 32) / (uint64_t)width + 1);
+}
+
 // A tensor that a call reads or writes.  Heads or rows of a written one may not fall on one another.
 int check_strides(const ps_attention_desc* d, const ps_strides& s, const void* base, int64_t rows, int64_t heads, bool written) {
     if (!base || ((uintptr_t)base & 15) != 0 || !good_strides(d, s)) return PS_EINVAL;
     return written && !strides_apart(s, rows, heads, d->head_dim) ? PS_EINVAL : PS_OK;
 }
 
-int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, void* workspace, Plan& p) {
+int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attention_local* local, bool backward, void* workspace, Plan& p, bool ahead) {
     if (!d || d->n_seq < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 || d->head_dim < 1 || d->max_q < 0 ||
         d->max_k < 0 || d->n_q < 0 || d->n_k < 0 || d->n_q > INT32_MAX || d->n_k > INT32_MAX || (d->dtype != 0 && d->dtype != 1) ||
         (d->causal != 0 && d->causal != 1))
@@ -614,6 +679,26 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
     // rows: lengths stand on the device.
     a.tile = tile_rows(d->dtype == 1 ? 2 : 4);
     a.key_tile = key_tile_rows(d->dtype == 1 ? 2 : 4, padded(d->head_dim));
+    // What a row sees of a sequence at most, and what sees a key: with a window, that of a block of rows (keys) and its first keys.
+    const int64_t rows_a_seq = (int64_t)a.max_q * group;
+    int64_t most_keys = a.max_k, most_rows = rows_a_seq, all_keys = d->n_k, all_rows = d->n_q * group;
+    a.left = a.right = INT32_MAX;
+    if (local) {
+        if (local->sinks < 0 || local->n_buckets < 0 || local->reach < 0) return PS_EINVAL;
+        if (local->n_buckets > 64 || local->reach > 65536 || (local->n_buckets > 0 && group > 32)) return PS_EUNSUPPORTED;
+        if (s && local->n_buckets > 0 && (!local->buckets || !local->bias || ((uintptr_t)local->buckets | (uintptr_t)local->bias) % 4 != 0)) return PS_EINVAL;
+        if (local->left >= 0) a.left = local->left;
+        if (local->right >= 0) a.right = local->right;
+        a.sinks = min(local->sinks, a.max_k);
+        a.reach = local->reach;
+        a.n_buckets = local->n_buckets;
+        const int64_t window = (int64_t)a.left + (ahead ? a.right : 0) + FIXED;
+        auto lower = [](int64_t& to, int64_t by) { to = by < to ? by : to; };   // (the host's min() has 32 bits)
+        lower(most_keys, window + a.sinks + 3 * a.tile);
+        lower(most_rows, window * group + 3 * a.key_tile);
+        lower(all_keys, d->n_seq * most_keys);
+        lower(all_rows, d->n_seq * most_rows);
+    }
     auto share = [&](int64_t blocks_a_seq, int64_t tokens, int64_t tokens_a_block, int64_t passing, int64_t all_passing, int tile, int32_t& parts,
                      int32_t& part_tiles, int64_t chain) {
         const int tiles = (int)((passing + tile - 1) / tile);
@@ -630,25 +715,36 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
         part_tiles = (int32_t)max((int64_t)part_tiles, (tiles + most - 1) / most);
         parts = (tiles + part_tiles - 1) / part_tiles;
     };
-    const int64_t rows_a_seq = (int64_t)a.max_q * group;
     // Few rows: shares of 16 tiles or more (four a wavefront), so many that there are some 256 of up to 32 tiles, and of longer ones some
     // 1024, long sequences' and short ones' (one cache of 65521 keys, 4 heads of 128: 256 shares 28.5 us, 512 33.7).
     a.few = !backward && (int64_t)a.max_q * group <= 32;
     if (a.few) {
         a.tile = 32;
-        const int64_t tiles = ((int64_t)a.max_k + 31) / 32, jobs = a.kv_heads * (d->n_k / 32 + d->n_seq);
+        const int64_t tiles = (most_keys + 31) / 32, jobs = a.kv_heads * (all_keys / 32 + d->n_seq);
         const int64_t most = max((int64_t)1, ((int64_t)64 << 20) / max((int64_t)1, d->n_q * d->heads * d->head_dim));
         a.part_tiles = (int32_t)max(max(min(max((int64_t)16, jobs / 256), (int64_t)32), jobs / 1024), (tiles + most - 1) / most);
         a.parts = (int32_t)max((int64_t)1, (tiles + a.part_tiles - 1) / a.part_tiles);
     } else {
-        share(a.row_blocks, d->n_q * group, FIXED, a.max_k, d->n_k, a.tile, a.parts, a.part_tiles, INT32_MAX);
+        share(a.row_blocks, d->n_q * group, FIXED, most_keys, all_keys, a.tile, a.parts, a.part_tiles, INT32_MAX);
     }
     // Of few blocks of keys, shares of 64 rows: a block's chain of tiles, the rows of all its head's heads, is all that takes time.  The sum's launch
     // is worth it above 256 rows, 128 in fp32 (passes of 1 sequence of 191 tokens, 48 heads on 12, 61 -> 52 us; 14 of up to 70, 16 heads of 128 on
     // 4, 49 -> 43; fp32, 4 of 56, 4 heads on 1, 82 -> 56; 4 of 128 rows, 12 heads, would take 34 for 28).
-    share((a.max_k + FIXED - 1) / FIXED, d->n_k, FIXED, rows_a_seq, d->n_q * group, a.key_tile, a.key_parts, a.key_part_tiles, d->dtype == 1 ? 256 : 128);
+    const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED;
+    share(key_blocks, d->n_k, FIXED, most_rows, all_rows, a.key_tile, a.key_parts, a.key_part_tiles, d->dtype == 1 ? 256 : 128);
+    // The first keys are seen from everywhere: where a window leaves other blocks of keys few rows, theirs are shared out, so that no share is longer
+    // than the others' chains, and within 256 MB.
+    if (backward && a.sinks > 0 && most_rows < rows_a_seq) {
+        a.sink_blocks = (a.sinks + FIXED - 1) / FIXED;                    // (a.sinks is at most max_k)
+        const int64_t tiles = (rows_a_seq + a.key_tile - 1) / a.key_tile, each = (int64_t)d->n_seq * a.sink_blocks * FIXED * a.kv_heads * a.head_dim;
+        const int64_t most = each < 1 || each >= 32 << 20 ? 1 : (32 << 20) / each;
+        int64_t own = most_rows > 512 ? (most_rows + a.key_tile - 1) / a.key_tile : 512 / a.key_tile;
+        if (own < (tiles + most - 1) / most) own = (tiles + most - 1) / most;
+        a.sink_part_tiles = (int32_t)(own < tiles ? own : tiles);
+        a.sink_parts = (int32_t)((tiles + a.sink_part_tiles - 1) / a.sink_part_tiles);
+    }
     // (a grid holds fewer than 2^32 threads)
-    if ((int64_t)a.kv_heads * a.row_blocks * a.parts >= 1 << 24 || (int64_t)a.kv_heads * ((a.max_k + FIXED - 1) / FIXED) * a.key_parts >= 1 << 24)
+    if ((int64_t)a.kv_heads * a.row_blocks * a.parts >= 1 << 24 || (int64_t)a.kv_heads * key_blocks * (int64_t)max(a.key_parts, a.sink_parts) >= 1 << 24)
         return PS_EUNSUPPORTED;
     size_t off = 0;
     uint8_t* base = (uint8_t*)workspace;
@@ -677,6 +773,20 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, bool backward, 
             a.part_dv = (float*)take(part);
         }
     }
+    if (a.sink_parts > 1) {
+        const size_t part = sizeof(float) * (size_t)a.sink_parts * d->n_seq * a.sink_blocks * FIXED * a.kv_heads * a.head_dim;
+        a.sink_dk = (float*)take(part);
+        a.sink_dv = (float*)take(part);
+    }
+    if (a.n_buckets > 0) {
+        a.table = (const float*)take(sizeof(float) * (size_t)a.heads * (2 * (size_t)a.reach + 1));
+        a.bucket_words = (const int32_t*)take(sizeof(int32_t) * (2 * (size_t)a.reach + 1));
+        set_width(a, a.tile + (FIXED - 1) / a.group + 2);   // (a tile of keys by FIXED rows)
+        if (backward) {
+            a.bias_blocks = d->n_q * group / FIXED + d->n_seq + 1;
+            a.bias_parts = (float*)take(sizeof(float) * (size_t)a.parts * a.bias_blocks * a.n_buckets * a.heads);
+        }
+    }
     p.bytes = off > 0 ? off : 256;     // (0 says that a call is refused)
     return PS_OK;
 }
@@ -693,6 +803,12 @@ void summarise_documents(const Args& a, hipStream_t st) {
     }
 }
 
+void make_table(const Args& a, const ps_attention_local* local, float by, hipStream_t st) {
+    if (!a.table) return;
+    hipLaunchKernelGGL(table_kernel, dim3((2 * a.reach + 256) / 256, a.heads), dim3(256), 0, st, local->buckets, local->bias, const_cast<float*>(a.table),
+                       const_cast<int32_t*>(a.bucket_words), a.reach, a.n_buckets, a.heads, by);
+}
+
 int check_sequences(const Args& a, hipStream_t st) {
     if (!a.status || a.n_seq == 0) return PS_OK;
     (void)hipGetLastError();
@@ -702,18 +818,25 @@ int check_sequences(const Args& a, hipStream_t st) {
 
 }  // namespace seqatt
 
-extern "C" size_t ps_attention_workspace_bytes(const ps_attention_desc* desc, int backward) {
-    Plan p, b;
-    if (plan(desc, nullptr, false, nullptr, p) != PS_OK || plan(desc, nullptr, true, nullptr, b) != PS_OK) return 0;
-    return backward && b.bytes > p.bytes ? b.bytes : p.bytes;
+namespace {
+
+size_t workspace_bytes_of(const ps_attention_desc* desc, const ps_attention_local* local, int backward) {
+    // (whether rows see keys behind them goes by the sequences too: enough for either)
+    size_t most = 0;
+    for (int i = 0; i < (local ? 4 : 2); ++i) {
+        Plan p;
+        if (plan(desc, nullptr, local, i & 1, nullptr, p, i < 2) != PS_OK) return 0;
+        if ((backward || !(i & 1)) && p.bytes > most) most = p.bytes;
+    }
+    return most;
 }
 
-extern "C" int ps_attention_forward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const void* q, const void* k,
-                                    const void* v, void* out, float* lse, void* out_rest, void* workspace, size_t workspace_bytes,
-                                    ps_status* status, void* hip_stream) {
+template <bool LOCAL>
+int forward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const ps_attention_local* local, const void* q, const void* k, const void* v,
+            void* out, float* lse, void* out_rest, void* workspace, size_t workspace_bytes, ps_status* status, void* hip_stream) {
     Plan p;
-    if (!seqs) return PS_EINVAL;
-    const int code = plan(desc, seqs, false, workspace, p);
+    if (!seqs || (LOCAL && !local)) return PS_EINVAL;
+    const int code = plan(desc, seqs, local, false, workspace, p, sees_ahead(desc, seqs));
     if (code != PS_OK) return code;
     p.a.status = status;
     if (p.a.n_seq == 0 || p.a.max_q == 0) return check_sequences(p.a, (hipStream_t)hip_stream);
@@ -729,10 +852,57 @@ extern "C" int ps_attention_forward(const ps_attention_desc* desc, const ps_atte
     hipStream_t st = (hipStream_t)hip_stream;
     (void)hipGetLastError();
     if (!a.few) summarise_documents(a, st);
-    switch (padded(desc->head_dim)) {
-        case 64: desc->dtype == 1 ? launch_attend<bf16, 64>(a, st) : launch_attend<float, 64>(a, st); break;
-        case 96: desc->dtype == 1 ? launch_attend<bf16, 96>(a, st) : launch_attend<float, 96>(a, st); break;
-        default: desc->dtype == 1 ? launch_attend<bf16, 128>(a, st) : launch_attend<float, 128>(a, st);
+    if (LOCAL) make_table(a, local, a.slope_by, st);
+    auto of_type = [&](auto biased) {
+        constexpr bool B = decltype(biased)::value;
+        switch (padded(desc->head_dim)) {
+            case 64: desc->dtype == 1 ? launch_attend<bf16, 64, LOCAL, B>(a, st) : launch_attend<float, 64, LOCAL, B>(a, st); break;
+            case 96: desc->dtype == 1 ? launch_attend<bf16, 96, LOCAL, B>(a, st) : launch_attend<float, 96, LOCAL, B>(a, st); break;
+            default: desc->dtype == 1 ? launch_attend<bf16, 128, LOCAL, B>(a, st) : launch_attend<float, 128, LOCAL, B>(a, st);
+        }
+    };
+    if constexpr (LOCAL) {
+        if (a.table) {
+            of_type(std::true_type());
+            return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
+        }
     }
+    of_type(std::false_type());
     return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
+}
+
+}  // namespace
+
+extern "C" size_t ps_attention_workspace_bytes(const ps_attention_desc* desc, int backward) { return workspace_bytes_of(desc, nullptr, backward); }
+
+extern "C" size_t ps_local_attention_workspace_bytes(const ps_attention_desc* desc, const ps_attention_local* local, int backward) {
+    return local ? workspace_bytes_of(desc, local, backward) : 0;
+}
+
+extern "C" int ps_attention_forward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const void* q, const void* k,
+                                    const void* v, void* out, float* lse, void* out_rest, void* workspace, size_t workspace_bytes,
+                                    ps_status* status, void* hip_stream) {
+    return forward<false>(desc, seqs, nullptr, q, k, v, out, lse, out_rest, workspace, workspace_bytes, status, hip_stream);
+}
+
+extern "C" int ps_local_attention_forward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const ps_attention_local* local, const void* q,
+                                          const void* k, const void* v, void* out, float* lse, void* out_rest, void* workspace, size_t workspace_bytes,
+                                          ps_status* status, void* hip_stream) {
+    return forward<true>(desc, seqs, local, q, k, v, out, lse, out_rest, workspace, workspace_bytes, status, hip_stream);
+}
+
+extern "C" int ps_bias_buckets(int32_t n, int32_t reach, int both_sides, int32_t* buckets) {
+    const int side = both_sides ? n / 2 : n, single = side / 2;
+    if (n < 1 || n > 64 || !buckets || (both_sides & ~1) || (both_sides && n % 2 != 0) || single < 1 || reach < single || reach > 65536) return PS_EINVAL;
+    for (int d = -reach; d <= reach; ++d) {
+        const int m = d < 0 ? -d : both_sides ? d : 0;
+        int b = m;
+        if (m >= single) {
+            // (a distance that is a bucket's first belongs to it, whatever the logarithms' last places say)
+            const double wide = reach == single ? side - single : log((double)m / single) / log((double)reach / single) * (side - single);
+            b = min(side - 1, single + (int)floor(fabs(wide - rint(wide)) < 1e-9 ? rint(wide) : wide));
+        }
+        buckets[reach + d] = b + (both_sides && d > 0 ? side : 0);
+    }
+    return PS_OK;
 }
