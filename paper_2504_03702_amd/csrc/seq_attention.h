@@ -57,7 +57,7 @@ struct Args {
     int32_t left, right, sinks;        // a row's window, and the first keys that it sees all the same
     int32_t sink_blocks, sink_parts, sink_part_tiles;   // blocks of keys that have some of those, if they are shared out apart
     float *sink_dk, *sink_dv;          // [sink_parts][n_seq][sink_blocks * FIXED][kv_heads][head_dim]
-    const float* table;                // [heads][2 reach + 1]: the learned bias of a distance, null without one (see Bias)
+    const float* table;                // [heads][2 reach + 1]: the learned bias of a distance, null without one (see Learned)
     const int32_t* bucket_words;       // [2 reach + 1]: where in a lane's sums the distance's bucket is
     float* bias_parts;                 // [parts][blocks of rows][buckets][heads]: sums of a bucket's gradients, null if not wanted
     int64_t bias_blocks;
@@ -259,6 +259,8 @@ __device__ __forceinline__ int64_t doc_block0(int first_token, int s) { return f
 constexpr int tile_rows(int eb) { return eb == 2 ? 64 : 32; }
 // Rows of a tile that passes by fixed keys: for heads of 128 half as many, which leaves room for a workgroup's values (below).
 constexpr int key_tile_rows(int eb, int dp) { return eb == 2 && dp < 128 ? 64 : 32; }
+// Rows of a tile that passes by fixed queries for their gradients: under a learned bias half as many for heads of 128, which leaves room for its sums.
+constexpr int query_tile_rows(int eb, int dp, bool biased) { return biased && eb == 2 && dp == 128 ? 32 : tile_rows(eb); }
 constexpr int padded(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : 128; }   // features of a tile
 
 template <typename T, int DP, int R = tile_rows(sizeof(T))>
@@ -353,15 +355,20 @@ struct FixedInLds {
 // product when its turn comes and waits for LDS every time (heads of 128, gradients of keys: 60 % of a wavefront's time).
 __device__ __forceinline__ void reads_first() { __builtin_amdgcn_sched_barrier(0); }
 
-// 32 passing rows (block b of the tile) times the fixed rows.
-template <typename T, int DP, typename F>
-__device__ __forceinline__ f32x16 dot(const unsigned char* tile, int b, const F& f, const Lanes<T, DP>& l) {
-    using L = Tile<T, DP>;
-    constexpr int N = F::READS ? 2 : L::NF <= 8 ? L::NF : L::NF / 2;
-    const int at = anew<L::ROWB>(l.row);
+__device__ __forceinline__ f32x16 no_start() {
     f32x16 s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
+    return s;
+}
+
+// 32 passing rows (block b of the tile) times the fixed rows, and what the sums start from.
+template <typename T, int DP, typename F>
+__device__ __forceinline__ f32x16 dot(const unsigned char* tile, int b, const F& f, const Lanes<T, DP>& l, const f32x16& start = no_start()) {
+    using L = Tile<T, DP>;
+    constexpr int N = F::READS ? 2 : L::NF <= 8 ? L::NF : L::NF / 2;
+    const int at = anew<L::ROWB>(l.row);
+    f32x16 s = start;
 #pragma unroll
     for (int n = 0; n < L::NF; n += N) {
         uint4 as[N], cs[N];
@@ -391,16 +398,16 @@ __device__ __forceinline__ f32x16 dot(const unsigned char* tile, int b, const F&
 // 108 -> 100 us).
 template <typename T, int DP, typename F, typename G>
 __device__ __forceinline__ void dots(const unsigned char* tile, int b, const F& f, f32x16& s, const unsigned char* tile2, int b2, const G& g, f32x16& s2,
-                                     const Lanes<T, DP>& l) {
+                                     const Lanes<T, DP>& l, const f32x16& start = no_start(), const f32x16& start2 = no_start()) {
     using L = Tile<T, DP>;
     if constexpr (L::EB == 4 || F::READS || G::READS) {
-        s = dot<T, DP>(tile, b, f, l);
-        s2 = dot<T, DP>(tile2, b2, g, l);
+        s = dot<T, DP>(tile, b, f, l, start);
+        s2 = dot<T, DP>(tile2, b2, g, l, start2);
     } else {
         constexpr int N = L::NF <= 4 ? L::NF : L::NF / 2;
         const int at = anew<L::ROWB>(l.row);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = s2[e] = 0.f;
+        s = start;
+        s2 = start2;
 #pragma unroll
         for (int n = 0; n < L::NF; n += N) {
             uint4 x[N], y[N];
@@ -614,7 +621,7 @@ struct Cap {
 // The bias of a distance d = key - place, clamped to -reach .. reach, is table[head][reach + d], made from buckets and values by a launch in
 // front.  A tile meets few of them, and as they are the same along its diagonals a stretch of bias_width for each head will do: it comes by DMA with the tile,
 // head g's words at g bias_width, of distances from `lowest` on.
-struct Bias {
+struct Learned {
     static __device__ __forceinline__ void send(int hk, int lowest, float* to) {
         const ArgsAgain a = again();
         const int lane = anew<256>((int)threadIdx.x) & 63, words = a->bias_words, width = a->bias_width, group = a->group, reach = a->reach;
@@ -633,6 +640,16 @@ struct Bias {
             const int32_t* from = a->bucket_words + reach + max(-reach, min(d, reach));
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)(to + w), 4, 0, 0);
         }
+    }
+    // The bias is what the product starts from (b(i), of passing row i of 32), if it bends no score: nothing is left to add then.
+    template <typename Of>
+    static __device__ __forceinline__ f32x16 start(bool is, int half, Of of) {
+        f32x16 s = no_start();
+        if (is) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = of(8 * (e >> 2) + (e & 3) + 4 * half);
+        }
+        return s;
     }
     // (places as far from all keys as any: distances stay in 32 bits)
     static __device__ __forceinline__ int place(int place) { return max(place, -(1 << 29)); }

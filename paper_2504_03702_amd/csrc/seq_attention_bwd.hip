@@ -20,17 +20,39 @@ namespace {
 // queries' / keys' gradients 499 / 860 -> 589 / 977 us, error against 64 bits 2.7e-3 -> 2.1e-3 of the norm (1.7e-3 is that of dq's and dk's
 // own rounding; 2.3e-3 without cap, where a product more would cost 5 to 10 %).  (Documents in two rows of 8192, where blocks are cut: 130 / 146
 // -> 144 / 160.)
-// LOCAL: bias(j), the learned bias, in powers of two, if there is one; late and windowed(j, is), which keys are in the window, as with `cut`; sums(j, e)
-// takes the gradients of the scores themselves, if they are wanted (that of x has the cap's slope too).
+// LOCAL: late and windowed(j, is), which keys are in the window, as with `cut`.  BIASED: uneven, whether the learned bias differs within the block, and
+// bias(j), in powers of two, if it does; summed, whether the gradients of the scores themselves are wanted (that of x has the cap's slope too): where(j, i)
+// has the words of their buckets' sums, to which `run` adds them, or, of an even block, they are added to `even`.
 struct Nothing {
     __device__ __forceinline__ float4 operator()(int) const { return make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void operator()(int, bool (&)[4]) const {}
-    __device__ __forceinline__ void operator()(int, const float (&)[4]) const {}
 };
-template <typename T, int STEP, bool LOCAL, bool BIASED, typename Lse, typename Delta, typename Distance, typename Front, typename Same, typename Learned, typename Windowed, typename Sums>
+// A lane's gradients of scores on their way to the sums of buckets, in LDS, a lane's own.  Keys come by in order, so a bucket's come one after the other, and go
+// to LDS when the next one's turn has come: an addition there takes 160 cycles of a wavefront's 64 lanes (64 sequences of up to 512 tokens, every
+// value added by itself: 202 us; this way RUNS us).
+struct Run {
+    int word;                          // a row's sum's, in words of all 32 rows
+    float sum;
+    // (a row's two lanes one after the other, so that the order is fixed)
+    __device__ __forceinline__ void flush(float* sums) const {
+        const bool second = anew<256>((int)threadIdx.x) & 32;
+        if (!second) __hip_atomic_fetch_add(sums + word, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        if (second) __hip_atomic_fetch_add(sums + word, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    }
+    __device__ __forceinline__ void add(float* sums, int to, float e) {
+        if (to != word) {
+            flush(sums);
+            word = to;
+            sum = 0.f;
+        }
+        sum += e;
+    }
+};
+template <typename T, int STEP, bool LOCAL, bool BIASED, typename Lse, typename Delta, typename Distance, typename Front, typename Same, typename Windowed, typename Bias,
+          typename Where>
 __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, Weights<T>& p, Weights<T>& d, Weights<T>& rest,
-                                          bool cut, bool docs, bool late, bool summed, Lse lse, Delta delta, Distance distance, Front in_front, Same same,
-                                          Learned bias, Windowed windowed, Sums sums) {
+                                          bool cut, bool docs, bool late, bool uneven, bool summed, Lse lse, Delta delta, Distance distance, Front in_front,
+                                          Same same, Windowed windowed, Bias bias, Where where, float* sums, Run& run, float& even) {
     const Cap cap = Cap::of<T>(a);
     const float c1 = a.scale * LOG2E;
 #pragma unroll
@@ -45,7 +67,7 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
                 u[k] = make_float4(u[k].x + off.x, u[k].y + off.y, u[k].z + off.z, u[k].w + off.w);
             }
         }
-        if (BIASED) {
+        if (BIASED && uneven && a.cap > 0.f) {                            // (else the products have started from it)
 #pragma unroll
             for (int k = 0; k < STEP; ++k) {
                 const float4 off = bias(j0 + k);
@@ -95,16 +117,6 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
         if (cut) only(in_front);
         if (docs) only(same);
         if (LOCAL && late) only(windowed);
-        if (BIASED && summed) {
-#pragma unroll
-            for (int k = 0; k < STEP; ++k) {
-                const float4 t = delta(j0 + k);
-                float e[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = (&u[k].x)[i] * (g[4 * (j0 + k) + i] - (&t.x)[i]);
-                sums(j0 + k, e);
-            }
-        }
 #pragma unroll
         for (int k = 0; k < STEP; ++k) {
             p.set(j0 + k, u[k]);
@@ -116,6 +128,46 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
                 for (int k = 0; k < STEP; ++k) {
                     const float4 r = d.get(j0 + k);
                     rest.set(j0 + k, make_float4(v[k].x - r.x, v[k].y - r.y, v[k].z - r.z, v[k].w - r.w));
+                }
+            }
+        if constexpr (BIASED && !std::is_same<Where, Nothing>::value)
+            if (summed) {
+                // (all words first: one that is read behind an addition waits for it)
+                int to[STEP];
+                bool wide = true;                                         // fours of the same bucket
+                if (uneven) {
+#pragma unroll
+                    for (int k = 0; k < STEP; ++k) to[k] = where(j0 + k, 0);
+#pragma unroll
+                    for (int k = 0; k < STEP; ++k) wide = wide && to[k] & 1;
+                    wide = __all(wide);
+                }
+#pragma unroll
+                for (int k = 0; k < STEP; ++k) {
+                    const float4 t = delta(j0 + k);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) (&u[k].x)[i] *= g[4 * (j0 + k) + i] - (&t.x)[i];
+                }
+                if (!uneven || wide) {
+#pragma unroll
+                    for (int k = 0; k < STEP; ++k) {
+                        const float all = (u[k].x + u[k].y) + (u[k].z + u[k].w);
+                        if (uneven)
+                            run.add(sums, to[k] & ~1, all);
+                        else
+                            even += all;
+                    }
+                } else {
+                    int each[STEP][4];
+#pragma unroll
+                    for (int k = 0; k < STEP; ++k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) each[k][i] = i == 0 ? to[k] : where(j0 + k, i);
+                    reads_first();
+#pragma unroll
+                    for (int k = 0; k < STEP; ++k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) run.add(sums, each[k][i] & ~1, (&u[k].x)[i]);
                 }
             }
     }
@@ -234,11 +286,15 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     // A learned bias: a lane's row's words for the keys from k0 on, if its token is the qi-th and the tile's last row's the last-th.
     auto places = [&](int buf, int qi, int head, int last) {
         if (!LOCAL) return;
-        if (wave == 0) s_at[buf][lane] = q.start - k0 + qi;
+        if (wave == 0) {
+            s_at[buf][lane] = q.start - k0 + qi;
+            s_place[buf][lane] = (float)(q.start - k0 + qi);
+        }
         if (BIASED) {
-            const int place = Bias::place(q.start + qi), far = Bias::place(q.start + last);
-            if (wave == 0) s_bias_at[buf][lane] = (head - hk * a.group) * a.bias_width + far - place;
-            Bias::send(hk, k0 - far, s_bias + buf * a.bias_words);
+            const ArgsAgain w = again();
+            const int place = Learned::place(q.start + qi), far = Learned::place(q.start + last), words = buf * w->bias_words;
+            if (wave == 0) s_bias_at[buf][lane] = words + (head - hk * w->group) * w->bias_width + far - place;
+            Learned::send(hk, k0 - far, s_bias + words);
         }
     };
     auto request = [&](int t, bool padded, int buf) {
@@ -249,8 +305,11 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
             Sender<T, DP, L::ROWS>::whole(smem[buf][0], qbase + token * a.qs.row, mine.q);
             Sender<T, DP, L::ROWS>::whole(smem[buf][1], gbase + token * a.gs.row, mine.g);
             if (has_words) send_words(words + 64 * buf, mine.word + (int64_t)t * word_step);
-            if (wave == 0) s_place[buf][lane] = (float)(q.start - k0 + (int)token + (int)over_group(a, lane % L::ROWS));
-            places(buf, (int)token + lane_token, lane_head, (int)token + (L::ROWS - 1) / a.group);
+            if (!LOCAL && wave == 0) s_place[buf][lane] = (float)(q.start - k0 + (int)token + (int)over_group(a, lane % L::ROWS));
+            if (LOCAL) {                                                  // (a lane's row worked out again: registers)
+                const int own = (anew<256>((int)threadIdx.x) & 63) % L::ROWS, of = (int)over_group(a, own);
+                places(buf, (int)token + of, hk * a.group + own - of * a.group, (int)token + (L::ROWS - 1) / a.group);
+            }
             return;
         }
         // (padding and rows past the end are zeros that see nothing)
@@ -264,7 +323,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         Sender<T, DP, L::ROWS>::rows(smem[buf][1], a.head_dim, there, [&](int i) { return row(gbase, a.gs, i); });
         const void* none = wave == 0 ? (const void*)&infinity_word : wave == 3 ? (const void*)&minus_one : (const void*)&zeros;
         if (has_words) send_words(words + 64 * buf, r0 + lane < rows ? word(q.q0 + qi, hk * a.group + r - qi * a.group) : none);
-        if (wave == 0) s_place[buf][lane] = (float)(q.start - k0 + qi);
+        if (!LOCAL && wave == 0) s_place[buf][lane] = (float)(q.start - k0 + qi);
         // (of 64 lanes only those of the tile's rows have words in it)
         const int of_tile = min(r0 + lane % L::ROWS, rows - 1), token = (int)over_group(a, of_tile);
         places(buf, token, hk * a.group + of_tile - token * a.group, (int)over_group(a, min(r0 + L::ROWS, rows) - 1));
@@ -299,10 +358,26 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
 #pragma unroll 1
             for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
                 f32x16 sc, g;
-                dots<T, DP>(smem[buf][0], b, kf, sc, smem[buf][1], b, vf, g, lanes);
-                Weights<T> p, d, rest;
+                float even = 0.f;
+                Run run = {};
                 auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
-                gradients<T, (DP > 64 ? 1 : 4), LOCAL, BIASED>(a, sc, g, p, d, rest, cut, docs, late, false, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
+                if constexpr (BIASED) {
+                    f32x16 start = no_start();
+                    if (a.cap == 0.f) {
+                        const float* own = s_bias + 32 * wave + (anew<256>((int)threadIdx.x) & 31);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int4 of = *(const int4*)&s_bias_at[buf][at(j)];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) start[4 * j + i] = own[(&of.x)[i]];
+                        }
+                    }
+                    dots<T, DP>(smem[buf][0], b, kf, sc, smem[buf][1], b, vf, g, lanes, start);
+                } else {
+                    dots<T, DP>(smem[buf][0], b, kf, sc, smem[buf][1], b, vf, g, lanes);
+                }
+                Weights<T> p, d, rest;
+                gradients<T, (DP > 64 ? 1 : 4), LOCAL, BIASED>(a, sc, g, p, d, rest, cut, docs, late, true, false, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
                              [&](int j) { return *(const float4*)&s_delta[buf][at(j)]; },
                              [&](int j) {
                                  const float4 by = *(const float4*)&s_slope[buf][at(j)], place = *(const float4*)&s_place[buf][at(j)];
@@ -326,11 +401,6 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
 #pragma unroll
                                  for (int i = 0; i < 4; ++i) is[i] = (&of.x)[i] == doc;
                              },
-                             [&](int j) {
-                                 const int4 of = *(const int4*)&s_bias_at[buf][at(j)];
-                                 const float* own = s_bias + buf * a.bias_words + 32 * wave + (anew<256>((int)threadIdx.x) & 31);
-                                 return make_float4(own[of.x], own[of.y], own[of.z], own[of.w]);
-                             },
                              [&](int j, bool(&is)[4]) {
                                  // (worked out again: few tiles are cut by a window.  Distances are 33 bits at most, a window without end 31)
                                  const int own = 32 * wave + (anew<256>((int)threadIdx.x) & 31);
@@ -341,7 +411,12 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
                                      is[i] = (off <= a.left && off >= -a.right) || k0 + own < a.sinks;
                                  }
                              },
-                             Nothing());
+                             [&](int j) {
+                                 const int4 of = *(const int4*)&s_bias_at[buf][at(j)];
+                                 const float* own = s_bias + 32 * wave + (anew<256>((int)threadIdx.x) & 31);
+                                 return make_float4(own[of.x], own[of.y], own[of.z], own[of.w]);
+                             },
+                             Nothing(), nullptr, run, even);
                 weigh<T, DP>(smem[buf][1], b, p, dv, lanes);
                 weigh<T, DP>(smem[buf][0], b, d, dk, lanes);
                 if (sizeof(T) == 2 && (cut || docs || late || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dk, lanes);
@@ -378,9 +453,9 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
 // waiting 22 % of theirs; documents in two rows of 8192, heads of 64: 147 us, 0.37 PFLOP/s, 33 %, 19 %, 1.5 wavefronts, 40 %.
 template <typename T, int DP, bool LOCAL, bool BIASED>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_gradients_kernel(Args a) {
-    using L = Tile<T, DP>;
-    // LOCAL with a bias: [buffer][a.bias_words], then, if its gradient is wanted, [buffer][bias_width, in whole wavefronts] places in a lane's sums, and
-    // [wavefront][buckets, and one for distances without][lane] sums
+    using L = Tile<T, DP, query_tile_rows(sizeof(T), DP, BIASED)>;
+    // BIASED: [buffer][a.bias_words], then, if its gradient is wanted, [buffer][bias_width, in whole wavefronts] words of buckets' sums, and
+    // [wavefront][buckets, and one for distances without][row] sums
     extern __shared__ __align__(16) float s_bias[];
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][keys, values]
     __shared__ __align__(16) int s_doc[2][64];
@@ -465,11 +540,27 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     const bool regular = keys.regular && values.regular;
     const int wend = LOCAL ? seen_to<LOCAL>(a, q, wnear) : 0, wbegin = LOCAL ? window_begin(a, wfar) : 0;   // the first to end, the last to begin
     const int wend_far = LOCAL ? seen_to<LOCAL>(a, q, wfar) : 0, wbegin_near = LOCAL ? window_begin(a, wnear) : 0;
-    const int bias_place = Bias::place(far), bias_from = BIASED ? (head - hk * a.group) * a.bias_width + bias_place - Bias::place(place) : 0;
-    const int widths = (a.bias_width + 63) & ~63, sums_a_wave = (a.n_buckets + 1) * 64;
+    // keys that some of the workgroup's rows have nearer than `reach`
+    const int wide_from = BIASED ? Learned::place(q.start + (int)over_group(a, r0)) - a.reach + 1 : 0, wide_to = BIASED ? (int)min((int64_t)far + a.reach, (int64_t)INT32_MAX) : 0;
+    const int bias_place = Learned::place(far), bias_from = BIASED ? (head - hk * a.group) * a.bias_width + bias_place - Learned::place(place) : 0;
+    const int widths = (a.bias_width + 63) & ~63, sums_a_wave = (a.n_buckets + 1) * 32;
     int* const s_bucket = (int*)(s_bias + 2 * a.bias_words);
     float* const s_sums = (float*)(s_bucket + 2 * widths);
     const bool summed = BIASED && a.bias_parts != nullptr;
+    // What is further than `reach` in front of the row, or behind it, has one bias: a lane's own two, in LDS, as is what few tiles ask for (registers).
+    enum Own { FRONT, BEHIND, SLOPE, DOC, END, OWN };
+    __shared__ float s_own[BIASED ? OWN : 1][BIASED ? 256 : 1];
+    auto kept = [&](Own which) { return s_own[which][anew<256>((int)threadIdx.x)]; };
+    if (BIASED) {
+        const float* const ends = a.table + (int64_t)head * (2 * a.reach + 1);
+        const float in_powers = a.cap > 0.f ? 1.f : a.scale * LOG2E;
+        s_own[FRONT][threadIdx.x] = ends[0] * in_powers;
+        s_own[BEHIND][threadIdx.x] = ends[2 * a.reach] * in_powers;
+        s_own[SLOPE][threadIdx.x] = slope;
+        s_own[DOC][threadIdx.x] = __int_as_float(doc);
+        s_own[END][threadIdx.x] = __int_as_float(end);
+    }
+    const int wnear_place = Learned::place(wnear), wfar_place = (int)min((int64_t)wfar, (int64_t)INT32_MAX - a.reach);   // (a key is below 2^30)
     if (summed)
         for (int i = threadIdx.x; i < 4 * sums_a_wave; i += 256) s_sums[i] = 0.f;   // (the first tile's barrier is behind this)
     auto request = [&](int t, bool padded, int buf) {
@@ -483,9 +574,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
             values.rows(smem[buf][1], a.head_dim, there, [&](int i) { return vbase + (k0 + i) * a.vs.row; });
         }
         if (a.k_docs && wave == 0) send_words(s_doc[buf], a.k_docs + q.k0 + min(k0 + lane, q.kn - 1));
-        if (BIASED) {
-            Bias::send(hk, k0 - bias_place, s_bias + buf * a.bias_words);
-            if (summed) Bias::send_buckets(k0 - bias_place, s_bucket + buf * widths);
+        if (BIASED && scalar(k0 + L::ROWS > wide_from && k0 < wide_to)) {
+            Learned::send(hk, k0 - bias_place, s_bias + buf * a.bias_words);
+            if (summed) Learned::send_buckets(k0 - bias_place, s_bucket + buf * widths);
         }
     };
 
@@ -495,6 +586,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
 #pragma unroll
         for (int e = 0; e < 16; ++e) dq[i][e] = 0.f;
 
+    Run run = {a.n_buckets * 32, 0.f};
     Walk walk;
     int t = walk.next(t0, t1, classify), buf = 0;
     if (t < t1) request(t, walk.is_padded(t), 0);
@@ -513,72 +605,96 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
 #pragma unroll 1
             for (int b = 0; b < L::BLOCKS; ++b) {                         // (one after the other: registers)
                 f32x16 sc, g;
-                dots<T, DP>(smem[buf][0], b, qf, sc, smem[buf][1], b, gf, g, lanes);
+                // a block whose distances all are `reach` and more on one side has one bias, which goes with lse
+                const int kb = k0 + 32 * b;
+                const bool front = BIASED && kb + 31 <= wnear_place - a.reach, uneven = BIASED && !front && kb < wfar_place + a.reach;
+                if constexpr (BIASED)
+                    dots<T, DP>(smem[buf][0], b, qf, sc, smem[buf][1], b, gf, g, lanes,
+                                Learned::start(uneven && a.cap == 0.f, half, [&](int i) { return s_bias[buf * a.bias_words + bias_from + 32 * b + i]; }));
+                else
+                    dots<T, DP>(smem[buf][0], b, qf, sc, smem[buf][1], b, gf, g, lanes);
                 Weights<T> p, d, rest;
                 auto at = [&](int j) { return 32 * b + 8 * j + 4 * half; };
-                const int left = end - k0 - 32 * b - 4 * half;
-                const float off = from - (float)(32 * b);
+                const int own_left = BIASED ? 0 : end - k0 - 32 * b - 4 * half;
+                const float own_off = from - (float)(32 * b);
                 // keys behind the first ones that are in front of the window (late tiles alone: the places are near enough to the window's length)
                 const unsigned hidden = LOCAL ? max(place - a.left - a.sinks, 0) : 0;
-                gradients<T, (BIASED && DP > 96 ? 1 : 4), LOCAL, BIASED>(a, sc, g, p, d, rest, cut, docs, late, summed, [&](int) { return make_float4(lse, lse, lse, lse); },
+                const float mine = BIASED && !uneven ? lse - kept(front ? FRONT : BEHIND) : lse;
+                float even = 0.f;
+                gradients<T, (BIASED && DP > 96 ? 1 : 4), LOCAL, BIASED>(a, sc, g, p, d, rest, cut, docs, late, uneven, summed, [&](int) { return make_float4(mine, mine, mine, mine); },
                              [&](int) { return make_float4(delta, delta, delta, delta); },
                              [&](int j) {
-                                 return make_float4(slope * fabsf(off - (float)(8 * j)), slope * fabsf(off - (float)(8 * j + 1)),
-                                                    slope * fabsf(off - (float)(8 * j + 2)), slope * fabsf(off - (float)(8 * j + 3)));
+                                 const float off = BIASED ? (float)(place - kb - 4 * half) : own_off, by = BIASED ? kept(SLOPE) : slope;
+                                 return make_float4(by * fabsf(off - (float)(8 * j)), by * fabsf(off - (float)(8 * j + 1)),
+                                                    by * fabsf(off - (float)(8 * j + 2)), by * fabsf(off - (float)(8 * j + 3)));
                              },
                              [&](int j, bool(&is)[4]) {
+                                 const int left = BIASED ? __float_as_int(kept(END)) - kb - 4 * half : own_left;
 #pragma unroll
                                  for (int i = 0; i < 4; ++i) is[i] = left > 8 * j + i;
                              },
                              // (padding is zeros on both sides, and its weights are 0 by its lse)
                              [&](int j, bool(&is)[4]) {
                                  const int4 of = *(const int4*)&s_doc[buf][at(j)];
+                                 const int own = BIASED ? __float_as_int(kept(DOC)) : doc;
 #pragma unroll
-                                 for (int i = 0; i < 4; ++i) is[i] = (&of.x)[i] == doc;
-                             },
-                             [&](int j) {
-                                 const float* own = s_bias + buf * a.bias_words + bias_from + at(j);
-                                 return make_float4(own[0], own[1], own[2], own[3]);
+                                 for (int i = 0; i < 4; ++i) is[i] = (&of.x)[i] == own;
                              },
                              [&](int j, bool(&is)[4]) {
 #pragma unroll
                                  for (int i = 0; i < 4; ++i) is[i] = (unsigned)(k0 + at(j) + i - a.sinks) >= hidden;
                              },
-                             [&](int j, const float(&e)[4]) {
-                                 const int* of = s_bucket + buf * widths + bias_place - Bias::place(place) + at(j);
-                                 float* mine = s_sums + wave * sums_a_wave + (anew<256>((int)threadIdx.x) & 63);
-#pragma unroll
-                                 for (int i = 0; i < 4; ++i) __hip_atomic_fetch_add(mine + of[i], e[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                             });
+                             [&](int j) {
+                                 const float* own = s_bias + buf * a.bias_words + bias_from + at(j);
+                                 return make_float4(own[0], own[1], own[2], own[3]);
+                             },
+                             [&](int j, int i) { return s_bucket[buf * widths + bias_place - Learned::place(place) + at(j) + i]; },
+                             s_sums + wave * sums_a_wave + (anew<256>((int)threadIdx.x) & 31), run, even);
+                if (summed && !uneven)
+                    run.add(s_sums + wave * sums_a_wave + (anew<256>((int)threadIdx.x) & 31), a.bucket_words[front ? 0 : 2 * a.reach] & ~1, even);
                 weigh<T, DP>(smem[buf][0], b, d, dq, lanes);
                 if (sizeof(T) == 2 && (cut || docs || late || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dq, lanes);
             }
         }
         buf ^= 1;
     }
-    __syncthreads();                                                      // (tiles are no longer read)
+    __syncthreads();                                                      // (tiles are no longer read, and the sums are there)
     if (summed) {
-        // a bucket's sums of a head's lanes added up, a thread each, the four wavefronts' rows one after the other
+        run.flush(s_sums + wave * sums_a_wave + col);
+        __syncthreads();
+        // A bucket's sums of a head's lanes added up by `slices` neighbouring threads, a share of the rows each, which start at other rows from bucket to
+        // bucket (all buckets have a row's sums in one bank).  Row r0 + x has head x % group less r0's.
         float* const to = a.bias_parts + ((int64_t)part * a.bias_blocks + (int64_t)q.q0 * a.group / FIXED + s + w.block) * a.n_buckets * a.heads;
-        for (int i = threadIdx.x; i < a.n_buckets * a.group; i += 256) {
-            const int b = i / a.group, h = i - b * a.group;
+        const int outs = a.n_buckets * a.group, most = min(256 / outs, 32), slices = most < 1 ? 1 : 1 << (31 - __builtin_clz(most)), slice = threadIdx.x & (slices - 1);
+        for (int first = 0; first < outs; first += 256 / slices) {
+            const int i = first + (int)threadIdx.x / slices, b = i / a.group, h = i - b * a.group;
+            const int x0 = (h + a.group - r0 % a.group) % a.group, n = (FIXED - x0 + a.group - 1) / a.group, turns = (FIXED / a.group + slices) / slices;
             float sum = 0.f;
-            // (row r0 + x has head (r0 + x) % group; both halves of a wavefront have its rows)
-            for (int x = (h + a.group - r0 % a.group) % a.group; x < FIXED; x += a.group) {
-                const float* of = s_sums + (x >> 5) * sums_a_wave + b * 64 + (x & 31);
-                sum += of[0] + of[32];
-            }
-            to[b * a.heads + hk * a.group + h] = sum;
+            if (i < outs)
+                for (int k = 0; k < turns; ++k) {
+                    const int m = slice + slices * ((k + i) % turns), x = x0 + m * a.group;
+                    if (m >= n) continue;
+                    sum += s_sums[(x >> 5) * sums_a_wave + b * 32 + (x & 31)];
+                }
+            for (int o = 1; o < slices; o *= 2) sum += __shfl_xor(sum, o, 64);
+            if (i < outs && slice == 0) to[b * a.heads + hk * a.group + h] = sum;
         }
     }
     if (wr0 >= rows) return;
     unsigned char* const mine = smem[0][0] + wave * PUT_BYTES;
     static_assert(sizeof(smem) >= 4 * PUT_BYTES, "rows on their way out");
+    int64_t to_token = token;
+    int to_head = head;
+    if (BIASED) {                                                         // (worked out again: registers)
+        const int own = min(wr0 + (anew<256>((int)threadIdx.x) & 31), rows - 1), of = (int)over_group(a, own);
+        to_token = q.q0 + of;
+        to_head = hk * a.group + own - of * a.group;
+    }
     if (a.parts > 1)
         put_rows<float, DP>(mine, dq, 1.f, a.head_dim,
-                            live ? a.part_o + (((int64_t)part * a.n_q + token) * a.heads + head) * a.head_dim : nullptr);
+                            live ? a.part_o + (((int64_t)part * a.n_q + to_token) * a.heads + to_head) * a.head_dim : nullptr);
     else
-        put_rows<T, DP>(mine, dq, by_x<T>(a), a.head_dim, live ? (T*)a.dq + token * a.dqs.row + head * a.dqs.head : nullptr);
+        put_rows<T, DP>(mine, dq, by_x<T>(a), a.head_dim, live ? (T*)a.dq + to_token * a.dqs.row + to_head * a.dqs.head : nullptr);
 }
 
 // A gradient's shares added up, a thread four neighbours: those of queries (z = 0), keys (1) and values (2).  3365 tokens, 8 heads of 80 on 4,
@@ -646,26 +762,32 @@ __global__ __launch_bounds__(256) void add_sinks_kernel(Args a) {
     }
 }
 
-// A learned bias's gradient from the sums of blocks of rows: 64 values a workgroup, four threads to each, a fourth of the blocks each.  Blocks are counted
-// over all of the tensor's rows, so that some belong to no sequence: those are left out.
-__global__ __launch_bounds__(256) void add_bias_kernel(Args a, float* dbias) {
-    __shared__ float s_sum[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n_buckets * a.heads, i = blockIdx.x * 64 + lane;
+// A learned bias's gradient from the sums of blocks of rows (zeros for blocks that there are not): 64 values a workgroup, `each` blocks, the sixteen
+// wavefronts taking turns; then, where those are not all, what they made of it in the same way.
+__global__ __launch_bounds__(1024) void add_bias_kernel(const float* from, int64_t blocks, int64_t each, int n, float* to) {
+    __shared__ float s_sum[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + lane;
+    const int64_t b0 = blockIdx.y * each, b1 = min(blocks, b0 + each);
     float sum = 0.f;
-    for (int s = 0; s < a.n_seq; ++s) {
-        Seq q;
-        if (!sequence(a, s, q)) continue;
-        const int blocks = (q.qn * a.group + FIXED - 1) / FIXED;
-        const float* from = a.bias_parts + ((int64_t)q.q0 * a.group / FIXED + s) * n + i;
-        for (int b = wave; b < blocks; b += 4) {
-            const int parts = shares_of<false, true>(a, q, b);
-            for (int p = 0; p < parts; ++p)
-                if (i < n) sum += from[((int64_t)p * a.bias_blocks + b) * n];
-        }
+    if (i < n) {
+#pragma unroll 8
+        for (int64_t b = b0 + wave; b < b1; b += 16) sum += from[b * n + i];
     }
     s_sum[wave][lane] = sum;
     __syncthreads();
-    if (wave == 0 && i < n) dbias[i] = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
+    if (wave != 0 || i >= n) return;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) sum += s_sum[w][lane];
+    to[(int64_t)blockIdx.y * n + i] = sum;
+}
+void add_bias(const Args& a, float* dbias, hipStream_t st) {
+    const int n = a.n_buckets * a.heads;
+    const int64_t blocks = a.parts * a.bias_blocks, each = blocks > 256 ? 128 : 256, chunks = (blocks + each - 1) / each;
+    const unsigned across = (unsigned)((n + 63) / 64);
+    float* const between = chunks > 1 ? a.bias_parts + blocks * n : dbias;
+    hipLaunchKernelGGL(add_bias_kernel, dim3(across, (unsigned)(chunks > 1 ? chunks : 1)), dim3(1024), 0, st, a.bias_parts, blocks, each, n, between);
+    if (chunks > 1) hipLaunchKernelGGL(add_bias_kernel, dim3(across), dim3(1024), 0, st, between, chunks, chunks, n, dbias);
 }
 
 template <typename T, int DP, bool LOCAL, bool BIASED>
@@ -686,10 +808,10 @@ void launch(const Args& a, hipStream_t st) {
     const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED, apart = min(key_blocks, (int64_t)a.sink_blocks);
     const int64_t key_jobs = a.kv_heads * (apart * a.sink_parts + (key_blocks - apart) * a.key_parts);
     const unsigned tile_lds = BIASED ? 2 * a.bias_words * sizeof(float) : 0;
-    const unsigned sums_lds = a.bias_parts ? (2 * ((a.bias_width + 63) & ~63) + 4 * (a.n_buckets + 1) * 64) * sizeof(float) : 0;
+    const unsigned sums_lds = a.bias_parts ? (2 * ((a.bias_width + 63) & ~63) + 4 * (a.n_buckets + 1) * 32) * sizeof(float) : 0;
     if (BIASED && tile_lds + sums_lds > 32 << 10) {
         static bool lds_attr_set = false;     // raising the limit twice is harmless, so no lock
-        if (!lds_attr_set && hipFuncSetAttribute((const void*)query_gradients_kernel<T, DP, LOCAL, BIASED>, hipFuncAttributeMaxDynamicSharedMemorySize, 92 << 10) != hipSuccess) return;
+        if (!lds_attr_set && hipFuncSetAttribute((const void*)query_gradients_kernel<T, DP, LOCAL, BIASED>, hipFuncAttributeMaxDynamicSharedMemorySize, 64 << 10) != hipSuccess) return;
         lds_attr_set = true;
     }
     in_turn(row_jobs, a.n_seq, [&](unsigned n) {
@@ -697,7 +819,7 @@ void launch(const Args& a, hipStream_t st) {
         hipLaunchKernelGGL((query_gradients_kernel<T, DP, LOCAL, BIASED>), dim3((unsigned)row_jobs * n), dim3(256), tile_lds + sums_lds, st, b);
     });
     in_turn(key_jobs, a.n_seq, [&](unsigned n) {
-        b.listed = add_up(n, key_blocks, max(a.key_parts, a.sink_parts));
+        b.listed = add_up(n, key_blocks, a.key_parts);
         if (BIASED) set_width(b, FIXED + (a.key_tile - 1) / a.group + 2);
         hipLaunchKernelGGL((key_gradients_kernel<T, DP, LOCAL, BIASED>), dim3((unsigned)key_jobs * n), dim3(256), BIASED ? 2 * b.bias_words * sizeof(float) : 0, st, b);
     });
@@ -729,15 +851,11 @@ int backward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const
     p.a.status = status;
     if (dbias && (p.a.n_buckets == 0 || (uintptr_t)dbias % 4 != 0)) return PS_EINVAL;
     if (!dbias) p.a.bias_parts = nullptr;
-    auto add_bias = [&](int32_t n_seq) {
-        Args b = p.a;
-        b.n_seq = n_seq;
-        if (dbias) hipLaunchKernelGGL(add_bias_kernel, dim3((unsigned)((b.n_buckets * b.heads + 63) / 64)), dim3(256), 0, (hipStream_t)hip_stream, b, dbias);
-    };
     if (p.a.n_seq == 0 || (p.a.n_q == 0 && p.a.n_k == 0)) {
-        if (dbias) {
+        if (dbias) {                       // (a sum over no blocks)
             (void)hipGetLastError();
-            add_bias(0);
+            p.a.bias_blocks = 0;
+            add_bias(p.a, dbias, (hipStream_t)hip_stream);
             if (hipGetLastError() != hipSuccess) return PS_EHIP;
         }
         return check_sequences(p.a, (hipStream_t)hip_stream);
@@ -757,7 +875,7 @@ int backward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const
     if (a.max_q == 0 && check_sequences(a, st) != PS_OK) return PS_EHIP;   // (else the queries' launch finds them)
     (void)hipGetLastError();
     summarise_documents(a, st);
-    if (LOCAL) make_table(a, local, LOG2E, st);
+    if (LOCAL) make_table(a, local, a.slope_by, st);                           // (and clears the sums of blocks)
     auto of_type = [&](auto biased) {
         constexpr bool B = decltype(biased)::value;
         switch (padded(desc->head_dim)) {
@@ -769,7 +887,7 @@ int backward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const
     if constexpr (LOCAL) {
         if (a.table) {
             of_type(std::true_type());
-            add_bias(a.n_seq);
+            if (dbias) add_bias(a, dbias, st);
             return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
         }
     }

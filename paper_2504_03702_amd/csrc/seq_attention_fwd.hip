@@ -43,16 +43,25 @@ struct Row {
 
     // A tile of keys from k0 on and its values.  cut: some of the wavefront's rows see only the keys in front of their `end`; docs: documents
     // of its keys, null if the tile's and all rows' are one; late: some of the rows' windows begin behind keys that are not in front of a.sinks;
-    // bias(i): the learned bias of key k0 + i, null if there is none.
-    template <typename Bias>
-    __device__ __forceinline__ void step(const Args& a, const unsigned char* keys, const unsigned char* values, const int* docs, int k0, bool cut, bool late, Bias bias) {
+    // uneven: the learned bias of key k0 + i is bias(i), else `even` for all of them, in powers of two.
+    template <typename Of>
+    __device__ __forceinline__ void step(const Args& a, const unsigned char* keys, const unsigned char* values, const int* docs, int k0, bool cut, bool late, bool uneven,
+                                         float even, Of bias) {
         f32x16 sc[L::BLOCKS];
+        const bool first = BIASED && uneven && a.cap == 0.f;              // (the bias is what the products start from)
 #pragma unroll
         for (int b = 0; b < L::BLOCKS; b += 2) {
-            if constexpr (L::BLOCKS % 2 == 0)
-                dots<T, DP>(keys, b, qf, sc[b], keys, b + 1, qf, sc[b + 1], lanes);
-            else
+            auto start = [&](int b) { return Learned::start(first, half, [&](int i) { return bias(32 * b + i); }); };
+            if constexpr (L::BLOCKS % 2 == 0) {
+                if constexpr (BIASED)
+                    dots<T, DP>(keys, b, qf, sc[b], keys, b + 1, qf, sc[b + 1], lanes, start(b), start(b + 1));
+                else
+                    dots<T, DP>(keys, b, qf, sc[b], keys, b + 1, qf, sc[b + 1], lanes);
+            } else if constexpr (BIASED) {
+                sc[b] = dot<T, DP>(keys, b, qf, lanes, start(b));
+            } else {
                 sc[b] = dot<T, DP>(keys, b, qf, lanes);
+            }
         }
         float c = a.scale * LOG2E;
         if (a.cap > 0.f) {
@@ -77,7 +86,7 @@ struct Row {
                 for (int e = 0; e < 16; ++e) sc[b][e] = fmaf(-slope, fabsf(from - (float)(32 * b + row_of(e))), sc[b][e]);
         }
         if constexpr (LOCAL) {
-            if (BIASED) {
+            if (BIASED && uneven && !first) {
 #pragma unroll
                 for (int b = 0; b < L::BLOCKS; ++b)
 #pragma unroll
@@ -117,6 +126,7 @@ struct Row {
             for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[b][e]);
         const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
         mx = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1])) * c;
+        if (BIASED) mx += even;
         // the reference follows the maximum lazily: it moves when a tile exceeds it by more than SLACK, so weights reach
         // 2^SLACK and the accumulators are rescaled a few times a row instead of at nearly every tile
         if (__any(mx > m + SLACK)) {
@@ -129,7 +139,7 @@ struct Row {
                 for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
             l *= alpha;
         }
-        const float ref = m == -INFINITY ? 0.f : m;                   // (a row that has seen nothing yet)
+        const float ref = (m == -INFINITY ? 0.f : m) - (BIASED ? even : 0.f);   // (a row that has seen nothing yet)
 #pragma unroll
         for (int b = 0; b < L::BLOCKS; ++b) {
             Weights<T> w, rest;
@@ -231,7 +241,13 @@ __global__ __launch_bounds__(256, DP == 64 && !BIASED ? 3 : 2) void attend_kerne
         if (LOCAL) return k0 + L::ROWS > wend;
         return k0 + L::ROWS > q.kn || (a.causal && k0 + L::ROWS - 1 > wnear && k0 + L::ROWS > q.prefix);
     };
-    const int place = Bias::place(far);
+    // A learned bias is one for all that is further than `reach` in front of the row, or behind it; keys that some of the workgroup's rows have nearer
+    const int place = Learned::place(far);
+    const int wide_from = BIASED ? Learned::place(q.start + (int)over_group(a, r0)) - a.reach + 1 : 0, wide_to = BIASED ? (int)min((int64_t)far + a.reach, (int64_t)INT32_MAX) : 0;
+    const float* const ends = BIASED ? a.table + (int64_t)row.head * (2 * a.reach + 1) : nullptr;
+    const float in_powers = a.cap > 0.f ? 1.f : a.scale * LOG2E;
+    const float bias_front = BIASED ? ends[0] * in_powers : 0.f, bias_behind = BIASED ? ends[2 * a.reach] * in_powers : 0.f;
+    const int wnear_place = Learned::place(wnear), wfar_place = (int)min((int64_t)wfar, (int64_t)INT32_MAX - a.reach);   // (a key is below 2^30)
 
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
@@ -249,7 +265,7 @@ __global__ __launch_bounds__(256, DP == 64 && !BIASED ? 3 : 2) void attend_kerne
             values.rows(smem[buf][1], a.head_dim, there, [&](int i) { return vbase + (k0 + i) * a.vs.row; });
         }
         if (a.k_docs && wave == 0) send_words(s_doc[buf], a.k_docs + q.k0 + min(k0 + lane, q.kn - 1));
-        if (BIASED) Bias::send(hk, k0 - place, s_bias + buf * a.bias_words);
+        if (BIASED && scalar(k0 + L::ROWS > wide_from && k0 < wide_to)) Learned::send(hk, k0 - place, s_bias + buf * a.bias_words);
     };
 
     Walk walk;
@@ -265,9 +281,10 @@ __global__ __launch_bounds__(256, DP == 64 && !BIASED ? 3 : 2) void attend_kerne
         // (a wavefront whose rows all stand before the tile, or whose windows do, has nothing in it)
         const bool none = LOCAL ? k0 >= wend_far || (k0 + L::ROWS <= wbegin_near && k0 >= a.sinks) : a.causal && k0 > wfar && k0 >= q.prefix;
         if (wr0 < rows && !none) {
-            const float* bias = BIASED ? s_bias + buf * a.bias_words + (row.head - hk * a.group) * a.bias_width + place - Bias::place(row.place) : nullptr;
-            row.step(a, smem[buf][0], smem[buf][1], one ? nullptr : s_doc[buf], k0, is_cut(k0), LOCAL && k0 < wbegin && k0 + L::ROWS > a.sinks,
-                     [&](int i) { return bias[i]; });
+            const float* bias = BIASED ? s_bias + buf * a.bias_words + (row.head - hk * a.group) * a.bias_width + place - Learned::place(row.place) : nullptr;
+            const bool front = BIASED && k0 + L::ROWS - 1 <= wnear_place - a.reach, uneven = BIASED && !front && k0 < wfar_place + a.reach;
+            row.step(a, smem[buf][0], smem[buf][1], one ? nullptr : s_doc[buf], k0, is_cut(k0), LOCAL && k0 < wbegin && k0 + L::ROWS > a.sinks, uneven,
+                     uneven ? 0.f : front ? bias_front : bias_behind, [&](int i) { return bias[i]; });
         }
         buf ^= 1;
     }
@@ -399,7 +416,9 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
         if (sent < t1) send_next();
     Row<T, DP, 32, LOCAL, BIASED> row(a, q, hk, min(col, rows - 1), col < rows);
     const float* table = BIASED ? a.table + (int64_t)row.head * (2 * a.reach + 1) + a.reach : nullptr;
-    const int place = Bias::place(row.place);
+    const int place = Learned::place(row.place), near_place = Learned::place(near), far_place = (int)min((int64_t)far, (int64_t)INT32_MAX - a.reach);
+    const float in_powers = a.cap > 0.f ? 1.f : a.scale * LOG2E;
+    const float bias_front = BIASED ? table[-a.reach] * in_powers : 0.f, bias_behind = BIASED ? table[a.reach] * in_powers : 0.f;
     while (t < t1) {
         // (with a tile behind it every send of this one is WAIT sends old; the last ones wait for all)
         if (STAGES > 1 && sent < t1)
@@ -408,8 +427,9 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
             vm_wait();
         const int k0 = span.at<LOCAL>(t) * 32;
         const bool cut = LOCAL ? k0 + 32 > end : k0 + 32 > q.kn || (a.causal && k0 + 31 > near && k0 + 32 > q.prefix);
+        const bool front = BIASED && k0 + 31 <= near_place - a.reach, uneven = BIASED && !front && k0 < far_place + a.reach;
         row.step(a, smem[wave][stage][0], smem[wave][stage][1], a.k_docs ? s_doc[wave][stage] : nullptr, k0, cut,
-                 LOCAL && k0 < begin && k0 + 32 > a.sinks, [&](int i) { return table[max(-a.reach, min(k0 + i - place, a.reach))]; });
+                 LOCAL && k0 < begin && k0 + 32 > a.sinks, uneven, uneven ? 0.f : front ? bias_front : bias_behind, [&](int i) { return table[max(-a.reach, min(k0 + i - place, a.reach))]; });
         asm volatile("" ::: "memory");                                    // (its reads are over: their products are on their way)
         stage = stage + 1 < STAGES ? stage + 1 : 0;
         t = walk.next(t + 1, t1, classify);
@@ -574,15 +594,22 @@ __global__ __launch_bounds__(256) void check_kernel(Args a) {
 }
 
 // The learned bias of every distance, a thread each of a head's, `by` times what the caller has (none for a bucket that there is not), and
-// where its bucket is in a lane's sums.
+// where its bucket is in a lane's sums.  The threads clear what the sums of blocks of rows go to, too, since some blocks belong to no sequence.
 __global__ __launch_bounds__(256) void table_kernel(const int32_t* buckets, const float* bias, float* table, int32_t* words, int reach, int n_buckets, int heads,
-                                                    float by) {
+                                                    float by, float* sums, int64_t n_sums) {
     const int d = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y;
-    if (d > 2 * reach) return;
+    const int64_t threads = (int64_t)gridDim.x * gridDim.y * 256;
+    for (int64_t i = ((int64_t)h * gridDim.x + blockIdx.x) * 256 + threadIdx.x; i < n_sums; i += threads) sums[i] = 0.f;
+    if (d > 2 * reach || h >= heads) return;
     const int b = buckets[d];
     const bool is = b >= 0 && b < n_buckets;
     table[(int64_t)h * (2 * reach + 1) + d] = is ? bias[(int64_t)b * heads + h] * by : 0.f;
-    if (words && h == 0) words[d] = (is ? b : n_buckets) * 64;
+    if (words && h == 0) {
+        // (its lowest bit: the next three distances have the same bucket)
+        bool same = true;
+        for (int i = 1; i < 4; ++i) same = same && buckets[min(d + i, 2 * reach)] == b;
+        words[d] = (is ? b : n_buckets) * 32 + (same ? 1 : 0);
+    }
 }
 
 template <typename T, int DP, bool LOCAL, bool BIASED>
@@ -677,7 +704,7 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
     // some 2048 shares of a length, of 256 keys (rows) or more each (fp32, one sequence of 3571, 12 heads of 80: 1024, 2048, 4096 shares 1766, 1602,
     // 1684 us a pass; bf16, 8192 tokens of 4 heads of 64: 430, 432, 620).  What blocks and tiles there are is estimated from the tensors'
     // rows: lengths stand on the device.
-    a.tile = tile_rows(d->dtype == 1 ? 2 : 4);
+    a.tile = query_tile_rows(d->dtype == 1 ? 2 : 4, padded(d->head_dim), backward && local && local->n_buckets > 0);
     a.key_tile = key_tile_rows(d->dtype == 1 ? 2 : 4, padded(d->head_dim));
     // What a row sees of a sequence at most, and what sees a key: with a window, that of a block of rows (keys) and its first keys.
     const int64_t rows_a_seq = (int64_t)a.max_q * group;
@@ -784,7 +811,7 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         set_width(a, a.tile + (FIXED - 1) / a.group + 2);   // (a tile of keys by FIXED rows)
         if (backward) {
             a.bias_blocks = d->n_q * group / FIXED + d->n_seq + 1;
-            a.bias_parts = (float*)take(sizeof(float) * (size_t)a.parts * a.bias_blocks * a.n_buckets * a.heads);
+            a.bias_parts = (float*)take(sizeof(float) * ((size_t)a.parts * a.bias_blocks + (size_t)a.parts * a.bias_blocks / 128 + 1) * a.n_buckets * a.heads);
         }
     }
     p.bytes = off > 0 ? off : 256;     // (0 says that a call is refused)
@@ -805,8 +832,12 @@ void summarise_documents(const Args& a, hipStream_t st) {
 
 void make_table(const Args& a, const ps_attention_local* local, float by, hipStream_t st) {
     if (!a.table) return;
-    hipLaunchKernelGGL(table_kernel, dim3((2 * a.reach + 256) / 256, a.heads), dim3(256), 0, st, local->buckets, local->bias, const_cast<float*>(a.table),
-                       const_cast<int32_t*>(a.bucket_words), a.reach, a.n_buckets, a.heads, by);
+    const int64_t n_sums = a.bias_parts ? a.parts * a.bias_blocks * a.n_buckets * a.heads : 0;
+    const unsigned across = (2 * a.reach + 256) / 256;
+    unsigned rows = a.heads;
+    while ((int64_t)rows * across * 2048 < n_sums && rows * across < 1024) rows *= 2;
+    hipLaunchKernelGGL(table_kernel, dim3(across, rows), dim3(256), 0, st, local->buckets, local->bias, const_cast<float*>(a.table),
+                       const_cast<int32_t*>(a.bucket_words), a.reach, a.n_buckets, a.heads, by, a.bias_parts, n_sums);
 }
 
 int check_sequences(const Args& a, hipStream_t st) {
