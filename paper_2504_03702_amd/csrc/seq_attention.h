@@ -55,8 +55,8 @@ struct Args {
     float slope_by, cap_in;            // see Row and Cap
     // ps_local_attention_*() alone, whose kernels are the same with LOCAL:
     int32_t left, right, sinks;        // a row's window, and the first keys that it sees all the same
-    int32_t sink_blocks, sink_parts, sink_part_tiles;   // blocks of keys that have some of those, if they are shared out apart
-    float *sink_dk, *sink_dv;          // [sink_parts][n_seq][sink_blocks * FIXED][kv_heads][head_dim]
+    int32_t sink_blocks, sink_parts, sink_part_tiles;   // those in blocks of 32, shares of their tiles of 32 rows
+    float *sink_dk, *sink_dv;          // [sink_parts][n_seq][sink_blocks * 32][kv_heads][head_dim]
     const float* table;                // [heads][2 reach + 1]: the learned bias of a distance, null without one (see Learned)
     const int32_t* bucket_words;       // [2 reach + 1]: where in a lane's sums the distance's bucket is
     float* bias_parts;                 // [parts][blocks of rows][buckets][heads]: sums of a bucket's gradients, null if not wanted
@@ -133,24 +133,18 @@ __device__ __forceinline__ Span key_tiles(const Args& a, const Seq& q, int r0) {
     }
     return s;
 }
-// Tiles of rows, from `first` on and in front of the returned one, that may see some of the FIXED keys from k0 on.  Shares are of these.
+// Tiles of rows, from `first` on and in front of the returned one, that may see some of the FIXED keys from k0 on (in their windows: the first keys
+// have a launch of their own).  Shares are of these.
 template <bool LOCAL>
 __device__ __forceinline__ int row_tiles(const Args& a, const Seq& q, int k0, int& first) {
     const int rows = q.qn * a.group, n = (rows + a.key_tile - 1) / a.key_tile;
     first = a.causal && k0 >= q.prefix ? (int)min((int64_t)n, max((int64_t)0, (int64_t)(k0 - q.start) * a.group / a.key_tile)) : 0;
-    if (!LOCAL || k0 < a.sinks) return n;
+    if (!LOCAL) return n;
     auto tile_of = [&](int64_t place) { return (int)min((int64_t)n, max((int64_t)0, (place - q.start) * a.group / a.key_tile)); };
     first = max(first, tile_of((int64_t)k0 - a.right));
     const int64_t behind = (int64_t)min(k0 + FIXED, q.kn) + a.left - q.start;   // the first token that none of them is seen by
     return max(first, behind >= q.qn ? n : behind <= 0 ? 0 : (int)((behind * a.group + a.key_tile - 1) / a.key_tile));
 }
-// The shares that a block of keys' row tiles may have, and a share's tiles.
-template <bool LOCAL>
-__device__ __forceinline__ bool shared_apart(const Args& a, int block) { return LOCAL && block < a.sink_blocks; }
-template <bool LOCAL>
-__device__ __forceinline__ int key_parts_of(const Args& a, int block) { return shared_apart<LOCAL>(a, block) ? a.sink_parts : a.key_parts; }
-template <bool LOCAL>
-__device__ __forceinline__ int key_part_tiles_of(const Args& a, int block) { return shared_apart<LOCAL>(a, block) ? a.sink_part_tiles : a.key_part_tiles; }
 __device__ __forceinline__ int shares(int tiles, int parts, int part_tiles) { return max(1, min(parts, (tiles + part_tiles - 1) / part_tiles)); }
 
 // A workgroup's part of a launch over blocks of rows (of keys, with KEYS) and shares of their tiles.
@@ -170,10 +164,10 @@ template <bool KEYS, bool LOCAL>
 __device__ __forceinline__ int shares_of(const Args& a, const Seq& q, int block) {
     const int n = KEYS ? q.kn : q.qn * a.group;
     if (block * FIXED >= n) return 0;
-    if ((KEYS ? key_parts_of<LOCAL>(a, block) : a.parts) == 1) return 1;
+    if ((KEYS ? a.key_parts : a.parts) == 1) return 1;
     int first = 0;
     const int tiles = KEYS ? row_tiles<LOCAL>(a, q, block * FIXED, first) : key_tiles<LOCAL>(a, q, block * FIXED).tiles;
-    return shares(tiles - first, KEYS ? key_parts_of<LOCAL>(a, block) : a.parts, KEYS ? key_part_tiles_of<LOCAL>(a, block) : a.part_tiles);
+    return shares(tiles - first, KEYS ? a.key_parts : a.parts, KEYS ? a.key_part_tiles : a.part_tiles);
 }
 // a.listed (at most 64 sequences of at most 64 blocks): the grid has a workgroup for what there could be, and the first so many take
 // what there is, found by adding it up a sequence to a lane.  Counted as the grid counts, what there is lay anywhere among it, and
@@ -186,16 +180,6 @@ __device__ __forceinline__ bool look_for_work(const Args& a, Seq& q, Work& w) {
     unsigned id = blockIdx.x;
     w.hk = id % a.kv_heads;
     id /= a.kv_heads;
-    if (LOCAL && KEYS && !a.listed && a.sink_blocks > 0) {                // (the longest first: blocks whose rows are shared out apart)
-        const int apart = min(a.sink_blocks, blocks) * a.sink_parts;
-        const unsigned jobs = apart + max(0, blocks - a.sink_blocks) * parts;
-        const unsigned first = id / (jobs * a.together) * a.together, rest = id - first * jobs, here = min((unsigned)a.together, a.seqs - first);
-        const int job = rest / here;
-        w.s = a.seq0 + first + rest % here;
-        w.block = job < apart ? job / a.sink_parts : a.sink_blocks + (job - apart) / parts;
-        w.part = job < apart ? job % a.sink_parts : (job - apart) % parts;
-        return sequence(a, w.s, q) && w.block * FIXED < q.kn;
-    }
     if (!a.listed) {
         w.part = id % parts;
         id /= parts;
@@ -550,6 +534,49 @@ __device__ __forceinline__ void send_words(void* to, const void* from) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)to, 4, 0, 0);
 }
 __device__ __forceinline__ void vm_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Tiles of 32 rows that a wavefront has to itself, by sends of its own.
+template <typename T, int DP>
+struct Few {
+    using L = Tile<T, DP, 32>;
+    static constexpr int SENDS = L::BYTES / 1024;                         // of 64 lanes, for a tile
+    // Tiles of a wavefront in LDS: two, or one of the largest; up to 128 KB of a unit's 160, in bf16 with heads of 64 by two workgroups.
+    static constexpr int STAGES = L::BYTES > 8192 ? 1 : 2, WORKGROUPS = L::BYTES > 4096 ? 1 : 2;
+    // Sends whose lanes' chunks differ; the others repeat them so many rows on (sends of no whole number of rows: none does).
+    static constexpr int PERIOD = 64 % L::CPR == 0 ? L::CPR / 4 : SENDS, ROWS_A_PERIOD = 64 * PERIOD / L::CPR;
+    static constexpr int WAIT = (STAGES - 1) * (2 * SENDS + 1);           // sends behind the oldest tile's, and a word for documents
+    unsigned off[2][PERIOD];
+    int64_t step[2];                                                      // bytes from row to row
+    __device__ __forceinline__ Few(const Args& a) : step{a.ks.row * L::EB, a.vs.row * L::EB} {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < PERIOD; ++j) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) off[x][j] = (unsigned)row_of(j, lane) * (unsigned)step[x] + element(j, lane, a.head_dim) * L::EB;
+        }
+    }
+    static __device__ __forceinline__ int row_of(int j, int lane) { return (j * 64 + lane) / L::CPR; }
+    static __device__ __forceinline__ int element(int j, int lane, int head_dim) {
+        return min((((j * 64 + lane) % L::CPR) ^ L::swz(row_of(j, lane))) * L::EPC, head_dim - L::EPC);
+    }
+    static __device__ __forceinline__ void send(unsigned char* tile, int j, const void* from) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)(tile + j * 1024), 16, 0, 0);
+    }
+    __device__ __forceinline__ void whole(unsigned char* tile, int x, const void* first) const {
+#pragma unroll
+        for (int j = 0; j < SENDS; ++j) send(tile, j, (const char*)first + j / PERIOD * ROWS_A_PERIOD * step[x] + off[x][j % PERIOD]);
+    }
+    // row(i): address of row i; there: bit i tells whether it is one, and not zeros
+    template <typename Address>
+    static __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, uint64_t there, Address row) {
+        const int lane = anew<256>((int)(threadIdx.x & 63));
+#pragma unroll
+        for (int j = 0; j < SENDS; ++j) {
+            const int i = row_of(j, lane);
+            send(tile, j, there >> i & 1 ? (const void*)(row(i) + element(j, lane, head_dim)) : (const void*)&zeros);
+        }
+    }
+};
 
 // ---- which tiles are seen: 64 of them at a time, a lane each, as masks ----------------------------------------------------
 // (scalars: the compiler does not see that all lanes have the same, and would count and address tiles in vector registers)

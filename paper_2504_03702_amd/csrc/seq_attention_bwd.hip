@@ -173,6 +173,13 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
     }
 }
 
+// Tiles of 32 rows that may see some of the 32 first keys from k0 on: from `first` on, in front of the returned one.
+__device__ __forceinline__ int first_keys_rows(const Args& a, const Seq& q, int k0, int& first) {
+    const int n = (q.qn * a.group + 31) / 32;
+    first = a.causal && k0 >= q.prefix ? (int)min((int64_t)n, max((int64_t)0, (int64_t)(k0 - q.start) * a.group / 32)) : 0;
+    return n;
+}
+
 template <typename T>
 __device__ __forceinline__ float by_x(const Args& a) { return a.cap > 0.f && sizeof(T) == 2 ? 4.f * a.scale : a.scale; }
 
@@ -203,8 +210,8 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int rows = q.qn * a.group;
     int first_tile;
-    const int tiles = row_tiles<LOCAL>(a, q, k0, first_tile), each = key_part_tiles_of<LOCAL>(a, w.block);
-    const int t0 = first_tile + part * each, t1 = min(tiles, t0 + each);
+    const int tiles = row_tiles<LOCAL>(a, q, k0, first_tile);
+    const int t0 = first_tile + part * a.key_part_tiles, t1 = min(tiles, t0 + a.key_part_tiles);
     if (part > 0 && t0 >= tiles) return;                                  // (part 0 writes, rows or not)
 
     // this lane's key
@@ -346,9 +353,9 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         if (LOCAL) {
             const ArgsAgain w = again();
             const int64_t left = w->left, right = w->right;
-            const int near = q.start + (int)over_group(a, t * L::ROWS), sinks = w->sinks;
-            late = wlast >= sinks && (near + right < wlast || far - left > max(wk0, sinks));
-            none = wk0 >= sinks && (far + right < wk0 || near - left > wlast);
+            const int near = q.start + (int)over_group(a, t * L::ROWS);
+            late = near + right < wlast || far - left > wk0;
+            none = far + right < wk0 || near - left > wlast;
         }
         t = walk.next(t + 1, t1, classify);
         vm_wait();
@@ -408,7 +415,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
 #pragma unroll
                                  for (int i = 0; i < 4; ++i) {
                                      const int off = (&place.x)[i] - own;   // (a row's place less the key's)
-                                     is[i] = (off <= a.left && off >= -a.right) || k0 + own < a.sinks;
+                                     is[i] = off <= a.left && off >= -a.right;
                                  }
                              },
                              [&](int j) {
@@ -429,16 +436,9 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
     unsigned char* const mine = smem[0][0] + wave * PUT_BYTES;
     static_assert(sizeof(smem) >= 4 * PUT_BYTES, "rows on their way out");
     const int own = wk0 + (anew<256>((int)threadIdx.x) & 31);              // (the key, worked out again)
-    const bool is = own < q.kn;
+    const bool is = own < q.kn && !(LOCAL && own < again()->sinks);              // (the first keys' gradients have a launch of their own)
     const int64_t to = q.k0 + own;
-    if (shared_apart<LOCAL>(a, w.block)) {
-        if (a.sink_parts > 1) {
-            const int64_t at = ((((int64_t)part * a.n_seq + s) * a.sink_blocks * FIXED + own) * a.kv_heads + hk) * a.head_dim;
-            put_rows<float, DP>(mine, dk, 1.f, a.head_dim, is ? a.sink_dk + at : nullptr);
-            put_rows<float, DP>(mine, dv, 1.f, a.head_dim, is ? a.sink_dv + at : nullptr);
-            return;
-        }
-    } else if (a.key_parts > 1) {
+    if (a.key_parts > 1) {
         const int64_t at = (((int64_t)part * a.n_k + to) * a.kv_heads + hk) * a.head_dim;
         put_rows<float, DP>(mine, dk, 1.f, a.head_dim, is ? a.part_dk + at : nullptr);
         put_rows<float, DP>(mine, dv, 1.f, a.head_dim, is ? a.part_dv + at : nullptr);
@@ -697,6 +697,180 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
         put_rows<T, DP>(mine, dq, by_x<T>(a), a.head_dim, live ? (T*)a.dq + to_token * a.dqs.row + to_head * a.dqs.head : nullptr);
 }
 
+// The first keys, which rows see wherever they stand: dk and dv of 32 of them and of a share of the rows that may see them, whose tiles the workgroup's wavefronts
+// take in turn, each with tiles of its own on their way through LDS; what they have is put together at the end.
+template <typename T, int DP, bool BIASED>
+__global__ __launch_bounds__(256, 1) void first_keys_kernel(Args a) {
+    using F = Few<T, DP>;
+    using L = typename F::L;
+    constexpr int STAGES = F::STAGES;
+    enum Word { LSE, DELTA, SLOPE, FRONT, DOC, PLACE, TABLE, WORDS };
+    __shared__ __align__(1024) unsigned char smem[4][STAGES][2][L::BYTES];   // [wavefront][stage][queries, dout]; at the end the wavefronts' sums
+    __shared__ __align__(16) float s_word[4][STAGES][WORDS][64];          // what rows bring along; PLACE and TABLE are integers
+    static_assert(sizeof(smem) >= 4 * 2 * 32 * DP * sizeof(float), "the wavefronts' sums");
+
+    unsigned id = blockIdx.x;
+    const int hk = id % a.kv_heads;
+    id /= a.kv_heads;
+    const int part = id % a.sink_parts;
+    id /= a.sink_parts;
+    const int k0 = (int)(id % a.sink_blocks) * 32, s = a.seq0 + (int)(id / a.sink_blocks);
+    Seq q;
+    if (!sequence(a, s, q) || k0 >= min(q.kn, a.sinks)) return;           // (faulty sequences: reported by the queries' launch)
+    const int rows = q.qn * a.group;
+    int first;
+    const int tiles = first_keys_rows(a, q, k0, first), t0 = first + part * a.sink_part_tiles, t1 = min(tiles, t0 + a.sink_part_tiles);
+    if (part > 0 && t0 >= tiles) return;                                  // (part 0 writes, rows or not)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+
+    const int key = k0 + col, keys = min(q.kn, a.sinks);
+    const int64_t token = q.k0 + min(key, q.kn - 1);
+    const int doc = a.k_docs ? a.k_docs[token] : 0;
+    const bool there = key < q.kn && doc >= 0;
+    const Lanes<T, DP> lanes(lane);
+    Fixed<T, DP> kf, vf;
+    kf.load((const T*)a.k + token * a.ks.row + hk * a.ks.head, there, a.head_dim, half);
+    vf.load((const T*)a.v + token * a.vs.row + hk * a.vs.head, there, a.head_dim, half);
+
+    auto request = [&](int t, int stage) {
+        const int r0 = t * 32, r = min(r0 + col, rows - 1), qi = (int)over_group(a, r), head = hk * a.group + r - qi * a.group;
+        const int64_t row = q.q0 + qi;
+        const bool is = r0 + col < rows && (!a.q_docs || a.q_docs[row] >= 0);   // (padding and rows past the end are zeros that see nothing)
+        const uint64_t live = __ballot(is);
+        auto from = [&](const void* base, const ps_strides& st, int i) -> const T* {
+            const int x = min(r0 + i, rows - 1), token = (int)over_group(a, x);
+            return (const T*)base + (q.q0 + token) * st.row + (hk * a.group + x - token * a.group) * st.head;
+        };
+        F::rows(smem[wave][stage][0], a.head_dim, live, [&](int i) { return from(a.q, a.qs, i); });
+        F::rows(smem[wave][stage][1], a.head_dim, live, [&](int i) { return from(a.dout, a.gs, i); });
+        float(*const to)[64] = s_word[wave][stage];
+        const int64_t at = head * a.n_q + row;
+        send_words(to[LSE], is ? (const void*)(a.row_lse + at) : (const void*)&infinity_word);
+        send_words(to[DELTA], is ? (const void*)(a.row_delta + at) : (const void*)&zeros);
+        if (a.slopes) send_words(to[SLOPE], a.slopes + head);
+        if (a.q_docs) send_words(to[DOC], is ? (const void*)(a.q_docs + row) : (const void*)&minus_one);
+        if (BIASED) send_words(to[FRONT], a.table + (int64_t)head * (2 * a.reach + 1));
+        to[PLACE][lane] = __int_as_float(q.start + qi);
+        if (BIASED) to[TABLE][lane] = __int_as_float(head * (2 * a.reach + 1) + a.reach);
+    };
+
+    f32x16 dk[L::NA], dv[L::NA];
+#pragma unroll
+    for (int i = 0; i < L::NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dk[i][e] = dv[i][e] = 0.f;
+    const float in_powers = a.cap > 0.f ? 1.f : a.scale * LOG2E;
+    int sent = t0 + wave, stage = 0, next_stage = 0;
+    auto send_next = [&] {
+        request(sent, next_stage);
+        next_stage = next_stage + 1 < STAGES ? next_stage + 1 : 0;
+        sent += 4;
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (sent < t1) send_next();
+    for (int t = t0 + wave; t < t1; t += 4) {
+        // (with two stages the next tile is sent for behind this one, which has landed by then)
+        vm_wait();
+        if (sent < t1) send_next();
+        if (STAGES == 1) vm_wait();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        const unsigned char *queries = smem[wave][stage][0], *douts = smem[wave][stage][1];
+        const float(*const word)[64] = s_word[wave][stage];
+        auto at = [&](int j) { return 8 * j + 4 * half; };
+        const int near = q.start + (int)over_group(a, t * 32);
+        const bool cut = a.causal && k0 + 31 > near && k0 + 31 >= q.prefix;
+        const bool uneven = BIASED && (int64_t)near - a.reach < k0 + 31;  // (else all stand `reach` and more behind the keys)
+        auto bias = [&](int j) {
+            const int4 place = *(const int4*)&word[PLACE][at(j)], of = *(const int4*)&word[TABLE][at(j)];
+            float4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) (&v.x)[i] = a.table[(&of.x)[i] + max(-a.reach, min(key - Learned::place((&place.x)[i]), a.reach))];
+            return v;
+        };
+        f32x16 sc, g;
+        f32x16 start = no_start();
+        if (BIASED && uneven && a.cap == 0.f) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 v = bias(j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) start[4 * j + i] = (&v.x)[i];
+            }
+        }
+        dots<T, DP>(queries, 0, kf, sc, douts, 0, vf, g, lanes, start);
+        Weights<T> p, d, rest;
+        Run run = {};
+        float even = 0.f;
+        gradients<T, 4, true, BIASED>(a, sc, g, p, d, rest, cut, a.q_docs != nullptr, false, uneven, false,
+                     [&](int j) {
+                         float4 v = *(const float4*)&word[LSE][at(j)];
+                         if (BIASED && !uneven) {
+                             const float4 off = *(const float4*)&word[FRONT][at(j)];
+                             v = make_float4(fmaf(-off.x, in_powers, v.x), fmaf(-off.y, in_powers, v.y), fmaf(-off.z, in_powers, v.z), fmaf(-off.w, in_powers, v.w));
+                         }
+                         return v;
+                     },
+                     [&](int j) { return *(const float4*)&word[DELTA][at(j)]; },
+                     [&](int j) {
+                         const float4 by = *(const float4*)&word[SLOPE][at(j)];
+                         const int4 place = *(const int4*)&word[PLACE][at(j)];
+                         return make_float4(by.x * LOG2E * fabsf((float)place.x - (float)key), by.y * LOG2E * fabsf((float)place.y - (float)key),
+                                            by.z * LOG2E * fabsf((float)place.z - (float)key), by.w * LOG2E * fabsf((float)place.w - (float)key));
+                     },
+                     [&](int j, bool(&is)[4]) {
+                         const int4 place = *(const int4*)&word[PLACE][at(j)];
+#pragma unroll
+                         for (int i = 0; i < 4; ++i) is[i] = key <= (&place.x)[i] || key < q.prefix;
+                     },
+                     [&](int j, bool(&is)[4]) {
+                         const int4 of = *(const int4*)&word[DOC][at(j)];
+#pragma unroll
+                         for (int i = 0; i < 4; ++i) is[i] = (&of.x)[i] == doc;
+                     },
+                     Nothing(), bias, Nothing(), nullptr, run, even);
+        weigh<T, DP>(douts, 0, p, dv, lanes);
+        weigh<T, DP>(queries, 0, d, dk, lanes);
+        if (sizeof(T) == 2 && (cut || a.q_docs || a.cap > 0.f)) weigh<T, DP>(queries, 0, rest, dk, lanes);
+        asm volatile("" ::: "memory");
+        stage = stage + 1 < STAGES ? stage + 1 : 0;
+    }
+
+    __syncthreads();
+    float* const sums = (float*)smem;                                     // [wavefront][dk, dv][key][DP]
+#pragma unroll
+    for (int i = 0; i < L::NA; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int f = 32 * i + 8 * g + 4 * half;
+            *(float4*)(sums + ((wave * 2 + 0) * 32 + col) * DP + f) = make_float4(dk[i][4 * g], dk[i][4 * g + 1], dk[i][4 * g + 2], dk[i][4 * g + 3]);
+            *(float4*)(sums + ((wave * 2 + 1) * 32 + col) * DP + f) = make_float4(dv[i][4 * g], dv[i][4 * g + 1], dv[i][4 * g + 2], dv[i][4 * g + 3]);
+        }
+    __syncthreads();
+    const int fours = a.head_dim / 4;
+    for (int i = threadIdx.x; i < 2 * 32 * fours; i += 256) {
+        const int z = i / (32 * fours), r = i / fours - z * 32, f = i % fours * 4;
+        if (k0 + r >= keys) continue;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float4 x = *(const float4*)(sums + ((w * 2 + z) * 32 + r) * DP + f);
+            v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+        }
+        if (a.sink_parts > 1) {
+            *(float4*)((z == 0 ? a.sink_dk : a.sink_dv) + ((((int64_t)part * a.n_seq + s) * a.sink_blocks * 32 + k0 + r) * a.kv_heads + hk) * a.head_dim + f) = v;
+            continue;
+        }
+        const ps_strides to = z == 0 ? a.dks : a.dvs;
+        const float by = z == 0 ? by_x<T>(a) : 1.f;
+        T* const out = (T*)(z == 0 ? a.dk : a.dv) + (int64_t)(q.k0 + k0 + r) * to.row + hk * to.head + f;
+        if constexpr (sizeof(T) == 2)
+            *(uint2*)out = make_uint2(cvt_pk_bf16(v.x * by, v.y * by), cvt_pk_bf16(v.z * by, v.w * by));
+        else
+            *(float4*)out = make_float4(v.x * by, v.y * by, v.z * by, v.w * by);
+    }
+}
+
 // A gradient's shares added up, a thread four neighbours: those of queries (z = 0), keys (1) and values (2).  3365 tokens, 8 heads of 80 on 4,
 // up to 4 shares: 61 MB in 18 us.
 template <typename T, bool LOCAL>
@@ -714,7 +888,7 @@ __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
     const float by = z == 2 ? 1.f : by_x<T>(a);
     for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
         const int row = i / fours, mine = row / heads, head = row % heads;
-        if (LOCAL && z > 0 && mine < a.sink_blocks * FIXED) continue;     // (shared out apart, added up apart)
+        if (LOCAL && z > 0 && mine < a.sinks) continue;                   // (added up apart)
         int first = 0;
         const int tiles = z == 0 ? key_tiles<LOCAL>(a, q, (mine * a.group + head % a.group) / FIXED * FIXED).tiles : row_tiles<LOCAL>(a, q, mine / FIXED * FIXED, first);
         const int parts = shares(tiles - first, of, each);
@@ -738,16 +912,16 @@ __global__ __launch_bounds__(256) void add_sinks_kernel(Args a) {
     const int z = blockIdx.z, s = a.seq0 + (int)blockIdx.y;
     Seq q;
     if (!sequence(a, s, q)) return;
-    const int fours = a.head_dim / 4, a_key = a.kv_heads * fours, keys = a.sink_blocks * FIXED;
-    const int64_t n = (int64_t)min(q.kn, keys) * a_key, step = (int64_t)a.n_seq * keys * a_key;
+    const int fours = a.head_dim / 4, a_key = a.kv_heads * fours, keys = a.sink_blocks * 32;
+    const int64_t n = (int64_t)min(q.kn, a.sinks) * a_key, step = (int64_t)a.n_seq * keys * a_key;
     const float4* part = (const float4*)(z == 0 ? a.sink_dk : a.sink_dv) + (int64_t)s * keys * a_key;
     const ps_strides to = z == 0 ? a.dks : a.dvs;
     T* out = (T*)(z == 0 ? a.dk : a.dv);
     const float by = z == 1 ? 1.f : by_x<T>(a);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int key = (int)(i / a_key), in_key = (int)(i - (int64_t)key * a_key), head = in_key / fours;
-        int first = 0;
-        const int tiles = row_tiles<true>(a, q, key / FIXED * FIXED, first), parts = shares(tiles - first, a.sink_parts, a.sink_part_tiles);
+        int first;
+        const int tiles = first_keys_rows(a, q, key / 32 * 32, first), parts = shares(tiles - first, a.sink_parts, a.sink_part_tiles);
         float4 sum = part[i];
 #pragma unroll 4
         for (int p = 1; p < parts; ++p) {
@@ -805,8 +979,7 @@ void launch(const Args& a, hipStream_t st) {
         }
     };
     const int64_t row_jobs = (int64_t)a.kv_heads * a.row_blocks * a.parts;
-    const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED, apart = min(key_blocks, (int64_t)a.sink_blocks);
-    const int64_t key_jobs = a.kv_heads * (apart * a.sink_parts + (key_blocks - apart) * a.key_parts);
+    const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED, key_jobs = a.kv_heads * key_blocks * a.key_parts;
     const unsigned tile_lds = BIASED ? 2 * a.bias_words * sizeof(float) : 0;
     const unsigned sums_lds = a.bias_parts ? (2 * ((a.bias_width + 63) & ~63) + 4 * (a.n_buckets + 1) * 32) * sizeof(float) : 0;
     if (BIASED && tile_lds + sums_lds > 32 << 10) {
@@ -823,9 +996,17 @@ void launch(const Args& a, hipStream_t st) {
         if (BIASED) set_width(b, FIXED + (a.key_tile - 1) / a.group + 2);
         hipLaunchKernelGGL((key_gradients_kernel<T, DP, LOCAL, BIASED>), dim3((unsigned)key_jobs * n), dim3(256), BIASED ? 2 * b.bias_words * sizeof(float) : 0, st, b);
     });
-    if (LOCAL && a.sink_parts > 1) {
-        const unsigned blocks = (unsigned)min((apart * FIXED * a.kv_heads * a.head_dim / 4 + 255) / 256, (int64_t)4096);
-        in_turn(blocks, 32768, [&](unsigned n) { hipLaunchKernelGGL(add_sinks_kernel<T>, dim3(blocks, n, 2), dim3(256), 0, st, b); });
+    if constexpr (LOCAL) {
+        if (a.sink_blocks > 0) {
+            const int64_t jobs = (int64_t)a.kv_heads * a.sink_blocks * a.sink_parts;
+            in_turn(jobs, a.n_seq, [&](unsigned n) {
+                hipLaunchKernelGGL((first_keys_kernel<T, DP, BIASED>), dim3((unsigned)jobs * n), dim3(256), 0, st, b);
+            });
+        }
+        if (a.sink_parts > 1) {
+            const unsigned blocks = (unsigned)min(((int64_t)a.sinks * a.kv_heads * a.head_dim / 4 + 255) / 256, (int64_t)4096);
+            in_turn(blocks, 32768, [&](unsigned n) { hipLaunchKernelGGL(add_sinks_kernel<T>, dim3(blocks, n, 2), dim3(256), 0, st, b); });
+        }
     }
     const int z0 = a.parts > 1 ? 0 : 1, z1 = a.key_parts > 1 ? 3 : 1;
     if (z0 == z1) return;

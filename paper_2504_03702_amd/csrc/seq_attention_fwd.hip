@@ -312,48 +312,6 @@ __global__ __launch_bounds__(256, DP == 64 && !BIASED ? 3 : 2) void attend_kerne
 // in 203 us, 5.2 TB/s (a copy reaches 5.1); one cache of 65521 keys, 4 heads, 134 MB in 27 us, 4.9 TB/s; 8 first rows over up to 512 keys
 // 8.5 us, most of it the way to the first tile and out.  In fp32 a tile of 128 features leaves room for one a wavefront: the caches, 2.1 GB,
 // 525 us, 4.0 TB/s; with heads of 64, two tiles a wavefront in one workgroup a unit, 1.05 GB at 4.1; 8 first rows 16 us.
-template <typename T, int DP>
-struct Few {
-    using L = Tile<T, DP, 32>;
-    static constexpr int SENDS = L::BYTES / 1024;                         // of 64 lanes, for a tile
-    // Tiles of a wavefront in LDS: two, or one of the largest; up to 128 KB of a unit's 160, in bf16 with heads of 64 by two workgroups.
-    static constexpr int STAGES = L::BYTES > 8192 ? 1 : 2, WORKGROUPS = L::BYTES > 4096 ? 1 : 2;
-    // Sends whose lanes' chunks differ; the others repeat them so many rows on (sends of no whole number of rows: none does).
-    static constexpr int PERIOD = 64 % L::CPR == 0 ? L::CPR / 4 : SENDS, ROWS_A_PERIOD = 64 * PERIOD / L::CPR;
-    static constexpr int WAIT = (STAGES - 1) * (2 * SENDS + 1);           // sends behind the oldest tile's, and a word for documents
-    unsigned off[2][PERIOD];
-    int64_t step[2];                                                      // bytes from row to row
-    __device__ __forceinline__ Few(const Args& a) : step{a.ks.row * L::EB, a.vs.row * L::EB} {
-        const int lane = threadIdx.x & 63;
-#pragma unroll
-        for (int j = 0; j < PERIOD; ++j) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x) off[x][j] = (unsigned)row_of(j, lane) * (unsigned)step[x] + element(j, lane, a.head_dim) * L::EB;
-        }
-    }
-    static __device__ __forceinline__ int row_of(int j, int lane) { return (j * 64 + lane) / L::CPR; }
-    static __device__ __forceinline__ int element(int j, int lane, int head_dim) {
-        return min((((j * 64 + lane) % L::CPR) ^ L::swz(row_of(j, lane))) * L::EPC, head_dim - L::EPC);
-    }
-    static __device__ __forceinline__ void send(unsigned char* tile, int j, const void* from) {
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)(tile + j * 1024), 16, 0, 0);
-    }
-    __device__ __forceinline__ void whole(unsigned char* tile, int x, const void* first) const {
-#pragma unroll
-        for (int j = 0; j < SENDS; ++j) send(tile, j, (const char*)first + j / PERIOD * ROWS_A_PERIOD * step[x] + off[x][j % PERIOD]);
-    }
-    // row(i): address of row i; there: bit i tells whether it is one, and not zeros
-    template <typename Address>
-    static __device__ __forceinline__ void rows(unsigned char* tile, int head_dim, uint64_t there, Address row) {
-        const int lane = anew<256>((int)(threadIdx.x & 63));
-#pragma unroll
-        for (int j = 0; j < SENDS; ++j) {
-            const int i = row_of(j, lane);
-            send(tile, j, there >> i & 1 ? (const void*)(row(i) + element(j, lane, head_dim)) : (const void*)&zeros);
-        }
-    }
-};
-
 template <typename T, int DP, bool LOCAL, bool BIASED>
 __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kernel(Args a) {
     using F = Few<T, DP>;
@@ -716,7 +674,7 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         if (s && local->n_buckets > 0 && (!local->buckets || !local->bias || ((uintptr_t)local->buckets | (uintptr_t)local->bias) % 4 != 0)) return PS_EINVAL;
         if (local->left >= 0) a.left = local->left;
         if (local->right >= 0) a.right = local->right;
-        a.sinks = min(local->sinks, a.max_k);
+        a.sinks = (local->left < 0 && local->right < 0) || a.max_q == 0 ? 0 : min(local->sinks, a.max_k);   // (without a window all are seen)
         a.reach = local->reach;
         a.n_buckets = local->n_buckets;
         const int64_t window = (int64_t)a.left + (ahead ? a.right : 0) + FIXED;
@@ -727,7 +685,8 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         lower(all_rows, d->n_seq * most_rows);
     }
     auto share = [&](int64_t blocks_a_seq, int64_t tokens, int64_t tokens_a_block, int64_t passing, int64_t all_passing, int tile, int32_t& parts,
-                     int32_t& part_tiles, int64_t chain) {
+                     int32_t& part_tiles, int64_t chain, bool windowed) {
+        constexpr int64_t ONCE = 512;
         const int tiles = (int)((passing + tile - 1) / tile);
         const int64_t all_tiles = all_passing / tile + a.n_seq;
         const int64_t blocks = a.kv_heads * min((int64_t)a.n_seq * blocks_a_seq, tokens / tokens_a_block + a.n_seq);
@@ -737,6 +696,8 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         if (blocks >= 512 || tiles < 2 * least / tile) return;
         const int64_t jobs = a.kv_heads * all_tiles * max((int64_t)1, blocks / max(1, a.n_seq * a.kv_heads));
         part_tiles = (int32_t)min((int64_t)tiles, max((int64_t)least / tile, jobs / 2048));
+        // (windows leave all blocks about the same: what fills the units once will do, and leaves less to be added up)
+        if (windowed) part_tiles = (int32_t)max((int64_t)least / tile, (tiles * blocks + ONCE - 1) / ONCE < tiles ? (tiles + ONCE / blocks - 1) / (ONCE / blocks) : (int64_t)tiles);
         // (what the shares leave to be added up stays within 256 MB)
         const int64_t most = max((int64_t)1, ((int64_t)64 << 20) / max((int64_t)1, tokens * a.kv_heads * a.head_dim));
         part_tiles = (int32_t)max((int64_t)part_tiles, (tiles + most - 1) / most);
@@ -752,26 +713,28 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         a.part_tiles = (int32_t)max(max(min(max((int64_t)16, jobs / 256), (int64_t)32), jobs / 1024), (tiles + most - 1) / most);
         a.parts = (int32_t)max((int64_t)1, (tiles + a.part_tiles - 1) / a.part_tiles);
     } else {
-        share(a.row_blocks, d->n_q * group, FIXED, most_keys, all_keys, a.tile, a.parts, a.part_tiles, INT32_MAX);
+        share(a.row_blocks, d->n_q * group, FIXED, most_keys, all_keys, a.tile, a.parts, a.part_tiles, INT32_MAX, most_keys < a.max_k);
     }
     // Of few blocks of keys, shares of 64 rows: a block's chain of tiles, the rows of all its head's heads, is all that takes time.  The sum's launch
     // is worth it above 256 rows, 128 in fp32 (passes of 1 sequence of 191 tokens, 48 heads on 12, 61 -> 52 us; 14 of up to 70, 16 heads of 128 on
     // 4, 49 -> 43; fp32, 4 of 56, 4 heads on 1, 82 -> 56; 4 of 128 rows, 12 heads, would take 34 for 28).
     const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED;
-    share(key_blocks, d->n_k, FIXED, most_rows, all_rows, a.key_tile, a.key_parts, a.key_part_tiles, d->dtype == 1 ? 256 : 128);
-    // The first keys are seen from everywhere: where a window leaves other blocks of keys few rows, theirs are shared out, so that no share is longer
-    // than the others' chains, and within 256 MB.
-    if (backward && a.sinks > 0 && most_rows < rows_a_seq) {
-        a.sink_blocks = (a.sinks + FIXED - 1) / FIXED;                    // (a.sinks is at most max_k)
-        const int64_t tiles = (rows_a_seq + a.key_tile - 1) / a.key_tile, each = (int64_t)d->n_seq * a.sink_blocks * FIXED * a.kv_heads * a.head_dim;
-        const int64_t most = each < 1 || each >= 32 << 20 ? 1 : (32 << 20) / each;
-        int64_t own = most_rows > 512 ? (most_rows + a.key_tile - 1) / a.key_tile : 512 / a.key_tile;
-        if (own < (tiles + most - 1) / most) own = (tiles + most - 1) / most;
-        a.sink_part_tiles = (int32_t)(own < tiles ? own : tiles);
+    share(key_blocks, d->n_k, FIXED, most_rows, all_rows, a.key_tile, a.key_parts, a.key_part_tiles, d->dtype == 1 ? 256 : 128, most_rows < rows_a_seq);
+    // The first keys are seen from everywhere, so they have a launch of their own, 32 to a workgroup, their rows in shares: some 512, of 256 rows or
+    // more, within 256 MB.
+    if (backward && a.sinks > 0 && d->n_seq > 0) {
+        a.sink_blocks = (a.sinks + 31) / 32;
+        const int64_t tiles = (rows_a_seq + 31) / 32, jobs = (int64_t)d->n_seq * a.kv_heads * a.sink_blocks, each = jobs * 32 * a.head_dim;
+        int64_t parts = jobs < 512 ? 512 / jobs : 1;
+        if (parts > (32 << 20) / each) parts = (32 << 20) / each;
+        if (parts > tiles / 8) parts = tiles / 8;
+        if (parts < 1) parts = 1;
+        a.sink_part_tiles = (int32_t)((tiles + parts - 1) / parts);
         a.sink_parts = (int32_t)((tiles + a.sink_part_tiles - 1) / a.sink_part_tiles);
+        if ((int64_t)a.kv_heads * a.sink_blocks * a.sink_parts >= 1 << 24) return PS_EUNSUPPORTED;
     }
     // (a grid holds fewer than 2^32 threads)
-    if ((int64_t)a.kv_heads * a.row_blocks * a.parts >= 1 << 24 || (int64_t)a.kv_heads * key_blocks * (int64_t)max(a.key_parts, a.sink_parts) >= 1 << 24)
+    if ((int64_t)a.kv_heads * a.row_blocks * a.parts >= 1 << 24 || (int64_t)a.kv_heads * key_blocks * a.key_parts >= 1 << 24)
         return PS_EUNSUPPORTED;
     size_t off = 0;
     uint8_t* base = (uint8_t*)workspace;
@@ -801,7 +764,7 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         }
     }
     if (a.sink_parts > 1) {
-        const size_t part = sizeof(float) * (size_t)a.sink_parts * d->n_seq * a.sink_blocks * FIXED * a.kv_heads * a.head_dim;
+        const size_t part = sizeof(float) * (size_t)a.sink_parts * d->n_seq * a.sink_blocks * 32 * a.kv_heads * a.head_dim;
         a.sink_dk = (float*)take(part);
         a.sink_dv = (float*)take(part);
     }
