@@ -61,7 +61,7 @@ struct Args {
     const int32_t* bucket_words;       // [2 reach + 1]: where in a lane's sums the distance's bucket is
     float* bias_parts;                 // [parts][blocks of rows][buckets][heads]: sums of a bucket's gradients, null if not wanted
     int64_t bias_blocks;
-    int32_t reach, n_buckets;
+    int32_t reach, n_buckets, sum_columns;   // sums of a bucket that a wavefront has: 64, or 32
     int32_t bias_width, bias_words;    // distances that a head has in a tile; words of all heads of a tile, in whole wavefronts
     uint32_t by_width;                 // 2^32 / bias_width + 1
 };

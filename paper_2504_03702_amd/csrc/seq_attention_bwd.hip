@@ -31,17 +31,21 @@ struct Nothing {
 // to LDS when the next one's turn has come: an addition there takes 160 cycles of a wavefront's 64 lanes (64 sequences of up to 512 tokens, every
 // value added by itself: 202 us; this way RUNS us).
 struct Run {
-    int word;                          // a row's sum's, in words of all 32 rows
+    int word;                          // where the bucket's sums of a wavefront's lanes (or rows) start
     float sum;
-    // (a row's two lanes one after the other, so that the order is fixed)
-    __device__ __forceinline__ void flush(float* sums) const {
-        const bool second = anew<256>((int)threadIdx.x) & 32;
-        if (!second) __hip_atomic_fetch_add(sums + word, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-        if (second) __hip_atomic_fetch_add(sums + word, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    // own: a lane has a sum of its own; else a row's two lanes share one, and come one after the other so that the order is fixed (told apart twice: the
+    // compiler would make one addition of the two)
+    __device__ __forceinline__ void flush(float* sums, bool own) const {
+        if (own) {
+            __hip_atomic_fetch_add(sums + word, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            return;
+        }
+        if (!(anew<256>((int)threadIdx.x) & 32)) __hip_atomic_fetch_add(sums + word, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        if (anew<256>((int)threadIdx.x) & 32) __hip_atomic_fetch_add(sums + word, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
-    __device__ __forceinline__ void add(float* sums, int to, float e) {
+    __device__ __forceinline__ void add(float* sums, bool own, int to, float e) {
         if (to != word) {
-            flush(sums);
+            flush(sums, own);
             word = to;
             sum = 0.f;
         }
@@ -52,7 +56,7 @@ template <typename T, int STEP, bool LOCAL, bool BIASED, typename Lse, typename 
           typename Where>
 __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, Weights<T>& p, Weights<T>& d, Weights<T>& rest,
                                           bool cut, bool docs, bool late, bool uneven, bool summed, Lse lse, Delta delta, Distance distance, Front in_front,
-                                          Same same, Windowed windowed, Bias bias, Where where, float* sums, Run& run, float& even) {
+                                          Same same, Windowed windowed, Bias bias, Where where, float* sums, bool own, Run& run, float& even) {
     const Cap cap = Cap::of<T>(a);
     const float c1 = a.scale * LOG2E;
 #pragma unroll
@@ -153,7 +157,7 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
                     for (int k = 0; k < STEP; ++k) {
                         const float all = (u[k].x + u[k].y) + (u[k].z + u[k].w);
                         if (uneven)
-                            run.add(sums, to[k] & ~1, all);
+                            run.add(sums, own, to[k] & ~1, all);
                         else
                             even += all;
                     }
@@ -167,7 +171,7 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
 #pragma unroll
                     for (int k = 0; k < STEP; ++k)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) run.add(sums, each[k][i] & ~1, (&u[k].x)[i]);
+                        for (int i = 0; i < 4; ++i) run.add(sums, own, each[k][i] & ~1, (&u[k].x)[i]);
                 }
             }
     }
@@ -423,7 +427,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
                                  const float* own = s_bias + 32 * wave + (anew<256>((int)threadIdx.x) & 31);
                                  return make_float4(own[of.x], own[of.y], own[of.z], own[of.w]);
                              },
-                             Nothing(), nullptr, run, even);
+                             Nothing(), nullptr, true, run, even);
                 weigh<T, DP>(smem[buf][1], b, p, dv, lanes);
                 weigh<T, DP>(smem[buf][0], b, d, dk, lanes);
                 if (sizeof(T) == 2 && (cut || docs || late || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dk, lanes);
@@ -455,7 +459,7 @@ template <typename T, int DP, bool LOCAL, bool BIASED>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_gradients_kernel(Args a) {
     using L = Tile<T, DP, query_tile_rows(sizeof(T), DP, BIASED)>;
     // BIASED: [buffer][a.bias_words], then, if its gradient is wanted, [buffer][bias_width, in whole wavefronts] words of buckets' sums, and
-    // [wavefront][buckets, and one for distances without][row] sums
+    // [wavefront][buckets, and one for distances without][lane, or row] sums
     extern __shared__ __align__(16) float s_bias[];
     __shared__ __align__(1024) unsigned char smem[2][2][L::BYTES];        // [buffer][keys, values]
     __shared__ __align__(16) int s_doc[2][64];
@@ -543,7 +547,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     // keys that some of the workgroup's rows have nearer than `reach`
     const int wide_from = BIASED ? Learned::place(q.start + (int)over_group(a, r0)) - a.reach + 1 : 0, wide_to = BIASED ? (int)min((int64_t)far + a.reach, (int64_t)INT32_MAX) : 0;
     const int bias_place = Learned::place(far), bias_from = BIASED ? (head - hk * a.group) * a.bias_width + bias_place - Learned::place(place) : 0;
-    const int widths = (a.bias_width + 63) & ~63, sums_a_wave = (a.n_buckets + 1) * 32;
+    const int widths = (a.bias_width + 63) & ~63, columns = a.sum_columns, sums_a_wave = (a.n_buckets + 1) * columns;
     int* const s_bucket = (int*)(s_bias + 2 * a.bias_words);
     float* const s_sums = (float*)(s_bucket + 2 * widths);
     const bool summed = BIASED && a.bias_parts != nullptr;
@@ -586,7 +590,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
 #pragma unroll
         for (int e = 0; e < 16; ++e) dq[i][e] = 0.f;
 
-    Run run = {a.n_buckets * 32, 0.f};
+    Run run = {a.n_buckets * columns, 0.f};
     Walk walk;
     int t = walk.next(t0, t1, classify), buf = 0;
     if (t < t1) request(t, walk.is_padded(t), 0);
@@ -649,9 +653,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
                                  return make_float4(own[0], own[1], own[2], own[3]);
                              },
                              [&](int j, int i) { return s_bucket[buf * widths + bias_place - Learned::place(place) + at(j) + i]; },
-                             s_sums + wave * sums_a_wave + (anew<256>((int)threadIdx.x) & 31), run, even);
+                             s_sums + wave * sums_a_wave + (anew<256>((int)threadIdx.x) & (columns - 1)), columns == 64, run, even);
                 if (summed && !uneven)
-                    run.add(s_sums + wave * sums_a_wave + (anew<256>((int)threadIdx.x) & 31), a.bucket_words[front ? 0 : 2 * a.reach] & ~1, even);
+                    run.add(s_sums + wave * sums_a_wave + (anew<256>((int)threadIdx.x) & (columns - 1)), columns == 64, a.bucket_words[front ? 0 : 2 * a.reach] & ~1, even);
                 weigh<T, DP>(smem[buf][0], b, d, dq, lanes);
                 if (sizeof(T) == 2 && (cut || docs || late || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dq, lanes);
             }
@@ -660,7 +664,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     }
     __syncthreads();                                                      // (tiles are no longer read, and the sums are there)
     if (summed) {
-        run.flush(s_sums + wave * sums_a_wave + col);
+        run.flush(s_sums + wave * sums_a_wave + (lane & (columns - 1)), columns == 64);
         __syncthreads();
         // A bucket's sums of a head's lanes added up by `slices` neighbouring threads, a share of the rows each, which start at other rows from bucket to
         // bucket (all buckets have a row's sums in one bank).  Row r0 + x has head x % group less r0's.
@@ -674,7 +678,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
                 for (int k = 0; k < turns; ++k) {
                     const int m = slice + slices * ((k + i) % turns), x = x0 + m * a.group;
                     if (m >= n) continue;
-                    sum += s_sums[(x >> 5) * sums_a_wave + b * 32 + (x & 31)];
+                    const float* of = s_sums + (x >> 5) * sums_a_wave + b * columns + (x & 31);
+                    sum += columns == 64 ? of[0] + of[32] : of[0];
                 }
             for (int o = 1; o < slices; o *= 2) sum += __shfl_xor(sum, o, 64);
             if (i < outs && slice == 0) to[b * a.heads + hk * a.group + h] = sum;
@@ -828,7 +833,7 @@ __global__ __launch_bounds__(256, 1) void first_keys_kernel(Args a) {
 #pragma unroll
                          for (int i = 0; i < 4; ++i) is[i] = (&of.x)[i] == doc;
                      },
-                     Nothing(), bias, Nothing(), nullptr, run, even);
+                     Nothing(), bias, Nothing(), nullptr, true, run, even);
         weigh<T, DP>(douts, 0, p, dv, lanes);
         weigh<T, DP>(queries, 0, d, dk, lanes);
         if (sizeof(T) == 2 && (cut || a.q_docs || a.cap > 0.f)) weigh<T, DP>(queries, 0, rest, dk, lanes);
@@ -981,7 +986,7 @@ void launch(const Args& a, hipStream_t st) {
     const int64_t row_jobs = (int64_t)a.kv_heads * a.row_blocks * a.parts;
     const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED, key_jobs = a.kv_heads * key_blocks * a.key_parts;
     const unsigned tile_lds = BIASED ? 2 * a.bias_words * sizeof(float) : 0;
-    const unsigned sums_lds = a.bias_parts ? (2 * ((a.bias_width + 63) & ~63) + 4 * (a.n_buckets + 1) * 32) * sizeof(float) : 0;
+    const unsigned sums_lds = a.bias_parts ? (2 * ((a.bias_width + 63) & ~63) + 4 * (a.n_buckets + 1) * a.sum_columns) * sizeof(float) : 0;
     if (BIASED && tile_lds + sums_lds > 32 << 10) {
         static bool lds_attr_set = false;     // raising the limit twice is harmless, so no lock
         if (!lds_attr_set && hipFuncSetAttribute((const void*)query_gradients_kernel<T, DP, LOCAL, BIASED>, hipFuncAttributeMaxDynamicSharedMemorySize, 64 << 10) != hipSuccess) return;

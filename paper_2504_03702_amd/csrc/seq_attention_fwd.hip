@@ -553,7 +553,7 @@ __global__ __launch_bounds__(256) void check_kernel(Args a) {
 
 // The learned bias of every distance, a thread each of a head's, `by` times what the caller has (none for a bucket that there is not), and
 // where its bucket is in a lane's sums.  The threads clear what the sums of blocks of rows go to, too, since some blocks belong to no sequence.
-__global__ __launch_bounds__(256) void table_kernel(const int32_t* buckets, const float* bias, float* table, int32_t* words, int reach, int n_buckets, int heads,
+__global__ __launch_bounds__(256) void table_kernel(const int32_t* buckets, const float* bias, float* table, int32_t* words, int reach, int n_buckets, int columns, int heads,
                                                     float by, float* sums, int64_t n_sums) {
     const int d = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y;
     const int64_t threads = (int64_t)gridDim.x * gridDim.y * 256;
@@ -566,7 +566,7 @@ __global__ __launch_bounds__(256) void table_kernel(const int32_t* buckets, cons
         // (its lowest bit: the next three distances have the same bucket)
         bool same = true;
         for (int i = 1; i < 4; ++i) same = same && buckets[min(d + i, 2 * reach)] == b;
-        words[d] = (is ? b : n_buckets) * 32 + (same ? 1 : 0);
+        words[d] = (is ? b : n_buckets) * columns + (same ? 1 : 0);
     }
 }
 
@@ -620,6 +620,9 @@ bool add_up(int32_t seqs, int64_t blocks, int32_t parts) { return seqs <= 64 && 
 
 // Distances that a head has in a tile, and the words of all heads.
 void set_width(Args& a, int width) {
+    // (heads' words in different banks: the rows of a wavefront stand at 32 / group places, and its halves at four more)
+    for (int heads = 1, banks = 64; heads < a.group && a.group <= 8; banks /= 2, heads *= 2)
+        if (2 * heads >= a.group) width += (banks / 2 - width % 64 + 64) % 64;
     a.bias_width = width;
     a.bias_words = (width * a.group + 63) / 64 * 64;
     a.by_width = (uint32_t)(((uint64_t)1 << 32) / (uint64_t)width + 1);
@@ -772,6 +775,7 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         a.table = (const float*)take(sizeof(float) * (size_t)a.heads * (2 * (size_t)a.reach + 1));
         a.bucket_words = (const int32_t*)take(sizeof(int32_t) * (2 * (size_t)a.reach + 1));
         set_width(a, a.tile + (FIXED - 1) / a.group + 2);   // (a tile of keys by FIXED rows)
+        a.sum_columns = a.n_buckets <= 32 && padded(d->head_dim) != 96 ? 64 : 32;   // (what leaves room for two workgroups a unit)
         if (backward) {
             a.bias_blocks = d->n_q * group / FIXED + d->n_seq + 1;
             a.bias_parts = (float*)take(sizeof(float) * ((size_t)a.parts * a.bias_blocks + (size_t)a.parts * a.bias_blocks / 128 + 1) * a.n_buckets * a.heads);
@@ -800,7 +804,7 @@ void make_table(const Args& a, const ps_attention_local* local, float by, hipStr
     unsigned rows = a.heads;
     while ((int64_t)rows * across * 2048 < n_sums && rows * across < 1024) rows *= 2;
     hipLaunchKernelGGL(table_kernel, dim3(across, rows), dim3(256), 0, st, local->buckets, local->bias, const_cast<float*>(a.table),
-                       const_cast<int32_t*>(a.bucket_words), a.reach, a.n_buckets, a.heads, by, a.bias_parts, n_sums);
+                       const_cast<int32_t*>(a.bucket_words), a.reach, a.n_buckets, a.sum_columns, a.heads, by, a.bias_parts, n_sums);
 }
 
 int check_sequences(const Args& a, hipStream_t st) {
