@@ -1,5 +1,5 @@
-"""The operators of a trained layer as functions with gradients (``torch.autograd``): rotary positions, attention over packed
-sequences, dropout with bias and residual.  Each call allocates its outputs and hands them to the binding, which runs the
+"""The operators of a trained layer as functions with gradients (``torch.autograd``): rotary positions, alone or behind norms of
+heads, attention over packed sequences, with windows and learned biases, dropout with bias and residual.  Each call allocates its outputs and hands them to the binding, which runs the
 library's kernels; there is no fallback.  A program that owns its buffers calls the binding itself."""
 from __future__ import annotations
 
@@ -90,12 +90,55 @@ class _Attention(torch.autograd.Function):
         return (*grads, None, None, None, None, None)
 
 
+class _LocalAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, bias, seqs, scale, softcap, causal, slopes, window, sinks, buckets):
+        train = any(ctx.needs_input_grad[:4])
+        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)             # (the kernels leave rows that no sequence has alone)
+        lse = torch.empty(q.shape[1], q.shape[0], device=q.device)
+        rest = torch.empty_like(out) if train and q.dtype == torch.bfloat16 else None
+        ctx.local = dict(left=window[0], right=window[1], sinks=sinks)
+        ctx.shape = (seqs.q_offsets.numel() - 1, q.shape[0], k.shape[0], seqs.max_q, seqs.max_k, q.shape[1], k.shape[1], q.shape[2], q.dtype)
+        table = None if bias is None else bias.detach().float().contiguous()
+        ctx.sizes = dict(n_buckets=0 if bias is None else bias.shape[0], reach=0 if bias is None else buckets.numel() // 2)
+        ws = ps.alloc_workspace(ps.ps_local_attention_workspace_bytes(*ctx.shape, **ctx.local, **ctx.sizes), q.device)
+        masks = dict(seqs.arguments(), slopes=slopes, buckets=buckets, bias=table)
+        ctx.how = dict(scale=scale, softcap=softcap, causal=causal, status=masks.pop("status"))
+        ctx.bounds, ctx.masks, ctx.bias = (seqs.max_q, seqs.max_k), tuple(masks), None if bias is None else bias.dtype
+        ps.ps_local_attention_forward(q, k, v, seqs.q_offsets, seqs.k_offsets, *ctx.bounds, out, lse, ws, out_rest=rest, **ctx.local, **masks, **ctx.how)
+        # (the bias itself too, so that what is written to it in between does not go unnoticed)
+        ctx.save_for_backward(q, k, v, out, lse, rest, seqs.q_offsets, seqs.k_offsets, bias, *masks.values())
+        return out
+
+    @staticmethod
+    @_first_only
+    def backward(ctx, dout):
+        q, k, v, out, lse, rest, q_offsets, k_offsets, _, *masks = ctx.saved_tensors
+        dout = dout.contiguous()
+        if dout.data_ptr() % 16:                                # (part of a larger gradient, as torch.cat hands them back)
+            dout = dout.clone()
+        masks = dict(zip(ctx.masks, masks))
+        # (rows that no sequence has get no gradient)
+        grads = [torch.zeros(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v)]
+        dbias = torch.empty_like(masks["bias"]) if ctx.bias is not None and ctx.needs_input_grad[3] else None
+        ws = ps.alloc_workspace(ps.ps_local_attention_workspace_bytes(*ctx.shape, backward=True, **ctx.local, **ctx.sizes), q.device)
+        ps.ps_local_attention_backward(q, k, v, out, lse, dout, q_offsets, k_offsets, *ctx.bounds, *grads, ws, dbias=dbias, out_rest=rest, **ctx.local,
+                                       **masks, **ctx.how)
+        return (*grads, None if dbias is None else dbias.to(ctx.bias), *[None] * 8)
+
+
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: Sequences, scale: Optional[float] = None, softcap: float = 0.0,
-              causal: bool = False, slopes: Optional[torch.Tensor] = None) -> torch.Tensor:
+              causal: bool = False, slopes: Optional[torch.Tensor] = None, window: Tuple[int, int] = (-1, -1), sinks: int = 0,
+              bias: Optional[torch.Tensor] = None, buckets: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of packed q [n_q, heads, size] to k, v [n_k, kv_heads, size]; slopes are constants.  Rows that no sequence has, or a
-    faulty one, are zeros, as is their gradient; faulty sequences are told in ``seqs.status``."""
+    faulty one, are zeros, as is their gradient; faulty sequences are told in ``seqs.status``.
+
+    window: how far rows see in front of themselves and behind (-1: without end); sinks: first keys that they see all the same; bias
+    [n_buckets, heads], which is learned, by the buckets of distances ([2 reach + 1] int32 on the GPU, ``binding.ps_bias_buckets``)."""
     _constant(slopes, "attention", "slopes")
-    return _Attention.apply(q, k, v, seqs, scale, softcap, causal, slopes)
+    if tuple(window) == (-1, -1) and bias is None and buckets is None:
+        return _Attention.apply(q, k, v, seqs, scale, softcap, causal, slopes)
+    return _LocalAttention.apply(q, k, v, bias, seqs, scale, softcap, causal, slopes, tuple(window), sinks, buckets)
 
 
 class _Rotary(torch.autograd.Function):

@@ -1,0 +1,160 @@
+"""Norms with rotary positions and local attention as they are used together: in a layer with gradients, against the same layer in 64 bits, and on
+what a program hands over: slices of a projection, another stream, long caches, the largest numbers.
+
+Bounds: fp32, each operator keeps 1e-5 of its result's norm and the layer has four in a row, forwards and backwards: 1e-4.  bf16 rounds
+each of a dozen tensors on the way to 2^-8 of a value at most (1.7e-3 in the mean square): 12 * 1.7e-3 = 2e-2, were they all to add up."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2504_03702_amd import binding as ps
+from paper_2504_03702_amd import layers
+from tests.test_gpu_local_attention import BUCKETS, DEV, T5, Local, i32
+
+pytestmark = pytest.mark.gpu
+
+
+def rotate(x, angle):
+    n = angle.shape[1]
+    a, b, c, s = x[..., :n], x[..., n:2 * n], angle.cos()[:, None], angle.sin()[:, None]
+    return torch.cat((a * c - b * s, a * s + b * c, x[..., 2 * n:]), -1)
+
+
+@pytest.mark.parametrize("dtype,bound", [(torch.float32, 1e-4), (torch.bfloat16, 2e-2)])
+@pytest.mark.parametrize("how", [dict(window=(20, 10), sinks=2), dict(causal=True, window=(30, -1), sinks=1, bias=True), dict(bias=True)], ids=["window", "both", "bias"])
+def test_a_layer_and_its_gradients(dtype, bound, how):
+    g = torch.Generator().manual_seed(3)
+    heads, kv, size, lens = 4, 2, 32, [70, 1, 140]
+    n, hidden, offsets = sum(lens), heads * size, np.cumsum([0] + lens)
+    made = lambda *s: (torch.randn(s, generator=g) * 0.5).to(dtype)
+    x, w_qkv, w_out, dy = made(n, hidden), made(hidden, (heads + 2 * kv) * size) * 0.2, made(hidden, hidden) * 0.2, made(n, hidden)
+    wq, wk, bias = 1 + 0.2 * made(size), 1 + 0.2 * made(size), made(9, heads).float()
+    pos, f = torch.cat([torch.arange(m) for m in lens]), ps.ps_rotary_frequencies(8)
+    buckets = torch.tensor(BUCKETS, dtype=torch.int32)
+    left, right = how.get("window", (-1, -1))
+
+    # in 64 bits
+    leaves = [t.double().requires_grad_() for t in (x, w_qkv, w_out, wq, wk, bias)]
+    xd, wd, od, wqd, wkd, bd = leaves
+    q, k, v = (xd @ wd).view(n, heads + 2 * kv, size).split((heads, kv, kv), 1)
+    angle = pos[:, None].double() * f.double()
+    normed = lambda t, w: t / (t.square().mean(-1, keepdim=True) + 1e-6).sqrt() * w
+    q, k = rotate(normed(q, wqd), angle), rotate(normed(k, wkd), angle)
+    rows = []
+    for s, m in enumerate(lens):
+        i = slice(offsets[s], offsets[s + 1])
+        apart = torch.arange(m)[None] - torch.arange(m)[:, None]
+        seen = (apart >= (-left if left >= 0 else -m)) & (apart <= (right if right >= 0 else m)) | (torch.arange(m) < how.get("sinks", 0))
+        if how.get("causal"):
+            seen = seen & (apart <= 0)
+        z = torch.einsum("ihd,jhd->hij", q[i], k[i].repeat_interleave(heads // kv, 1)) * size ** -0.5
+        if how.get("bias"):
+            z = z + bd[buckets[apart.clamp(-7, 7) + 7].long()].permute(2, 0, 1)
+        rows.append(torch.einsum("hij,jhd->ihd", z.masked_fill(~seen, -torch.inf).softmax(-1), v[i].repeat_interleave(heads // kv, 1)))
+    want = torch.cat(rows).reshape(n, hidden) @ od
+    wanted = torch.autograd.grad(want, leaves, dy.double(), allow_unused=True)
+
+    own = [t.to(DEV).requires_grad_() for t in (x, w_qkv, w_out, wq, wk, bias)]
+    xg, wg, og, wqg, wkg, bg = own
+    q, k, v = (xg @ wg).view(n, heads + 2 * kv, size).split((heads, kv, kv), 1)
+    q, k = layers.norm_rotary(q, k, wqg, wkg, i32(pos), f.to(DEV))
+    status = ps.new_status(DEV)
+    seqs = layers.Sequences(i32(offsets), i32(offsets), max(lens), max(lens), status=status)
+    more = dict(bias=bg, buckets=buckets.to(DEV)) if how.get("bias") else {}
+    y = layers.attention(q, k, v, seqs, **{**how, **more} if more else how).reshape(n, hidden) @ og
+    got = torch.autograd.grad(y, own, dy.to(DEV), allow_unused=True)
+    assert ps.ps_status_read(status) == (0, -1)
+    near = lambda a, b: float((a.double().cpu() - b).norm() / b.norm())
+    assert near(y, want) <= bound
+    for name, a, b in zip(("x", "qkv", "out", "wq", "wk", "bias"), got, wanted):
+        assert (a is None) == (b is None) and (a is None or near(a, b) <= bound), (name, near(a, b))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_layer_function_alone(dtype):
+    """Rows of no sequence, a bias of the tensors' type, second derivatives, what is written again."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    q, k, v = (torch.randn(50, h, 16, generator=g, device=DEV).to(dtype).requires_grad_() for h in (4, 2, 2))
+    bias = torch.randn(9, 4, generator=g, device=DEV).to(dtype).requires_grad_()
+    buckets = i32(BUCKETS)
+    seqs = layers.Sequences(i32([5, 45]), i32([0, 40]), 40, 40)
+    out = layers.attention(q, k, v, seqs, window=(9, 3), sinks=1, bias=bias, buckets=buckets)
+    assert torch.all(out[:5] == 0) and torch.all(out[45:] == 0) and torch.all(out[5:45].abs().sum((1, 2)) > 0)
+    grads = torch.autograd.grad(out.square().sum(), (q, k, v, bias), create_graph=True)
+    assert grads[3].dtype == dtype and torch.all(grads[0][:5] == 0) and torch.all(grads[1][40:] == 0)
+    with pytest.raises(RuntimeError):
+        grads[3].sum().backward()
+    out = layers.attention(q, k, v, seqs, bias=bias, buckets=buckets)
+    with torch.no_grad():
+        bias.add_(1)
+    with pytest.raises(RuntimeError):
+        out.sum().backward()
+    with torch.no_grad():
+        (only,) = (layers.attention(q, k, v, seqs, window=(9, 3)),)
+    assert not only.requires_grad
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_slices_of_a_projection(dtype):
+    """Queries, keys and values inside one map's output, results inside larger tensors: as from dense ones, and nothing else is written."""
+    p = Local(dtype, [130, 9, 70], [130, 9, 70], left=30, right=9, sinks=40, buckets=T5, n_buckets=32)
+    want = p.both()
+    n, size = p.q.shape[0], 64
+    packed = torch.cat((p.q, p.k, p.v), 1).contiguous()
+    p.q, p.k, p.v = packed.split((4, 2, 2), 1)
+    wide = [torch.full((n, h + 1, size), 7.0, device=DEV, dtype=dtype) for h in (4, 4, 2, 2)]
+    out, dq, dk, dv = (t[:, :-1] for t in wide)
+    lse, rest = torch.empty(4, n, device=DEV), torch.empty(n, 4, size, dtype=dtype, device=DEV) if dtype == torch.bfloat16 else None
+    dbias = torch.empty_like(p.bias)
+    args, more = p.arguments(), p.more()
+    ps.ps_local_attention_forward(p.q, p.k, p.v, i32(p.qo), i32(p.ko), 130, 130, out, lse, p.workspace(False), out_rest=rest, **more, **args)
+    ps.ps_local_attention_backward(p.q, p.k, p.v, out, lse, p.dout, i32(p.qo), i32(p.ko), 130, 130, dq, dk, dv, p.workspace(True), dbias=dbias, out_rest=rest, **more, **args)
+    assert all(torch.equal(a, b) for a, b in zip((out, lse, dq, dk, dv, dbias), want)) and all(torch.all(t[:, -1] == 7.0) for t in wide)
+
+
+def test_calls_on_two_streams():
+    a, b = (Local(torch.bfloat16, [500, 30], [500, 30], seed=s, left=64, right=20, sinks=3, buckets=T5, n_buckets=32) for s in (1, 2))
+    want = [p.both() for p in (a, b)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for p, s in zip((a, b), streams):
+        with torch.cuda.stream(s):
+            got.append(p.both())
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for g, w in zip(got, want) for x, y in zip(g, w))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_largest_numbers(dtype):
+    """Windows that end beyond 32 bits and first keys beyond all keys: as without a window."""
+    top = 2 ** 31 - 1
+    plain = Local(dtype, [150, 20], [150, 20], q_start=[-(1 << 30), 1 << 30]).both()
+    for how in (dict(left=top, right=top), dict(left=0, right=0, sinks=top), dict(left=top, right=0, sinks=150)):
+        p = Local(dtype, [150, 20], [150, 20], q_start=[-(1 << 30), 1 << 30], **how)
+        p.check()
+        near = lambda a, b: float((a - b).float().norm()) <= 1e-2 * float(b.float().norm())
+        if how.get("sinks"):
+            assert all(near(a, b) for a, b in zip(p.both(), plain))
+    # one bucket, of one distance, and a bias that leaves one key
+    Local(dtype, [70, 3], [70, 3], buckets=[0], n_buckets=1).check()
+    p = Local(dtype, [70, 3], [70, 3], buckets=[0, 1, 0], n_buckets=2)
+    p.bias = torch.tensor([[-200.0] * 4, [200.0] * 4], device=DEV)
+    out, lse = p.forward()
+    assert torch.allclose(out.float(), p.v.repeat_interleave(2, 1).float(), atol=1e-6)
+
+
+def test_long_offsets():
+    """A cache of more than 2^31 elements: the window's keys at its end."""
+    n, kv, size, w = 1100000, 16, 128, 300
+    cache = torch.empty(n, kv, size, dtype=torch.bfloat16, device=DEV)
+    cache[-w - 8:] = torch.randn(w + 8, kv, size, device=DEV).bfloat16()
+    cache[:4] = torch.randn(4, kv, size, device=DEV).bfloat16()
+    q = torch.randn(1, kv, size, device=DEV).bfloat16()
+    short = torch.cat((cache[:4], cache[-w:])).contiguous()
+    got = []
+    for c, how in ((cache, dict(left=w - 1, sinks=4)), (short, {})):
+        out, lse = torch.empty_like(q), torch.empty(kv, 1, device=DEV)
+        ws = ps.alloc_workspace(ps.ps_local_attention_workspace_bytes(1, 1, c.shape[0], 1, c.shape[0], kv, kv, size, torch.bfloat16, **how), DEV)
+        ps.ps_local_attention_forward(q, c, c, i32([0, 1]), i32([0, c.shape[0]]), 1, c.shape[0], out, lse, ws, causal=True, **how)
+        got.append((out, lse))
+    assert torch.allclose(got[0][0].float(), got[1][0].float(), atol=2e-2) and torch.allclose(got[0][1], got[1][1], atol=1e-4)
