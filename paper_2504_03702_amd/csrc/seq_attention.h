@@ -23,6 +23,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int FIXED = 128;             // fixed rows of a workgroup, 32 a wavefront
+constexpr int FEW = 512;               // keys that a row sees where the rounding of their weights' gradients does not average out
 constexpr int DOC_BLOCK = 64;          // tokens to a summary of their documents
 
 struct Args {
@@ -55,6 +56,7 @@ struct Args {
     float slope_by, cap_in;            // see Row and Cap
     // ps_local_attention_*() alone, whose kernels are the same with LOCAL:
     int32_t left, right, sinks;        // a row's window, and the first keys that it sees all the same
+    int32_t few_seen;                  // the window holds FEW keys at most, or has no end in front
     int32_t sink_blocks, sink_parts, sink_part_tiles;   // those in blocks of 32, shares of their tiles of 32 rows
     float *sink_dk, *sink_dv;          // [sink_parts][n_seq][sink_blocks * 32][kv_heads][head_dim]
     const float* table;                // [heads][2 reach + 1]: the learned bias of a distance, null without one (see Learned)

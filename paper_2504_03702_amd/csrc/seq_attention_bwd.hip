@@ -20,8 +20,9 @@ namespace {
 // queries' / keys' gradients 499 / 860 -> 589 / 977 us, error against 64 bits 2.7e-3 -> 2.1e-3 of the norm (1.7e-3 is that of dq's and dk's
 // own rounding; 2.3e-3 without cap, where a product more would cost 5 to 10 %).  (Documents in two rows of 8192, where blocks are cut: 130 / 146
 // -> 144 / 160.)
+// (LOCAL: cut blocks whose rows may see no more than FEW keys.  Where a window leaves them more, its edges are no reason.)
 // LOCAL: late and windowed(j, is), which keys are in the window, as with `cut`.  BIASED: uneven, whether the learned bias differs within the block, and
-// bias(j), in powers of two, if it does; summed, whether the gradients of the scores themselves are wanted (that of x has the cap's slope too): where(j, i)
+// bias(j), in powers of two, if it does; summed, whether the gradients of the scores themselves are wanted (that of x has the cap's slope too): where
 // has the words of their buckets' sums, to which `run` adds them, or, of an even block, they are added to `even`.
 struct Nothing {
     __device__ __forceinline__ float4 operator()(int) const { return make_float4(0.f, 0.f, 0.f, 0.f); }
@@ -44,18 +45,22 @@ struct Run {
         if (anew<256>((int)threadIdx.x) & 32) __hip_atomic_fetch_add(sums + word, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
     __device__ __forceinline__ void add(float* sums, bool own, int to, float e) {
-        if (to != word) {
-            flush(sums, own);
-            word = to;
-            sum = 0.f;
-        }
-        sum += e;
+        const bool next = to != word;
+        if (next) flush(sums, own);
+        sum = (next ? 0.f : sum) + e;
+        word = to;
     }
+};
+// The words of a block's distances, in LDS: a sum's in the low half, and whether the next three distances have the same.
+struct Words {
+    const int* at;
+    __device__ __forceinline__ int first(int j) const { return at[8 * j]; }
+    __device__ __forceinline__ unsigned low(int j, int i) const { return *(const unsigned short*)(at + 8 * j + i); }
 };
 template <typename T, int STEP, bool LOCAL, bool BIASED, typename Lse, typename Delta, typename Distance, typename Front, typename Same, typename Windowed, typename Bias,
           typename Where>
 __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const f32x16& g, Weights<T>& p, Weights<T>& d, Weights<T>& rest,
-                                          bool cut, bool docs, bool late, bool uneven, bool summed, Lse lse, Delta delta, Distance distance, Front in_front,
+                                          bool cut, bool docs, bool late, bool left_over, bool uneven, bool summed, Lse lse, Delta delta, Distance distance, Front in_front,
                                           Same same, Windowed windowed, Bias bias, Where where, float* sums, bool own, Run& run, float& even) {
     const Cap cap = Cap::of<T>(a);
     const float c1 = a.scale * LOG2E;
@@ -127,7 +132,7 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
             d.set(j0 + k, v[k]);
         }
         if constexpr (sizeof(T) == 2)
-            if (cut || docs || (LOCAL && late) || a.cap > 0.f) {
+            if (left_over) {
 #pragma unroll
                 for (int k = 0; k < STEP; ++k) {
                     const float4 r = d.get(j0 + k);
@@ -141,9 +146,9 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
                 bool wide = true;                                         // fours of the same bucket
                 if (uneven) {
 #pragma unroll
-                    for (int k = 0; k < STEP; ++k) to[k] = where(j0 + k, 0);
+                    for (int k = 0; k < STEP; ++k) to[k] = where.first(j0 + k);
 #pragma unroll
-                    for (int k = 0; k < STEP; ++k) wide = wide && to[k] & 1;
+                    for (int k = 0; k < STEP; ++k) wide = wide && to[k] >> 16;
                     wide = __all(wide);
                 }
 #pragma unroll
@@ -157,21 +162,21 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
                     for (int k = 0; k < STEP; ++k) {
                         const float all = (u[k].x + u[k].y) + (u[k].z + u[k].w);
                         if (uneven)
-                            run.add(sums, own, to[k] & ~1, all);
+                            run.add(sums, own, to[k] & 0xffff, all);
                         else
                             even += all;
                     }
                 } else {
-                    int each[STEP][4];
+                    unsigned each[STEP][4];
 #pragma unroll
                     for (int k = 0; k < STEP; ++k)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) each[k][i] = i == 0 ? to[k] : where(j0 + k, i);
+                        for (int i = 0; i < 4; ++i) each[k][i] = i == 0 ? to[k] & 0xffff : where.low(j0 + k, i);
                     reads_first();
 #pragma unroll
                     for (int k = 0; k < STEP; ++k)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) run.add(sums, own, each[k][i] & ~1, (&u[k].x)[i]);
+                        for (int i = 0; i < 4; ++i) run.add(sums, own, (int)each[k][i], (&u[k].x)[i]);
                 }
             }
     }
@@ -353,14 +358,16 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
         const bool docs = !walk.is_one(t), cut = a.causal && wlast > q.start + (int)over_group(a, t * L::ROWS) && wlast >= q.prefix;
         const int far = q.start + (int)over_group(a, min(t * L::ROWS + L::ROWS, rows) - 1);
         // whether some of the wavefront's keys are not in some rows' windows, and none in any's (64 bits: a window may end beyond 32)
-        bool late = false, none = false;
+        bool late = false, none = false, few = true;
         if (LOCAL) {
             const ArgsAgain w = again();
             const int64_t left = w->left, right = w->right;
             const int near = q.start + (int)over_group(a, t * L::ROWS);
             late = near + right < wlast || far - left > wk0;
             none = far + right < wk0 || near - left > wlast;
+            few = w->few_seen || q.kn <= FEW || (a.causal && near < FEW);
         }
+        const bool left_over = docs || a.cap > 0.f || ((cut || late) && few);
         t = walk.next(t + 1, t1, classify);
         vm_wait();
         __syncthreads();                                                  // the tile has landed, the one before it is no longer read
@@ -388,7 +395,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
                     dots<T, DP>(smem[buf][0], b, kf, sc, smem[buf][1], b, vf, g, lanes);
                 }
                 Weights<T> p, d, rest;
-                gradients<T, (DP > 64 ? 1 : 4), LOCAL, BIASED>(a, sc, g, p, d, rest, cut, docs, late, true, false, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
+                gradients<T, (DP > 64 ? 1 : 4), LOCAL, BIASED>(a, sc, g, p, d, rest, cut, docs, late, left_over, true, false, [&](int j) { return *(const float4*)&s_lse[buf][at(j)]; },
                              [&](int j) { return *(const float4*)&s_delta[buf][at(j)]; },
                              [&](int j) {
                                  const float4 by = *(const float4*)&s_slope[buf][at(j)], place = *(const float4*)&s_place[buf][at(j)];
@@ -430,7 +437,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
                              Nothing(), nullptr, true, run, even);
                 weigh<T, DP>(smem[buf][1], b, p, dv, lanes);
                 weigh<T, DP>(smem[buf][0], b, d, dk, lanes);
-                if (sizeof(T) == 2 && (cut || docs || late || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dk, lanes);
+                if (sizeof(T) == 2 && left_over) weigh<T, DP>(smem[buf][0], b, rest, dk, lanes);
             }
         }
         buf ^= 1;
@@ -599,6 +606,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
         const int k0 = span.at<LOCAL>(t) * L::ROWS;
         const bool cut = LOCAL ? k0 + L::ROWS > wend : k0 + L::ROWS > q.kn || (a.causal && k0 + L::ROWS - 1 > wnear && k0 + L::ROWS > q.prefix);
         const bool late = LOCAL && k0 < wbegin && k0 + L::ROWS > a.sinks;
+        const bool left_over = docs || a.cap > 0.f || ((cut || late) && (!LOCAL || a.few_seen || q.kn <= FEW || (a.causal && wnear < FEW)));
         const bool none = LOCAL ? k0 >= wend_far || (k0 + L::ROWS <= wbegin_near && k0 >= a.sinks) : a.causal && k0 > wfar && k0 >= q.prefix;
         const float from = (float)(place - k0 - 4 * half);
         t = walk.next(t + 1, t1, classify);
@@ -625,7 +633,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
                 const unsigned hidden = LOCAL ? max(place - a.left - a.sinks, 0) : 0;
                 const float mine = BIASED && !uneven ? lse - kept(front ? FRONT : BEHIND) : lse;
                 float even = 0.f;
-                gradients<T, (BIASED && DP > 96 ? 1 : 4), LOCAL, BIASED>(a, sc, g, p, d, rest, cut, docs, late, uneven, summed, [&](int) { return make_float4(mine, mine, mine, mine); },
+                gradients<T, (BIASED && DP > 96 ? 1 : 4), LOCAL, BIASED>(a, sc, g, p, d, rest, cut, docs, late, left_over, uneven, summed, [&](int) { return make_float4(mine, mine, mine, mine); },
                              [&](int) { return make_float4(delta, delta, delta, delta); },
                              [&](int j) {
                                  const float off = BIASED ? (float)(place - kb - 4 * half) : own_off, by = BIASED ? kept(SLOPE) : slope;
@@ -652,12 +660,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
                                  const float* own = s_bias + buf * a.bias_words + bias_from + at(j);
                                  return make_float4(own[0], own[1], own[2], own[3]);
                              },
-                             [&](int j, int i) { return s_bucket[buf * widths + bias_place - Learned::place(place) + at(j) + i]; },
+                             Words{s_bucket + buf * widths + bias_place - Learned::place(place) + at(0)},
                              s_sums + wave * sums_a_wave + (anew<256>((int)threadIdx.x) & (columns - 1)), columns == 64, run, even);
                 if (summed && !uneven)
-                    run.add(s_sums + wave * sums_a_wave + (anew<256>((int)threadIdx.x) & (columns - 1)), columns == 64, a.bucket_words[front ? 0 : 2 * a.reach] & ~1, even);
+                    run.add(s_sums + wave * sums_a_wave + (anew<256>((int)threadIdx.x) & (columns - 1)), columns == 64, a.bucket_words[front ? 0 : 2 * a.reach] & 0xffff, even);
                 weigh<T, DP>(smem[buf][0], b, d, dq, lanes);
-                if (sizeof(T) == 2 && (cut || docs || late || a.cap > 0.f)) weigh<T, DP>(smem[buf][0], b, rest, dq, lanes);
+                if (sizeof(T) == 2 && left_over) weigh<T, DP>(smem[buf][0], b, rest, dq, lanes);
             }
         }
         buf ^= 1;
@@ -704,6 +712,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
 
 // The first keys, which rows see wherever they stand: dk and dv of 32 of them and of a share of the rows that may see them, whose tiles the workgroup's wavefronts
 // take in turn, each with tiles of its own on their way through LDS; what they have is put together at the end.
+// (The first rows of causal calls and a narrow window's see few keys, see gradients().)
 template <typename T, int DP, bool BIASED>
 __global__ __launch_bounds__(256, 1) void first_keys_kernel(Args a) {
     using F = Few<T, DP>;
@@ -785,6 +794,7 @@ __global__ __launch_bounds__(256, 1) void first_keys_kernel(Args a) {
         auto at = [&](int j) { return 8 * j + 4 * half; };
         const int near = q.start + (int)over_group(a, t * 32);
         const bool cut = a.causal && k0 + 31 > near && k0 + 31 >= q.prefix;
+        const bool left_over = a.q_docs || a.cap > 0.f || a.few_seen || q.kn <= FEW || cut;
         const bool uneven = BIASED && (int64_t)near - a.reach < k0 + 31;  // (else all stand `reach` and more behind the keys)
         auto bias = [&](int j) {
             const int4 place = *(const int4*)&word[PLACE][at(j)], of = *(const int4*)&word[TABLE][at(j)];
@@ -807,7 +817,7 @@ __global__ __launch_bounds__(256, 1) void first_keys_kernel(Args a) {
         Weights<T> p, d, rest;
         Run run = {};
         float even = 0.f;
-        gradients<T, 4, true, BIASED>(a, sc, g, p, d, rest, cut, a.q_docs != nullptr, false, uneven, false,
+        gradients<T, 4, true, BIASED>(a, sc, g, p, d, rest, cut, a.q_docs != nullptr, false, left_over, uneven, false,
                      [&](int j) {
                          float4 v = *(const float4*)&word[LSE][at(j)];
                          if (BIASED && !uneven) {
@@ -836,7 +846,7 @@ __global__ __launch_bounds__(256, 1) void first_keys_kernel(Args a) {
                      Nothing(), bias, Nothing(), nullptr, true, run, even);
         weigh<T, DP>(douts, 0, p, dv, lanes);
         weigh<T, DP>(queries, 0, d, dk, lanes);
-        if (sizeof(T) == 2 && (cut || a.q_docs || a.cap > 0.f)) weigh<T, DP>(queries, 0, rest, dk, lanes);
+        if (sizeof(T) == 2 && left_over) weigh<T, DP>(queries, 0, rest, dk, lanes);
         asm volatile("" ::: "memory");
         stage = stage + 1 < STAGES ? stage + 1 : 0;
     }
@@ -911,10 +921,12 @@ __global__ __launch_bounds__(256) void add_kernel(Args a, int z0) {
     }
 }
 
-// The same of the first keys' gradients, dk (z = 0) and dv (1).
+// The same of the first keys' gradients, dk (z = 0) and dv (1), whose shares are many and values few: 16 threads to four neighbours, every sixteenth share
+// each (16384 rows in 256 shares 26 -> ADD us).
 template <typename T>
 __global__ __launch_bounds__(256) void add_sinks_kernel(Args a) {
-    const int z = blockIdx.z, s = a.seq0 + (int)blockIdx.y;
+    __shared__ float4 s_sum[16][16];
+    const int z = blockIdx.z, s = a.seq0 + (int)blockIdx.y, lane = threadIdx.x & 15, turn = threadIdx.x >> 4;
     Seq q;
     if (!sequence(a, s, q)) return;
     const int fours = a.head_dim / 4, a_key = a.kv_heads * fours, keys = a.sink_blocks * 32;
@@ -923,21 +935,34 @@ __global__ __launch_bounds__(256) void add_sinks_kernel(Args a) {
     const ps_strides to = z == 0 ? a.dks : a.dvs;
     T* out = (T*)(z == 0 ? a.dk : a.dv);
     const float by = z == 1 ? 1.f : by_x<T>(a);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i0 = (int64_t)blockIdx.x * 16; i0 < n; i0 += (int64_t)gridDim.x * 16) {
+        const int64_t i = i0 + lane;
         const int key = (int)(i / a_key), in_key = (int)(i - (int64_t)key * a_key), head = in_key / fours;
-        int first;
-        const int tiles = first_keys_rows(a, q, key / 32 * 32, first), parts = shares(tiles - first, a.sink_parts, a.sink_part_tiles);
-        float4 sum = part[i];
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < n) {
+            int first;
+            const int tiles = first_keys_rows(a, q, key / 32 * 32, first), parts = shares(tiles - first, a.sink_parts, a.sink_part_tiles);
 #pragma unroll 4
-        for (int p = 1; p < parts; ++p) {
-            const float4 v = part[p * step + i];
-            sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+            for (int p = turn; p < parts; p += 16) {
+                const float4 v = part[p * step + i];
+                sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+            }
         }
-        T* at = out + (int64_t)(q.k0 + key) * to.row + head * to.head + (in_key - head * fours) * 4;
-        if constexpr (sizeof(T) == 2)
-            *(uint2*)at = make_uint2(cvt_pk_bf16(sum.x * by, sum.y * by), cvt_pk_bf16(sum.z * by, sum.w * by));
-        else
-            *(float4*)at = make_float4(sum.x * by, sum.y * by, sum.z * by, sum.w * by);
+        s_sum[turn][lane] = sum;
+        __syncthreads();
+        if (turn == 0 && i < n) {
+#pragma unroll
+            for (int t = 1; t < 16; ++t) {
+                const float4 v = s_sum[t][lane];
+                sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+            }
+            T* at = out + (int64_t)(q.k0 + key) * to.row + head * to.head + (in_key - head * fours) * 4;
+            if constexpr (sizeof(T) == 2)
+                *(uint2*)at = make_uint2(cvt_pk_bf16(sum.x * by, sum.y * by), cvt_pk_bf16(sum.z * by, sum.w * by));
+            else
+                *(float4*)at = make_float4(sum.x * by, sum.y * by, sum.z * by, sum.w * by);
+        }
+        __syncthreads();
     }
 }
 
@@ -1009,7 +1034,7 @@ void launch(const Args& a, hipStream_t st) {
             });
         }
         if (a.sink_parts > 1) {
-            const unsigned blocks = (unsigned)min(((int64_t)a.sinks * a.kv_heads * a.head_dim / 4 + 255) / 256, (int64_t)4096);
+            const unsigned blocks = (unsigned)min(((int64_t)a.sinks * a.kv_heads * a.head_dim / 4 + 15) / 16, (int64_t)4096);
             in_turn(blocks, 32768, [&](unsigned n) { hipLaunchKernelGGL(add_sinks_kernel<T>, dim3(blocks, n, 2), dim3(256), 0, st, b); });
         }
     }

@@ -43,7 +43,7 @@ struct Row {
 
     // A tile of keys from k0 on and its values.  cut: some of the wavefront's rows see only the keys in front of their `end`; docs: documents
     // of its keys, null if the tile's and all rows' are one; late: some of the rows' windows begin behind keys that are not in front of a.sinks;
-    // uneven: the learned bias of key k0 + i is bias(i), else `even` for all of them, in powers of two.
+    // uneven: the learned bias of the tile's block b is bias(b), else `even` for all of them, in powers of two.
     template <typename Of>
     __device__ __forceinline__ void step(const Args& a, const unsigned char* keys, const unsigned char* values, const int* docs, int k0, bool cut, bool late, bool uneven,
                                          float even, Of bias) {
@@ -51,7 +51,7 @@ struct Row {
         const bool first = BIASED && uneven && a.cap == 0.f;              // (the bias is what the products start from)
 #pragma unroll
         for (int b = 0; b < L::BLOCKS; b += 2) {
-            auto start = [&](int b) { return Learned::start(first, half, [&](int i) { return bias(32 * b + i); }); };
+            auto start = [&](int b) { return first ? bias(b) : no_start(); };
             if constexpr (L::BLOCKS % 2 == 0) {
                 if constexpr (BIASED)
                     dots<T, DP>(keys, b, qf, sc[b], keys, b + 1, qf, sc[b + 1], lanes, start(b), start(b + 1));
@@ -88,9 +88,7 @@ struct Row {
         if constexpr (LOCAL) {
             if (BIASED && uneven && !first) {
 #pragma unroll
-                for (int b = 0; b < L::BLOCKS; ++b)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) sc[b][e] += bias(32 * b + row_of(e) + 4 * half);
+                for (int b = 0; b < L::BLOCKS; ++b) sc[b] += bias(b);
             }
             if (late) {
                 const int from = k0 + 4 * half - a.sinks;
@@ -284,7 +282,7 @@ __global__ __launch_bounds__(256, DP == 64 && !BIASED ? 3 : 2) void attend_kerne
             const float* bias = BIASED ? s_bias + buf * a.bias_words + (row.head - hk * a.group) * a.bias_width + place - Learned::place(row.place) : nullptr;
             const bool front = BIASED && k0 + L::ROWS - 1 <= wnear_place - a.reach, uneven = BIASED && !front && k0 < wfar_place + a.reach;
             row.step(a, smem[buf][0], smem[buf][1], one ? nullptr : s_doc[buf], k0, is_cut(k0), LOCAL && k0 < wbegin && k0 + L::ROWS > a.sinks, uneven,
-                     uneven ? 0.f : front ? bias_front : bias_behind, [&](int i) { return bias[i]; });
+                     uneven ? 0.f : front ? bias_front : bias_behind, [&](int b) { return Learned::start(true, half, [&](int i) { return bias[32 * b + i]; }); });
         }
         buf ^= 1;
     }
@@ -373,10 +371,18 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
     for (int i = 0; i < STAGES; ++i)
         if (sent < t1) send_next();
     Row<T, DP, 32, LOCAL, BIASED> row(a, q, hk, min(col, rows - 1), col < rows);
-    const float* table = BIASED ? a.table + (int64_t)row.head * (2 * a.reach + 1) + a.reach : nullptr;
+    // A learned bias: a row has one for all keys `reach` and more in front of it, one for those behind it, and others for few tiles.  (Asked for in front of all
+    // tiles they came no sooner: 64 single tokens over up to 4096 keys 90 us either way, 77 without a bias, 6 of the difference for its table.)
+    const float* const table = BIASED ? a.table + (int64_t)row.head * (2 * a.reach + 1) + a.reach : nullptr;
     const int place = Learned::place(row.place), near_place = Learned::place(near), far_place = (int)min((int64_t)far, (int64_t)INT32_MAX - a.reach);
     const float in_powers = a.cap > 0.f ? 1.f : a.scale * LOG2E;
     const float bias_front = BIASED ? table[-a.reach] * in_powers : 0.f, bias_behind = BIASED ? table[a.reach] * in_powers : 0.f;
+    auto biases = [&](int k0) {
+        f32x16 v;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = table[max(-a.reach, min(k0 + seqatt::row_of(e) + 4 * half - place, a.reach))];
+        return v;
+    };
     while (t < t1) {
         // (with a tile behind it every send of this one is WAIT sends old; the last ones wait for all)
         if (STAGES > 1 && sent < t1)
@@ -387,7 +393,7 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
         const bool cut = LOCAL ? k0 + 32 > end : k0 + 32 > q.kn || (a.causal && k0 + 31 > near && k0 + 32 > q.prefix);
         const bool front = BIASED && k0 + 31 <= near_place - a.reach, uneven = BIASED && !front && k0 < far_place + a.reach;
         row.step(a, smem[wave][stage][0], smem[wave][stage][1], a.k_docs ? s_doc[wave][stage] : nullptr, k0, cut,
-                 LOCAL && k0 < begin && k0 + 32 > a.sinks, uneven, uneven ? 0.f : front ? bias_front : bias_behind, [&](int i) { return table[max(-a.reach, min(k0 + i - place, a.reach))]; });
+                 LOCAL && k0 < begin && k0 + 32 > a.sinks, uneven, uneven ? 0.f : front ? bias_front : bias_behind, [&](int) { return biases(k0); });
         asm volatile("" ::: "memory");                                    // (its reads are over: their products are on their way)
         stage = stage + 1 < STAGES ? stage + 1 : 0;
         t = walk.next(t + 1, t1, classify);
@@ -563,10 +569,10 @@ __global__ __launch_bounds__(256) void table_kernel(const int32_t* buckets, cons
     const bool is = b >= 0 && b < n_buckets;
     table[(int64_t)h * (2 * reach + 1) + d] = is ? bias[(int64_t)b * heads + h] * by : 0.f;
     if (words && h == 0) {
-        // (its lowest bit: the next three distances have the same bucket)
+        // (bit 16: the next three distances have the same bucket)
         bool same = true;
         for (int i = 1; i < 4; ++i) same = same && buckets[min(d + i, 2 * reach)] == b;
-        words[d] = (is ? b : n_buckets) * columns + (same ? 1 : 0);
+        words[d] = (is ? b : n_buckets) * columns + (same ? 1 << 16 : 0);
     }
 }
 
@@ -680,6 +686,7 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         a.sinks = (local->left < 0 && local->right < 0) || a.max_q == 0 ? 0 : min(local->sinks, a.max_k);   // (without a window all are seen)
         a.reach = local->reach;
         a.n_buckets = local->n_buckets;
+        a.few_seen = a.left == INT32_MAX || (int64_t)a.left + (ahead ? a.right : 0) < FEW;   // (without a window in front as ps_attention_backward())
         const int64_t window = (int64_t)a.left + (ahead ? a.right : 0) + FIXED;
         auto lower = [](int64_t& to, int64_t by) { to = by < to ? by : to; };   // (the host's min() has 32 bits)
         lower(most_keys, window + a.sinks + 3 * a.tile);
@@ -714,6 +721,15 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         const int64_t tiles = (most_keys + 31) / 32, jobs = a.kv_heads * (all_keys / 32 + d->n_seq);
         const int64_t most = max((int64_t)1, ((int64_t)64 << 20) / max((int64_t)1, d->n_q * d->heads * d->head_dim));
         a.part_tiles = (int32_t)max(max(min(max((int64_t)16, jobs / 256), (int64_t)32), jobs / 1024), (tiles + most - 1) / most);
+        // (windows leave all sequences about the same: no more shares than fill the units, of 16 tiles or more)
+        const int64_t alone = (int64_t)a.kv_heads * d->n_seq, once = padded(d->head_dim) == 64 && d->dtype == 1 ? 512 : 256;
+        if (most_keys < a.max_k && alone > 0) {
+            int64_t wanted = alone < once ? once / alone : 1;
+            if (wanted > tiles / 16) wanted = tiles / 16;
+            if (wanted < 1) wanted = 1;
+            if (wanted > most) wanted = most;
+            a.part_tiles = (int32_t)((tiles + wanted - 1) / wanted);
+        }
         a.parts = (int32_t)max((int64_t)1, (tiles + a.part_tiles - 1) / a.part_tiles);
     } else {
         share(a.row_blocks, d->n_q * group, FIXED, most_keys, all_keys, a.tile, a.parts, a.part_tiles, INT32_MAX, most_keys < a.max_k);
@@ -723,12 +739,13 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
     // 4, 49 -> 43; fp32, 4 of 56, 4 heads on 1, 82 -> 56; 4 of 128 rows, 12 heads, would take 34 for 28).
     const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED;
     share(key_blocks, d->n_k, FIXED, most_rows, all_rows, a.key_tile, a.key_parts, a.key_part_tiles, d->dtype == 1 ? 256 : 128, most_rows < rows_a_seq);
-    // The first keys are seen from everywhere, so they have a launch of their own, 32 to a workgroup, their rows in shares: some 512, of 256 rows or
+    // The first keys are seen from everywhere, so they have a launch of their own, 32 to a workgroup, their rows in shares that fill the units once, of 256 rows or
     // more, within 256 MB.
     if (backward && a.sinks > 0 && d->n_seq > 0) {
         a.sink_blocks = (a.sinks + 31) / 32;
         const int64_t tiles = (rows_a_seq + 31) / 32, jobs = (int64_t)d->n_seq * a.kv_heads * a.sink_blocks, each = jobs * 32 * a.head_dim;
-        int64_t parts = jobs < 512 ? 512 / jobs : 1;
+        const int64_t once = padded(d->head_dim) == 64 && d->dtype == 1 ? 512 : 256;   // workgroups that the units hold
+        int64_t parts = jobs < once ? once / jobs : 1;
         if (parts > (32 << 20) / each) parts = (32 << 20) / each;
         if (parts > tiles / 8) parts = tiles / 8;
         if (parts < 1) parts = 1;
@@ -860,7 +877,7 @@ int forward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const 
         }
     };
     if constexpr (LOCAL) {
-        if (a.table) {
+        if (a.n_buckets > 0) {
             of_type(std::true_type());
             return hipGetLastError() == hipSuccess ? PS_OK : PS_EHIP;
         }
