@@ -707,9 +707,10 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         const int64_t jobs = a.kv_heads * all_tiles * max((int64_t)1, blocks / max(1, a.n_seq * a.kv_heads));
         part_tiles = (int32_t)min((int64_t)tiles, max((int64_t)least / tile, jobs / 2048));
         // (windows leave all blocks about the same: what fills the units once will do, and leaves less to be added up)
-        if (windowed) part_tiles = (int32_t)max((int64_t)least / tile, (tiles * blocks + ONCE - 1) / ONCE < tiles ? (tiles + ONCE / blocks - 1) / (ONCE / blocks) : (int64_t)tiles);
+        if (windowed && blocks > 0) part_tiles = (int32_t)max((int64_t)least / tile, (tiles * blocks + ONCE - 1) / ONCE < tiles ? (tiles + ONCE / blocks - 1) / (ONCE / blocks) : (int64_t)tiles);
         // (what the shares leave to be added up stays within 256 MB)
-        const int64_t most = max((int64_t)1, ((int64_t)64 << 20) / max((int64_t)1, tokens * a.kv_heads * a.head_dim));
+        const int64_t a_part = tokens * a.kv_heads * a.head_dim;
+        const int64_t most = local && a_part > INT32_MAX ? 1 : max((int64_t)1, ((int64_t)64 << 20) / max((int64_t)1, a_part));   // (the host's max() has 32 bits)
         part_tiles = (int32_t)max((int64_t)part_tiles, (tiles + most - 1) / most);
         parts = (tiles + part_tiles - 1) / part_tiles;
     };

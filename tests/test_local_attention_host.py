@@ -97,6 +97,16 @@ def test_workspace(lib):
     assert size(1, 1 << 20, 1 << 20, 1 << 20, 1 << 20, 8, 8, 64, bf16, True, left=1023, right=0, sinks=1 << 20) < 1 << 31
 
 
+# Bounds that leave no blocks of keys or rows, beside windows that are shorter than what is left; blocks whose number does not fit 32 bits.
+@pytest.mark.parametrize("n_seq,n_q,n_k,max_q,max_k", [(1, 1000, 33, 1000, 0), (1000, 1000, 100000, 1 << 20, 0), (0, 4096, 1 << 20, 1 << 20, 127), (2, 33, 1 << 20, 0, 1 << 20),
+                                                       (100000, 4096, 0, 1 << 20, 1000)])
+@pytest.mark.parametrize("how", [dict(left=1, right=0, sinks=1), dict(left=0), dict(left=100, right=100, sinks=1000, n_buckets=8, reach=16)])
+def test_workspace_without_blocks(lib, n_seq, n_q, n_k, max_q, max_k, how):
+    for heads, dtype in ((10, torch.bfloat16), (2, torch.float32)):
+        for back in (False, True):
+            assert 0 < ps.ps_local_attention_workspace_bytes(n_seq, n_q, n_k, max_q, max_k, heads, 2, 64, dtype, back, **how) < 1 << 30
+
+
 def test_the_binding_refuses():
     t = torch.zeros(4, 2, 8)
     with pytest.raises((TypeError, ValueError)):
