@@ -357,7 +357,8 @@ int ps_attention_backward(const ps_attention_desc* desc, const ps_attention_seqs
  *   reach        >= 0, at most 65536: larger distances have the bucket of that one
  *   buckets      [2 reach + 1] int32 on the device, as ps_bias_buckets() makes them or any others; a bucket that there is not (-1): no bias
  *   bias         [n_buckets][heads] float on the device
- * A key head's rows have at most 32 heads where there is a bias.  The time goes by the keys that are seen; tiles outside of all windows of a block of
+ * Where there is a bias, a key head's rows have at most 32 heads, heads is below 2^16 and heads * (2 reach + 1) below 2^31.  A bias of -infinity or
+ * of the type's lowest value hides its pairs.  The time goes by the keys that are seen; tiles outside of all windows of a block of
  * rows are not read. */
 typedef struct ps_attention_local {
     int32_t left, right, sinks, n_buckets, reach;

@@ -630,7 +630,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
                 const int own_left = BIASED ? 0 : end - k0 - 32 * b - 4 * half;
                 const float own_off = from - (float)(32 * b);
                 // keys behind the first ones that are in front of the window (late tiles alone: the places are near enough to the window's length)
-                const unsigned hidden = LOCAL ? max(place - a.left - a.sinks, 0) : 0;
+                const unsigned hidden = LOCAL ? max((int)((unsigned)place - (unsigned)a.left - (unsigned)a.sinks), 0) : 0;
                 const float mine = BIASED && !uneven ? lse - kept(front ? FRONT : BEHIND) : lse;
                 float even = 0.f;
                 gradients<T, (BIASED && DP > 96 ? 1 : 4), LOCAL, BIASED>(a, sc, g, p, d, rest, cut, docs, late, left_over, uneven, summed, [&](int) { return make_float4(mine, mine, mine, mine); },
@@ -987,7 +987,7 @@ __global__ __launch_bounds__(1024) void add_bias_kernel(const float* from, int64
 }
 void add_bias(const Args& a, float* dbias, hipStream_t st) {
     const int n = a.n_buckets * a.heads;
-    const int64_t blocks = a.parts * a.bias_blocks, each = blocks > 256 ? 128 : 256, chunks = (blocks + each - 1) / each;
+    const int64_t blocks = a.parts * a.bias_blocks, each = blocks > 256 ? 128 + blocks / 32768 : 256, chunks = (blocks + each - 1) / each;
     const unsigned across = (unsigned)((n + 63) / 64);
     float* const between = chunks > 1 ? a.bias_parts + blocks * n : dbias;
     hipLaunchKernelGGL(add_bias_kernel, dim3(across, (unsigned)(chunks > 1 ? chunks : 1)), dim3(1024), 0, st, a.bias_parts, blocks, each, n, between);

@@ -680,6 +680,8 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
     if (local) {
         if (local->sinks < 0 || local->n_buckets < 0 || local->reach < 0) return PS_EINVAL;
         if (local->n_buckets > 64 || local->reach > 65536 || (local->n_buckets > 0 && group > 32)) return PS_EUNSUPPORTED;
+        // (a grid's second dimension; places in the table have 32 bits)
+        if (local->n_buckets > 0 && (d->heads > 65535 || d->heads * (2 * (int64_t)local->reach + 1) > INT32_MAX)) return PS_EUNSUPPORTED;
         if (s && local->n_buckets > 0 && (!local->buckets || !local->bias || ((uintptr_t)local->buckets | (uintptr_t)local->bias) % 4 != 0)) return PS_EINVAL;
         if (local->left >= 0) a.left = local->left;
         if (local->right >= 0) a.right = local->right;

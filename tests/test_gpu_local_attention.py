@@ -185,6 +185,33 @@ def test_faulty_sequences(dtype):
     assert torch.equal(none.backward(*none.forward())[3], torch.zeros_like(none.bias))
 
 
+# Biases that hide a bucket's pairs: near ones and those of all that is further behind than reach, in tiles of one bias and of many.
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lowest", [float("-inf"), torch.finfo(torch.float32).min])
+@pytest.mark.parametrize("how", [dict(), dict(causal=True, cap=20.0), dict(left=200, right=150, sinks=3)], ids=["all", "cap", "window"])
+def test_a_bias_that_hides(dtype, lowest, how):
+    p = Local(dtype, [300, 7, 1], [300, 260, 260], 4, 2, 64, buckets=ol.buckets(32, 32), n_buckets=32, **how)
+    p.bias[3], p.bias[15], p.bias[17, 1], p.bias[31] = lowest, lowest, lowest, lowest
+    got = p.check()
+    assert not got[-1][3].any() and not got[-1][15].any()
+    p.bias[:] = lowest                                                       # nothing is left
+    out, lse, *grads = p.both()
+    assert not out.any() and (lse == -np.inf).all() and not any(g.any() for g in grads)
+
+
+# Calls whose bounds say that no sequence has a key, or a row.
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_bounds_of_zero(dtype):
+    p = Local(dtype, [700, 0, 40], [0, 0, 0], 4, 2, 64, left=3, right=2, sinks=5, buckets=BUCKETS, n_buckets=9)
+    p.max_k = 0
+    out, lse, dq, dk, dv, dbias = p.both()
+    assert not out.any() and (lse == -np.inf).all() and not dq.any() and not dbias.any()
+    p = Local(dtype, [0, 0], [700, 40], 4, 2, 64, left=3, right=2, sinks=5, buckets=BUCKETS, n_buckets=9)
+    p.max_q = 0
+    out, lse, dq, dk, dv, dbias = p.both()
+    assert not dk.any() and not dv.any() and not dbias.any()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_the_same_bits_every_time(dtype):
     p = Local(dtype, [900, 333], [900, 333], 8, 2, left=200, right=100, sinks=4, buckets=T5, n_buckets=32)

@@ -59,6 +59,7 @@ def test_refusals(lib, call):
     for change in (dict(n_buckets=65), dict(reach=65537)):
         assert call(lib, l=local(**change)) == EUNSUPPORTED, change
     assert call(lib, desc(heads=66, kv_heads=2, head_dim=8), local()) == EUNSUPPORTED
+    assert call(lib, desc(heads=65536, kv_heads=65536), local()) == call(lib, desc(heads=16384, kv_heads=16384), local(reach=65536)) == EUNSUPPORTED
     for change in (dict(dtype=2), dict(heads=3), dict(scale=0.0), dict(causal=2), dict(q=ps.ps_strides(256, 60))):
         assert call(lib, desc(**change), local()) == EINVAL, change
     assert call(lib, desc(head_dim=136), local()) == EUNSUPPORTED
