@@ -427,7 +427,7 @@ int ps_rotary_frequencies(int32_t n_pairs, double base, int scaling, double fact
  *   weight      [head_dim] of `dtype`, the same for all heads, or NULL: ones
  *   x2, weight2, out2  NULL, or a second pair of tensors (the keys) with heads2 heads and a weight of their own (or NULL), turned by the same angles
  *   positions   [n_rows] int32, any value;  frequencies [n_pairs] float (ps_rotary_frequencies()); n_pairs 0: no rotation, both may be NULL
- *   eps > 0;  strides: multiples of one element; heads whose size and turning pieces are multiples of 16 bytes, or 8, are moved faster
+ *   eps >= 2^-126;  strides: multiples of one element; heads whose size and turning pieces are multiples of 16 bytes, or 8, are moved faster
  * Errors: PS_EINVAL (null pointers, negative sizes or strides, 2 n_pairs > head_dim, eps), PS_EUNSUPPORTED (head_dim above 512, more than 2^26
  * elements in a row's heads, n_rows above 2^31 - 1), PS_EHIP. */
 typedef struct ps_norm_rotary_desc {

@@ -2,6 +2,7 @@
 //     r = 1 / sqrt(mean x^2 + eps),  u = r x,  out = turn(u w);   g = turn back(dout),  dw = sum g u,  dx = r (g w - u mean(g w u)).
 // A head stays in the registers of a few neighbouring lanes, which have all they need of it to themselves but two sums: those of x^2 and,
 // backwards, of g w x, which do not wait for one another.  So every tensor is read once and written once, and memory bounds the call.
+#include <float.h>
 #include <math.h>
 
 #include "internal.h"
@@ -321,7 +322,7 @@ int check(const ps_norm_rotary_desc* d, const void* x2) {
     if (!d || (d->dtype != 0 && d->dtype != 1) || d->head_dim < 1 || d->n_pairs < 0 || (int64_t)2 * d->n_pairs > d->head_dim || d->heads < 1 ||
         d->heads2 < 0 || d->n_rows < 0 || (d->interleaved & ~1) || (d->heads2 > 0) != (x2 != nullptr))
         return PS_EINVAL;
-    if (!(d->eps > 0.f) || isinf(d->eps)) return PS_EINVAL;
+    if (!(d->eps >= FLT_MIN) || isinf(d->eps)) return PS_EINVAL;          // (the root takes no smaller numbers, and a head may be zeros)
     // (a workgroup counts the heads of its rows, 16 at most, in 32 bits)
     if (d->head_dim > 512 || ((int64_t)d->heads + d->heads2) * d->head_dim > 1 << 26 || d->n_rows > INT32_MAX) return PS_EUNSUPPORTED;
     return PS_OK;

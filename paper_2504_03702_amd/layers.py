@@ -136,6 +136,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: Sequences
     window: how far rows see in front of themselves and behind (-1: without end); sinks: first keys that they see all the same; bias
     [n_buckets, heads], which is learned, by the buckets of distances ([2 reach + 1] int32 on the GPU, ``binding.ps_bias_buckets``)."""
     _constant(slopes, "attention", "slopes")
+    if (bias is None) != (buckets is None):
+        raise ValueError("attention: a bias goes with its buckets")
     if tuple(window) == (-1, -1) and bias is None and buckets is None:
         return _Attention.apply(q, k, v, seqs, scale, softcap, causal, slopes)
     return _LocalAttention.apply(q, k, v, bias, seqs, scale, softcap, causal, slopes, tuple(window), sinks, buckets)

@@ -64,7 +64,7 @@ def test_a_layer_and_its_gradients(dtype, bound, how):
     y = layers.attention(q, k, v, seqs, **{**how, **more} if more else how).reshape(n, hidden) @ og
     got = torch.autograd.grad(y, own, dy.to(DEV), allow_unused=True)
     assert ps.ps_status_read(status) == (0, -1)
-    near = lambda a, b: float((a.double().cpu() - b).norm() / b.norm())
+    near = lambda a, b: float((a.detach().double().cpu() - b).norm() / b.norm())
     assert near(y, want) <= bound
     for name, a, b in zip(("x", "qkv", "out", "wq", "wk", "bias"), got, wanted):
         assert (a is None) == (b is None) and (a is None or near(a, b) <= bound), (name, near(a, b))
@@ -132,7 +132,7 @@ def test_the_largest_numbers(dtype):
     for how in (dict(left=top, right=top), dict(left=0, right=0, sinks=top), dict(left=top, right=0, sinks=150)):
         p = Local(dtype, [150, 20], [150, 20], q_start=[-(1 << 30), 1 << 30], **how)
         p.check()
-        near = lambda a, b: float((a - b).float().norm()) <= 1e-2 * float(b.float().norm())
+        near = lambda a, b: float((a - b).detach().float().norm()) <= 1e-2 * float(b.detach().float().norm())
         if how.get("sinks"):
             assert all(near(a, b) for a, b in zip(p.both(), plain))
     # one bucket, of one distance, and a bias that leaves one key

@@ -125,3 +125,6 @@ def test_layer_function_refuses():
     seqs = layers.Sequences(torch.tensor([0, 4]), torch.tensor([0, 4]), 4, 4)
     with pytest.raises(ValueError):
         layers.attention(q, q, q, seqs, slopes=torch.zeros(2, requires_grad=True), window=(1, 1))
+    for how in (dict(bias=torch.zeros(3, 2)), dict(buckets=torch.zeros(3, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            layers.attention(q, q, q, seqs, **how)

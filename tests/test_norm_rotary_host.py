@@ -43,7 +43,7 @@ def backward(lib, **change):
 
 
 BOTH = [dict(d_dtype=2), dict(d_dtype=-1), dict(d_head_dim=0), dict(d_n_pairs=33), dict(d_n_pairs=-1), dict(d_heads=0), dict(d_heads2=-1), dict(d_heads2=0),
-        dict(d_n_rows=-1), dict(d_interleaved=2), dict(d_eps=0.0), dict(d_eps=-1.0), dict(d_eps=float("nan")), dict(d_eps=float("inf")),
+        dict(d_n_rows=-1), dict(d_interleaved=2), dict(d_eps=0.0), dict(d_eps=-1.0), dict(d_eps=1e-40), dict(d_eps=float("nan")), dict(d_eps=float("inf")),
         dict(x=None), dict(x2=None), dict(positions=None), dict(frequencies=None), dict(x=257), dict(weight=257), dict(weight2=257),
         dict(d_x=ps.ps_strides(-1, 64)), dict(d_x2=ps.ps_strides(128, -1))]
 
