@@ -158,3 +158,37 @@ def test_long_offsets():
         ps.ps_local_attention_forward(q, c, c, i32([0, 1]), i32([0, c.shape[0]]), 1, c.shape[0], out, lse, ws, causal=True, **how)
         got.append((out, lse))
     assert torch.allclose(got[0][0].float(), got[1][0].float(), atol=2e-2) and torch.allclose(got[0][1], got[1][1], atol=1e-4)
+
+
+def test_a_step_is_played_again():
+    """Forwards and backwards of both functions as one graph, over inputs that change from play to play."""
+    g = torch.Generator(device=DEV).manual_seed(5)
+    new = lambda *s: torch.randn(*s, generator=g, device=DEV)
+    n, offsets = 330, i32([0, 300, 330])
+    q, k, v = (new(n, h, 64).bfloat16().requires_grad_() for h in (4, 2, 2))
+    wq, wk = (new(64).bfloat16().requires_grad_() for _ in range(2))
+    bias, dy = new(32, 4).requires_grad_(), new(n, 4, 64).bfloat16()
+    buckets, positions, frequencies = ps.ps_bias_buckets(32, 128).to(DEV), torch.arange(n, dtype=torch.int32, device=DEV), ps.ps_rotary_frequencies(32).to(DEV)
+    seqs = layers.Sequences(offsets, offsets, 300, 300)
+
+    def step():
+        a, b = layers.norm_rotary(q, k, wq, wk, positions, frequencies)
+        y = layers.attention(a, b, v, seqs, causal=True, window=(100, -1), sinks=3, bias=bias, buckets=buckets)
+        return [y.detach(), *torch.autograd.grad(y, (q, k, v, wq, wk, bias), dy)]
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for play in range(3):
+        with torch.no_grad():
+            for t in (q, k, v, wq, wk, bias, dy):
+                t.copy_(torch.randn(t.shape, generator=g, device=DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = [t.clone() for t in got]
+        assert all(torch.equal(a, b) for a, b in zip(kept, step())), play
