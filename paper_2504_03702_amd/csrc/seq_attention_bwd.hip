@@ -573,7 +573,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
     }
     const int wnear_place = Learned::place(wnear), wfar_place = (int)min((int64_t)wfar, (int64_t)INT32_MAX - a.reach);   // (a key is below 2^30)
     if (summed)
-        for (int i = threadIdx.x; i < 4 * sums_a_wave; i += 256) s_sums[i] = 0.f;   // (the first tile's barrier is behind this)
+        for (int i = threadIdx.x; i < sums_a_wave; i += 256) ((float4*)s_sums)[i] = make_float4(0.f, 0.f, 0.f, 0.f);   // (the first tile's barrier is behind this)
     auto request = [&](int t, bool padded, int buf) {
         const int k0 = span.at<LOCAL>(t) * L::ROWS;
         if (k0 + L::ROWS <= q.kn && !padded && regular) {
@@ -677,20 +677,45 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
         // A bucket's sums of a head's lanes added up by `slices` neighbouring threads, a share of the rows each, which start at other rows from bucket to
         // bucket (all buckets have a row's sums in one bank).  Row r0 + x has head x % group less r0's.
         float* const to = a.bias_parts + ((int64_t)part * a.bias_blocks + (int64_t)q.q0 * a.group / FIXED + s + w.block) * a.n_buckets * a.heads;
-        const int outs = a.n_buckets * a.group, most = min(256 / outs, 32), slices = most < 1 ? 1 : 1 << (31 - __builtin_clz(most)), slice = threadIdx.x & (slices - 1);
-        for (int first = 0; first < outs; first += 256 / slices) {
-            const int i = first + (int)threadIdx.x / slices, b = i / a.group, h = i - b * a.group;
-            const int x0 = (h + a.group - r0 % a.group) % a.group, n = (FIXED - x0 + a.group - 1) / a.group, turns = (FIXED / a.group + slices) / slices;
-            float sum = 0.f;
-            if (i < outs)
-                for (int k = 0; k < turns; ++k) {
-                    const int m = slice + slices * ((k + i) % turns), x = x0 + m * a.group;
-                    if (m >= n) continue;
-                    const float* of = s_sums + (x >> 5) * sums_a_wave + b * columns + (x & 31);
-                    sum += columns == 64 ? of[0] + of[32] : of[0];
-                }
-            for (int o = 1; o < slices; o *= 2) sum += __shfl_xor(sum, o, 64);
-            if (i < outs && slice == 0) to[b * a.heads + hk * a.group + h] = sum;
+        if ((a.group & (a.group - 1)) == 0) {
+            // (heads that share keys by ones, twos, fours ..: a row's head goes by its column.  Eight neighbouring threads have a bucket, four columns of all
+            // wavefronts each)
+            const int c = threadIdx.x & 7;
+            for (int b = threadIdx.x >> 3; b < a.n_buckets; b += 32) {
+                float4 v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    v[i] = i < 4 || columns == 64 ? *(const float4*)(s_sums + (i & 3) * sums_a_wave + b * columns + 32 * (i >> 2) + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int n = 4; n > 0; n /= 2)
+#pragma unroll
+                    for (int i = 0; i < n; ++i) v[i] = make_float4(v[i].x + v[i + n].x, v[i].y + v[i + n].y, v[i].z + v[i + n].z, v[i].w + v[i + n].w);
+                float4 sum = v[0];
+                for (int o = 4; 4 * o >= a.group && o > 0; o /= 2)
+                    sum = make_float4(sum.x + __shfl_xor(sum.x, o, 64), sum.y + __shfl_xor(sum.y, o, 64), sum.z + __shfl_xor(sum.z, o, 64), sum.w + __shfl_xor(sum.w, o, 64));
+                if (a.group <= 2) sum = make_float4(sum.x + sum.z, sum.y + sum.w, 0.f, 0.f);
+                if (a.group == 1) sum.x += sum.y;
+                float* const mine = to + b * a.heads + hk * a.group + 4 * c;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (4 * c + i < a.group) mine[i] = (&sum.x)[i];
+            }
+        } else {
+            const int outs = a.n_buckets * a.group, most = min(256 / outs, 32), slices = most < 1 ? 1 : 1 << (31 - __builtin_clz(most)), slice = threadIdx.x & (slices - 1);
+            for (int first = 0; first < outs; first += 256 / slices) {
+                const int i = first + (int)threadIdx.x / slices, b = i / a.group, h = i - b * a.group;
+                const int x0 = (h + a.group - r0 % a.group) % a.group, n = (FIXED - x0 + a.group - 1) / a.group, turns = (FIXED / a.group + slices) / slices;
+                float sum = 0.f;
+                if (i < outs)
+                    for (int k = 0; k < turns; ++k) {
+                        const int m = slice + slices * ((k + i) % turns), x = x0 + m * a.group;
+                        if (m >= n) continue;
+                        const float* of = s_sums + (x >> 5) * sums_a_wave + b * columns + (x & 31);
+                        sum += columns == 64 ? of[0] + of[32] : of[0];
+                    }
+                for (int o = 1; o < slices; o *= 2) sum += __shfl_xor(sum, o, 64);
+                if (i < outs && slice == 0) to[b * a.heads + hk * a.group + h] = sum;
+            }
         }
     }
     if (wr0 >= rows) return;
