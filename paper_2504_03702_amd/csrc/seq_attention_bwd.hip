@@ -1043,11 +1043,11 @@ void launch(const Args& a, hipStream_t st) {
         lds_attr_set = true;
     }
     in_turn(row_jobs, a.n_seq, [&](unsigned n) {
-        b.listed = add_up(n, a.row_blocks, a.parts);
+        b.listed = add_up(a, n, a.row_blocks, a.parts);
         hipLaunchKernelGGL((query_gradients_kernel<T, DP, LOCAL, BIASED>), dim3((unsigned)row_jobs * n), dim3(256), tile_lds + sums_lds, st, b);
     });
     in_turn(key_jobs, a.n_seq, [&](unsigned n) {
-        b.listed = add_up(n, key_blocks, a.key_parts);
+        b.listed = add_up(a, n, key_blocks, a.key_parts);
         if (BIASED) set_width(b, FIXED + (a.key_tile - 1) / a.group + 2);
         hipLaunchKernelGGL((key_gradients_kernel<T, DP, LOCAL, BIASED>), dim3((unsigned)key_jobs * n), dim3(256), BIASED ? 2 * b.bias_words * sizeof(float) : 0, st, b);
     });

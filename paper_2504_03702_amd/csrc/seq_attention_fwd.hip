@@ -586,7 +586,7 @@ void launch_attend(const Args& a, hipStream_t st) {
         b.seq0 = s0;
         b.seqs = n;
         b.together = turns(per_seq, n);
-        b.listed = add_up(n, a.row_blocks, a.parts);
+        b.listed = add_up(a, n, a.row_blocks, a.parts);
         const dim3 grid((unsigned)(per_seq * n));
         const unsigned lds = BIASED ? 2 * a.bias_words * sizeof(float) : 0;
         if (a.few)
@@ -622,7 +622,10 @@ namespace seqatt {
 
 // Whether workgroups add up what work there is: where blocks are shared out, which leaves much of the grid without any.  Of whole blocks
 // the empty ones do not matter (64 sequences of 4 to 512 tokens, forwards / keys' gradients 37 / 53 us either way).
-bool add_up(int32_t seqs, int64_t blocks, int32_t parts) { return seqs <= 64 && blocks <= 64 && parts > 1; }
+// (longest first, more than the units hold take less time all the same, see look_for_work())
+bool add_up(const Args& a, int32_t seqs, int64_t blocks, int32_t parts) {
+    return seqs <= 64 && blocks <= 64 && (parts > 1 || (a.sorted && seqs * blocks * a.kv_heads > 512));
+}
 
 // Distances that a head has in a tile, and the words of all heads.
 void set_width(Args& a, int width) {
@@ -691,6 +694,7 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         a.few_seen = a.left == INT32_MAX || (int64_t)a.left + (ahead ? a.right : 0) < FEW;   // (without a window in front as ps_attention_backward())
         const int64_t window = (int64_t)a.left + (ahead ? a.right : 0) + FIXED;
         auto lower = [](int64_t& to, int64_t by) { to = by < to ? by : to; };   // (the host's min() has 32 bits)
+        a.sorted = window + a.sinks + 3 * a.tile >= a.max_k;
         lower(most_keys, window + a.sinks + 3 * a.tile);
         lower(most_rows, window * group + 3 * a.key_tile);
         lower(all_keys, d->n_seq * most_keys);
