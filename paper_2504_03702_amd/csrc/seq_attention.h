@@ -56,6 +56,7 @@ struct Args {
     float slope_by, cap_in;            // see Row and Cap
     // ps_local_attention_*() alone, whose kernels are the same with LOCAL:
     int32_t left, right, sinks;        // a row's window, and the first keys that it sees all the same
+    int32_t local;                     // 1
     int32_t sorted;                    // sequences' work goes by their lengths: the longest first, if workgroups find it by adding up
     int32_t few_seen;                  // the window holds FEW keys at most, or has no end in front
     int32_t sink_blocks, sink_parts, sink_part_tiles;   // those in blocks of 32, shares of their tiles of 32 rows

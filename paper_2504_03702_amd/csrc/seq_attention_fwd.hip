@@ -623,9 +623,10 @@ namespace seqatt {
 
 // Whether workgroups add up what work there is: where blocks are shared out, which leaves much of the grid without any.  Of whole blocks
 // the empty ones do not matter (64 sequences of 4 to 512 tokens, forwards / keys' gradients 37 / 53 us either way).
-// (longest first, more than the units hold take less time all the same, see look_for_work())
+// (LOCAL: launches of more than one to a unit take less time all the same: 8 fp32 sequences of 100 to 1023 tokens, 8 heads of 80 on 4, window 50 and 77,
+// forwards / queries' gradients 61 / 99 -> 40 / 56 us; 8 of 1500 to 2048, 16 heads of 128 on 4, window 768, 186 / 410 -> 180 / 382)
 bool add_up(const Args& a, int32_t seqs, int64_t blocks, int32_t parts) {
-    return seqs <= 64 && blocks <= 64 && (parts > 1 || (a.sorted && seqs * blocks * a.kv_heads > 512));
+    return seqs <= 64 && blocks <= 64 && (parts > 1 || (a.local && seqs > 1 && seqs * blocks * a.kv_heads > 256));
 }
 
 // Distances that a head has in a tile, and the words of all heads.
@@ -693,28 +694,42 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         a.reach = local->reach;
         a.n_buckets = local->n_buckets;
         a.few_seen = a.left == INT32_MAX || (int64_t)a.left + (ahead ? a.right : 0) < FEW;   // (without a window in front as ps_attention_backward())
-        const int64_t window = (int64_t)a.left + (ahead ? a.right : 0) + FIXED;
+        const int64_t window = (int64_t)a.left + (ahead ? a.right : 0) + FIXED, key_window = window - FIXED + FIXED / group + 2;
         auto lower = [](int64_t& to, int64_t by) { to = by < to ? by : to; };   // (the host's min() has 32 bits)
-        a.sorted = window + a.sinks + 3 * a.tile >= a.max_k;
-        lower(most_keys, window + a.sinks + 3 * a.tile);
+        lower(most_keys, key_window + a.sinks + 3 * a.tile);
+        a.local = 1;
+        a.sorted = most_keys == a.max_k;
         lower(most_rows, window * group + 3 * a.key_tile);
         lower(all_keys, d->n_seq * most_keys);
         lower(all_rows, d->n_seq * most_rows);
     }
     auto share = [&](int64_t blocks_a_seq, int64_t tokens, int64_t tokens_a_block, int64_t passing, int64_t all_passing, int tile, int32_t& parts,
-                     int32_t& part_tiles, int64_t chain, bool windowed) {
-        constexpr int64_t ONCE = 512;
+                     int32_t& part_tiles, int64_t chain, bool windowed, bool alone) {
         const int tiles = (int)((passing + tile - 1) / tile);
         const int64_t all_tiles = all_passing / tile + a.n_seq;
         const int64_t blocks = a.kv_heads * min((int64_t)a.n_seq * blocks_a_seq, tokens / tokens_a_block + a.n_seq);
         parts = 1;
         part_tiles = tiles;
         const int least = blocks < 128 && passing > chain ? 64 : 256;
-        if (blocks >= 512 || tiles < 2 * least / tile) return;
+        if (blocks >= 512 || tiles < (windowed ? 8 : 2 * least / tile)) return;
         const int64_t jobs = a.kv_heads * all_tiles * max((int64_t)1, blocks / max(1, a.n_seq * a.kv_heads));
         part_tiles = (int32_t)min((int64_t)tiles, max((int64_t)least / tile, jobs / 2048));
-        // (windows leave all blocks about the same: what fills the units once will do, and leaves less to be added up)
-        if (windowed && blocks > 0) part_tiles = (int32_t)max((int64_t)least / tile, (tiles * blocks + ONCE - 1) / ONCE < tiles ? (tiles + ONCE / blocks - 1) / (ONCE / blocks) : (int64_t)tiles);
+        // Windows leave all blocks about the same, so they come in rounds of what the units hold, two workgroups or one (alone: fp32 products take all of a unit), as many shares as make the
+        // rounds' tiles fewest, with two for what a share takes besides and two for the sum (8 fp32 sequences of 100 to 1023 tokens, 8 heads of 80 on 4, window 50
+        // and 77: keys' gradients 131 -> 95 us).
+        if (windowed) {
+            const int64_t by_tokens = tokens / tokens_a_block + (a.n_seq + 1) / 2, by_bounds = a.n_seq * blocks_a_seq;
+            const int64_t likely = a.kv_heads * (by_bounds < by_tokens ? by_bounds : by_tokens), once = alone ? 256 : 512;
+            int64_t fewest = (likely + once - 1) / once * (tiles + 2);
+            part_tiles = tiles;
+            for (int p = 2; tiles >= 4 * p && p <= 16; ++p) {
+                const int each = (tiles + p - 1) / p;
+                const int64_t all = (likely * p + once - 1) / once * (each + 2) + 2;
+                if (all >= fewest) continue;
+                fewest = all;
+                part_tiles = each;
+            }
+        }
         // (what the shares leave to be added up stays within 256 MB)
         const int64_t a_part = tokens * a.kv_heads * a.head_dim;
         const int64_t most = local && a_part > INT32_MAX ? 1 : max((int64_t)1, ((int64_t)64 << 20) / max((int64_t)1, a_part));   // (the host's max() has 32 bits)
@@ -740,13 +755,13 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         }
         a.parts = (int32_t)max((int64_t)1, (tiles + a.part_tiles - 1) / a.part_tiles);
     } else {
-        share(a.row_blocks, d->n_q * group, FIXED, most_keys, all_keys, a.tile, a.parts, a.part_tiles, INT32_MAX, most_keys < a.max_k);
+        share(a.row_blocks, d->n_q * group, FIXED, most_keys, all_keys, a.tile, a.parts, a.part_tiles, INT32_MAX, most_keys < a.max_k, d->dtype == 0);
     }
     // Of few blocks of keys, shares of 64 rows: a block's chain of tiles, the rows of all its head's heads, is all that takes time.  The sum's launch
     // is worth it above 256 rows, 128 in fp32 (passes of 1 sequence of 191 tokens, 48 heads on 12, 61 -> 52 us; 14 of up to 70, 16 heads of 128 on
     // 4, 49 -> 43; fp32, 4 of 56, 4 heads on 1, 82 -> 56; 4 of 128 rows, 12 heads, would take 34 for 28).
     const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED;
-    share(key_blocks, d->n_k, FIXED, most_rows, all_rows, a.key_tile, a.key_parts, a.key_part_tiles, d->dtype == 1 ? 256 : 128, most_rows < rows_a_seq);
+    share(key_blocks, d->n_k, FIXED, most_rows, all_rows, a.key_tile, a.key_parts, a.key_part_tiles, d->dtype == 1 ? 256 : 128, most_rows < rows_a_seq, d->dtype == 0);
     // The first keys are seen from everywhere, so they have a launch of their own, 32 to a workgroup, their rows in shares that fill the units once, of 256 rows or
     // more, within 256 MB.
     if (backward && a.sinks > 0 && d->n_seq > 0) {
