@@ -64,7 +64,7 @@ def test_a_layer_and_its_gradients(dtype, bound, how):
     y = layers.attention(q, k, v, seqs, **{**how, **more} if more else how).reshape(n, hidden) @ og
     got = torch.autograd.grad(y, own, dy.to(DEV), allow_unused=True)
     assert ps.ps_status_read(status) == (0, -1)
-    near = lambda a, b: float((a.detach().double().cpu() - b.detach()).norm() / b.norm())
+    near = lambda a, b: float((a.detach().double().cpu() - b.detach()).norm() / b.detach().norm())
     assert near(y, want) <= bound
     for name, a, b in zip(("x", "qkv", "out", "wq", "wk", "bias"), got, wanted):
         assert (a is None) == (b is None) and (a is None or near(a, b) <= bound), (name, near(a, b))
