@@ -185,6 +185,42 @@ def test_faulty_sequences(dtype):
     assert torch.equal(none.backward(*none.forward())[3], torch.zeros_like(none.bias))
 
 
+def many(seed, n, longest):
+    """Lengths of n sequences: none, one, the longest and others in no order."""
+    r = np.random.RandomState(seed)
+    lens = [int(x) for x in r.randint(1, 1 + longest // 4, n)]
+    for i, m in zip(r.permutation(n)[:7], (0, 0, 1, longest, longest, longest - 1, longest // 2)):
+        lens[i] = m
+    return lens
+
+
+# More blocks than units: of 64 sequences and fewer workgroups add up what there is, the longest first without a window; of more they count as the grid does.
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,longest", [(64, 300), (33, 300), (67, 200)])
+@pytest.mark.parametrize("how", [dict(buckets=T5, n_buckets=32), dict(causal=True, left=30, sinks=3, buckets=BUCKETS, n_buckets=9), dict(causal=True, left=1000)], ids=["bias", "both", "causal"])
+def test_many_sequences(dtype, n, longest, how):
+    lens = many(n, n, longest)
+    Local(dtype, lens, lens, 4, 4, 64, **how).check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("how", [dict(buckets=T5, n_buckets=32), dict(left=30, right=20, sinks=3)], ids=["bias", "window"])
+def test_faulty_ones_among_many(dtype, how):
+    lens = many(5, 64, 300)
+    p = Local(dtype, lens, lens, 4, 4, 64, **how)
+    whole = p.both()
+    p.max_q, p.status = 298, ps.new_status(DEV)
+    got = p.both()
+    bad = [s for s in range(64) if lens[s] > 298]
+    code, which = ps.ps_status_read(p.status)
+    assert len(bad) == 3 and code == ps.PS_ST_BAD_LENGTH and which in bad
+    # (their shares may be others, for other bounds: fp32 sums in another order, rounded once)
+    for i in (0, 2, 3, 4):
+        for s in range(64):
+            x, y = (t[i][p.qo[s]:p.qo[s + 1]].float() for t in (got, whole))
+            assert torch.all(x == 7.0) if s in bad else torch.allclose(x, y, rtol=2.0 ** -7, atol=1e-5), (i, s)
+
+
 # Biases that hide a bucket's pairs: near ones and those of all that is further behind than reach, in tiles of one bias and of many.
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("lowest", [float("-inf"), torch.finfo(torch.float32).min])
