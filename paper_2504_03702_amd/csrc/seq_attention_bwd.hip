@@ -151,11 +151,19 @@ __device__ __forceinline__ void gradients(const Args& a, const f32x16& s, const 
                     for (int k = 0; k < STEP; ++k) wide = wide && to[k] >> 16;
                     wide = __all(wide);
                 }
+                // (without a cap they are d.  Under one they are made of p, of pairs that have some: a hidden one's dout . v may pass all numbers)
 #pragma unroll
                 for (int k = 0; k < STEP; ++k) {
+                    if (a.cap == 0.f) {
+                        u[k] = v[k];
+                        continue;
+                    }
                     const float4 t = delta(j0 + k);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) (&u[k].x)[i] *= g[4 * (j0 + k) + i] - (&t.x)[i];
+                    for (int i = 0; i < 4; ++i) {
+                        float& e = (&u[k].x)[i];
+                        e = e == 0.f ? 0.f : e * (g[4 * (j0 + k) + i] - (&t.x)[i]);
+                    }
                 }
                 if (!uneven || wide) {
 #pragma unroll
