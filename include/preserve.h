@@ -359,7 +359,8 @@ int ps_attention_backward(const ps_attention_desc* desc, const ps_attention_seqs
  *   bias         [n_buckets][heads] float on the device
  * Where there is a bias, a key head's rows have at most 32 heads, heads is below 2^16 and heads * (2 reach + 1) below 2^31.  A bias of -infinity or
  * of the type's lowest value hides its pairs.  The time goes by the keys that are seen; tiles outside of all windows of a block of
- * rows are not read. */
+ * rows are not read.  A key that no row of its sequence has in its window, or among the first ones, matters to nobody in the forward call, whatever it holds (rows of
+ * a cache between the first keys and the window that were given to others); in the backward call it has to be finite, as other keys that a query does not see. */
 typedef struct ps_attention_local {
     int32_t left, right, sinks, n_buckets, reach;
     const int32_t* buckets;

@@ -79,6 +79,9 @@ __device__ __forceinline__ ArgsAgain again() {
     return a;
 }
 
+// (scalars: the compiler does not see that all lanes have the same, and would count and address tiles in vector registers)
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 struct Seq {
     int q0, qn, k0, kn, start, prefix;
 };
@@ -500,6 +503,19 @@ __device__ __forceinline__ void weigh(const unsigned char* tile, int b, const We
     }
 }
 
+// Keys that some of a workgroup's rows see in their windows or among the first ones.  A key outside of all windows may be anything (a cache's row that is somebody else's by
+// now), and its weight of 0 is to make zeros of its values: so they are zeros in a tile.  (One token over each of 8 short caches 7.4 -> 7.7 us, two rows of 8192 in a window of 128 288 -> 289;
+// with zeros in place of the keys too, and in the queries' gradients, 8.0 and 290.)
+struct SeenKeys {
+    int begin, end, sinks;
+    __device__ __forceinline__ SeenKeys(const Args& a, const Seq& q, int near, int far)
+        : begin(scalar(window_begin(a, near))), end(scalar(seen_to<true>(a, q, far))), sinks(a.sinks) {}
+    __device__ __forceinline__ bool all(int k0, int n) const { return (k0 + n <= end) & ((k0 >= begin) | (k0 + n <= sinks)); }
+    __device__ __forceinline__ bool has(int k) const { return (k < end) & ((k >= begin) | (k < sinks)); }
+    // of a tile from k0 on, a bit each
+    __device__ __forceinline__ uint64_t those(int k0) const { return __ballot(has(k0 + (int)(threadIdx.x & 63))); }
+};
+
 static __device__ const uint4 zeros = {0, 0, 0, 0};
 static __device__ const uint32_t infinity_word = 0x7f800000u, minus_one = 0xffffffffu;
 
@@ -549,6 +565,13 @@ struct Sender {
             const int i = row_of(j, thread);
             send(tile, j, there >> i & 1 ? (const void*)(row(i) + element(j, thread, head_dim)) : (const void*)&zeros);
         }
+    }
+    // zeros for the rows that are not among the seen keys
+    __device__ __forceinline__ void whole(unsigned char* tile, const T* first, int k0, const SeenKeys& seen) const {
+        const int thread = anew<256>((int)threadIdx.x);
+#pragma unroll
+        for (int j = 0; j < L::PER_THREAD; ++j)
+            send(tile, j, seen.has(k0 + row_of(j, thread)) ? (const char*)first + (SAME ? j * apart : 0) + off[SAME ? 0 : j] : (const char*)&zeros);
     }
 };
 // Which rows of a tile from k0 on are keys and no padding (asked only of tiles that have some), a bit each.
@@ -603,11 +626,15 @@ struct Few {
             send(tile, j, there >> i & 1 ? (const void*)(row(i) + element(j, lane, head_dim)) : (const void*)&zeros);
         }
     }
+    __device__ __forceinline__ void whole(unsigned char* tile, int x, const void* first, int k0, const SeenKeys& seen) const {
+        const int lane = anew<256>((int)(threadIdx.x & 63));
+#pragma unroll
+        for (int j = 0; j < SENDS; ++j)
+            send(tile, j, seen.has(k0 + row_of(j, lane)) ? (const char*)first + j / PERIOD * ROWS_A_PERIOD * step[x] + off[x][j % PERIOD] : (const char*)&zeros);
+    }
 };
 
 // ---- which tiles are seen: 64 of them at a time, a lane each, as masks ----------------------------------------------------
-// (scalars: the compiler does not see that all lanes have the same, and would count and address tiles in vector registers)
-__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ uint64_t scalars(uint64_t x) { return (uint64_t)(uint32_t)scalar((int)(x >> 32)) << 32 | (uint32_t)scalar((int)x); }
 struct Walk {
     int group = -1;

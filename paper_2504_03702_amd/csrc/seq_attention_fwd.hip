@@ -247,6 +247,7 @@ __global__ __launch_bounds__(256, DP == 64 && !BIASED ? 3 : 2) void attend_kerne
     const float bias_front = BIASED ? ends[0] * in_powers : 0.f, bias_behind = BIASED ? ends[2 * a.reach] * in_powers : 0.f;
     const int wnear_place = Learned::place(wnear), wfar_place = (int)min((int64_t)wfar, (int64_t)INT32_MAX - a.reach);   // (a key is below 2^30)
 
+    const SeenKeys seen(a, q, q.start + (int)over_group(a, r0), far);
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
     const Sender<T, DP, L::ROWS, true> keys(a.ks, 1, a.head_dim), values(a.vs, 1, a.head_dim);
@@ -256,9 +257,13 @@ __global__ __launch_bounds__(256, DP == 64 && !BIASED ? 3 : 2) void attend_kerne
         // (rows past the keys, and padding, are zeros: their weights are, and nothing is to come of them)
         if (k0 + L::ROWS <= q.kn && !padded && regular) {
             keys.whole(smem[buf][0], kbase + k0 * a.ks.row);
-            values.whole(smem[buf][1], vbase + k0 * a.vs.row);
+            if (!LOCAL || seen.all(k0, L::ROWS))
+                values.whole(smem[buf][1], vbase + k0 * a.vs.row);
+            else
+                values.whole(smem[buf][1], vbase + k0 * a.vs.row, k0, seen);
         } else {
-            const uint64_t there = keys_there(a, q, k0, padded);
+            uint64_t there = keys_there(a, q, k0, padded);
+            if (LOCAL) there &= seen.those(k0);
             keys.rows(smem[buf][0], a.head_dim, there, [&](int i) { return kbase + (k0 + i) * a.ks.row; });
             values.rows(smem[buf][1], a.head_dim, there, [&](int i) { return vbase + (k0 + i) * a.vs.row; });
         }
@@ -336,6 +341,7 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
     const int tiles = span.tiles, t0 = part * a.part_tiles, t1 = min(tiles, t0 + a.part_tiles);
     if (t0 > 0 && t0 >= tiles) return;                                    // (part 0 writes, keys or not)
 
+    const SeenKeys seen(a, q, q.start, q.start + q.qn - 1);
     const T* kbase = (const T*)a.k + q.k0 * a.ks.row + hk * a.ks.head;
     const T* vbase = (const T*)a.v + q.k0 * a.vs.row + hk * a.vs.head;
     const F few(a);
@@ -345,9 +351,13 @@ __global__ __launch_bounds__(256, (Few<T, DP>::WORKGROUPS)) void attend_few_kern
         unsigned char *keys = smem[wave][stage][0], *values = smem[wave][stage][1];
         if (regular && k0 + 32 <= q.kn && !a.k_docs) {
             few.whole(keys, 0, kbase + k0 * a.ks.row);
-            few.whole(values, 1, vbase + k0 * a.vs.row);
+            if (!LOCAL || seen.all(k0, 32))
+                few.whole(values, 1, vbase + k0 * a.vs.row);
+            else
+                few.whole(values, 1, vbase + k0 * a.vs.row, k0, seen);
         } else {
-            const uint64_t there = keys_there(a, q, k0, a.k_docs != nullptr);
+            uint64_t there = keys_there(a, q, k0, a.k_docs != nullptr);
+            if (LOCAL) there &= seen.those(k0);
             F::rows(keys, a.head_dim, there, [&](int i) { return kbase + (k0 + i) * a.ks.row; });
             F::rows(values, a.head_dim, there, [&](int i) { return vbase + (k0 + i) * a.vs.row; });
         }

@@ -42,3 +42,57 @@ def test_hidden_values_may_be_the_largest(dtype, cap, kind):
         p.v[gone] = torch.finfo(dtype).max * torch.sign(p.v[gone])
         for name, x, y in zip(("out", "lse", "dq", "dk", "dv", "dbias"), p.both(), clean):
             assert torch.equal(x, y), name
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("kind", ["window", "causal", "ahead"])
+@pytest.mark.parametrize("bias", [{}, BIASES], ids=["plain", "bias"])
+def test_keys_outside_of_all_windows_may_be_anything(dtype, bad, kind, bias):
+    """Forwards: rows of a cache that were never written, or are somebody else's by now, in front of all windows, behind all, in tiles that are read and
+    in such that are not."""
+    q_lens, k_lens, how = UNSEEN[kind]
+    for heads, kv_heads, size in ((4, 2, 64), (3, 3, 80), (16, 4, 128)):
+        p = Local(dtype, q_lens, k_lens, heads, kv_heads, size, **bias, **how)
+        clean, gone = p.forward(), nobody_sees(p)
+        p.k[gone] = p.v[gone] = bad
+        assert all(torch.equal(x, y) for x, y in zip(p.forward(), clean)), (heads, size)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("bias", [{}, BIASES], ids=["plain", "bias"])
+def test_single_tokens_over_freed_keys(dtype, causal, bias):
+    """One token a sequence, or a few: by one workgroup for all keys and by several."""
+    for q_lens, k_lens, left in (([1, 1, 3], [5000, 700, 301], 1500), ([1, 1], [129, 4001], 60)):
+        for heads, kv_heads, size in ((4, 2, 64), (3, 3, 80), (8, 2, 128)):
+            p = Local(dtype, q_lens, k_lens, heads, kv_heads, size, causal=causal, left=left, right=0, sinks=5, **bias)
+            clean, gone = p.forward(), nobody_sees(p)
+            p.k[gone] = p.v[gone] = float("nan")
+            assert all(torch.equal(x, y) for x, y in zip(p.forward(), clean))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("heads,kv_heads", [(2, 1), (4, 4)])
+def test_rows_of_far_tiles_are_not_read(dtype, heads, kv_heads):
+    """A key's gradients come from the rows in whose windows its block is: others', of tiles further on, may be anything.  (Blocks of 128 keys, tiles of at most 64 tokens: rows
+    from 700 on are in no tile of a window of keys in front of 512; blocks of rows in front of 640 have none of them.)"""
+    p = Local(dtype, [1300, 40], [1300, 40], heads, kv_heads, left=30, right=20)
+    clean = p.both()
+    p.q[700:1300] = p.dout[700:1300] = float("nan")
+    for name, x, y in zip(("out", "lse", "dq", "dk", "dv"), p.both(), clean):
+        if name == "lse":
+            x, y = x.t(), y.t()
+        n = 512 if name in ("dk", "dv") else 640
+        assert torch.equal(x[:n], y[:n]) and torch.equal(x[1300:], y[1300:]), name
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bias", [{}, BIASES], ids=["plain", "bias"])
+def test_keys_of_far_tiles_are_not_read(dtype, bias):
+    """Both directions, where keys in front of all windows fill their tiles (keys in front of 256 for rows from 400 on, which see 60)."""
+    p = Local(dtype, [40, 5], [440, 5], causal=True, left=60, **bias)
+    clean = p.both()
+    p.k[:256] = p.v[:256] = float("nan")
+    for name, x, y in zip(("out", "lse", "dq", "dk", "dv", "dbias"), p.both(), clean):
+        assert torch.equal(x, y), name
