@@ -58,7 +58,7 @@ struct Args {
     int32_t left, right, sinks;        // a row's window, and the first keys that it sees all the same
     int32_t local;                     // 1
     int32_t sorted;                    // sequences' work goes by their lengths: the longest first, if workgroups find it by adding up
-    int32_t few_seen;                  // the window holds FEW keys at most, or has no end in front
+    int32_t few_first, few_last;       // see few_in_window()
     int32_t sink_blocks, sink_parts, sink_part_tiles;   // those in blocks of 32, shares of their tiles of 32 rows
     float *sink_dk, *sink_dv;          // [sink_parts][n_seq][sink_blocks * 32][kv_heads][head_dim]
     const float* table;                // [heads][2 reach + 1]: the learned bias of a distance, null without one (see Learned)
@@ -119,6 +119,12 @@ template <bool LOCAL>
 __device__ __forceinline__ int seen_to(const Args& a, const Seq& q, int place) {
     const int end = seen_end(a, q, place);
     return LOCAL ? min(end, max((int)min((int64_t)q.kn, (int64_t)place + a.right + 1), a.sinks)) : end;
+}
+// Whether some of the rows from place `near` to place `far` have FEW keys or less in their windows: the first ones, whose windows begin with the keys, or the last ones, whose
+// windows end with them, or all rows (few_first is then above all places).  The arguments as they are, or read again.  (A place is from -2^30 to 2^31 - 1, keys are 2^30 at most.)
+template <typename A>
+__device__ __forceinline__ bool few_in_window(const A& a, const Seq& q, int near, int far) {
+    return q.kn <= FEW || near < a.few_first || far - q.kn >= a.few_last;
 }
 
 // Tiles of keys that some of the FIXED rows from r0 on may see: `tiles` of them, `front` from the first on and the others `skip` further on (without

@@ -20,7 +20,8 @@ namespace {
 // queries' / keys' gradients 499 / 860 -> 589 / 977 us, error against 64 bits 2.7e-3 -> 2.1e-3 of the norm (1.7e-3 is that of dq's and dk's
 // own rounding; 2.3e-3 without cap, where a product more would cost 5 to 10 %).  (Documents in two rows of 8192, where blocks are cut: 130 / 146
 // -> 144 / 160.)
-// (LOCAL: cut blocks whose rows may see no more than FEW keys.  Where a window leaves them more, its edges are no reason.)
+// (LOCAL: blocks that are cut and have rows with no more than FEW keys in their windows, the first and the last ones of long windows among them.  Where a window leaves them more, its edges
+// are no reason.)
 // LOCAL: late and windowed(j, is), which keys are in the window, as with `cut`.  BIASED: uneven, whether the learned bias differs within the block, and
 // bias(j), in powers of two, if it does; summed, whether the gradients of the scores themselves are wanted (that of x has the cap's slope too): where
 // has the words of their buckets' sums, to which `run` adds them, or, of an even block, they are added to `even`.
@@ -373,7 +374,7 @@ __global__ __launch_bounds__(256, DP == 64 || sizeof(T) == 2 ? 2 : 1) void key_g
             const int near = q.start + (int)over_group(a, t * L::ROWS);
             late = near + right < wlast || far - left > wk0;
             none = far + right < wk0 || near - left > wlast;
-            few = w->few_seen || q.kn <= FEW || (a.causal && near < FEW);
+            few = few_in_window(*w, q, near, far);
         }
         const bool left_over = docs || a.cap > 0.f || ((cut || late) && few);
         t = walk.next(t + 1, t1, classify);
@@ -614,7 +615,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
         const int k0 = span.at<LOCAL>(t) * L::ROWS;
         const bool cut = LOCAL ? k0 + L::ROWS > wend : k0 + L::ROWS > q.kn || (a.causal && k0 + L::ROWS - 1 > wnear && k0 + L::ROWS > q.prefix);
         const bool late = LOCAL && k0 < wbegin && k0 + L::ROWS > a.sinks;
-        const bool left_over = docs || a.cap > 0.f || ((cut || late) && (!LOCAL || a.few_seen || q.kn <= FEW || (a.causal && wnear < FEW)));
+        const bool left_over = docs || a.cap > 0.f || ((cut || late) && (!LOCAL || few_in_window(a, q, wnear, wfar)));
         const bool none = LOCAL ? k0 >= wend_far || (k0 + L::ROWS <= wbegin_near && k0 >= a.sinks) : a.causal && k0 > wfar && k0 >= q.prefix;
         const float from = (float)(place - k0 - 4 * half);
         t = walk.next(t + 1, t1, classify);
@@ -745,7 +746,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void query_
 
 // The first keys, which rows see wherever they stand: dk and dv of 32 of them and of a share of the rows that may see them, whose tiles the workgroup's wavefronts
 // take in turn, each with tiles of its own on their way through LDS; what they have is put together at the end.
-// (The first rows of causal calls and a narrow window's see few keys, see gradients().)
+// (Rows that have few keys in their windows, see gradients().)
 template <typename T, int DP, bool BIASED>
 __global__ __launch_bounds__(256, 1) void first_keys_kernel(Args a) {
     using F = Few<T, DP>;
@@ -827,7 +828,7 @@ __global__ __launch_bounds__(256, 1) void first_keys_kernel(Args a) {
         auto at = [&](int j) { return 8 * j + 4 * half; };
         const int near = q.start + (int)over_group(a, t * 32);
         const bool cut = a.causal && k0 + 31 > near && k0 + 31 >= q.prefix;
-        const bool left_over = a.q_docs || a.cap > 0.f || a.few_seen || q.kn <= FEW || cut;
+        const bool left_over = a.q_docs || a.cap > 0.f || cut || few_in_window(a, q, near, q.start + (int)over_group(a, min(t * 32 + 31, rows - 1)));
         const bool uneven = BIASED && (int64_t)near - a.reach < k0 + 31;  // (else all stand `reach` and more behind the keys)
         auto bias = [&](int j) {
             const int4 place = *(const int4*)&word[PLACE][at(j)], of = *(const int4*)&word[TABLE][at(j)];

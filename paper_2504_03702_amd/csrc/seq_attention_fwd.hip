@@ -703,7 +703,9 @@ int plan(const ps_attention_desc* d, const ps_attention_seqs* s, const ps_attent
         a.sinks = (local->left < 0 && local->right < 0) || a.max_q == 0 ? 0 : min(local->sinks, a.max_k);   // (without a window all are seen)
         a.reach = local->reach;
         a.n_buckets = local->n_buckets;
-        a.few_seen = a.left == INT32_MAX || (int64_t)a.left + (ahead ? a.right : 0) < FEW;   // (without a window in front as ps_attention_backward())
+        const bool all = a.left == INT32_MAX || (int64_t)a.left + (a.causal ? 0 : a.right) < FEW;   // (without a window in front as ps_attention_backward())
+        a.few_first = all ? INT32_MAX : a.causal ? FEW : FEW - a.right;
+        a.few_last = a.left - FEW;
         const int64_t window = (int64_t)a.left + (ahead ? a.right : 0) + FIXED, key_window = window - FIXED + FIXED / group + 2;
         auto lower = [](int64_t& to, int64_t by) { to = by < to ? by : to; };   // (the host's min() has 32 bits)
         lower(most_keys, key_window + a.sinks + 3 * a.tile);

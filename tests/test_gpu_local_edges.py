@@ -96,3 +96,41 @@ def test_keys_of_far_tiles_are_not_read(dtype, bias):
     p.k[:256] = p.v[:256] = float("nan")
     for name, x, y in zip(("out", "lse", "dq", "dk", "dv", "dbias"), p.both(), clean):
         assert torch.equal(x, y), name
+
+
+@pytest.mark.parametrize("kind", ["window", "bias"])
+@pytest.mark.parametrize("size", [64, 128])
+def test_a_window_that_ends_at_its_row_is_a_causal_one(kind, size):
+    """The same pairs, so the same sums, with what the rounding of d leaves where rows see few keys: equal to the bit.  (All rows see the first key either way.)"""
+    for lens in ([700], [1100, 30]):
+        how = dict(BIASES if kind == "bias" else {}, sinks=1)
+        one, other = (Local(torch.bfloat16, lens, lens, size=size, left=600, **how, **end) for end in (dict(causal=True), dict(right=0)))
+        for name, x, y in zip(("out", "lse", "dq", "dk", "dv", "dbias"), one.both(), other.both()):
+            assert torch.equal(x, y), name
+
+
+@pytest.mark.parametrize("size", [64, 128])
+@pytest.mark.parametrize("how", [dict(left=600, right=0), dict(left=0, right=600)], ids=["first", "last"])
+def test_rows_that_see_few_keys_of_a_long_window(how, size):
+    """A row's dq is scale sum d_j k_j, and where keys have much in common (here `far`, besides what they differ by) it stays small because sum d_j is 0: of d's rounding
+    it may keep no more than two bf16 pieces leave, 2^-16 of every term.  Besides: D = dout . out from two pieces of out, 2^-16 of S = sum |dout| |out|; weights p from fp32
+    scores of size `far` |q| (at most 2^-24 log2(head_dim) + 1 = 8 roundings of that, 2^-17 here), in d twice, by D and by itself.  So an element of
+    dq is off by less than scale max |k| sum_j p_j 2^-15 (|dp_j| + |D| + S), and its own rounding 2^-8."""
+    far, n, few = 8.0, 1000, 60 if size == 64 else 30                        # (rows whose keys are all in one tile, which their end cuts: of 64 keys, of 32 for heads of 128 under a bias)
+    p = Local(torch.bfloat16, [n], [n], 2, 1, size, seed=4, **BIASES, **how)
+    p.k += far
+    p.bias.zero_()
+    out, lse, dq, *_ = p.both()
+    scale, k, v = size ** -0.5, p.k[:, 0].double(), p.v[:, 0].double()
+    rows = torch.arange(few, device=DEV) if how["left"] else torch.arange(n - few, n, device=DEV)
+    apart = torch.arange(n, device=DEV)[None] - rows[:, None]
+    seen = (apart >= -how["left"]) & (apart <= how["right"])
+    for h in range(2):
+        q, do = p.q[rows, h].double(), p.dout[rows, h].double()
+        w = (q @ k.t().contiguous() * scale).masked_fill(~seen, -torch.inf).softmax(1)
+        o, dp = w @ v, do @ v.t().contiguous()
+        big_d = (do * o).sum(1, keepdim=True)
+        want = scale * ((w * (dp - big_d)) @ k)
+        bound = scale * k.abs().max() * (w * (dp.abs() + big_d.abs() + (do * o).abs().sum(1, keepdim=True))).sum(1, keepdim=True) * 2.0 ** -15 + 2.0 ** -8 * want.abs()
+        off = (dq[rows, h].double() - want).abs()
+        assert torch.all(off <= bound), float((off / bound).max())
