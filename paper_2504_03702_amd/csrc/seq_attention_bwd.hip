@@ -1045,12 +1045,8 @@ void launch(const Args& a, hipStream_t st) {
     const int64_t row_jobs = (int64_t)a.kv_heads * a.row_blocks * a.parts;
     const int64_t key_blocks = (a.max_k + FIXED - 1) / FIXED, key_jobs = a.kv_heads * key_blocks * a.key_parts;
     const unsigned tile_lds = BIASED ? 2 * a.bias_words * sizeof(float) : 0;
+    // (up to 52 KB, with the tiles 113: a launch gets 160 without a word)
     const unsigned sums_lds = a.bias_parts ? (2 * ((a.bias_width + 63) & ~63) + 4 * (a.n_buckets + 1) * a.sum_columns) * sizeof(float) : 0;
-    if (BIASED && tile_lds + sums_lds > 32 << 10) {
-        static bool lds_attr_set = false;     // raising the limit twice is harmless, so no lock
-        if (!lds_attr_set && hipFuncSetAttribute((const void*)query_gradients_kernel<T, DP, LOCAL, BIASED>, hipFuncAttributeMaxDynamicSharedMemorySize, 64 << 10) != hipSuccess) return;
-        lds_attr_set = true;
-    }
     in_turn(row_jobs, a.n_seq, [&](unsigned n) {
         b.listed = add_up(a, n, a.row_blocks, a.parts);
         hipLaunchKernelGGL((query_gradients_kernel<T, DP, LOCAL, BIASED>), dim3((unsigned)row_jobs * n), dim3(256), tile_lds + sums_lds, st, b);

@@ -134,3 +134,12 @@ def test_rows_that_see_few_keys_of_a_long_window(how, size):
         bound = scale * k.abs().max() * (w * (dp.abs() + big_d.abs() + (do * o).abs().sum(1, keepdim=True))).sum(1, keepdim=True) * 2.0 ** -15 + 2.0 ** -8 * want.abs()
         off = (dq[rows, h].double() - want).abs()
         assert torch.all(off <= bound), float((off / bound).max())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("heads,kv_heads", [(4, 4), (8, 2), (5, 1), (32, 1)])
+@pytest.mark.parametrize("size", [64, 128])
+def test_as_many_buckets_as_there_may_be(dtype, heads, kv_heads, size):
+    """64, of which a row's lanes share a column, and the most LDS that a call asks for (32 heads to a key head)."""
+    Local(dtype, [150, 33, 1], [150, 33, 1], heads, kv_heads, size, buckets=ol.buckets(64, 100), n_buckets=64).check()
+    Local(dtype, [260], [260], heads, kv_heads, size, causal=True, left=150, sinks=2, buckets=ol.buckets(64, 90, False), n_buckets=64).check()
