@@ -143,3 +143,25 @@ def test_as_many_buckets_as_there_may_be(dtype, heads, kv_heads, size):
     """64, of which a row's lanes share a column, and the most LDS that a call asks for (32 heads to a key head)."""
     Local(dtype, [150, 33, 1], [150, 33, 1], heads, kv_heads, size, buckets=ol.buckets(64, 100), n_buckets=64).check()
     Local(dtype, [260], [260], heads, kv_heads, size, causal=True, left=150, sinks=2, buckets=ol.buckets(64, 90, False), n_buckets=64).check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n_buckets", [32, 64])
+def test_a_bias_gradient_of_many_blocks(dtype, n_buckets):
+    """8 sequences of up to 1100 tokens, 4 heads to a key head, are 280 blocks of 128 rows and more, whose sums are added up in two launches."""
+    lens = [1100, 1100, 1099, 1100, 1000, 1100, 1100, 1100]
+    p = Local(dtype, lens, lens, 4, 1, 64, causal=True, left=40, buckets=ol.buckets(n_buckets, 128, False), n_buckets=n_buckets)
+    # (in 64 bits on the card, a sequence at a time: the same definition as the oracle's)
+    got, want = p.both()[5].double(), torch.zeros(n_buckets, 4, dtype=torch.float64, device=DEV)
+    buckets = torch.tensor(p.buckets, device=DEV)
+    for s, n in enumerate(lens):
+        i = slice(p.qo[s], p.qo[s + 1])
+        apart = torch.arange(n, device=DEV)[None] - torch.arange(n, device=DEV)[:, None]
+        of, seen = buckets[apart.clamp(-128, 128) + 128], (apart <= 0) & (apart >= -40)
+        k, v = p.k[i, 0].double().t().contiguous(), p.v[i, 0].double().t().contiguous()
+        for h in range(4):
+            q, do = p.q[i, h].double(), p.dout[i, h].double()
+            w = (q @ k * 0.125 + p.bias[:, h].double()[of]).masked_fill(~seen, -torch.inf).softmax(1)
+            dp = do @ v
+            want[:, h].index_add_(0, of.flatten(), (w * (dp - (w * dp).sum(1, keepdim=True))).flatten())
+    assert float((got - want).norm()) <= (3e-5 if dtype == torch.bfloat16 else 1e-5) * float(want.norm())
