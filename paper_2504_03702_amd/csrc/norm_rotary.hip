@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(NormArgs a) {
             }
             squares = over_lanes(squares);
             if (BACK) along = over_lanes(along);
-            const float by = __builtin_amdgcn_rsqf(fmaf(squares, of_head, a.eps)), mean = along * by * of_head, counted = there[b] ? by : 0.f;
+            const float by = __builtin_amdgcn_rsqf(fmaf(squares, of_head, a.eps)), mean = along * by * of_head;
 #pragma unroll
             for (int k = 0; k < PER; ++k) {
                 float v[2][VEC];
@@ -181,7 +181,9 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(NormArgs a) {
                     for (int j = 0; j < VEC; ++j) {
                         const float u = (float)x[b][k][i].v[j] * by;
                         if (BACK) {
-                            acc[k][i][j] = fmaf(gv[k][i][j], WHOLE ? (float)x[b][k][i].v[j] * counted : u, acc[k][i][j]);
+                            // (chosen, not multiplied by zero: a head that is there again may be overwritten by its own dx in the meantime)
+                            const float with = fmaf(gv[k][i][j], u, acc[k][i][j]);
+                            acc[k][i][j] = !WHOLE || there[b] ? with : acc[k][i][j];
                             v[i][j] = by * fmaf(-u, mean, gv[k][i][j] * w[k][i][j]);
                         } else {
                             v[i][j] = u * w[k][i][j];

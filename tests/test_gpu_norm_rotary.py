@@ -196,3 +196,22 @@ def test_another_stream_and_a_graph(direction):
         out.zero_(), dw.zero_()
         call()
         assert torch.equal(got[0], out) and torch.equal(got[1], dw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("place", ["x", "dout"])
+def test_gradients_past_all_numbers_in_place(dtype, place):
+    """A head of zeros under a small eps has a dx that no number holds and adds nothing to dweight, in place as elsewhere.  (80 heads of a tile are 64 and 16: lanes without
+    one read the tile's last head again, whose dx may be there by then.)"""
+    rows = 16 * 512
+    x, g = made(rows, (5, 5), 64, dtype, 12)
+    x[15::16, 4] = 0.0
+    g[15::16, 4] *= 1e25
+    w, pos, f = torch.ones(64, device=DEV, dtype=dtype), places(rows), ps.ps_rotary_frequencies(32).to(DEV)
+    ws = ps.alloc_workspace(ps.ps_norm_rotary_workspace_bytes(rows, 5, 0, 64), DEV)
+    dx, dw, dw_again = torch.empty_like(x), torch.empty(64, device=DEV), torch.empty(64, device=DEV)
+    ps.ps_norm_rotary_backward(x, w, pos, f, g, dx, dw, ws, eps=1e-37)
+    assert torch.isfinite(dw).all() and not torch.isfinite(dx[15::16, 4]).any()
+    own = {"x": x, "dout": g}[place].clone()
+    ps.ps_norm_rotary_backward(own if place == "x" else x, w, pos, f, own if place == "dout" else g, own, dw_again, ws, eps=1e-37)
+    assert torch.equal(dw, dw_again) and torch.equal(dx.nan_to_num(), own.nan_to_num())
