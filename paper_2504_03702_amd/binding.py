@@ -186,11 +186,19 @@ def _extension():
         return None
 
 
+def _on_current_device(t: torch.Tensor, name: str) -> None:
+    """The stream is the current device's: tensors of another would be read by a kernel of the wrong one."""
+    here = torch.cuda.current_device()
+    if t.device.index != here:
+        raise ValueError(f"{name}: is on cuda:{t.device.index}, the current device is cuda:{here}")
+
+
 def _ptr(t: Optional[torch.Tensor], dtype: torch.dtype, name: str) -> Optional[int]:
     if t is None:
         return None
     if not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
         raise TypeError(f"{name}: need a contiguous {dtype} tensor on the GPU")
+    _on_current_device(t, name)
     return t.data_ptr()
 
 
@@ -433,6 +441,7 @@ def _heads_ptr(t: torch.Tensor, shape: Tuple[int, int, int], dtype: torch.dtype,
     """Address and strides of a tensor [rows, heads, head_dim] whose last dimension is dense."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
         raise TypeError(f"{name}: need a {dtype} tensor on the GPU")
+    _on_current_device(t, name)
     if tuple(t.shape) != shape:
         raise ValueError(f"{name}: has shape {tuple(t.shape)}, not {shape}")
     if t.shape[2] > 1 and t.stride(2) != 1:
@@ -564,6 +573,7 @@ def _rows_ptr(t: Optional[torch.Tensor], shape: Tuple[int, int], dtype: torch.dt
         return None, 0
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
         raise TypeError(f"{name}: need a {dtype} tensor on the GPU")
+    _on_current_device(t, name)
     if tuple(t.shape) != shape or (shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{name}: need shape {shape} and dense rows")
     return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
@@ -602,14 +612,6 @@ def ps_dropout_backward(dout: torch.Tensor, rng: torch.Tensor, p: float, dx: tor
         _ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(), _stream()), "ps_dropout_backward")
 
 
-def _on_current_device(where: str, *tensors) -> None:
-    """The stream is the current device's: tensors of another would be read by a kernel of the wrong one."""
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != here:
-            raise ValueError(f"{where}: a tensor is on cuda:{t.device.index}, the current device is cuda:{here}")
-
-
 def ps_norm_rotary_workspace_bytes(n_rows: int, heads: int, heads2: int, head_dim: int) -> int:
     return int(load_library().ps_norm_rotary_workspace_bytes(n_rows, heads, heads2, head_dim))
 
@@ -643,7 +645,6 @@ def ps_norm_rotary_forward(x: torch.Tensor, weight: Optional[torch.Tensor], posi
         return
     d, at, pos, freq, size = _norm_rotary("ps_norm_rotary_forward", x, x2, positions, frequencies, eps, interleaved, magnitude,
                                           {"x": x, "out": out, "x2": x2, "out2": out2})
-    _on_current_device("ps_norm_rotary_forward", x, weight, positions, frequencies, out, x2, weight2, out2)
     _check(load_library().ps_norm_rotary_forward(
         ctypes.byref(d), at["x"], _sized_ptr(weight, x.dtype, size, "weight"), at["out"], at["x2"], _sized_ptr(weight2, x.dtype, size, "weight2"),
         at["out2"], pos, freq, _stream()), "ps_norm_rotary_forward")
@@ -660,7 +661,6 @@ def ps_norm_rotary_backward(x: torch.Tensor, weight: Optional[torch.Tensor], pos
         return
     d, at, pos, freq, size = _norm_rotary("ps_norm_rotary_backward", x, x2, positions, frequencies, eps, interleaved, magnitude,
                                           {"x": x, "dout": dout, "dx": dx, "x2": x2, "dout2": dout2, "dx2": dx2})
-    _on_current_device("ps_norm_rotary_backward", x, weight, positions, frequencies, dout, dx, dweight, workspace, x2, weight2, dout2, dx2, dweight2)
     f32 = torch.float32
     _check(load_library().ps_norm_rotary_backward(
         ctypes.byref(d), at["x"], _sized_ptr(weight, x.dtype, size, "weight"), at["dout"], at["dx"], _sized_ptr(dweight, f32, size, "dweight"),
@@ -714,8 +714,6 @@ def ps_local_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor
     d, seqs, at, n_lse = _attention(where, q, k, q_offsets, k_offsets, max_q, max_k, scale, softcap, causal, k_lengths, q_start, prefix, slopes,
                                     q_docs, k_docs, {"q": (q, False), "k": (k, True), "v": (v, True), "out": (out, False)})
     local = _local(where, q.shape[1], left, right, sinks, buckets, bias)
-    _on_current_device(where, q, k, v, q_offsets, k_offsets, out, lse, workspace, buckets, bias, k_lengths, q_start, prefix, slopes, q_docs, k_docs,
-                       status, out_rest)
     _check(load_library().ps_local_attention_forward(
         ctypes.byref(d), ctypes.byref(seqs), ctypes.byref(local), at["q"], at["k"], at["v"], at["out"], _sized_ptr(lse, torch.float32, n_lse, "lse"),
         _sized_ptr(out_rest, torch.bfloat16, q.numel(), "out_rest"), _ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
@@ -741,8 +739,6 @@ def ps_local_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tenso
                                     q_docs, k_docs, {"q": (q, False), "k": (k, True), "v": (v, True), "out": (out, False), "dout": (dout, False),
                                                      "dq": (dq, False), "dk": (dk, True), "dv": (dv, True)})
     local = _local(where, q.shape[1], left, right, sinks, buckets, bias, dbias)
-    _on_current_device(where, q, k, v, out, lse, dout, q_offsets, k_offsets, dq, dk, dv, workspace, buckets, bias, dbias, k_lengths, q_start, prefix,
-                       slopes, q_docs, k_docs, status, out_rest)
     _check(load_library().ps_local_attention_backward(
         ctypes.byref(d), ctypes.byref(seqs), ctypes.byref(local), at["q"], at["k"], at["v"], at["out"], _sized_ptr(lse, torch.float32, n_lse, "lse"),
         _sized_ptr(out_rest, torch.bfloat16, q.numel(), "out_rest"), at["dout"], at["dq"], at["dk"], at["dv"],

@@ -4,7 +4,7 @@
 // Host time of the calls of a management period, ctypes / so: 29.5 / 10.0 us; the period itself 31.8 -> 23.8 us, which is what
 // its three launches take on the GPU.
 //
-// Only calls with nothing to object to are made here: tensors of the plain type, on the GPU, contiguous, of the right type and
+// Only calls with nothing to object to are made here: tensors of the plain type, on the current GPU, contiguous, of the right type and
 // size, integers that fit.  Anything else returns NotImplemented with nothing done, and binding.py goes its own way, which
 // says what is wrong.
 #include <Python.h>
@@ -132,6 +132,7 @@ struct Args {
         if (!good || !THPVariable_CheckExact(o)) { good = false; return nullptr; }
         const at::Tensor& t = THPVariable_Unpack(o);
         if (!t.defined() || !t.is_cuda() || t.dim() != 2) { good = false; return nullptr; }
+        seen(t);
         if (shape[0] < 0) {
             *type = t.scalar_type();
             if (*type != at::kFloat && *type != at::kBFloat16) good = false;
@@ -174,9 +175,8 @@ bool current_stream(void** s, long* device) {
 }
 
 // parse: fills in the arguments and returns the call (given the stream), which is made without the interpreter's lock.
-// here: the tensors have to be on the current device.
 template <typename Parse>
-PyObject* make_call(PyObject* const* at, Py_ssize_t n, Py_ssize_t want, Parse parse, bool here = false) {
+PyObject* make_call(PyObject* const* at, Py_ssize_t n, Py_ssize_t want, Parse parse) {
     if (n != want) Py_RETURN_NOTIMPLEMENTED;
     try {
         Args a{at};
@@ -185,7 +185,7 @@ PyObject* make_call(PyObject* const* at, Py_ssize_t n, Py_ssize_t want, Parse pa
         void* stream;
         long device = -1;
         if (!current_stream(&stream, &device)) return nullptr;
-        if (here && (!a.one_device || a.device != device)) Py_RETURN_NOTIMPLEMENTED;
+        if (!a.one_device || (a.device >= 0 && a.device != device)) Py_RETURN_NOTIMPLEMENTED;
         int code = PS_OK;
         bool thrown = false;
         Py_BEGIN_ALLOW_THREADS
@@ -530,7 +530,7 @@ PyObject* norm_rotary_forward(PyObject*, PyObject* const* at, Py_ssize_t n) {
         t.others(a, 2, 8);
         const void *w = a.sized<void>(1, t.type, t.shape[2], true), *w2 = a.sized<void>(6, t.type, t.shape[2], true);
         return [=](void* s) { return g_calls.norm_rotary_forward(&t.d, x, w, out, x2, w2, out2, t.positions, t.frequencies, s); };
-    }, true);
+    });
 }
 
 PyObject* norm_rotary_backward(PyObject*, PyObject* const* at, Py_ssize_t n) {
@@ -550,7 +550,7 @@ PyObject* norm_rotary_backward(PyObject*, PyObject* const* at, Py_ssize_t n) {
         return [=](void* s) {
             return g_calls.norm_rotary_backward(&t.d, x, w, dout, dx, dw, x2, w2, dout2, dx2, dw2, t.positions, t.frequencies, workspace, (size_t)ws, s);
         };
-    }, true);
+    });
 }
 
 // at[i] and on: left, right, sinks, buckets, bias
@@ -586,7 +586,7 @@ PyObject* local_attention_forward(PyObject*, PyObject* const* at, Py_ssize_t n) 
         return [=](void* s) {
             return g_calls.local_attention_forward(&t.d, &t.s, &l, q, k, v, out, lse, rest, t.workspace, (size_t)t.ws, t.status, s);
         };
-    }, true);
+    });
 }
 
 PyObject* local_attention_backward(PyObject*, PyObject* const* at, Py_ssize_t n) {
@@ -605,7 +605,7 @@ PyObject* local_attention_backward(PyObject*, PyObject* const* at, Py_ssize_t n)
         return [=](void* s) {
             return g_calls.local_attention_backward(&t.d, &t.s, &l, q, k, v, out, lse, rest, dout, dq, dk, dv, dbias, t.workspace, (size_t)t.ws, t.status, s);
         };
-    }, true);
+    });
 }
 
 #define PS_METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
