@@ -357,8 +357,10 @@ int ps_attention_backward(const ps_attention_desc* desc, const ps_attention_seqs
  *   reach        >= 0, at most 65536: larger distances have the bucket of that one
  *   buckets      [2 reach + 1] int32 on the device, as ps_bias_buckets() makes them or any others; a bucket that there is not (-1): no bias
  *   bias         [n_buckets][heads] float on the device
- * Where there is a bias, a key head's rows have at most 32 heads, heads is below 2^16 and heads * (2 reach + 1) below 2^31.  A bias of -infinity or
- * of the type's lowest value hides its pairs.  The time goes by the keys that are seen; tiles outside of all windows of a block of
+ * Where there is a bias, a key head's rows have at most 32 heads, heads is below 2^16 and heads * (2 reach + 1) below 2^31.  A bias of -2^20 or less, as -infinity
+ * and the type's lowest value are, hides its pairs: they have weight 0 (their scale * (q_i . k_j) and dout_i . v_j have to be finite), and a row that sees no others gets zeros.  Scores are fp32
+ * sums that the bias is part of, so a large one costs places (fp32 calls are off by 6e-7 of the norm of `out` where it is of a few units, 4e-6 where it is 20 everywhere, 2e-3 at
+ * 1e4); it has to be below 2^20.  The time goes by the keys that are seen; tiles outside of all windows of a block of
  * rows are not read.  A key that no row of its sequence has in its window, or among the first ones, matters to nobody in the forward call, whatever it holds (rows of
  * a cache between the first keys and the window that were given to others); in the backward call it has to be finite, as other keys that a query does not see. */
 typedef struct ps_attention_local {

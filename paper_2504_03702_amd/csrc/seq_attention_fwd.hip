@@ -569,7 +569,8 @@ __global__ __launch_bounds__(256) void check_kernel(Args a) {
 }
 
 // The learned bias of every distance, a thread each of a head's, `by` times what the caller has (none for a bucket that there is not), and
-// where its bucket is in a lane's sums.  The threads clear what the sums of blocks of rows go to, too, since some blocks belong to no sequence.
+// where its bucket is in a lane's sums.  -2^20 and less is -infinity: a row that sees nothing else would have weights of the places that scores of that size
+// lose (2^-24 of them: a sixteenth there, powers of e^60 at -1e9, NaN at -1e30), and its gradients with them.  The threads clear what the sums of blocks of rows go to, too, since some blocks belong to no sequence.
 __global__ __launch_bounds__(256) void table_kernel(const int32_t* buckets, const float* bias, float* table, int32_t* words, int reach, int n_buckets, int columns, int heads,
                                                     float by, float* sums, int64_t n_sums) {
     const int d = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y;
@@ -578,7 +579,8 @@ __global__ __launch_bounds__(256) void table_kernel(const int32_t* buckets, cons
     if (d > 2 * reach || h >= heads) return;
     const int b = buckets[d];
     const bool is = b >= 0 && b < n_buckets;
-    table[(int64_t)h * (2 * reach + 1) + d] = is ? bias[(int64_t)b * heads + h] * by : 0.f;
+    const float value = is ? bias[(int64_t)b * heads + h] : 0.f;
+    table[(int64_t)h * (2 * reach + 1) + d] = value <= -0x1p20f ? -INFINITY : value * by;
     if (words && h == 0) {
         // (bit 16: the next three distances have the same bucket)
         bool same = true;

@@ -165,3 +165,17 @@ def test_a_bias_gradient_of_many_blocks(dtype, n_buckets):
             dp = do @ v
             want[:, h].index_add_(0, of.flatten(), (w * (dp - (w * dp).sum(1, keepdim=True))).flatten())
     assert float((got - want).norm()) <= (3e-5 if dtype == torch.bfloat16 else 1e-5) * float(want.norm())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("value", [-1e30, -1e9, -2.0 ** 20])
+@pytest.mark.parametrize("how", [dict(), dict(causal=True, cap=20.0), dict(left=200, right=150, sinks=3)], ids=["all", "cap", "window"])
+def test_a_large_negative_bias_hides_too(dtype, value, how):
+    """As -infinity does, rows that see nothing else included: equal to the bit."""
+    p = Local(dtype, [300, 7, 1, 40], [300, 260, 260, 20], 4, 2, 64, buckets=ol.buckets(32, 32), n_buckets=32, **how)
+    for gone in ((3, 15, 31), (0, 1), tuple(range(32))):
+        p.bias[list(gone)] = -torch.inf
+        want = p.both()
+        assert all(torch.isfinite(t).all() for t in (want[0], *want[2:])), gone
+        p.bias[list(gone)] = value
+        assert all(torch.equal(x, y) for x, y in zip(p.both(), want)), gone
