@@ -380,7 +380,7 @@ extern "C" int ps_norm_rotary_forward(const ps_norm_rotary_desc* d, const void* 
 }
 
 extern "C" size_t ps_norm_rotary_workspace_bytes(int64_t n_rows, int32_t heads, int32_t heads2, int32_t head_dim) {
-    if (n_rows < 0 || n_rows > INT32_MAX || heads < 1 || heads2 < 0 || head_dim < 1 || head_dim > 512) return 0;
+    if (n_rows < 0 || n_rows > INT32_MAX || heads < 1 || heads2 < 0 || head_dim < 1 || head_dim > 512 || ((int64_t)heads + heads2) * head_dim > 1 << 26) return 0;
     // (workgroups along the rows times shares of the heads of both tensors: two of the one, or 512 and a tile's more)
     return align_up(sizeof(float) * 2 * (size_t)head_dim * MOST_BLOCKS, 256);
 }

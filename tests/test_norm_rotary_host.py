@@ -80,3 +80,9 @@ def test_the_binding_refuses():
             ps.ps_norm_rotary_forward(**a)
     with pytest.raises((TypeError, ValueError)):
         ps.ps_norm_rotary_backward(x, None, None, None, x, x, None, x)
+
+
+def test_workspace_of_heads_that_the_calls_refuse(lib):
+    size = ps.ps_norm_rotary_workspace_bytes
+    assert size(5, 1 << 20, 0, 64) > 0 and size(5, 1 << 19, 1 << 19, 64) > 0
+    assert size(5, (1 << 20) + 1, 0, 64) == size(5, 1, 1 << 20, 64) == size(5, (1 << 31) - 1, (1 << 31) - 1, 1) == 0
