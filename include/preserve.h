@@ -373,7 +373,8 @@ typedef struct ps_attention_local {
  * and its bad numbers and pointers, PS_EUNSUPPORTED for n_buckets, reach and heads above those.  Of `local`, the workspace goes by the numbers alone, and
  * not by `causal` of `desc`.
  * dbias: [n_buckets][heads] float, NULL: not wanted; overwritten with the gradient of the bias, of pair ij and its distance's bucket p_ij (dout_i . v_j - D_i),
- * over all rows of all sequences that are not faulty.  Its sums are fp32 too, in an order that is fixed by the shapes. */
+ * over all rows of all sequences that are not faulty.  Its sums are fp32 too, in an order that is fixed by the shapes.  Without out_rest, in both directions of a bf16 call, D_i is that of
+ * an `out` of weights and values rounded to bf16, and dbias is off by 1e-3 of its norm (2e-6 with it). */
 size_t ps_local_attention_workspace_bytes(const ps_attention_desc* desc, const ps_attention_local* local, int backward);
 int ps_local_attention_forward(const ps_attention_desc* desc, const ps_attention_seqs* seqs, const ps_attention_local* local, const void* q, const void* k,
                                const void* v, void* out, float* lse, void* out_rest, void* workspace, size_t workspace_bytes, ps_status* status,

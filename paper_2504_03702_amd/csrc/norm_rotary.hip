@@ -2,6 +2,7 @@
 //     r = 1 / sqrt(mean x^2 + eps),  u = r x,  out = turn(u w);   g = turn back(dout),  dw = sum g u,  dx = r (g w - u mean(g w u)).
 // A head stays in the registers of a few neighbouring lanes, which have all they need of it to themselves but two sums: those of x^2 and,
 // backwards, of g w x, which do not wait for one another.  So every tensor is read once and written once, and memory bounds the call.
+// dw is a sum in fp32, of a lane's heads, lanes and workgroups in turn, of u that the hardware's root (one place off at most) has made: 2e-7 of its norm from 64 bits at 3333 and 32768 rows.
 #include <float.h>
 #include <math.h>
 

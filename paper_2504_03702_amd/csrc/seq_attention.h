@@ -447,7 +447,8 @@ __device__ __forceinline__ void dots(const unsigned char* tile, int b, const F& 
 }
 
 // The weights of a block's 32 passing rows for a lane's fixed row, as the second product takes them: floats, or bf16 in the order of
-// the accumulator's elements.
+// the accumulator's elements.  (bf16 because the matrix units take both operands alike, and a second product for what rounding leaves takes as long as the first: `out` is 2.1e-3 to
+// 2.3e-3 of its norm from 64 bits, 1.65e-3 of which are its own rounding.  Where the rest does matter, a second product is made: see Row::step() and gradients().)
 template <typename T>
 struct Weights {
     float w[16];
@@ -728,7 +729,9 @@ struct Learned {
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (SEQATT_LDS void*)(to + w), 4, 0, 0);
         }
     }
-    // The bias is what the product starts from (b(i), of passing row i of 32), if it bends no score: nothing is left to add then.
+    // The bias is what the product starts from (b(i), of passing row i of 32), if it bends no score: nothing is left to add then.  Every step of the accumulation rounds
+    // at the size of bias / scale for that, where a bias added at the end would round once: with biases of a few units fp32 results are off by 6e-7 of their norm (4e-7
+    // without a bias), with 20 added to all of them 3.8e-6, with 1e4 2e-3 (elementary operations in 32 bits 3.5e-7, 6e-7, 2.5e-4).
     template <typename Of>
     static __device__ __forceinline__ f32x16 start(bool is, int half, Of of) {
         f32x16 s = no_start();

@@ -157,7 +157,8 @@ struct Row {
             }
             weigh<T, DP>(values, b, w, o, lanes);
             // what the rounding of the weights left, where gradients are to come: the bias's is made of fp32 sums, and dout . out, which every pair's
-            // gradient is less, would be off by as much as weights of 8 bits make it (1e-3 of the norm of dbias; 3e-6 with it)
+            // gradient is less, would be off by as much as weights of 8 bits make it (1.3e-3 of the norm of dbias; 2.2e-6 with it, which
+            // is what the two pieces of out leave)
             if constexpr (BIASED && sizeof(T) == 2)
                 if (a.rest_w) weigh<T, DP>(values, b, rest, o, lanes);
         }
